@@ -46,6 +46,10 @@ typedef enum {
   OCN_NUM_DTYPES
 } ocn_dtype;
 
+/* Brain floating point (the upper 16 bits of a float): a type of the operators over heads below
+ * alone.  Every other call refuses it with OCN_ERR_DTYPE. */
+#define OCN_BFLOAT16 32
+
 /* The paper's unified tensor type (sections 2.2 and 3.1.3) reduced to a plain descriptor. */
 typedef struct {
   void *base;                    /* device pointer to the start of the storage; borrowed  */
@@ -304,6 +308,110 @@ typedef enum { OCN_MODE_STANDARD = 0, OCN_MODE_WARNING, OCN_MODE_ERROR, OCN_MODE
 size_t ocn_unary_mode_workspace_bytes(int op, int mode, const ocn_tensor *a);
 int ocn_unary_mode(int op, int mode, const ocn_tensor *a, const ocn_tensor *out, const ocn_tensor *out_complex,
                    void *workspace, size_t workspace_bytes, int *outside, void *stream);
+
+/* ---- operators over heads: positions, norms, a 4-bit cache and attention over it ------------
+ *
+ * The attention path of a transformer layer.  Tensors of heads have the dimensions [..., heads, channels]
+ * and any byte strides; the leading dimensions together are the tokens (fewer than 2^31).  Element types are OCN_HALF,
+ * OCN_BFLOAT16 and OCN_FLOAT; a call's tensors of heads share one type, arithmetic is done in single precision or more and
+ * rounded once, on store.  Tensors of indices are OCN_INT32 or OCN_INT64.  Operands in the other byte order are
+ * OCN_ERR_BYTEORDER.  A head has at most OCN_MAX_CHANNELS channels.  An output may be the identical view of the input
+ * that it takes the place of (in place); any other sharing of bytes with an input, or between outputs, is OCN_ERR_ALIAS. Heads that
+ * lie side by side in one buffer (as a projection leaves queries, keys and values) do not share bytes.
+ */
+#define OCN_MAX_CHANNELS 512
+
+/* A rotation by position: pair i < rotary_dim / 2 of a head's first rotary_dim channels turns by the angle
+ *     positions[token] * frequencies[i]          (radians, formed and reduced in double precision)
+ * and is multiplied by magnitude; the other channels stay.  positions broadcasts against the leading dimensions of
+ * the tensor that is rotated (right-aligned, as in ocn_binary); frequencies: OCN_DOUBLE, [rotary_dim / 2]. */
+typedef enum {
+  OCN_ROTARY_HALF = 0,      /* pair i: channels i and i + rotary_dim / 2 */
+  OCN_ROTARY_INTERLEAVED    /* pair i: channels 2 i and 2 i + 1          */
+} ocn_rotary_layout;
+typedef struct {
+  const ocn_tensor *positions;
+  const ocn_tensor *frequencies;
+  int32_t rotary_dim;       /* even, 2 .. channels */
+  int32_t layout;           /* ocn_rotary_layout */
+  double magnitude;         /* 1 for a pure rotation */
+} ocn_rotation;
+
+/* Frequencies for a rotation, computed on the HOST: frequencies[i] = base^(-2 i / rotary_dim) for i < rotary_dim / 2, changed for contexts longer
+ * than the `original` tokens that a model was trained on, by `factor`:
+ *   OCN_STRETCH_NONE      as they are
+ *   OCN_STRETCH_LINEAR    divided by factor
+ *   OCN_STRETCH_BASE      with the base multiplied by factor^(rotary_dim / (rotary_dim - 2))
+ *   OCN_STRETCH_TURNS     a frequency that makes `high` turns or more within `original` tokens stays, one of `low` or fewer
+ *                         is divided by factor, between them the two are mixed linearly in the number of turns
+ *   OCN_STRETCH_INDEX     the same ends, mixed linearly in i between the indices (rounded down for `high`, up for `low`) where the number of
+ *                         turns is `high` and `low`; *magnitude = 0.1 ln(factor) + 1 where factor > 1
+ * *magnitude is 1 otherwise.  OCN_ERR_SHAPE for parameters outside these formulas. */
+typedef enum { OCN_STRETCH_NONE = 0, OCN_STRETCH_LINEAR, OCN_STRETCH_BASE, OCN_STRETCH_TURNS, OCN_STRETCH_INDEX } ocn_stretch;
+int ocn_rotary_frequencies(int32_t rotary_dim, double base, int stretch, double factor, double original, double low, double high,
+                           double *frequencies, double *magnitude);
+
+/* out = x rotated.  With OCN_ROTATE_BACK by the negative angles (times magnitude as before): the gradient with respect to x
+ * for x = the gradient with respect to out. */
+#define OCN_ROTATE_BACK 2u
+int ocn_rotary(const ocn_tensor *x, const ocn_rotation *rotation, const ocn_tensor *out, uint32_t flags, void *stream);
+
+/* The norm of every head, and the rotation in the same pass, for queries and keys in one launch:
+ *     out = rotated( x / sqrt(mean(x^2) + eps) * weight ),    the mean over a head's channels.
+ * weight: [channels], half, bfloat16 or float, or NULL for ones.  rotation may be NULL.  k, k_weight and k_out may be NULL (queries
+ * alone); q and k have the same leading dimensions and channels. */
+int ocn_norm_rotary(const ocn_tensor *q, const ocn_tensor *q_weight, const ocn_tensor *q_out, const ocn_tensor *k,
+                    const ocn_tensor *k_weight, const ocn_tensor *k_out, double eps, const ocn_rotation *rotation, void *stream);
+
+/* Its gradient: q_gin and q_gweight are the gradients with respect to q and q_weight for q_gout, that with respect to q_out
+ * (q_gin may be the identical view of q_gout or of q).  q_gweight: [channels], half, bfloat16 or float, overwritten; NULL where it is not wanted or there
+ * are no weights.  The same bits every time.  workspace: DEVICE scratch of
+ * ocn_norm_rotary_grad_workspace_bytes(q, k) bytes, 256-byte aligned; not needed where both weight gradients are NULL. */
+size_t ocn_norm_rotary_grad_workspace_bytes(const ocn_tensor *q, const ocn_tensor *k);
+int ocn_norm_rotary_grad(const ocn_tensor *q_gout, const ocn_tensor *q, const ocn_tensor *q_weight, const ocn_tensor *q_gin, const ocn_tensor *q_gweight,
+                         const ocn_tensor *k_gout, const ocn_tensor *k, const ocn_tensor *k_weight, const ocn_tensor *k_gin, const ocn_tensor *k_gweight,
+                         double eps, const ocn_rotation *rotation, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * A paged cache of keys and values in four bits: an OCN_UINT8 tensor [pages, heads, block] whose last dimension is contiguous
+ * and whose base, offset and other strides are multiples of 16 bytes.  A block holds one head's keys and values of a page's P
+ * tokens, P a multiple of 16, D = 64, 128 or 256 channels each: ocn_cache_block_bytes(P, D) = P * D * 9 / 8 bytes (0 for
+ * other P or D), which gives P back where D is known.  Channels are held in groups of 32 with one half-precision scale:
+ *     value = scale * { 0, 1, 2, 3, 4, 6, 8, 12 }[code & 7],  negative where code & 8.
+ * In a block, in this order:
+ *     K codes   [P][D/2]              channel 2 i in the low half of byte i, 2 i + 1 in the high half
+ *     V codes   [P/4][16][4][D/32]    token 4 a + r, channels D/16 * j ... D/16 * (j+1) - 1 at [a][j][r], paired as above
+ *     K scales  [D/32][P]
+ *     V scales  [D/32][P]
+ * the orders in which attention's lanes read them.  scale = max|x| / 12 of the group rounded to nine significant bits
+ * (at most 5456: values beyond +-65472 saturate), so that every value is exact in half precision; a code is that of the
+ * nearest value to x / scale, ties to the even code.  A group with an infinity or a NaN has a NaN as its scale.
+ */
+size_t ocn_cache_block_bytes(int64_t page_tokens, int32_t channels);
+
+/* Appends keys and values, the keys rotated on the way (rotation may be NULL): k and v are [..., heads, channels], slots has their leading
+ * dimensions and says where each token goes: page * P + place in the page.  A token whose slot is
+ * negative or past the last page is left out.  Of tokens with one slot, which is kept is not defined. */
+int ocn_cache_append(const ocn_tensor *k, const ocn_tensor *v, const ocn_rotation *rotation, const ocn_tensor *slots,
+                     const ocn_tensor *cache, void *stream);
+
+/* The values that the cache holds at slots, into k and v (either may be NULL) in their type.  A slot outside the cache is not followed: its
+ * rows keep their old contents. */
+int ocn_cache_read(const ocn_tensor *cache, const ocn_tensor *slots, const ocn_tensor *k, const ocn_tensor *v, void *stream);
+
+/* Attention of q [batch, queries, heads, channels] over the cache:
+ *     out = sum_j p_j v_j,  p = softmax_j(scale * q . k_j),  over the tokens j of the sequence that the query sees,
+ *     max(0, n - window) <= j < n,  n = visible[batch, query], at most columns * P  (window 0: all j < n).
+ * Token j of sequence b lies in page table[b, j / P] (table: [batch, columns]); a token whose page is not one of the cache
+ * is not seen.  visible: [batch, queries], or 1 in the place of either.  heads is a multiple of the cache's heads: query head h
+ * reads head h / (heads / cache heads).  A query that sees nothing gets zeros.  log_sum (or NULL): OCN_FLOAT [batch, queries, heads], the natural
+ * logarithm of sum_j exp(scale * q . k_j), -inf where nothing is seen.  Scores, sums and the softmax are
+ * held in single precision.  workspace: DEVICE scratch of ocn_cache_attention_workspace_bytes(...) bytes (a function
+ * of the shapes alone; 0 where none is needed), 256-byte aligned.  The same bits every time. */
+size_t ocn_cache_attention_workspace_bytes(const ocn_tensor *q, const ocn_tensor *cache, const ocn_tensor *table);
+int ocn_cache_attention(const ocn_tensor *q, const ocn_tensor *cache, const ocn_tensor *table, const ocn_tensor *visible,
+                        double scale, int64_t window, const ocn_tensor *out, const ocn_tensor *log_sum, void *workspace,
+                        size_t workspace_bytes, void *stream);
 
 /* Bytes of workspace ocn_reduce needs for these arguments (0 when it runs in one pass).
  * Returns 0 as well when the arguments are invalid; ocn_reduce then reports the error. */

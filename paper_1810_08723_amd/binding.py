@@ -20,6 +20,7 @@ LIB_PATH = os.path.join(HERE, "libocn.so")
 DTYPES = ("bool", "int8", "int16", "int32", "int64", "uint8", "uint16", "uint32", "uint64",
           "half", "float", "double", "chalf", "cfloat", "cdouble")
 DTYPE_CODE = {n: i for i, n in enumerate(DTYPES)}
+DTYPE_CODE["bfloat16"] = 32      # (a type of the operators over heads alone)
 UNARY_OPS = ("ident", "neg", "abs", "conj", "lnot", "bnot", "sqrt", "sin", "cos", "tan", "exp", "log", "bswap",
              "asin", "acos", "atan", "sinh", "cosh", "tanh")
 BINARY_OPS = ("add", "sub", "mul", "div", "min", "max", "band", "bor", "bxor", "land", "lor",
@@ -44,13 +45,21 @@ EXPORTS = ("ocn_unary", "ocn_binary", "ocn_cast_copy", "ocn_reduce", "ocn_reduce
            "ocn_binary_reduce", "ocn_binary_reduce_workspace_bytes", "ocn_plan_binary_reduce",
            "ocn_index_offsets", "ocn_mask_offsets", "ocn_mask_offsets_workspace_bytes", "ocn_gather",
            "ocn_scatter", "ocn_domain_check", "ocn_domain_check_workspace_bytes", "ocn_reduce_scratch",
-           "ocn_unary_mode", "ocn_unary_mode_workspace_bytes", "ocn_set_max_launch_blocks")
+           "ocn_unary_mode", "ocn_unary_mode_workspace_bytes", "ocn_set_max_launch_blocks",
+           "ocn_rotary_frequencies", "ocn_rotary", "ocn_norm_rotary", "ocn_norm_rotary_grad",
+           "ocn_norm_rotary_grad_workspace_bytes", "ocn_cache_block_bytes", "ocn_cache_append", "ocn_cache_read",
+           "ocn_cache_attention", "ocn_cache_attention_workspace_bytes")
 
 
 class OcnTensor(C.Structure):
     _fields_ = [("base", C.c_void_p), ("offset", C.c_int64), ("dtype", C.c_int32),
                 ("ndim", C.c_int32), ("size", C.c_int64 * MAX_DIMS),
                 ("stride", C.c_int64 * MAX_DIMS), ("device", C.c_int32), ("byteswapped", C.c_int32)]
+
+
+class OcnRotation(C.Structure):
+    _fields_ = [("positions", C.POINTER(OcnTensor)), ("frequencies", C.POINTER(OcnTensor)), ("rotary_dim", C.c_int32),
+                ("layout", C.c_int32), ("magnitude", C.c_double)]
 
 
 class OcnPlanInfo(C.Structure):
@@ -139,6 +148,20 @@ def lib() -> C.CDLL:
                                        C.c_size_t, C.c_void_p]
         L.ocn_gather.argtypes = [T, C.c_void_p, C.c_int64, C.c_int64, C.c_int64, T, C.c_void_p]
         L.ocn_scatter.argtypes = [T, C.c_void_p, C.c_int64, C.c_int64, C.c_int64, T, C.c_void_p]
+        R, D, V, Z = C.POINTER(OcnRotation), C.c_double, C.c_void_p, C.c_size_t
+        L.ocn_rotary_frequencies.argtypes = [C.c_int32, D, C.c_int, D, D, D, D, C.POINTER(D), C.POINTER(D)]
+        L.ocn_rotary.argtypes = [T, R, T, C.c_uint32, V]
+        L.ocn_norm_rotary.argtypes = [T, T, T, T, T, T, D, R, V]
+        L.ocn_norm_rotary_grad.argtypes = [T] * 10 + [D, R, V, Z, V]
+        L.ocn_norm_rotary_grad_workspace_bytes.argtypes = [T, T]
+        L.ocn_norm_rotary_grad_workspace_bytes.restype = Z
+        L.ocn_cache_block_bytes.argtypes = [C.c_int64, C.c_int32]
+        L.ocn_cache_block_bytes.restype = Z
+        L.ocn_cache_append.argtypes = [T, T, R, T, T, V]
+        L.ocn_cache_read.argtypes = [T, T, T, T, V]
+        L.ocn_cache_attention.argtypes = [T, T, T, T, D, C.c_int64, T, T, V, Z, V]
+        L.ocn_cache_attention_workspace_bytes.argtypes = [T, T, T]
+        L.ocn_cache_attention_workspace_bytes.restype = Z
         for name, direct in _direct.items():
             direct.address = C.cast(getattr(L, "ocn_" + name), C.c_void_p).value
         _lib = L
@@ -283,7 +306,8 @@ def _function(name: str):
 
 
 for _name in ("ocn_unary", "ocn_binary", "ocn_cast_copy", "ocn_reduce", "ocn_binary_reduce", "ocn_reduce_scratch",
-              "ocn_index_offsets", "ocn_mask_offsets", "ocn_gather", "ocn_scatter"):
+              "ocn_index_offsets", "ocn_mask_offsets", "ocn_gather", "ocn_scatter", "ocn_rotary", "ocn_norm_rotary",
+              "ocn_norm_rotary_grad", "ocn_cache_append", "ocn_cache_read", "ocn_cache_attention"):
     globals()["_" + _name] = _function(_name)
 
 
@@ -402,6 +426,119 @@ def scatter(src: Tensor, offsets, lo: int, hi: int, out_inner: Tensor, stream=No
     n = offsets.numel()
     rc = _ocn_scatter(src._ref or src._make_ref(), offsets.data_ptr() if n else None, n, lo, hi,
                       out_inner._ref or out_inner._make_ref(), _stream(stream))
+    if rc:
+        _check(rc)
+
+
+ROTARY_LAYOUTS = ("half", "interleaved")
+STRETCHES = ("none", "linear", "base", "turns", "index")
+ROTATE_BACK = 2
+
+
+class Rotation:
+    """A rotation by position, as the calls over heads take it: the first `rotary_dim` channels of every head, in pairs
+    (i, i + rotary_dim/2) (layout "half") or (2i, 2i + 1) ("interleaved"), by positions * frequencies.  It keeps its
+    tensors; a program makes it once for its buffers."""
+
+    def __init__(self, positions: Tensor, frequencies: Tensor, rotary_dim: int, layout: str = "half", magnitude: float = 1.0):
+        struct = OcnRotation(C.pointer(positions.desc()), C.pointer(frequencies.desc()), rotary_dim, ROTARY_LAYOUTS.index(layout), magnitude)
+        self.__dict__.update(positions=positions, frequencies=frequencies, rotary_dim=rotary_dim, layout=layout, magnitude=magnitude,
+                             _struct=struct, _ref=C.byref(struct))
+
+    def __setattr__(self, name, value):
+        raise AttributeError("a Rotation stays as it was made")
+
+
+def rotary_frequencies(rotary_dim: int, base: float = 10000.0, stretch: str = "none", factor: float = 1.0, original: float = 0.0,
+                       low: float = 1.0, high: float = 4.0) -> Tuple[list, float]:
+    """Frequencies (radians per position, rotary_dim/2 of them) and the magnitude of a rotation, on the host: base^(-2i/rotary_dim),
+    changed for long contexts by one of STRETCHES (see ocn.h)."""
+    f, m = (C.c_double * max(rotary_dim // 2, 1))(), C.c_double()
+    _check(lib().ocn_rotary_frequencies(rotary_dim, base, STRETCHES.index(stretch), factor, original, low, high, f, C.byref(m)))
+    return list(f), m.value
+
+
+def _optional(t):
+    return None if t is None else t._ref or t._make_ref()
+
+
+def rotary(x: Tensor, rotation: Rotation, out: Tensor, inverse: bool = False, stream=None) -> None:
+    """out = x rotated by position; `inverse`: by the negative angles, which takes the gradient of out to that of x."""
+    rc = _ocn_rotary(x._ref or x._make_ref(), rotation._ref, out._ref or out._make_ref(), ROTATE_BACK if inverse else 0, _stream(stream))
+    if rc:
+        _check(rc)
+
+
+def norm_rotary(q: Tensor, q_weight: Optional[Tensor], q_out: Tensor, k: Optional[Tensor] = None, k_weight: Optional[Tensor] = None,
+                k_out: Optional[Tensor] = None, eps: float = 1e-6, rotation: Optional[Rotation] = None, stream=None) -> None:
+    """The norm of every head of q (and of k) over its channels, times the weights, and the rotation: one launch."""
+    rc = _ocn_norm_rotary(q._ref or q._make_ref(), _optional(q_weight), q_out._ref or q_out._make_ref(), _optional(k), _optional(k_weight),
+                          _optional(k_out), eps, None if rotation is None else rotation._ref, _stream(stream))
+    if rc:
+        _check(rc)
+
+
+def norm_rotary_grad_workspace_bytes(q: Tensor, k: Optional[Tensor] = None) -> int:
+    return int(lib().ocn_norm_rotary_grad_workspace_bytes(_optional(q), _optional(k)))
+
+
+def norm_rotary_grad(q_gout: Tensor, q: Tensor, q_weight: Optional[Tensor], q_gin: Tensor, q_gweight: Optional[Tensor] = None,
+                     k_gout: Optional[Tensor] = None, k: Optional[Tensor] = None, k_weight: Optional[Tensor] = None,
+                     k_gin: Optional[Tensor] = None, k_gweight: Optional[Tensor] = None, eps: float = 1e-6,
+                     rotation: Optional[Rotation] = None, workspace=None, stream=None) -> None:
+    """Gradients of norm_rotary with respect to q and q_weight (and k and k_weight); `workspace` as for reduce()."""
+    ws_ptr, ws_bytes = None, 0
+    if workspace is None and (q_gweight is not None or k_gweight is not None):
+        need = norm_rotary_grad_workspace_bytes(q, k)
+        if need:
+            workspace = _scratch(need, q.device, stream)
+    if workspace is not None:
+        ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel()
+    rc = _ocn_norm_rotary_grad(_optional(q_gout), _optional(q), _optional(q_weight), _optional(q_gin), _optional(q_gweight), _optional(k_gout),
+                               _optional(k), _optional(k_weight), _optional(k_gin), _optional(k_gweight), eps,
+                               None if rotation is None else rotation._ref, ws_ptr, ws_bytes, _stream(stream))
+    if rc:
+        _check(rc)
+
+
+def cache_block_bytes(page_tokens: int, channels: int) -> int:
+    """Bytes of a block of the 4-bit cache: one head's keys and values of a page (0: no such page)."""
+    return int(lib().ocn_cache_block_bytes(page_tokens, channels))
+
+
+def cache_append(k: Tensor, v: Tensor, slots: Tensor, cache: Tensor, rotation: Optional[Rotation] = None, stream=None) -> None:
+    """Keys (rotated on the way) and values [..., heads, channels] into the 4-bit cache at `slots` (page * P + place; negative: left out)."""
+    rc = _ocn_cache_append(k._ref or k._make_ref(), v._ref or v._make_ref(), None if rotation is None else rotation._ref,
+                           slots._ref or slots._make_ref(), cache._ref or cache._make_ref(), _stream(stream))
+    if rc:
+        _check(rc)
+
+
+def cache_read(cache: Tensor, slots: Tensor, k: Optional[Tensor], v: Optional[Tensor], stream=None) -> None:
+    """The values that the cache holds at `slots`, into k and v (either may be None)."""
+    rc = _ocn_cache_read(cache._ref or cache._make_ref(), slots._ref or slots._make_ref(), _optional(k), _optional(v), _stream(stream))
+    if rc:
+        _check(rc)
+
+
+def cache_attention_workspace_bytes(q: Tensor, cache: Tensor, table: Tensor) -> int:
+    return int(lib().ocn_cache_attention_workspace_bytes(_optional(q), _optional(cache), _optional(table)))
+
+
+def cache_attention(q: Tensor, cache: Tensor, table: Tensor, visible: Tensor, out: Tensor, scale: float, window: int = 0,
+                    log_sum: Optional[Tensor] = None, workspace=None, stream=None) -> None:
+    """Attention of q [batch, queries, heads, channels] over the cached tokens that each query sees (`visible`: how many, the
+    last `window` of them where it is not 0), found through the page table [batch, columns]; `workspace` as for reduce()."""
+    ws_ptr, ws_bytes = None, 0
+    if workspace is None:
+        need = cache_attention_workspace_bytes(q, cache, table)
+        if need:
+            workspace = _scratch(need, q.device, stream)
+    if workspace is not None:
+        ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel()
+    rc = _ocn_cache_attention(q._ref or q._make_ref(), cache._ref or cache._make_ref(), table._ref or table._make_ref(),
+                              visible._ref or visible._make_ref(), scale, window, out._ref or out._make_ref(), _optional(log_sum),
+                              ws_ptr, ws_bytes, _stream(stream))
     if rc:
         _check(rc)
 

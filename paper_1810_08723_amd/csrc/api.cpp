@@ -200,7 +200,7 @@ size_t ocn_reduce_workspace_bytes(int op, const ocn_tensor *a, const int32_t *ax
 
 int ocn_promote(int dtype_a, int dtype_b) { return promote(dtype_a, dtype_b); }
 
-int ocn_dtype_size(int dtype) { return dtype >= 0 && dtype < DT_COUNT ? dt_size(dtype) : 0; }
+int ocn_dtype_size(int dtype) { return dtype >= 0 && dtype < DT_COUNT ? dt_size(dtype) : dtype == OCN_BFLOAT16 ? 2 : 0; }
 
 const char *ocn_error_string(int code) {
   switch (code) {
