@@ -18,103 +18,649 @@ struct AttentionArgs {
   int64_t lb, lt, lh;                          // of log_sum
   int64_t tb, tc, sb, st;                      // of table (batch, column) and visible (batch, query)
   int64_t page_stride, head_stride;
-  int64_t pages, columns, window;
-  int32_t batch, queries, heads, per_kv;       // query heads to a head of the cache
+  int64_t pages, window;
+  int32_t queries, per_kv;                     // query heads to a head of the cache
   int32_t page, type, table_wide, seen_wide;
-  FastDiv page_div;
+  int32_t capacity;                            // tokens that a row of the table has pages for
+  int32_t least;                               // tiles of a split, at least
+  int32_t whole_q, whole_out;                  // rows are aligned and without gaps
+  uint32_t first_item;                         // of this launch
+  FastDiv page_div, per_kv_div, splits_div, blocks_div, kv_div;
+  float *parts, *part_sums;                    // [items][rows of a unit][channels], [..][2]: maximum and sum
   float scale;                                 // of the scores, times log2(e)
 };
 
-// A workgroup has one query head of one query.  Each wavefront goes over tiles of 64 tokens with a running maximum and
-// sum: a lane has a token's score, then its channels of the weighted values.
-template <int D> __global__ __launch_bounds__(kBlock) void attention_kernel(const AttentionArgs a) {
-  constexpr int W = kBlock / kWave, C = D / kWave;
-  __shared__ float query[D];
-  __shared__ float weight[W][kWave];
-  __shared__ int64_t place[W][kWave];
-  __shared__ float sums[W][D], top_of[W], total_of[W];
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  for (int64_t unit = blockIdx.x; unit < (int64_t)a.batch * a.queries * a.heads; unit += gridDim.x) {
-    const int h = (int)(unit % a.heads), t = (int)(unit / a.heads % a.queries), b = (int)(unit / a.heads / a.queries);
-    for (int c = threadIdx.x; c < D; c += kBlock)
-      query[c] = load_as_float(a.q + b * a.qb + t * a.qt + h * a.qh + c * a.qe, a.type) * a.scale;
-    __syncthreads();
-    const int64_t n = min(load_index(a.seen + b * a.sb + t * a.st, a.seen_wide), a.columns * a.page);
-    const int64_t first = a.window > 0 ? max(n - a.window, (int64_t)0) : 0;
-    float top = -__builtin_inff(), total = 0.0f, acc[C];
+constexpr int64_t kLeastTiles = 8;             // of a split: two for each wavefront
+constexpr int64_t kMaxSplits = kWave;          // a lane each when they are joined
+constexpr int64_t kWorkgroups = 1024;          // worth launching: four to a CU
+
+// ---------------------------------------------------------------------------------------
+// The kernel.  Query heads of one head of the cache, of one or more queries, are the rows of its tiles: 16 a tile.  For 32 tokens at a
+// time a wavefront forms scores^T = K Q^T and out^T += V^T P^T with 16x16x32 products in half precision, sums in single:
+//
+//   scores^T   lane (n = lane % 16, g = lane / 16): row n, tokens 16 a + 4 g + r.  K is the left operand: its lane has token n of
+//              a half tile and, of each step's 32 channels, eight; a code's eight channels are a word, and which 32 channels make a step is free as
+//              long as Q has the same, so that a lane's words lie together in memory (16 bytes of a row of 128 channels).
+//   out^T      row n, channels D/16 (4 g + r) + i of tile i.  The order of the 32 tokens inside a step is free as well: the
+//              scores' own order is taken, and no weight crosses lanes between the two products.
+//
+// A code becomes a half in one conversion for two; times its group's scale it is exact (two bits of the code, nine of the
+// scale), so that K and V lose nothing.  V's pairs are two tokens of a channel: nibbles of two rows are put side by side (one shift and one bit
+// select for eight codes) before they are converted.  Q is exact where its type has no more than 11 bits: a row is scaled by a power of two so that its
+// largest channel is near 2^13.  Weights are rounded to half (2^-11, below half a step of a bfloat16 result); for half results
+// a second product adds what that rounding left (PARTS_P = 2), for float results Q has two parts as well (PARTS_Q = 2).
+//
+// The maximum of a row that its weights are relative to is raised, and sums rescaled, only where a score is 2^4 above it; weights are times 2^11, so
+// that they stay below 2^15.  The sum of the weights is one more product, with ones.
+//
+// Weights that far below the largest are not numbers that a half (or the second part of one) holds to its full precision; left
+// at that, a channel that is zero in the tokens with large weights would lose what the others give it.  A tile with weights below kFloor
+// takes them out and multiplies them apart, times a power of two, in as many steps as they need: weights keep their relative precision down to 2^-126.
+// ---------------------------------------------------------------------------------------
+
+constexpr float kWeightBits = 11.0f, kRaise = 4.0f;
+template <int PARTS_P> struct Floor {
+  static constexpr int kBits = PARTS_P == 1 ? -14 : -4;       // log2 of the smallest weight that is taken as it is
+  static constexpr int kStep = 14 - kBits;                    // what smaller ones are multiplied by, and again: below 2^14 then
+  static constexpr float kLeast = PARTS_P == 1 ? 0x1p-14f : 0x1p-4f, kUp = PARTS_P == 1 ? 0x1p28f : 0x1p18f, kDown = 1.0f / kUp;
+};
+constexpr int kTile = 32;            // tokens
+
+template <int D> struct Shape {
+  static constexpr int kWords = D / 32;                   // of a token's codes in a lane; steps of the scores; groups
+  static constexpr int kRun = kWords < 4 ? kWords : 4;    // words that lie together
+  static constexpr int kChunks = kWords / kRun;
+  static constexpr int kTiles = D / 16;                   // of out^T
+};
+
+// what a lane holds of a tile's codes and scales, as they come from memory
+template <int D> struct Raw {
+  uint32_t k[2][Shape<D>::kWords], v[2][Shape<D>::kWords];
+  f16 k_scale[2][Shape<D>::kChunks];
+  u32x2 v_scale[2];
+};
+
+// a half tile's page: the address of its tokens' codes and scales; the same in all lanes
+struct Place {
+  const char *codes, *scales;
+  bool fine;
+};
+
+template <int N> __device__ __forceinline__ void load_words(uint32_t *to, const char *from) {
+  if constexpr (N % 4 == 0) {
 #pragma unroll
-    for (int c = 0; c < C; ++c) acc[c] = 0.0f;
-    for (int64_t base = first / kWave * kWave + wave * kWave; base < n; base += W * kWave) {
-      const int64_t j = base + lane;
-      float score = -__builtin_inff();
-      place[wave][lane] = -1;
-      if (j >= first && j < n) {
-        const int64_t column = j / a.page, page = load_index(a.table + b * a.tb + column * a.tc, a.table_wide);
-        const int at = (int)(j - column * a.page);
-        if (page >= 0 && page < a.pages) {
-          const int64_t block = page * a.page_stride + (h / a.per_kv) * a.head_stride;
-          place[wave][lane] = block * 2 * kMaxPage + at;
-          score = 0.0f;
-          for (int g = 0; g < D / 32; ++g) {
-            float part = 0.0f;
-            for (int c = 0; c < 32; c += 8) {
-              const uint32_t codes = *(const uint32_t *)(a.cache + block + block_k_codes(a.page, D, at, g * 32 + c));
-              const f16x2 c0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, 2.0f, 0), c1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, 2.0f, 1);
-              const f16x2 c2 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, 2.0f, 2), c3 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, 2.0f, 3);
-              const float *q = query + g * 32 + c;
-              part += (float)c0.x * q[0] + (float)c0.y * q[1] + (float)c1.x * q[2] + (float)c1.y * q[3] + (float)c2.x * q[4] +
-                      (float)c2.y * q[5] + (float)c3.x * q[6] + (float)c3.y * q[7];
-            }
-            score += part * (float)*(const f16 *)(a.cache + block + block_scale(a.page, D, false, g, at));
-          }
-        }
-      }
-      float most = score;
-      for (int m = 1; m < kWave; m <<= 1) most = fmaxf(most, __shfl_xor(most, m));
-      const float now = fmaxf(top, most), shift = now == -__builtin_inff() ? 0.0f : now;
-      const float p = __builtin_amdgcn_exp2f(score - shift), keep = __builtin_amdgcn_exp2f(top - shift);
-      top = now;
-      float add = p;
-      for (int m = 1; m < kWave; m <<= 1) add += __shfl_xor(add, m);
-      total = total * keep + add;
-      weight[wave][lane] = p;
-#pragma unroll
-      for (int c = 0; c < C; ++c) acc[c] *= keep;
-      for (int i = 0; i < kWave; ++i) {
-        const int64_t where = place[wave][i];
-        if (where < 0) continue;
-        const int at = (int)(where & (2 * kMaxPage - 1));
-        const char *block = a.cache + where / (2 * kMaxPage);
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-          const int channel = lane * C + c;
-          const uint32_t codes = *(const uint8_t *)(block + block_v_codes(a.page, D, at, channel));
-          const f16x2 v = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, 2.0f, 0);
-          const float s = (float)*(const f16 *)(block + block_scale(a.page, D, true, channel / 32, at));
-          acc[c] += weight[wave][i] * ((float)(channel & 1 ? v.y : v.x) * s);
-        }
-      }
+    for (int i = 0; i < N; i += 4) {
+      const u32x4 w = *(const u32x4 *)(from + 4 * i);
+      to[i] = w.x, to[i + 1] = w.y, to[i + 2] = w.z, to[i + 3] = w.w;
     }
-#pragma unroll
-    for (int c = 0; c < C; ++c) sums[wave][lane * C + c] = acc[c];
-    if (lane == 0) {
-      top_of[wave] = top;
-      total_of[wave] = total;
-    }
-    __syncthreads();
-    float all = -__builtin_inff(), sum = 0.0f;
-    for (int w = 0; w < W; ++w) all = fmaxf(all, top_of[w]);
-    const float shift = all == -__builtin_inff() ? 0.0f : all;
-    for (int w = 0; w < W; ++w) sum += total_of[w] * __builtin_amdgcn_exp2f(top_of[w] - shift);
-    for (int c = threadIdx.x; c < D; c += kBlock) {
-      float v = 0.0f;
-      for (int w = 0; w < W; ++w) v += sums[w][c] * __builtin_amdgcn_exp2f(top_of[w] - shift);
-      store_from_float(a.out + b * a.ob + t * a.ot + h * a.oh + c * a.oe, a.type, sum == 0.0f ? 0.0f : v / sum);
-    }
-    if (a.log_sum && threadIdx.x == 0)
-      *(float *)(a.log_sum + b * a.lb + t * a.lt + h * a.lh) = sum == 0.0f ? -__builtin_inff() : 0.69314718f * (all + __builtin_log2f(sum));
-    __syncthreads();
+  } else {
+    const u32x2 w = *(const u32x2 *)from;
+    to[0] = w.x, to[1] = w.y;
   }
+}
+
+// the page of 16 tokens from j on (a multiple of 16); past the sequence's end and in pages outside the cache it is page 0, which may be read
+template <int D> __device__ __forceinline__ Place place_of(const AttentionArgs &a, const char *row, int64_t head, int j, int end) {
+  Place p;
+  p.fine = j < end;
+  int64_t page = 0;
+  int at = 0;
+  if (p.fine) {
+    const int column = (int)fast_quotient((uint32_t)j, a.page_div);
+    at = j - column * a.page;
+    typedef const __attribute__((address_space(4))) int64_t *Wide;
+    typedef const __attribute__((address_space(4))) int32_t *Narrow;
+    const char *entry = row + column * a.tc;
+    page = a.table_wide ? *(Wide)(uintptr_t)entry : (int64_t)*(Narrow)(uintptr_t)entry;
+    p.fine = page >= 0 && page < a.pages;
+    if (!p.fine) page = 0, at = 0;
+  }
+  const char *block = a.cache + page * a.page_stride + head;
+  p.codes = block + at * (D / 2);
+  p.scales = block + at * 2;
+  return p;
+}
+
+struct LaneOffsets { uint32_t k, v, k_scale, k_scale_step, v_scale; };
+
+template <int D> __device__ __forceinline__ LaneOffsets lane_offsets(const AttentionArgs &a, int n, int g) {
+  typedef Shape<D> S;
+  LaneOffsets o;
+  o.k = n * (D / 2) + g * (4 * S::kRun);
+  o.v = a.page * (D / 2) + (g * 16 + n) * (D / 8);
+  o.k_scale = a.page * D + 2 * ((S::kRun * g / 4) * a.page + n);
+  o.k_scale_step = 2 * S::kRun * a.page;
+  o.v_scale = a.page * D + 2 * ((S::kWords + S::kWords * n / 16) * a.page + 4 * g);
+  return o;
+}
+
+template <int D> __device__ __forceinline__ void load_raw(Raw<D> &r, const Place *p, const LaneOffsets &o) {
+  typedef Shape<D> S;
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+#pragma unroll
+    for (int h = 0; h < S::kChunks; ++h) {
+      load_words<S::kRun>(&r.k[x][h * S::kRun], p[x].codes + o.k + h * 16 * S::kRun);
+      r.k_scale[x][h] = *(const f16 *)(p[x].scales + o.k_scale + h * o.k_scale_step);
+    }
+    load_words<S::kWords>(r.v[x], p[x].codes + o.v);
+    r.v_scale[x] = *(const u32x2 *)(p[x].scales + o.v_scale);
+  }
+}
+
+template <int BYTE> __device__ __forceinline__ f16x2 two_codes(uint32_t w) { return __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 2.0f, BYTE); }
+
+union Frag {
+  f16x8 v;
+  f16x2 p[4];
+  uint32_t u[4];
+};
+
+// bits of a where the mask has ones, of b elsewhere
+__device__ __forceinline__ uint32_t select_bits(uint32_t mask, uint32_t a, uint32_t b) { return (a & mask) | (b & ~mask); }
+
+// pair `i` of out^T tiles' operands from the codes of tokens 2 i and 2 i + 1 of a lane's four
+template <int D> __device__ __forceinline__ void pair_of_tokens(const uint32_t *v, int i, f16x2 scale, f16x2 *out) {
+  constexpr uint32_t low = 0x0f0f0f0fu;
+  if constexpr (D == 64) {
+    const uint32_t w = v[i], even = select_bits(low, w, w >> 12), odd = select_bits(low, w >> 4, w >> 16);
+    out[0] = two_codes<0>(even) * scale, out[1] = two_codes<0>(odd) * scale;
+    out[2] = two_codes<1>(even) * scale, out[3] = two_codes<1>(odd) * scale;
+  } else {
+#pragma unroll
+    for (int q = 0; q < D / 128; ++q) {
+      const uint32_t a = v[2 * i * (D / 128) + q], b = v[(2 * i + 1) * (D / 128) + q];
+      const uint32_t even = select_bits(low, a, b << 4), odd = select_bits(low, a >> 4, b);
+      f16x2 *o = out + 8 * q;
+      o[0] = two_codes<0>(even) * scale, o[1] = two_codes<0>(odd) * scale;
+      o[2] = two_codes<1>(even) * scale, o[3] = two_codes<1>(odd) * scale;
+      o[4] = two_codes<2>(even) * scale, o[5] = two_codes<2>(odd) * scale;
+      o[6] = two_codes<3>(even) * scale, o[7] = two_codes<3>(odd) * scale;
+    }
+  }
+}
+
+// the largest of the four lanes that hold a row
+__device__ __forceinline__ float row_max(float x) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+  const uint32_t a0 = a[0], a1 = a[1];
+  x = fmaxf(__builtin_bit_cast(float, a0), __builtin_bit_cast(float, a1));
+  const auto b = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+  const uint32_t b0 = b[0], b1 = b[1];
+  return fmaxf(__builtin_bit_cast(float, b0), __builtin_bit_cast(float, b1));
+}
+
+__device__ __forceinline__ int wave_max(int x) {
+  for (int m = 1; m < kWave; m <<= 1) x = max(x, __shfl_xor(x, m));
+  return __builtin_amdgcn_readfirstlane(x);
+}
+
+__device__ __forceinline__ f32x4 product(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+// Sums of one wavefront's rows: row n of lane (n, g)
+template <int D, int RT> struct Sums {
+  f32x4 out[RT][Shape<D>::kTiles];   // out^T
+  f32x4 total[RT];                   // of the weights (all four the same)
+  f32x4 bad[RT];                     // how many tokens with a NaN as V's scale a row sees, in tiles that are not seen whole
+  float top[RT];                     // what weights are relative to (base 2)
+};
+
+template <int D, int RT, int PARTS_Q> struct Rows {
+  f16x8 q[RT][PARTS_Q][Shape<D>::kWords];
+  float scale[RT];                   // of a score
+  int lo[RT], hi[RT];                // tokens that a row sees
+};
+
+template <int D, int RT, int PARTS_Q, int PARTS_P, bool WHOLE>
+__device__ __forceinline__ void one_tile(Sums<D, RT> &s, const Rows<D, RT, PARTS_Q> &rows, const Raw<D> &raw, int g, int j0, bool fine0, bool fine1) {
+  typedef Shape<D> S;
+  f32x4 score[RT][2];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+    for (int x = 0; x < 2; ++x) score[rt][x] = f32x4{0, 0, 0, 0};
+#pragma unroll
+  for (int x = 0; x < 2; ++x)
+#pragma unroll
+    for (int w = 0; w < S::kWords; ++w) {
+      const uint32_t codes = raw.k[x][w];
+      const f16 sc = raw.k_scale[x][w / S::kRun];
+      const f16x2 scale = {sc, sc};
+      Frag k;
+      k.p[0] = two_codes<0>(codes) * scale, k.p[1] = two_codes<1>(codes) * scale;
+      k.p[2] = two_codes<2>(codes) * scale, k.p[3] = two_codes<3>(codes) * scale;
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int part = 0; part < PARTS_Q; ++part) score[rt][x] = product(k.v, rows.q[rt][part][w], score[rt][x]);
+    }
+  f16x2 v_scale[2][2];
+  // Weights of zero do not make a token's NaN go away: in a tile that some row does not see whole, a scale that is NaN (or none that
+  // appending writes: places that were never written) counts as zero, and rows that do see its token are marked by one more product.
+  Frag nan_of;         // 1 for such tokens
+#pragma unroll
+  for (int x = 0; x < 2; ++x)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t two = raw.v_scale[x][i];     // (an element of a vector has no address to cast from)
+      f16x2 sc = __builtin_bit_cast(f16x2, two);
+      if constexpr (!WHOLE) {
+        f16x2 bad = {0, 0};
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          if (!(sc[e] <= (f16)5456.0f && sc[e] >= (f16)-5456.0f)) { sc[e] = (f16)0.0f; bad[e] = (f16)1.0f; }
+        }
+        nan_of.p[2 * x + i] = bad;
+      }
+      v_scale[x][i] = sc;
+    }
+  typedef Floor<PARTS_P> F;
+  const f16x8 ones = {1, 1, 1, 1, 1, 1, 1, 1};
+  Frag p[RT][PARTS_P];
+  float small[RT][8];
+  bool apart = false;          // whether some weights are below the floor
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    float v[8], most = -__builtin_inff(), least = __builtin_inff();
+    Frag sees;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      v[i] = score[rt][i / 4][i % 4] * rows.scale[rt];
+      if constexpr (!WHOLE) {
+        const int j = j0 + 16 * (i / 4) + 4 * g + i % 4;
+        const bool in = j >= rows.lo[rt] && j < rows.hi[rt] && (i < 4 ? fine0 : fine1);
+        sees.v[i] = in ? (f16)1.0f : (f16)0.0f;
+        least = fminf(least, in ? v[i] : __builtin_inff());
+        if (!in) v[i] = -__builtin_inff();
+      } else {
+        least = fminf(least, v[i]);
+      }
+      most = fmaxf(most, v[i]);
+    }
+    most = row_max(most);
+    if (__builtin_amdgcn_ballot_w64(most > s.top[rt] + kRaise)) {
+      const float now = fmaxf(s.top[rt], most), keep = now == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(s.top[rt] - now);
+      s.top[rt] = now;
+#pragma unroll
+      for (int i = 0; i < S::kTiles; ++i) s.out[rt][i] *= keep;
+      s.total[rt] *= keep;
+    }
+    const float shift = (s.top[rt] == -__builtin_inff() ? 0.0f : s.top[rt]) - kWeightBits;
+    const bool low = __builtin_amdgcn_ballot_w64(least < shift + F::kBits) != 0;
+    apart |= low;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float w = __builtin_amdgcn_exp2f(v[i] - shift);
+      small[rt][i] = 0.0f;
+      if (low) {
+        small[rt][i] = w < F::kLeast ? w : 0.0f;
+        w = w < F::kLeast ? 0.0f : w;
+      }
+      p[rt][0].v[i] = (f16)w;
+      if constexpr (PARTS_P == 2) p[rt][1].v[i] = (f16)(w - (float)p[rt][0].v[i]);
+    }
+#pragma unroll
+    for (int part = 0; part < PARTS_P; ++part) s.total[rt] = product(ones, p[rt][part].v, s.total[rt]);
+    if constexpr (!WHOLE) s.bad[rt] = product(nan_of.v, sees.v, s.bad[rt]);
+  }
+  f16x2 pairs[2][2][S::kTiles];
+#pragma unroll
+  for (int x = 0; x < 2; ++x)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) pair_of_tokens<D>(raw.v[x], i, v_scale[x][i], pairs[x][i]);
+#pragma unroll
+  for (int t = 0; t < S::kTiles; ++t) {
+    Frag f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f.p[i] = pairs[i / 2][i % 2][t];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+      for (int part = 0; part < PARTS_P; ++part) s.out[rt][t] = product(f.v, p[rt][part].v, s.out[rt][t]);
+  }
+  if (apart) {
+    float down = F::kDown;
+#pragma nounroll
+    for (int step = 0; step < (126 + F::kStep - 1) / F::kStep; ++step, down *= F::kDown) {
+      bool left = false;
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float x = small[rt][i] * F::kUp, w = x < F::kLeast ? 0.0f : x;
+          small[rt][i] = x < F::kLeast ? x : 0.0f;
+          left |= small[rt][i] > 0.0f;
+          p[rt][0].v[i] = (f16)w;
+          if constexpr (PARTS_P == 2) p[rt][1].v[i] = (f16)(w - (float)p[rt][0].v[i]);
+        }
+        f32x4 add = {0, 0, 0, 0};
+#pragma unroll
+        for (int part = 0; part < PARTS_P; ++part) add = product(ones, p[rt][part].v, add);
+        s.total[rt] += add * down;
+      }
+#pragma unroll
+      for (int t = 0; t < S::kTiles; ++t) {
+        Frag f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f.p[i] = pairs[i / 2][i % 2][t];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+          f32x4 add = {0, 0, 0, 0};
+#pragma unroll
+          for (int part = 0; part < PARTS_P; ++part) add = product(f.v, p[rt][part].v, add);
+          s.out[rt][t] += add * down;
+        }
+      }
+      if (!__builtin_amdgcn_ballot_w64(left)) break;
+    }
+  }
+}
+
+// PARTS_Q and PARTS_P say which type a call's tensors have
+template <int PARTS_Q, int PARTS_P> struct TypeOfParts { typedef bf16 T; };
+template <> struct TypeOfParts<1, 2> { typedef f16 T; };
+template <> struct TypeOfParts<2, 2> { typedef float T; };
+
+// N channels of a row to memory
+template <class T, int N> __device__ __forceinline__ void store_row(const AttentionArgs &a, char *row, int channel, const float *v) {
+  if (a.whole_out) {
+    typedef T Four __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int i = 0; i < N; i += 4) *(Four *)(row + (channel + i) * (int)sizeof(T)) = Four{(T)v[i], (T)v[i + 1], (T)v[i + 2], (T)v[i + 3]};
+  } else {
+    int64_t step = a.oe;
+    asm volatile("" : "+s"(step)::"memory");
+#pragma unroll
+    for (int i = 0; i < N; ++i) *(T *)(row + (channel + i) * step) = (T)v[i];
+  }
+}
+
+__device__ __forceinline__ float log_of(float top, float total) { return total == 0.0f ? -__builtin_inff() : 0.69314718f * (top - kWeightBits + __builtin_log2f(total)); }
+
+// eight channels of a query, as they are in memory
+template <int PARTS_Q> __device__ __forceinline__ void load_channels(uint32_t *to, const char *row, int channel, bool any, const AttentionArgs &a) {
+  constexpr int N = 4 * PARTS_Q;
+#pragma unroll
+  for (int i = 0; i < N; ++i) to[i] = 0;
+  if (!any) return;
+  if (a.whole_q) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) load_words<4>(to + i, row + channel * (2 * PARTS_Q) + 4 * i);
+  } else {
+    int64_t step = a.qe;
+    asm volatile("" : "+s"(step)::"memory");   // (here and now: hoisted out of all loops, the addresses took more registers than the tiles)
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if constexpr (PARTS_Q == 2) to[i] = *(const uint32_t *)(row + (channel + i) * step);
+      else to[i] = *(const uint16_t *)(row + (channel + 2 * i) * step) | (uint32_t)*(const uint16_t *)(row + (channel + 2 * i + 1) * step) << 16;
+    }
+  }
+}
+template <int PARTS_Q, int PARTS_P> __device__ __forceinline__ void channels_of(float *x, const uint32_t *from) {
+#pragma unroll
+  for (int i = 0; i < 4 * PARTS_Q; ++i) {
+    if constexpr (PARTS_Q == 2) {
+      x[i] = __builtin_bit_cast(float, from[i]);
+    } else if constexpr (PARTS_P == 1) {
+      x[2 * i] = __builtin_bit_cast(float, from[i] << 16);
+      x[2 * i + 1] = __builtin_bit_cast(float, from[i] & 0xffff0000u);
+    } else {
+      const f16x2 h = __builtin_bit_cast(f16x2, from[i]);
+      x[2 * i] = (float)h.x, x[2 * i + 1] = (float)h.y;
+    }
+  }
+}
+
+// SHARE: a workgroup's wavefronts have the same rows and every fourth tile each, and join their sums in LDS; otherwise each has rows of its own and all tiles.
+template <int D, int RT, int PARTS_Q, int PARTS_P, bool SHARE>
+__global__ __launch_bounds__(kBlock, D * RT <= 128 ? 2 : 1) void attention_kernel(const AttentionArgs a) {
+  typedef Shape<D> S;
+  typedef typename TypeOfParts<PARTS_Q, PARTS_P>::T T;
+  constexpr int W = kBlock / kWave, kPart = S::kTiles < 8 ? S::kTiles : 8;
+  constexpr int kRows = 16 * RT * (SHARE ? 1 : W);             // of a unit
+  __shared__ float part[SHARE ? W : 1][SHARE ? 16 : 1][16][SHARE ? kPart : 1];
+  __shared__ float tops[W][RT][16], totals[W][RT][16];
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), n = lane % 16, g = lane / 16;
+  const LaneOffsets lanes = lane_offsets<D>(a, n, g);
+  const uint32_t item = a.first_item + blockIdx.x;
+  // items: splits fastest, then blocks of rows, heads of the cache, sequences
+  const uint32_t unit = fast_quotient(item, a.splits_div), split = item - unit * a.splits_div.d;
+  const uint32_t bh = fast_quotient(unit, a.blocks_div), block = unit - bh * a.blocks_div.d;
+  const int b = (int)fast_quotient(bh, a.kv_div), kv = (int)bh - b * (int)a.kv_div.d;
+  const int first_row = (int)block * kRows + (SHARE ? 0 : wave * 16 * RT), all_rows = a.queries * a.per_kv;
+  Rows<D, RT, PARTS_Q> rows;
+  Sums<D, RT> sums;
+  int hi_most = 0, hi_least = 0x7fffffff, lo_least = 0x7fffffff, lo_most = 0;
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int row = first_row + rt * 16 + n, t = row < all_rows ? (int)fast_quotient((uint32_t)row, a.per_kv_div) : 0;
+    rows.lo[rt] = 0;
+    rows.hi[rt] = 0x7fffffff;
+    uint32_t q[S::kWords][8 * PARTS_Q / 2];       // as they are in memory: two 16-bit channels, or a float, in a word
+    float most = 0.0f;
+    if (row < all_rows) {
+      const int64_t seen = load_index(a.seen + b * a.sb + t * a.st, a.seen_wide);
+      rows.hi[rt] = (int)max((int64_t)0, min(seen, (int64_t)a.capacity));
+      rows.lo[rt] = a.window > 0 ? (int)max((int64_t)0, rows.hi[rt] - a.window) : 0;
+      hi_most = max(hi_most, rows.hi[rt]);
+      hi_least = min(hi_least, rows.hi[rt]);
+      lo_most = max(lo_most, rows.lo[rt]);
+      if (rows.hi[rt] > 0) lo_least = min(lo_least, rows.lo[rt]);
+    }
+    const char *from = a.q + b * a.qb + t * a.qt + (int64_t)(kv * a.per_kv + row - t * a.per_kv) * a.qh;
+#pragma unroll
+    for (int w = 0; w < S::kWords; ++w) {
+      const int channel = 8 * (w / S::kRun * 4 * S::kRun + S::kRun * g + w % S::kRun);
+      load_channels<PARTS_Q>(q[w], from, channel, row < all_rows, a);
+      float x[8];
+      channels_of<PARTS_Q, PARTS_P>(x, q[w]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) most = fmaxf(most, __builtin_fabsf(x[i]));
+    }
+    most = row_max(most);
+    const int up = most > 0.0f ? 13 - (int)((__builtin_bit_cast(uint32_t, most) >> 23) & 255) + 127 : 0;
+    rows.scale[rt] = __builtin_amdgcn_ldexpf(a.scale, -up);
+#pragma unroll
+    for (int w = 0; w < S::kWords; ++w) {
+      float x[8];
+      channels_of<PARTS_Q, PARTS_P>(x, q[w]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        x[i] = __builtin_amdgcn_ldexpf(x[i], up);
+        rows.q[rt][0][w][i] = (f16)x[i];
+        if constexpr (PARTS_Q == 2) rows.q[rt][1][w][i] = (f16)(x[i] - (float)rows.q[rt][0][w][i]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < S::kTiles; ++i) sums.out[rt][i] = f32x4{0, 0, 0, 0};
+    sums.total[rt] = sums.bad[rt] = f32x4{0, 0, 0, 0};
+    sums.top[rt] = -__builtin_inff();
+  }
+  hi_most = wave_max(hi_most);
+  hi_least = -wave_max(-hi_least);
+  lo_most = wave_max(lo_most);
+  lo_least = -wave_max(-lo_least);
+  // this split's tiles: all of [lo_least, hi_most) in parts of at least a.least tiles
+  const int begin = hi_most > 0 ? lo_least / kTile : 0, end = (int)(((int64_t)hi_most + kTile - 1) / kTile);
+  const int each = max(a.least, (int)((end - begin + a.splits_div.d - 1) / a.splits_div.d));
+  const int64_t from = begin + (int64_t)split * each;
+  const int stop = (int)min((int64_t)end, from + each);
+  const char *table = a.table + b * a.tb;
+  const int64_t head = kv * a.head_stride;
+  constexpr int kStep = SHARE ? W : 1;
+  const int64_t start = from + (SHARE ? wave : 0);
+  if (start < stop) {
+    Raw<D> raw;
+    Place p[2] = {place_of<D>(a, table, head, (int)start * kTile, hi_most), place_of<D>(a, table, head, (int)start * kTile + 16, hi_most)};
+    load_raw<D>(raw, p, lanes);
+    for (int t = (int)start; t < stop; t += kStep) {
+      Raw<D> next;
+      Place np[2] = {p[0], p[1]};
+      if (t + kStep < stop) {
+        const int j = (t + kStep) * kTile;
+        np[0] = place_of<D>(a, table, head, j, hi_most);
+        np[1] = place_of<D>(a, table, head, j + 16, hi_most);
+        load_raw<D>(next, np, lanes);
+      }
+      const int j0 = t * kTile;
+      if (p[0].fine && p[1].fine && j0 >= lo_most && j0 + kTile <= hi_least)
+        one_tile<D, RT, PARTS_Q, PARTS_P, true>(sums, rows, raw, g, j0, true, true);
+      else
+        one_tile<D, RT, PARTS_Q, PARTS_P, false>(sums, rows, raw, g, j0, p[0].fine, p[1].fine);
+      raw = next;
+      p[0] = np[0], p[1] = np[1];
+    }
+  }
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+    for (int i = 0; i < S::kTiles; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (sums.bad[rt][r] > 0.0f) sums.out[rt][i][r] = __builtin_nanf("");
+  const bool whole = a.splits_div.d == 1;
+  if constexpr (SHARE) {
+    // the wavefronts' sums, relative to the largest of their maxima
+    if (g == 0) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        tops[wave][rt][n] = sums.top[rt];
+        totals[wave][rt][n] = sums.total[rt][0];
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      float top = -__builtin_inff();
+#pragma unroll
+      for (int w = 0; w < W; ++w) top = fmaxf(top, tops[w][rt][n]);
+      const float keep = top == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(sums.top[rt] - top);
+#pragma unroll
+      for (int at = 0; at < S::kTiles; at += kPart) {
+        if (rt + at > 0) __syncthreads();
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int i = 0; i < kPart; ++i) part[wave][n][4 * g + r][i] = sums.out[rt][at + i][r] * keep;
+        __syncthreads();
+        // a thread has D/16 (eight at a time) channels of a row now
+        const int rn = threadIdx.x / 16, rj = threadIdx.x % 16, row = first_row + rt * 16 + rn;
+        float v[kPart], most = -__builtin_inff(), total = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kPart; ++i) v[i] = 0.0f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) most = fmaxf(most, tops[w][rt][rn]);
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+          total += most == -__builtin_inff() ? totals[w][rt][rn] : totals[w][rt][rn] * __builtin_amdgcn_exp2f(tops[w][rt][rn] - most);
+#pragma unroll
+          for (int i = 0; i < kPart; ++i) v[i] += part[w][rn][rj][i];
+        }
+        if (row >= all_rows) continue;
+        const int channel = rj * S::kTiles + at;
+        if (whole) {
+          const int t = (int)fast_quotient((uint32_t)row, a.per_kv_div), h = kv * a.per_kv + row - t * a.per_kv;
+          const float over = total == 0.0f ? 0.0f : 1.0f / total;
+#pragma unroll
+          for (int i = 0; i < kPart; ++i) v[i] = total == 0.0f ? 0.0f : v[i] * over;
+          store_row<T, kPart>(a, a.out + b * a.ob + t * a.ot + h * a.oh, channel, v);
+          if (a.log_sum && rj == 0 && at == 0) *(float *)(a.log_sum + b * a.lb + t * a.lt + h * a.lh) = log_of(most, total);
+        } else {
+          const int64_t at_row = (int64_t)item * kRows + rt * 16 + rn;
+          float *to = a.parts + at_row * D + channel;
+#pragma unroll
+          for (int i = 0; i < kPart; i += 4) *(f32x4 *)(to + i) = f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]};
+          if (rj == 0 && at == 0) *(float2 *)(a.part_sums + at_row * 2) = float2{most, total};
+        }
+      }
+    }
+  } else {
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const int row = first_row + rt * 16 + n;
+      if (row >= all_rows) continue;
+      const float total = sums.total[rt][0], over = total == 0.0f ? 0.0f : 1.0f / total;
+      const int t = (int)fast_quotient((uint32_t)row, a.per_kv_div), h = kv * a.per_kv + row - t * a.per_kv;
+      const int64_t at_row = (int64_t)item * kRows + wave * 16 * RT + rt * 16 + n;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int channel = (4 * g + r) * S::kTiles;
+        float v[S::kTiles];
+#pragma unroll
+        for (int i = 0; i < S::kTiles; ++i) v[i] = !whole ? sums.out[rt][i][r] : total == 0.0f ? 0.0f : sums.out[rt][i][r] * over;
+        if (whole) {
+          store_row<T, S::kTiles>(a, a.out + b * a.ob + t * a.ot + h * a.oh, channel, v);
+        } else {
+#pragma unroll
+          for (int i = 0; i < S::kTiles; i += 4) *(f32x4 *)(a.parts + at_row * D + channel + i) = f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]};
+        }
+      }
+      if (g == 0) {
+        if (whole && a.log_sum) *(float *)(a.log_sum + b * a.lb + t * a.lt + h * a.lh) = log_of(sums.top[rt], total);
+        if (!whole) *(float2 *)(a.part_sums + at_row * 2) = float2{sums.top[rt], total};
+      }
+    }
+  }
+}
+
+// The parts of a row joined: a wavefront has a row, its lanes first the parts' sums, then the channels.  Parts that saw nothing have a sum of zero
+// and are not read.
+template <int D> __global__ __launch_bounds__(kBlock) void attention_join_kernel(const AttentionArgs a, uint32_t rows, int unit_rows) {
+  constexpr int C = D / kWave;
+  const int lane = threadIdx.x % kWave;
+  for (uint32_t r = blockIdx.x * (kBlock / kWave) + threadIdx.x / kWave; r < rows; r += gridDim.x * (kBlock / kWave)) {
+    // rows: query heads fastest, then queries, sequences
+    const int all_rows = a.queries * a.per_kv, splits = (int)a.splits_div.d;
+    const int bh = (int)(r / (uint32_t)all_rows), row = (int)(r % (uint32_t)all_rows), b = bh / (int)a.kv_div.d, kv = bh % (int)a.kv_div.d;
+    const int64_t unit = (int64_t)bh * a.blocks_div.d + row / unit_rows, place = row % unit_rows;
+    float2 ml = {-__builtin_inff(), 0.0f};
+    if (lane < splits) ml = *(const float2 *)(a.part_sums + ((unit * splits + lane) * unit_rows + place) * 2);
+    float top = ml.x;
+    for (int m = 1; m < kWave; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
+    const float w = ml.y == 0.0f ? 0.0f : top == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(ml.x - top);
+    float total = ml.y == 0.0f ? 0.0f : ml.y * w;
+    for (int m = 1; m < kWave; m <<= 1) total += __shfl_xor(total, m);
+    float v[C];
+#pragma unroll
+    for (int i = 0; i < C; ++i) v[i] = 0.0f;
+    for (uint64_t left = __builtin_amdgcn_ballot_w64(ml.y != 0.0f); left; left &= left - 1) {
+      const int s = __builtin_ctzll(left);
+      const float ws = __shfl(w, s);
+      const float *from = a.parts + ((unit * splits + s) * unit_rows + place) * D + lane * C;
+#pragma unroll
+      for (int i = 0; i < C; ++i) v[i] += ws * from[i];
+    }
+    const int t = row / a.per_kv, h = kv * a.per_kv + row % a.per_kv;
+    char *to = a.out + b * a.ob + t * a.ot + h * a.oh;
+#pragma unroll
+    for (int i = 0; i < C; ++i) store_from_float(to + (lane * C + i) * a.oe, a.type, total == 0.0f ? 0.0f : v[i] / total);
+    if (a.log_sum && lane == 0) *(float *)(a.log_sum + b * a.lb + t * a.lt + h * a.lh) = log_of(top, total);
+  }
+}
+
+// ---------------------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------------------
+
+// How a call's rows and tokens go to workgroups; a function of the shapes alone.
+struct Launch {
+  int row_tiles;        // of a wavefront
+  bool share;           // whether a workgroup's wavefronts have the same rows
+  int64_t unit_rows, blocks, units, splits, items;
+};
+
+Launch launch_of(int64_t batch, int64_t queries, int64_t heads, int64_t kv, int64_t channels, int64_t capacity) {
+  Launch l;
+  const int64_t rows = queries * (heads / kv);
+  l.row_tiles = rows <= 16 || channels == 256 ? 1 : 2;
+  l.share = rows <= 64;
+  l.unit_rows = 16 * l.row_tiles * (l.share ? 1 : kBlock / kWave);
+  l.blocks = (rows + l.unit_rows - 1) / l.unit_rows;
+  l.units = batch * kv * l.blocks;
+  const int64_t tiles = (capacity + kTile - 1) / kTile, most = std::max<int64_t>(1, tiles / kLeastTiles);
+  l.splits = std::min<int64_t>({most, kMaxSplits, std::max<int64_t>(1, (kWorkgroups + l.units - 1) / std::max<int64_t>(l.units, 1))});
+  l.items = l.units * l.splits;
+  return l;
 }
 
 int done(hipError_t e) {
@@ -136,13 +682,54 @@ int check_shapes(const ocn_tensor *q, const ocn_tensor *cache, const ocn_tensor 
   if (table->size[0] != q->size[0]) return OCN_ERR_SHAPE;
   if (q->size[2] > 0 && (kv == 0 || q->size[2] % kv != 0)) return OCN_ERR_SHAPE;
   const int64_t most = (int64_t)1 << 31;
-  if (table->size[1] > most / *page) return OCN_ERR_SHAPE;        // (tokens of a sequence)
+  if (table->size[1] > (most - 64) / *page) return OCN_ERR_SHAPE;        // (tokens of a sequence)
   int64_t units = 1;
   for (int d = 0; d < 3; ++d) {
-    if (q->size[d] != 0 && units > (most - 1) / q->size[d]) return OCN_ERR_SHAPE;
+    if (q->size[d] != 0 && units > (most >> 6) / q->size[d]) return OCN_ERR_SHAPE;
     units *= q->size[d];
   }
   return OCN_OK;
+}
+
+bool whole_rows(const ocn_tensor *t) {
+  if (t->stride[3] != head_type_size(t->dtype) || ((intptr_t)t->base + t->offset) % 16 != 0) return false;
+  for (int d = 0; d < 3; ++d)
+    if (t->size[d] > 1 && t->stride[d] % 16 != 0) return false;
+  return true;
+}
+
+template <int D> void launch_attention(const AttentionArgs &a, const Launch &l, uint32_t grid, hipStream_t stream) {
+#define OCN_ATTENTION(RT, SHARE)                                                                                                       \
+  do {                                                                                                                                 \
+    if (a.type == OCN_BFLOAT16) hipLaunchKernelGGL((attention_kernel<D, RT, 1, 1, SHARE>), dim3(grid), dim3(kBlock), 0, stream, a);     \
+    else if (a.type == OCN_HALF) hipLaunchKernelGGL((attention_kernel<D, RT, 1, 2, SHARE>), dim3(grid), dim3(kBlock), 0, stream, a);    \
+    else hipLaunchKernelGGL((attention_kernel<D, RT, 2, 2, SHARE>), dim3(grid), dim3(kBlock), 0, stream, a);                            \
+  } while (0)
+  if constexpr (D < 256) {
+    if (l.row_tiles == 2) {
+      if (l.share) OCN_ATTENTION(2, true);
+      else OCN_ATTENTION(2, false);
+    }
+  }
+  if (l.row_tiles == 1) {
+    if (l.share) OCN_ATTENTION(1, true);
+    else if constexpr (D == 256) OCN_ATTENTION(1, false);
+  }
+#undef OCN_ATTENTION
+}
+
+template <int D> int run_attention(AttentionArgs &a, const Launch &l, uint32_t rows, hipStream_t stream) {
+  // (no loop over items in the kernel: what a loop's first instructions share would be kept in registers that the tiles need)
+  for (int64_t at = 0; at < l.items; at += max_launch_blocks()) {
+    a.first_item = (uint32_t)at;
+    launch_attention<D>(a, l, (uint32_t)std::min(l.items - at, max_launch_blocks()), stream);
+    const int rc = done(hipGetLastError());
+    if (rc != OCN_OK) return rc;
+  }
+  if (l.splits == 1) return OCN_OK;
+  const uint32_t joins = (uint32_t)std::min<int64_t>((rows + kBlock / kWave - 1) / (kBlock / kWave), max_launch_blocks());
+  hipLaunchKernelGGL((attention_join_kernel<D>), dim3(joins), dim3(kBlock), 0, stream, a, rows, (int)l.unit_rows);
+  return done(hipGetLastError());
 }
 
 }  // namespace
@@ -154,8 +741,9 @@ extern "C" {
 
 size_t ocn_cache_attention_workspace_bytes(const ocn_tensor *q, const ocn_tensor *cache, const ocn_tensor *table) {
   int64_t page;
-  if (check_shapes(q, cache, table, &page) != OCN_OK) return 0;
-  return 0;
+  if (check_shapes(q, cache, table, &page) != OCN_OK || q->size[0] * q->size[1] * q->size[2] == 0) return 0;
+  const Launch l = launch_of(q->size[0], q->size[1], q->size[2], cache->size[1], q->size[3], table->size[1] * page);
+  return l.splits == 1 ? 0 : (size_t)l.items * l.unit_rows * (q->size[3] + 2) * sizeof(float);
 }
 
 int ocn_cache_attention(const ocn_tensor *q, const ocn_tensor *cache, const ocn_tensor *table, const ocn_tensor *visible,
@@ -198,24 +786,39 @@ int ocn_cache_attention(const ocn_tensor *q, const ocn_tensor *cache, const ocn_
   a.page_stride = cache->stride[0];
   a.head_stride = cache->stride[1];
   a.pages = cache->size[0];
-  a.columns = table->size[1];
   a.window = window;
-  a.batch = (int32_t)q->size[0], a.queries = (int32_t)q->size[1], a.heads = (int32_t)q->size[2];
-  const int64_t units = (int64_t)a.batch * a.queries * a.heads, d = q->size[3];
-  if (units == 0) return OCN_OK;
-  a.per_kv = a.heads / (int32_t)cache->size[1];
+  const int64_t rows = q->size[0] * q->size[1] * q->size[2], d = q->size[3], kv = cache->size[1];
+  if (rows == 0) return OCN_OK;
+  const int64_t capacity = table->size[1] * page;
+  const Launch l = launch_of(q->size[0], q->size[1], q->size[2], kv, d, capacity);
+  if (l.items >= (int64_t)1 << 31) return OCN_ERR_SHAPE;
+  if (l.splits > 1) {
+    const size_t parts = (size_t)l.items * l.unit_rows * d;
+    if (!workspace || workspace_bytes < (parts + (size_t)l.items * l.unit_rows * 2) * sizeof(float)) return OCN_ERR_WORKSPACE;
+    if ((uintptr_t)workspace % 256 != 0) return OCN_ERR_ALIGN;
+    a.parts = (float *)workspace;
+    a.part_sums = a.parts + parts;
+  }
+  a.queries = (int32_t)q->size[1];
+  a.per_kv = (int32_t)(q->size[2] / kv);
+  a.capacity = a.pages > 0 ? (int32_t)capacity : 0;
+  a.least = (int32_t)kLeastTiles;
+  a.whole_q = whole_rows(q);
+  a.whole_out = whole_rows(out);
   a.page = (int32_t)page;
   a.page_div = make_fastdiv((uint32_t)page);
+  a.per_kv_div = make_fastdiv((uint32_t)a.per_kv);
+  a.splits_div = make_fastdiv((uint32_t)l.splits);
+  a.blocks_div = make_fastdiv((uint32_t)l.blocks);
+  a.kv_div = make_fastdiv((uint32_t)kv);
   a.type = q->dtype;
   a.table_wide = table->dtype == OCN_INT64;
   a.seen_wide = visible->dtype == OCN_INT64;
   a.scale = (float)(scale * 1.4426950408889634074);
-  const uint32_t grid = (uint32_t)std::min<int64_t>(units, max_launch_blocks());
   const hipStream_t s = (hipStream_t)stream;
-  if (d == 64) hipLaunchKernelGGL((attention_kernel<64>), dim3(grid), dim3(kBlock), 0, s, a);
-  else if (d == 128) hipLaunchKernelGGL((attention_kernel<128>), dim3(grid), dim3(kBlock), 0, s, a);
-  else hipLaunchKernelGGL((attention_kernel<256>), dim3(grid), dim3(kBlock), 0, s, a);
-  return done(hipGetLastError());
+  if (d == 64) return run_attention<64>(a, l, (uint32_t)rows, s);
+  if (d == 128) return run_attention<128>(a, l, (uint32_t)rows, s);
+  return run_attention<256>(a, l, (uint32_t)rows, s);
 }
 
 }  // extern "C"
