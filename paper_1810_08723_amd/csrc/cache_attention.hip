@@ -30,9 +30,13 @@ struct AttentionArgs {
   float scale;                                 // of the scores, times log2(e)
 };
 
-constexpr int64_t kLeastTiles = 8;             // of a split: two for each wavefront
+#ifndef OCN_LEAST
+#define OCN_LEAST 8
+#define OCN_WG 1024
+#endif
+constexpr int64_t kLeastTiles = OCN_LEAST;             // of a split: two for each wavefront
 constexpr int64_t kMaxSplits = kWave;          // a lane each when they are joined
-constexpr int64_t kWorkgroups = 1024;          // worth launching: four to a CU
+constexpr int64_t kWorkgroups = OCN_WG;          // worth launching: four to a CU
 
 // ---------------------------------------------------------------------------------------
 // The kernel.  Query heads of one head of the cache, of one or more queries, are the rows of its tiles: 16 a tile.  For 32 tokens at a
@@ -59,12 +63,13 @@ constexpr int64_t kWorkgroups = 1024;          // worth launching: four to a CU
 // ---------------------------------------------------------------------------------------
 
 constexpr float kWeightBits = 11.0f, kRaise = 4.0f;
-template <int PARTS_P> struct Floor {
-  static constexpr int kBits = PARTS_P == 1 ? -14 : -4;       // log2 of the smallest weight that is taken as it is
+template <int PARTS_Q> struct Floor {     // (float results keep 2^-20 of a small weight, the others half of their own step)
+  static constexpr int kBits = PARTS_Q == 1 ? -14 : -4;       // log2 of the smallest weight that is taken as it is
   static constexpr int kStep = 14 - kBits;                    // what smaller ones are multiplied by, and again: below 2^14 then
-  static constexpr float kLeast = PARTS_P == 1 ? 0x1p-14f : 0x1p-4f, kUp = PARTS_P == 1 ? 0x1p28f : 0x1p18f, kDown = 1.0f / kUp;
+  static constexpr float kLeast = PARTS_Q == 1 ? 0x1p-14f : 0x1p-4f, kUp = PARTS_Q == 1 ? 0x1p28f : 0x1p18f, kDown = 1.0f / kUp;
 };
 constexpr int kTile = 32;            // tokens
+constexpr int kAhead = 1;             // tiles on their way (two: 67.99 for 66.03 us of two contexts of 100 k and 131 k tokens)
 
 template <int D> struct Shape {
   static constexpr int kWords = D / 32;                   // of a token's codes in a lane; steps of the scores; groups
@@ -76,48 +81,59 @@ template <int D> struct Shape {
 // what a lane holds of a tile's codes and scales, as they come from memory
 template <int D> struct Raw {
   uint32_t k[2][Shape<D>::kWords], v[2][Shape<D>::kWords];
-  f16 k_scale[2][Shape<D>::kChunks];
-  u32x2 v_scale[2];
+  uint32_t k_scale[2][Shape<D>::kChunks];   // (a half in a word of its own: an array of halves would go to memory)
+  uint32_t v_scale[2][2];
 };
 
-// a half tile's page: the address of its tokens' codes and scales; the same in all lanes
+// A half tile's entry in the table, as loaded, and its page: the address of its tokens' codes and scales.  The same in all lanes.
+struct Entry {
+  uint32_t lo, hi;
+  int at;
+  bool in;
+};
+typedef const __attribute__((address_space(1))) char *Global;
 struct Place {
-  const char *codes, *scales;
+  Global codes, scales;
   bool fine;
 };
 
-template <int N> __device__ __forceinline__ void load_words(uint32_t *to, const char *from) {
+template <int N> __device__ __forceinline__ void load_words(uint32_t *to, Global from) {
   if constexpr (N % 4 == 0) {
 #pragma unroll
     for (int i = 0; i < N; i += 4) {
-      const u32x4 w = *(const u32x4 *)(from + 4 * i);
+      const u32x4 w = *(const __attribute__((address_space(1))) u32x4 *)(from + 4 * i);
       to[i] = w.x, to[i + 1] = w.y, to[i + 2] = w.z, to[i + 3] = w.w;
     }
   } else {
-    const u32x2 w = *(const u32x2 *)from;
+    const u32x2 w = *(const __attribute__((address_space(1))) u32x2 *)from;
     to[0] = w.x, to[1] = w.y;
   }
 }
 
-// the page of 16 tokens from j on (a multiple of 16); past the sequence's end and in pages outside the cache it is page 0, which may be read
-template <int D> __device__ __forceinline__ Place place_of(const AttentionArgs &a, const char *row, int64_t head, int j, int end) {
+// the entry of 16 tokens from j on (a multiple of 16); past the sequence's end some other entry, which is not used
+__device__ __forceinline__ Entry entry_of(const AttentionArgs &a, const char *row, int64_t j, int end) {
+  typedef const __attribute__((address_space(4))) uint32_t *Word;
+  Entry e;
+  e.in = j < end;
+  const uint32_t k = e.in ? (uint32_t)j : 0, column = fast_quotient(k, a.page_div);
+  e.at = (int)(k - column * (uint32_t)a.page);
+  const char *entry = row + column * a.tc;
+  e.lo = *(Word)(uintptr_t)entry;
+  e.hi = *(Word)(uintptr_t)(entry + (a.table_wide ? 4 : 0));
+  return e;
+}
+// tokens past the end and in pages outside the cache are read from page 0 and not seen
+template <int D> __device__ __forceinline__ Place place_of(const AttentionArgs &a, int64_t head, const Entry &e) {
+  const int64_t page = a.table_wide ? (int64_t)((uint64_t)e.hi << 32 | e.lo) : (int64_t)(int32_t)e.lo;
   Place p;
-  p.fine = j < end;
-  int64_t page = 0;
-  int at = 0;
-  if (p.fine) {
-    const int column = (int)fast_quotient((uint32_t)j, a.page_div);
-    at = j - column * a.page;
-    typedef const __attribute__((address_space(4))) int64_t *Wide;
-    typedef const __attribute__((address_space(4))) int32_t *Narrow;
-    const char *entry = row + column * a.tc;
-    page = a.table_wide ? *(Wide)(uintptr_t)entry : (int64_t)*(Narrow)(uintptr_t)entry;
-    p.fine = page >= 0 && page < a.pages;
-    if (!p.fine) page = 0, at = 0;
-  }
-  const char *block = a.cache + page * a.page_stride + head;
-  p.codes = block + at * (D / 2);
-  p.scales = block + at * 2;
+  p.fine = e.in && page >= 0 && page < a.pages;
+  const int at = p.fine ? e.at : 0;
+  // (said to be the same in all lanes, so that loads take it as a scalar with a lane's 32-bit offset)
+  const uint64_t block = (uint64_t)a.cache + (p.fine ? page : 0) * a.page_stride + head;
+  const uint64_t same = (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)block) |
+                        (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(block >> 32)) << 32;
+  p.codes = (Global)same + at * (D / 2);
+  p.scales = (Global)same + at * 2;
   return p;
 }
 
@@ -134,18 +150,15 @@ template <int D> __device__ __forceinline__ LaneOffsets lane_offsets(const Atten
   return o;
 }
 
-template <int D> __device__ __forceinline__ void load_raw(Raw<D> &r, const Place *p, const LaneOffsets &o) {
+template <int D> __device__ __forceinline__ void load_half(Raw<D> &r, int x, const Place &p, const LaneOffsets &o) {
   typedef Shape<D> S;
 #pragma unroll
-  for (int x = 0; x < 2; ++x) {
-#pragma unroll
-    for (int h = 0; h < S::kChunks; ++h) {
-      load_words<S::kRun>(&r.k[x][h * S::kRun], p[x].codes + o.k + h * 16 * S::kRun);
-      r.k_scale[x][h] = *(const f16 *)(p[x].scales + o.k_scale + h * o.k_scale_step);
-    }
-    load_words<S::kWords>(r.v[x], p[x].codes + o.v);
-    r.v_scale[x] = *(const u32x2 *)(p[x].scales + o.v_scale);
+  for (int h = 0; h < S::kChunks; ++h) {
+    load_words<S::kRun>(&r.k[x][h * S::kRun], p.codes + (o.k + h * 16 * S::kRun));
+    r.k_scale[x][h] = *(const __attribute__((address_space(1))) uint16_t *)(p.scales + (o.k_scale + h * o.k_scale_step));
   }
+  load_words<S::kWords>(r.v[x], p.codes + o.v);
+  load_words<2>(r.v_scale[x], p.scales + o.v_scale);
 }
 
 template <int BYTE> __device__ __forceinline__ f16x2 two_codes(uint32_t w) { return __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 2.0f, BYTE); }
@@ -159,35 +172,49 @@ union Frag {
 // bits of a where the mask has ones, of b elsewhere
 __device__ __forceinline__ uint32_t select_bits(uint32_t mask, uint32_t a, uint32_t b) { return (a & mask) | (b & ~mask); }
 
-// pair `i` of out^T tiles' operands from the codes of tokens 2 i and 2 i + 1 of a lane's four
-template <int D> __device__ __forceinline__ void pair_of_tokens(const uint32_t *v, int i, f16x2 scale, f16x2 *out) {
+// The codes of a lane's tokens 2 i and 2 i + 1 side by side: byte k of even[q] (odd[q]) has both tokens' codes of channel 2 k (2 k + 1) of word q
+template <int D> struct Twins { uint32_t even[D / 128 ? D / 128 : 1], odd[D / 128 ? D / 128 : 1]; };
+template <int D> __device__ __forceinline__ Twins<D> twins_of(const uint32_t *v, int i) {
   constexpr uint32_t low = 0x0f0f0f0fu;
+  Twins<D> w;
   if constexpr (D == 64) {
-    const uint32_t w = v[i], even = select_bits(low, w, w >> 12), odd = select_bits(low, w >> 4, w >> 16);
-    out[0] = two_codes<0>(even) * scale, out[1] = two_codes<0>(odd) * scale;
-    out[2] = two_codes<1>(even) * scale, out[3] = two_codes<1>(odd) * scale;
+    w.even[0] = select_bits(low, v[i], v[i] >> 12);
+    w.odd[0] = select_bits(low, v[i] >> 4, v[i] >> 16);
   } else {
 #pragma unroll
     for (int q = 0; q < D / 128; ++q) {
       const uint32_t a = v[2 * i * (D / 128) + q], b = v[(2 * i + 1) * (D / 128) + q];
-      const uint32_t even = select_bits(low, a, b << 4), odd = select_bits(low, a >> 4, b);
-      f16x2 *o = out + 8 * q;
-      o[0] = two_codes<0>(even) * scale, o[1] = two_codes<0>(odd) * scale;
-      o[2] = two_codes<1>(even) * scale, o[3] = two_codes<1>(odd) * scale;
-      o[4] = two_codes<2>(even) * scale, o[5] = two_codes<2>(odd) * scale;
-      o[6] = two_codes<3>(even) * scale, o[7] = two_codes<3>(odd) * scale;
+      w.even[q] = select_bits(low, a, b << 4);
+      w.odd[q] = select_bits(low, a >> 4, b);
     }
+  }
+  return w;
+}
+// channel t of a lane's, of both tokens
+template <int D> __device__ __forceinline__ f16x2 twin_codes(const Twins<D> &w, int t) {
+  const uint32_t x = t % 2 ? w.odd[t / 8] : w.even[t / 8];
+  switch (t % 8 / 2) {       // (t is known when this is compiled)
+    case 0: return two_codes<0>(x);
+    case 1: return two_codes<1>(x);
+    case 2: return two_codes<2>(x);
+    default: return two_codes<3>(x);
   }
 }
 
+// (the compiler's own maximum first quiets NaNs that it cannot rule out: two instructions more)
+__device__ __forceinline__ float larger(float a, float b) {
+  float c;
+  asm("v_max_f32 %0, %1, %2" : "=v"(c) : "v"(a), "v"(b));
+  return c;
+}
 // the largest of the four lanes that hold a row
 __device__ __forceinline__ float row_max(float x) {
   const auto a = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
   const uint32_t a0 = a[0], a1 = a[1];
-  x = fmaxf(__builtin_bit_cast(float, a0), __builtin_bit_cast(float, a1));
+  x = larger(__builtin_bit_cast(float, a0), __builtin_bit_cast(float, a1));
   const auto b = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
   const uint32_t b0 = b[0], b1 = b[1];
-  return fmaxf(__builtin_bit_cast(float, b0), __builtin_bit_cast(float, b1));
+  return larger(__builtin_bit_cast(float, b0), __builtin_bit_cast(float, b1));
 }
 
 __device__ __forceinline__ int wave_max(int x) {
@@ -211,21 +238,23 @@ template <int D, int RT, int PARTS_Q> struct Rows {
   int lo[RT], hi[RT];                // tokens that a row sees
 };
 
-template <int D, int RT, int PARTS_Q, int PARTS_P, bool WHOLE>
-__device__ __forceinline__ void one_tile(Sums<D, RT> &s, const Rows<D, RT, PARTS_Q> &rows, const Raw<D> &raw, int g, int j0, bool fine0, bool fine1) {
+// whole: every row sees every token of the tile
+template <int D, int RT, int PARTS_Q, int PARTS_P>
+__device__ __forceinline__ void one_tile(Sums<D, RT> &s, const Rows<D, RT, PARTS_Q> &rows, Raw<D> &raw, int g, int j0, bool whole, bool fine0, bool fine1) {
   typedef Shape<D> S;
+  typedef Floor<PARTS_Q> F;
+  const f16x8 ones = {1, 1, 1, 1, 1, 1, 1, 1};
   f32x4 score[RT][2];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
     for (int x = 0; x < 2; ++x) score[rt][x] = f32x4{0, 0, 0, 0};
 #pragma unroll
-  for (int x = 0; x < 2; ++x)
+  for (int w = 0; w < S::kWords; ++w)
 #pragma unroll
-    for (int w = 0; w < S::kWords; ++w) {
-      const uint32_t codes = raw.k[x][w];
-      const f16 sc = raw.k_scale[x][w / S::kRun];
-      const f16x2 scale = {sc, sc};
+    for (int x = 0; x < 2; ++x) {
+      const uint32_t codes = raw.k[x][w], both = raw.k_scale[x][w / S::kRun];
+      const f16x2 one = __builtin_bit_cast(f16x2, both), scale = {one.x, one.x};
       Frag k;
       k.p[0] = two_codes<0>(codes) * scale, k.p[1] = two_codes<1>(codes) * scale;
       k.p[2] = two_codes<2>(codes) * scale, k.p[3] = two_codes<3>(codes) * scale;
@@ -234,50 +263,52 @@ __device__ __forceinline__ void one_tile(Sums<D, RT> &s, const Rows<D, RT, PARTS
 #pragma unroll
         for (int part = 0; part < PARTS_Q; ++part) score[rt][x] = product(k.v, rows.q[rt][part][w], score[rt][x]);
     }
-  f16x2 v_scale[2][2];
-  // Weights of zero do not make a token's NaN go away: in a tile that some row does not see whole, a scale that is NaN (or none that
-  // appending writes: places that were never written) counts as zero, and rows that do see its token are marked by one more product.
-  Frag nan_of;         // 1 for such tokens
-#pragma unroll
-  for (int x = 0; x < 2; ++x)
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const uint32_t two = raw.v_scale[x][i];     // (an element of a vector has no address to cast from)
-      f16x2 sc = __builtin_bit_cast(f16x2, two);
-      if constexpr (!WHOLE) {
-        f16x2 bad = {0, 0};
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          if (!(sc[e] <= (f16)5456.0f && sc[e] >= (f16)-5456.0f)) { sc[e] = (f16)0.0f; bad[e] = (f16)1.0f; }
-        }
-        nan_of.p[2 * x + i] = bad;
-      }
-      v_scale[x][i] = sc;
-    }
-  typedef Floor<PARTS_P> F;
-  const f16x8 ones = {1, 1, 1, 1, 1, 1, 1, 1};
-  Frag p[RT][PARTS_P];
-  float small[RT][8];
-  bool apart = false;          // whether some weights are below the floor
+  float least[RT];       // (unseen places may make it too small, and the tile takes longer)
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    float v[8], most = -__builtin_inff(), least = __builtin_inff();
-    Frag sees;
+    least[rt] = score[rt][0][0];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      v[i] = score[rt][i / 4][i % 4] * rows.scale[rt];
-      if constexpr (!WHOLE) {
+    for (int i = 1; i < 8; ++i) least[rt] = fminf(least[rt], score[rt][i / 4][i % 4]);
+  }
+  uint32_t sees[RT];     // which of its eight tokens a lane's row sees
+  if (!whole) {
+    // Weights of zero do not make a token's NaN go away: in a tile that some row does not see whole, a scale that is NaN (or none that
+    // appending writes: places that were never written) counts as zero, and rows that do see its token are marked by one more product.
+    Frag nan_of;         // 1 for such tokens
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t two = raw.v_scale[i / 2][i % 2];
+      f16x2 sc = __builtin_bit_cast(f16x2, two), bad = {0, 0};
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        if (!(sc[e] <= (f16)5456.0f && sc[e] >= (f16)-5456.0f)) { sc[e] = (f16)0.0f; bad[e] = (f16)1.0f; }
+      raw.v_scale[i / 2][i % 2] = __builtin_bit_cast(uint32_t, sc);
+      nan_of.p[i] = bad;
+    }
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      Frag seen;
+      sees[rt] = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
         const int j = j0 + 16 * (i / 4) + 4 * g + i % 4;
         const bool in = j >= rows.lo[rt] && j < rows.hi[rt] && (i < 4 ? fine0 : fine1);
-        sees.v[i] = in ? (f16)1.0f : (f16)0.0f;
-        least = fminf(least, in ? v[i] : __builtin_inff());
-        if (!in) v[i] = -__builtin_inff();
-      } else {
-        least = fminf(least, v[i]);
+        seen.v[i] = in ? (f16)1.0f : (f16)0.0f;
+        sees[rt] |= in ? 1u << i : 0u;
+        if (!in) score[rt][i / 4][i % 4] = -__builtin_inff();
       }
-      most = fmaxf(most, v[i]);
+      s.bad[rt] = product(nan_of.v, seen.v, s.bad[rt]);
     }
-    most = row_max(most);
+  }
+  Frag p[RT][PARTS_P];
+  float weight[RT][8];
+  bool apart = false;    // whether some weights are below the floor
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    float most = score[rt][0][0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) most = fmaxf(most, score[rt][i / 4][i % 4]);
+    most = row_max(most) * rows.scale[rt];
     if (__builtin_amdgcn_ballot_w64(most > s.top[rt] + kRaise)) {
       const float now = fmaxf(s.top[rt], most), keep = now == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(s.top[rt] - now);
       s.top[rt] = now;
@@ -285,74 +316,90 @@ __device__ __forceinline__ void one_tile(Sums<D, RT> &s, const Rows<D, RT, PARTS
       for (int i = 0; i < S::kTiles; ++i) s.out[rt][i] *= keep;
       s.total[rt] *= keep;
     }
-    const float shift = (s.top[rt] == -__builtin_inff() ? 0.0f : s.top[rt]) - kWeightBits;
-    const bool low = __builtin_amdgcn_ballot_w64(least < shift + F::kBits) != 0;
-    apart |= low;
+    const float shift = kWeightBits - (s.top[rt] == -__builtin_inff() ? 0.0f : s.top[rt]);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float w = __builtin_amdgcn_exp2f(v[i] - shift);
-      small[rt][i] = 0.0f;
-      if (low) {
-        small[rt][i] = w < F::kLeast ? w : 0.0f;
-        w = w < F::kLeast ? 0.0f : w;
-      }
-      p[rt][0].v[i] = (f16)w;
-      if constexpr (PARTS_P == 2) p[rt][1].v[i] = (f16)(w - (float)p[rt][0].v[i]);
+    for (int i = 0; i < 8; ++i) weight[rt][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(score[rt][i / 4][i % 4], rows.scale[rt], shift));
+    if (!whole) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) weight[rt][i] = sees[rt] >> i & 1 ? weight[rt][i] : 0.0f;
     }
-#pragma unroll
-    for (int part = 0; part < PARTS_P; ++part) s.total[rt] = product(ones, p[rt][part].v, s.total[rt]);
-    if constexpr (!WHOLE) s.bad[rt] = product(nan_of.v, sees.v, s.bad[rt]);
+    if (__builtin_amdgcn_ballot_w64(__builtin_fmaf(least[rt], rows.scale[rt], shift) < F::kBits)) apart = true;
   }
-  f16x2 pairs[2][2][S::kTiles];
+  Twins<D> twins[4];
+  f16x2 scale[4];
 #pragma unroll
-  for (int x = 0; x < 2; ++x)
-#pragma unroll
-    for (int i = 0; i < 2; ++i) pair_of_tokens<D>(raw.v[x], i, v_scale[x][i], pairs[x][i]);
-#pragma unroll
-  for (int t = 0; t < S::kTiles; ++t) {
-    Frag f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) f.p[i] = pairs[i / 2][i % 2][t];
+  for (int i = 0; i < 4; ++i) {
+    twins[i] = twins_of<D>(raw.v[i / 2], i % 2);
+    const uint32_t two = raw.v_scale[i / 2][i % 2];
+    scale[i] = __builtin_bit_cast(f16x2, two);
+  }
+  if (apart) {
+    float small[RT][8], down = F::kDown;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-      for (int part = 0; part < PARTS_P; ++part) s.out[rt][t] = product(f.v, p[rt][part].v, s.out[rt][t]);
-  }
-  if (apart) {
-    float down = F::kDown;
+      for (int i = 0; i < 8; ++i) {
+        small[rt][i] = weight[rt][i] < F::kLeast ? weight[rt][i] : 0.0f;
+        weight[rt][i] = weight[rt][i] < F::kLeast ? 0.0f : weight[rt][i];
+      }
 #pragma nounroll
     for (int step = 0; step < (126 + F::kStep - 1) / F::kStep; ++step, down *= F::kDown) {
-      bool left = false;
+      bool left = false, any = false;
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const float x = small[rt][i] * F::kUp, w = x < F::kLeast ? 0.0f : x;
           small[rt][i] = x < F::kLeast ? x : 0.0f;
+          any |= w > 0.0f;
           left |= small[rt][i] > 0.0f;
           p[rt][0].v[i] = (f16)w;
           if constexpr (PARTS_P == 2) p[rt][1].v[i] = (f16)(w - (float)p[rt][0].v[i]);
         }
-        f32x4 add = {0, 0, 0, 0};
-#pragma unroll
-        for (int part = 0; part < PARTS_P; ++part) add = product(ones, p[rt][part].v, add);
-        s.total[rt] += add * down;
       }
+      if (__builtin_amdgcn_ballot_w64(any)) {
 #pragma unroll
-      for (int t = 0; t < S::kTiles; ++t) {
-        Frag f;
+        for (int t = 0; t < S::kTiles; ++t) {
+          Frag f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) f.p[i] = pairs[i / 2][i % 2][t];
+          for (int i = 0; i < 4; ++i) f.p[i] = twin_codes<D>(twins[i], t) * scale[i];
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-          f32x4 add = {0, 0, 0, 0};
+          for (int rt = 0; rt < RT; ++rt) {
+            f32x4 add = {0, 0, 0, 0};
 #pragma unroll
-          for (int part = 0; part < PARTS_P; ++part) add = product(f.v, p[rt][part].v, add);
-          s.out[rt][t] += add * down;
+            for (int part = 0; part < PARTS_P; ++part) add = product(f.v, p[rt][part].v, add);
+            s.out[rt][t] += add * down;
+            if (t == 0) {
+              add = f32x4{0, 0, 0, 0};
+#pragma unroll
+              for (int part = 0; part < PARTS_P; ++part) add = product(ones, p[rt][part].v, add);
+              s.total[rt] += add * down;
+            }
+          }
         }
       }
       if (!__builtin_amdgcn_ballot_w64(left)) break;
     }
+  }
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      p[rt][0].v[i] = (f16)weight[rt][i];
+      if constexpr (PARTS_P == 2) p[rt][1].v[i] = (f16)(weight[rt][i] - (float)p[rt][0].v[i]);
+    }
+#pragma unroll
+    for (int part = 0; part < PARTS_P; ++part) s.total[rt] = product(ones, p[rt][part].v, s.total[rt]);
+  }
+#pragma unroll
+  for (int t = 0; t < S::kTiles; ++t) {
+    Frag f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f.p[i] = twin_codes<D>(twins[i], t) * scale[i];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+      for (int part = 0; part < PARTS_P; ++part) s.out[rt][t] = product(f.v, p[rt][part].v, s.out[rt][t]);
   }
 }
 
@@ -385,7 +432,7 @@ template <int PARTS_Q> __device__ __forceinline__ void load_channels(uint32_t *t
   if (!any) return;
   if (a.whole_q) {
 #pragma unroll
-    for (int i = 0; i < N; i += 4) load_words<4>(to + i, row + channel * (2 * PARTS_Q) + 4 * i);
+    for (int i = 0; i < N; i += 4) load_words<4>(to + i, (Global)(uint64_t)(row + channel * (2 * PARTS_Q) + 4 * i));
   } else {
     int64_t step = a.qe;
     asm volatile("" : "+s"(step)::"memory");   // (here and now: hoisted out of all loops, the addresses took more registers than the tiles)
@@ -459,14 +506,16 @@ __global__ __launch_bounds__(kBlock, D * RT <= 128 ? 2 : 1) void attention_kerne
     }
     most = row_max(most);
     const int up = most > 0.0f ? 13 - (int)((__builtin_bit_cast(uint32_t, most) >> 23) & 255) + 127 : 0;
-    rows.scale[rt] = __builtin_amdgcn_ldexpf(a.scale, -up);
+    // (not zero, so that minus infinity stays what it is; a negative scale turns the queries)
+    rows.scale[rt] = fmaxf(__builtin_amdgcn_ldexpf(__builtin_fabsf(a.scale), -up), 0x1p-126f);
+    const float sign = a.scale < 0.0f ? -1.0f : 1.0f;
 #pragma unroll
     for (int w = 0; w < S::kWords; ++w) {
       float x[8];
       channels_of<PARTS_Q, PARTS_P>(x, q[w]);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        x[i] = __builtin_amdgcn_ldexpf(x[i], up);
+        x[i] = __builtin_amdgcn_ldexpf(x[i], up) * sign;
         rows.q[rt][0][w][i] = (f16)x[i];
         if constexpr (PARTS_Q == 2) rows.q[rt][1][w][i] = (f16)(x[i] - (float)rows.q[rt][0][w][i]);
       }
@@ -490,25 +539,40 @@ __global__ __launch_bounds__(kBlock, D * RT <= 128 ? 2 : 1) void attention_kerne
   constexpr int kStep = SHARE ? W : 1;
   const int64_t start = from + (SHARE ? wave : 0);
   if (start < stop) {
-    Raw<D> raw;
-    Place p[2] = {place_of<D>(a, table, head, (int)start * kTile, hi_most), place_of<D>(a, table, head, (int)start * kTile + 16, hi_most)};
-    load_raw<D>(raw, p, lanes);
-    for (int t = (int)start; t < stop; t += kStep) {
-      Raw<D> next;
-      Place np[2] = {p[0], p[1]};
-      if (t + kStep < stop) {
-        const int j = (t + kStep) * kTile;
-        np[0] = place_of<D>(a, table, head, j, hi_most);
-        np[1] = place_of<D>(a, table, head, j + 16, hi_most);
-        load_raw<D>(next, np, lanes);
+    // kAhead tiles are on their way while one is worked on, and the entries of one more: loads are issued whether or not there are tiles left,
+    // so that every wait is for a known number of them (past the end they go to the sequence's first entry's page, or page 0).
+    Raw<D> raw[kAhead + 1];
+    uint32_t fine = 0;            // two bits for each buffer: whether its half tiles' pages are
+    Entry e0, e1;
+    const auto entries = [&](int64_t tile) {
+      const int64_t j = tile < stop ? tile * kTile : (int64_t)hi_most;
+      e0 = entry_of(a, table, j, hi_most);
+      e1 = entry_of(a, table, j + 16, hi_most);
+    };
+    const auto load = [&](Raw<D> &to, int buffer) {
+      const Place p0 = place_of<D>(a, head, e0), p1 = place_of<D>(a, head, e1);
+      fine = (fine & ~(3u << 2 * buffer)) | (p0.fine ? 1u : 0u) << 2 * buffer | (p1.fine ? 2u : 0u) << 2 * buffer;
+      load_half<D>(to, 0, p0, lanes);
+      load_half<D>(to, 1, p1, lanes);
+    };
+    entries(start);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      load(raw[i], i);
+      entries(start + (i + 1) * kStep);
+    }
+    for (int64_t t = start; t < stop;) {
+#pragma unroll
+      for (int i = 0; i <= kAhead; ++i) {
+        load(raw[(i + kAhead) % (kAhead + 1)], (i + kAhead) % (kAhead + 1));
+        entries(t + (kAhead + 1) * kStep);
+        const int j0 = (int)t * kTile;
+        const uint32_t mine = fine >> 2 * i & 3;
+        one_tile<D, RT, PARTS_Q, PARTS_P>(sums, rows, raw[i], g, j0, mine == 3 && j0 >= lo_most && j0 + kTile <= hi_least, (mine & 1) != 0,
+                                          (mine & 2) != 0);
+        t += kStep;
+        if (t >= stop) break;
       }
-      const int j0 = t * kTile;
-      if (p[0].fine && p[1].fine && j0 >= lo_most && j0 + kTile <= hi_least)
-        one_tile<D, RT, PARTS_Q, PARTS_P, true>(sums, rows, raw, g, j0, true, true);
-      else
-        one_tile<D, RT, PARTS_Q, PARTS_P, false>(sums, rows, raw, g, j0, p[0].fine, p[1].fine);
-      raw = next;
-      p[0] = np[0], p[1] = np[1];
     }
   }
 #pragma unroll
@@ -603,13 +667,14 @@ __global__ __launch_bounds__(kBlock, D * RT <= 128 ? 2 : 1) void attention_kerne
   }
 }
 
-// The parts of a row joined: a wavefront has a row, its lanes first the parts' sums, then the channels.  Parts that saw nothing have a sum of zero
-// and are not read.
+// The parts of a row joined.  A workgroup has a row: lanes first have the parts' sums, then each wavefront adds up every fourth part, four of them on
+// their way at a time, and the four meet in LDS.  Parts that saw nothing have a sum of zero and are not read.
 template <int D> __global__ __launch_bounds__(kBlock) void attention_join_kernel(const AttentionArgs a, uint32_t rows, int unit_rows) {
-  constexpr int C = D / kWave;
-  const int lane = threadIdx.x % kWave;
-  for (uint32_t r = blockIdx.x * (kBlock / kWave) + threadIdx.x / kWave; r < rows; r += gridDim.x * (kBlock / kWave)) {
-    // rows: query heads fastest, then queries, sequences
+  constexpr int C = D / kWave, W = kBlock / kWave, U = 4;
+  __shared__ float part[W][D];
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  for (uint32_t r = blockIdx.x; r < rows; r += gridDim.x) {
+    // rows: query heads fastest, then queries, heads of the cache, sequences
     const int all_rows = a.queries * a.per_kv, splits = (int)a.splits_div.d;
     const int bh = (int)(r / (uint32_t)all_rows), row = (int)(r % (uint32_t)all_rows), b = bh / (int)a.kv_div.d, kv = bh % (int)a.kv_div.d;
     const int64_t unit = (int64_t)bh * a.blocks_div.d + row / unit_rows, place = row % unit_rows;
@@ -620,21 +685,43 @@ template <int D> __global__ __launch_bounds__(kBlock) void attention_join_kernel
     const float w = ml.y == 0.0f ? 0.0f : top == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(ml.x - top);
     float total = ml.y == 0.0f ? 0.0f : ml.y * w;
     for (int m = 1; m < kWave; m <<= 1) total += __shfl_xor(total, m);
+    const uint64_t any = __builtin_amdgcn_ballot_w64(ml.y != 0.0f);
     float v[C];
 #pragma unroll
     for (int i = 0; i < C; ++i) v[i] = 0.0f;
-    for (uint64_t left = __builtin_amdgcn_ballot_w64(ml.y != 0.0f); left; left &= left - 1) {
-      const int s = __builtin_ctzll(left);
-      const float ws = __shfl(w, s);
-      const float *from = a.parts + ((unit * splits + s) * unit_rows + place) * D + lane * C;
+    for (int s0 = wave; s0 < splits; s0 += W * U) {
+      float x[U][C];
 #pragma unroll
-      for (int i = 0; i < C; ++i) v[i] += ws * from[i];
+      for (int u = 0; u < U; ++u) {
+        const int s = s0 + u * W;
+#pragma unroll
+        for (int i = 0; i < C; ++i) x[u][i] = 0.0f;
+        if (s < splits && any >> s & 1) {
+          const float *from = a.parts + ((unit * splits + s) * unit_rows + place) * D + lane * C;
+#pragma unroll
+          for (int i = 0; i < C; ++i) x[u][i] = from[i];
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float ws = __shfl(w, (s0 + u * W) & 63);
+#pragma unroll
+        for (int i = 0; i < C; ++i) v[i] += ws * x[u][i];
+      }
     }
+#pragma unroll
+    for (int i = 0; i < C; ++i) part[wave][lane * C + i] = v[i];
+    __syncthreads();
     const int t = row / a.per_kv, h = kv * a.per_kv + row % a.per_kv;
     char *to = a.out + b * a.ob + t * a.ot + h * a.oh;
+    for (int c = threadIdx.x; c < D; c += kBlock) {
+      float x = 0.0f;
 #pragma unroll
-    for (int i = 0; i < C; ++i) store_from_float(to + (lane * C + i) * a.oe, a.type, total == 0.0f ? 0.0f : v[i] / total);
-    if (a.log_sum && lane == 0) *(float *)(a.log_sum + b * a.lb + t * a.lt + h * a.lh) = log_of(top, total);
+      for (int i = 0; i < W; ++i) x += part[i][c];
+      store_from_float(to + c * a.oe, a.type, total == 0.0f ? 0.0f : x / total);
+    }
+    if (a.log_sum && threadIdx.x == 0) *(float *)(a.log_sum + b * a.lb + t * a.lt + h * a.lh) = log_of(top, total);
+    __syncthreads();
   }
 }
 
@@ -727,7 +814,7 @@ template <int D> int run_attention(AttentionArgs &a, const Launch &l, uint32_t r
     if (rc != OCN_OK) return rc;
   }
   if (l.splits == 1) return OCN_OK;
-  const uint32_t joins = (uint32_t)std::min<int64_t>((rows + kBlock / kWave - 1) / (kBlock / kWave), max_launch_blocks());
+  const uint32_t joins = (uint32_t)std::min<int64_t>(rows, max_launch_blocks());
   hipLaunchKernelGGL((attention_join_kernel<D>), dim3(joins), dim3(kBlock), 0, stream, a, rows, (int)l.unit_rows);
   return done(hipGetLastError());
 }
