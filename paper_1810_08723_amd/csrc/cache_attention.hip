@@ -25,18 +25,16 @@ struct AttentionArgs {
   int32_t least;                               // tiles of a split, at least
   int32_t whole_q, whole_out;                  // rows are aligned and without gaps
   uint32_t first_item;                         // of this launch
-  FastDiv page_div, per_kv_div, splits_div, blocks_div, kv_div;
+  uint32_t splits;
+  FastDiv page_div, per_kv_div, units_div, blocks_div, kv_div;
   float *parts, *part_sums;                    // [items][rows of a unit][channels], [..][2]: maximum and sum
   float scale;                                 // of the scores, times log2(e)
 };
 
-#ifndef OCN_LEAST
-#define OCN_LEAST 8
-#define OCN_WG 1024
-#endif
-constexpr int64_t kLeastTiles = OCN_LEAST;             // of a split: two for each wavefront
+constexpr int64_t kLeastTiles = 8;             // of a split: two for each wavefront
+constexpr int64_t kAloneTiles = 20;            // up to so many a second launch costs more than splits gain (17 tiles: 9.6 us, 11.0 in splits)
 constexpr int64_t kMaxSplits = kWave;          // a lane each when they are joined
-constexpr int64_t kWorkgroups = OCN_WG;          // worth launching: four to a CU
+constexpr int64_t kWorkgroups = 768;           // worth launching: three to a CU
 
 // ---------------------------------------------------------------------------------------
 // The kernel.  Query heads of one head of the cache, of one or more queries, are the rows of its tiles: 16 a tile.  For 32 tokens at a
@@ -217,8 +215,12 @@ __device__ __forceinline__ float row_max(float x) {
   return larger(__builtin_bit_cast(float, b0), __builtin_bit_cast(float, b1));
 }
 
-__device__ __forceinline__ int wave_max(int x) {
-  for (int m = 1; m < kWave; m <<= 1) x = max(x, __shfl_xor(x, m));
+// the largest of sixteen lanes, which the four lanes of a row repeat: of all rows
+__device__ __forceinline__ int rows_max(int x) {
+  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x128, 0xf, 0xf, false));    // (rotations by 8, 4, 2 and 1 lanes)
+  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x124, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x122, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(x, x, 0x121, 0xf, 0xf, false));
   return __builtin_amdgcn_readfirstlane(x);
 }
 
@@ -470,23 +472,21 @@ __global__ __launch_bounds__(kBlock, D * RT <= 128 ? 2 : 1) void attention_kerne
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), n = lane % 16, g = lane / 16;
   const LaneOffsets lanes = lane_offsets<D>(a, n, g);
   const uint32_t item = a.first_item + blockIdx.x;
-  // items: splits fastest, then blocks of rows, heads of the cache, sequences
-  const uint32_t unit = fast_quotient(item, a.splits_div), split = item - unit * a.splits_div.d;
+  // Items: blocks of rows fastest, then heads of the cache, sequences, and splits: workgroups go to the XCDs in turn, and where sequences are
+  // of different lengths the later splits are empty (with splits fastest some XCDs had most of the work: 105 for 44 us).
+  const uint32_t split = fast_quotient(item, a.units_div), unit = item - split * a.units_div.d;
   const uint32_t bh = fast_quotient(unit, a.blocks_div), block = unit - bh * a.blocks_div.d;
   const int b = (int)fast_quotient(bh, a.kv_div), kv = (int)bh - b * (int)a.kv_div.d;
   const int first_row = (int)block * kRows + (SHARE ? 0 : wave * 16 * RT), all_rows = a.queries * a.per_kv;
   Rows<D, RT, PARTS_Q> rows;
-  Sums<D, RT> sums;
   int hi_most = 0, hi_least = 0x7fffffff, lo_least = 0x7fffffff, lo_most = 0;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    const int row = first_row + rt * 16 + n, t = row < all_rows ? (int)fast_quotient((uint32_t)row, a.per_kv_div) : 0;
+    const int row = first_row + rt * 16 + n;
     rows.lo[rt] = 0;
     rows.hi[rt] = 0x7fffffff;
-    uint32_t q[S::kWords][8 * PARTS_Q / 2];       // as they are in memory: two 16-bit channels, or a float, in a word
-    float most = 0.0f;
     if (row < all_rows) {
-      const int64_t seen = load_index(a.seen + b * a.sb + t * a.st, a.seen_wide);
+      const int64_t seen = load_index(a.seen + b * a.sb + fast_quotient((uint32_t)row, a.per_kv_div) * a.st, a.seen_wide);
       rows.hi[rt] = (int)max((int64_t)0, min(seen, (int64_t)a.capacity));
       rows.lo[rt] = a.window > 0 ? (int)max((int64_t)0, rows.hi[rt] - a.window) : 0;
       hi_most = max(hi_most, rows.hi[rt]);
@@ -494,11 +494,36 @@ __global__ __launch_bounds__(kBlock, D * RT <= 128 ? 2 : 1) void attention_kerne
       lo_most = max(lo_most, rows.lo[rt]);
       if (rows.hi[rt] > 0) lo_least = min(lo_least, rows.lo[rt]);
     }
-    const char *from = a.q + b * a.qb + t * a.qt + (int64_t)(kv * a.per_kv + row - t * a.per_kv) * a.qh;
+  }
+  hi_most = rows_max(hi_most);
+  hi_least = -rows_max(-hi_least);
+  lo_most = rows_max(lo_most);
+  lo_least = -rows_max(-lo_least);
+  // this split's tiles: all of [lo_least, hi_most) in equal parts, none of fewer than a.least tiles
+  const int begin = hi_most > 0 ? lo_least / kTile : 0, end = (int)(((int64_t)hi_most + kTile - 1) / kTile);
+  const int each = max(a.least, (int)((end - begin + a.splits - 1) / a.splits));
+  const int64_t from = begin + (int64_t)split * each;
+  if (a.splits > 1 && from >= end) {      // nothing left for this split
+    for (int i = SHARE ? threadIdx.x : lane; i < (SHARE ? kRows : 16 * RT); i += SHARE ? kBlock : kWave)
+      *(float2 *)(a.part_sums + ((int64_t)item * kRows + (SHARE ? 0 : wave * 16 * RT) + i) * 2) = float2{-__builtin_inff(), 0.0f};
+    return;
+  }
+  const int stop = (int)min((int64_t)end, from + each);
+  const char *table = a.table + b * a.tb;
+  const int64_t head = kv * a.head_stride;
+  constexpr int kStep = SHARE ? W : 1;
+  const int64_t start = from + (SHARE ? wave : 0);
+  Sums<D, RT> sums;
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int row = first_row + rt * 16 + n, t = row < all_rows ? (int)fast_quotient((uint32_t)row, a.per_kv_div) : 0;
+    uint32_t q[S::kWords][8 * PARTS_Q / 2];       // as they are in memory: two 16-bit channels, or a float, in a word
+    float most = 0.0f;
+    const char *from_row = a.q + b * a.qb + t * a.qt + (int64_t)(kv * a.per_kv + row - t * a.per_kv) * a.qh;
 #pragma unroll
     for (int w = 0; w < S::kWords; ++w) {
       const int channel = 8 * (w / S::kRun * 4 * S::kRun + S::kRun * g + w % S::kRun);
-      load_channels<PARTS_Q>(q[w], from, channel, row < all_rows, a);
+      load_channels<PARTS_Q>(q[w], from_row, channel, row < all_rows, a);
       float x[8];
       channels_of<PARTS_Q, PARTS_P>(x, q[w]);
 #pragma unroll
@@ -525,19 +550,6 @@ __global__ __launch_bounds__(kBlock, D * RT <= 128 ? 2 : 1) void attention_kerne
     sums.total[rt] = sums.bad[rt] = f32x4{0, 0, 0, 0};
     sums.top[rt] = -__builtin_inff();
   }
-  hi_most = wave_max(hi_most);
-  hi_least = -wave_max(-hi_least);
-  lo_most = wave_max(lo_most);
-  lo_least = -wave_max(-lo_least);
-  // this split's tiles: all of [lo_least, hi_most) in parts of at least a.least tiles
-  const int begin = hi_most > 0 ? lo_least / kTile : 0, end = (int)(((int64_t)hi_most + kTile - 1) / kTile);
-  const int each = max(a.least, (int)((end - begin + a.splits_div.d - 1) / a.splits_div.d));
-  const int64_t from = begin + (int64_t)split * each;
-  const int stop = (int)min((int64_t)end, from + each);
-  const char *table = a.table + b * a.tb;
-  const int64_t head = kv * a.head_stride;
-  constexpr int kStep = SHARE ? W : 1;
-  const int64_t start = from + (SHARE ? wave : 0);
   if (start < stop) {
     // kAhead tiles are on their way while one is worked on, and the entries of one more: loads are issued whether or not there are tiles left,
     // so that every wait is for a known number of them (past the end they go to the sequence's first entry's page, or page 0).
@@ -582,7 +594,7 @@ __global__ __launch_bounds__(kBlock, D * RT <= 128 ? 2 : 1) void attention_kerne
 #pragma unroll
       for (int r = 0; r < 4; ++r)
         if (sums.bad[rt][r] > 0.0f) sums.out[rt][i][r] = __builtin_nanf("");
-  const bool whole = a.splits_div.d == 1;
+  const bool whole = a.splits == 1;
   if constexpr (SHARE) {
     // the wavefronts' sums, relative to the largest of their maxima
     if (g == 0) {
@@ -675,11 +687,12 @@ template <int D> __global__ __launch_bounds__(kBlock) void attention_join_kernel
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   for (uint32_t r = blockIdx.x; r < rows; r += gridDim.x) {
     // rows: query heads fastest, then queries, heads of the cache, sequences
-    const int all_rows = a.queries * a.per_kv, splits = (int)a.splits_div.d;
+    const int all_rows = a.queries * a.per_kv, splits = (int)a.splits;
+    const int64_t units = a.units_div.d;
     const int bh = (int)(r / (uint32_t)all_rows), row = (int)(r % (uint32_t)all_rows), b = bh / (int)a.kv_div.d, kv = bh % (int)a.kv_div.d;
     const int64_t unit = (int64_t)bh * a.blocks_div.d + row / unit_rows, place = row % unit_rows;
     float2 ml = {-__builtin_inff(), 0.0f};
-    if (lane < splits) ml = *(const float2 *)(a.part_sums + ((unit * splits + lane) * unit_rows + place) * 2);
+    if (lane < splits) ml = *(const float2 *)(a.part_sums + ((lane * units + unit) * unit_rows + place) * 2);
     float top = ml.x;
     for (int m = 1; m < kWave; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
     const float w = ml.y == 0.0f ? 0.0f : top == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(ml.x - top);
@@ -697,7 +710,7 @@ template <int D> __global__ __launch_bounds__(kBlock) void attention_join_kernel
 #pragma unroll
         for (int i = 0; i < C; ++i) x[u][i] = 0.0f;
         if (s < splits && any >> s & 1) {
-          const float *from = a.parts + ((unit * splits + s) * unit_rows + place) * D + lane * C;
+          const float *from = a.parts + ((s * units + unit) * unit_rows + place) * D + lane * C;
 #pragma unroll
           for (int i = 0; i < C; ++i) x[u][i] = from[i];
         }
@@ -744,8 +757,8 @@ Launch launch_of(int64_t batch, int64_t queries, int64_t heads, int64_t kv, int6
   l.unit_rows = 16 * l.row_tiles * (l.share ? 1 : kBlock / kWave);
   l.blocks = (rows + l.unit_rows - 1) / l.unit_rows;
   l.units = batch * kv * l.blocks;
-  const int64_t tiles = (capacity + kTile - 1) / kTile, most = std::max<int64_t>(1, tiles / kLeastTiles);
-  l.splits = std::min<int64_t>({most, kMaxSplits, std::max<int64_t>(1, (kWorkgroups + l.units - 1) / std::max<int64_t>(l.units, 1))});
+  const int64_t tiles = (capacity + kTile - 1) / kTile, most = tiles <= kAloneTiles ? 1 : tiles / kLeastTiles;
+  l.splits = std::min<int64_t>({most, kMaxSplits, std::max<int64_t>(1, kWorkgroups / std::max<int64_t>(l.units, 1))});
   l.items = l.units * l.splits;
   return l;
 }
@@ -895,7 +908,8 @@ int ocn_cache_attention(const ocn_tensor *q, const ocn_tensor *cache, const ocn_
   a.page = (int32_t)page;
   a.page_div = make_fastdiv((uint32_t)page);
   a.per_kv_div = make_fastdiv((uint32_t)a.per_kv);
-  a.splits_div = make_fastdiv((uint32_t)l.splits);
+  a.splits = (uint32_t)l.splits;
+  a.units_div = make_fastdiv((uint32_t)l.units);
   a.blocks_div = make_fastdiv((uint32_t)l.blocks);
   a.kv_div = make_fastdiv((uint32_t)kv);
   a.type = q->dtype;

@@ -22,6 +22,7 @@ namespace {
 
 constexpr int kEight = 8;              // channels of a lane
 constexpr int kTable = 2048;           // cosines, and sines, that a workgroup holds
+constexpr int kPasses = 8;              // of a workgroup's lanes over its rows, at most
 constexpr int kFoldBlocks = 512;       // workgroups that sum a gradient of weights, at most
 
 // ---------------------------------------------------------------------------------------
@@ -36,7 +37,7 @@ struct HeadJob {                       // one tensor of heads
   int64_t xl[kMaxLead], gl[kMaxLead], ol[kMaxLead];
   int64_t weight_stride;
   int32_t weight_type;
-  int32_t heads, per;                  // heads of a token; of an item
+  int32_t heads, per, per_tokens;      // heads of a token; heads and tokens of an item
   FastDiv per_div, blocks_div;         // by `per`; by items along the heads
   uint32_t items;
   int32_t workers;                     // backward: workgroups
@@ -54,30 +55,27 @@ struct HeadArgs {
   int32_t pos_wide, interleaved;
   int32_t half, row;                   // pairs of a head; floats from one token's cosines to the next
   FastDiv half_div;
-  int32_t d, lanes_log2, per_tokens;   // channels; lanes of a row; tokens of an item
-  uint32_t items;
+  int32_t d, lanes_log2;               // channels; lanes of a row
+  uint32_t items, first_item;          // of all launches; of this one
   // the cache
   const char *slots;
   int64_t slot_l[kMaxLead], page_stride, head_stride, slot_count;
   char *cache;
   int32_t slots_wide, page;
+  FastDiv page_div;
 };
 
-struct Offsets { int64_t x, g, o, pos, slot; };
-
-// where a token's rows begin in the operands of a job
-__device__ __forceinline__ Offsets offsets_of(const HeadArgs &a, const HeadJob &j, uint32_t t) {
-  Offsets f = {0, 0, 0, 0, 0};
-  for (int d = a.lead.n - 1; d >= 0; --d) {
-    const uint32_t q = d > 0 ? fast_quotient(t, a.lead.div[d]) : 0, i = t - q * a.lead.div[d].d;
-    f.x += i * j.xl[d];
-    f.g += i * j.gl[d];
-    f.o += i * j.ol[d];
-    f.pos += i * a.pos_l[d];
-    f.slot += i * a.slot_l[d];
-    t = q;
+// an offset along the tokens' dimensions
+__device__ __forceinline__ int64_t along(const HeadArgs &a, const int64_t *stride, uint32_t token) {
+  if (a.lead.n == 1) return (int64_t)token * stride[0];
+  int64_t o = 0;
+#pragma nounroll
+  for (int d = a.lead.n - 1; d > 0; --d) {
+    const uint32_t q = fast_quotient(token, a.lead.div[d]);
+    o += (int64_t)(token - q * a.lead.div[d].d) * stride[d];
+    token = q;
   }
-  return f;
+  return o + (int64_t)token * stride[0];
 }
 
 // ---------------------------------------------------------------------------------------
@@ -113,12 +111,13 @@ __device__ __forceinline__ void sine_cosine(double t, double *s, double *c) {
   *c = (quarter + 1) & 2 ? -b : b;
 }
 
-struct Table { float c[kTable], s[kTable]; };
+struct alignas(16) Table { float c[kTable], s[kTable]; };
 
-__device__ __forceinline__ void fill_table(const HeadArgs &a, const HeadJob &j, Table &tab, uint32_t token, int tokens) {
+__device__ __forceinline__ void fill_table(const HeadArgs &a, Table &tab, uint32_t token, int tokens) {
+#pragma nounroll
   for (int i = threadIdx.x; i < tokens * a.half; i += kBlock) {
     const int t = (int)fast_quotient((uint32_t)i, a.half_div), p = i - t * a.half;
-    const int64_t at = load_index(a.pos + offsets_of(a, j, token + t).pos, a.pos_wide);
+    const int64_t at = load_index(a.pos + along(a, a.pos_l, token + t), a.pos_wide);
     double s, c;
     sine_cosine((double)at * *(const double *)(a.freq + p * a.freq_stride), &s, &c);
     tab.c[t * a.row + p] = (float)(c * a.magnitude);
@@ -130,8 +129,8 @@ __device__ __forceinline__ void fill_table(const HeadArgs &a, const HeadJob &j, 
 // rows
 // ---------------------------------------------------------------------------------------
 
-// How the partners of a lane's eight channels are loaded.  kPairsFour: pairs end inside a lane's eight, at a
-// multiple of four; kPairsOne: anywhere, or rows that are not made of whole aligned vectors.
+// Where the pairs of a lane's eight channels lie.  kPairsInside: among the eight; kPairsEight: the partners of all eight are eight more
+// channels in a row; kPairsFour: of each half of them; kPairsOne: anywhere.
 enum { kPairsNone = 0, kPairsInside, kPairsEight, kPairsFour, kPairsOne };
 
 template <class T> using eight_t = typename Eight<T>::V;
@@ -161,13 +160,12 @@ template <class T, bool VEC> __device__ __forceinline__ void store_eight(char *r
   }
 }
 
-// the other channels of the pairs that channels e ... e + 7 belong to (channel i < half goes with i + half); `kind` is
-// the same for the whole launch
-template <class T, bool VEC> __device__ __forceinline__ eight_t<T> load_partners(const char *row, int64_t step, int e, int half, int kind) {
+// the other channels of the pairs that channels e ... e + 7 belong to (channel i < half goes with i + half), where they lie apart
+template <class T, int KIND> __device__ __forceinline__ eight_t<T> load_partners(const char *row, int64_t step, int e, int half) {
   eight_t<T> v = {};
-  if (VEC && kind == kPairsEight) {
+  if constexpr (KIND == kPairsEight) {
     if (e < 2 * half) v = *(const eight_t<T> *)(row + (e < half ? e + half : e - half) * (int)sizeof(T));
-  } else if (VEC && kind == kPairsFour) {
+  } else if constexpr (KIND == kPairsFour) {
 #pragma unroll
     for (int k = 0; k < kEight; k += 4) {
       const int f = e + k;
@@ -177,7 +175,7 @@ template <class T, bool VEC> __device__ __forceinline__ eight_t<T> load_partners
         for (int i = 0; i < 4; ++i) v[k + i] = w[i];
       }
     }
-  } else if (kind >= kPairsEight) {
+  } else if constexpr (KIND == kPairsOne) {
 #pragma unroll
     for (int i = 0; i < kEight; ++i) {
       const int f = e + i;
@@ -188,9 +186,8 @@ template <class T, bool VEC> __device__ __forceinline__ eight_t<T> load_partners
 }
 
 // x turned; p: the partners (of pairs that lie apart)
-__device__ __forceinline__ void turn(float *x, const float *p, const float *c, const float *s, int e, int half, int kind) {
-  if (kind == kPairsInside) {
-    if (e >= 2 * half) return;
+template <int KIND> __device__ __forceinline__ void turn(float *x, const float *p, const float *c, const float *s, int e, int half) {
+  if constexpr (KIND == kPairsInside) {
 #pragma unroll
     for (int i = 0; i < kEight; i += 2) {
       if (e + i >= 2 * half) continue;
@@ -198,15 +195,15 @@ __device__ __forceinline__ void turn(float *x, const float *p, const float *c, c
       x[i] = a * cc - b * ss;
       x[i + 1] = b * cc + a * ss;
     }
-  } else if (kind == kPairsEight) {
+  } else if constexpr (KIND == kPairsEight) {
     if (e >= 2 * half) return;
     const int at = e < half ? e : e - half;
+    f32x4 cc[2], ss[2];
 #pragma unroll
-    for (int i = 0; i < kEight; ++i) {
-      const float ss = s[at + i];
-      x[i] = x[i] * c[at + i] + p[i] * (e < half ? -ss : ss);
-    }
-  } else if (kind != kPairsNone) {
+    for (int k = 0; k < 2; ++k) cc[k] = *(const f32x4 *)(c + at + 4 * k), ss[k] = *(const f32x4 *)(s + at + 4 * k);
+#pragma unroll
+    for (int i = 0; i < kEight; ++i) x[i] = x[i] * cc[i / 4][i % 4] + p[i] * (e < half ? -ss[i / 4][i % 4] : ss[i / 4][i % 4]);
+  } else if constexpr (KIND != kPairsNone) {
 #pragma unroll
     for (int i = 0; i < kEight; ++i) {
       const int f = e + i;
@@ -223,88 +220,88 @@ __device__ __forceinline__ float sum_over_row(float v, int lanes) {
   return v;
 }
 
-struct Item { const HeadJob *job; int which; uint32_t token; int tokens, head; };
+struct Item { int which, tokens, head; uint32_t token; };
 
+// a workgroup's tokens and heads
 __device__ __forceinline__ Item item_of(const HeadArgs &a, uint32_t i) {
   Item r;
   r.which = i >= a.job[0].items;
-  r.job = &a.job[r.which];
+  const HeadJob &j = a.job[r.which];
   if (r.which) i -= a.job[0].items;
-  const uint32_t block = fast_quotient(i, r.job->blocks_div);
-  r.head = (int)(i - block * r.job->blocks_div.d) * r.job->per;
-  r.token = block * a.per_tokens;
-  r.tokens = (int)min((uint32_t)a.per_tokens, a.lead.tokens - r.token);
+  const uint32_t block = fast_quotient(i, j.blocks_div);
+  r.head = (int)(i - block * j.blocks_div.d) * j.per;
+  r.token = block * j.per_tokens;
+  r.tokens = (int)min((uint32_t)j.per_tokens, a.lead.tokens - r.token);
   return r;
 }
 
 // a lane's weights: those of its channels, and of their partners
-__device__ __forceinline__ void load_weights(const HeadJob &j, int d, int e, int half, int kind, float *w, float *wp) {
+template <int KIND> __device__ __forceinline__ void load_weights(const HeadJob &j, int d, int e, int half, float *w, float *wp) {
 #pragma unroll
   for (int i = 0; i < kEight; ++i) {
     const int f = e + i, g = f < half ? f + half : f - half;
     w[i] = j.weight && f < d ? load_as_float(j.weight + f * j.weight_stride, j.weight_type) : 1.0f;
-    wp[i] = j.weight && kind >= kPairsEight && f < 2 * half ? load_as_float(j.weight + g * j.weight_stride, j.weight_type) : 1.0f;
+    wp[i] = j.weight && KIND >= kPairsEight && f < 2 * half ? load_as_float(j.weight + g * j.weight_stride, j.weight_type) : 1.0f;
   }
 }
 
-// Rotation, with the norm before it where NORM is set.
-template <class T, bool VEC, bool NORM> __global__ __launch_bounds__(kBlock) void head_rows_kernel(const HeadArgs a, int kind_of_pairs) {
-  constexpr int U = sizeof(T) == 2 ? 4 : 2;   // rows of a lane at a time
+// Rotation, with the norm before it where NORM is set.  (No loop over items in the kernel: what their first instructions share would be kept in registers;
+// launches take up to as many as a launch may have.)
+template <class T, bool VEC, int KIND, bool NORM> __global__ __launch_bounds__(kBlock) void head_rows_kernel(const HeadArgs a) {
+  constexpr int U = 2;                  // rows of a lane at a time
   __shared__ Table tab;
   const int lanes = 1 << a.lanes_log2, e = (threadIdx.x & (lanes - 1)) * kEight, rows = kBlock >> a.lanes_log2, d = a.d;
-  for (uint32_t it = blockIdx.x; it < a.items; it += gridDim.x) {
-    const Item item = item_of(a, it);
-    const HeadJob &j = *item.job;
-    const int kind = kind_of_pairs, total = item.tokens * j.per;
-    float w[kEight], wp[kEight];
-    if constexpr (NORM) load_weights(j, d, e, a.half, kind, w, wp);
-    for (int base = 0; base < total; base += U * rows) {
-      eight_t<T> x[U], p[U];
-      char *to[U];
-      int tt[U];
+  const Item item = item_of(a, a.first_item + blockIdx.x);
+  const HeadJob &j = a.job[item.which];
+  const int total = item.tokens * j.per;
+  float w[kEight], wp[kEight];
+  for (int base = 0; base < total; base += U * rows) {
+    eight_t<T> x[U], p[U];
+    char *to[U];
+    int tt[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int r = base + u * rows + (threadIdx.x >> a.lanes_log2), t = (int)fast_quotient((uint32_t)r, j.per_div), h = item.head + r - t * j.per;
-        to[u] = nullptr;
-        tt[u] = t;
-        if (r < total && h < j.heads && e < d) {
-          const Offsets f = offsets_of(a, j, item.token + t);
-          const char *row = j.x + f.x + h * j.xh;
-          x[u] = load_eight<T, VEC>(row, j.xe, e, d);
-          p[u] = load_partners<T, VEC>(row, j.xe, e, a.half, kind);
-          to[u] = j.out + f.o + h * j.oh;
-        }
-      }
-      if (base == 0 && kind != kPairsNone) {
-        fill_table(a, j, tab, item.token, item.tokens);
-        __syncthreads();
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        float v[kEight], q[kEight], r = 1.0f;
-        if constexpr (NORM) {
-          float sum = 0.0f;
-          if (to[u]) {
-#pragma unroll
-            for (int i = 0; i < kEight; ++i) sum = __builtin_fmaf((float)x[u][i], (float)x[u][i], sum);
-          }
-          r = __builtin_amdgcn_rsqf(sum_over_row(sum, lanes) * a.over_d + a.eps);
-        }
-        if (!to[u]) continue;
-#pragma unroll
-        for (int i = 0; i < kEight; ++i) {
-          v[i] = (float)x[u][i];
-          q[i] = (float)p[u][i];
-          if constexpr (NORM) {
-            v[i] = v[i] * r * w[i];
-            q[i] = q[i] * r * wp[i];
-          }
-        }
-        turn(v, q, tab.c + tt[u] * a.row, tab.s + tt[u] * a.row, e, a.half, kind);
-        store_eight<T, VEC>(to[u], j.oe, e, d, v);
+    for (int u = 0; u < U; ++u) {
+      const int r = base + u * rows + (threadIdx.x >> a.lanes_log2), t = (int)fast_quotient((uint32_t)r, j.per_div), h = item.head + r - t * j.per;
+      to[u] = nullptr;
+      tt[u] = t;
+      if (r < total && h < j.heads && e < d) {
+        const char *row = j.x + along(a, j.xl, item.token + t) + h * j.xh;
+        x[u] = load_eight<T, VEC>(row, j.xe, e, d);
+        p[u] = load_partners<T, KIND>(row, j.xe, e, a.half);
+        to[u] = j.out + along(a, j.ol, item.token + t) + h * j.oh;
       }
     }
-    __syncthreads();
+    if (base == 0) {
+      if constexpr (NORM) load_weights<KIND>(j, d, e, a.half, w, wp);
+      if constexpr (KIND != kPairsNone) {
+        fill_table(a, tab, item.token, item.tokens);
+        __syncthreads();
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float v[kEight], q[kEight], r = 1.0f;
+      if constexpr (NORM) {
+        float sum = 0.0f;
+        if (to[u]) {
+#pragma unroll
+          for (int i = 0; i < kEight; ++i) sum = __builtin_fmaf((float)x[u][i], (float)x[u][i], sum);
+        }
+        r = __builtin_amdgcn_rsqf(sum_over_row(sum, lanes) * a.over_d + a.eps);
+      }
+      if (!to[u]) continue;
+#pragma unroll
+      for (int i = 0; i < kEight; ++i) {
+        v[i] = (float)x[u][i];
+        q[i] = (float)p[u][i];
+        if constexpr (NORM) {
+          v[i] = v[i] * r * w[i];
+          q[i] = q[i] * r * wp[i];
+        }
+      }
+      turn<KIND>(v, q, tab.c + tt[u] * a.row, tab.s + tt[u] * a.row, e, a.half);
+      store_eight<T, VEC>(to[u], j.oe, e, d, v);
+    }
   }
 }
 
@@ -312,72 +309,55 @@ template <class T, bool VEC, bool NORM> __global__ __launch_bounds__(kBlock) voi
 //     gradient of x = r (h w - u mean(h w u)),    gradient of w = the sum of h u over all rows.
 // A lane keeps its channels' sums over all rows of its workgroup; workgroups leave theirs in the workspace, and a second launch
 // adds those up in a fixed order: no atomics, the same bits every time.
-template <class T, bool VEC> __global__ __launch_bounds__(kBlock) void head_grad_kernel(const HeadArgs a, int kind) {
-  constexpr int U = 2;
+template <class T, bool VEC, int KIND> __global__ __launch_bounds__(kBlock) void head_grad_kernel(const HeadArgs a) {
   __shared__ Table tab;
   __shared__ float sums[kBlock * kEight];
   const int lanes = 1 << a.lanes_log2, e = (threadIdx.x & (lanes - 1)) * kEight, rows = kBlock >> a.lanes_log2, d = a.d;
   // a workgroup's items are of one job: blockIdx.y
   const HeadJob &j = a.job[blockIdx.y];
   if (blockIdx.x >= (uint32_t)j.workers) return;
-  float w[kEight], wp[kEight], gw[kEight];
-  load_weights(j, d, e, a.half, kind, w, wp);
+  float w[kEight], gw[kEight];
 #pragma unroll
-  for (int i = 0; i < kEight; ++i) gw[i] = 0.0f;
+  for (int i = 0; i < kEight; ++i) {
+    gw[i] = 0.0f;
+    w[i] = j.weight && e + i < d ? load_as_float(j.weight + (e + i) * j.weight_stride, j.weight_type) : 1.0f;
+  }
   for (uint32_t it = blockIdx.x; it < j.items; it += j.workers) {
     const Item item = item_of(a, it + (blockIdx.y ? a.job[0].items : 0));
     const int total = item.tokens * j.per;
-    for (int base = 0; base < total; base += U * rows) {
-      eight_t<T> x[U], g[U], p[U];
-      char *to[U];
-      int tt[U];
+    if constexpr (KIND != kPairsNone) {
+      fill_table(a, tab, item.token, item.tokens);
+      __syncthreads();
+    }
+    for (int base = 0; base < total; base += rows) {
+      const int r = base + (threadIdx.x >> a.lanes_log2), t = (int)fast_quotient((uint32_t)r, j.per_div), n = item.head + r - t * j.per;
+      const bool mine = r < total && n < j.heads && e < d;
+      float v[kEight], h[kEight], square = 0.0f, cross = 0.0f;
+      if (mine) {
+        const char *row = j.g + along(a, j.gl, item.token + t) + n * j.gh;
+        const eight_t<T> x = load_eight<T, VEC>(j.x + along(a, j.xl, item.token + t) + n * j.xh, j.xe, e, d);
+        const eight_t<T> g = load_eight<T, VEC>(row, j.ge, e, d), p = load_partners<T, KIND>(row, j.ge, e, a.half);
+        float q[kEight];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int r = base + u * rows + (threadIdx.x >> a.lanes_log2), t = (int)fast_quotient((uint32_t)r, j.per_div), h = item.head + r - t * j.per;
-        to[u] = nullptr;
-        tt[u] = t;
-        if (r < total && h < j.heads && e < d) {
-          const Offsets f = offsets_of(a, j, item.token + t);
-          const char *row = j.g + f.g + h * j.gh;
-          x[u] = load_eight<T, VEC>(j.x + f.x + h * j.xh, j.xe, e, d);
-          g[u] = load_eight<T, VEC>(row, j.ge, e, d);
-          p[u] = load_partners<T, VEC>(row, j.ge, e, a.half, kind);
-          to[u] = j.out + f.o + h * j.oh;
-        }
-      }
-      if (base == 0 && kind != kPairsNone) {
-        fill_table(a, j, tab, item.token, item.tokens);
-        __syncthreads();
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        float v[kEight], h[kEight], q[kEight], square = 0.0f, cross = 0.0f;
-        if (to[u]) {
-#pragma unroll
-          for (int i = 0; i < kEight; ++i) {
-            v[i] = (float)x[u][i];
-            h[i] = (float)g[u][i];
-            q[i] = (float)p[u][i];
-          }
-          turn(h, q, tab.c + tt[u] * a.row, tab.s + tt[u] * a.row, e, a.half, kind);
-#pragma unroll
-          for (int i = 0; i < kEight; ++i) {
-            square = __builtin_fmaf(v[i], v[i], square);
-            cross = __builtin_fmaf(h[i] * w[i], v[i], cross);
-          }
-        }
-        square = sum_over_row(square, lanes);
-        cross = sum_over_row(cross, lanes);
-        if (!to[u]) continue;
-        const float r = __builtin_amdgcn_rsqf(square * a.over_d + a.eps), mean = cross * r * a.over_d;
+        for (int i = 0; i < kEight; ++i) v[i] = (float)x[i], h[i] = (float)g[i], q[i] = (float)p[i];
+        turn<KIND>(h, q, tab.c + t * a.row, tab.s + t * a.row, e, a.half);
 #pragma unroll
         for (int i = 0; i < kEight; ++i) {
-          const float unit = v[i] * r;
-          gw[i] = __builtin_fmaf(h[i], unit, gw[i]);
-          v[i] = r * (h[i] * w[i] - unit * mean);
+          square = __builtin_fmaf(v[i], v[i], square);
+          cross = __builtin_fmaf(h[i] * w[i], v[i], cross);
         }
-        store_eight<T, VEC>(to[u], j.oe, e, d, v);
       }
+      square = sum_over_row(square, lanes);
+      cross = sum_over_row(cross, lanes);
+      if (!mine) continue;
+      const float over = __builtin_amdgcn_rsqf(square * a.over_d + a.eps), mean = cross * over * a.over_d;
+#pragma unroll
+      for (int i = 0; i < kEight; ++i) {
+        const float unit = v[i] * over;
+        gw[i] = __builtin_fmaf(h[i], unit, gw[i]);
+        v[i] = over * (h[i] * w[i] - unit * mean);
+      }
+      store_eight<T, VEC>(j.out + along(a, j.ol, item.token + t) + n * j.oh, j.oe, e, d, v);
     }
     __syncthreads();
   }
@@ -419,6 +399,15 @@ __global__ __launch_bounds__(kBlock) void head_fold_kernel(const FoldArgs a) {
 // the cache
 // ---------------------------------------------------------------------------------------
 
+struct Slot { int64_t page; int place; };
+// (slots within 2^31 are divided in 32 bits)
+__device__ __forceinline__ Slot slot_of(const HeadArgs &a, int64_t slot) {
+  Slot s;
+  s.page = slot < 0x7fffffff ? (int64_t)fast_quotient((uint32_t)slot, a.page_div) : slot / a.page;
+  s.place = (int)(slot - s.page * a.page);
+  return s;
+}
+
 // nine significant bits of a float, ties to even, as a half
 __device__ __forceinline__ f16 nine_bits(float m) {
   const uint32_t b = __builtin_bit_cast(uint32_t, m);
@@ -427,123 +416,105 @@ __device__ __forceinline__ f16 nine_bits(float m) {
 
 // Keys and values into the cache: job 0 the keys, job 1 the values.  A group's 32 channels are four lanes'.  Each lane's eight codes are four
 // bytes of a token's row; the conversion of two floats to two codes is one instruction and rounds to nearest even.
-template <class T, bool VEC> __global__ __launch_bounds__(kBlock) void cache_append_kernel(const HeadArgs a, int kind_of_keys) {
-  constexpr int U = 2;
+template <class T, bool VEC, int KIND> __global__ __launch_bounds__(kBlock) void cache_append_kernel(const HeadArgs a) {
   __shared__ Table tab;
   const int lanes = 1 << a.lanes_log2, e = (threadIdx.x & (lanes - 1)) * kEight, rows = kBlock >> a.lanes_log2, d = a.d;
-  for (uint32_t it = blockIdx.x; it < a.items; it += gridDim.x) {
-    const Item item = item_of(a, it);
-    const HeadJob &j = *item.job;
-    const int kind = item.which ? (int)kPairsNone : kind_of_keys, total = item.tokens * j.per;
-    for (int base = 0; base < total; base += U * rows) {
-      eight_t<T> x[U], p[U];
-      int64_t slot[U];
-      int head[U], tt[U];
+  const Item item = item_of(a, a.first_item + blockIdx.x);
+  const HeadJob &j = a.job[item.which];
+  const int total = item.tokens * j.per;
+  for (int base = 0; base < total; base += rows) {
+    const int r = base + (threadIdx.x >> a.lanes_log2), t = (int)fast_quotient((uint32_t)r, j.per_div), h = item.head + r - t * j.per;
+    eight_t<T> x, p;
+    int64_t slot = -1;
+    if (r < total && h < j.heads) {
+      const char *row = j.x + along(a, j.xl, item.token + t) + h * j.xh;
+      slot = load_index(a.slots + along(a, a.slot_l, item.token + t), a.slots_wide);
+      x = load_eight<T, VEC>(row, j.xe, e, d);
+      if (!item.which) p = load_partners<T, KIND>(row, j.xe, e, a.half);
+    }
+    if (KIND != kPairsNone && base == 0 && !item.which) {
+      fill_table(a, tab, item.token, item.tokens);
+      __syncthreads();
+    }
+    float v[kEight], top = 0.0f;
+    bool fine = true;
+    const bool mine = slot >= 0 && slot < a.slot_count;
+    if (mine) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int r = base + u * rows + (threadIdx.x >> a.lanes_log2), t = (int)fast_quotient((uint32_t)r, j.per_div), h = item.head + r - t * j.per;
-        slot[u] = -1;
-        tt[u] = t;
-        head[u] = h;
-        if (r < total && h < j.heads) {
-          const Offsets f = offsets_of(a, j, item.token + t);
-          const char *row = j.x + f.x + h * j.xh;
-          slot[u] = load_index(a.slots + f.slot, a.slots_wide);
-          x[u] = load_eight<T, VEC>(row, j.xe, e, d);
-          p[u] = load_partners<T, VEC>(row, j.xe, e, a.half, kind);
-        }
+      for (int i = 0; i < kEight; ++i) v[i] = (float)x[i];
+      if (!item.which) {
+        float q[kEight];
+#pragma unroll
+        for (int i = 0; i < kEight; ++i) q[i] = (float)p[i];
+        turn<KIND>(v, q, tab.c + t * a.row, tab.s + t * a.row, e, a.half);
       }
-      if (base == 0 && kind != kPairsNone) {
-        fill_table(a, j, tab, item.token, item.tokens);
-        __syncthreads();
-      }
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        float v[kEight], q[kEight], top = 0.0f;
-        bool fine = true;
-        const bool mine = slot[u] >= 0 && slot[u] < a.slot_count;
-        if (mine) {
-#pragma unroll
-          for (int i = 0; i < kEight; ++i) {
-            v[i] = (float)x[u][i];
-            q[i] = (float)p[u][i];
-          }
-          turn(v, q, tab.c + tt[u] * a.row, tab.s + tt[u] * a.row, e, a.half, kind);
-#pragma unroll
-          for (int i = 0; i < kEight; ++i) {
-            top = fmaxf(top, __builtin_fabsf(v[i]));
-            fine &= __builtin_fabsf(v[i]) < __builtin_inff();
-          }
-        }
-        if (!fine) top = __builtin_inff();     // (not NaN, which maxima leave out)
-        top = fmaxf(top, __shfl_xor(top, 1));
-        top = fmaxf(top, __shfl_xor(top, 2));
-        if (!mine) continue;
-        const f16 scale = top == __builtin_inff() ? (f16)__builtin_nanf("") : nine_bits(fminf(top * (float)(1.0 / 12.0), 5456.0f));
-        // x / scale, correctly rounded: the reciprocal's quotient and one step with the exact remainder
-        const float s = (float)scale, inverse = s > 0.0f ? 1.0f / s : 0.0f;
-        uint32_t codes = 0;
-        float y[kEight];
-#pragma unroll
-        for (int i = 0; i < kEight; ++i) {
-          const float y0 = v[i] * inverse;
-          y[i] = __builtin_fmaf(__builtin_fmaf(-y0, s, v[i]), inverse, y0);
-          y[i] = __builtin_amdgcn_fmed3f(y[i], -12.0f, 12.0f);
-          if (!(s > 0.0f)) y[i] = __builtin_copysignf(0.0f, v[i]);
-        }
-        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, y[0], y[1], 2.0f, 0);
-        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, y[2], y[3], 2.0f, 1);
-        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, y[4], y[5], 2.0f, 2);
-        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, y[6], y[7], 2.0f, 3);
-        const int64_t page = slot[u] / a.page;
-        const int place = (int)(slot[u] - page * a.page);
-        char *block = a.cache + page * a.page_stride + head[u] * a.head_stride;
-        if (!item.which) {
-          *(uint32_t *)(block + block_k_codes(a.page, d, place, e)) = codes;
-        } else if (d == 64) {      // (four channels of a token lie together)
-          *(uint16_t *)(block + block_v_codes(a.page, d, place, e)) = (uint16_t)codes;
-          *(uint16_t *)(block + block_v_codes(a.page, d, place, e + 4)) = (uint16_t)(codes >> 16);
-        } else {
-          *(uint32_t *)(block + block_v_codes(a.page, d, place, e)) = codes;
-        }
-        if (e % 32 == 0) *(f16 *)(block + block_scale(a.page, d, item.which != 0, e / 32, place)) = scale;
+      for (int i = 0; i < kEight; ++i) {
+        top = fmaxf(top, __builtin_fabsf(v[i]));
+        fine &= __builtin_fabsf(v[i]) < __builtin_inff();
       }
     }
-    __syncthreads();
+    if (!fine) top = __builtin_inff();     // (not NaN, which maxima leave out)
+    top = fmaxf(top, __shfl_xor(top, 1));
+    top = fmaxf(top, __shfl_xor(top, 2));
+    if (!mine) continue;
+    const f16 scale = top == __builtin_inff() ? (f16)__builtin_nanf("") : nine_bits(fminf(top * (float)(1.0 / 12.0), 5456.0f));
+    // x / scale, correctly rounded: the reciprocal's quotient and one step with the exact remainder
+    const float s = (float)scale, inverse = s > 0.0f ? 1.0f / s : 0.0f;
+    uint32_t codes = 0;
+    float y[kEight];
+#pragma unroll
+    for (int i = 0; i < kEight; ++i) {
+      const float y0 = v[i] * inverse;
+      y[i] = __builtin_fmaf(__builtin_fmaf(-y0, s, v[i]), inverse, y0);
+      y[i] = __builtin_amdgcn_fmed3f(y[i], -12.0f, 12.0f);
+      if (!(s > 0.0f)) y[i] = __builtin_copysignf(0.0f, v[i]);
+    }
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, y[0], y[1], 2.0f, 0);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, y[2], y[3], 2.0f, 1);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, y[4], y[5], 2.0f, 2);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, y[6], y[7], 2.0f, 3);
+    const Slot at = slot_of(a, slot);
+    char *block = a.cache + at.page * a.page_stride + h * a.head_stride;
+    if (!item.which) {
+      *(uint32_t *)(block + block_k_codes(a.page, d, at.place, e)) = codes;
+    } else if (d == 64) {      // (four channels of a token lie together)
+      *(uint16_t *)(block + block_v_codes(a.page, d, at.place, e)) = (uint16_t)codes;
+      *(uint16_t *)(block + block_v_codes(a.page, d, at.place, e + 4)) = (uint16_t)(codes >> 16);
+    } else {
+      *(uint32_t *)(block + block_v_codes(a.page, d, at.place, e)) = codes;
+    }
+    if (e % 32 == 0) *(f16 *)(block + block_scale(a.page, d, item.which != 0, e / 32, at.place)) = scale;
   }
 }
 
 // The values at slots: job 0 the keys, job 1 the values.
 template <class T, bool VEC> __global__ __launch_bounds__(kBlock) void cache_read_kernel(const HeadArgs a) {
   const int lanes = 1 << a.lanes_log2, e = (threadIdx.x & (lanes - 1)) * kEight, rows = kBlock >> a.lanes_log2, d = a.d;
-  for (uint32_t it = blockIdx.x; it < a.items; it += gridDim.x) {
-    const Item item = item_of(a, it);
-    const HeadJob &j = *item.job;
-    const int total = item.tokens * j.per;
-    for (int r = threadIdx.x >> a.lanes_log2; r < total; r += rows) {
-      const int t = (int)fast_quotient((uint32_t)r, j.per_div), h = item.head + r - t * j.per;
-      if (h >= j.heads) continue;
-      const Offsets f = offsets_of(a, j, item.token + t);
-      const int64_t slot = load_index(a.slots + f.slot, a.slots_wide);
-      if (slot < 0 || slot >= a.slot_count) continue;
-      const int64_t page = slot / a.page;
-      const int place = (int)(slot - page * a.page);
-      const char *block = a.cache + page * a.page_stride + h * a.head_stride;
-      uint32_t codes;
-      if (!item.which)
-        codes = *(const uint32_t *)(block + block_k_codes(a.page, d, place, e));
-      else if (d == 64)
-        codes = *(const uint16_t *)(block + block_v_codes(a.page, d, place, e)) |
-                (uint32_t)*(const uint16_t *)(block + block_v_codes(a.page, d, place, e + 4)) << 16;
-      else
-        codes = *(const uint32_t *)(block + block_v_codes(a.page, d, place, e));
-      const float s = (float)*(const f16 *)(block + block_scale(a.page, d, item.which != 0, e / 32, place));
-      const f16x2 c0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, 2.0f, 0), c1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, 2.0f, 1);
-      const f16x2 c2 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, 2.0f, 2), c3 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, 2.0f, 3);
-      const float v[kEight] = {(float)c0.x * s, (float)c0.y * s, (float)c1.x * s, (float)c1.y * s,
-                               (float)c2.x * s, (float)c2.y * s, (float)c3.x * s, (float)c3.y * s};
-      store_eight<T, VEC>(j.out + f.o + h * j.oh, j.oe, e, d, v);
-    }
+  const Item item = item_of(a, a.first_item + blockIdx.x);
+  const HeadJob &j = a.job[item.which];
+  const int total = item.tokens * j.per;
+  for (int r = threadIdx.x >> a.lanes_log2; r < total; r += rows) {
+    const int t = (int)fast_quotient((uint32_t)r, j.per_div), h = item.head + r - t * j.per;
+    if (h >= j.heads) continue;
+    const int64_t slot = load_index(a.slots + along(a, a.slot_l, item.token + t), a.slots_wide);
+    if (slot < 0 || slot >= a.slot_count) continue;
+    const Slot at = slot_of(a, slot);
+    const char *block = a.cache + at.page * a.page_stride + h * a.head_stride;
+    uint32_t codes;
+    if (!item.which)
+      codes = *(const uint32_t *)(block + block_k_codes(a.page, d, at.place, e));
+    else if (d == 64)
+      codes = *(const uint16_t *)(block + block_v_codes(a.page, d, at.place, e)) |
+              (uint32_t)*(const uint16_t *)(block + block_v_codes(a.page, d, at.place, e + 4)) << 16;
+    else
+      codes = *(const uint32_t *)(block + block_v_codes(a.page, d, at.place, e));
+    const float s = (float)*(const f16 *)(block + block_scale(a.page, d, item.which != 0, e / 32, at.place));
+    const f16x2 c0 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, 2.0f, 0), c1 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, 2.0f, 1);
+    const f16x2 c2 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, 2.0f, 2), c3 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, 2.0f, 3);
+    const float v[kEight] = {(float)c0.x * s, (float)c0.y * s, (float)c1.x * s, (float)c1.y * s,
+                             (float)c2.x * s, (float)c2.y * s, (float)c3.x * s, (float)c3.y * s};
+    store_eight<T, VEC>(j.out + along(a, j.ol, item.token + t) + h * j.oh, j.oe, e, d, v);
   }
 }
 
@@ -612,23 +583,18 @@ bool shape_of_launch(HeadArgs &a, const ocn_rotation *r, int64_t d, int jobs) {
     a.freq = (const char *)r->frequencies->base + r->frequencies->offset;
     a.freq_stride = r->frequencies->stride[0];
   }
-  // Rows of an item: four passes of the workgroup's lanes share the cosines; one where that leaves CUs without work.
+  // Rows of an item: up to kPasses passes of the workgroup's lanes share the cosines, fewer where that leaves CUs without work.
   const int rows = kBlock >> a.lanes_log2;
-  int64_t all = 0;
+  int64_t all = 0, want = kPasses * rows, items = 0;
   for (int i = 0; i < jobs; ++i) all += (int64_t)a.lead.tokens * a.job[i].heads;
-  int64_t want = 4 * rows;
-  while (want > rows && all / want < 2 * kNumCUs) want /= 2;
-  int64_t most_tokens = r ? std::max<int64_t>(1, kTable / a.row) : 64;
-  int64_t heads = 1;
-  for (int i = 0; i < jobs; ++i) heads = std::max<int64_t>(heads, a.job[i].heads);
-  a.per_tokens = (int32_t)std::min<int64_t>(most_tokens, std::max<int64_t>(1, want / heads));
-  const int64_t blocks = (a.lead.tokens + a.per_tokens - 1) / a.per_tokens;
-  int64_t items = 0;
+  while (want > rows && all / want < 8 * kNumCUs) want /= 2;
+  const int64_t most_tokens = r ? std::max<int64_t>(1, kTable / a.row) : 64;
   for (int i = 0; i < jobs; ++i) {
     HeadJob &j = a.job[i];
-    const int64_t parts = std::max<int64_t>(1, ((int64_t)j.heads * a.per_tokens + want - 1) / want);
+    const int64_t parts = std::max<int64_t>(1, (j.heads + want - 1) / want);
     j.per = (int32_t)std::max<int64_t>(1, (j.heads + parts - 1) / parts);
-    const int64_t across = j.heads ? (j.heads + j.per - 1) / j.per : 0;
+    j.per_tokens = (int32_t)std::min<int64_t>(most_tokens, std::max<int64_t>(1, want / j.per));
+    const int64_t blocks = ((int64_t)a.lead.tokens + j.per_tokens - 1) / j.per_tokens, across = j.heads ? (j.heads + j.per - 1) / j.per : 0;
     j.per_div = make_fastdiv((uint32_t)j.per);
     j.blocks_div = make_fastdiv((uint32_t)std::max<int64_t>(across, 1));
     j.items = (uint32_t)(blocks * across);
@@ -651,14 +617,39 @@ int check_weight(const ocn_tensor *w, int64_t channels) {
   return w->ndim != 1 || w->size[0] != channels ? OCN_ERR_SHAPE : OCN_OK;
 }
 
-#define OCN_BY_TYPE(dtype, vec, CALL)                                            \
-  do {                                                                           \
-    if ((dtype) == OCN_HALF) { if (vec) CALL(f16, true); else CALL(f16, false); } \
-    else if ((dtype) == OCN_BFLOAT16) { if (vec) CALL(bf16, true); else CALL(bf16, false); } \
-    else { if (vec) CALL(float, true); else CALL(float, false); }                \
+// CALL(type, whole vectors, kind of pairs) for a launch's
+#define OCN_BY_KIND(T, vec, k, CALL)                        \
+  do {                                                      \
+    if (vec) {                                              \
+      if ((k) == kPairsNone) CALL(T, true, kPairsNone);  \
+      else if ((k) == kPairsInside) CALL(T, true, kPairsInside); \
+      else if ((k) == kPairsEight) CALL(T, true, kPairsEight);   \
+      else if ((k) == kPairsFour) CALL(T, true, kPairsFour);     \
+      else CALL(T, true, kPairsOne);                        \
+    } else {                                                \
+      if ((k) == kPairsNone) CALL(T, false, kPairsNone); \
+      else if ((k) == kPairsInside) CALL(T, false, kPairsInside); \
+      else CALL(T, false, kPairsOne);                       \
+    }                                                       \
+  } while (0)
+#define OCN_BY_TYPE(dtype, vec, kind, CALL)                             \
+  do {                                                                  \
+    const int pairs_ = (kind);                                          \
+    if ((dtype) == OCN_HALF) OCN_BY_KIND(f16, vec, pairs_, CALL);       \
+    else if ((dtype) == OCN_BFLOAT16) OCN_BY_KIND(bf16, vec, pairs_, CALL); \
+    else OCN_BY_KIND(float, vec, pairs_, CALL);                         \
   } while (0)
 
-uint32_t grid_of(uint32_t items) { return (uint32_t)std::min<int64_t>(items, max_launch_blocks()); }
+// `launch` for all items, as many at a time as a launch may have
+template <class Launch> int for_all_items(HeadArgs &a, Launch launch) {
+  for (int64_t at = 0; at < a.items; at += max_launch_blocks()) {
+    a.first_item = (uint32_t)at;
+    launch((uint32_t)std::min<int64_t>(a.items - at, max_launch_blocks()));
+    const int rc = done(hipGetLastError());
+    if (rc != OCN_OK) return rc;
+  }
+  return OCN_OK;
+}
 
 int run_rows(bool norm, const ocn_tensor *const *x, const ocn_tensor *const *w, const ocn_tensor *const *out, int jobs, double eps,
              const ocn_rotation *r, bool back, hipStream_t stream) {
@@ -713,15 +704,15 @@ int run_rows(bool norm, const ocn_tensor *const *x, const ocn_tensor *const *w, 
   a.eps = (float)eps;
   a.sign = back ? -1.0f : 1.0f;
   const int kind = kind_of_pairs(r, vec);
-  const uint32_t grid = grid_of(a.items);
-#define OCN_ROWS(T, VEC)                                                                                          \
-  do {                                                                                                            \
-    if (norm) hipLaunchKernelGGL((head_rows_kernel<T, VEC, true>), dim3(grid), dim3(kBlock), 0, stream, a, kind);  \
-    else hipLaunchKernelGGL((head_rows_kernel<T, VEC, false>), dim3(grid), dim3(kBlock), 0, stream, a, kind);      \
+  return for_all_items(a, [&](uint32_t grid) {
+#define OCN_ROWS(T, VEC, KIND)                                                                                           \
+  do {                                                                                                                   \
+    if (norm) hipLaunchKernelGGL((head_rows_kernel<T, VEC, KIND, true>), dim3(grid), dim3(kBlock), 0, stream, a);         \
+    else if constexpr (KIND != kPairsNone) hipLaunchKernelGGL((head_rows_kernel<T, VEC, KIND, false>), dim3(grid), dim3(kBlock), 0, stream, a); \
   } while (0)
-  OCN_BY_TYPE(x[0]->dtype, vec, OCN_ROWS);
+    OCN_BY_TYPE(x[0]->dtype, vec, kind, OCN_ROWS);
 #undef OCN_ROWS
-  return done(hipGetLastError());
+  });
 }
 
 // k, v, slots and cache of ocn_cache_append (out: false) and ocn_cache_read (true); either of k and v may be null in the latter
@@ -779,20 +770,20 @@ int run_cache(const ocn_tensor *k, const ocn_tensor *v, const ocn_rotation *r, c
   a.page_stride = cache->stride[0];
   a.head_stride = cache->stride[1];
   a.page = (int32_t)page;
+  a.page_div = make_fastdiv((uint32_t)page);
   a.slot_count = cache->size[0] * page;
   if (!shape_of_launch(a, r, d, 2)) return OCN_ERR_SHAPE;
   if (a.items == 0 || a.slot_count == 0) return OCN_OK;
   a.sign = 1.0f;
   const int kind = kind_of_pairs(r, vec);
-  const uint32_t grid = grid_of(a.items);
-#define OCN_CACHE(T, VEC)                                                                                        \
-  do {                                                                                                           \
-    if (out) hipLaunchKernelGGL((cache_read_kernel<T, VEC>), dim3(grid), dim3(kBlock), 0, stream, a);            \
-    else hipLaunchKernelGGL((cache_append_kernel<T, VEC>), dim3(grid), dim3(kBlock), 0, stream, a, kind);        \
-  } while (0)
-  OCN_BY_TYPE(first->dtype, vec, OCN_CACHE);
-#undef OCN_CACHE
-  return done(hipGetLastError());
+  return for_all_items(a, [&](uint32_t grid) {
+#define OCN_READ(T, VEC, KIND) hipLaunchKernelGGL((cache_read_kernel<T, VEC>), dim3(grid), dim3(kBlock), 0, stream, a)
+#define OCN_APPEND(T, VEC, KIND) hipLaunchKernelGGL((cache_append_kernel<T, VEC, KIND>), dim3(grid), dim3(kBlock), 0, stream, a)
+    if (out) OCN_BY_TYPE(first->dtype, vec, kPairsNone, OCN_READ);
+    else OCN_BY_TYPE(first->dtype, vec, kind, OCN_APPEND);
+#undef OCN_READ
+#undef OCN_APPEND
+  });
 }
 
 // workgroups that sum one job's gradient of weights
@@ -914,8 +905,8 @@ int ocn_norm_rotary_grad(const ocn_tensor *q_gout, const ocn_tensor *q, const oc
   a.sign = -1.0f;
   const int kind = kind_of_pairs(rotation, vec), across = std::max(f.count[0], f.count[1]);
   const hipStream_t s = (hipStream_t)stream;
-#define OCN_GRAD(T, VEC) hipLaunchKernelGGL((head_grad_kernel<T, VEC>), dim3(across, jobs), dim3(kBlock), 0, s, a, kind)
-  OCN_BY_TYPE(q->dtype, vec, OCN_GRAD);
+#define OCN_GRAD(T, VEC, KIND) hipLaunchKernelGGL((head_grad_kernel<T, VEC, KIND>), dim3(across, jobs), dim3(kBlock), 0, s, a)
+  OCN_BY_TYPE(q->dtype, vec, kind, OCN_GRAD);
 #undef OCN_GRAD
   rc = done(hipGetLastError());
   if (rc != OCN_OK || !sums) return rc;
