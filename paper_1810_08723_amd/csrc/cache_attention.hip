@@ -5,6 +5,7 @@
 #include <cmath>
 #include <cstring>
 
+#include "dev_types.hpp"
 #include "head_types.hpp"
 #include "heads.hpp"
 
@@ -471,6 +472,7 @@ __global__ __launch_bounds__(kBlock, D * RT <= 128 ? 2 : 1) void attention_kerne
   __shared__ float tops[W][RT][16], totals[W][RT][16];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), n = lane % 16, g = lane / 16;
   const LaneOffsets lanes = lane_offsets<D>(a, n, g);
+  warm_arguments<AttentionArgs>();
   const uint32_t item = a.first_item + blockIdx.x;
   // Items: blocks of rows fastest, then heads of the cache, sequences, and splits: workgroups go to the XCDs in turn, and where sequences are
   // of different lengths the later splits are empty (with splits fastest some XCDs had most of the work: 105 for 44 us).

@@ -14,6 +14,7 @@
 #include <algorithm>
 #include <cstring>
 
+#include "dev_types.hpp"
 #include "head_types.hpp"
 #include "heads.hpp"
 
@@ -21,9 +22,13 @@ namespace ocn {
 namespace {
 
 constexpr int kEight = 8;              // channels of a lane
-constexpr int kTable = 2048;           // cosines, and sines, that a workgroup holds
-constexpr int kPasses = 8;              // of a workgroup's lanes over its rows, at most
-constexpr int kFoldBlocks = 512;       // workgroups that sum a gradient of weights, at most
+constexpr int kTable = 2048;           // channels, of all its tokens, that a workgroup holds factors of
+constexpr int kPasses = 4;              // of a workgroup's lanes over its rows, at most
+constexpr int kFoldBlocks = 1024;      // workgroups that sum a gradient of weights, at most
+
+// Where the pairs of a lane's eight channels lie.  kPairsInside: among the eight; kPairsEight: the partners of all eight are eight more
+// channels in a row; kPairsFour: of each half of them; kPairsOne: anywhere.
+enum { kPairsNone = 0, kPairsInside, kPairsEight, kPairsFour, kPairsOne };
 
 // ---------------------------------------------------------------------------------------
 // arguments
@@ -37,6 +42,7 @@ struct HeadJob {                       // one tensor of heads
   int64_t xl[kMaxLead], gl[kMaxLead], ol[kMaxLead];
   int64_t weight_stride;
   int32_t weight_type;
+  bool stream;                         // the output is too large to stay cached
   int32_t heads, per, per_tokens;      // heads of a token; heads and tokens of an item
   FastDiv per_div, blocks_div;         // by `per`; by items along the heads
   uint32_t items;
@@ -53,7 +59,7 @@ struct HeadArgs {
   float sign;                          // -1: turned back
   float eps, over_d;
   int32_t pos_wide, interleaved;
-  int32_t half, row;                   // pairs of a head; floats from one token's cosines to the next
+  int32_t half, row;                   // pairs of a head; floats of a token in the table
   FastDiv half_div;
   int32_t d, lanes_log2;               // channels; lanes of a row
   uint32_t items, first_item;          // of all launches; of this one
@@ -84,24 +90,29 @@ __device__ __forceinline__ int64_t along(const HeadArgs &a, const int64_t *strid
 
 // sin and cos of t: t less a multiple of pi/2 (in two parts, the first 53 bits and the next 53), then the Taylor series up to
 // x^15 and x^16, whose remainders on [-pi/4, pi/4] are below 2^-54.
+// (The coefficients are kept in scalar registers: the compiler puts them all in vector registers, 32 of them, and the kernels around this lose wavefronts.)
+__device__ __forceinline__ double scalar(double x) {
+  asm("" : "+s"(x));
+  return x;
+}
 __device__ __forceinline__ void sine_cosine(double t, double *s, double *c) {
-  const double n = __builtin_rint(t * 0.63661977236758134308);
-  double x = __builtin_fma(-n, 1.57079632679489655800, t);
-  x = __builtin_fma(-n, 6.12323399573676603587e-17, x);
+  const double n = __builtin_rint(t * scalar(0.63661977236758134308));
+  double x = __builtin_fma(-n, scalar(1.57079632679489655800), t);
+  x = __builtin_fma(-n, scalar(6.12323399573676603587e-17), x);
   const double z = x * x;
-  double p = -1.0 / 1307674368000.0, q = 1.0 / 20922789888000.0;
-  p = __builtin_fma(p, z, 1.0 / 6227020800.0);
-  q = __builtin_fma(q, z, -1.0 / 87178291200.0);
-  p = __builtin_fma(p, z, -1.0 / 39916800.0);
-  q = __builtin_fma(q, z, 1.0 / 479001600.0);
-  p = __builtin_fma(p, z, 1.0 / 362880.0);
-  q = __builtin_fma(q, z, -1.0 / 3628800.0);
-  p = __builtin_fma(p, z, -1.0 / 5040.0);
-  q = __builtin_fma(q, z, 1.0 / 40320.0);
-  p = __builtin_fma(p, z, 1.0 / 120.0);
-  q = __builtin_fma(q, z, -1.0 / 720.0);
-  p = __builtin_fma(p, z, -1.0 / 6.0);
-  q = __builtin_fma(q, z, 1.0 / 24.0);
+  double p = scalar(-1.0 / 1307674368000.0), q = scalar(1.0 / 20922789888000.0);
+  p = __builtin_fma(p, z, scalar(1.0 / 6227020800.0));
+  q = __builtin_fma(q, z, scalar(-1.0 / 87178291200.0));
+  p = __builtin_fma(p, z, scalar(-1.0 / 39916800.0));
+  q = __builtin_fma(q, z, scalar(1.0 / 479001600.0));
+  p = __builtin_fma(p, z, scalar(1.0 / 362880.0));
+  q = __builtin_fma(q, z, scalar(-1.0 / 3628800.0));
+  p = __builtin_fma(p, z, scalar(-1.0 / 5040.0));
+  q = __builtin_fma(q, z, scalar(1.0 / 40320.0));
+  p = __builtin_fma(p, z, scalar(1.0 / 120.0));
+  q = __builtin_fma(q, z, scalar(-1.0 / 720.0));
+  p = __builtin_fma(p, z, scalar(-1.0 / 6.0));
+  q = __builtin_fma(q, z, scalar(1.0 / 24.0));
   q = __builtin_fma(q, z, -0.5);
   p = __builtin_fma(p * z, x, x);
   q = __builtin_fma(q, z, 1.0);
@@ -111,27 +122,34 @@ __device__ __forceinline__ void sine_cosine(double t, double *s, double *c) {
   *c = (quarter + 1) & 2 ? -b : b;
 }
 
-struct alignas(16) Table { float c[kTable], s[kTable]; };
+// For each of the channels that rotate, of each token of an item: what the channel and its partner in the pair are multiplied by.  (Weights of a norm
+// are in them already, and the signs: a channel takes two products and a sum.)
+struct alignas(16) Table { float own[kTable], other[kTable]; };
 
-__device__ __forceinline__ void fill_table(const HeadArgs &a, Table &tab, uint32_t token, int tokens) {
+template <int KIND> __device__ __forceinline__ void fill_table(const HeadArgs &a, const HeadJob &j, Table &tab, uint32_t token, int tokens, bool weights) {
 #pragma nounroll
   for (int i = threadIdx.x; i < tokens * a.half; i += kBlock) {
     const int t = (int)fast_quotient((uint32_t)i, a.half_div), p = i - t * a.half;
     const int64_t at = load_index(a.pos + along(a, a.pos_l, token + t), a.pos_wide);
     double s, c;
     sine_cosine((double)at * *(const double *)(a.freq + p * a.freq_stride), &s, &c);
-    tab.c[t * a.row + p] = (float)(c * a.magnitude);
-    tab.s[t * a.row + p] = (float)(s * a.magnitude) * a.sign;
+    const float cc = (float)(c * a.magnitude), ss = (float)(s * a.magnitude) * a.sign;
+    const int one = KIND == kPairsInside ? 2 * p : p, two = KIND == kPairsInside ? 2 * p + 1 : p + a.half;
+    float w1 = 1.0f, w2 = 1.0f;
+    if (weights && j.weight) {
+      w1 = load_as_float(j.weight + one * j.weight_stride, j.weight_type);
+      w2 = load_as_float(j.weight + two * j.weight_stride, j.weight_type);
+    }
+    tab.own[t * a.row + one] = cc * w1;
+    tab.other[t * a.row + one] = -ss * w2;
+    tab.own[t * a.row + two] = cc * w2;
+    tab.other[t * a.row + two] = ss * w1;
   }
 }
 
 // ---------------------------------------------------------------------------------------
 // rows
 // ---------------------------------------------------------------------------------------
-
-// Where the pairs of a lane's eight channels lie.  kPairsInside: among the eight; kPairsEight: the partners of all eight are eight more
-// channels in a row; kPairsFour: of each half of them; kPairsOne: anywhere.
-enum { kPairsNone = 0, kPairsInside, kPairsEight, kPairsFour, kPairsOne };
 
 template <class T> using eight_t = typename Eight<T>::V;
 template <class T> struct Four { typedef T V __attribute__((ext_vector_type(4))); };
@@ -147,12 +165,19 @@ template <class T, bool VEC> __device__ __forceinline__ eight_t<T> load_eight(co
     return v;
   }
 }
-template <class T, bool VEC> __device__ __forceinline__ void store_eight(char *row, int64_t step, int e, int d, const float *v) {
+// (stream: past the caches, for outputs that they could not keep)
+template <class T, bool VEC> __device__ __forceinline__ void store_eight(char *row, int64_t step, int e, int d, const float *v, bool stream) {
   if constexpr (VEC) {
     eight_t<T> o;
 #pragma unroll
     for (int i = 0; i < kEight; ++i) o[i] = (T)v[i];
-    *(eight_t<T> *)(row + e * (int)sizeof(T)) = o;
+    if (stream) {
+      asm volatile("");     // (these keep the two apart: made into one store, they would be an ordinary one)
+      __builtin_nontemporal_store(o, (eight_t<T> *)(row + e * (int)sizeof(T)));
+      asm volatile("");
+    } else {
+      *(eight_t<T> *)(row + e * (int)sizeof(T)) = o;
+    }
   } else {
 #pragma unroll
     for (int i = 0; i < kEight; ++i)
@@ -185,38 +210,33 @@ template <class T, int KIND> __device__ __forceinline__ eight_t<T> load_partners
   return v;
 }
 
-// x turned; p: the partners (of pairs that lie apart)
-template <int KIND> __device__ __forceinline__ void turn(float *x, const float *p, const float *c, const float *s, int e, int half) {
-  if constexpr (KIND == kPairsInside) {
+// x turned, with the row's part of the table; p: the partners of pairs that lie apart
+template <int KIND> __device__ __forceinline__ void turn(float *x, const float *p, const float *own, const float *other, int e, int half) {
+  if constexpr (KIND == kPairsNone) return;
+  if (e >= 2 * half) return;
+  float q[kEight];
 #pragma unroll
-    for (int i = 0; i < kEight; i += 2) {
-      if (e + i >= 2 * half) continue;
-      const float a = x[i], b = x[i + 1], cc = c[e / 2 + i / 2], ss = s[e / 2 + i / 2];
-      x[i] = a * cc - b * ss;
-      x[i + 1] = b * cc + a * ss;
-    }
-  } else if constexpr (KIND == kPairsEight) {
-    if (e >= 2 * half) return;
-    const int at = e < half ? e : e - half;
-    f32x4 cc[2], ss[2];
+  for (int i = 0; i < kEight; ++i) q[i] = KIND == kPairsInside ? x[i ^ 1] : p[i];
+  // (a token's part of the table is padded to eights)
+  f32x4 a[2], b[2];
 #pragma unroll
-    for (int k = 0; k < 2; ++k) cc[k] = *(const f32x4 *)(c + at + 4 * k), ss[k] = *(const f32x4 *)(s + at + 4 * k);
+  for (int k = 0; k < 2; ++k) a[k] = *(const f32x4 *)(own + e + 4 * k), b[k] = *(const f32x4 *)(other + e + 4 * k);
 #pragma unroll
-    for (int i = 0; i < kEight; ++i) x[i] = x[i] * cc[i / 4][i % 4] + p[i] * (e < half ? -ss[i / 4][i % 4] : ss[i / 4][i % 4]);
-  } else if constexpr (KIND != kPairsNone) {
-#pragma unroll
-    for (int i = 0; i < kEight; ++i) {
-      const int f = e + i;
-      if (f >= 2 * half) continue;
-      const int at = f < half ? f : f - half;
-      const float ss = s[at];
-      x[i] = x[i] * c[at] + p[i] * (f < half ? -ss : ss);
-    }
-  }
+  for (int i = 0; i < kEight; ++i)
+    if (KIND == kPairsEight || e + i < 2 * half) x[i] = x[i] * a[i / 4][i % 4] + q[i] * b[i / 4][i % 4];
 }
 
+template <int CTRL> __device__ __forceinline__ float other_lane(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+}
+// the sum over a row's lanes (1, 2, 4 ... 64 of them): exchanges inside sixteen lanes cost no trip through LDS
 __device__ __forceinline__ float sum_over_row(float v, int lanes) {
-  for (int m = 1; m < lanes; m <<= 1) v += __shfl_xor(v, m);
+  if (lanes > 1) v += other_lane<0xb1>(v);      // 1 0 3 2
+  if (lanes > 2) v += other_lane<0x4e>(v);      // 2 3 0 1
+  if (lanes > 4) v += other_lane<0x141>(v);     // eight lanes mirrored
+  if (lanes > 8) v += other_lane<0x140>(v);     // sixteen lanes mirrored
+  if (lanes > 16) v += __shfl_xor(v, 16);
+  if (lanes > 32) v += __shfl_xor(v, 32);
   return v;
 }
 
@@ -235,26 +255,17 @@ __device__ __forceinline__ Item item_of(const HeadArgs &a, uint32_t i) {
   return r;
 }
 
-// a lane's weights: those of its channels, and of their partners
-template <int KIND> __device__ __forceinline__ void load_weights(const HeadJob &j, int d, int e, int half, float *w, float *wp) {
-#pragma unroll
-  for (int i = 0; i < kEight; ++i) {
-    const int f = e + i, g = f < half ? f + half : f - half;
-    w[i] = j.weight && f < d ? load_as_float(j.weight + f * j.weight_stride, j.weight_type) : 1.0f;
-    wp[i] = j.weight && KIND >= kPairsEight && f < 2 * half ? load_as_float(j.weight + g * j.weight_stride, j.weight_type) : 1.0f;
-  }
-}
-
 // Rotation, with the norm before it where NORM is set.  (No loop over items in the kernel: what their first instructions share would be kept in registers;
 // launches take up to as many as a launch may have.)
 template <class T, bool VEC, int KIND, bool NORM> __global__ __launch_bounds__(kBlock) void head_rows_kernel(const HeadArgs a) {
+  warm_arguments<HeadArgs>();
   constexpr int U = 2;                  // rows of a lane at a time
   __shared__ Table tab;
   const int lanes = 1 << a.lanes_log2, e = (threadIdx.x & (lanes - 1)) * kEight, rows = kBlock >> a.lanes_log2, d = a.d;
   const Item item = item_of(a, a.first_item + blockIdx.x);
   const HeadJob &j = a.job[item.which];
   const int total = item.tokens * j.per;
-  float w[kEight], wp[kEight];
+  float w[kEight];                      // of channels that do not rotate
   for (int base = 0; base < total; base += U * rows) {
     eight_t<T> x[U], p[U];
     char *to[U];
@@ -272,9 +283,13 @@ template <class T, bool VEC, int KIND, bool NORM> __global__ __launch_bounds__(k
       }
     }
     if (base == 0) {
-      if constexpr (NORM) load_weights<KIND>(j, d, e, a.half, w, wp);
+      if constexpr (NORM) {
+#pragma unroll
+        for (int i = 0; i < kEight; ++i)
+          w[i] = j.weight && e + i >= 2 * a.half && e + i < d ? load_as_float(j.weight + (e + i) * j.weight_stride, j.weight_type) : 1.0f;
+      }
       if constexpr (KIND != kPairsNone) {
-        fill_table(a, tab, item.token, item.tokens);
+        fill_table<KIND>(a, j, tab, item.token, item.tokens, NORM);
         __syncthreads();
       }
     }
@@ -296,11 +311,11 @@ template <class T, bool VEC, int KIND, bool NORM> __global__ __launch_bounds__(k
         q[i] = (float)p[u][i];
         if constexpr (NORM) {
           v[i] = v[i] * r * w[i];
-          q[i] = q[i] * r * wp[i];
+          q[i] = q[i] * r;
         }
       }
-      turn<KIND>(v, q, tab.c + tt[u] * a.row, tab.s + tt[u] * a.row, e, a.half);
-      store_eight<T, VEC>(to[u], j.oe, e, d, v);
+      turn<KIND>(v, q, tab.own + tt[u] * a.row, tab.other + tt[u] * a.row, e, a.half);
+      store_eight<T, VEC>(to[u], j.oe, e, d, v, j.stream);
     }
   }
 }
@@ -310,8 +325,10 @@ template <class T, bool VEC, int KIND, bool NORM> __global__ __launch_bounds__(k
 // A lane keeps its channels' sums over all rows of its workgroup; workgroups leave theirs in the workspace, and a second launch
 // adds those up in a fixed order: no atomics, the same bits every time.
 template <class T, bool VEC, int KIND> __global__ __launch_bounds__(kBlock) void head_grad_kernel(const HeadArgs a) {
+  warm_arguments<HeadArgs>();
   __shared__ Table tab;
-  __shared__ float sums[kBlock * kEight];
+  static_assert(kTable >= kBlock * kEight, "the sums take the table's place");
+  float *const sums = tab.own;
   const int lanes = 1 << a.lanes_log2, e = (threadIdx.x & (lanes - 1)) * kEight, rows = kBlock >> a.lanes_log2, d = a.d;
   // a workgroup's items are of one job: blockIdx.y
   const HeadJob &j = a.job[blockIdx.y];
@@ -325,39 +342,54 @@ template <class T, bool VEC, int KIND> __global__ __launch_bounds__(kBlock) void
   for (uint32_t it = blockIdx.x; it < j.items; it += j.workers) {
     const Item item = item_of(a, it + (blockIdx.y ? a.job[0].items : 0));
     const int total = item.tokens * j.per;
+    // two rows of a lane are on their way while it works on one
+    eight_t<T> x[2], g[2], p[2];
+    const auto load = [&](int base, int u) {
+      const int r = base + (threadIdx.x >> a.lanes_log2), t = (int)fast_quotient((uint32_t)r, j.per_div), n = item.head + r - t * j.per;
+      if (r < total && n < j.heads && e < d) {
+        const char *row = j.g + along(a, j.gl, item.token + t) + n * j.gh;
+        x[u] = load_eight<T, VEC>(j.x + along(a, j.xl, item.token + t) + n * j.xh, j.xe, e, d);
+        g[u] = load_eight<T, VEC>(row, j.ge, e, d);
+        p[u] = load_partners<T, KIND>(row, j.ge, e, a.half);
+      }
+    };
+    load(0, 0);
+    load(rows, 1);
     if constexpr (KIND != kPairsNone) {
-      fill_table(a, tab, item.token, item.tokens);
+      fill_table<KIND>(a, j, tab, item.token, item.tokens, false);
       __syncthreads();
     }
-    for (int base = 0; base < total; base += rows) {
-      const int r = base + (threadIdx.x >> a.lanes_log2), t = (int)fast_quotient((uint32_t)r, j.per_div), n = item.head + r - t * j.per;
-      const bool mine = r < total && n < j.heads && e < d;
-      float v[kEight], h[kEight], square = 0.0f, cross = 0.0f;
-      if (mine) {
-        const char *row = j.g + along(a, j.gl, item.token + t) + n * j.gh;
-        const eight_t<T> x = load_eight<T, VEC>(j.x + along(a, j.xl, item.token + t) + n * j.xh, j.xe, e, d);
-        const eight_t<T> g = load_eight<T, VEC>(row, j.ge, e, d), p = load_partners<T, KIND>(row, j.ge, e, a.half);
-        float q[kEight];
+    for (int both = 0; both < total; both += 2 * rows) {
 #pragma unroll
-        for (int i = 0; i < kEight; ++i) v[i] = (float)x[i], h[i] = (float)g[i], q[i] = (float)p[i];
-        turn<KIND>(h, q, tab.c + t * a.row, tab.s + t * a.row, e, a.half);
+      for (int u = 0; u < 2; ++u) {
+        const int base = both + u * rows, r = base + (threadIdx.x >> a.lanes_log2), t = (int)fast_quotient((uint32_t)r, j.per_div), n = item.head + r - t * j.per;
+        const bool mine = r < total && n < j.heads && e < d;
+        float v[kEight], h[kEight], square = 0.0f, cross = 0.0f;
+        if (mine) {
+          float q[kEight];
 #pragma unroll
-        for (int i = 0; i < kEight; ++i) {
-          square = __builtin_fmaf(v[i], v[i], square);
-          cross = __builtin_fmaf(h[i] * w[i], v[i], cross);
+          for (int i = 0; i < kEight; ++i) v[i] = (float)x[u][i], h[i] = (float)g[u][i], q[i] = (float)p[u][i];
+          turn<KIND>(h, q, tab.own + t * a.row, tab.other + t * a.row, e, a.half);
+#pragma unroll
+          for (int i = 0; i < kEight; ++i) {
+            square = __builtin_fmaf(v[i], v[i], square);
+            cross = __builtin_fmaf(h[i] * w[i], v[i], cross);
+          }
+        }
+        load(base + 2 * rows, u);
+        square = sum_over_row(square, lanes);
+        cross = sum_over_row(cross, lanes);
+        if (mine) {
+          const float over = __builtin_amdgcn_rsqf(square * a.over_d + a.eps), mean = cross * over * a.over_d;
+#pragma unroll
+          for (int i = 0; i < kEight; ++i) {
+            const float unit = v[i] * over;
+            gw[i] = __builtin_fmaf(h[i], unit, gw[i]);
+            v[i] = over * (h[i] * w[i] - unit * mean);
+          }
+          store_eight<T, VEC>(j.out + along(a, j.ol, item.token + t) + n * j.oh, j.oe, e, d, v, j.stream);
         }
       }
-      square = sum_over_row(square, lanes);
-      cross = sum_over_row(cross, lanes);
-      if (!mine) continue;
-      const float over = __builtin_amdgcn_rsqf(square * a.over_d + a.eps), mean = cross * over * a.over_d;
-#pragma unroll
-      for (int i = 0; i < kEight; ++i) {
-        const float unit = v[i] * over;
-        gw[i] = __builtin_fmaf(h[i], unit, gw[i]);
-        v[i] = over * (h[i] * w[i] - unit * mean);
-      }
-      store_eight<T, VEC>(j.out + along(a, j.ol, item.token + t) + n * j.oh, j.oe, e, d, v);
     }
     __syncthreads();
   }
@@ -372,6 +404,8 @@ template <class T, bool VEC, int KIND> __global__ __launch_bounds__(kBlock) void
   }
 }
 
+constexpr int kFoldLanes = 1024;
+
 struct FoldArgs {
   const float *partial[2];
   char *out[2];
@@ -380,19 +414,21 @@ struct FoldArgs {
 };
 
 // eight channels of a job have a workgroup; sums of sums in double precision
-__global__ __launch_bounds__(kBlock) void head_fold_kernel(const FoldArgs a) {
-  __shared__ double part[kBlock];
-  const int which = blockIdx.y, c = blockIdx.x * kEight + (threadIdx.x & 7);
+__global__ __launch_bounds__(kFoldLanes) void head_fold_kernel(const FoldArgs a) {
+  __shared__ double part[kFoldLanes / 8][8];
+  const int which = blockIdx.y, lane = threadIdx.x & 7, row = threadIdx.x >> 3, c = blockIdx.x * 8 + lane;
   if (!a.out[which]) return;
   double s = 0.0;
-  if (c < a.d)
-    for (int i = threadIdx.x >> 3; i < a.count[which]; i += kBlock / 8) s += a.partial[which][(int64_t)i * a.d + c];
-  part[threadIdx.x] = s;
-  __syncthreads();
-  if (threadIdx.x < 8 && c < a.d) {
-    for (int i = 1; i < kBlock / 8; ++i) s += part[i * 8 + threadIdx.x];
-    store_from_float(a.out[which] + c * a.stride[which], a.type[which], (float)s);
+  if (c < a.d) {
+#pragma unroll 8
+    for (int i = row; i < a.count[which]; i += kFoldLanes / 8) s += a.partial[which][(int64_t)i * a.d + c];
   }
+  part[row][lane] = s;
+  for (int half = kFoldLanes / 16; half > 0; half /= 2) {
+    __syncthreads();
+    if (row < half) part[row][lane] += part[row + half][lane];
+  }
+  if (row == 0 && c < a.d) store_from_float(a.out[which] + c * a.stride[which], a.type[which], (float)part[0][lane]);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -417,6 +453,7 @@ __device__ __forceinline__ f16 nine_bits(float m) {
 // Keys and values into the cache: job 0 the keys, job 1 the values.  A group's 32 channels are four lanes'.  Each lane's eight codes are four
 // bytes of a token's row; the conversion of two floats to two codes is one instruction and rounds to nearest even.
 template <class T, bool VEC, int KIND> __global__ __launch_bounds__(kBlock) void cache_append_kernel(const HeadArgs a) {
+  warm_arguments<HeadArgs>();
   __shared__ Table tab;
   const int lanes = 1 << a.lanes_log2, e = (threadIdx.x & (lanes - 1)) * kEight, rows = kBlock >> a.lanes_log2, d = a.d;
   const Item item = item_of(a, a.first_item + blockIdx.x);
@@ -433,7 +470,7 @@ template <class T, bool VEC, int KIND> __global__ __launch_bounds__(kBlock) void
       if (!item.which) p = load_partners<T, KIND>(row, j.xe, e, a.half);
     }
     if (KIND != kPairsNone && base == 0 && !item.which) {
-      fill_table(a, tab, item.token, item.tokens);
+      fill_table<KIND>(a, j, tab, item.token, item.tokens, false);
       __syncthreads();
     }
     float v[kEight], top = 0.0f;
@@ -446,7 +483,7 @@ template <class T, bool VEC, int KIND> __global__ __launch_bounds__(kBlock) void
         float q[kEight];
 #pragma unroll
         for (int i = 0; i < kEight; ++i) q[i] = (float)p[i];
-        turn<KIND>(v, q, tab.c + t * a.row, tab.s + t * a.row, e, a.half);
+        turn<KIND>(v, q, tab.own + t * a.row, tab.other + t * a.row, e, a.half);
       }
 #pragma unroll
       for (int i = 0; i < kEight; ++i) {
@@ -455,8 +492,8 @@ template <class T, bool VEC, int KIND> __global__ __launch_bounds__(kBlock) void
       }
     }
     if (!fine) top = __builtin_inff();     // (not NaN, which maxima leave out)
-    top = fmaxf(top, __shfl_xor(top, 1));
-    top = fmaxf(top, __shfl_xor(top, 2));
+    top = fmaxf(top, other_lane<0xb1>(top));
+    top = fmaxf(top, other_lane<0x4e>(top));
     if (!mine) continue;
     const f16 scale = top == __builtin_inff() ? (f16)__builtin_nanf("") : nine_bits(fminf(top * (float)(1.0 / 12.0), 5456.0f));
     // x / scale, correctly rounded: the reciprocal's quotient and one step with the exact remainder
@@ -490,6 +527,7 @@ template <class T, bool VEC, int KIND> __global__ __launch_bounds__(kBlock) void
 
 // The values at slots: job 0 the keys, job 1 the values.
 template <class T, bool VEC> __global__ __launch_bounds__(kBlock) void cache_read_kernel(const HeadArgs a) {
+  warm_arguments<HeadArgs>();
   const int lanes = 1 << a.lanes_log2, e = (threadIdx.x & (lanes - 1)) * kEight, rows = kBlock >> a.lanes_log2, d = a.d;
   const Item item = item_of(a, a.first_item + blockIdx.x);
   const HeadJob &j = a.job[item.which];
@@ -514,7 +552,7 @@ template <class T, bool VEC> __global__ __launch_bounds__(kBlock) void cache_rea
     const f16x2 c2 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, 2.0f, 2), c3 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, 2.0f, 3);
     const float v[kEight] = {(float)c0.x * s, (float)c0.y * s, (float)c1.x * s, (float)c1.y * s,
                              (float)c2.x * s, (float)c2.y * s, (float)c3.x * s, (float)c3.y * s};
-    store_eight<T, VEC>(j.out + along(a, j.ol, item.token + t) + h * j.oh, j.oe, e, d, v);
+    store_eight<T, VEC>(j.out + along(a, j.ol, item.token + t) + h * j.oh, j.oe, e, d, v, j.stream);
   }
 }
 
@@ -530,6 +568,12 @@ int done(hipError_t e) {
 
 int64_t channels_of(const ocn_tensor *t) { return t->size[t->ndim - 1]; }
 int64_t heads_of(const ocn_tensor *t) { return t->size[t->ndim - 2]; }
+
+int64_t tokens_of(const ocn_tensor *t) {
+  int64_t n = 1;
+  for (int d = 0; d + 2 < t->ndim; ++d) n = t->size[d] > 0 && n > ((int64_t)1 << 31) / t->size[d] ? (int64_t)1 << 31 : n * t->size[d];
+  return n;
+}
 
 int check_heads(const ocn_tensor *t) {
   const int rc = check_operand(t, kHeadTypes);
@@ -573,7 +617,7 @@ bool shape_of_launch(HeadArgs &a, const ocn_rotation *r, int64_t d, int jobs) {
   a.lanes_log2 = 0;
   while ((kEight << a.lanes_log2) < d) ++a.lanes_log2;
   a.half = r ? r->rotary_dim / 2 : 0;
-  a.row = (a.half + 7) & ~7;
+  a.row = (2 * a.half + 7) & ~7;
   a.half_div = make_fastdiv((uint32_t)std::max(a.half, 1));
   if (r) {
     a.magnitude = r->magnitude;
@@ -607,6 +651,7 @@ bool shape_of_launch(HeadArgs &a, const ocn_rotation *r, int64_t d, int jobs) {
 void set_rows(HeadJob &j, const ocn_tensor *x, const ocn_tensor *g, const ocn_tensor *out) {
   if (x) { j.x = (const char *)x->base + x->offset; j.xh = x->stride[x->ndim - 2]; j.xe = x->stride[x->ndim - 1]; }
   if (g) { j.g = (const char *)g->base + g->offset; j.gh = g->stride[g->ndim - 2]; j.ge = g->stride[g->ndim - 1]; }
+  if (out) j.stream = (int64_t)tokens_of(out) * heads_of(out) * channels_of(out) * head_type_size(out->dtype) >= kStreamBytes;
   if (out) { j.out = (char *)out->base + out->offset; j.oh = out->stride[out->ndim - 2]; j.oe = out->stride[out->ndim - 1]; }
 }
 
@@ -786,16 +831,10 @@ int run_cache(const ocn_tensor *k, const ocn_tensor *v, const ocn_rotation *r, c
   });
 }
 
-// workgroups that sum one job's gradient of weights
-int grad_blocks(int64_t tokens, int64_t heads, int jobs) {
-  const int64_t most = kFoldBlocks / jobs;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(most, tokens * heads / 16));
-}
-
-int64_t tokens_of(const ocn_tensor *t) {
-  int64_t n = 1;
-  for (int d = 0; d + 2 < t->ndim; ++d) n = t->size[d] > 0 && n > ((int64_t)1 << 31) / t->size[d] ? (int64_t)1 << 31 : n * t->size[d];
-  return n;
+// workgroups that sum a gradient of weights, of `heads` of all heads of a token
+int grad_blocks(int64_t tokens, int64_t heads, int64_t all) {
+  const int64_t share = all > 0 ? kFoldBlocks * heads / all : 0;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(share, tokens * heads / 16));
 }
 
 }  // namespace
@@ -821,8 +860,9 @@ int ocn_norm_rotary(const ocn_tensor *q, const ocn_tensor *q_weight, const ocn_t
 
 size_t ocn_norm_rotary_grad_workspace_bytes(const ocn_tensor *q, const ocn_tensor *k) {
   if (check_heads(q) != OCN_OK || (k && check_heads(k) != OCN_OK)) return 0;
-  size_t n = (size_t)grad_blocks(tokens_of(q), heads_of(q), k ? 2 : 1) * channels_of(q);
-  if (k) n += (size_t)grad_blocks(tokens_of(k), heads_of(k), 2) * channels_of(k);
+  const int64_t all = heads_of(q) + (k ? heads_of(k) : 0);
+  size_t n = (size_t)grad_blocks(tokens_of(q), heads_of(q), all) * channels_of(q);
+  if (k) n += (size_t)grad_blocks(tokens_of(k), heads_of(k), all) * channels_of(k);
   return n * sizeof(float);
 }
 
@@ -884,7 +924,7 @@ int ocn_norm_rotary_grad(const ocn_tensor *q_gout, const ocn_tensor *q, const oc
       j.weight_type = w[i]->dtype;
     }
     vec = vec && whole_vectors(x[i]) && whole_vectors(g[i]) && whole_vectors(out[i]);
-    f.count[i] = j.workers = grad_blocks(a.lead.tokens, j.heads, jobs);
+    j.workers = grad_blocks(a.lead.tokens, j.heads, heads_of(q) + (k ? heads_of(k) : 0));
     if (gw[i]) {
       sums = true;
       f.partial[i] = j.partial = (float *)workspace + need;
@@ -901,6 +941,11 @@ int ocn_norm_rotary_grad(const ocn_tensor *q_gout, const ocn_tensor *q, const oc
   std::memcpy(a.pos_l, strides[6], sizeof a.pos_l);
   if (d == 0) return OCN_OK;
   if (!shape_of_launch(a, rotation, d, jobs)) return OCN_ERR_SHAPE;
+  for (int i = 0; i < jobs; ++i) {     // as many items for each, or one fewer for some
+    HeadJob &j = a.job[i];
+    const uint32_t rounds = std::max<uint32_t>(1, (j.items + j.workers - 1) / j.workers);
+    f.count[i] = j.workers = (int32_t)std::max<uint32_t>(1, (j.items + rounds - 1) / rounds);
+  }
   a.eps = (float)eps;
   a.sign = -1.0f;
   const int kind = kind_of_pairs(rotation, vec), across = std::max(f.count[0], f.count[1]);
@@ -911,7 +956,7 @@ int ocn_norm_rotary_grad(const ocn_tensor *q_gout, const ocn_tensor *q, const oc
   rc = done(hipGetLastError());
   if (rc != OCN_OK || !sums) return rc;
   f.d = (int32_t)d;
-  hipLaunchKernelGGL(head_fold_kernel, dim3((uint32_t)((d + 7) / 8), jobs), dim3(kBlock), 0, s, f);
+  hipLaunchKernelGGL(head_fold_kernel, dim3((uint32_t)((d + 7) / 8), jobs), dim3(kFoldLanes), 0, s, f);
   return done(hipGetLastError());
 }
 
