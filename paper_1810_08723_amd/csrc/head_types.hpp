@@ -39,14 +39,14 @@ __device__ __forceinline__ void store_from_float(char *p, int dtype, float v) {
   else *(bf16 *)p = (bf16)v;
 }
 
-// ---- a block of the cache: bytes of its parts for P tokens of D channels ---------------------------
-__device__ __forceinline__ int64_t block_k_codes(int page, int d, int token, int channel) { return (int64_t)token * (d / 2) + channel / 2; }
-__device__ __forceinline__ int64_t block_v_codes(int page, int d, int token, int channel) {
-  const int wide = d / 16, j = channel / wide;
-  return (int64_t)page * (d / 2) + (((token / 4) * 16 + j) * 4 + token % 4) * (wide / 2) + (channel % wide) / 2;
+// ---- a block of the cache: bytes of its parts for P tokens of D channels (a power of two) ------------
+__device__ __forceinline__ int block_k_codes(int page, int d, int token, int channel) { return token * (d / 2) + channel / 2; }
+__device__ __forceinline__ int block_v_codes(int page, int d, int token, int channel) {
+  const int log2 = 27 - __builtin_clz(d), j = channel >> log2;         // a lane of attention has D/16 channels
+  return page * (d / 2) + (((((token >> 2) * 16 + j) * 4 + (token & 3)) << log2) >> 1) + ((channel & ((1 << log2) - 1)) >> 1);
 }
-__device__ __forceinline__ int64_t block_scale(int page, int d, bool v, int group, int token) {
-  return (int64_t)page * d + 2 * ((int64_t)((v ? d / 32 : 0) + group) * page + token);
+__device__ __forceinline__ int block_scale(int page, int d, bool v, int group, int token) {
+  return page * d + 2 * (((v ? d / 32 : 0) + group) * page + token);
 }
 
 }  // namespace ocn

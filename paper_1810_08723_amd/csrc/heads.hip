@@ -62,26 +62,29 @@ struct HeadArgs {
   int32_t half, row;                   // pairs of a head; floats of a token in the table
   FastDiv half_div;
   int32_t d, lanes_log2;               // channels; lanes of a row
+  int32_t small;                       // one leading dimension, strides and what an item spans in 24 and 31 bits
   uint32_t items, first_item;          // of all launches; of this one
   // the cache
   const char *slots;
   int64_t slot_l[kMaxLead], page_stride, head_stride, slot_count;
   char *cache;
-  int32_t slots_wide, page;
+  int32_t slots_wide, page, small_cache;   // the cache's strides in 32 bits
   FastDiv page_div;
 };
 
-// an offset along the tokens' dimensions
-__device__ __forceinline__ int64_t along(const HeadArgs &a, const int64_t *stride, uint32_t token) {
-  if (a.lead.n == 1) return (int64_t)token * stride[0];
-  int64_t o = 0;
+// The address of head h of a workgroup's token t (from `token` on, which all lanes share).  Products of 64 bits are some twenty times the work
+// of one of 24; where strides are small (a.small) only the shared part takes them, in scalar registers.
+__device__ __forceinline__ const char *address(const HeadArgs &a, const char *base, const int64_t *stride, uint32_t token, int t, int64_t head_stride, int h) {
+  if (a.small) return base + (int64_t)token * stride[0] + (__mul24(t, (int)stride[0]) + __mul24(h, (int)head_stride));
+  uint32_t i = token + t;
+  int64_t o = h * head_stride;
 #pragma nounroll
   for (int d = a.lead.n - 1; d > 0; --d) {
-    const uint32_t q = fast_quotient(token, a.lead.div[d]);
-    o += (int64_t)(token - q * a.lead.div[d].d) * stride[d];
-    token = q;
+    const uint32_t q = fast_quotient(i, a.lead.div[d]);
+    o += (int64_t)(i - q * a.lead.div[d].d) * stride[d];
+    i = q;
   }
-  return o + (int64_t)token * stride[0];
+  return base + (o + (int64_t)i * stride[0]);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -130,7 +133,7 @@ template <int KIND> __device__ __forceinline__ void fill_table(const HeadArgs &a
 #pragma nounroll
   for (int i = threadIdx.x; i < tokens * a.half; i += kBlock) {
     const int t = (int)fast_quotient((uint32_t)i, a.half_div), p = i - t * a.half;
-    const int64_t at = load_index(a.pos + along(a, a.pos_l, token + t), a.pos_wide);
+    const int64_t at = load_index(address(a, a.pos, a.pos_l, token, t, 0, 0), a.pos_wide);
     double s, c;
     sine_cosine((double)at * *(const double *)(a.freq + p * a.freq_stride), &s, &c);
     const float cc = (float)(c * a.magnitude), ss = (float)(s * a.magnitude) * a.sign;
@@ -229,6 +232,7 @@ template <int KIND> __device__ __forceinline__ void turn(float *x, const float *
 template <int CTRL> __device__ __forceinline__ float other_lane(float x) {
   return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
 }
+template <int CTRL> __device__ __forceinline__ uint32_t other_lane_bits(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true); }
 // the sum over a row's lanes (1, 2, 4 ... 64 of them): exchanges inside sixteen lanes cost no trip through LDS
 __device__ __forceinline__ float sum_over_row(float v, int lanes) {
   if (lanes > 1) v += other_lane<0xb1>(v);      // 1 0 3 2
@@ -276,10 +280,10 @@ template <class T, bool VEC, int KIND, bool NORM> __global__ __launch_bounds__(k
       to[u] = nullptr;
       tt[u] = t;
       if (r < total && h < j.heads && e < d) {
-        const char *row = j.x + along(a, j.xl, item.token + t) + h * j.xh;
+        const char *row = address(a, j.x, j.xl, item.token, t, j.xh, h);
         x[u] = load_eight<T, VEC>(row, j.xe, e, d);
         p[u] = load_partners<T, KIND>(row, j.xe, e, a.half);
-        to[u] = j.out + along(a, j.ol, item.token + t) + h * j.oh;
+        to[u] = (char *)address(a, j.out, j.ol, item.token, t, j.oh, h);
       }
     }
     if (base == 0) {
@@ -347,8 +351,8 @@ template <class T, bool VEC, int KIND> __global__ __launch_bounds__(kBlock) void
     const auto load = [&](int base, int u) {
       const int r = base + (threadIdx.x >> a.lanes_log2), t = (int)fast_quotient((uint32_t)r, j.per_div), n = item.head + r - t * j.per;
       if (r < total && n < j.heads && e < d) {
-        const char *row = j.g + along(a, j.gl, item.token + t) + n * j.gh;
-        x[u] = load_eight<T, VEC>(j.x + along(a, j.xl, item.token + t) + n * j.xh, j.xe, e, d);
+        const char *row = address(a, j.g, j.gl, item.token, t, j.gh, n);
+        x[u] = load_eight<T, VEC>(address(a, j.x, j.xl, item.token, t, j.xh, n), j.xe, e, d);
         g[u] = load_eight<T, VEC>(row, j.ge, e, d);
         p[u] = load_partners<T, KIND>(row, j.ge, e, a.half);
       }
@@ -387,7 +391,7 @@ template <class T, bool VEC, int KIND> __global__ __launch_bounds__(kBlock) void
             gw[i] = __builtin_fmaf(h[i], unit, gw[i]);
             v[i] = over * (h[i] * w[i] - unit * mean);
           }
-          store_eight<T, VEC>(j.out + along(a, j.ol, item.token + t) + n * j.oh, j.oe, e, d, v, j.stream);
+          store_eight<T, VEC>((char *)address(a, j.out, j.ol, item.token, t, j.oh, n), j.oe, e, d, v, j.stream);
         }
       }
     }
@@ -444,6 +448,11 @@ __device__ __forceinline__ Slot slot_of(const HeadArgs &a, int64_t slot) {
   return s;
 }
 
+__device__ __forceinline__ char *block_of(const HeadArgs &a, int64_t page, int h) {
+  if (a.small_cache) return a.cache + ((uint64_t)(uint32_t)page * (uint32_t)a.page_stride + (uint64_t)(uint32_t)h * (uint32_t)a.head_stride);
+  return a.cache + page * a.page_stride + h * a.head_stride;
+}
+
 // nine significant bits of a float, ties to even, as a half
 __device__ __forceinline__ f16 nine_bits(float m) {
   const uint32_t b = __builtin_bit_cast(uint32_t, m);
@@ -459,69 +468,74 @@ template <class T, bool VEC, int KIND> __global__ __launch_bounds__(kBlock) void
   const Item item = item_of(a, a.first_item + blockIdx.x);
   const HeadJob &j = a.job[item.which];
   const int total = item.tokens * j.per;
-  for (int base = 0; base < total; base += rows) {
-    const int r = base + (threadIdx.x >> a.lanes_log2), t = (int)fast_quotient((uint32_t)r, j.per_div), h = item.head + r - t * j.per;
-    eight_t<T> x, p;
-    int64_t slot = -1;
-    if (r < total && h < j.heads) {
-      const char *row = j.x + along(a, j.xl, item.token + t) + h * j.xh;
-      slot = load_index(a.slots + along(a, a.slot_l, item.token + t), a.slots_wide);
-      x = load_eight<T, VEC>(row, j.xe, e, d);
-      if (!item.which) p = load_partners<T, KIND>(row, j.xe, e, a.half);
+  constexpr int U = 2;                   // rows of a lane at a time
+  for (int base = 0; base < total; base += U * rows) {
+    eight_t<T> x[U], p[U];
+    int64_t slots[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int r = base + u * rows + (threadIdx.x >> a.lanes_log2), t = (int)fast_quotient((uint32_t)r, j.per_div), h = item.head + r - t * j.per;
+      slots[u] = -1;
+      if (r < total && h < j.heads) {
+        const char *row = address(a, j.x, j.xl, item.token, t, j.xh, h);
+        slots[u] = load_index(address(a, a.slots, a.slot_l, item.token, t, 0, 0), a.slots_wide);
+        x[u] = load_eight<T, VEC>(row, j.xe, e, d);
+        if (!item.which) p[u] = load_partners<T, KIND>(row, j.xe, e, a.half);
+      }
     }
     if (KIND != kPairsNone && base == 0 && !item.which) {
       fill_table<KIND>(a, j, tab, item.token, item.tokens, false);
       __syncthreads();
     }
-    float v[kEight], top = 0.0f;
-    bool fine = true;
-    const bool mine = slot >= 0 && slot < a.slot_count;
-    if (mine) {
 #pragma unroll
-      for (int i = 0; i < kEight; ++i) v[i] = (float)x[i];
-      if (!item.which) {
-        float q[kEight];
+    for (int u = 0; u < U; ++u) {
+      const int r = base + u * rows + (threadIdx.x >> a.lanes_log2), t = (int)fast_quotient((uint32_t)r, j.per_div), h = item.head + r - t * j.per;
+      const int64_t slot = slots[u];
+      float v[kEight];
+      uint32_t bits = 0;                     // of the largest magnitude: as whole numbers, infinities are above all others and NaNs above them
+      const bool mine = slot >= 0 && slot < a.slot_count;
+      if (mine) {
 #pragma unroll
-        for (int i = 0; i < kEight; ++i) q[i] = (float)p[i];
-        turn<KIND>(v, q, tab.own + t * a.row, tab.other + t * a.row, e, a.half);
+        for (int i = 0; i < kEight; ++i) v[i] = (float)x[u][i];
+        if (!item.which) {
+          float q[kEight];
+#pragma unroll
+          for (int i = 0; i < kEight; ++i) q[i] = (float)p[u][i];
+          turn<KIND>(v, q, tab.own + t * a.row, tab.other + t * a.row, e, a.half);
+        }
+#pragma unroll
+        for (int i = 0; i < kEight; ++i) bits = max(bits, __builtin_bit_cast(uint32_t, v[i]) & 0x7fffffffu);
       }
+      bits = max(bits, other_lane_bits<0xb1>(bits));
+      bits = max(bits, other_lane_bits<0x4e>(bits));
+      if (!mine) continue;
+      const f16 scale = bits >= 0x7f800000u ? (f16)__builtin_nanf("") : nine_bits(fminf(__builtin_bit_cast(float, bits) * (float)(1.0 / 12.0), 5456.0f));
+      // x / scale, correctly rounded: the reciprocal's quotient and one step with the exact remainder.  (Zeros get their signs back; beyond +-12
+      // the conversion saturates.)
+      const float s = (float)scale, inverse = s > 0.0f ? 1.0f / s : 0.0f;
+      uint32_t codes = 0;
+      float y[kEight];
 #pragma unroll
       for (int i = 0; i < kEight; ++i) {
-        top = fmaxf(top, __builtin_fabsf(v[i]));
-        fine &= __builtin_fabsf(v[i]) < __builtin_inff();
+        const float y0 = v[i] * inverse;
+        y[i] = __builtin_copysignf(__builtin_fmaf(__builtin_fmaf(-y0, s, v[i]), inverse, y0), v[i]);
       }
+      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, y[0], y[1], 2.0f, 0);
+      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, y[2], y[3], 2.0f, 1);
+      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, y[4], y[5], 2.0f, 2);
+      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, y[6], y[7], 2.0f, 3);
+      const Slot at = slot_of(a, slot);
+      char *block = block_of(a, at.page, h);
+      if (!item.which) {
+        *(uint32_t *)(block + block_k_codes(a.page, d, at.place, e)) = codes;
+      } else if (d == 64) {      // (four channels of a token lie together)
+        *(uint16_t *)(block + block_v_codes(a.page, d, at.place, e)) = (uint16_t)codes;
+        *(uint16_t *)(block + block_v_codes(a.page, d, at.place, e + 4)) = (uint16_t)(codes >> 16);
+      } else {
+        *(uint32_t *)(block + block_v_codes(a.page, d, at.place, e)) = codes;
+      }
+      if (e % 32 == 0) *(f16 *)(block + block_scale(a.page, d, item.which != 0, e / 32, at.place)) = scale;
     }
-    if (!fine) top = __builtin_inff();     // (not NaN, which maxima leave out)
-    top = fmaxf(top, other_lane<0xb1>(top));
-    top = fmaxf(top, other_lane<0x4e>(top));
-    if (!mine) continue;
-    const f16 scale = top == __builtin_inff() ? (f16)__builtin_nanf("") : nine_bits(fminf(top * (float)(1.0 / 12.0), 5456.0f));
-    // x / scale, correctly rounded: the reciprocal's quotient and one step with the exact remainder
-    const float s = (float)scale, inverse = s > 0.0f ? 1.0f / s : 0.0f;
-    uint32_t codes = 0;
-    float y[kEight];
-#pragma unroll
-    for (int i = 0; i < kEight; ++i) {
-      const float y0 = v[i] * inverse;
-      y[i] = __builtin_fmaf(__builtin_fmaf(-y0, s, v[i]), inverse, y0);
-      y[i] = __builtin_amdgcn_fmed3f(y[i], -12.0f, 12.0f);
-      if (!(s > 0.0f)) y[i] = __builtin_copysignf(0.0f, v[i]);
-    }
-    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, y[0], y[1], 2.0f, 0);
-    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, y[2], y[3], 2.0f, 1);
-    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, y[4], y[5], 2.0f, 2);
-    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, y[6], y[7], 2.0f, 3);
-    const Slot at = slot_of(a, slot);
-    char *block = a.cache + at.page * a.page_stride + h * a.head_stride;
-    if (!item.which) {
-      *(uint32_t *)(block + block_k_codes(a.page, d, at.place, e)) = codes;
-    } else if (d == 64) {      // (four channels of a token lie together)
-      *(uint16_t *)(block + block_v_codes(a.page, d, at.place, e)) = (uint16_t)codes;
-      *(uint16_t *)(block + block_v_codes(a.page, d, at.place, e + 4)) = (uint16_t)(codes >> 16);
-    } else {
-      *(uint32_t *)(block + block_v_codes(a.page, d, at.place, e)) = codes;
-    }
-    if (e % 32 == 0) *(f16 *)(block + block_scale(a.page, d, item.which != 0, e / 32, at.place)) = scale;
   }
 }
 
@@ -535,10 +549,10 @@ template <class T, bool VEC> __global__ __launch_bounds__(kBlock) void cache_rea
   for (int r = threadIdx.x >> a.lanes_log2; r < total; r += rows) {
     const int t = (int)fast_quotient((uint32_t)r, j.per_div), h = item.head + r - t * j.per;
     if (h >= j.heads) continue;
-    const int64_t slot = load_index(a.slots + along(a, a.slot_l, item.token + t), a.slots_wide);
+    const int64_t slot = load_index(address(a, a.slots, a.slot_l, item.token, t, 0, 0), a.slots_wide);
     if (slot < 0 || slot >= a.slot_count) continue;
     const Slot at = slot_of(a, slot);
-    const char *block = a.cache + at.page * a.page_stride + h * a.head_stride;
+    const char *block = block_of(a, at.page, h);
     uint32_t codes;
     if (!item.which)
       codes = *(const uint32_t *)(block + block_k_codes(a.page, d, at.place, e));
@@ -552,7 +566,7 @@ template <class T, bool VEC> __global__ __launch_bounds__(kBlock) void cache_rea
     const f16x2 c2 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, 2.0f, 2), c3 = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, 2.0f, 3);
     const float v[kEight] = {(float)c0.x * s, (float)c0.y * s, (float)c1.x * s, (float)c1.y * s,
                              (float)c2.x * s, (float)c2.y * s, (float)c3.x * s, (float)c3.y * s};
-    store_eight<T, VEC>(j.out + along(a, j.ol, item.token + t) + h * j.oh, j.oe, e, d, v, j.stream);
+    store_eight<T, VEC>((char *)address(a, j.out, j.ol, item.token, t, j.oh, h), j.oe, e, d, v, j.stream);
   }
 }
 
@@ -631,18 +645,29 @@ bool shape_of_launch(HeadArgs &a, const ocn_rotation *r, int64_t d, int jobs) {
   const int rows = kBlock >> a.lanes_log2;
   int64_t all = 0, want = kPasses * rows, items = 0;
   for (int i = 0; i < jobs; ++i) all += (int64_t)a.lead.tokens * a.job[i].heads;
-  while (want > rows && all / want < 8 * kNumCUs) want /= 2;
+  while (want > rows && all / want < 4 * kNumCUs) want /= 2;
   const int64_t most_tokens = r ? std::max<int64_t>(1, kTable / a.row) : 64;
   for (int i = 0; i < jobs; ++i) {
     HeadJob &j = a.job[i];
     const int64_t parts = std::max<int64_t>(1, (j.heads + want - 1) / want);
     j.per = (int32_t)std::max<int64_t>(1, (j.heads + parts - 1) / parts);
-    j.per_tokens = (int32_t)std::min<int64_t>(most_tokens, std::max<int64_t>(1, want / j.per));
+    j.per_tokens = (int32_t)std::min<int64_t>(most_tokens, std::max<int64_t>(1, (want + j.per / 2) / j.per));
     const int64_t blocks = ((int64_t)a.lead.tokens + j.per_tokens - 1) / j.per_tokens, across = j.heads ? (j.heads + j.per - 1) / j.per : 0;
     j.per_div = make_fastdiv((uint32_t)j.per);
     j.blocks_div = make_fastdiv((uint32_t)std::max<int64_t>(across, 1));
     j.items = (uint32_t)(blocks * across);
     items += blocks * across;
+  }
+  // 24-bit products: counts and strides below 2^23, and what an item's tokens and a token's heads span below 2^30 each
+  const auto fits = [](int64_t stride, int64_t count) {
+    const int64_t s = stride < 0 ? -stride : stride;
+    return s < (1 << 23) && count < (1 << 23) && s * count < (1 << 30);
+  };
+  a.small = a.lead.n == 1;
+  for (int i = 0; i < jobs; ++i) {
+    const HeadJob &j = a.job[i];
+    a.small = a.small && fits(a.pos_l[0], j.per_tokens) && fits(a.slot_l[0], j.per_tokens) && fits(j.xl[0], j.per_tokens) && fits(j.gl[0], j.per_tokens) && fits(j.ol[0], j.per_tokens) && fits(j.xh, j.heads) &&
+              fits(j.gh, j.heads) && fits(j.oh, j.heads);
   }
   a.items = (uint32_t)items;
   return items < ((int64_t)1 << 31);
@@ -814,6 +839,7 @@ int run_cache(const ocn_tensor *k, const ocn_tensor *v, const ocn_rotation *r, c
   a.cache = (char *)cache->base + cache->offset;
   a.page_stride = cache->stride[0];
   a.head_stride = cache->stride[1];
+  a.small_cache = a.page_stride >= 0 && a.page_stride < ((int64_t)1 << 32) && a.head_stride >= 0 && a.head_stride < ((int64_t)1 << 32);
   a.page = (int32_t)page;
   a.page_div = make_fastdiv((uint32_t)page);
   a.slot_count = cache->size[0] * page;
