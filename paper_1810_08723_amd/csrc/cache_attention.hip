@@ -241,9 +241,67 @@ template <int D, int RT, int PARTS_Q> struct Rows {
   int lo[RT], hi[RT];                // tokens that a row sees
 };
 
+// Scales of V that are NaN (or none that appending writes: places that were never written) count as zero in a tile that some row does not see whole,
+// because weights of zero would not make a NaN go away; `bad` marks their tokens.
+__device__ __forceinline__ Frag fix_scales(uint32_t (*v_scale)[2]) {
+  Frag bad;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t two = v_scale[i / 2][i % 2];
+    f16x2 sc = __builtin_bit_cast(f16x2, two), no = {0, 0};
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      if (!(sc[e] <= (f16)5456.0f && sc[e] >= (f16)-5456.0f)) { sc[e] = (f16)0.0f; no[e] = (f16)1.0f; }
+    v_scale[i / 2][i % 2] = __builtin_bit_cast(uint32_t, sc);
+    bad.p[i] = no;
+  }
+  return bad;
+}
+
+// Where a tile's operands come from: a wavefront's own registers ...
+template <int D> struct FromRegisters {
+  typedef Shape<D> S;
+  Raw<D> &raw;
+  Twins<D> twins[4];
+  f16x2 scale[4];
+  __device__ __forceinline__ f16x8 k(int x, int w) const {
+    const uint32_t codes = raw.k[x][w], both = raw.k_scale[x][w / S::kRun];
+    const f16x2 one = __builtin_bit_cast(f16x2, both), s = {one.x, one.x};
+    Frag f;
+    f.p[0] = two_codes<0>(codes) * s, f.p[1] = two_codes<1>(codes) * s;
+    f.p[2] = two_codes<2>(codes) * s, f.p[3] = two_codes<3>(codes) * s;
+    return f.v;
+  }
+  __device__ __forceinline__ f16x8 bad() { return fix_scales(raw.v_scale).v; }
+  __device__ __forceinline__ void start_v() {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      twins[i] = twins_of<D>(raw.v[i / 2], i % 2);
+      const uint32_t two = raw.v_scale[i / 2][i % 2];
+      scale[i] = __builtin_bit_cast(f16x2, two);
+    }
+  }
+  __device__ __forceinline__ f16x8 v(int t) const {
+    Frag f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f.p[i] = twin_codes<D>(twins[i], t) * scale[i];
+    return f.v;
+  }
+};
+
+// ... or LDS, where a workgroup's wavefronts have put them: K [half tile][word], V [channel of a lane], the tokens with bad scales; 16 bytes of each lane
+template <int D> struct FromLds {
+  typedef Shape<D> S;
+  const f16x8 *at;         // of this lane
+  __device__ __forceinline__ f16x8 k(int x, int w) const { return at[(x * S::kWords + w) * kWave]; }
+  __device__ __forceinline__ f16x8 v(int t) const { return at[(2 * S::kWords + t) * kWave]; }
+  __device__ __forceinline__ f16x8 bad() const { return at[(2 * S::kWords + S::kTiles) * kWave]; }
+  __device__ __forceinline__ void start_v() const {}
+};
+
 // whole: every row sees every token of the tile
-template <int D, int RT, int PARTS_Q, int PARTS_P>
-__device__ __forceinline__ void one_tile(Sums<D, RT> &s, const Rows<D, RT, PARTS_Q> &rows, Raw<D> &raw, int g, int j0, bool whole, bool fine0, bool fine1) {
+template <int D, int RT, int PARTS_Q, int PARTS_P, class Source>
+__device__ __forceinline__ void one_tile(Sums<D, RT> &s, const Rows<D, RT, PARTS_Q> &rows, Source &source, int g, int j0, bool whole, bool fine0, bool fine1) {
   typedef Shape<D> S;
   typedef Floor<PARTS_Q> F;
   const f16x8 ones = {1, 1, 1, 1, 1, 1, 1, 1};
@@ -256,15 +314,11 @@ __device__ __forceinline__ void one_tile(Sums<D, RT> &s, const Rows<D, RT, PARTS
   for (int w = 0; w < S::kWords; ++w)
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      const uint32_t codes = raw.k[x][w], both = raw.k_scale[x][w / S::kRun];
-      const f16x2 one = __builtin_bit_cast(f16x2, both), scale = {one.x, one.x};
-      Frag k;
-      k.p[0] = two_codes<0>(codes) * scale, k.p[1] = two_codes<1>(codes) * scale;
-      k.p[2] = two_codes<2>(codes) * scale, k.p[3] = two_codes<3>(codes) * scale;
+      const f16x8 k = source.k(x, w);
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-        for (int part = 0; part < PARTS_Q; ++part) score[rt][x] = product(k.v, rows.q[rt][part][w], score[rt][x]);
+        for (int part = 0; part < PARTS_Q; ++part) score[rt][x] = product(k, rows.q[rt][part][w], score[rt][x]);
     }
   float least[RT];       // (unseen places may make it too small, and the tile takes longer)
 #pragma unroll
@@ -275,19 +329,7 @@ __device__ __forceinline__ void one_tile(Sums<D, RT> &s, const Rows<D, RT, PARTS
   }
   uint32_t sees[RT];     // which of its eight tokens a lane's row sees
   if (!whole) {
-    // Weights of zero do not make a token's NaN go away: in a tile that some row does not see whole, a scale that is NaN (or none that
-    // appending writes: places that were never written) counts as zero, and rows that do see its token are marked by one more product.
-    Frag nan_of;         // 1 for such tokens
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t two = raw.v_scale[i / 2][i % 2];
-      f16x2 sc = __builtin_bit_cast(f16x2, two), bad = {0, 0};
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-        if (!(sc[e] <= (f16)5456.0f && sc[e] >= (f16)-5456.0f)) { sc[e] = (f16)0.0f; bad[e] = (f16)1.0f; }
-      raw.v_scale[i / 2][i % 2] = __builtin_bit_cast(uint32_t, sc);
-      nan_of.p[i] = bad;
-    }
+    const f16x8 bad = source.bad();     // rows that see such tokens are marked by one more product
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       Frag seen;
@@ -300,7 +342,7 @@ __device__ __forceinline__ void one_tile(Sums<D, RT> &s, const Rows<D, RT, PARTS
         sees[rt] |= in ? 1u << i : 0u;
         if (!in) score[rt][i / 4][i % 4] = -__builtin_inff();
       }
-      s.bad[rt] = product(nan_of.v, seen.v, s.bad[rt]);
+      s.bad[rt] = product(bad, seen.v, s.bad[rt]);
     }
   }
   Frag p[RT][PARTS_P];
@@ -328,14 +370,7 @@ __device__ __forceinline__ void one_tile(Sums<D, RT> &s, const Rows<D, RT, PARTS
     }
     if (__builtin_amdgcn_ballot_w64(__builtin_fmaf(least[rt], rows.scale[rt], shift) < F::kBits)) apart = true;
   }
-  Twins<D> twins[4];
-  f16x2 scale[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    twins[i] = twins_of<D>(raw.v[i / 2], i % 2);
-    const uint32_t two = raw.v_scale[i / 2][i % 2];
-    scale[i] = __builtin_bit_cast(f16x2, two);
-  }
+  source.start_v();
   if (apart) {
     float small[RT][8], down = F::kDown;
 #pragma unroll
@@ -363,14 +398,12 @@ __device__ __forceinline__ void one_tile(Sums<D, RT> &s, const Rows<D, RT, PARTS
       if (__builtin_amdgcn_ballot_w64(any)) {
 #pragma unroll
         for (int t = 0; t < S::kTiles; ++t) {
-          Frag f;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) f.p[i] = twin_codes<D>(twins[i], t) * scale[i];
+          const f16x8 f = source.v(t);
 #pragma unroll
           for (int rt = 0; rt < RT; ++rt) {
             f32x4 add = {0, 0, 0, 0};
 #pragma unroll
-            for (int part = 0; part < PARTS_P; ++part) add = product(f.v, p[rt][part].v, add);
+            for (int part = 0; part < PARTS_P; ++part) add = product(f, p[rt][part].v, add);
             s.out[rt][t] += add * down;
             if (t == 0) {
               add = f32x4{0, 0, 0, 0};
@@ -396,13 +429,11 @@ __device__ __forceinline__ void one_tile(Sums<D, RT> &s, const Rows<D, RT, PARTS
   }
 #pragma unroll
   for (int t = 0; t < S::kTiles; ++t) {
-    Frag f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) f.p[i] = twin_codes<D>(twins[i], t) * scale[i];
+    const f16x8 f = source.v(t);
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-      for (int part = 0; part < PARTS_P; ++part) s.out[rt][t] = product(f.v, p[rt][part].v, s.out[rt][t]);
+      for (int part = 0; part < PARTS_P; ++part) s.out[rt][t] = product(f, p[rt][part].v, s.out[rt][t]);
   }
 }
 
@@ -461,27 +492,12 @@ template <int PARTS_Q, int PARTS_P> __device__ __forceinline__ void channels_of(
   }
 }
 
-// SHARE: a workgroup's wavefronts have the same rows and every fourth tile each, and join their sums in LDS; otherwise each has rows of its own and all tiles.
-template <int D, int RT, int PARTS_Q, int PARTS_P, bool SHARE>
-__global__ __launch_bounds__(kBlock, D * RT <= 128 ? 2 : 1) void attention_kernel(const AttentionArgs a) {
-  typedef Shape<D> S;
-  typedef typename TypeOfParts<PARTS_Q, PARTS_P>::T T;
-  constexpr int W = kBlock / kWave, kPart = S::kTiles < 8 ? S::kTiles : 8;
-  constexpr int kRows = 16 * RT * (SHARE ? 1 : W);             // of a unit
-  __shared__ float part[SHARE ? W : 1][SHARE ? 16 : 1][16][SHARE ? kPart : 1];
-  __shared__ float tops[W][RT][16], totals[W][RT][16];
-  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), n = lane % 16, g = lane / 16;
-  const LaneOffsets lanes = lane_offsets<D>(a, n, g);
-  warm_arguments<AttentionArgs>();
-  const uint32_t item = a.first_item + blockIdx.x;
-  // Items: blocks of rows fastest, then heads of the cache, sequences, and splits: workgroups go to the XCDs in turn, and where sequences are
-  // of different lengths the later splits are empty (with splits fastest some XCDs had most of the work: 105 for 44 us).
-  const uint32_t split = fast_quotient(item, a.units_div), unit = item - split * a.units_div.d;
-  const uint32_t bh = fast_quotient(unit, a.blocks_div), block = unit - bh * a.blocks_div.d;
-  const int b = (int)fast_quotient(bh, a.kv_div), kv = (int)bh - b * (int)a.kv_div.d;
-  const int first_row = (int)block * kRows + (SHARE ? 0 : wave * 16 * RT), all_rows = a.queries * a.per_kv;
-  Rows<D, RT, PARTS_Q> rows;
-  int hi_most = 0, hi_least = 0x7fffffff, lo_least = 0x7fffffff, lo_most = 0;
+// what an item's rows see: the tokens of a row, and the ends of all of them
+struct Reach { int hi_most, hi_least, lo_least, lo_most; };
+
+template <int D, int RT, int PARTS_Q>
+__device__ __forceinline__ Reach reach_of(const AttentionArgs &a, Rows<D, RT, PARTS_Q> &rows, int b, int first_row, int all_rows, int n) {
+  Reach r = {0, 0x7fffffff, 0x7fffffff, 0};
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const int row = first_row + rt * 16 + n;
@@ -491,31 +507,35 @@ __global__ __launch_bounds__(kBlock, D * RT <= 128 ? 2 : 1) void attention_kerne
       const int64_t seen = load_index(a.seen + b * a.sb + fast_quotient((uint32_t)row, a.per_kv_div) * a.st, a.seen_wide);
       rows.hi[rt] = (int)max((int64_t)0, min(seen, (int64_t)a.capacity));
       rows.lo[rt] = a.window > 0 ? (int)max((int64_t)0, rows.hi[rt] - a.window) : 0;
-      hi_most = max(hi_most, rows.hi[rt]);
-      hi_least = min(hi_least, rows.hi[rt]);
-      lo_most = max(lo_most, rows.lo[rt]);
-      if (rows.hi[rt] > 0) lo_least = min(lo_least, rows.lo[rt]);
+      r.hi_most = max(r.hi_most, rows.hi[rt]);
+      r.hi_least = min(r.hi_least, rows.hi[rt]);
+      r.lo_most = max(r.lo_most, rows.lo[rt]);
+      if (rows.hi[rt] > 0) r.lo_least = min(r.lo_least, rows.lo[rt]);
     }
   }
-  hi_most = rows_max(hi_most);
-  hi_least = -rows_max(-hi_least);
-  lo_most = rows_max(lo_most);
-  lo_least = -rows_max(-lo_least);
-  // this split's tiles: all of [lo_least, hi_most) in equal parts, none of fewer than a.least tiles
-  const int begin = hi_most > 0 ? lo_least / kTile : 0, end = (int)(((int64_t)hi_most + kTile - 1) / kTile);
-  const int each = max(a.least, (int)((end - begin + a.splits - 1) / a.splits));
-  const int64_t from = begin + (int64_t)split * each;
-  if (a.splits > 1 && from >= end) {      // nothing left for this split
-    for (int i = SHARE ? threadIdx.x : lane; i < (SHARE ? kRows : 16 * RT); i += SHARE ? kBlock : kWave)
-      *(float2 *)(a.part_sums + ((int64_t)item * kRows + (SHARE ? 0 : wave * 16 * RT) + i) * 2) = float2{-__builtin_inff(), 0.0f};
-    return;
-  }
-  const int stop = (int)min((int64_t)end, from + each);
-  const char *table = a.table + b * a.tb;
-  const int64_t head = kv * a.head_stride;
-  constexpr int kStep = SHARE ? W : 1;
-  const int64_t start = from + (SHARE ? wave : 0);
-  Sums<D, RT> sums;
+  r.hi_most = rows_max(r.hi_most);
+  r.hi_least = -rows_max(-r.hi_least);
+  r.lo_most = rows_max(r.lo_most);
+  r.lo_least = -rows_max(-r.lo_least);
+  return r;
+}
+
+// a split's tiles [from, stop): all of [lo_least, hi_most) in equal parts, none of fewer than a.least tiles
+struct Part { int64_t from; int stop, end; };
+__device__ __forceinline__ Part part_of(const AttentionArgs &a, const Reach &r, uint32_t split) {
+  const int begin = r.hi_most > 0 ? r.lo_least / kTile : 0;
+  Part p;
+  p.end = (int)(((int64_t)r.hi_most + kTile - 1) / kTile);
+  const int each = max(a.least, (int)((p.end - begin + a.splits - 1) / a.splits));
+  p.from = begin + (int64_t)split * each;
+  p.stop = (int)min((int64_t)p.end, p.from + each);
+  return p;
+}
+
+// queries as operands, and sums at their start
+template <int D, int RT, int PARTS_Q, int PARTS_P>
+__device__ __forceinline__ void start_rows(const AttentionArgs &a, Rows<D, RT, PARTS_Q> &rows, Sums<D, RT> &sums, int b, int kv, int first_row, int all_rows, int n, int g) {
+  typedef Shape<D> S;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const int row = first_row + rt * 16 + n, t = row < all_rows ? (int)fast_quotient((uint32_t)row, a.per_kv_div) : 0;
@@ -552,6 +572,59 @@ __global__ __launch_bounds__(kBlock, D * RT <= 128 ? 2 : 1) void attention_kerne
     sums.total[rt] = sums.bad[rt] = f32x4{0, 0, 0, 0};
     sums.top[rt] = -__builtin_inff();
   }
+}
+
+template <int D, int RT> __device__ __forceinline__ void mark_bad(Sums<D, RT> &sums) {
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+    for (int i = 0; i < Shape<D>::kTiles; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (sums.bad[rt][r] > 0.0f) sums.out[rt][i][r] = __builtin_nanf("");
+}
+
+// a workgroup's place: items are blocks of rows fastest, then heads of the cache, sequences, and splits.  (Workgroups go to the XCDs in turn, and where
+// sequences are of different lengths the later splits are empty: with splits fastest some XCDs had most of the work.)
+struct Work { uint32_t item, split, block; int b, kv; };
+__device__ __forceinline__ Work work_of(const AttentionArgs &a, uint32_t item) {
+  Work w;
+  w.item = item;
+  w.split = fast_quotient(item, a.units_div);
+  const uint32_t unit = item - w.split * a.units_div.d, bh = fast_quotient(unit, a.blocks_div);
+  w.block = unit - bh * a.blocks_div.d;
+  w.b = (int)fast_quotient(bh, a.kv_div);
+  w.kv = (int)bh - w.b * (int)a.kv_div.d;
+  return w;
+}
+
+// Few rows: a workgroup's four wavefronts have the same rows and every fourth tile each, and join their sums in LDS.  Memory bounds this; what a
+// wavefront needs of a tile goes from memory to its registers, 4-bit codes, and becomes halves there.
+template <int D, int RT, int PARTS_Q, int PARTS_P>
+__global__ __launch_bounds__(kBlock, D * RT <= (PARTS_Q == 1 ? 256 : 128) ? 2 : 1) void attention_kernel(const AttentionArgs a) {
+  typedef Shape<D> S;
+  typedef typename TypeOfParts<PARTS_Q, PARTS_P>::T T;
+  constexpr int W = kBlock / kWave, kPart = S::kTiles < 8 ? S::kTiles : 8;
+  constexpr int kRows = 16 * RT;             // of a unit
+  __shared__ float part[W][16][16][kPart];
+  __shared__ float tops[W][RT][16], totals[W][RT][16];
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), n = lane % 16, g = lane / 16;
+  const LaneOffsets lanes = lane_offsets<D>(a, n, g);
+  warm_arguments<AttentionArgs>();
+  const Work work = work_of(a, a.first_item + blockIdx.x);
+  const int b = work.b, kv = work.kv, first_row = (int)work.block * kRows, all_rows = a.queries * a.per_kv;
+  Rows<D, RT, PARTS_Q> rows;
+  const Reach reach = reach_of<D, RT, PARTS_Q>(a, rows, b, first_row, all_rows, n);
+  const Part range = part_of(a, reach, work.split);
+  if (a.splits > 1 && range.from >= range.end) {      // nothing left for this split
+    if (threadIdx.x < kRows) *(float2 *)(a.part_sums + ((int64_t)work.item * kRows + threadIdx.x) * 2) = float2{-__builtin_inff(), 0.0f};
+    return;
+  }
+  Sums<D, RT> sums;
+  start_rows<D, RT, PARTS_Q, PARTS_P>(a, rows, sums, b, kv, first_row, all_rows, n, g);
+  const char *table = a.table + b * a.tb;
+  const int64_t head = kv * a.head_stride, start = range.from + wave;
+  const int stop = range.stop;
   if (start < stop) {
     // kAhead tiles are on their way while one is worked on, and the entries of one more: loads are issued whether or not there are tiles left,
     // so that every wait is for a known number of them (past the end they go to the sequence's first entry's page, or page 0).
@@ -559,9 +632,9 @@ __global__ __launch_bounds__(kBlock, D * RT <= 128 ? 2 : 1) void attention_kerne
     uint32_t fine = 0;            // two bits for each buffer: whether its half tiles' pages are
     Entry e0, e1;
     const auto entries = [&](int64_t tile) {
-      const int64_t j = tile < stop ? tile * kTile : (int64_t)hi_most;
-      e0 = entry_of(a, table, j, hi_most);
-      e1 = entry_of(a, table, j + 16, hi_most);
+      const int64_t j = tile < stop ? tile * kTile : (int64_t)reach.hi_most;
+      e0 = entry_of(a, table, j, reach.hi_most);
+      e1 = entry_of(a, table, j + 16, reach.hi_most);
     };
     const auto load = [&](Raw<D> &to, int buffer) {
       const Place p0 = place_of<D>(a, head, e0), p1 = place_of<D>(a, head, e1);
@@ -573,110 +646,230 @@ __global__ __launch_bounds__(kBlock, D * RT <= 128 ? 2 : 1) void attention_kerne
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       load(raw[i], i);
-      entries(start + (i + 1) * kStep);
+      entries(start + (i + 1) * W);
     }
     for (int64_t t = start; t < stop;) {
 #pragma unroll
       for (int i = 0; i <= kAhead; ++i) {
         load(raw[(i + kAhead) % (kAhead + 1)], (i + kAhead) % (kAhead + 1));
-        entries(t + (kAhead + 1) * kStep);
+        entries(t + (kAhead + 1) * W);
         const int j0 = (int)t * kTile;
         const uint32_t mine = fine >> 2 * i & 3;
-        one_tile<D, RT, PARTS_Q, PARTS_P>(sums, rows, raw[i], g, j0, mine == 3 && j0 >= lo_most && j0 + kTile <= hi_least, (mine & 1) != 0,
+        FromRegisters<D> source = {raw[i]};
+        one_tile<D, RT, PARTS_Q, PARTS_P>(sums, rows, source, g, j0, mine == 3 && j0 >= reach.lo_most && j0 + kTile <= reach.hi_least, (mine & 1) != 0,
                                           (mine & 2) != 0);
-        t += kStep;
+        t += W;
         if (t >= stop) break;
       }
     }
   }
+  mark_bad<D, RT>(sums);
+  const bool whole = a.splits == 1;
+  // the wavefronts' sums, relative to the largest of their maxima
+  if (g == 0) {
 #pragma unroll
-  for (int rt = 0; rt < RT; ++rt)
+    for (int rt = 0; rt < RT; ++rt) {
+      tops[wave][rt][n] = sums.top[rt];
+      totals[wave][rt][n] = sums.total[rt][0];
+    }
+  }
+  __syncthreads();
 #pragma unroll
-    for (int i = 0; i < S::kTiles; ++i)
+  for (int rt = 0; rt < RT; ++rt) {
+    float top = -__builtin_inff();
+#pragma unroll
+    for (int w = 0; w < W; ++w) top = fmaxf(top, tops[w][rt][n]);
+    const float keep = top == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(sums.top[rt] - top);
+#pragma unroll
+    for (int at = 0; at < S::kTiles; at += kPart) {
+      if (rt + at > 0) __syncthreads();
 #pragma unroll
       for (int r = 0; r < 4; ++r)
-        if (sums.bad[rt][r] > 0.0f) sums.out[rt][i][r] = __builtin_nanf("");
-  const bool whole = a.splits == 1;
-  if constexpr (SHARE) {
-    // the wavefronts' sums, relative to the largest of their maxima
-    if (g == 0) {
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        tops[wave][rt][n] = sums.top[rt];
-        totals[wave][rt][n] = sums.total[rt][0];
+        for (int i = 0; i < kPart; ++i) part[wave][n][4 * g + r][i] = sums.out[rt][at + i][r] * keep;
+      __syncthreads();
+      // a thread has D/16 (eight at a time) channels of a row now
+      const int rn = threadIdx.x / 16, rj = threadIdx.x % 16, row = first_row + rt * 16 + rn;
+      float v[kPart], most = -__builtin_inff(), total = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kPart; ++i) v[i] = 0.0f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) most = fmaxf(most, tops[w][rt][rn]);
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        total += most == -__builtin_inff() ? totals[w][rt][rn] : totals[w][rt][rn] * __builtin_amdgcn_exp2f(tops[w][rt][rn] - most);
+#pragma unroll
+        for (int i = 0; i < kPart; ++i) v[i] += part[w][rn][rj][i];
       }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      float top = -__builtin_inff();
-#pragma unroll
-      for (int w = 0; w < W; ++w) top = fmaxf(top, tops[w][rt][n]);
-      const float keep = top == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(sums.top[rt] - top);
-#pragma unroll
-      for (int at = 0; at < S::kTiles; at += kPart) {
-        if (rt + at > 0) __syncthreads();
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-          for (int i = 0; i < kPart; ++i) part[wave][n][4 * g + r][i] = sums.out[rt][at + i][r] * keep;
-        __syncthreads();
-        // a thread has D/16 (eight at a time) channels of a row now
-        const int rn = threadIdx.x / 16, rj = threadIdx.x % 16, row = first_row + rt * 16 + rn;
-        float v[kPart], most = -__builtin_inff(), total = 0.0f;
-#pragma unroll
-        for (int i = 0; i < kPart; ++i) v[i] = 0.0f;
-#pragma unroll
-        for (int w = 0; w < W; ++w) most = fmaxf(most, tops[w][rt][rn]);
-#pragma unroll
-        for (int w = 0; w < W; ++w) {
-          total += most == -__builtin_inff() ? totals[w][rt][rn] : totals[w][rt][rn] * __builtin_amdgcn_exp2f(tops[w][rt][rn] - most);
-#pragma unroll
-          for (int i = 0; i < kPart; ++i) v[i] += part[w][rn][rj][i];
-        }
-        if (row >= all_rows) continue;
-        const int channel = rj * S::kTiles + at;
-        if (whole) {
-          const int t = (int)fast_quotient((uint32_t)row, a.per_kv_div), h = kv * a.per_kv + row - t * a.per_kv;
-          const float over = total == 0.0f ? 0.0f : 1.0f / total;
-#pragma unroll
-          for (int i = 0; i < kPart; ++i) v[i] = total == 0.0f ? 0.0f : v[i] * over;
-          store_row<T, kPart>(a, a.out + b * a.ob + t * a.ot + h * a.oh, channel, v);
-          if (a.log_sum && rj == 0 && at == 0) *(float *)(a.log_sum + b * a.lb + t * a.lt + h * a.lh) = log_of(most, total);
-        } else {
-          const int64_t at_row = (int64_t)item * kRows + rt * 16 + rn;
-          float *to = a.parts + at_row * D + channel;
-#pragma unroll
-          for (int i = 0; i < kPart; i += 4) *(f32x4 *)(to + i) = f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]};
-          if (rj == 0 && at == 0) *(float2 *)(a.part_sums + at_row * 2) = float2{most, total};
-        }
-      }
-    }
-  } else {
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      const int row = first_row + rt * 16 + n;
       if (row >= all_rows) continue;
-      const float total = sums.total[rt][0], over = total == 0.0f ? 0.0f : 1.0f / total;
-      const int t = (int)fast_quotient((uint32_t)row, a.per_kv_div), h = kv * a.per_kv + row - t * a.per_kv;
-      const int64_t at_row = (int64_t)item * kRows + wave * 16 * RT + rt * 16 + n;
+      const int channel = rj * S::kTiles + at;
+      if (whole) {
+        const int t = (int)fast_quotient((uint32_t)row, a.per_kv_div), h = kv * a.per_kv + row - t * a.per_kv;
+        const float over = total == 0.0f ? 0.0f : 1.0f / total;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int channel = (4 * g + r) * S::kTiles;
-        float v[S::kTiles];
+        for (int i = 0; i < kPart; ++i) v[i] = total == 0.0f ? 0.0f : v[i] * over;
+        store_row<T, kPart>(a, a.out + b * a.ob + t * a.ot + h * a.oh, channel, v);
+        if (a.log_sum && rj == 0 && at == 0) *(float *)(a.log_sum + b * a.lb + t * a.lt + h * a.lh) = log_of(most, total);
+      } else {
+        const int64_t at_row = (int64_t)work.item * kRows + rt * 16 + rn;
+        float *to = a.parts + at_row * D + channel;
 #pragma unroll
-        for (int i = 0; i < S::kTiles; ++i) v[i] = !whole ? sums.out[rt][i][r] : total == 0.0f ? 0.0f : sums.out[rt][i][r] * over;
-        if (whole) {
-          store_row<T, S::kTiles>(a, a.out + b * a.ob + t * a.ot + h * a.oh, channel, v);
-        } else {
+        for (int i = 0; i < kPart; i += 4) *(f32x4 *)(to + i) = f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]};
+        if (rj == 0 && at == 0) *(float2 *)(a.part_sums + at_row * 2) = float2{most, total};
+      }
+    }
+  }
+}
+
+// Many rows: each of a workgroup's wavefronts has rows of its own, and all go over the same tiles.  Products bound this, and what is done to the codes before
+// them: each wavefront makes a quarter of a tile's operands, for all four, in LDS; two tiles have room there, so that one is made while the other is used.
+template <int D, int RT, int PARTS_Q, int PARTS_P>
+__global__ __launch_bounds__(kBlock, 2) void attention_many_kernel(const AttentionArgs a) {
+  typedef Shape<D> S;
+  typedef typename TypeOfParts<PARTS_Q, PARTS_P>::T T;
+  constexpr int W = kBlock / kWave, kRows = 16 * RT * W, kFrags = 2 * S::kWords + S::kTiles + 1;
+  constexpr int kMyK = 2 * S::kWords / W, kMyV = S::kTiles / W;        // operands that a wavefront makes
+  __shared__ f16x8 operands[2][kFrags * kWave];
+  __shared__ Reach reaches[W];
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), n = lane % 16, g = lane / 16;
+  const LaneOffsets lanes = lane_offsets<D>(a, n, g);
+  warm_arguments<AttentionArgs>();
+  const Work work = work_of(a, a.first_item + blockIdx.x);
+  const int b = work.b, kv = work.kv, first_row = (int)work.block * kRows + wave * 16 * RT, all_rows = a.queries * a.per_kv;
+  Rows<D, RT, PARTS_Q> rows;
+  Reach reach = reach_of<D, RT, PARTS_Q>(a, rows, b, first_row, all_rows, n);
+  if (lane == 0) reaches[wave] = reach;
+  __syncthreads();
 #pragma unroll
-          for (int i = 0; i < S::kTiles; i += 4) *(f32x4 *)(a.parts + at_row * D + channel + i) = f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]};
+  for (int w = 0; w < W; ++w) {
+    reach.hi_most = max(reach.hi_most, reaches[w].hi_most);
+    reach.hi_least = min(reach.hi_least, reaches[w].hi_least);
+    reach.lo_least = min(reach.lo_least, reaches[w].lo_least);
+    reach.lo_most = max(reach.lo_most, reaches[w].lo_most);
+  }
+  reach.hi_most = __builtin_amdgcn_readfirstlane(reach.hi_most);
+  reach.hi_least = __builtin_amdgcn_readfirstlane(reach.hi_least);
+  reach.lo_least = __builtin_amdgcn_readfirstlane(reach.lo_least);
+  reach.lo_most = __builtin_amdgcn_readfirstlane(reach.lo_most);
+  const Part range = part_of(a, reach, work.split);
+  if (a.splits > 1 && range.from >= range.end) {      // nothing left for this split
+    for (int i = threadIdx.x; i < kRows; i += kBlock) *(float2 *)(a.part_sums + ((int64_t)work.item * kRows + i) * 2) = float2{-__builtin_inff(), 0.0f};
+    return;
+  }
+  Sums<D, RT> sums;
+  start_rows<D, RT, PARTS_Q, PARTS_P>(a, rows, sums, b, kv, first_row, all_rows, n, g);
+  const char *table = a.table + b * a.tb;
+  const int64_t head = kv * a.head_stride;
+  const int start = (int)range.from, stop = range.stop;
+  if (start < stop) {
+    // A wavefront's share: words wave, wave + 4 ... of K's (D = 64: one word of one half tile), channels of V likewise
+    struct Share {
+      uint32_t k[kMyK], k_scale[kMyK], v[2][S::kWords], v_scale[2][2];
+      bool fine[2];
+    } share;
+    Entry e0, e1;
+    const auto entries = [&](int64_t tile) {
+      const int64_t j = tile < stop ? tile * kTile : (int64_t)reach.hi_most;
+      e0 = entry_of(a, table, j, reach.hi_most);
+      e1 = entry_of(a, table, j + 16, reach.hi_most);
+    };
+    const auto load = [&]() {
+      const Place p0 = place_of<D>(a, head, e0), p1 = place_of<D>(a, head, e1);
+      share.fine[0] = p0.fine;
+      share.fine[1] = p1.fine;
+#pragma unroll
+      for (int i = 0; i < kMyK; ++i) {
+        const int f = i * W + wave, w = S::kWords == 2 ? f % 2 : f % S::kWords;     // operand f: half tile f / words, word f % words
+        const Place &p = f < S::kWords ? p0 : p1;
+        share.k[i] = *(const __attribute__((address_space(1))) uint32_t *)(p.codes + (lanes.k + w / S::kRun * 16 * S::kRun + w % S::kRun * 4));
+        share.k_scale[i] = *(const __attribute__((address_space(1))) uint16_t *)(p.scales + (lanes.k_scale + w / S::kRun * lanes.k_scale_step));
+      }
+      load_words<S::kWords>(share.v[0], p0.codes + lanes.v);
+      load_words<S::kWords>(share.v[1], p1.codes + lanes.v);
+      load_words<2>(share.v_scale[0], p0.scales + lanes.v_scale);
+      load_words<2>(share.v_scale[1], p1.scales + lanes.v_scale);
+    };
+    const auto whole_tile = [&](int tile) {
+      return share.fine[0] && share.fine[1] && tile * kTile >= reach.lo_most && tile * kTile + kTile <= reach.hi_least;
+    };
+    const auto make = [&](f16x8 *to, bool whole) {
+#pragma unroll
+      for (int i = 0; i < kMyK; ++i) {
+        const uint32_t codes = share.k[i], both = share.k_scale[i];
+        const f16x2 one = __builtin_bit_cast(f16x2, both), s = {one.x, one.x};
+        Frag f;
+        f.p[0] = two_codes<0>(codes) * s, f.p[1] = two_codes<1>(codes) * s;
+        f.p[2] = two_codes<2>(codes) * s, f.p[3] = two_codes<3>(codes) * s;
+        to[(i * W + wave) * kWave + lane] = f.v;
+      }
+      if (!whole) {
+        const Frag bad = fix_scales(share.v_scale);
+        if (wave == 0) to[(2 * S::kWords + S::kTiles) * kWave + lane] = bad.v;
+      }
+      // channels of V: two of a byte of the codes for each wavefront (one where there are four)
+      Twins<D> twins[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) twins[i] = twins_of<D>(share.v[i / 2], i % 2);
+#pragma unroll
+      for (int c = 0; c < kMyV; ++c) {
+        const int t = S::kTiles == 4 ? wave : c / 2 * 8 + 2 * wave + c % 2;
+        Frag f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t two = share.v_scale[i / 2][i % 2];
+          uint32_t word;
+          if constexpr (S::kTiles == 4) word = (wave & 1 ? twins[i].odd[0] : twins[i].even[0]) >> 8 * (wave >> 1);
+          else word = (c % 2 ? twins[i].odd[c / 2] : twins[i].even[c / 2]) >> 8 * wave;
+          f.p[i] = two_codes<0>(word) * __builtin_bit_cast(f16x2, two);
         }
+        to[(2 * S::kWords + t) * kWave + lane] = f.v;
       }
-      if (g == 0) {
-        if (whole && a.log_sum) *(float *)(a.log_sum + b * a.lb + t * a.lt + h * a.lh) = log_of(sums.top[rt], total);
-        if (!whole) *(float2 *)(a.part_sums + at_row * 2) = float2{sums.top[rt], total};
+    };
+    entries(start);
+    load();
+    entries(start + 1);
+    bool fine0 = share.fine[0], fine1 = share.fine[1], whole = whole_tile(start);
+    make(operands[0], whole);
+    load();
+    entries(start + 2);
+    __syncthreads();
+    for (int t = start; t < stop; ++t) {
+      const int now = (t - start) & 1;
+      const bool next_fine0 = share.fine[0], next_fine1 = share.fine[1], next_whole = whole_tile(t + 1);
+      if (t + 1 < stop) make(operands[1 - now], next_whole);
+      load();
+      entries(t + 3);
+      FromLds<D> source = {&operands[now][lane]};
+      one_tile<D, RT, PARTS_Q, PARTS_P>(sums, rows, source, g, t * kTile, whole, fine0, fine1);
+      fine0 = next_fine0, fine1 = next_fine1, whole = next_whole;
+      __syncthreads();
+    }
+  }
+  mark_bad<D, RT>(sums);
+  const bool alone = a.splits == 1;
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int row = first_row + rt * 16 + n;
+    if (row >= all_rows) continue;
+    const float total = sums.total[rt][0], over = total == 0.0f ? 0.0f : 1.0f / total;
+    const int t = (int)fast_quotient((uint32_t)row, a.per_kv_div), h = kv * a.per_kv + row - t * a.per_kv;
+    const int64_t at_row = (int64_t)work.item * kRows + wave * 16 * RT + rt * 16 + n;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int channel = (4 * g + r) * S::kTiles;
+      float v[S::kTiles];
+#pragma unroll
+      for (int i = 0; i < S::kTiles; ++i) v[i] = !alone ? sums.out[rt][i][r] : total == 0.0f ? 0.0f : sums.out[rt][i][r] * over;
+      if (alone) {
+        store_row<T, S::kTiles>(a, a.out + b * a.ob + t * a.ot + h * a.oh, channel, v);
+      } else {
+#pragma unroll
+        for (int i = 0; i < S::kTiles; i += 4) *(f32x4 *)(a.parts + at_row * D + channel + i) = f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]};
       }
+    }
+    if (g == 0) {
+      if (alone && a.log_sum) *(float *)(a.log_sum + b * a.lb + t * a.lt + h * a.lh) = log_of(sums.top[rt], total);
+      if (!alone) *(float2 *)(a.part_sums + at_row * 2) = float2{sums.top[rt], total};
     }
   }
 }
@@ -801,22 +994,16 @@ bool whole_rows(const ocn_tensor *t) {
 }
 
 template <int D> void launch_attention(const AttentionArgs &a, const Launch &l, uint32_t grid, hipStream_t stream) {
-#define OCN_ATTENTION(RT, SHARE)                                                                                                       \
-  do {                                                                                                                                 \
-    if (a.type == OCN_BFLOAT16) hipLaunchKernelGGL((attention_kernel<D, RT, 1, 1, SHARE>), dim3(grid), dim3(kBlock), 0, stream, a);     \
-    else if (a.type == OCN_HALF) hipLaunchKernelGGL((attention_kernel<D, RT, 1, 2, SHARE>), dim3(grid), dim3(kBlock), 0, stream, a);    \
-    else hipLaunchKernelGGL((attention_kernel<D, RT, 2, 2, SHARE>), dim3(grid), dim3(kBlock), 0, stream, a);                            \
+#define OCN_ATTENTION(KERNEL, RT)                                                                                              \
+  do {                                                                                                                         \
+    if (a.type == OCN_BFLOAT16) hipLaunchKernelGGL((KERNEL<D, RT, 1, 1>), dim3(grid), dim3(kBlock), 0, stream, a);              \
+    else if (a.type == OCN_HALF) hipLaunchKernelGGL((KERNEL<D, RT, 1, 2>), dim3(grid), dim3(kBlock), 0, stream, a);             \
+    else hipLaunchKernelGGL((KERNEL<D, RT, 2, 2>), dim3(grid), dim3(kBlock), 0, stream, a);                                     \
   } while (0)
-  if constexpr (D < 256) {
-    if (l.row_tiles == 2) {
-      if (l.share) OCN_ATTENTION(2, true);
-      else OCN_ATTENTION(2, false);
-    }
-  }
-  if (l.row_tiles == 1) {
-    if (l.share) OCN_ATTENTION(1, true);
-    else if constexpr (D == 256) OCN_ATTENTION(1, false);
-  }
+  constexpr int kMany = D == 256 ? 1 : 2;      // row tiles whose sums and queries fit a wavefront's registers, two wavefronts to a SIMD
+  if (!l.share) OCN_ATTENTION(attention_many_kernel, kMany);
+  else if (l.row_tiles == 1) OCN_ATTENTION(attention_kernel, 1);
+  else if constexpr (D < 256) OCN_ATTENTION(attention_kernel, 2);
 #undef OCN_ATTENTION
 }
 
