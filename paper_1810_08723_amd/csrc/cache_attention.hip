@@ -110,7 +110,7 @@ template <int N> __device__ __forceinline__ void load_words(uint32_t *to, Global
 }
 
 // the entry of 16 tokens from j on (a multiple of 16); past the sequence's end some other entry, which is not used
-__device__ __forceinline__ Entry entry_of(const AttentionArgs &a, const char *row, int64_t j, int end) {
+__device__ __forceinline__ Entry entry_of(const AttentionArgs &a, const char *row, int j, int end) {
   typedef const __attribute__((address_space(4))) uint32_t *Word;
   Entry e;
   e.in = j < end;
@@ -206,6 +206,20 @@ __device__ __forceinline__ float larger(float a, float b) {
   asm("v_max_f32 %0, %1, %2" : "=v"(c) : "v"(a), "v"(b));
   return c;
 }
+// The largest and smallest of a lane's eight scores; NaNs are passed over.  (No assembly here: the compiler keeps a reader of a product's result
+// waiting, assembly it does not.)
+__device__ __forceinline__ float largest(const f32x4 *s) {
+  float m = s[0][0];
+#pragma unroll
+  for (int i = 1; i < 8; ++i) m = fmaxf(m, s[i / 4][i % 4]);
+  return m;
+}
+__device__ __forceinline__ float smallest(const f32x4 *s) {
+  float m = s[0][0];
+#pragma unroll
+  for (int i = 1; i < 8; ++i) m = fminf(m, s[i / 4][i % 4]);
+  return m;
+}
 // the largest of the four lanes that hold a row
 __device__ __forceinline__ float row_max(float x) {
   const auto a = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
@@ -232,7 +246,9 @@ template <int D, int RT> struct Sums {
   f32x4 out[RT][Shape<D>::kTiles];   // out^T
   f32x4 total[RT];                   // of the weights (all four the same)
   f32x4 bad[RT];                     // how many tokens with a NaN as V's scale a row sees, in tiles that are not seen whole
-  float top[RT];                     // what weights are relative to (base 2)
+  float shift[RT];                   // a weight is 2^(score * scale + shift): kWeightBits less what weights are relative to
+  float raise[RT];                   // a score above this raises that; minus infinity before the first
+  __device__ __forceinline__ float top(int rt) const { return raise[rt] == -__builtin_inff() ? -__builtin_inff() : kWeightBits - shift[rt]; }
 };
 
 template <int D, int RT, int PARTS_Q> struct Rows {
@@ -273,6 +289,7 @@ template <int D> struct FromRegisters {
     return f.v;
   }
   __device__ __forceinline__ f16x8 bad() { return fix_scales(raw.v_scale).v; }
+  __device__ __forceinline__ void early() const {}
   __device__ __forceinline__ void start_v() {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -290,13 +307,18 @@ template <int D> struct FromRegisters {
 };
 
 // ... or LDS, where a workgroup's wavefronts have put them: K [half tile][word], V [channel of a lane], the tokens with bad scales; 16 bytes of each lane
-template <int D> struct FromLds {
+template <int D, int EARLY> struct FromLds {
   typedef Shape<D> S;
   const f16x8 *at;         // of this lane
   __device__ __forceinline__ f16x8 k(int x, int w) const { return at[(x * S::kWords + w) * kWave]; }
-  __device__ __forceinline__ f16x8 v(int t) const { return at[(2 * S::kWords + t) * kWave]; }
+  f16x8 first[EARLY];     // V's, read before the weights are formed (the compiler moves no read over their branches): 558 us without, 518 with six
+  __device__ __forceinline__ f16x8 v(int t) const { return t < EARLY ? first[t] : at[(2 * S::kWords + t) * kWave]; }
   __device__ __forceinline__ f16x8 bad() const { return at[(2 * S::kWords + S::kTiles) * kWave]; }
   __device__ __forceinline__ void start_v() const {}
+  __device__ __forceinline__ void early() {
+#pragma unroll
+    for (int t = 0; t < EARLY; ++t) first[t] = at[(2 * S::kWords + t) * kWave];
+  }
 };
 
 // whole: every row sees every token of the tile
@@ -320,12 +342,12 @@ __device__ __forceinline__ void one_tile(Sums<D, RT> &s, const Rows<D, RT, PARTS
 #pragma unroll
         for (int part = 0; part < PARTS_Q; ++part) score[rt][x] = product(k, rows.q[rt][part][w], score[rt][x]);
     }
+  source.early();
   float least[RT];       // (unseen places may make it too small, and the tile takes longer)
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    least[rt] = score[rt][0][0];
-#pragma unroll
-    for (int i = 1; i < 8; ++i) least[rt] = fminf(least[rt], score[rt][i / 4][i % 4]);
+    least[rt] = smallest(score[rt]);
+    asm volatile("" : "+v"(least[rt]));      // (here: put off to where it is used, it would keep a second copy of the scores)
   }
   uint32_t sees[RT];     // which of its eight tokens a lane's row sees
   if (!whole) {
@@ -350,18 +372,18 @@ __device__ __forceinline__ void one_tile(Sums<D, RT> &s, const Rows<D, RT, PARTS
   bool apart = false;    // whether some weights are below the floor
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    float most = score[rt][0][0];
-#pragma unroll
-    for (int i = 1; i < 8; ++i) most = fmaxf(most, score[rt][i / 4][i % 4]);
-    most = row_max(most) * rows.scale[rt];
-    if (__builtin_amdgcn_ballot_w64(most > s.top[rt] + kRaise)) {
-      const float now = fmaxf(s.top[rt], most), keep = now == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(s.top[rt] - now);
-      s.top[rt] = now;
+    const float most = largest(score[rt]);
+    if (__builtin_amdgcn_ballot_w64(most > s.raise[rt])) {
+      // (the four lanes of a row meet here alone: most tiles do not come here)
+      const float before = s.top(rt), now = fmaxf(before, row_max(most) * rows.scale[rt]);
+      const float keep = now == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(before - now);
+      s.shift[rt] = now == -__builtin_inff() ? kWeightBits : kWeightBits - now;
+      s.raise[rt] = (now + kRaise) / rows.scale[rt];
 #pragma unroll
       for (int i = 0; i < S::kTiles; ++i) s.out[rt][i] *= keep;
       s.total[rt] *= keep;
     }
-    const float shift = kWeightBits - (s.top[rt] == -__builtin_inff() ? 0.0f : s.top[rt]);
+    const float shift = s.shift[rt];
 #pragma unroll
     for (int i = 0; i < 8; ++i) weight[rt][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(score[rt][i / 4][i % 4], rows.scale[rt], shift));
     if (!whole) {
@@ -570,7 +592,8 @@ __device__ __forceinline__ void start_rows(const AttentionArgs &a, Rows<D, RT, P
 #pragma unroll
     for (int i = 0; i < S::kTiles; ++i) sums.out[rt][i] = f32x4{0, 0, 0, 0};
     sums.total[rt] = sums.bad[rt] = f32x4{0, 0, 0, 0};
-    sums.top[rt] = -__builtin_inff();
+    sums.shift[rt] = kWeightBits;
+    sums.raise[rt] = -__builtin_inff();
   }
 }
 
@@ -632,7 +655,7 @@ __global__ __launch_bounds__(kBlock, D * RT <= (PARTS_Q == 1 ? 256 : 128) ? 2 : 
     uint32_t fine = 0;            // two bits for each buffer: whether its half tiles' pages are
     Entry e0, e1;
     const auto entries = [&](int64_t tile) {
-      const int64_t j = tile < stop ? tile * kTile : (int64_t)reach.hi_most;
+      const int j = tile < stop ? (int)tile * kTile : reach.hi_most;       // (16 more stay below 2^31: a table has pages for 64 tokens fewer)
       e0 = entry_of(a, table, j, reach.hi_most);
       e1 = entry_of(a, table, j + 16, reach.hi_most);
     };
@@ -669,7 +692,7 @@ __global__ __launch_bounds__(kBlock, D * RT <= (PARTS_Q == 1 ? 256 : 128) ? 2 : 
   if (g == 0) {
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      tops[wave][rt][n] = sums.top[rt];
+      tops[wave][rt][n] = sums.top(rt);
       totals[wave][rt][n] = sums.total[rt][0];
     }
   }
@@ -679,7 +702,7 @@ __global__ __launch_bounds__(kBlock, D * RT <= (PARTS_Q == 1 ? 256 : 128) ? 2 : 
     float top = -__builtin_inff();
 #pragma unroll
     for (int w = 0; w < W; ++w) top = fmaxf(top, tops[w][rt][n]);
-    const float keep = top == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(sums.top[rt] - top);
+    const float keep = top == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(sums.top(rt) - top);
 #pragma unroll
     for (int at = 0; at < S::kTiles; at += kPart) {
       if (rt + at > 0) __syncthreads();
@@ -727,6 +750,7 @@ template <int D, int RT, int PARTS_Q, int PARTS_P>
 __global__ __launch_bounds__(kBlock, 2) void attention_many_kernel(const AttentionArgs a) {
   typedef Shape<D> S;
   typedef typename TypeOfParts<PARTS_Q, PARTS_P>::T T;
+  constexpr int kEarly = PARTS_Q == 2 ? 1 : D == 128 ? 6 : 4;          // what the registers have room for
   constexpr int W = kBlock / kWave, kRows = 16 * RT * W, kFrags = 2 * S::kWords + S::kTiles + 1;
   constexpr int kMyK = 2 * S::kWords / W, kMyV = S::kTiles / W;        // operands that a wavefront makes
   __shared__ f16x8 operands[2][kFrags * kWave];
@@ -768,8 +792,8 @@ __global__ __launch_bounds__(kBlock, 2) void attention_many_kernel(const Attenti
       bool fine[2];
     } share;
     Entry e0, e1;
-    const auto entries = [&](int64_t tile) {
-      const int64_t j = tile < stop ? tile * kTile : (int64_t)reach.hi_most;
+    const auto entries = [&](int tile) {
+      const int j = tile < stop ? tile * kTile : reach.hi_most;
       e0 = entry_of(a, table, j, reach.hi_most);
       e1 = entry_of(a, table, j + 16, reach.hi_most);
     };
@@ -839,7 +863,7 @@ __global__ __launch_bounds__(kBlock, 2) void attention_many_kernel(const Attenti
       if (t + 1 < stop) make(operands[1 - now], next_whole);
       load();
       entries(t + 3);
-      FromLds<D> source = {&operands[now][lane]};
+      FromLds<D, kEarly> source = {&operands[now][lane]};
       one_tile<D, RT, PARTS_Q, PARTS_P>(sums, rows, source, g, t * kTile, whole, fine0, fine1);
       fine0 = next_fine0, fine1 = next_fine1, whole = next_whole;
       __syncthreads();
@@ -868,8 +892,8 @@ __global__ __launch_bounds__(kBlock, 2) void attention_many_kernel(const Attenti
       }
     }
     if (g == 0) {
-      if (alone && a.log_sum) *(float *)(a.log_sum + b * a.lb + t * a.lt + h * a.lh) = log_of(sums.top[rt], total);
-      if (!alone) *(float2 *)(a.part_sums + at_row * 2) = float2{sums.top[rt], total};
+      if (alone && a.log_sum) *(float *)(a.log_sum + b * a.lb + t * a.lt + h * a.lh) = log_of(sums.top(rt), total);
+      if (!alone) *(float2 *)(a.part_sums + at_row * 2) = float2{sums.top(rt), total};
     }
   }
 }
