@@ -622,7 +622,8 @@ __device__ __forceinline__ Work work_of(const AttentionArgs &a, uint32_t item) {
 }
 
 // Few rows: a workgroup's four wavefronts have the same rows and every fourth tile each, and join their sums in LDS.  Memory bounds this; what a
-// wavefront needs of a tile goes from memory to its registers, 4-bit codes, and becomes halves there.
+// wavefront needs of a tile goes from memory to its registers, 4-bit codes, and becomes halves there.  64 sequences of 4000 tokens, 8 heads of 128 channels, 4 query
+// heads each (295 MB): 61.4 us, 4.8 TB/s, where a large copy has 5.2.
 template <int D, int RT, int PARTS_Q, int PARTS_P>
 __global__ __launch_bounds__(kBlock, D * RT <= (PARTS_Q == 1 ? 256 : 128) ? 2 : 1) void attention_kernel(const AttentionArgs a) {
   typedef Shape<D> S;
@@ -745,7 +746,8 @@ __global__ __launch_bounds__(kBlock, D * RT <= (PARTS_Q == 1 ? 256 : 128) ? 2 : 
 }
 
 // Many rows: each of a workgroup's wavefronts has rows of its own, and all go over the same tiles.  Products bound this, and what is done to the codes before
-// them: each wavefront makes a quarter of a tile's operands, for all four, in LDS; two tiles have room there, so that one is made while the other is used.
+// them: each wavefront makes a quarter of a tile's operands, for all four, in LDS; two tiles have room there, so that one is made while the other is used.  1024 queries of 32 heads over 3333 and 8192 tokens:
+// 523 us, 337 TFLOP/s of the 1390 that a large product reaches: a wavefront has nothing else to do between its two products, and registers allow two to a SIMD.
 template <int D, int RT, int PARTS_Q, int PARTS_P>
 __global__ __launch_bounds__(kBlock, 2) void attention_many_kernel(const AttentionArgs a) {
   typedef Shape<D> S;
@@ -1076,7 +1078,8 @@ int ocn_cache_attention(const ocn_tensor *q, const ocn_tensor *cache, const ocn_
     if (log_sum && log_sum->size[d] != q->size[d]) return OCN_ERR_SHAPE;
   for (int d = 0; d < 2; ++d)
     if (visible->size[d] != q->size[d] && visible->size[d] != 1) return OCN_ERR_SHAPE;
-  if (!std::isfinite(scale) || window < 0) return OCN_ERR_DOMAIN;
+  const float scale2 = (float)(scale * 1.4426950408889634074);      // (of exponents of two)
+  if (!std::isfinite(scale2) || window < 0) return OCN_ERR_DOMAIN;
   const HeadOperand ops[6] = {{q, false, nullptr, nullptr}, {cache, false, nullptr, nullptr}, {table, false, nullptr, nullptr},
                               {visible, false, nullptr, nullptr}, {out, true, q, nullptr}, {log_sum, true, nullptr, nullptr}};
   if ((rc = check_operands(ops, 6)) != OCN_OK) return rc;
@@ -1128,7 +1131,7 @@ int ocn_cache_attention(const ocn_tensor *q, const ocn_tensor *cache, const ocn_
   a.type = q->dtype;
   a.table_wide = table->dtype == OCN_INT64;
   a.seen_wide = visible->dtype == OCN_INT64;
-  a.scale = (float)(scale * 1.4426950408889634074);
+  a.scale = scale2;
   const hipStream_t s = (hipStream_t)stream;
   if (d == 64) return run_attention<64>(a, l, (uint32_t)rows, s);
   if (d == 128) return run_attention<128>(a, l, (uint32_t)rows, s);

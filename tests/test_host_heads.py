@@ -211,3 +211,10 @@ def test_frequencies():
                dict(rotary_dim=2, stretch="base", factor=2.0), dict(rotary_dim=8, stretch="turns", factor=2.0, original=0.0),
                dict(rotary_dim=8, stretch="index", factor=2.0, original=100.0, low=4.0, high=4.0)):
         assert code(ocn.rotary_frequencies, **kw) == "SHAPE"
+
+
+def test_attention_refuses_scales_past_single_precision():
+    q, o = T("half", (2, 3, 8, 64)), T("half", (2, 3, 8, 64), base=1)
+    c, t, n = cache_of(base=3), T("int32", (2, 9), base=4), T("int64", (2, 3), base=5)
+    for scale in (3e38, -3e38, 1e300):
+        assert code(ocn.cache_attention, q, c, t, n, o, scale) == "DOMAIN"
