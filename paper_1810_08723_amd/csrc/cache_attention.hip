@@ -35,7 +35,14 @@ struct AttentionArgs {
 constexpr int64_t kLeastTiles = 8;             // of a split: two for each wavefront
 constexpr int64_t kAloneTiles = 20;            // up to so many a second launch costs more than splits gain (17 tiles: 9.6 us, 11.0 in splits)
 constexpr int64_t kMaxSplits = kWave;          // a lane each when they are joined
-constexpr int64_t kWorkgroups = 768;           // worth launching: three to a CU
+constexpr int64_t kAtOnce = 512;               // workgroups that keep all CUs at work, two to each: so many units are not split where memory bounds them
+                                               // (512 of 4000 tokens: 62 us, 65 in three splits)
+constexpr int64_t kWorkgroups = 1536;          // fewer units are, into so many: sequences of different lengths even out (256 units of 1 to 8190 tokens: 47 us, 52 in 768;
+constexpr int64_t kWorkgroupsWide = 768;       // of 256 channels, which two wavefronts of a SIMD take: 128 units of 100 to 8000 tokens 49.6 us, 52.2 in 1536)
+constexpr int64_t kManyWorkgroups = 2048;      // where a workgroup's wavefronts have rows of their own
+constexpr int64_t kManyLeast = 16;             // tiles of a split, at least, where units leave CUs without work (352 units of 256 tiles: 457 us in two splits, 365 in five)
+constexpr int64_t kManyLeastFull = 64;         // and where they do not (512 units of 256 tiles: 518 and 426 us in four, 512 of 47 tiles: 96 and 156 in three)
+constexpr uint32_t kJoinRows = 1024;           // from so many on a wavefront joins a row, a workgroup below
 
 // ---------------------------------------------------------------------------------------
 // The kernel.  Query heads of one head of the cache, of one or more queries, are the rows of its tiles: 16 a tile.  For 32 tokens at a
@@ -747,7 +754,7 @@ __global__ __launch_bounds__(kBlock, D * RT <= (PARTS_Q == 1 ? 256 : 128) ? 2 : 
 
 // Many rows: each of a workgroup's wavefronts has rows of its own, and all go over the same tiles.  Products bound this, and what is done to the codes before
 // them: each wavefront makes a quarter of a tile's operands, for all four, in LDS; two tiles have room there, so that one is made while the other is used.  1024 queries of 32 heads over 3333 and 8192 tokens:
-// 523 us, 337 TFLOP/s of the 1390 that a large product reaches: a wavefront has nothing else to do between its two products, and registers allow two to a SIMD.
+// 433 us, 406 TFLOP/s of the 1390 that a large product reaches: a wavefront has nothing else to do between its two products, and registers allow two to a SIMD.
 template <int D, int RT, int PARTS_Q, int PARTS_P>
 __global__ __launch_bounds__(kBlock, 2) void attention_many_kernel(const AttentionArgs a) {
   typedef Shape<D> S;
@@ -900,16 +907,19 @@ __global__ __launch_bounds__(kBlock, 2) void attention_many_kernel(const Attenti
   }
 }
 
-// The parts of a row joined.  A workgroup has a row: lanes first have the parts' sums, then each wavefront adds up every fourth part, four of them on
-// their way at a time, and the four meet in LDS.  Parts that saw nothing have a sum of zero and are not read.
-template <int D> __global__ __launch_bounds__(kBlock) void attention_join_kernel(const AttentionArgs a, uint32_t rows, int unit_rows) {
-  constexpr int C = D / kWave, W = kBlock / kWave, U = 4;
-  __shared__ float part[W][D];
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  for (uint32_t r = blockIdx.x; r < rows; r += gridDim.x) {
+// The parts of a row joined.  Lanes first have the parts' sums; then WAVES wavefronts add up every WAVES-th part, four of them on their way at a time, and
+// meet in LDS: all four of a workgroup where rows are few, one to a row where there are kJoinRows of them (65536 rows in four parts: 92 us less than with four).
+// Parts that saw nothing have a sum of zero and are not read.
+template <int D, int WAVES> __global__ __launch_bounds__(kBlock) void attention_join_kernel(const AttentionArgs a, uint32_t rows, int unit_rows) {
+  constexpr int C = D / kWave, U = 4, R = kBlock / kWave / WAVES;     // R: rows of a workgroup
+  __shared__ float part[WAVES > 1 ? WAVES : 1][WAVES > 1 ? D : 1];
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) % WAVES;
+  const int all_rows = a.queries * a.per_kv, splits = (int)a.splits;
+  const int64_t units = a.units_div.d;
+  for (uint32_t r0 = blockIdx.x; r0 < (rows + R - 1) / R; r0 += gridDim.x) {
+    const uint32_t r = r0 * R + (R > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) : 0);
+    if (r >= rows) break;            // (R > 1: of one wavefront, and no barrier follows)
     // rows: query heads fastest, then queries, heads of the cache, sequences
-    const int all_rows = a.queries * a.per_kv, splits = (int)a.splits;
-    const int64_t units = a.units_div.d;
     const int bh = (int)(r / (uint32_t)all_rows), row = (int)(r % (uint32_t)all_rows), b = bh / (int)a.kv_div.d, kv = bh % (int)a.kv_div.d;
     const int64_t unit = (int64_t)bh * a.blocks_div.d + row / unit_rows, place = row % unit_rows;
     float2 ml = {-__builtin_inff(), 0.0f};
@@ -923,11 +933,11 @@ template <int D> __global__ __launch_bounds__(kBlock) void attention_join_kernel
     float v[C];
 #pragma unroll
     for (int i = 0; i < C; ++i) v[i] = 0.0f;
-    for (int s0 = wave; s0 < splits; s0 += W * U) {
+    for (int s0 = wave; s0 < splits; s0 += WAVES * U) {
       float x[U][C];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int s = s0 + u * W;
+        const int s = s0 + u * WAVES;
 #pragma unroll
         for (int i = 0; i < C; ++i) x[u][i] = 0.0f;
         if (s < splits && any >> s & 1) {
@@ -938,24 +948,30 @@ template <int D> __global__ __launch_bounds__(kBlock) void attention_join_kernel
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const float ws = __shfl(w, (s0 + u * W) & 63);
+        const float ws = __shfl(w, (s0 + u * WAVES) & 63);
 #pragma unroll
         for (int i = 0; i < C; ++i) v[i] += ws * x[u][i];
       }
     }
-#pragma unroll
-    for (int i = 0; i < C; ++i) part[wave][lane * C + i] = v[i];
-    __syncthreads();
     const int t = row / a.per_kv, h = kv * a.per_kv + row % a.per_kv;
     char *to = a.out + b * a.ob + t * a.ot + h * a.oh;
-    for (int c = threadIdx.x; c < D; c += kBlock) {
-      float x = 0.0f;
+    if constexpr (WAVES == 1) {
 #pragma unroll
-      for (int i = 0; i < W; ++i) x += part[i][c];
-      store_from_float(to + c * a.oe, a.type, total == 0.0f ? 0.0f : x / total);
+      for (int i = 0; i < C; ++i) store_from_float(to + (lane * C + i) * a.oe, a.type, total == 0.0f ? 0.0f : v[i] / total);
+      if (a.log_sum && lane == 0) *(float *)(a.log_sum + b * a.lb + t * a.lt + h * a.lh) = log_of(top, total);
+    } else {
+#pragma unroll
+      for (int i = 0; i < C; ++i) part[wave][lane * C + i] = v[i];
+      __syncthreads();
+      for (int c = threadIdx.x; c < D; c += kBlock) {
+        float x = 0.0f;
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) x += part[i][c];
+        store_from_float(to + c * a.oe, a.type, total == 0.0f ? 0.0f : x / total);
+      }
+      if (a.log_sum && threadIdx.x == 0) *(float *)(a.log_sum + b * a.lb + t * a.lt + h * a.lh) = log_of(top, total);
+      __syncthreads();
     }
-    if (a.log_sum && threadIdx.x == 0) *(float *)(a.log_sum + b * a.lb + t * a.lt + h * a.lh) = log_of(top, total);
-    __syncthreads();
   }
 }
 
@@ -979,7 +995,12 @@ Launch launch_of(int64_t batch, int64_t queries, int64_t heads, int64_t kv, int6
   l.blocks = (rows + l.unit_rows - 1) / l.unit_rows;
   l.units = batch * kv * l.blocks;
   const int64_t tiles = (capacity + kTile - 1) / kTile, most = tiles <= kAloneTiles ? 1 : tiles / kLeastTiles;
-  l.splits = std::min<int64_t>({most, kMaxSplits, std::max<int64_t>(1, kWorkgroups / std::max<int64_t>(l.units, 1))});
+  const int64_t wanted = l.units >= kAtOnce ? 1 : (channels == 256 ? kWorkgroupsWide : kWorkgroups) / std::max<int64_t>(l.units, 1);
+  l.splits = std::max<int64_t>(1, std::min<int64_t>({most, kMaxSplits, wanted}));
+  if (!l.share) {
+    const int64_t least = l.units < kAtOnce ? kManyLeast : kManyLeastFull;
+    l.splits = std::max<int64_t>(1, std::min<int64_t>({most, tiles / least, kMaxSplits, kManyWorkgroups / std::max<int64_t>(l.units, 1)}));
+  }
   l.items = l.units * l.splits;
   return l;
 }
@@ -1042,8 +1063,14 @@ template <int D> int run_attention(AttentionArgs &a, const Launch &l, uint32_t r
     if (rc != OCN_OK) return rc;
   }
   if (l.splits == 1) return OCN_OK;
-  const uint32_t joins = (uint32_t)std::min<int64_t>(rows, max_launch_blocks());
-  hipLaunchKernelGGL((attention_join_kernel<D>), dim3(joins), dim3(kBlock), 0, stream, a, rows, (int)l.unit_rows);
+  constexpr int kWaves = kBlock / kWave;
+  if (rows >= kJoinRows) {
+    const uint32_t joins = (uint32_t)std::min<int64_t>((rows + kWaves - 1) / kWaves, max_launch_blocks());
+    hipLaunchKernelGGL((attention_join_kernel<D, 1>), dim3(joins), dim3(kBlock), 0, stream, a, rows, (int)l.unit_rows);
+  } else {
+    const uint32_t joins = (uint32_t)std::min<int64_t>(rows, max_launch_blocks());
+    hipLaunchKernelGGL((attention_join_kernel<D, kWaves>), dim3(joins), dim3(kBlock), 0, stream, a, rows, (int)l.unit_rows);
+  }
   return done(hipGetLastError());
 }
 

@@ -220,3 +220,8 @@ def test_gradient_of_the_norm_in_a_graph():
         torch.cuda.synchronize()
         for a, b in zip(*outs):
             assert torch.equal(a, b), i
+
+
+def test_several_launches_of_many_rows():
+    """As above, with so many rows that a wavefront joins each"""
+    test_several_launches(60, 60)
