@@ -4,6 +4,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <type_traits>
 
 #include "dev_types.hpp"
 #include "head_types.hpp"
@@ -57,22 +58,25 @@ constexpr uint32_t kJoinRows = 1024;           // from so many on a wavefront jo
 // A code becomes a half in one conversion for two; times its group's scale it is exact (two bits of the code, nine of the
 // scale), so that K and V lose nothing.  V's pairs are two tokens of a channel: nibbles of two rows are put side by side (one shift and one bit
 // select for eight codes) before they are converted.  Q is exact where its type has no more than 11 bits: a row is scaled by a power of two so that its
-// largest channel is near 2^13.  Weights are rounded to half (2^-11, below half a step of a bfloat16 result); for half results
-// a second product adds what that rounding left (PARTS_P = 2), for float results Q has two parts as well (PARTS_Q = 2).
+// largest channel is near 2^13; for float tensors it has two parts.  A weight is the sum of two halves, and a second product adds what the first
+// leaves (to half alone, 2^-11, bfloat16 results differed from those of single precision in one channel of twenty by a step; 433 us instead of 495 for the prompt below).
 //
 // The maximum of a row that its weights are relative to is raised, and sums rescaled, only where a score is 2^4 above it; weights are times 2^11, so
 // that they stay below 2^15.  The sum of the weights is one more product, with ones.
 //
-// Weights that far below the largest are not numbers that a half (or the second part of one) holds to its full precision; left
-// at that, a channel that is zero in the tokens with large weights would lose what the others give it.  A tile with weights below kFloor
-// takes them out and multiplies them apart, times a power of two, in as many steps as they need: weights keep their relative precision down to 2^-126.
+// Two halves hold a weight to 2^-22 of itself, or, where the second is among the smallest that a half holds, to 2^-36 of the largest. Left at that, a channel that is
+// zero in the tokens with large weights would lose what the others give it.  A tile with weights below Floor::kLeast
+// takes them out and multiplies them apart, times a power of two, in as many steps as they need: down to 2^-126 no weight is further off than 2^-11 of itself (2^-21
+// for float results).
 // ---------------------------------------------------------------------------------------
 
 constexpr float kWeightBits = 11.0f, kRaise = 4.0f;
-template <int PARTS_Q> struct Floor {     // (float results keep 2^-20 of a small weight, the others half of their own step)
-  static constexpr int kBits = PARTS_Q == 1 ? -14 : -4;       // log2 of the smallest weight that is taken as it is
+constexpr int kWeightParts = 2;           // halves that a weight is the sum of
+template <class T> constexpr int kQueryParts = sizeof(T) == 4 ? 2 : 1;    // ... and a channel of a query
+template <class T> struct Floor {     // (float results keep 2^-21 of a small weight, the others 2^-11)
+  static constexpr int kBits = kQueryParts<T> == 1 ? -14 : -4;       // log2 of the smallest weight that is taken as it is
   static constexpr int kStep = 14 - kBits;                    // what smaller ones are multiplied by, and again: below 2^14 then
-  static constexpr float kLeast = PARTS_Q == 1 ? 0x1p-14f : 0x1p-4f, kUp = PARTS_Q == 1 ? 0x1p28f : 0x1p18f, kDown = 1.0f / kUp;
+  static constexpr float kLeast = kQueryParts<T> == 1 ? 0x1p-14f : 0x1p-4f, kUp = kQueryParts<T> == 1 ? 0x1p28f : 0x1p18f, kDown = 1.0f / kUp;
 };
 constexpr int kTile = 32;            // tokens
 constexpr int kAhead = 1;             // tiles on their way (two: 67.99 for 66.03 us of two contexts of 100 k and 131 k tokens)
@@ -175,6 +179,18 @@ union Frag {
   uint32_t u[4];
 };
 
+// Weights 2 i and 2 i + 1 of eight as sums of two halves each.  (What the first leaves is one instruction a weight, which reads it as a half: the factor
+// is hidden, or the compiler converts it back and subtracts.)
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ void in_parts(Frag *p, int i, float w0, float w1) {
+  p[0].p[i] = __builtin_convertvector((f32x2{w0, w1}), f16x2);
+  asm("" : "+v"(p[0].u[i]));      // (or each is converted by itself once more)
+  const f16x2 h = p[0].p[i];
+  float minus = -1.0f;
+  asm("" : "+s"(minus));
+  p[1].p[i] = __builtin_convertvector((f32x2{__builtin_fmaf((float)h.x, minus, w0), __builtin_fmaf((float)h.y, minus, w1)}), f16x2);
+}
+
 // bits of a where the mask has ones, of b elsewhere
 __device__ __forceinline__ uint32_t select_bits(uint32_t mask, uint32_t a, uint32_t b) { return (a & mask) | (b & ~mask); }
 
@@ -258,8 +274,8 @@ template <int D, int RT> struct Sums {
   __device__ __forceinline__ float top(int rt) const { return raise[rt] == -__builtin_inff() ? -__builtin_inff() : kWeightBits - shift[rt]; }
 };
 
-template <int D, int RT, int PARTS_Q> struct Rows {
-  f16x8 q[RT][PARTS_Q][Shape<D>::kWords];
+template <int D, int RT, class T> struct Rows {
+  f16x8 q[RT][kQueryParts<T>][Shape<D>::kWords];
   float scale[RT];                   // of a score
   int lo[RT], hi[RT];                // tokens that a row sees
 };
@@ -329,10 +345,10 @@ template <int D, int EARLY> struct FromLds {
 };
 
 // whole: every row sees every token of the tile
-template <int D, int RT, int PARTS_Q, int PARTS_P, class Source>
-__device__ __forceinline__ void one_tile(Sums<D, RT> &s, const Rows<D, RT, PARTS_Q> &rows, Source &source, int g, int j0, bool whole, bool fine0, bool fine1) {
+template <int D, int RT, class T, class Source>
+__device__ __forceinline__ void one_tile(Sums<D, RT> &s, const Rows<D, RT, T> &rows, Source &source, int g, int j0, bool whole, bool fine0, bool fine1) {
   typedef Shape<D> S;
-  typedef Floor<PARTS_Q> F;
+  typedef Floor<T> F;
   const f16x8 ones = {1, 1, 1, 1, 1, 1, 1, 1};
   f32x4 score[RT][2];
 #pragma unroll
@@ -347,7 +363,7 @@ __device__ __forceinline__ void one_tile(Sums<D, RT> &s, const Rows<D, RT, PARTS
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-        for (int part = 0; part < PARTS_Q; ++part) score[rt][x] = product(k, rows.q[rt][part][w], score[rt][x]);
+        for (int part = 0; part < kQueryParts<T>; ++part) score[rt][x] = product(k, rows.q[rt][part][w], score[rt][x]);
     }
   source.early();
   float least[RT];       // (unseen places may make it too small, and the tile takes longer)
@@ -374,7 +390,7 @@ __device__ __forceinline__ void one_tile(Sums<D, RT> &s, const Rows<D, RT, PARTS
       s.bad[rt] = product(bad, seen.v, s.bad[rt]);
     }
   }
-  Frag p[RT][PARTS_P];
+  Frag p[RT][kWeightParts];
   float weight[RT][8];
   bool apart = false;    // whether some weights are below the floor
 #pragma unroll
@@ -414,14 +430,20 @@ __device__ __forceinline__ void one_tile(Sums<D, RT> &s, const Rows<D, RT, PARTS
       bool left = false, any = false;
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
+        float two[2];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const float x = small[rt][i] * F::kUp, w = x < F::kLeast ? 0.0f : x;
           small[rt][i] = x < F::kLeast ? x : 0.0f;
           any |= w > 0.0f;
           left |= small[rt][i] > 0.0f;
-          p[rt][0].v[i] = (f16)w;
-          if constexpr (PARTS_P == 2) p[rt][1].v[i] = (f16)(w - (float)p[rt][0].v[i]);
+          two[i % 2] = w;
+          if constexpr (kQueryParts<T> == 2) {      // (a weight at a time: pairs take four registers more than there are)
+            p[rt][0].v[i] = (f16)w;
+            p[rt][1].v[i] = (f16)(w - (float)p[rt][0].v[i]);
+          } else if (i % 2) {
+            in_parts(p[rt], i / 2, two[0], two[1]);
+          }
         }
       }
       if (__builtin_amdgcn_ballot_w64(any)) {
@@ -432,12 +454,12 @@ __device__ __forceinline__ void one_tile(Sums<D, RT> &s, const Rows<D, RT, PARTS
           for (int rt = 0; rt < RT; ++rt) {
             f32x4 add = {0, 0, 0, 0};
 #pragma unroll
-            for (int part = 0; part < PARTS_P; ++part) add = product(f, p[rt][part].v, add);
+            for (int part = 0; part < kWeightParts; ++part) add = product(f, p[rt][part].v, add);
             s.out[rt][t] += add * down;
             if (t == 0) {
               add = f32x4{0, 0, 0, 0};
 #pragma unroll
-              for (int part = 0; part < PARTS_P; ++part) add = product(ones, p[rt][part].v, add);
+              for (int part = 0; part < kWeightParts; ++part) add = product(ones, p[rt][part].v, add);
               s.total[rt] += add * down;
             }
           }
@@ -449,12 +471,9 @@ __device__ __forceinline__ void one_tile(Sums<D, RT> &s, const Rows<D, RT, PARTS
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      p[rt][0].v[i] = (f16)weight[rt][i];
-      if constexpr (PARTS_P == 2) p[rt][1].v[i] = (f16)(weight[rt][i] - (float)p[rt][0].v[i]);
-    }
+    for (int i = 0; i < 4; ++i) in_parts(p[rt], i, weight[rt][2 * i], weight[rt][2 * i + 1]);
 #pragma unroll
-    for (int part = 0; part < PARTS_P; ++part) s.total[rt] = product(ones, p[rt][part].v, s.total[rt]);
+    for (int part = 0; part < kWeightParts; ++part) s.total[rt] = product(ones, p[rt][part].v, s.total[rt]);
   }
 #pragma unroll
   for (int t = 0; t < S::kTiles; ++t) {
@@ -462,14 +481,9 @@ __device__ __forceinline__ void one_tile(Sums<D, RT> &s, const Rows<D, RT, PARTS
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-      for (int part = 0; part < PARTS_P; ++part) s.out[rt][t] = product(f, p[rt][part].v, s.out[rt][t]);
+      for (int part = 0; part < kWeightParts; ++part) s.out[rt][t] = product(f, p[rt][part].v, s.out[rt][t]);
   }
 }
-
-// PARTS_Q and PARTS_P say which type a call's tensors have
-template <int PARTS_Q, int PARTS_P> struct TypeOfParts { typedef bf16 T; };
-template <> struct TypeOfParts<1, 2> { typedef f16 T; };
-template <> struct TypeOfParts<2, 2> { typedef float T; };
 
 // N channels of a row to memory
 template <class T, int N> __device__ __forceinline__ void store_row(const AttentionArgs &a, char *row, int channel, const float *v) {
@@ -488,30 +502,30 @@ template <class T, int N> __device__ __forceinline__ void store_row(const Attent
 __device__ __forceinline__ float log_of(float top, float total) { return total == 0.0f ? -__builtin_inff() : 0.69314718f * (top - kWeightBits + __builtin_log2f(total)); }
 
 // eight channels of a query, as they are in memory
-template <int PARTS_Q> __device__ __forceinline__ void load_channels(uint32_t *to, const char *row, int channel, bool any, const AttentionArgs &a) {
-  constexpr int N = 4 * PARTS_Q;
+template <class T> __device__ __forceinline__ void load_channels(uint32_t *to, const char *row, int channel, bool any, const AttentionArgs &a) {
+  constexpr int N = 2 * (int)sizeof(T);
 #pragma unroll
   for (int i = 0; i < N; ++i) to[i] = 0;
   if (!any) return;
   if (a.whole_q) {
 #pragma unroll
-    for (int i = 0; i < N; i += 4) load_words<4>(to + i, (Global)(uint64_t)(row + channel * (2 * PARTS_Q) + 4 * i));
+    for (int i = 0; i < N; i += 4) load_words<4>(to + i, (Global)(uint64_t)(row + channel * (int)sizeof(T) + 4 * i));
   } else {
     int64_t step = a.qe;
     asm volatile("" : "+s"(step)::"memory");   // (here and now: hoisted out of all loops, the addresses took more registers than the tiles)
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      if constexpr (PARTS_Q == 2) to[i] = *(const uint32_t *)(row + (channel + i) * step);
+      if constexpr (sizeof(T) == 4) to[i] = *(const uint32_t *)(row + (channel + i) * step);
       else to[i] = *(const uint16_t *)(row + (channel + 2 * i) * step) | (uint32_t)*(const uint16_t *)(row + (channel + 2 * i + 1) * step) << 16;
     }
   }
 }
-template <int PARTS_Q, int PARTS_P> __device__ __forceinline__ void channels_of(float *x, const uint32_t *from) {
+template <class T> __device__ __forceinline__ void channels_of(float *x, const uint32_t *from) {
 #pragma unroll
-  for (int i = 0; i < 4 * PARTS_Q; ++i) {
-    if constexpr (PARTS_Q == 2) {
+  for (int i = 0; i < 2 * (int)sizeof(T); ++i) {
+    if constexpr (sizeof(T) == 4) {
       x[i] = __builtin_bit_cast(float, from[i]);
-    } else if constexpr (PARTS_P == 1) {
+    } else if constexpr (std::is_same_v<T, bf16>) {
       x[2 * i] = __builtin_bit_cast(float, from[i] << 16);
       x[2 * i + 1] = __builtin_bit_cast(float, from[i] & 0xffff0000u);
     } else {
@@ -524,8 +538,8 @@ template <int PARTS_Q, int PARTS_P> __device__ __forceinline__ void channels_of(
 // what an item's rows see: the tokens of a row, and the ends of all of them
 struct Reach { int hi_most, hi_least, lo_least, lo_most; };
 
-template <int D, int RT, int PARTS_Q>
-__device__ __forceinline__ Reach reach_of(const AttentionArgs &a, Rows<D, RT, PARTS_Q> &rows, int b, int first_row, int all_rows, int n) {
+template <int D, int RT, class T>
+__device__ __forceinline__ Reach reach_of(const AttentionArgs &a, Rows<D, RT, T> &rows, int b, int first_row, int all_rows, int n) {
   Reach r = {0, 0x7fffffff, 0x7fffffff, 0};
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
@@ -562,21 +576,21 @@ __device__ __forceinline__ Part part_of(const AttentionArgs &a, const Reach &r, 
 }
 
 // queries as operands, and sums at their start
-template <int D, int RT, int PARTS_Q, int PARTS_P>
-__device__ __forceinline__ void start_rows(const AttentionArgs &a, Rows<D, RT, PARTS_Q> &rows, Sums<D, RT> &sums, int b, int kv, int first_row, int all_rows, int n, int g) {
+template <int D, int RT, class T>
+__device__ __forceinline__ void start_rows(const AttentionArgs &a, Rows<D, RT, T> &rows, Sums<D, RT> &sums, int b, int kv, int first_row, int all_rows, int n, int g) {
   typedef Shape<D> S;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const int row = first_row + rt * 16 + n, t = row < all_rows ? (int)fast_quotient((uint32_t)row, a.per_kv_div) : 0;
-    uint32_t q[S::kWords][8 * PARTS_Q / 2];       // as they are in memory: two 16-bit channels, or a float, in a word
+    uint32_t q[S::kWords][2 * sizeof(T)];       // as they are in memory: two 16-bit channels, or a float, in a word
     float most = 0.0f;
     const char *from_row = a.q + b * a.qb + t * a.qt + (int64_t)(kv * a.per_kv + row - t * a.per_kv) * a.qh;
 #pragma unroll
     for (int w = 0; w < S::kWords; ++w) {
       const int channel = 8 * (w / S::kRun * 4 * S::kRun + S::kRun * g + w % S::kRun);
-      load_channels<PARTS_Q>(q[w], from_row, channel, row < all_rows, a);
+      load_channels<T>(q[w], from_row, channel, row < all_rows, a);
       float x[8];
-      channels_of<PARTS_Q, PARTS_P>(x, q[w]);
+      channels_of<T>(x, q[w]);
 #pragma unroll
       for (int i = 0; i < 8; ++i) most = fmaxf(most, __builtin_fabsf(x[i]));
     }
@@ -588,12 +602,12 @@ __device__ __forceinline__ void start_rows(const AttentionArgs &a, Rows<D, RT, P
 #pragma unroll
     for (int w = 0; w < S::kWords; ++w) {
       float x[8];
-      channels_of<PARTS_Q, PARTS_P>(x, q[w]);
+      channels_of<T>(x, q[w]);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         x[i] = __builtin_amdgcn_ldexpf(x[i], up) * sign;
         rows.q[rt][0][w][i] = (f16)x[i];
-        if constexpr (PARTS_Q == 2) rows.q[rt][1][w][i] = (f16)(x[i] - (float)rows.q[rt][0][w][i]);
+        if constexpr (kQueryParts<T> == 2) rows.q[rt][1][w][i] = (f16)(x[i] - (float)rows.q[rt][0][w][i]);
       }
     }
 #pragma unroll
@@ -628,13 +642,16 @@ __device__ __forceinline__ Work work_of(const AttentionArgs &a, uint32_t item) {
   return w;
 }
 
+// Wavefronts of a SIMD: what registers allow without spilling (of 256 channels twenty spill; one wavefront instead takes 65.9 us for 57.8 of 128 units of 100 to 8000 tokens).
+// Three for 128 channels: 49.7 us for 54.7 of 256 units of 1 to 8190 tokens.
+template <int D, int RT, class T> constexpr int kWavesOfSimd = kQueryParts<T> == 1 && D == 128 && RT == 1 ? 3 : D * RT <= (kQueryParts<T> == 1 ? 256 : 128) ? 2 : 1;
+
 // Few rows: a workgroup's four wavefronts have the same rows and every fourth tile each, and join their sums in LDS.  Memory bounds this; what a
 // wavefront needs of a tile goes from memory to its registers, 4-bit codes, and becomes halves there.  64 sequences of 4000 tokens, 8 heads of 128 channels, 4 query
-// heads each (295 MB): 61.4 us, 4.8 TB/s, where a large copy has 5.2.
-template <int D, int RT, int PARTS_Q, int PARTS_P>
-__global__ __launch_bounds__(kBlock, D * RT <= (PARTS_Q == 1 ? 256 : 128) ? 2 : 1) void attention_kernel(const AttentionArgs a) {
+// heads each (295 MB): 62.6 us, 4.7 TB/s, where a large copy has 5.2.
+template <int D, int RT, class T>
+__global__ __launch_bounds__(kBlock, (kWavesOfSimd<D, RT, T>)) void attention_kernel(const AttentionArgs a) {
   typedef Shape<D> S;
-  typedef typename TypeOfParts<PARTS_Q, PARTS_P>::T T;
   constexpr int W = kBlock / kWave, kPart = S::kTiles < 8 ? S::kTiles : 8;
   constexpr int kRows = 16 * RT;             // of a unit
   __shared__ float part[W][16][16][kPart];
@@ -644,15 +661,15 @@ __global__ __launch_bounds__(kBlock, D * RT <= (PARTS_Q == 1 ? 256 : 128) ? 2 : 
   warm_arguments<AttentionArgs>();
   const Work work = work_of(a, a.first_item + blockIdx.x);
   const int b = work.b, kv = work.kv, first_row = (int)work.block * kRows, all_rows = a.queries * a.per_kv;
-  Rows<D, RT, PARTS_Q> rows;
-  const Reach reach = reach_of<D, RT, PARTS_Q>(a, rows, b, first_row, all_rows, n);
+  Rows<D, RT, T> rows;
+  const Reach reach = reach_of<D, RT, T>(a, rows, b, first_row, all_rows, n);
   const Part range = part_of(a, reach, work.split);
   if (a.splits > 1 && range.from >= range.end) {      // nothing left for this split
     if (threadIdx.x < kRows) *(float2 *)(a.part_sums + ((int64_t)work.item * kRows + threadIdx.x) * 2) = float2{-__builtin_inff(), 0.0f};
     return;
   }
   Sums<D, RT> sums;
-  start_rows<D, RT, PARTS_Q, PARTS_P>(a, rows, sums, b, kv, first_row, all_rows, n, g);
+  start_rows<D, RT, T>(a, rows, sums, b, kv, first_row, all_rows, n, g);
   const char *table = a.table + b * a.tb;
   const int64_t head = kv * a.head_stride, start = range.from + wave;
   const int stop = range.stop;
@@ -687,7 +704,7 @@ __global__ __launch_bounds__(kBlock, D * RT <= (PARTS_Q == 1 ? 256 : 128) ? 2 : 
         const int j0 = (int)t * kTile;
         const uint32_t mine = fine >> 2 * i & 3;
         FromRegisters<D> source = {raw[i]};
-        one_tile<D, RT, PARTS_Q, PARTS_P>(sums, rows, source, g, j0, mine == 3 && j0 >= reach.lo_most && j0 + kTile <= reach.hi_least, (mine & 1) != 0,
+        one_tile<D, RT, T>(sums, rows, source, g, j0, mine == 3 && j0 >= reach.lo_most && j0 + kTile <= reach.hi_least, (mine & 1) != 0,
                                           (mine & 2) != 0);
         t += W;
         if (t >= stop) break;
@@ -754,12 +771,11 @@ __global__ __launch_bounds__(kBlock, D * RT <= (PARTS_Q == 1 ? 256 : 128) ? 2 : 
 
 // Many rows: each of a workgroup's wavefronts has rows of its own, and all go over the same tiles.  Products bound this, and what is done to the codes before
 // them: each wavefront makes a quarter of a tile's operands, for all four, in LDS; two tiles have room there, so that one is made while the other is used.  1024 queries of 32 heads over 3333 and 8192 tokens:
-// 433 us, 406 TFLOP/s of the 1390 that a large product reaches: a wavefront has nothing else to do between its two products, and registers allow two to a SIMD.
-template <int D, int RT, int PARTS_Q, int PARTS_P>
+// 495 us, 356 TFLOP/s of the 1390 that a large product reaches: a wavefront has nothing else to do between its two products, and registers allow two to a SIMD.
+template <int D, int RT, class T>
 __global__ __launch_bounds__(kBlock, 2) void attention_many_kernel(const AttentionArgs a) {
   typedef Shape<D> S;
-  typedef typename TypeOfParts<PARTS_Q, PARTS_P>::T T;
-  constexpr int kEarly = PARTS_Q == 2 ? 1 : D == 128 ? 6 : 4;          // what the registers have room for
+  constexpr int kEarly = kQueryParts<T> == 2 ? 1 : D == 128 ? 6 : 4;          // what the registers have room for
   constexpr int W = kBlock / kWave, kRows = 16 * RT * W, kFrags = 2 * S::kWords + S::kTiles + 1;
   constexpr int kMyK = 2 * S::kWords / W, kMyV = S::kTiles / W;        // operands that a wavefront makes
   __shared__ f16x8 operands[2][kFrags * kWave];
@@ -769,8 +785,8 @@ __global__ __launch_bounds__(kBlock, 2) void attention_many_kernel(const Attenti
   warm_arguments<AttentionArgs>();
   const Work work = work_of(a, a.first_item + blockIdx.x);
   const int b = work.b, kv = work.kv, first_row = (int)work.block * kRows + wave * 16 * RT, all_rows = a.queries * a.per_kv;
-  Rows<D, RT, PARTS_Q> rows;
-  Reach reach = reach_of<D, RT, PARTS_Q>(a, rows, b, first_row, all_rows, n);
+  Rows<D, RT, T> rows;
+  Reach reach = reach_of<D, RT, T>(a, rows, b, first_row, all_rows, n);
   if (lane == 0) reaches[wave] = reach;
   __syncthreads();
 #pragma unroll
@@ -790,7 +806,7 @@ __global__ __launch_bounds__(kBlock, 2) void attention_many_kernel(const Attenti
     return;
   }
   Sums<D, RT> sums;
-  start_rows<D, RT, PARTS_Q, PARTS_P>(a, rows, sums, b, kv, first_row, all_rows, n, g);
+  start_rows<D, RT, T>(a, rows, sums, b, kv, first_row, all_rows, n, g);
   const char *table = a.table + b * a.tb;
   const int64_t head = kv * a.head_stride;
   const int start = (int)range.from, stop = range.stop;
@@ -873,7 +889,7 @@ __global__ __launch_bounds__(kBlock, 2) void attention_many_kernel(const Attenti
       load();
       entries(t + 3);
       FromLds<D, kEarly> source = {&operands[now][lane]};
-      one_tile<D, RT, PARTS_Q, PARTS_P>(sums, rows, source, g, t * kTile, whole, fine0, fine1);
+      one_tile<D, RT, T>(sums, rows, source, g, t * kTile, whole, fine0, fine1);
       fine0 = next_fine0, fine1 = next_fine1, whole = next_whole;
       __syncthreads();
     }
@@ -1043,9 +1059,9 @@ bool whole_rows(const ocn_tensor *t) {
 template <int D> void launch_attention(const AttentionArgs &a, const Launch &l, uint32_t grid, hipStream_t stream) {
 #define OCN_ATTENTION(KERNEL, RT)                                                                                              \
   do {                                                                                                                         \
-    if (a.type == OCN_BFLOAT16) hipLaunchKernelGGL((KERNEL<D, RT, 1, 1>), dim3(grid), dim3(kBlock), 0, stream, a);              \
-    else if (a.type == OCN_HALF) hipLaunchKernelGGL((KERNEL<D, RT, 1, 2>), dim3(grid), dim3(kBlock), 0, stream, a);             \
-    else hipLaunchKernelGGL((KERNEL<D, RT, 2, 2>), dim3(grid), dim3(kBlock), 0, stream, a);                                     \
+    if (a.type == OCN_BFLOAT16) hipLaunchKernelGGL((KERNEL<D, RT, bf16>), dim3(grid), dim3(kBlock), 0, stream, a);              \
+    else if (a.type == OCN_HALF) hipLaunchKernelGGL((KERNEL<D, RT, f16>), dim3(grid), dim3(kBlock), 0, stream, a);             \
+    else hipLaunchKernelGGL((KERNEL<D, RT, float>), dim3(grid), dim3(kBlock), 0, stream, a);                                     \
   } while (0)
   constexpr int kMany = D == 256 ? 1 : 2;      // row tiles whose sums and queries fit a wavefront's registers, two wavefronts to a SIMD
   if (!l.share) OCN_ATTENTION(attention_many_kernel, kMany);
