@@ -1123,8 +1123,7 @@ int ocn_cache_attention(const ocn_tensor *q, const ocn_tensor *cache, const ocn_
     if (visible->size[d] != q->size[d] && visible->size[d] != 1) return OCN_ERR_SHAPE;
   const float scale2 = (float)(scale * 1.4426950408889634074);      // (of exponents of two)
   if (!std::isfinite(scale2) || window < 0) return OCN_ERR_DOMAIN;
-  const HeadOperand ops[6] = {{q, false, nullptr, nullptr}, {cache, false, nullptr, nullptr}, {table, false, nullptr, nullptr},
-                              {visible, false, nullptr, nullptr}, {out, true, q, nullptr}, {log_sum, true, nullptr, nullptr}};
+  const HeadOperand ops[6] = {{q, false}, {cache, false}, {table, false}, {visible, false}, {out, true, 0}, {log_sum, true}};
   if ((rc = check_operands(ops, 6)) != OCN_OK) return rc;
   AttentionArgs a;
   std::memset(&a, 0, sizeof a);

@@ -110,7 +110,7 @@ int check_operands(const HeadOperand *o, int n) {
     for (int j = 0; o[i].t && o[i].output && j < n; ++j) {
       const ocn_tensor *in = o[j].t;
       if (j == i || !in || (o[j].output && j > i)) continue;
-      if (!o[j].output && (in == o[i].in_place || in == o[i].in_place_b) && identical_views(in, o[i].t)) continue;
+      if (!o[j].output && (j == o[i].in_place || j == o[i].in_place_b) && identical_views(in, o[i].t)) continue;
       if (share_bytes(in, o[i].t)) return OCN_ERR_ALIAS;
     }
   return OCN_OK;

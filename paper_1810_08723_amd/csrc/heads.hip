@@ -735,13 +735,14 @@ int run_rows(bool norm, const ocn_tensor *const *x, const ocn_tensor *const *w, 
   }
   if ((rc = check_rotation(r, channels_of(x[0]), x[0]->device)) != OCN_OK) return rc;
   for (int i = 0; i < jobs; ++i) {
-    ops[n++] = {x[i], false, nullptr, nullptr};
-    ops[n++] = {out[i], true, x[i], nullptr};
-    if (norm && w[i]) ops[n++] = {w[i], false, nullptr, nullptr};
+    ops[n++] = {x[i], false};
+    ops[n] = {out[i], true, n - 1};
+    ++n;
+    if (norm && w[i]) ops[n++] = {w[i], false};
   }
   if (r) {
-    ops[n++] = {r->positions, false, nullptr, nullptr};
-    ops[n++] = {r->frequencies, false, nullptr, nullptr};
+    ops[n++] = {r->positions, false};
+    ops[n++] = {r->frequencies, false};
   }
   if ((rc = check_operands(ops, n)) != OCN_OK) return rc;
   HeadArgs a;
@@ -802,7 +803,7 @@ int run_cache(const ocn_tensor *k, const ocn_tensor *v, const ocn_rotation *r, c
     if (!first) first = x[i];
     if (x[i]->dtype != first->dtype) return OCN_ERR_DTYPE;
     if (!same_shape(x[i], first)) return OCN_ERR_SHAPE;
-    ops[n++] = {x[i], out, nullptr, nullptr};
+    ops[n++] = {x[i], out};
   }
   if (!first) return OCN_ERR_NULLPTR;
   const int64_t d = channels_of(first);
@@ -812,11 +813,11 @@ int run_cache(const ocn_tensor *k, const ocn_tensor *v, const ocn_rotation *r, c
   if (slots->ndim != first->ndim - 2) return OCN_ERR_SHAPE;
   for (int i = 0; i < slots->ndim; ++i)
     if (slots->size[i] != first->size[i]) return OCN_ERR_SHAPE;
-  ops[n++] = {slots, false, nullptr, nullptr};
-  ops[n++] = {cache, !out, nullptr, nullptr};
+  ops[n++] = {slots, false};
+  ops[n++] = {cache, !out};
   if (r) {
-    ops[n++] = {r->positions, false, nullptr, nullptr};
-    ops[n++] = {r->frequencies, false, nullptr, nullptr};
+    ops[n++] = {r->positions, false};
+    ops[n++] = {r->frequencies, false};
   }
   if ((rc = check_operands(ops, n)) != OCN_OK) return rc;
   HeadArgs a;
@@ -911,15 +912,16 @@ int ocn_norm_rotary_grad(const ocn_tensor *q_gout, const ocn_tensor *q, const oc
   }
   if ((rc = check_rotation(rotation, channels_of(x[0]), x[0]->device)) != OCN_OK) return rc;
   for (int i = 0; i < jobs; ++i) {
-    ops[n++] = {x[i], false, nullptr, nullptr};
-    ops[n++] = {g[i], false, nullptr, nullptr};
-    ops[n++] = {out[i], true, x[i], g[i]};
-    if (w[i]) ops[n++] = {w[i], false, nullptr, nullptr};
-    if (gw[i]) ops[n++] = {gw[i], true, nullptr, nullptr};
+    ops[n++] = {x[i], false};
+    ops[n++] = {g[i], false};
+    ops[n] = {out[i], true, n - 2, n - 1};
+    ++n;
+    if (w[i]) ops[n++] = {w[i], false};
+    if (gw[i]) ops[n++] = {gw[i], true};
   }
   if (rotation) {
-    ops[n++] = {rotation->positions, false, nullptr, nullptr};
-    ops[n++] = {rotation->frequencies, false, nullptr, nullptr};
+    ops[n++] = {rotation->positions, false};
+    ops[n++] = {rotation->frequencies, false};
   }
   if ((rc = check_operands(ops, n)) != OCN_OK) return rc;
   HeadArgs a;

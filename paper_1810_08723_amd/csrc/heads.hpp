@@ -13,12 +13,11 @@ namespace ocn {
 
 constexpr int kMaxLead = OCN_MAX_DIMS - 2;   // dimensions before heads and channels
 
-// An operand of a call as its checks see it: at most eight in one call.
+// An operand of a call as its checks see it (t null: none).
 struct HeadOperand {
   const ocn_tensor *t;
   bool output;
-  const ocn_tensor *in_place;   // inputs that an output may be the identical view of
-  const ocn_tensor *in_place_b;
+  int in_place = -1, in_place_b = -1;   // places among the operands of the inputs that an output may be the identical view of (one descriptor may be at several)
 };
 
 // The tokens: leading dimensions, merged where every operand's strides allow it, fastest last; with strides for each operand.
