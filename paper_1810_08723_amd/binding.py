@@ -452,7 +452,7 @@ class Rotation:
 def rotary_frequencies(rotary_dim: int, base: float = 10000.0, stretch: str = "none", factor: float = 1.0, original: float = 0.0,
                        low: float = 1.0, high: float = 4.0) -> Tuple[list, float]:
     """Frequencies (radians per position, rotary_dim/2 of them) and the magnitude of a rotation, on the host: base^(-2i/rotary_dim),
-    changed for long contexts by one of STRETCHES (see ocn.h)."""
+    changed for long contexts by one of STRETCHES (see ocn.h; `low` and `high` serve "turns" and "index", whose models differ in them)."""
     f, m = (C.c_double * max(rotary_dim // 2, 1))(), C.c_double()
     _check(lib().ocn_rotary_frequencies(rotary_dim, base, STRETCHES.index(stretch), factor, original, low, high, f, C.byref(m)))
     return list(f), m.value

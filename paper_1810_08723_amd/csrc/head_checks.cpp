@@ -199,16 +199,16 @@ extern "C" int ocn_rotary_frequencies(int32_t rotary_dim, double base, int stret
     base *= std::pow(factor, rotary_dim / (rotary_dim - 2.0));
   }
   const double two_pi = 6.283185307179586476925286766559;
-  // the index at which a frequency makes `turns` turns within the original length
-  const double per_log = rotary_dim / (2.0 * std::log(base));
-  const double first = std::max(0.0, std::floor(per_log * std::log(original / (mixed ? high * two_pi : 1.0))));
-  const double last = std::min(rotary_dim / 2 - 1.0, std::ceil(per_log * std::log(original / (mixed ? low * two_pi : 1.0))));
+  // The index, as a real number, at which a frequency makes so many turns within the original length; rounded outwards (and apart, should
+  // their logarithms be one number).  Either may lie the frequencies that there are: then the mixture begins or ends there.
+  const auto index_of = [&](double turns) { return rotary_dim * (std::log(original) - std::log(turns) - std::log(two_pi)) / (2.0 * std::log(base)); };
+  const double first = mixed ? std::floor(index_of(high)) : 0.0, last = mixed ? std::max(first + 1.0, std::ceil(index_of(low))) : 1.0;
   for (int i = 0; i < rotary_dim / 2; ++i) {
     const double f = std::pow(base, -2.0 * i / rotary_dim);
     double keep = 1.0;    // the share of the frequency as it is, the rest divided by factor
     if (stretch == OCN_STRETCH_LINEAR) keep = 0.0;
     if (stretch == OCN_STRETCH_TURNS) keep = std::min(1.0, std::max(0.0, (original * f / two_pi - low) / (high - low)));
-    if (stretch == OCN_STRETCH_INDEX) keep = 1.0 - std::min(1.0, std::max(0.0, (i - first) / std::max(last - first, 0.001)));
+    if (stretch == OCN_STRETCH_INDEX) keep = 1.0 - std::min(1.0, std::max(0.0, (i - first) / (last - first)));
     frequencies[i] = keep == 1.0 ? f : f / factor * (1.0 - keep) + f * keep;
   }
   *magnitude = stretch == OCN_STRETCH_INDEX && factor > 1.0 ? 0.1 * std::log(factor) + 1.0 : 1.0;
