@@ -1,9 +1,8 @@
 """Which operands of the operators over heads may share bytes: told by their place in a call, not by the descriptor that names them (no GPU)."""
 import paper_1810_08723_amd as ocn
-from test_host_heads import T, code, x
+from test_host_heads import FakeSpace, T, code, rot, x
 
 W = T("float", (64,), base=4)
-FAR = T("float", (64,), base=4, device=1)      # (a call that gets past the sharing of bytes is refused for this)
 
 
 def test_one_descriptor_for_queries_and_keys():
@@ -21,9 +20,11 @@ def test_one_descriptor_for_queries_and_keys():
 
 
 def test_what_may_be_in_place_still_is():
+    """Such calls are refused later: for positions that fit no call, or for too small a workspace"""
     q, k, g, kg = x(), x(base=3), x(base=5), x(base=6)
-    assert code(ocn.norm_rotary, q, W, q, k, FAR, k) == "DEVICE"
-    assert code(ocn.norm_rotary, q, W, x(base=7), q, FAR, k) == "DEVICE"        # read twice, written elsewhere
-    f = ocn.norm_rotary_grad
-    assert code(f, g, q, W, g, None, kg, k, FAR, k) == "DEVICE"
-    assert code(f, q, q, W, q, None, kg, k, FAR, kg) == "DEVICE"                # (the gradient of half the sum of squares)
+    off = rot(2, pos=T("int32", (1000,), base=8))
+    assert code(ocn.norm_rotary, q, W, q, k, W, k, rotation=off) == "SHAPE"
+    assert code(ocn.norm_rotary, q, W, x(base=7), q, W, k, rotation=off) == "SHAPE"        # read twice, written elsewhere
+    f, gw, small = ocn.norm_rotary_grad, T("float", (64,), base=9), FakeSpace(0x7000000000, 16)
+    assert code(f, g, q, W, g, gw, kg, k, W, k, workspace=small) == "WORKSPACE"
+    assert code(f, q, q, W, q, gw, kg, k, W, kg, workspace=small) == "WORKSPACE"           # (the gradient of half the sum of squares)
