@@ -39,11 +39,14 @@ int check_operand(const ocn_tensor *t, int types) {
   return OCN_OK;
 }
 
-// [lo, hi) of the bytes that dimensions from `first` on span, relative to the element at their start
-static void span_of(const ocn_tensor *t, int first, int64_t *lo, int64_t *hi) {
+// sets of dimensions, a bit each
+constexpr uint32_t kAllDims = ~0u;
+
+// [lo, hi) of the bytes that dimensions `dims` span, relative to the element at their start
+static void span_of(const ocn_tensor *t, uint32_t dims, int64_t *lo, int64_t *hi) {
   int64_t l = 0, h = 0;
-  for (int d = first; d < t->ndim; ++d) {
-    if (t->size[d] <= 1) continue;
+  for (int d = 0; d < t->ndim; ++d) {
+    if (t->size[d] <= 1 || !(dims >> d & 1)) continue;
     const int64_t s = (t->size[d] - 1) * t->stride[d];
     if (s < 0) l += s; else h += s;
   }
@@ -57,12 +60,12 @@ static bool empty_tensor(const ocn_tensor *t) {
   return false;
 }
 
-// whether dimensions [0, n) of t, taken by stride, each step over everything that lies below them: `extent` bytes at first
-static bool steps_over(const ocn_tensor *t, int n, int64_t extent) {
+// whether dimensions `dims` of t, taken by stride, each step over everything that lies below them: `extent` bytes at first
+static bool steps_over(const ocn_tensor *t, uint32_t dims, int64_t extent) {
   int64_t st[kMaxDims], sz[kMaxDims];
   int m = 0;
-  for (int d = 0; d < n; ++d)
-    if (t->size[d] > 1) { st[m] = std::llabs(t->stride[d]); sz[m++] = t->size[d]; }
+  for (int d = 0; d < t->ndim; ++d)
+    if (t->size[d] > 1 && (dims >> d & 1)) { st[m] = std::llabs(t->stride[d]); sz[m++] = t->size[d]; }
   for (int i = 1; i < m; ++i)
     for (int j = i; j > 0 && st[j] < st[j - 1]; --j) { std::swap(st[j], st[j - 1]); std::swap(sz[j], sz[j - 1]); }
   for (int i = 0; i < m; ++i) {
@@ -83,18 +86,26 @@ bool share_bytes(const ocn_tensor *a, const ocn_tensor *b) {
   if (empty_tensor(a) || empty_tensor(b)) return false;
   const int64_t pa = (intptr_t)a->base + a->offset, pb = (intptr_t)b->base + b->offset;
   int64_t la, ha, lb, hb;
-  span_of(a, 0, &la, &ha);
-  span_of(b, 0, &lb, &hb);
+  span_of(a, kAllDims, &la, &ha);
+  span_of(b, kAllDims, &lb, &hb);
   if (pa + ha <= pb + lb || pb + hb <= pa + la) return false;
-  // Heads side by side in rows of one buffer: the same steps from row to row, each over both views' heads, and heads that do not meet
-  if (a->ndim != b->ndim || a->ndim < 3) return true;
-  const int lead = a->ndim - 2;
-  for (int d = 0; d < lead; ++d)
-    if (a->size[d] != b->size[d] || (a->size[d] > 1 && a->stride[d] != b->stride[d])) return true;
-  span_of(a, lead, &la, &ha);
-  span_of(b, lead, &lb, &hb);
-  if (!(pa + ha <= pb + lb || pb + hb <= pa + la)) return true;
-  return !steps_over(a, lead, std::max(pa + ha, pb + hb) - std::min(pa + la, pb + lb));
+  // Heads side by side in one buffer, whatever the order of its dimensions.  Where some dimensions, those of the longest strides, take both views through the
+  // same steps, each over all that either view has below them, what lies below them need only not meet.
+  if (a->ndim != b->ndim) return true;
+  uint32_t outer = 0;
+  for (;;) {
+    int next = -1;
+    for (int d = 0; d < a->ndim; ++d)
+      if (!(outer >> d & 1) && a->size[d] > 1 && a->size[d] == b->size[d] && a->stride[d] == b->stride[d] &&
+          (next < 0 || std::llabs(a->stride[d]) > std::llabs(a->stride[next])))
+        next = d;
+    if (next < 0) return true;
+    outer |= 1u << next;
+    span_of(a, ~outer, &la, &ha);
+    span_of(b, ~outer, &lb, &hb);
+    const bool apart = pa + ha <= pb + lb || pb + hb <= pa + la;
+    if (apart && steps_over(a, outer, std::max(pa + ha, pb + hb) - std::min(pa + la, pb + lb))) return false;
+  }
 }
 
 int check_operands(const HeadOperand *o, int n) {
@@ -104,7 +115,7 @@ int check_operands(const HeadOperand *o, int n) {
       if (o[j].t && o[j].t->device != o[i].t->device) return OCN_ERR_DEVICE;
   }
   for (int i = 0; i < n; ++i)
-    if (o[i].t && o[i].output && !empty_tensor(o[i].t) && !steps_over(o[i].t, o[i].t->ndim, head_type_size(o[i].t->dtype)))
+    if (o[i].t && o[i].output && !empty_tensor(o[i].t) && !steps_over(o[i].t, kAllDims, head_type_size(o[i].t->dtype)))
       return OCN_ERR_OVERLAP_OUT;
   for (int i = 0; i < n; ++i)
     for (int j = 0; o[i].t && o[i].output && j < n; ++j) {
