@@ -41,8 +41,9 @@ constexpr int64_t kAtOnce = 512;               // workgroups that keep all CUs a
 constexpr int64_t kWorkgroups = 1536;          // fewer units are, into so many: sequences of different lengths even out (256 units of 1 to 8190 tokens: 47 us, 52 in 768;
 constexpr int64_t kWorkgroupsWide = 768;       // of 256 channels, which two wavefronts of a SIMD take: 128 units of 100 to 8000 tokens 49.6 us, 52.2 in 1536)
 constexpr int64_t kManyWorkgroups = 2048;      // where a workgroup's wavefronts have rows of their own
-constexpr int64_t kManyLeast = 16;             // tiles of a split, at least, where units leave CUs without work (352 units of 256 tiles: 457 us in two splits, 365 in five)
-constexpr int64_t kManyLeastFull = 64;         // and where they do not (512 units of 256 tiles: 518 and 426 us in four, 512 of 47 tiles: 96 and 156 in three)
+constexpr int64_t kManyLeast = 16;             // tiles of a table that a split has room for, at least, where units leave CUs without work (352 units of 256 tiles: 457 us in two
+                                               // splits, 365 in five); of a sequence shorter than its table it has kLeastTiles (32 units of 22 tiles: 30 us in three, 46 in two)
+constexpr int64_t kManyLeastFull = 64;         // of either, where they do not (512 units of 47 tiles in a table of 256: 163 us in one split, 173 in four)
 constexpr uint32_t kJoinRows = 1024;           // from so many on a wavefront joins a row, a workgroup below
 
 // ---------------------------------------------------------------------------------------
@@ -771,7 +772,7 @@ __global__ __launch_bounds__(kBlock, (kWavesOfSimd<D, RT, T>)) void attention_ke
 
 // Many rows: each of a workgroup's wavefronts has rows of its own, and all go over the same tiles.  Products bound this, and what is done to the codes before
 // them: each wavefront makes a quarter of a tile's operands, for all four, in LDS; two tiles have room there, so that one is made while the other is used.  1024 queries of 32 heads over 3333 and 8192 tokens:
-// 495 us, 356 TFLOP/s of the 1390 that a large product reaches: a wavefront has nothing else to do between its two products, and registers allow two to a SIMD.
+// 485 us, 364 TFLOP/s of the 1390 that a large product reaches: a wavefront has nothing else to do between its two products, and registers allow two to a SIMD.
 template <int D, int RT, class T>
 __global__ __launch_bounds__(kBlock, 2) void attention_many_kernel(const AttentionArgs a) {
   typedef Shape<D> S;
@@ -1000,6 +1001,7 @@ struct Launch {
   int row_tiles;        // of a wavefront
   bool share;           // whether a workgroup's wavefronts have the same rows
   int64_t unit_rows, blocks, units, splits, items;
+  int64_t least;        // tiles of a split, at least: of a sequence shorter than its table too
 };
 
 Launch launch_of(int64_t batch, int64_t queries, int64_t heads, int64_t kv, int64_t channels, int64_t capacity) {
@@ -1013,9 +1015,11 @@ Launch launch_of(int64_t batch, int64_t queries, int64_t heads, int64_t kv, int6
   const int64_t tiles = (capacity + kTile - 1) / kTile, most = tiles <= kAloneTiles ? 1 : tiles / kLeastTiles;
   const int64_t wanted = l.units >= kAtOnce ? 1 : (channels == 256 ? kWorkgroupsWide : kWorkgroups) / std::max<int64_t>(l.units, 1);
   l.splits = std::max<int64_t>(1, std::min<int64_t>({most, kMaxSplits, wanted}));
+  l.least = kLeastTiles;
   if (!l.share) {
-    const int64_t least = l.units < kAtOnce ? kManyLeast : kManyLeastFull;
-    l.splits = std::max<int64_t>(1, std::min<int64_t>({most, tiles / least, kMaxSplits, kManyWorkgroups / std::max<int64_t>(l.units, 1)}));
+    const bool full = l.units >= kAtOnce;
+    if (full) l.least = kManyLeastFull;
+    l.splits = std::max<int64_t>(1, std::min<int64_t>({most, tiles / (full ? kManyLeastFull : kManyLeast), kMaxSplits, kManyWorkgroups / std::max<int64_t>(l.units, 1)}));
   }
   l.items = l.units * l.splits;
   return l;
@@ -1160,7 +1164,7 @@ int ocn_cache_attention(const ocn_tensor *q, const ocn_tensor *cache, const ocn_
   a.queries = (int32_t)q->size[1];
   a.per_kv = (int32_t)(q->size[2] / kv);
   a.capacity = a.pages > 0 ? (int32_t)capacity : 0;
-  a.least = (int32_t)kLeastTiles;
+  a.least = (int32_t)l.least;
   a.whole_q = whole_rows(q);
   a.whole_out = whole_rows(out);
   a.page = (int32_t)page;
