@@ -60,10 +60,11 @@ constexpr uint32_t kJoinRows = 1024;           // from so many on a wavefront jo
 // scale), so that K and V lose nothing.  V's pairs are two tokens of a channel: nibbles of two rows are put side by side (one shift and one bit
 // select for eight codes) before they are converted.  Q is exact where its type has no more than 11 bits: a row is scaled by a power of two so that its
 // largest channel is near 2^13; for float tensors it has two parts.  A weight is the sum of two halves, and a second product adds what the first
-// leaves (to half alone, 2^-11, bfloat16 results differed from those of single precision in one channel of twenty by a step; 433 us instead of 495 for the prompt below).
+// leaves (to half alone, 2^-11, bfloat16 results differed from those of single precision in one channel of twenty by a step; 62 us less of 495 for the prompt below).
 //
-// The maximum of a row that its weights are relative to is raised, and sums rescaled, only where a score is 2^4 above it; weights are times 2^11, so
-// that they stay below 2^15.  The sum of the weights is one more product, with ones.
+// The maximum of a row that its weights are relative to is raised, and sums rescaled, only where a weight is 2^4 above it; weights are times 2^11, so
+// that they stay below 2^15.  The difference of scores is formed before it is scaled: the other way round one subtraction is saved (486 for 493 us of the prompt below), but a score times the scale is
+// off by half a step of itself, and from 2^23 on weights were infinite.  The sum of the weights is one more product, with ones.
 //
 // Two halves hold a weight to 2^-22 of itself, or, where the second is among the smallest that a half holds, to 2^-36 of the largest. Left at that, a channel that is
 // zero in the tokens with large weights would lose what the others give it.  A tile with weights below Floor::kLeast
@@ -270,9 +271,7 @@ template <int D, int RT> struct Sums {
   f32x4 out[RT][Shape<D>::kTiles];   // out^T
   f32x4 total[RT];                   // of the weights (all four the same)
   f32x4 bad[RT];                     // how many tokens with a NaN as V's scale a row sees, in tiles that are not seen whole
-  float shift[RT];                   // a weight is 2^(score * scale + shift): kWeightBits less what weights are relative to
-  float raise[RT];                   // a score above this raises that; minus infinity before the first
-  __device__ __forceinline__ float top(int rt) const { return raise[rt] == -__builtin_inff() ? -__builtin_inff() : kWeightBits - shift[rt]; }
+  float best[RT];                    // a weight is 2^((score - best) * scale + kWeightBits); minus infinity before the first
 };
 
 template <int D, int RT, class T> struct Rows {
@@ -397,24 +396,24 @@ __device__ __forceinline__ void one_tile(Sums<D, RT> &s, const Rows<D, RT, T> &r
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const float most = largest(score[rt]);
-    if (__builtin_amdgcn_ballot_w64(most > s.raise[rt])) {
+    if (__builtin_amdgcn_ballot_w64((most - s.best[rt]) * rows.scale[rt] > kRaise)) {
       // (the four lanes of a row meet here alone: most tiles do not come here)
-      const float before = s.top(rt), now = fmaxf(before, row_max(most) * rows.scale[rt]);
-      const float keep = now == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(before - now);
-      s.shift[rt] = now == -__builtin_inff() ? kWeightBits : kWeightBits - now;
-      s.raise[rt] = (now + kRaise) / rows.scale[rt];
+      const float before = s.best[rt], now = fmaxf(before, row_max(most));
+      const float keep = now == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f((before - now) * rows.scale[rt]);
+      s.best[rt] = now;
 #pragma unroll
       for (int i = 0; i < S::kTiles; ++i) s.out[rt][i] *= keep;
       s.total[rt] *= keep;
     }
-    const float shift = s.shift[rt];
+    // (the difference first: a score times the scale, less its largest, is off by as much as the score's steps, and past 2^23 that is more than a half's range)
+    const float best = s.best[rt];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) weight[rt][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(score[rt][i / 4][i % 4], rows.scale[rt], shift));
+    for (int i = 0; i < 8; ++i) weight[rt][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(score[rt][i / 4][i % 4] - best, rows.scale[rt], kWeightBits));
     if (!whole) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) weight[rt][i] = sees[rt] >> i & 1 ? weight[rt][i] : 0.0f;
     }
-    if (__builtin_amdgcn_ballot_w64(__builtin_fmaf(least[rt], rows.scale[rt], shift) < F::kBits)) apart = true;
+    if (__builtin_amdgcn_ballot_w64(__builtin_fmaf(least[rt] - best, rows.scale[rt], kWeightBits) < F::kBits)) apart = true;
   }
   source.start_v();
   if (apart) {
@@ -614,8 +613,7 @@ __device__ __forceinline__ void start_rows(const AttentionArgs &a, Rows<D, RT, T
 #pragma unroll
     for (int i = 0; i < S::kTiles; ++i) sums.out[rt][i] = f32x4{0, 0, 0, 0};
     sums.total[rt] = sums.bad[rt] = f32x4{0, 0, 0, 0};
-    sums.shift[rt] = kWeightBits;
-    sums.raise[rt] = -__builtin_inff();
+    sums.best[rt] = -__builtin_inff();
   }
 }
 
@@ -718,7 +716,7 @@ __global__ __launch_bounds__(kBlock, (kWavesOfSimd<D, RT, T>)) void attention_ke
   if (g == 0) {
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      tops[wave][rt][n] = sums.top(rt);
+      tops[wave][rt][n] = sums.best[rt] * rows.scale[rt];
       totals[wave][rt][n] = sums.total[rt][0];
     }
   }
@@ -728,7 +726,7 @@ __global__ __launch_bounds__(kBlock, (kWavesOfSimd<D, RT, T>)) void attention_ke
     float top = -__builtin_inff();
 #pragma unroll
     for (int w = 0; w < W; ++w) top = fmaxf(top, tops[w][rt][n]);
-    const float keep = top == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(sums.top(rt) - top);
+    const float keep = top == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(sums.best[rt] * rows.scale[rt] - top);
 #pragma unroll
     for (int at = 0; at < S::kTiles; at += kPart) {
       if (rt + at > 0) __syncthreads();
@@ -772,7 +770,7 @@ __global__ __launch_bounds__(kBlock, (kWavesOfSimd<D, RT, T>)) void attention_ke
 
 // Many rows: each of a workgroup's wavefronts has rows of its own, and all go over the same tiles.  Products bound this, and what is done to the codes before
 // them: each wavefront makes a quarter of a tile's operands, for all four, in LDS; two tiles have room there, so that one is made while the other is used.  1024 queries of 32 heads over 3333 and 8192 tokens:
-// 485 us, 364 TFLOP/s of the 1390 that a large product reaches: a wavefront has nothing else to do between its two products, and registers allow two to a SIMD.
+// 493 us, 358 TFLOP/s of the 1390 that a large product reaches: a wavefront has nothing else to do between its two products, and registers allow two to a SIMD.
 template <int D, int RT, class T>
 __global__ __launch_bounds__(kBlock, 2) void attention_many_kernel(const AttentionArgs a) {
   typedef Shape<D> S;
@@ -918,8 +916,8 @@ __global__ __launch_bounds__(kBlock, 2) void attention_many_kernel(const Attenti
       }
     }
     if (g == 0) {
-      if (alone && a.log_sum) *(float *)(a.log_sum + b * a.lb + t * a.lt + h * a.lh) = log_of(sums.top(rt), total);
-      if (!alone) *(float2 *)(a.part_sums + at_row * 2) = float2{sums.top(rt), total};
+      if (alone && a.log_sum) *(float *)(a.log_sum + b * a.lb + t * a.lt + h * a.lh) = log_of(sums.best[rt] * rows.scale[rt], total);
+      if (!alone) *(float2 *)(a.part_sums + at_row * 2) = float2{sums.best[rt] * rows.scale[rt], total};
     }
   }
 }
