@@ -407,7 +407,8 @@ int ocn_cache_read(const ocn_tensor *cache, const ocn_tensor *slots, const ocn_t
  * reads head h / (heads / cache heads).  A query that sees nothing gets zeros.  log_sum (or NULL): OCN_FLOAT [batch, queries, heads], the natural
  * logarithm of sum_j exp(scale * q . k_j), -inf where nothing is seen.  Scores, sums and the softmax are
  * held in single precision (a scale past its range is OCN_ERR_DOMAIN); for the product with v a weight p_j is the sum of two halves, which are off by at most
- * 2^-21 of it or 2^-36 of the row's largest weight, whichever is more, and for half and bfloat16 by at most 2^-11 (float: 2^-21) of the weight itself.  workspace: DEVICE scratch of ocn_cache_attention_workspace_bytes(...) bytes (a function
+ * 2^-21 of it or 2^-36 of the row's largest weight, whichever is more, and for half and bfloat16 by at most 2^-11 (float: 2^-21) of the weight itself;
+ * weights below 2^-122 of the row's largest may be taken as zero, as exponentials past the range of single precision are.  workspace: DEVICE scratch of ocn_cache_attention_workspace_bytes(...) bytes (a function
  * of the shapes alone; 0 where none is needed), 256-byte aligned.  The same bits every time. */
 size_t ocn_cache_attention_workspace_bytes(const ocn_tensor *q, const ocn_tensor *cache, const ocn_tensor *table);
 int ocn_cache_attention(const ocn_tensor *q, const ocn_tensor *cache, const ocn_tensor *table, const ocn_tensor *visible,
