@@ -68,8 +68,8 @@ constexpr uint32_t kJoinRows = 1024;           // from so many on a wavefront jo
 //
 // Two halves hold a weight to 2^-22 of itself, or, where the second is among the smallest that a half holds, to 2^-36 of the largest. Left at that, a channel that is
 // zero in the tokens with large weights would lose what the others give it.  A tile with weights below Floor::kLeast
-// takes them out and multiplies them apart, times a power of two, in as many steps as they need: down to 2^-126 no weight is further off than 2^-11 of itself (2^-21
-// for float results).
+// takes them out and multiplies them apart, times a power of two, in as many steps as they need: down to 2^-122 of the largest no weight is further off than 2^-11 of
+// itself (2^-21 for float results).  Below, the factors that sums are rescaled by, 2^4 less at most, leave the range of single precision and are zero.
 // ---------------------------------------------------------------------------------------
 
 constexpr float kWeightBits = 11.0f, kRaise = 4.0f;
@@ -641,7 +641,7 @@ __device__ __forceinline__ Work work_of(const AttentionArgs &a, uint32_t item) {
   return w;
 }
 
-// Wavefronts of a SIMD: what registers allow without spilling (of 256 channels twenty spill; one wavefront instead takes 65.9 us for 57.8 of 128 units of 100 to 8000 tokens).
+// Wavefronts of a SIMD: what registers allow (of 256 channels five spill, which whole tiles do not touch; one wavefront instead takes 65.9 us for 57.5 of 128 units of 100 to 8000 tokens).
 // Three for 128 channels: 49.7 us for 54.7 of 256 units of 1 to 8190 tokens.
 template <int D, int RT, class T> constexpr int kWavesOfSimd = kQueryParts<T> == 1 && D == 128 && RT == 1 ? 3 : D * RT <= (kQueryParts<T> == 1 ? 256 : 128) ? 2 : 1;
 
@@ -866,7 +866,7 @@ __global__ __launch_bounds__(kBlock, 2) void attention_many_kernel(const Attenti
         for (int i = 0; i < 4; ++i) {
           const uint32_t two = share.v_scale[i / 2][i % 2];
           uint32_t word;
-          if constexpr (S::kTiles == 4) word = (wave & 1 ? twins[i].odd[0] : twins[i].even[0]) >> 8 * (wave >> 1);
+          if constexpr (S::kTiles == 4) word = select_bits(wave & 1 ? ~0u : 0u, twins[i].odd[0], twins[i].even[0]) >> 8 * (wave >> 1);      // (a choice between the two would put them into memory)
           else word = (c % 2 ? twins[i].odd[c / 2] : twins[i].even[c / 2]) >> 8 * wave;
           f.p[i] = two_codes<0>(word) * __builtin_bit_cast(f16x2, two);
         }
