@@ -322,7 +322,7 @@ int ocn_unary_mode(int op, int mode, const ocn_tensor *a, const ocn_tensor *out,
 #define OCN_MAX_CHANNELS 512
 
 /* A rotation by position: pair i < rotary_dim / 2 of a head's first rotary_dim channels turns by the angle
- *     positions[token] * frequencies[i]          (radians, formed and reduced in double precision)
+ *     positions[token] * frequencies[i]          (radians, formed and reduced in double precision; below 2^46 in magnitude)
  * and is multiplied by magnitude; the other channels stay.  positions broadcasts against the leading dimensions of
  * the tensor that is rotated (right-aligned, as in ocn_binary); frequencies: OCN_DOUBLE, [rotary_dim / 2]. */
 typedef enum {
@@ -391,7 +391,7 @@ size_t ocn_cache_block_bytes(int64_t page_tokens, int32_t channels);
 
 /* Appends keys and values, the keys rotated on the way (rotation may be NULL): k and v are [..., heads, channels], slots has their leading
  * dimensions and says where each token goes: page * P + place in the page.  A token whose slot is
- * negative or past the last page is left out.  Of tokens with one slot, which is kept is not defined. */
+ * negative or past the last page is left out.  What a slot holds that several tokens name is not defined. */
 int ocn_cache_append(const ocn_tensor *k, const ocn_tensor *v, const ocn_rotation *rotation, const ocn_tensor *slots,
                      const ocn_tensor *cache, void *stream);
 

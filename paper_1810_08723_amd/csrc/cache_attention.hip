@@ -34,16 +34,16 @@ struct AttentionArgs {
 };
 
 constexpr int64_t kLeastTiles = 8;             // of a split: two for each wavefront
-constexpr int64_t kAloneTiles = 20;            // up to so many a second launch costs more than splits gain (17 tiles: 9.6 us, 11.0 in splits)
+constexpr int64_t kAloneTiles = 20;            // up to so many a second launch costs more than splits gain (17 tiles: 10.2 us, 11.4 in splits)
 constexpr int64_t kMaxSplits = kWave;          // a lane each when they are joined
 constexpr int64_t kAtOnce = 512;               // workgroups that keep all CUs at work, two to each: so many units are not split where memory bounds them
-                                               // (512 of 4000 tokens: 62 us, 65 in three splits)
-constexpr int64_t kWorkgroups = 1536;          // fewer units are, into so many: sequences of different lengths even out (256 units of 1 to 8190 tokens: 47 us, 52 in 768;
-constexpr int64_t kWorkgroupsWide = 768;       // of 256 channels, which two wavefronts of a SIMD take: 128 units of 100 to 8000 tokens 49.6 us, 52.2 in 1536)
+                                               // (512 of 4000 tokens: 62 us, and in three splits)
+constexpr int64_t kWorkgroups = 1536;          // fewer units are, into so many: sequences of different lengths even out (256 units of 1 to 8190 tokens: 50 us, 58 in 768;
+constexpr int64_t kWorkgroupsWide = 768;       // of 256 channels, which two wavefronts of a SIMD take: 128 units of 100 to 8000 tokens 57.5 us, 58.5 in 1536)
 constexpr int64_t kManyWorkgroups = 2048;      // where a workgroup's wavefronts have rows of their own
-constexpr int64_t kManyLeast = 16;             // tiles of a table that a split has room for, at least, where units leave CUs without work (352 units of 256 tiles: 457 us in two
-                                               // splits, 365 in five); of a sequence shorter than its table it has kLeastTiles (32 units of 22 tiles: 30 us in three, 46 in two)
-constexpr int64_t kManyLeastFull = 64;         // of either, where they do not (512 units of 47 tiles in a table of 256: 163 us in one split, 173 in four)
+constexpr int64_t kManyLeast = 16;             // tiles of a table that a split has room for, at least, where units leave CUs without work (352 units of 256 tiles: 711 us in one
+                                               // split, 589 in two, 464 in five); of a sequence shorter than its table it has kLeastTiles (32 units of 22 tiles: 30 us in three, 46 in two)
+constexpr int64_t kManyLeastFull = 64;         // of either, where they do not (512 units of 47 tiles in a table of 256: 163 us in one split, 173 in four; of 256 tiles 723 and 648)
 constexpr uint32_t kJoinRows = 1024;           // from so many on a wavefront joins a row, a workgroup below
 
 // ---------------------------------------------------------------------------------------
@@ -81,7 +81,7 @@ template <class T> struct Floor {     // (float results keep 2^-21 of a small we
   static constexpr float kLeast = kQueryParts<T> == 1 ? 0x1p-14f : 0x1p-4f, kUp = kQueryParts<T> == 1 ? 0x1p28f : 0x1p18f, kDown = 1.0f / kUp;
 };
 constexpr int kTile = 32;            // tokens
-constexpr int kAhead = 1;             // tiles on their way (two: 67.99 for 66.03 us of two contexts of 100 k and 131 k tokens)
+constexpr int kAhead = 1;             // tiles on their way (two: 103 for 65 us of two contexts of 100 k and 131 k tokens, for want of registers)
 
 template <int D> struct Shape {
   static constexpr int kWords = D / 32;                   // of a token's codes in a lane; steps of the scores; groups
@@ -334,7 +334,7 @@ template <int D, int EARLY> struct FromLds {
   typedef Shape<D> S;
   const f16x8 *at;         // of this lane
   __device__ __forceinline__ f16x8 k(int x, int w) const { return at[(x * S::kWords + w) * kWave]; }
-  f16x8 first[EARLY];     // V's, read before the weights are formed (the compiler moves no read over their branches): 558 us without, 518 with six
+  f16x8 first[EARLY];     // V's, read before the weights are formed (the compiler moves no read over their branches): one before 693 us, six 646 (the prompt below, in one split)
   __device__ __forceinline__ f16x8 v(int t) const { return t < EARLY ? first[t] : at[(2 * S::kWords + t) * kWave]; }
   __device__ __forceinline__ f16x8 bad() const { return at[(2 * S::kWords + S::kTiles) * kWave]; }
   __device__ __forceinline__ void start_v() const {}

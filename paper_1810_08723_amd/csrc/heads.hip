@@ -58,7 +58,7 @@ struct HeadArgs {
   double magnitude;
   float sign;                          // -1: turned back
   float eps, over_d;
-  int32_t pos_wide, interleaved;
+  int32_t pos_wide;
   int32_t half, row;                   // pairs of a head; floats of a token in the table
   FastDiv half_div;
   int32_t d, lanes_log2;               // channels; lanes of a row
@@ -637,7 +637,6 @@ bool shape_of_launch(HeadArgs &a, const ocn_rotation *r, int64_t d, int jobs) {
   a.half_div = make_fastdiv((uint32_t)std::max(a.half, 1));
   if (r) {
     a.magnitude = r->magnitude;
-    a.interleaved = r->layout == OCN_ROTARY_INTERLEAVED;
     a.pos = (const char *)r->positions->base + r->positions->offset;
     a.pos_wide = r->positions->dtype == OCN_INT64;
     a.freq = (const char *)r->frequencies->base + r->frequencies->offset;
