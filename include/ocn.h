@@ -324,7 +324,10 @@ int ocn_unary_mode(int op, int mode, const ocn_tensor *a, const ocn_tensor *out,
 /* A rotation by position: pair i < rotary_dim / 2 of a head's first rotary_dim channels turns by the angle
  *     positions[token] * frequencies[i]          (radians, formed and reduced in double precision; below 2^46 in magnitude)
  * and is multiplied by magnitude; the other channels stay.  positions broadcasts against the leading dimensions of
- * the tensor that is rotated (right-aligned, as in ocn_binary); frequencies: OCN_DOUBLE, [rotary_dim / 2]. */
+ * the tensor that is rotated (right-aligned, as in ocn_binary); frequencies: OCN_DOUBLE, [rotary_dim / 2].
+ * With several axes (time, height and width of images and video) frequencies is [axes, rotary_dim / 2] and positions has the axes as its first
+ * dimension, before those that broadcast: the angle is the sum over the axes of positions[axis][token] * frequencies[axis][i]. */
+#define OCN_MAX_AXES 4
 typedef enum {
   OCN_ROTARY_HALF = 0,      /* pair i: channels i and i + rotary_dim / 2 */
   OCN_ROTARY_INTERLEAVED    /* pair i: channels 2 i and 2 i + 1          */
@@ -350,6 +353,13 @@ typedef struct {
 typedef enum { OCN_STRETCH_NONE = 0, OCN_STRETCH_LINEAR, OCN_STRETCH_BASE, OCN_STRETCH_TURNS, OCN_STRETCH_INDEX } ocn_stretch;
 int ocn_rotary_frequencies(int32_t rotary_dim, double base, int stretch, double factor, double original, double low, double high,
                            double *frequencies, double *magnitude);
+
+/* A table of frequencies for several axes, computed on the HOST, in which every pair belongs to one axis: pairs[a] of them to axis a, pairs 0 .. n - 1
+ * in all (n: their sum).  table: [axes][n], frequencies[i] (those of ocn_rotary_frequencies, say) for the axis of pair i, 0 for the others.
+ *   OCN_AXES_IN_ROW       the pairs of axis 0, then those of axis 1, ...
+ *   OCN_AXES_IN_TURN      one of each axis in turn, as long as it has any left */
+typedef enum { OCN_AXES_IN_ROW = 0, OCN_AXES_IN_TURN } ocn_axes_order;
+int ocn_rotary_axes(int32_t axes, const int32_t *pairs, int order, const double *frequencies, double *table);
 
 /* out = x rotated.  With OCN_ROTATE_BACK by the negative angles (times magnitude as before): the gradient with respect to x
  * for x = the gradient with respect to out. */
@@ -414,6 +424,54 @@ size_t ocn_cache_attention_workspace_bytes(const ocn_tensor *q, const ocn_tensor
 int ocn_cache_attention(const ocn_tensor *q, const ocn_tensor *cache, const ocn_tensor *table, const ocn_tensor *visible,
                         double scale, int64_t window, const ocn_tensor *out, const ocn_tensor *log_sum, void *workspace,
                         size_t workspace_bytes, void *stream);
+
+/*
+ * Attention of whole sequences over keys and values as they are: prompts, training, single tokens over a past that is not in four bits.
+ *     out_i = sum_j p_ij v_j,   p_i = softmax_j(scale * q_i . k_j),   over the keys j of the sequence that query i sees.
+ * Sequences are packed one behind the other: q and out are [tokens, heads, channels], k and v [key tokens, kv heads, channels], and sequence s has the queries
+ * q_starts[s] ... q_starts[s + 1] - 1 and the keys k_starts[s] ... k_starts[s + 1] - 1.  q_starts and k_starts: [sequences + 1], ascending (a start outside of its
+ * tensor is taken as the nearest end of it; where starts descend, what is written to the tokens of the tensor is not defined).  Tokens of no sequence keep
+ * what out holds.  With both NULL the sequences are a dimension of their own: q and out [batch, queries, heads, channels], k and v [batch, keys, kv heads, channels].
+ * heads is a multiple of kv heads: query head h reads head h / (heads / kv heads).  At most OCN_MAX_ATTENTION_CHANNELS channels.
+ * In a sequence of n queries and m keys a query sees all keys; with OCN_CAUSAL query i sees the keys j <= i + m - n (the last query sees the last key), and the
+ * last `window` of those where window is not 0 (without OCN_CAUSAL it has to be 0).  A query that sees nothing gets zeros.  What a query does not see, infinities
+ * and NaNs among it, does not reach its results.  log_sum (or NULL): OCN_FLOAT [tokens, heads] ([batch, queries, heads]), the natural logarithm of
+ * sum_j exp(scale * q_i . k_j), -inf where nothing is seen.  Scores, sums and the softmax are held in single precision (a scale past its range is
+ * OCN_ERR_DOMAIN); for half and bfloat16 a weight (relative to the largest of its row, so far) is rounded to that type for the product with v, half a step
+ * at most.  workspace: DEVICE scratch of ocn_attention_workspace_bytes(...) bytes (a function of the shapes alone; 0 where none is needed), 256-byte
+ * aligned.  The same bits every time. */
+#define OCN_CAUSAL 4u
+#define OCN_MAX_ATTENTION_CHANNELS 256
+size_t ocn_attention_workspace_bytes(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *q_starts);
+int ocn_attention(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *v, const ocn_tensor *q_starts, const ocn_tensor *k_starts, double scale,
+                  int64_t window, uint32_t flags, const ocn_tensor *out, const ocn_tensor *log_sum, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Its gradient: q_gin, k_gin and v_gin are the gradients with respect to q, k and v for gout, that with respect to out; out and log_sum are what
+ * ocn_attention gave for the same q, k, v and arguments.  With D_i = gout_i . out_i and s_ij = p_ij (gout_i . v_j - D_i)
+ *     v_gin_j = sum_i p_ij gout_i,    q_gin_i = scale * sum_j s_ij k_j,    k_gin_j = scale * sum_i s_ij q_i,
+ * over all query heads that read a head, for k and v; zeros for keys that no query sees.  For half and bfloat16 p_ij and s_ij are rounded to that type for these products.
+ * q_gin may be NULL, and k_gin and v_gin both; no output may share bytes with an input.  An infinity or a NaN in a sequence may reach all of that sequence's gradients, and those of
+ * no other.  workspace: DEVICE scratch of ocn_attention_grad_workspace_bytes(...) bytes, 256-byte aligned.  The same bits every time. */
+size_t ocn_attention_grad_workspace_bytes(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *q_starts);
+int ocn_attention_grad(const ocn_tensor *gout, const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *v, const ocn_tensor *out, const ocn_tensor *log_sum,
+                       const ocn_tensor *q_starts, const ocn_tensor *k_starts, double scale, int64_t window, uint32_t flags, const ocn_tensor *q_gin,
+                       const ocn_tensor *k_gin, const ocn_tensor *v_gin, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The layer norm over the last dimension, of at most OCN_MAX_WIDTH channels, of tensors of any strides with up to six dimensions before it (fewer than 2^31 rows):
+ *     out = (x - mean(x)) / sqrt(mean((x - mean(x))^2) + eps) * weight + bias.
+ * x and out share one of the types of heads; weight and bias: [channels], half, bfloat16 or float each, or NULL for ones and zeros.  Arithmetic, sharing of bytes
+ * and errors are as for the operators over heads; out may be the identical view of x. */
+#define OCN_MAX_WIDTH 16384
+int ocn_layer_norm(const ocn_tensor *x, const ocn_tensor *weight, const ocn_tensor *bias, const ocn_tensor *out, double eps, void *stream);
+
+/* Its gradient: gin, gweight and gbias are the gradients with respect to x, weight and bias for gout, that with respect to out (gin may be the identical view
+ * of gout or of x).  gweight and gbias: [channels], half, bfloat16 or float, overwritten (zeros where there are no rows), NULL where they are not wanted;
+ * gweight needs a weight.  The same bits every time.  workspace: DEVICE scratch of ocn_layer_norm_grad_workspace_bytes(x) bytes, 256-byte aligned; not needed
+ * where gweight and gbias are NULL. */
+size_t ocn_layer_norm_grad_workspace_bytes(const ocn_tensor *x);
+int ocn_layer_norm_grad(const ocn_tensor *gout, const ocn_tensor *x, const ocn_tensor *weight, const ocn_tensor *gin, const ocn_tensor *gweight,
+                        const ocn_tensor *gbias, double eps, void *workspace, size_t workspace_bytes, void *stream);
 
 /* Bytes of workspace ocn_reduce needs for these arguments (0 when it runs in one pass).
  * Returns 0 as well when the arguments are invalid; ocn_reduce then reports the error. */

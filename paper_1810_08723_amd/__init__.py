@@ -11,13 +11,17 @@ from .binding import (BINARY_OPS, DTYPES, REDUCE_OPS, STRICT_TYPES, UNARY_OPS, O
                       gather, index_offsets, mask_offsets, scatter,
                       plan_binary, plan_binary_reduce, plan_reduce, plan_unary, promote, reduce,
                       reduce_scratch, reduce_workspace_bytes, unary, unary_mode,
-                      Rotation, rotary, rotary_frequencies, norm_rotary, norm_rotary_grad, norm_rotary_grad_workspace_bytes,
-                      cache_append, cache_attention, cache_attention_workspace_bytes, cache_block_bytes, cache_read)
+                      Rotation, rotary, rotary_axes, rotary_frequencies, norm_rotary, norm_rotary_grad, norm_rotary_grad_workspace_bytes,
+                      cache_append, cache_attention, cache_attention_workspace_bytes, cache_block_bytes, cache_read,
+                      attention, attention_workspace_bytes, attention_grad, attention_grad_workspace_bytes,
+                      layer_norm, layer_norm_grad, layer_norm_grad_workspace_bytes)
 
 __all__ = ["BINARY_OPS", "DTYPES", "REDUCE_OPS", "STRICT_TYPES", "UNARY_OPS", "OcnError", "Tensor",
            "binary", "binary_reduce", "binary_reduce_workspace_bytes", "cast_copy", "domain_check", "dtype_size",
            "gather", "index_offsets", "mask_offsets", "scatter",
            "plan_binary", "plan_binary_reduce", "plan_reduce", "plan_unary", "promote", "reduce",
            "reduce_scratch", "reduce_workspace_bytes", "unary", "unary_mode",
-           "Rotation", "rotary", "rotary_frequencies", "norm_rotary", "norm_rotary_grad", "norm_rotary_grad_workspace_bytes",
-           "cache_append", "cache_attention", "cache_attention_workspace_bytes", "cache_block_bytes", "cache_read"]
+           "Rotation", "rotary", "rotary_axes", "rotary_frequencies", "norm_rotary", "norm_rotary_grad", "norm_rotary_grad_workspace_bytes",
+           "cache_append", "cache_attention", "cache_attention_workspace_bytes", "cache_block_bytes", "cache_read",
+           "attention", "attention_workspace_bytes", "attention_grad", "attention_grad_workspace_bytes",
+           "layer_norm", "layer_norm_grad", "layer_norm_grad_workspace_bytes"]

@@ -48,7 +48,9 @@ EXPORTS = ("ocn_unary", "ocn_binary", "ocn_cast_copy", "ocn_reduce", "ocn_reduce
            "ocn_unary_mode", "ocn_unary_mode_workspace_bytes", "ocn_set_max_launch_blocks",
            "ocn_rotary_frequencies", "ocn_rotary", "ocn_norm_rotary", "ocn_norm_rotary_grad",
            "ocn_norm_rotary_grad_workspace_bytes", "ocn_cache_block_bytes", "ocn_cache_append", "ocn_cache_read",
-           "ocn_cache_attention", "ocn_cache_attention_workspace_bytes")
+           "ocn_cache_attention", "ocn_cache_attention_workspace_bytes", "ocn_rotary_axes", "ocn_layer_norm", "ocn_layer_norm_grad",
+           "ocn_layer_norm_grad_workspace_bytes", "ocn_attention", "ocn_attention_workspace_bytes", "ocn_attention_grad",
+           "ocn_attention_grad_workspace_bytes")
 
 
 class OcnTensor(C.Structure):
@@ -151,6 +153,7 @@ def lib() -> C.CDLL:
         R, D, V, Z = C.POINTER(OcnRotation), C.c_double, C.c_void_p, C.c_size_t
         L.ocn_rotary_frequencies.argtypes = [C.c_int32, D, C.c_int, D, D, D, D, C.POINTER(D), C.POINTER(D)]
         L.ocn_rotary.argtypes = [T, R, T, C.c_uint32, V]
+        L.ocn_rotary_axes.argtypes = [C.c_int32, C.POINTER(C.c_int32), C.c_int, C.POINTER(D), C.POINTER(D)]
         L.ocn_norm_rotary.argtypes = [T, T, T, T, T, T, D, R, V]
         L.ocn_norm_rotary_grad.argtypes = [T] * 10 + [D, R, V, Z, V]
         L.ocn_norm_rotary_grad_workspace_bytes.argtypes = [T, T]
@@ -162,6 +165,15 @@ def lib() -> C.CDLL:
         L.ocn_cache_attention.argtypes = [T, T, T, T, D, C.c_int64, T, T, V, Z, V]
         L.ocn_cache_attention_workspace_bytes.argtypes = [T, T, T]
         L.ocn_cache_attention_workspace_bytes.restype = Z
+        L.ocn_layer_norm.argtypes = [T, T, T, T, D, V]
+        L.ocn_layer_norm_grad.argtypes = [T] * 6 + [D, V, Z, V]
+        L.ocn_layer_norm_grad_workspace_bytes.argtypes = [T]
+        L.ocn_layer_norm_grad_workspace_bytes.restype = Z
+        L.ocn_attention.argtypes = [T] * 5 + [D, C.c_int64, C.c_uint32, T, T, V, Z, V]
+        L.ocn_attention_grad.argtypes = [T] * 8 + [D, C.c_int64, C.c_uint32, T, T, T, V, Z, V]
+        for f in (L.ocn_attention_workspace_bytes, L.ocn_attention_grad_workspace_bytes):
+            f.argtypes = [T, T, T]
+            f.restype = Z
         for name, direct in _direct.items():
             direct.address = C.cast(getattr(L, "ocn_" + name), C.c_void_p).value
         _lib = L
@@ -307,7 +319,8 @@ def _function(name: str):
 
 for _name in ("ocn_unary", "ocn_binary", "ocn_cast_copy", "ocn_reduce", "ocn_binary_reduce", "ocn_reduce_scratch",
               "ocn_index_offsets", "ocn_mask_offsets", "ocn_gather", "ocn_scatter", "ocn_rotary", "ocn_norm_rotary",
-              "ocn_norm_rotary_grad", "ocn_cache_append", "ocn_cache_read", "ocn_cache_attention"):
+              "ocn_norm_rotary_grad", "ocn_cache_append", "ocn_cache_read", "ocn_cache_attention", "ocn_layer_norm", "ocn_layer_norm_grad",
+              "ocn_attention", "ocn_attention_grad"):
     globals()["_" + _name] = _function(_name)
 
 
@@ -431,14 +444,15 @@ def scatter(src: Tensor, offsets, lo: int, hi: int, out_inner: Tensor, stream=No
 
 
 ROTARY_LAYOUTS = ("half", "interleaved")
+AXES_ORDERS = ("row", "turn")
 STRETCHES = ("none", "linear", "base", "turns", "index")
 ROTATE_BACK = 2
 
 
 class Rotation:
     """A rotation by position, as the calls over heads take it: the first `rotary_dim` channels of every head, in pairs
-    (i, i + rotary_dim/2) (layout "half") or (2i, 2i + 1) ("interleaved"), by positions * frequencies.  It keeps its
-    tensors; a program makes it once for its buffers."""
+    (i, i + rotary_dim/2) (layout "half") or (2i, 2i + 1) ("interleaved"), by positions * frequencies.  Frequencies [axes, rotary_dim/2]
+    and positions [axes, ...] rotate by the sum over several axes.  It keeps its tensors; a program makes it once for its buffers."""
 
     def __init__(self, positions: Tensor, frequencies: Tensor, rotary_dim: int, layout: str = "half", magnitude: float = 1.0):
         struct = OcnRotation(C.pointer(positions.desc()), C.pointer(frequencies.desc()), rotary_dim, ROTARY_LAYOUTS.index(layout), magnitude)
@@ -456,6 +470,17 @@ def rotary_frequencies(rotary_dim: int, base: float = 10000.0, stretch: str = "n
     f, m = (C.c_double * max(rotary_dim // 2, 1))(), C.c_double()
     _check(lib().ocn_rotary_frequencies(rotary_dim, base, STRETCHES.index(stretch), factor, original, low, high, f, C.byref(m)))
     return list(f), m.value
+
+
+def rotary_axes(pairs: Sequence[int], frequencies: Sequence[float], order: str = "row") -> list:
+    """Frequencies [axes][pairs] of a rotation by positions on several axes, on the host: axis a has pairs[a] of the pairs, one axis behind the
+    other (order "row") or in turn ("turn"); frequencies[i] is pair i's, whichever axis it belongs to."""
+    n = sum(pairs)
+    if len(frequencies) != n:
+        raise ValueError(f"{len(frequencies)} frequencies for {n} pairs")
+    table = (C.c_double * max(len(pairs) * n, 1))()
+    _check(lib().ocn_rotary_axes(len(pairs), (C.c_int32 * max(len(pairs), 1))(*pairs), AXES_ORDERS.index(order), (C.c_double * max(n, 1))(*frequencies), table))
+    return [list(table[a * n:(a + 1) * n]) for a in range(len(pairs))]
 
 
 def _optional(t):
@@ -538,6 +563,81 @@ def cache_attention(q: Tensor, cache: Tensor, table: Tensor, visible: Tensor, ou
         ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel()
     rc = _ocn_cache_attention(q._ref or q._make_ref(), cache._ref or cache._make_ref(), table._ref or table._make_ref(),
                               visible._ref or visible._make_ref(), scale, window, out._ref or out._make_ref(), _optional(log_sum),
+                              ws_ptr, ws_bytes, _stream(stream))
+    if rc:
+        _check(rc)
+
+
+CAUSAL = 4
+
+
+def attention_workspace_bytes(q: Tensor, k: Tensor, q_starts: Optional[Tensor] = None) -> int:
+    return int(lib().ocn_attention_workspace_bytes(_optional(q), _optional(k), _optional(q_starts)))
+
+
+def attention(q: Tensor, k: Tensor, v: Tensor, out: Tensor, scale: float, q_starts: Optional[Tensor] = None, k_starts: Optional[Tensor] = None,
+              causal: bool = True, window: int = 0, log_sum: Optional[Tensor] = None, workspace=None, stream=None) -> None:
+    """Attention of packed sequences (q and out [tokens, heads, channels], k and v [key tokens, kv heads, channels], `q_starts` and `k_starts`
+    [sequences + 1]), or of [batch, tokens, heads, channels] without starts.  `causal`: the last query sees the last key, each one before it a key
+    less, of those the last `window` where it is not 0; `workspace` as for reduce()."""
+    ws_ptr, ws_bytes = None, 0
+    if workspace is None:
+        need = attention_workspace_bytes(q, k, q_starts)
+        if need:
+            workspace = _scratch(need, q.device, stream)
+    if workspace is not None:
+        ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel()
+    rc = _ocn_attention(_optional(q), _optional(k), _optional(v), _optional(q_starts), _optional(k_starts), scale, window, CAUSAL if causal else 0,
+                        _optional(out), _optional(log_sum), ws_ptr, ws_bytes, _stream(stream))
+    if rc:
+        _check(rc)
+
+
+def attention_grad_workspace_bytes(q: Tensor, k: Tensor, q_starts: Optional[Tensor] = None) -> int:
+    return int(lib().ocn_attention_grad_workspace_bytes(_optional(q), _optional(k), _optional(q_starts)))
+
+
+def attention_grad(gout: Tensor, q: Tensor, k: Tensor, v: Tensor, out: Tensor, log_sum: Tensor, q_gin: Optional[Tensor], k_gin: Optional[Tensor],
+                   v_gin: Optional[Tensor], scale: float, q_starts: Optional[Tensor] = None, k_starts: Optional[Tensor] = None, causal: bool = True,
+                   window: int = 0, workspace=None, stream=None) -> None:
+    """Gradients of attention with respect to q, k and v (q_gin may be None, and k_gin and v_gin both); out and log_sum as attention left them,
+    the other arguments as it took them."""
+    ws_ptr, ws_bytes = None, 0
+    if workspace is None:
+        need = attention_grad_workspace_bytes(q, k, q_starts)
+        if need:
+            workspace = _scratch(need, q.device, stream)
+    if workspace is not None:
+        ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel()
+    rc = _ocn_attention_grad(_optional(gout), _optional(q), _optional(k), _optional(v), _optional(out), _optional(log_sum), _optional(q_starts),
+                             _optional(k_starts), scale, window, CAUSAL if causal else 0, _optional(q_gin), _optional(k_gin), _optional(v_gin),
+                             ws_ptr, ws_bytes, _stream(stream))
+    if rc:
+        _check(rc)
+
+
+def layer_norm(x: Tensor, weight: Optional[Tensor], bias: Optional[Tensor], out: Tensor, eps: float = 1e-5, stream=None) -> None:
+    """out = (x - mean) / sqrt(variance + eps) * weight + bias over the last dimension."""
+    rc = _ocn_layer_norm(x._ref or x._make_ref(), _optional(weight), _optional(bias), out._ref or out._make_ref(), eps, _stream(stream))
+    if rc:
+        _check(rc)
+
+
+def layer_norm_grad_workspace_bytes(x: Tensor) -> int:
+    return int(lib().ocn_layer_norm_grad_workspace_bytes(_optional(x)))
+
+
+def layer_norm_grad(gout: Tensor, x: Tensor, weight: Optional[Tensor], gin: Tensor, gweight: Optional[Tensor] = None, gbias: Optional[Tensor] = None,
+                    eps: float = 1e-5, workspace=None, stream=None) -> None:
+    """Gradients of layer_norm with respect to x, weight and bias; `workspace` as for reduce()."""
+    ws_ptr, ws_bytes = None, 0
+    if workspace is None and (gweight is not None or gbias is not None):
+        need = layer_norm_grad_workspace_bytes(x)
+        if need:
+            workspace = _scratch(need, x.device, stream)
+    if workspace is not None:
+        ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel()
+    rc = _ocn_layer_norm_grad(_optional(gout), _optional(x), _optional(weight), _optional(gin), _optional(gweight), _optional(gbias), eps,
                               ws_ptr, ws_bytes, _stream(stream))
     if rc:
         _check(rc)

@@ -27,7 +27,9 @@ COMMON = ["--offload-arch=gfx950", *os.environ.get("OCN_EXTRA_FLAGS", "").split(
           "-Wno-unused-command-line-argument"]
 
 SOURCES = (["api.cpp", "planner.cpp", "ew_launch.cpp", "red_launch.cpp", "ew_interp.hip", "ew_interleave.hip", "ew_pixels.hip", "index.hip",
-            "head_checks.cpp", "heads.hip", "cache_attention.hip"]
+            "head_checks.cpp", "heads.hip", "layer_norm.hip", "cache_attention.hip",
+            "attention_checks.cpp", "attention_half.hip", "attention_bfloat16.hip", "attention_float.hip",
+            "attention_grad_half.hip", "attention_grad_bfloat16.hip", "attention_grad_float.hip"]
            + [f"ew_slice_{i}.hip" for i in range(8)] + [f"red_slice_{i}.hip" for i in range(4)]
            + [f"fred_slice_{i}.hip" for i in range(4)])
 

@@ -1,0 +1,469 @@
+// Kernels of attention over whole sequences, for one type.
+#pragma once
+
+#include <algorithm>
+
+#include "attention.hpp"
+#include "attention_tiles.hpp"
+
+namespace ocn {
+namespace {
+
+// ---------------------------------------------------------------------------------------
+// One pass over the keys.  A wavefront has the rows of one tile; for some keys at a time it forms scores^T = K Q^T and out^T += V^T P^T, so that a lane holds scores
+// and results of one row: the row's largest score, the sum of its weights and what results are scaled by need no other lane than the one or three that share the row.
+// A score's maximum is raised, and results rescaled, only where a weight would pass 2^kRaise.  The difference of scores is formed before it is scaled, so that it is never
+// above zero by more than that, however large scores are.
+// ---------------------------------------------------------------------------------------
+
+constexpr float kRaise = 4.0f;
+// log2 of the weight of a row's largest score.  A half holds 2^-14 ... 2^16 without loss: weights are put near its upper end.
+template <class T> constexpr float kTop = std::is_same<T, f16>::value ? 11.0f : 0.0f;
+
+// What a wavefront has of its rows
+template <class T, int D> struct Rows {
+  frag_t<T> q[D / 16];
+  acc_t<T> out[D / Tile<T>::kSide];
+  float best, total;           // the score that weights are relative to (minus infinity: none yet), the sum of a lane's own weights
+  int lo, hi;                  // keys that the row sees
+};
+
+template <class T> __device__ __forceinline__ acc_t<T> zero_acc() {
+  acc_t<T> a;
+#pragma unroll
+  for (int i = 0; i < Tile<T>::kOwn; ++i) a[i] = 0.0f;
+  return a;
+}
+
+// Whether there is anything but numbers among KEYS keys' values in LDS.  Weights of zero would make NaNs of those in the products.
+template <class T, int D, int KEYS> __device__ __forceinline__ bool odd_values(const char *v, int lane) {
+  constexpr uint32_t exponent = std::is_same<T, float>::value ? 0x7f800000u : std::is_same<T, f16>::value ? 0x7c007c00u : 0x7f807f80u;
+  constexpr uint32_t one = std::is_same<T, float>::value ? 0x00800000u : std::is_same<T, f16>::value ? 0x04000400u : 0x00800080u;
+  uint32_t odd = 0;
+#pragma nounroll
+  for (int i = lane; i < KEYS * Held<T, D>::kPieces; i += kWave) {
+    const u32x4 x = *(const u32x4 *)(v + Held<T, D>::at(i / Held<T, D>::kPieces, i % Held<T, D>::kPieces));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) odd |= (x[e] & exponent) + one;      // (into the sign's place where all bits of an exponent are set)
+  }
+  return __any((odd & (sizeof(T) == 2 ? 0x80008000u : 0x80000000u)) != 0);
+}
+
+// A row by itself, key by key: what a tile's row that does not see such a value gets instead.  Lanes have channels.
+template <class T, int D> struct SlowRow {
+  static constexpr int kEach = (D + kWave - 1) / kWave;
+  float best, total, x[kEach];
+  __device__ __forceinline__ void run(const AttentionArgs &a, const char *q, const char *k, const char *v, int lo, int hi, int lane) {
+    float mine[kEach];
+    best = -__builtin_inff(), total = 0.0f;
+#pragma unroll
+    for (int c = 0; c < kEach; ++c) {
+      const int e = c * kWave + lane;
+      x[c] = 0.0f;
+      mine[c] = e < a.channels && !a.nothing ? (float)*(const T *)(q + e * a.q.channel) * (a.negative ? -1.0f : 1.0f) : 0.0f;
+    }
+#pragma nounroll
+    for (int j = lo; j < hi; ++j) {
+      float s = 0.0f;
+#pragma unroll
+      for (int c = 0; c < kEach; ++c) {
+        const int e = c * kWave + lane;
+        if (e < a.channels) s = __builtin_fmaf(mine[c], (float)*(const T *)(k + (int64_t)j * a.k.token + e * a.k.channel), s);
+      }
+      s = sum_over_row(s, kWave);
+      float keep = 1.0f;
+      if ((s - best) * a.scale > kRaise) {
+        keep = best > -__builtin_inff() ? __builtin_amdgcn_exp2f((best - s) * a.scale) : 0.0f;
+        best = s;
+      }
+      const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s - (best > -__builtin_inff() ? best : 0.0f), a.scale, kTop<T>));
+      total = __builtin_fmaf(total, keep, p);
+#pragma unroll
+      for (int c = 0; c < kEach; ++c) {
+        const int e = c * kWave + lane;
+        if (e < a.channels) x[c] = __builtin_fmaf(x[c], keep, p * (float)*(const T *)(v + (int64_t)j * a.v.token + e * a.v.channel));
+      }
+    }
+  }
+};
+
+// KEYS keys of a tile in LDS, from key `first` of the sequence on.  `masked`: some row does not see all of them; true: and values that it does not see may have reached it.
+template <class T, int D, int KEYS> __device__ __forceinline__ bool attend(Rows<T, D> &r, const char *k, const char *v, int first, bool masked, float scale, int lane) {
+  constexpr int SIDE = Tile<T>::kSide, TILES = KEYS / SIDE, OWN = Tile<T>::kOwn, STEPS = Tile<T>::kSteps;
+  const int n = lane & (SIDE - 1), h = lane / SIDE;
+  acc_t<T> s[TILES];
+#pragma unroll
+  for (int t = 0; t < TILES; ++t) {
+    s[t] = zero_acc<T>();
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) s[t] = product(rows_fragment<T, D>(k, t * SIDE, c, n, h), r.q[c], s[t]);
+  }
+  if (masked) {
+#pragma unroll
+    for (int t = 0; t < TILES; ++t)
+#pragma unroll
+      for (int i = 0; i < OWN; ++i) {
+        const int j = first + t * SIDE + own_index<T>(i) + 4 * h;
+        if (j < r.lo || j >= r.hi) s[t][i] = -__builtin_inff();
+      }
+  }
+  float top = s[0][0];
+#pragma unroll
+  for (int t = 0; t < TILES; ++t)
+#pragma unroll
+    for (int i = 0; i < OWN; ++i) top = fmaxf(top, s[t][i]);
+  top = column_max<T>(top);
+  if (__any((top - r.best) * scale > kRaise)) {       // (the first finite score is above minus infinity by more than that; no score at all is not)
+    const float best = fmaxf(r.best, top), keep = r.best > -__builtin_inff() ? __builtin_amdgcn_exp2f((r.best - best) * scale) : 0.0f;
+    r.best = best;
+    r.total *= keep;
+#pragma unroll
+    for (int ct = 0; ct < D / SIDE; ++ct)
+#pragma unroll
+      for (int i = 0; i < OWN; ++i) r.out[ct][i] *= keep;
+  }
+  const float best = r.best > -__builtin_inff() ? r.best : 0.0f;
+#pragma unroll
+  for (int t = 0; t < TILES; ++t)
+#pragma unroll
+    for (int i = 0; i < OWN; ++i) {
+      s[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i] - best, scale, kTop<T>));
+      r.total += s[t][i];
+    }
+#pragma unroll
+  for (int t = 0; t < TILES; ++t)
+#pragma unroll
+    for (int x = 0; x < STEPS; ++x) {
+      const frag_t<T> p = as_fragment<T>(s[t], x);
+#pragma unroll
+      for (int ct = 0; ct < D / SIDE; ++ct) r.out[ct] = product(columns_fragment<T, D>(v, t * SIDE + 16 * x, ct, lane), p, r.out[ct]);
+    }
+  return masked && odd_values<T, D, KEYS>(v, lane);
+}
+
+// Keys [first, first + KEYS) of a sequence on their way into LDS, by `LANES` lanes; those past the end are zero.
+template <class T, int D, bool VEC, int KEYS, int LANES> struct Carried {
+  static constexpr int kAll = KEYS * Held<T, D>::kPieces, kEach = (kAll + LANES - 1) / LANES;
+  u32x4 k[kEach], v[kEach];
+  __device__ __forceinline__ void load(const AttentionArgs &a, const char *pk, const char *pv, int first, int count, int lane) {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int at = i * LANES + lane, row = at / Held<T, D>::kPieces, e = at % Held<T, D>::kPieces * (16 / (int)sizeof(T)), j = first + row;
+      const bool in = (kAll % LANES == 0 || at < kAll) && j < count;
+      k[i] = load_piece<T, VEC>(pk + (int64_t)(in ? j : 0) * a.k.token, a.k.channel, e, in ? a.channels : 0);
+      v[i] = load_piece<T, VEC>(pv + (int64_t)(in ? j : 0) * a.v.token, a.v.channel, e, in ? a.channels : 0);
+    }
+  }
+  __device__ __forceinline__ void store(char *hk, char *hv, int lane) const {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int at = i * LANES + lane;
+      if (kAll % LANES != 0 && at >= kAll) continue;
+      const int place = Held<T, D>::at(at / Held<T, D>::kPieces, at % Held<T, D>::kPieces);
+      *(u32x4 *)(hk + place) = k[i];
+      *(u32x4 *)(hv + place) = v[i];
+    }
+  }
+};
+
+// the row that lane n of a tile has, and its queries: Q, and the keys that it sees
+template <class T, int D, bool VEC> __device__ __forceinline__ void start_rows(Rows<T, D> &r, const AttentionArgs &a, const Work &w, int row, int lane, const char *q) {
+  constexpr int SIDE = Tile<T>::kSide;
+  const int h = lane / SIDE;
+  const RowPlace p = row_place(a, w, row);
+  Limits l = limits_of(a, w, p.query);
+  r.lo = l.lo, r.hi = l.hi;
+  r.best = -__builtin_inff();
+  r.total = 0.0f;
+#pragma unroll
+  for (int ct = 0; ct < D / SIDE; ++ct) r.out[ct] = zero_acc<T>();
+  const char *at = q + (int64_t)p.query * a.q.token + (int64_t)p.head * a.q.head;
+#pragma unroll
+  for (int c = 0; c < D / 16; ++c) {
+    union { u32x4 v; frag_t<T> f; uint32_t u[4]; } x;
+    x.v = load_piece<T, VEC>(at, a.q.channel, 16 * c + Tile<T>::kFrag * h, p.in && !a.nothing ? a.channels : 0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x.u[i] ^= a.negative ? (sizeof(T) == 2 ? 0x80008000u : 0x80000000u) : 0u;
+    r.q[c] = x.f;
+  }
+}
+
+// four neighbouring channels of a row, rounded
+template <class T, bool VEC> __device__ __forceinline__ void store_four(char *row, int64_t step, int e, int d, const float *v) {
+  if constexpr (VEC) {
+    typedef T V __attribute__((ext_vector_type(4)));
+    V o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = (T)v[i];
+    if (e < d) *(V *)(row + e * (int)sizeof(T)) = o;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (e + i < d) *(T *)(row + (e + i) * step) = (T)v[i];
+  }
+}
+
+// log of the sum of exponentials of a row, in natural logarithms
+template <class T> __device__ __forceinline__ float log_sum_of(const AttentionArgs &a, float best, float total) {
+  return total > 0.0f || total != total ? __builtin_fmaf(best > -__builtin_inff() ? best : 0.0f, a.plain_scale, (__builtin_amdgcn_logf(total) - kTop<T>) * 0.69314718055994530942f) : -__builtin_inff();
+}
+
+// where a row lies in a tensor of query heads
+__device__ __forceinline__ int64_t row_offset(const HeadView &x, const AttentionArgs &a, const Work &w, const RowPlace &p) {
+  return w.sequence * x.batch + (w.q.first + p.query) * x.token + ((int64_t)w.kv * a.per_kv + p.head) * x.head;
+}
+
+// a row's results, lanes having channels 64 apart
+template <class T, int D> __device__ __forceinline__ void finish_row(const AttentionArgs &a, const Work &w, const RowPlace &p, const float *x, float best, float total, int lane) {
+  const float over = total > 0.0f || total != total ? 1.0f / total : 0.0f;
+  char *const out = a.out.base + row_offset(a.out, a, w, p);
+#pragma unroll
+  for (int c = 0; c < (D + kWave - 1) / kWave; ++c)
+    if (c * kWave + lane < a.channels) *(T *)(out + (c * kWave + lane) * a.out.channel) = (T)(x[c] * over);
+  if (a.log_sum.base && lane == 0) *(float *)(a.log_sum.base + row_offset(a.log_sum, a, w, p)) = log_sum_of<T>(a, best, total);
+}
+
+// Many rows: the wavefronts of a workgroup have a tile of rows each and share the keys, which go through LDS once for all of them, the next ones on their way.
+template <class T, int D, bool VEC, int WAVES, int KEYS> __global__ __launch_bounds__(WAVES *kWave) void attention_rows_kernel(const AttentionArgs a, uint32_t first_block) {
+  warm_arguments<AttentionArgs>();
+  constexpr int SIDE = Tile<T>::kSide, PITCH = Held<T, D>::kPitch;
+  __shared__ __align__(16) char lds[2 * 2 * KEYS * PITCH];        // [2][keys, values][KEYS][PITCH]
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+  Work w;
+  if (!find_work(a, first_block + blockIdx.x, &w)) return;
+  Rows<T, D> r;
+  const int row = wave * SIDE + (lane & (SIDE - 1));
+  start_rows<T, D, VEC>(r, a, w, row, lane, a.q.base + w.sequence * a.q.batch + w.q.first * a.q.token + (int64_t)w.kv * a.per_kv * a.q.head);
+  const char *pk = a.k.base + w.sequence * a.k.batch + w.k.first * a.k.token + (int64_t)w.kv * a.k.head, *pv = a.v.base + w.sequence * a.v.batch + w.k.first * a.v.token + (int64_t)w.kv * a.v.head;
+  const Limits all = limits_of_block(a, w);
+  const int hi_first = __builtin_amdgcn_readfirstlane(r.hi), hi_last = __builtin_amdgcn_readlane(r.hi, SIDE - 1), lo_first = __builtin_amdgcn_readfirstlane(r.lo),
+            lo_last = __builtin_amdgcn_readlane(r.lo, SIDE - 1);
+  Carried<T, D, VEC, KEYS, WAVES * kWave> next;
+  bool odd = false;
+  int at = all.lo / KEYS * KEYS, turn = 0;
+  if (at < all.hi) {
+    next.load(a, pk, pv, at, w.k.count, threadIdx.x);
+    next.store(lds, lds + KEYS * PITCH, threadIdx.x);
+    __syncthreads();
+  }
+  for (; at < all.hi; at += KEYS, turn ^= 1) {
+    char *const k = lds + turn * 2 * KEYS * PITCH, *const other = lds + (turn ^ 1) * 2 * KEYS * PITCH;
+    const bool more = at + KEYS < all.hi;
+    if (more) next.load(a, pk, pv, at + KEYS, w.k.count, threadIdx.x);
+    if (at < hi_last && at + KEYS > lo_first) odd |= attend<T, D, KEYS>(r, k, k + KEYS * PITCH, at, at + KEYS > hi_first || at < lo_last, a.scale, lane);
+    if (more) next.store(other, other + KEYS * PITCH, threadIdx.x);
+    __syncthreads();
+  }
+  if (odd) {
+#pragma nounroll
+    for (int i = wave * SIDE; i < wave * SIDE + SIDE; ++i) {
+      const RowPlace p = row_place(a, w, i);
+      if (!p.in) continue;
+      const Limits l = limits_of(a, w, p.query);
+      SlowRow<T, D> slow;
+      slow.run(a, a.q.base + row_offset(a.q, a, w, p), pk, pv, l.lo, l.hi, lane);
+      finish_row<T, D>(a, w, p, slow.x, slow.best, slow.total, lane);
+    }
+    return;
+  }
+  const float total = column_sum<T>(r.total), over = total > 0.0f || total != total ? 1.0f / total : 0.0f;
+  const RowPlace p = row_place(a, w, row);
+  if (!p.in) return;
+  char *const out = a.out.base + row_offset(a.out, a, w, p);
+#pragma unroll
+  for (int ct = 0; ct < D / SIDE; ++ct)
+#pragma unroll
+    for (int i = 0; i < Tile<T>::kOwn; i += 4) {
+      float v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = r.out[ct][i + e] * over;
+      store_four<T, VEC>(out, a.out.channel, ct * SIDE + own_index<T>(i) + 4 * (lane / SIDE), a.channels, v);
+    }
+  if (a.log_sum.base && lane < SIDE)
+    *(float *)(a.log_sum.base + row_offset(a.log_sum, a, w, p)) = log_sum_of<T>(a, r.best, total);
+}
+
+// Few rows (single tokens): the wavefronts of a workgroup have the same tile of rows and take every fourth tile of keys, through a part of LDS of their own; a long sequence is
+// split over workgroups as well.  What they found is joined here, and that of several workgroups by a second launch.
+
+struct Split { int first, end; bool alone, mine; };      // keys of a split; whether it is the only one; whether there is it
+__device__ __forceinline__ Split split_of(const AttentionArgs &a, const Limits &all, int side, int split) {
+  const int lo = all.lo / side, hi = (all.hi + side - 1) / side, tiles = hi > lo ? hi - lo : 0;
+  int per = (tiles + a.splits - 1) / a.splits;
+  if (per < kLeastTiles) per = kLeastTiles;
+  Split s;
+  s.alone = tiles <= per;
+  s.mine = split == 0 || split * per < tiles;
+  s.first = (lo + split * per) * side;
+  s.end = (lo + (split * per + per < tiles ? split * per + per : tiles)) * side;
+  if (s.end > all.hi) s.end = all.hi;
+  return s;
+}
+
+template <class T, int D, bool VEC> __global__ __launch_bounds__(kFewWaves *kWave) void attention_few_kernel(const AttentionArgs a, uint32_t first_block) {
+  warm_arguments<AttentionArgs>();
+  constexpr int SIDE = Tile<T>::kSide, PITCH = Held<T, D>::kPitch, PART = 2 * SIDE * PITCH;
+  static_assert(SIDE * D * 4 <= PART, "a wavefront's results take the place of its keys and values");
+  __shared__ __align__(16) char lds[kFewWaves * PART];        // [wavefronts][keys, values][SIDE][PITCH]
+  __shared__ float bests[kFewWaves][SIDE], totals[kFewWaves][SIDE];
+  __shared__ bool odds[kFewWaves];
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, n = lane & (SIDE - 1);
+  Work w;
+  if (!find_work(a, first_block + blockIdx.x, &w)) return;
+  const Limits all = limits_of_block(a, w);
+  const Split split = split_of(a, all, SIDE, w.split);
+  if (!split.mine) return;
+  Rows<T, D> r;
+  start_rows<T, D, VEC>(r, a, w, n, lane, a.q.base + w.sequence * a.q.batch + w.q.first * a.q.token + (int64_t)w.kv * a.per_kv * a.q.head);
+  const char *pk = a.k.base + w.sequence * a.k.batch + w.k.first * a.k.token + (int64_t)w.kv * a.k.head, *pv = a.v.base + w.sequence * a.v.batch + w.k.first * a.v.token + (int64_t)w.kv * a.v.head;
+  const int hi_first = __builtin_amdgcn_readfirstlane(r.hi), lo_last = __builtin_amdgcn_readlane(r.lo, SIDE - 1);
+  char *const k = lds + wave * PART, *const v = k + SIDE * PITCH;
+  Carried<T, D, VEC, SIDE, kWave> next;
+  int at = split.first + wave * SIDE;
+  bool odd = false;
+  if (at < split.end) next.load(a, pk, pv, at, w.k.count, lane);
+  for (; at < split.end; at += kFewWaves * SIDE) {
+    next.store(k, v, lane);
+    if (at + kFewWaves * SIDE < split.end) next.load(a, pk, pv, at + kFewWaves * SIDE, w.k.count, lane);
+    __builtin_amdgcn_wave_barrier();
+    odd |= attend<T, D, SIDE>(r, k, v, at, at + SIDE > hi_first || at < lo_last, a.scale, lane);
+    __builtin_amdgcn_wave_barrier();
+  }
+  const float total = column_sum<T>(r.total);
+  if (lane < SIDE) bests[wave][n] = r.best, totals[wave][n] = total;
+  if (lane == 0) odds[wave] = odd;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kFewWaves; ++i) odd |= odds[i];
+  if (odd) {
+#pragma nounroll
+    for (int i = wave; i < SIDE; i += kFewWaves) {
+      const RowPlace p = row_place(a, w, i);
+      if (!p.in) continue;
+      const Limits l = limits_of(a, w, p.query);
+      SlowRow<T, D> slow;
+      slow.run(a, a.q.base + row_offset(a.q, a, w, p), pk, pv, l.lo > split.first ? l.lo : split.first, l.hi < split.end ? l.hi : split.end, lane);
+      if (split.alone) {
+        finish_row<T, D>(a, w, p, slow.x, slow.best, slow.total, lane);
+      } else {
+        const int64_t part = ((int64_t)w.unit * a.splits + w.split) * SIDE + i;
+#pragma unroll
+        for (int c = 0; c < SlowRow<T, D>::kEach; ++c)
+          if (c * kWave + lane < D) a.parts[part * D + c * kWave + lane] = slow.x[c];
+        if (lane == 0) a.part_sums[2 * part] = slow.best, a.part_sums[2 * part + 1] = slow.total;
+      }
+    }
+    return;
+  }
+  float best = bests[0][n];
+#pragma unroll
+  for (int i = 1; i < kFewWaves; ++i) best = fmaxf(best, bests[i][n]);
+  const float keep = r.best > -__builtin_inff() ? __builtin_amdgcn_exp2f((r.best - best) * a.scale) : 0.0f;
+  float *const own = (float *)k;       // [SIDE][D]
+#pragma unroll
+  for (int ct = 0; ct < D / SIDE; ++ct)
+#pragma unroll
+    for (int i = 0; i < Tile<T>::kOwn; ++i) own[n * D + ct * SIDE + own_index<T>(i) + 4 * (lane / SIDE)] = r.out[ct][i] * keep;
+  __syncthreads();
+  for (int i = threadIdx.x; i < SIDE * (D / 4); i += kFewWaves * kWave) {
+    const int row = i / (D / 4), e = i % (D / 4) * 4;
+    const RowPlace p = row_place(a, w, row);
+    if (!p.in) continue;
+    float top = bests[0][row], sum = 0.0f, x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int u = 1; u < kFewWaves; ++u) top = fmaxf(top, bests[u][row]);
+#pragma unroll
+    for (int u = 0; u < kFewWaves; ++u) {
+      const float b = bests[u][row];
+      sum += totals[u][row] * (b > -__builtin_inff() ? __builtin_amdgcn_exp2f((b - top) * a.scale) : 1.0f);
+      const f32x4 y = *(const f32x4 *)(lds + u * PART + (row * D + e) * 4);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) x[c] += y[c];
+    }
+    if (split.alone) {
+      const float over = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) x[c] *= over;
+      store_four<T, VEC>(a.out.base + row_offset(a.out, a, w, p), a.out.channel, e, a.channels, x);
+      if (a.log_sum.base && e == 0) *(float *)(a.log_sum.base + row_offset(a.log_sum, a, w, p)) = log_sum_of<T>(a, top, sum);
+    } else {
+      const int64_t part = ((int64_t)w.unit * a.splits + w.split) * SIDE + row;
+      *(f32x4 *)(a.parts + part * D + e) = f32x4{x[0], x[1], x[2], x[3]};
+      if (e == 0) a.part_sums[2 * part] = top, a.part_sums[2 * part + 1] = sum;
+    }
+  }
+}
+
+// What several workgroups found of a row, joined: a wavefront to a row.
+template <class T, int D> __global__ __launch_bounds__(kBlock) void attention_join_kernel(const AttentionArgs a, uint32_t first_unit) {
+  constexpr int SIDE = Tile<T>::kSide, EACH = (D + kWave - 1) / kWave;
+  const int lane = threadIdx.x & (kWave - 1);
+  Work w;
+  if (!find_work(a, (first_unit + blockIdx.x) * (uint32_t)a.splits, &w)) return;
+  const Limits all = limits_of_block(a, w);
+  if (split_of(a, all, SIDE, 0).alone) return;
+  for (int row = threadIdx.x / kWave; row < SIDE; row += kBlock / kWave) {
+    const RowPlace p = row_place(a, w, row);
+    if (!p.in) continue;
+    const int64_t part = (int64_t)w.unit * a.splits * SIDE + row;
+    const bool there = lane < a.splits && split_of(a, all, SIDE, lane).mine;
+    const float own = there ? a.part_sums[2 * (part + (int64_t)lane * SIDE)] : -__builtin_inff();
+    float top = own;
+#pragma unroll
+    for (int o = 32; o > 0; o /= 2) top = fmaxf(top, __shfl_xor(top, o));
+    const float keep = !there ? 0.0f : own > -__builtin_inff() ? __builtin_amdgcn_exp2f((own - top) * a.scale) : 1.0f;
+    float sum = there ? a.part_sums[2 * (part + (int64_t)lane * SIDE) + 1] * keep : 0.0f;
+#pragma unroll
+    for (int o = 32; o > 0; o /= 2) sum += __shfl_xor(sum, o);
+    float x[EACH];
+#pragma unroll
+    for (int c = 0; c < EACH; ++c) x[c] = 0.0f;
+    for (int s = 0; s < a.splits && split_of(a, all, SIDE, s).mine; ++s) {
+      const float f = __shfl(keep, s);
+#pragma unroll
+      for (int c = 0; c < EACH; ++c)
+        if (c * kWave + lane < D) x[c] = __builtin_fmaf(a.parts[(part + (int64_t)s * SIDE) * D + c * kWave + lane], f, x[c]);
+    }
+    finish_row<T, D>(a, w, p, x, top, sum, lane);
+  }
+}
+
+// ---------------------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------------------
+
+int done(hipError_t e) {
+  if (e == hipSuccess) return OCN_OK;
+  record_hip_error((int)e);
+  return OCN_ERR_LAUNCH;
+}
+
+template <class T> constexpr int kRowKeys = sizeof(T) == 2 ? 64 : 32;
+
+template <class T, int D, bool VEC> int run(AttentionArgs &a, const AttentionPlan &p, hipStream_t stream) {
+  const int64_t blocks = p.units * p.splits;
+  int rc;
+  const int64_t most = max_launch_blocks();
+  for (int64_t at = 0; at < blocks; at += most) {
+    const uint32_t grid = (uint32_t)std::min(blocks - at, most), first = (uint32_t)at;
+    if (p.few) hipLaunchKernelGGL((attention_few_kernel<T, D, VEC>), dim3(grid), dim3(kFewWaves * kWave), 0, stream, a, first);
+    else hipLaunchKernelGGL((attention_rows_kernel<T, D, VEC, kRowWaves, kRowKeys<T>>), dim3(grid), dim3(kRowWaves * kWave), 0, stream, a, first);
+    if ((rc = done(hipGetLastError())) != OCN_OK) return rc;
+  }
+  if (p.splits == 1) return OCN_OK;
+  for (int64_t at = 0; at < p.units; at += most) {
+    const uint32_t grid = (uint32_t)std::min(p.units - at, most), first = (uint32_t)at;
+    hipLaunchKernelGGL((attention_join_kernel<T, D>), dim3(grid), dim3(kBlock), 0, stream, a, first);
+    if ((rc = done(hipGetLastError())) != OCN_OK) return rc;
+  }
+  return OCN_OK;
+}
+
+template <class T> int run_type(AttentionArgs &a, const AttentionPlan &p, bool vec, hipStream_t stream) {
+#define OCN_RUN(T, D, VEC) return run<T, D, VEC>(a, p, stream)
+  OCN_BY_PADDED(T, a.channels, vec, OCN_RUN);
+#undef OCN_RUN
+}
+
+}  // namespace
+}  // namespace ocn

@@ -1,0 +1,8 @@
+// Gradient of attention over whole sequences: kernels for bfloat16.
+#include "attention_backward.hpp"
+
+namespace ocn {
+int run_attention_grad_bfloat16(AttentionArgs &a, const AttentionSizes &s, const AttentionGrad &p, bool vec, void *workspace, void *stream) {
+  return run_grad_type<bf16>(a, s, p, vec, workspace, (hipStream_t)stream);
+}
+}  // namespace ocn

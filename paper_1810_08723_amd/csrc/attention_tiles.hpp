@@ -1,0 +1,233 @@
+// What attention's kernels over whole sequences and their gradients share: tiles of the matrix units, operands in LDS, and which sequence a workgroup has.
+//
+// Rows are the queries of a sequence with the query heads that share a head of keys and values: row r is query r / per_kv, head r % per_kv of the group.
+// A tile is kSide keys by kSide rows.  Products are formed so that a lane holds one column of the result and the sixteen (four) other indices that are
+// its own come in runs of four:
+//
+//     16-bit types   32x32x16 products: lane (n = lane % 32, h = lane / 32), element i of the result: column n, index 8 (i / 4) + 4 h + i % 4
+//     float          16x16x4 products:  lane (n = lane % 16, h = lane / 16), element i: column n, index 4 h + i
+//
+// A fragment is 16 bytes of a lane, an operand's share of 16 steps of a sum.  Which of the 16 a lane has is free as long as both operands agree: where a result
+// is the next product's operand, its own order is taken, so that nothing crosses lanes, and the other operand, transposed, is read from LDS in that order.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <type_traits>
+
+#include "attention.hpp"
+#include "dev_types.hpp"
+#include "head_types.hpp"
+
+namespace ocn {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+template <class T> struct Tile {
+  static constexpr int kSide = sizeof(T) == 2 ? 32 : 16;
+  static constexpr int kOwn = sizeof(T) == 2 ? 16 : 4;            // elements of a result in a lane
+  static constexpr int kGroups = kWave / kSide;                   // h
+  static constexpr int kFrag = 16 / (int)sizeof(T);               // elements of a fragment in a lane
+  static constexpr int kSteps = kSide / 16;                       // fragments along a tile's side
+  typedef T Frag __attribute__((ext_vector_type(16 / sizeof(T))));
+  typedef float Acc __attribute__((ext_vector_type(sizeof(T) == 2 ? 16 : 4)));
+};
+template <class T> using frag_t = typename Tile<T>::Frag;
+template <class T> using acc_t = typename Tile<T>::Acc;
+
+__device__ __forceinline__ f32x16 product(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16 product(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 product(f32x4 a, f32x4 b, f32x4 c) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
+  return c;
+}
+
+// index of element i of a result (of which 4 h is the lane's own part)
+template <class T> __device__ __forceinline__ constexpr int own_index(int i) { return 8 * (i / 4) + i % 4; }
+
+// elements 16 s ... of a result as a fragment, rounded to the type
+template <class T> __device__ __forceinline__ frag_t<T> as_fragment(const acc_t<T> &a, int s) {
+  frag_t<T> f;
+  constexpr int N = Tile<T>::kFrag;
+#pragma unroll
+  for (int e = 0; e < N; ++e) f[e] = (T)a[s * N + e];
+  return f;
+}
+
+// over the lanes that hold a column
+template <class T> __device__ __forceinline__ float column_max(float x) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+  const uint32_t a0 = a[0], a1 = a[1];
+  x = fmaxf(__builtin_bit_cast(float, a0), __builtin_bit_cast(float, a1));
+  if constexpr (Tile<T>::kSide == 16) {
+    const auto b = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+    const uint32_t b0 = b[0], b1 = b[1];
+    x = fmaxf(__builtin_bit_cast(float, b0), __builtin_bit_cast(float, b1));
+  }
+  return x;
+}
+template <class T> __device__ __forceinline__ float column_sum(float x) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+  const uint32_t a0 = a[0], a1 = a[1];
+  x = __builtin_bit_cast(float, a0) + __builtin_bit_cast(float, a1);
+  if constexpr (Tile<T>::kSide == 16) {
+    const auto b = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+    const uint32_t b0 = b[0], b1 = b[1];
+    x = __builtin_bit_cast(float, b0) + __builtin_bit_cast(float, b1);
+  }
+  return x;
+}
+
+// ---- operands in LDS ---------------------------------------------------------------------------
+//
+// Rows of D channels, each at a power of two of bytes, in pieces of 16 bytes.  Piece c of row r lies at place c ^ turn(r), so that
+// neither sixteen rows' same piece nor four rows' pieces of sixteen channels (a transposed read) meet in a bank.
+template <class T, int D> struct Held {
+  static constexpr int kPitch = (D * (int)sizeof(T) <= 128 ? 128 : D * (int)sizeof(T) <= 256 ? 256 : D * (int)sizeof(T) <= 512 ? 512 : 1024);
+  static constexpr int kPieces = D * (int)sizeof(T) / 16;
+  __device__ __forceinline__ static int turn(int row) {
+    if constexpr (sizeof(T) == 4) return row & 15;
+    else if constexpr (kPitch == 128) return (2 * ((row >> 1) & 3)) | ((row >> 3) & 1);
+    else return (2 * (row & 7)) | ((row >> 3) & 1);
+  }
+  __device__ __forceinline__ static int at(int row, int piece) { return row * kPitch + ((piece ^ turn(row)) << 4); }
+};
+
+// A fragment of 16 channels (16 step ...) of rows `row` + n
+template <class T, int D> __device__ __forceinline__ frag_t<T> rows_fragment(const char *held, int row, int step, int n, int h) {
+  return *(const frag_t<T> *)(held + Held<T, D>::at(row + n, step * (int)sizeof(T) + h));
+}
+
+// Its transpose: lane n has channel side * tile + n of the 16 rows row ... row + 15, in a result's order
+template <class T, int D> __device__ __forceinline__ frag_t<T> columns_fragment(const char *held, int row, int tile, int lane) {
+  frag_t<T> f;
+  if constexpr (sizeof(T) == 2) {
+    const int h = lane >> 5, j = lane & 15, channel = tile * 32 + (lane & 16) + 4 * (j & 3), r = row + 4 * h + (j >> 2);
+    typedef __attribute__((address_space(3))) s16x4 *Lds;
+    union { s16x4 s[2]; frag_t<T> f; } u;
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      u.s[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(held + Held<T, D>::at(r + 8 * k, channel >> 3) + 2 * (channel & 7)));
+    f = u.f;
+  } else {
+    const int h = lane >> 4, channel = tile * 16 + (lane & 15);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f[e] = *(const float *)(held + Held<T, D>::at(row + 4 * h + e, channel >> 2) + 4 * (channel & 3));
+  }
+  return f;
+}
+
+// 16 bytes of a row in memory, from channel e on; what lies outside of the row's d channels is zero
+template <class T, bool VEC> __device__ __forceinline__ u32x4 load_piece(const char *row, int64_t step, int e, int d) {
+  u32x4 v = {0, 0, 0, 0};
+  if constexpr (VEC) {
+    if (e < d) v = *(const u32x4 *)(row + e * (int)sizeof(T));
+  } else {
+    union { T t[16 / sizeof(T)]; u32x4 v; } u;
+    u.v = v;
+#pragma unroll
+    for (int i = 0; i < (int)(16 / sizeof(T)); ++i)
+      if (e + i < d) u.t[i] = *(const T *)(row + (e + i) * step);
+    v = u.v;
+  }
+  return v;
+}
+
+// ---- sequences ---------------------------------------------------------------------------------
+
+struct Span { int64_t first; int32_t count; };      // tokens of a sequence
+
+__device__ __forceinline__ int64_t start_at(const Starts &s, int i) {
+  const int64_t at = load_index(s.p + i * s.stride, s.wide);
+  return at < 0 ? 0 : at > s.all ? s.all : at;
+}
+__device__ __forceinline__ Span span_of(const Starts &s, int i) {
+  if (!s.p) return {0, (int32_t)s.all};
+  const int64_t first = start_at(s, i), end = start_at(s, i + 1);
+  return {first, (int32_t)(end > first ? end - first : 0)};
+}
+
+// Blocks of `size` tokens: a packed sequence has the slots start / size + its number up to the next one's, one for each of its blocks at least, as
+// a sequence that begins inside of a block's size may have one more than its length makes.
+__device__ __forceinline__ bool find_slot(const Starts &s, const FastDiv &size, uint32_t slot, int *sequence, uint32_t *block) {
+  // the last sequence whose first slot is not behind this one; all lanes of a wavefront look at once
+  int lo = 0, hi = s.sequences;      // in [lo, hi)
+  const int lane = threadIdx.x & (kWave - 1);
+  while (hi - lo > 1) {
+    const int step = (hi - lo + kWave - 1) / kWave, at = lo + lane * step;
+    const bool fits = at < hi && fast_quotient((uint32_t)start_at(s, at), size) + (uint32_t)at <= slot;
+    const uint64_t all = __ballot(fits);
+    const int last = all ? 63 - __builtin_clzll(all) : 0;
+    lo += last * step;
+    hi = lo + step < hi ? lo + step : hi;
+  }
+  *sequence = lo;
+  const uint32_t first = fast_quotient((uint32_t)start_at(s, lo), size) + (uint32_t)lo;
+  *block = slot - first;
+  return slot >= first;
+}
+
+// What a workgroup has: a block of a sequence's queries (or keys), with some heads that share a head of keys and values
+struct Work {
+  uint32_t unit, block;
+  int split, sequence, kv, head_block;
+  Span q, k;
+};
+
+// KEYS: blocks are of keys.  False: there is no such block.  (Blocks go from the last to the first: with a causal mask the later ones have more to do.)
+template <bool KEYS> __device__ __forceinline__ bool find_work_of(const AttentionArgs &a, uint32_t index, Work *w) {
+  w->unit = fast_quotient(index, a.splits_div);
+  w->split = (int)(index - w->unit * (uint32_t)a.splits);
+  const uint32_t down = fast_quotient(w->unit, a.across_div), across = w->unit - down * a.across_div.d;
+  if (down >= a.slots) return false;
+  const uint32_t slot = KEYS ? down : a.slots - 1 - down;
+  w->kv = (int)fast_quotient(across, a.head_blocks_div);
+  w->head_block = (int)(across - (uint32_t)w->kv * (uint32_t)a.head_blocks);
+  const Starts &s = KEYS ? a.k_starts : a.q_starts;
+  if (s.p) {
+    if (!find_slot(s, a.tokens_div, slot, &w->sequence, &w->block)) return false;
+  } else {
+    w->sequence = (int)fast_quotient(slot, a.per_sequence_div);
+    w->block = slot - (uint32_t)w->sequence * a.per_sequence;
+  }
+  w->q = span_of(a.q_starts, w->sequence);
+  w->k = span_of(a.k_starts, w->sequence);
+  return (int64_t)w->block * a.tokens < (KEYS ? w->k.count : w->q.count);
+}
+__device__ __forceinline__ bool find_work(const AttentionArgs &a, uint32_t index, Work *w) { return find_work_of<false>(a, index, w); }
+
+// Row `row` of a block: its query (of the sequence) and head (of the group); those past the end are taken as the last ones
+struct RowPlace { int query, head; bool in; };
+__device__ __forceinline__ RowPlace row_place(const AttentionArgs &a, const Work &w, int row) {
+  const int t = (int)fast_quotient((uint32_t)row, a.heads_div);
+  RowPlace p;
+  p.head = w.head_block * a.heads + row - t * a.heads;
+  const int64_t query = (int64_t)w.block * a.tokens + t;
+  p.in = t < a.tokens && query < w.q.count && p.head < a.per_kv;
+  p.query = (int)(query < w.q.count ? query : w.q.count - 1);
+  if (p.head >= a.per_kv) p.head = a.per_kv - 1;
+  return p;
+}
+
+struct Limits { int lo, hi; };       // keys lo <= j < hi of the sequence
+__device__ __forceinline__ Limits limits_of(const AttentionArgs &a, const Work &w, int query) {
+  Limits l = {0, w.k.count};
+  if (a.causal) {
+    const int end = query - w.q.count + w.k.count + 1;
+    l.hi = end < 0 ? 0 : end;
+    if (a.window && end > a.window) l.lo = end - a.window;
+  }
+  return l;
+}
+// what some row of a block of queries sees
+__device__ __forceinline__ Limits limits_of_block(const AttentionArgs &a, const Work &w) {
+  const int64_t first = (int64_t)w.block * a.tokens, end = first + a.tokens < w.q.count ? first + a.tokens : w.q.count;
+  const Limits one = limits_of(a, w, (int)first), last = limits_of(a, w, (int)end - 1);
+  return {one.lo, last.hi};
+}
+
+}  // namespace ocn

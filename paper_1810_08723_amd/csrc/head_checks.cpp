@@ -190,7 +190,12 @@ int check_rotation(const ocn_rotation *r, int64_t channels, int32_t device) {
   if (rc != OCN_OK) return rc;
   if (r->layout != OCN_ROTARY_HALF && r->layout != OCN_ROTARY_INTERLEAVED) return OCN_ERR_OP;
   if (r->rotary_dim < 2 || r->rotary_dim % 2 != 0 || r->rotary_dim > channels) return OCN_ERR_SHAPE;
-  if (r->frequencies->ndim != 1 || r->frequencies->size[0] != r->rotary_dim / 2) return OCN_ERR_SHAPE;
+  const int own = r->frequencies->ndim;
+  if ((own != 1 && own != 2) || r->frequencies->size[own - 1] != r->rotary_dim / 2) return OCN_ERR_SHAPE;
+  if (own == 2) {      // a row for each axis, and positions on each
+    const int64_t axes = r->frequencies->size[0];
+    if (axes < 1 || axes > OCN_MAX_AXES || r->positions->ndim < 1 || r->positions->size[0] != axes) return OCN_ERR_SHAPE;
+  }
   if (r->positions->device != device || r->frequencies->device != device) return OCN_ERR_DEVICE;
   return OCN_OK;
 }
@@ -223,5 +228,25 @@ extern "C" int ocn_rotary_frequencies(int32_t rotary_dim, double base, int stret
     frequencies[i] = keep == 1.0 ? f : f / factor * (1.0 - keep) + f * keep;
   }
   *magnitude = stretch == OCN_STRETCH_INDEX && factor > 1.0 ? 0.1 * std::log(factor) + 1.0 : 1.0;
+  return OCN_OK;
+}
+
+extern "C" int ocn_rotary_axes(int32_t axes, const int32_t *pairs, int order, const double *frequencies, double *table) {
+  if (!pairs || !frequencies || !table) return OCN_ERR_NULLPTR;
+  if (order != OCN_AXES_IN_ROW && order != OCN_AXES_IN_TURN) return OCN_ERR_OP;
+  if (axes < 1 || axes > OCN_MAX_AXES) return OCN_ERR_SHAPE;
+  int64_t all = 0, left[OCN_MAX_AXES];
+  for (int a = 0; a < axes; ++a) {
+    if (pairs[a] < 0) return OCN_ERR_SHAPE;
+    all += left[a] = pairs[a];
+  }
+  if (all < 1 || all > OCN_MAX_CHANNELS / 2) return OCN_ERR_SHAPE;
+  int at = 0;      // the axis whose turn it is
+  for (int64_t i = 0; i < all; ++i) {
+    while (left[at] == 0) at = (at + 1) % axes;
+    for (int a = 0; a < axes; ++a) table[a * all + i] = a == at ? frequencies[i] : 0.0;
+    --left[at];
+    if (order == OCN_AXES_IN_TURN) at = (at + 1) % axes;
+  }
   return OCN_OK;
 }

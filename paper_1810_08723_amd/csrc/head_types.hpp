@@ -39,6 +39,57 @@ __device__ __forceinline__ void store_from_float(char *p, int dtype, float v) {
   else *(bf16 *)p = (bf16)v;
 }
 
+// ---- rows: eight channels of a lane -------------------------------------------------------------------
+constexpr int kEight = 8;
+template <class T> using eight_t = typename Eight<T>::V;
+
+// eight channels from e on; those outside the row are zero
+template <class T, bool VEC> __device__ __forceinline__ eight_t<T> load_eight(const char *row, int64_t step, int e, int d) {
+  if constexpr (VEC) {
+    return *(const eight_t<T> *)(row + e * (int)sizeof(T));
+  } else {
+    eight_t<T> v;
+#pragma unroll
+    for (int i = 0; i < kEight; ++i) v[i] = e + i < d ? *(const T *)(row + (e + i) * step) : (T)0.0f;
+    return v;
+  }
+}
+// (stream: past the caches, for outputs that they could not keep)
+template <class T, bool VEC> __device__ __forceinline__ void store_eight(char *row, int64_t step, int e, int d, const float *v, bool stream) {
+  if constexpr (VEC) {
+    eight_t<T> o;
+#pragma unroll
+    for (int i = 0; i < kEight; ++i) o[i] = (T)v[i];
+    if (stream) {
+      asm volatile("");     // (these keep the two apart: made into one store, they would be an ordinary one)
+      __builtin_nontemporal_store(o, (eight_t<T> *)(row + e * (int)sizeof(T)));
+      asm volatile("");
+    } else {
+      *(eight_t<T> *)(row + e * (int)sizeof(T)) = o;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kEight; ++i)
+      if (e + i < d) *(T *)(row + (e + i) * step) = (T)v[i];
+  }
+}
+
+// ---- lanes ----------------------------------------------------------------------------------------------
+template <int CTRL> __device__ __forceinline__ float other_lane(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+}
+template <int CTRL> __device__ __forceinline__ uint32_t other_lane_bits(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true); }
+// the sum over a row's lanes (1, 2, 4 ... 64 of them): exchanges inside sixteen lanes cost no trip through LDS
+__device__ __forceinline__ float sum_over_row(float v, int lanes) {
+  if (lanes > 1) v += other_lane<0xb1>(v);      // 1 0 3 2
+  if (lanes > 2) v += other_lane<0x4e>(v);      // 2 3 0 1
+  if (lanes > 4) v += other_lane<0x141>(v);     // eight lanes mirrored
+  if (lanes > 8) v += other_lane<0x140>(v);     // sixteen lanes mirrored
+  if (lanes > 16) v += __shfl_xor(v, 16);
+  if (lanes > 32) v += __shfl_xor(v, 32);
+  return v;
+}
+
 // ---- a block of the cache: bytes of its parts for P tokens of D channels (a power of two) ------------
 __device__ __forceinline__ int block_k_codes(int page, int d, int token, int channel) { return token * (d / 2) + channel / 2; }
 __device__ __forceinline__ int block_v_codes(int page, int d, int token, int channel) {

@@ -21,7 +21,6 @@
 namespace ocn {
 namespace {
 
-constexpr int kEight = 8;              // channels of a lane
 constexpr int kTable = 2048;           // channels, of all its tokens, that a workgroup holds factors of
 constexpr int kPasses = 4;              // of a workgroup's lanes over its rows, at most
 constexpr int kFoldBlocks = 1024;      // workgroups that sum a gradient of weights, at most
@@ -55,10 +54,11 @@ struct HeadArgs {
   const char *pos;
   const char *freq;
   int64_t pos_l[kMaxLead], freq_stride;
+  int64_t pos_axis, freq_axis;         // strides from axis to axis
   double magnitude;
   float sign;                          // -1: turned back
   float eps, over_d;
-  int32_t pos_wide;
+  int32_t pos_wide, axes;
   int32_t half, row;                   // pairs of a head; floats of a token in the table
   FastDiv half_div;
   int32_t d, lanes_log2;               // channels; lanes of a row
@@ -133,9 +133,12 @@ template <int KIND> __device__ __forceinline__ void fill_table(const HeadArgs &a
 #pragma nounroll
   for (int i = threadIdx.x; i < tokens * a.half; i += kBlock) {
     const int t = (int)fast_quotient((uint32_t)i, a.half_div), p = i - t * a.half;
-    const int64_t at = load_index(address(a, a.pos, a.pos_l, token, t, 0, 0), a.pos_wide);
-    double s, c;
-    sine_cosine((double)at * *(const double *)(a.freq + p * a.freq_stride), &s, &c);
+    const char *pos = address(a, a.pos, a.pos_l, token, t, 0, 0), *freq = a.freq + p * a.freq_stride;
+    double angle = (double)load_index(pos, a.pos_wide) * *(const double *)freq, s, c;
+#pragma nounroll
+    for (int k = 1; k < a.axes; ++k)
+      angle = __builtin_fma((double)load_index(pos + k * a.pos_axis, a.pos_wide), *(const double *)(freq + k * a.freq_axis), angle);
+    sine_cosine(angle, &s, &c);
     const float cc = (float)(c * a.magnitude), ss = (float)(s * a.magnitude) * a.sign;
     const int one = KIND == kPairsInside ? 2 * p : p, two = KIND == kPairsInside ? 2 * p + 1 : p + a.half;
     float w1 = 1.0f, w2 = 1.0f;
@@ -154,39 +157,7 @@ template <int KIND> __device__ __forceinline__ void fill_table(const HeadArgs &a
 // rows
 // ---------------------------------------------------------------------------------------
 
-template <class T> using eight_t = typename Eight<T>::V;
 template <class T> struct Four { typedef T V __attribute__((ext_vector_type(4))); };
-
-// eight channels from e on; those outside the row are zero
-template <class T, bool VEC> __device__ __forceinline__ eight_t<T> load_eight(const char *row, int64_t step, int e, int d) {
-  if constexpr (VEC) {
-    return *(const eight_t<T> *)(row + e * (int)sizeof(T));
-  } else {
-    eight_t<T> v;
-#pragma unroll
-    for (int i = 0; i < kEight; ++i) v[i] = e + i < d ? *(const T *)(row + (e + i) * step) : (T)0.0f;
-    return v;
-  }
-}
-// (stream: past the caches, for outputs that they could not keep)
-template <class T, bool VEC> __device__ __forceinline__ void store_eight(char *row, int64_t step, int e, int d, const float *v, bool stream) {
-  if constexpr (VEC) {
-    eight_t<T> o;
-#pragma unroll
-    for (int i = 0; i < kEight; ++i) o[i] = (T)v[i];
-    if (stream) {
-      asm volatile("");     // (these keep the two apart: made into one store, they would be an ordinary one)
-      __builtin_nontemporal_store(o, (eight_t<T> *)(row + e * (int)sizeof(T)));
-      asm volatile("");
-    } else {
-      *(eight_t<T> *)(row + e * (int)sizeof(T)) = o;
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < kEight; ++i)
-      if (e + i < d) *(T *)(row + (e + i) * step) = (T)v[i];
-  }
-}
 
 // the other channels of the pairs that channels e ... e + 7 belong to (channel i < half goes with i + half), where they lie apart
 template <class T, int KIND> __device__ __forceinline__ eight_t<T> load_partners(const char *row, int64_t step, int e, int half) {
@@ -227,21 +198,6 @@ template <int KIND> __device__ __forceinline__ void turn(float *x, const float *
 #pragma unroll
   for (int i = 0; i < kEight; ++i)
     if (KIND == kPairsEight || e + i < 2 * half) x[i] = x[i] * a[i / 4][i % 4] + q[i] * b[i / 4][i % 4];
-}
-
-template <int CTRL> __device__ __forceinline__ float other_lane(float x) {
-  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
-}
-template <int CTRL> __device__ __forceinline__ uint32_t other_lane_bits(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true); }
-// the sum over a row's lanes (1, 2, 4 ... 64 of them): exchanges inside sixteen lanes cost no trip through LDS
-__device__ __forceinline__ float sum_over_row(float v, int lanes) {
-  if (lanes > 1) v += other_lane<0xb1>(v);      // 1 0 3 2
-  if (lanes > 2) v += other_lane<0x4e>(v);      // 2 3 0 1
-  if (lanes > 4) v += other_lane<0x141>(v);     // eight lanes mirrored
-  if (lanes > 8) v += other_lane<0x140>(v);     // sixteen lanes mirrored
-  if (lanes > 16) v += __shfl_xor(v, 16);
-  if (lanes > 32) v += __shfl_xor(v, 32);
-  return v;
 }
 
 struct Item { int which, tokens, head; uint32_t token; };
@@ -625,6 +581,18 @@ int kind_of_pairs(const ocn_rotation *r, bool vec) {
   return !vec ? kPairsOne : half % 8 == 0 ? kPairsEight : half % 4 == 0 ? kPairsFour : kPairsOne;
 }
 
+// the positions on one axis, as they broadcast
+ocn_tensor one_axis(const ocn_rotation *r) {
+  ocn_tensor t;
+  std::memset(&t, 0, sizeof t);
+  if (!r) return t;
+  t = *r->positions;
+  if (r->frequencies->ndim == 1) return t;
+  --t.ndim;
+  for (int d = 0; d < t.ndim; ++d) t.size[d] = r->positions->size[d + 1], t.stride[d] = r->positions->stride[d + 1];
+  return t;
+}
+
 // what does not hang on the tensors' addresses: rotation, lanes, and how the tokens and heads go to items
 // (false where there are too many items for the kernels' 31 bits)
 bool shape_of_launch(HeadArgs &a, const ocn_rotation *r, int64_t d, int jobs) {
@@ -640,7 +608,9 @@ bool shape_of_launch(HeadArgs &a, const ocn_rotation *r, int64_t d, int jobs) {
     a.pos = (const char *)r->positions->base + r->positions->offset;
     a.pos_wide = r->positions->dtype == OCN_INT64;
     a.freq = (const char *)r->frequencies->base + r->frequencies->offset;
-    a.freq_stride = r->frequencies->stride[0];
+    a.axes = rotation_axes(r);
+    a.freq_stride = r->frequencies->stride[r->frequencies->ndim - 1];
+    if (a.axes > 1) a.pos_axis = r->positions->stride[0], a.freq_axis = r->frequencies->stride[0];
   }
   // Rows of an item: up to kPasses passes of the workgroup's lanes share the cosines, fewer where that leaves CUs without work.
   const int rows = kBlock >> a.lanes_log2;
@@ -746,7 +716,8 @@ int run_rows(bool norm, const ocn_tensor *const *x, const ocn_tensor *const *w, 
   if ((rc = check_operands(ops, n)) != OCN_OK) return rc;
   HeadArgs a;
   std::memset(&a, 0, sizeof a);
-  const ocn_tensor *with[5] = {x[0], out[0], jobs > 1 ? x[1] : nullptr, jobs > 1 ? out[1] : nullptr, r ? r->positions : nullptr};
+  const ocn_tensor of_axis = one_axis(r);
+  const ocn_tensor *with[5] = {x[0], out[0], jobs > 1 ? x[1] : nullptr, jobs > 1 ? out[1] : nullptr, r ? &of_axis : nullptr};
   const int inner[5] = {2, 2, 2, 2, 0};
   int64_t strides[5][kMaxLead];
   if (jobs > 1) {
@@ -821,7 +792,8 @@ int run_cache(const ocn_tensor *k, const ocn_tensor *v, const ocn_rotation *r, c
   if ((rc = check_operands(ops, n)) != OCN_OK) return rc;
   HeadArgs a;
   std::memset(&a, 0, sizeof a);
-  const ocn_tensor *with[4] = {k, v, slots, r ? r->positions : nullptr};
+  const ocn_tensor of_axis = one_axis(r);
+  const ocn_tensor *with[4] = {k, v, slots, r ? &of_axis : nullptr};
   const int inner[4] = {2, 2, 0, 0};
   int64_t strides[4][kMaxLead];
   if ((rc = merge_lead(first, 2, with, inner, 4, &a.lead, strides)) != OCN_OK) return rc;
@@ -925,7 +897,8 @@ int ocn_norm_rotary_grad(const ocn_tensor *q_gout, const ocn_tensor *q, const oc
   if ((rc = check_operands(ops, n)) != OCN_OK) return rc;
   HeadArgs a;
   std::memset(&a, 0, sizeof a);
-  const ocn_tensor *with[7] = {x[0], g[0], out[0], x[1], g[1], out[1], rotation ? rotation->positions : nullptr};
+  const ocn_tensor of_axis = one_axis(rotation);
+  const ocn_tensor *with[7] = {x[0], g[0], out[0], x[1], g[1], out[1], rotation ? &of_axis : nullptr};
   const int inner[7] = {2, 2, 2, 2, 2, 2, 0};
   int64_t strides[7][kMaxLead];
   if (k) {

@@ -48,5 +48,6 @@ inline bool cache_channels(int64_t d) { return d == 64 || d == 128 || d == 256; 
 int check_cache(const ocn_tensor *cache, int64_t channels, int64_t heads, int64_t *page);
 
 int check_rotation(const ocn_rotation *r, int64_t channels, int32_t device);
+inline int rotation_axes(const ocn_rotation *r) { return r->frequencies->ndim == 1 ? 1 : (int)r->frequencies->size[0]; }
 
 }  // namespace ocn
