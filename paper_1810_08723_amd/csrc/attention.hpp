@@ -62,7 +62,7 @@ bool set_key_blocks(AttentionArgs &a, const AttentionSizes &s, int64_t keys);
 
 // What the shapes alone decide of a call: whether rows are few (the wavefronts of a workgroup then share them and take keys in turn), rows of a block, the parts that a
 // sequence's keys go to, units.
-constexpr int kRowWaves = 4, kFewWaves = 4;
+constexpr int kRowWaves = 8, kFewWaves = 4;
 constexpr int kLeastTiles = 2 * kFewWaves;        // tiles of keys of a part, at least
 struct AttentionPlan { bool few; int rows, splits; int64_t units; };
 int run_attention_half(AttentionArgs &a, const AttentionPlan &p, bool vec, void *stream);

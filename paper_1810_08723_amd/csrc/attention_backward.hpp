@@ -24,6 +24,7 @@ template <class T> constexpr float kWeightTop = std::is_same<T, f16>::value ? 12
 template <class T, bool VEC> __global__ __launch_bounds__(kBlock) void attention_along_kernel(const AttentionArgs a, uint32_t rows, FastDiv heads, FastDiv queries, f32x2 *stats) {
   constexpr int LANES = 16, EACH = 16 / (int)sizeof(T);        // of a row; channels of a piece
   const int lane = threadIdx.x % LANES;
+  if (blockIdx.x == 0 && threadIdx.x == 0) stats[rows] = f32x2{-__builtin_inff(), 0.0f};      // (of a row that is none)
   for (uint32_t r = blockIdx.x * (kBlock / LANES) + threadIdx.x / LANES; r < rows; r += gridDim.x * (kBlock / LANES)) {
     const uint32_t t = fast_quotient(r, heads), h = r - t * heads.d, b = fast_quotient(t, queries);
     const int64_t token = t - b * queries.d;
@@ -68,15 +69,10 @@ template <class T> struct Range {
   __device__ __forceinline__ float back() const { return !kNeeded ? 1.0f : factor > 0.0f ? 1.0f / factor : 0.0f; }
 };
 
-// p (times 2^kWeightTop) and s of a tile, out of scores and gout v.  `best` and `along`: of the elements' rows
-template <class T, class Row> __device__ __forceinline__ void weights_of(acc_t<T> &p, acc_t<T> &s, float scale, const Row &row) {
-#pragma unroll
-  for (int i = 0; i < Tile<T>::kOwn; ++i) {
-    const f32x2 r = row(i);
-    // (above the row's sum by rounding alone, but of scores of any size)
-    p[i] = __builtin_amdgcn_exp2f(fminf(__builtin_fmaf(p[i], scale, r.x), kWeightTop<T>));
-    s[i] = p[i] * (s[i] - r.y);
-  }
+// A weight from its exponent: above its row's sum by rounding alone, but of scores of any size.  (Up to 1 the instruction itself holds it to that.)
+template <class T> __device__ __forceinline__ float weight(float x) {
+  if constexpr (kWeightTop<T> > 0.0f) return __builtin_amdgcn_exp2f(fminf(x, kWeightTop<T>));
+  return __builtin_amdgcn_fmed3f(__builtin_amdgcn_exp2f(x), 0.0f, 1.0f);
 }
 
 // s as fragments: times the column's factor
@@ -146,113 +142,109 @@ template <class T> __device__ __forceinline__ acc_t<T> no_sum() {
   return a;
 }
 
-// Two tensors' rows on their way into LDS
-template <class T, int D, int ROWS, int LANES> struct Pair {
-  static constexpr int kAll = ROWS * Held<T, D>::kPieces, kEach = (kAll + LANES - 1) / LANES;
-  u32x4 x[kEach], y[kEach];
-  // place(row, &x's row, &y's row): false where there is none
-  template <bool VEC, class Place> __device__ __forceinline__ void load(const Place &place, int64_t x_step, int64_t y_step, int d, int lane) {
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const int at = i * LANES + lane, row = at / Held<T, D>::kPieces, e = at % Held<T, D>::kPieces * (16 / (int)sizeof(T));
-      const char *px, *py;
-      const bool in = place(row, &px, &py) && (kAll % LANES == 0 || at < kAll);
-      x[i] = load_piece<T, VEC>(px, x_step, e, in ? d : 0);
-      y[i] = load_piece<T, VEC>(py, y_step, e, in ? d : 0);
-    }
-  }
-  __device__ __forceinline__ void store(char *hx, char *hy, int lane) const {
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const int at = i * LANES + lane;
-      if (kAll % LANES != 0 && at >= kAll) continue;
-      const int to = Held<T, D>::at(at / Held<T, D>::kPieces, at % Held<T, D>::kPieces);
-      *(u32x4 *)(hx + to) = x[i];
-      *(u32x4 *)(hy + to) = y[i];
-    }
-  }
-};
+// Gradients of keys and values: a wavefront has a tile's side of keys, in registers, with the sums for them (values, where registers are short, lie in LDS); rows go through
+// LDS, the next ones on their way: some whole queries with the query heads of the group, or some of those.
+template <int D> constexpr bool kValuesHeld = D > 64;
 
-// Gradients of keys and values: a wavefront has a tile's side of keys, in registers, with the sums for them; rows go through LDS, the next ones on their way.
-template <class T, int D, bool VEC, int WAVES> __global__ __launch_bounds__(WAVES *kWave) void attention_keys_kernel(const AttentionArgs a, uint32_t first_block, const f32x2 *stats) {
+template <class T, int D, bool VEC, int WAVES>
+__global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kWavesAtOnce<T, D>))) void attention_keys_kernel(const AttentionArgs a, uint32_t first_block, const f32x2 *stats, const f32x2 *no_row) {
   warm_arguments<AttentionArgs>();
-  constexpr int SIDE = Tile<T>::kSide, PITCH = Held<T, D>::kPitch, OWN = Tile<T>::kOwn;
+  constexpr int SIDE = Tile<T>::kSide, PITCH = Held<T, D>::kPitch, OWN = Tile<T>::kOwn, BLOCK = WAVES * SIDE;
+  constexpr bool HELD = kValuesHeld<D>;
   __shared__ __align__(16) char held[2 * 2 * SIDE * PITCH];      // [2][q, gout][SIDE][PITCH]
-  __shared__ __align__(16) f32x2 of_row[2][SIDE];
-  __shared__ __align__(16) int ends[2][SIDE];                    // keys before which a row sees
+  __shared__ __align__(16) char values[HELD ? BLOCK * PITCH : 16];
+  __shared__ __align__(16) f32x2 of_row[2][kWave / 2];
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, n = lane & (SIDE - 1), h = lane / SIDE;
   Work w;
   if (!find_work_of<true>(a, first_block + blockIdx.x, &w)) return;
-  const int block = (int)(w.block * (uint32_t)(WAVES * SIDE)), key = block + wave * SIDE + n;
+  const int block = (int)(w.block * (uint32_t)BLOCK), key = block + wave * SIDE + n, end = block + BLOCK < w.k.count ? block + BLOCK : w.k.count;
   const bool mine = key < w.k.count;
   const int64_t token = w.k.first + (mine ? key : 0);
-  frag_t<T> k[D / 16], v[D / 16];
+  if (VEC && a.channels < D) {
+    clear_lds<WAVES * kWave>(held, sizeof held);
+    if (HELD) clear_lds<WAVES * kWave>(values, sizeof values);
+    __syncthreads();
+  }
+  // queries that see some key of the workgroup's; query i sees the keys before i - ahead + 1
+  const int ahead = w.q.count - w.k.count;
+  int lo = 0, hi = w.q.count;
+  if (a.causal) {
+    lo = block + ahead > 0 ? block + ahead : 0;
+    if (a.window && (int64_t)end - 1 + a.window + ahead < hi) hi = end - 1 + a.window + ahead;
+  }
+  const int across = (a.per_kv + a.heads - 1) / a.heads;         // tiles that a query's heads take
+  const int64_t head = (int64_t)w.kv * a.per_kv, heads = (int64_t)a.kv * a.per_kv;
+  const char *const pq = a.q.base + w.sequence * a.q.batch + w.q.first * a.q.token + head * a.q.head;
+  const char *const pg = a.gout.base + w.sequence * a.gout.batch + w.q.first * a.gout.token + head * a.gout.head;
+  const f32x2 *const ps = stats + (w.sequence * (a.q_starts.p ? 0 : a.q_starts.all) + w.q.first) * heads + head;
+  Carrier<T, D, SIDE, WAVES, VEC> cq, cg;
+  const auto load = [&](int at, int part, int turn) {
+    char *const q = held + turn * 2 * SIDE * PITCH;
+    const int last = hi - 1 - at, past = a.per_kv - 1 - part * a.heads;
+    const auto row = [&](const HeadView &x, const char *p, int i) {       // (rows that are none are some other one)
+      asm("" : "+v"(i));         // (nor is this)
+      int t = (int)fast_quotient((uint32_t)i, a.heads_div), g = i - t * a.heads;
+      t = t < last ? t : last, g = g < past ? g : past;
+      return p + (int64_t)(at + t) * x.token + (int64_t)(part * a.heads + g) * x.head;
+    };
+    cq.load(q, [&](int i) { return row(a.q, pq, i); }, a.q.channel, a.channels);
+    cg.load(q + SIDE * PITCH, [&](int i) { return row(a.gout, pg, i); }, a.gout.channel, a.channels);
+    if (wave == 0) {      // what the rows have in stats: a word of each lane
+      int i = lane / 2;
+      asm("" : "+v"(i));
+      const int t = (int)fast_quotient((uint32_t)i, a.heads_div), g = i - t * a.heads;
+      const f32x2 *from = i < SIDE && t < a.tokens && t <= last && g <= past ? ps + (int64_t)(at + t) * heads + part * a.heads + g : no_row;
+      load_word_to_lds(__builtin_amdgcn_readfirstlane(lds_address((const char *)of_row[turn])), (const char *)from + (lane & 1) * 4);
+    }
+  };
+  const auto store = [&](int turn) {
+    cq.store(held + turn * 2 * SIDE * PITCH);
+    cg.store(held + (turn * 2 + 1) * SIDE * PITCH);
+  };
+  int at = lo, part = 0, turn = 0;
+  if constexpr (HELD) {
+    Carrier<T, D, BLOCK, WAVES, VEC> cv;
+    const char *const pv = a.v.base + w.sequence * a.v.batch + w.k.first * a.v.token + (int64_t)w.kv * a.v.head;
+    cv.load(values, [&](int i) { return pv + (int64_t)(block + i < end ? block + i : end - 1) * a.v.token; }, a.v.channel, a.channels);
+    cv.store(values);
+  }
+  if (at < hi) load(at, 0, 0);
+  frag_t<T> k[D / 16], v[HELD ? 1 : D / 16];
   load_fragments<T, D, VEC>(k, a.k.base + w.sequence * a.k.batch + token * a.k.token + w.kv * a.k.head, a.k.channel, mine && !a.nothing ? a.channels : 0, h, a.negative);
-  load_fragments<T, D, VEC>(v, a.v.base + w.sequence * a.v.batch + token * a.v.token + w.kv * a.v.head, a.v.channel, mine ? a.channels : 0, h, false);
+  if constexpr (!HELD)
+    load_fragments<T, D, VEC>(v, a.v.base + w.sequence * a.v.batch + token * a.v.token + w.kv * a.v.head, a.v.channel, mine ? a.channels : 0, h, false);
   acc_t<T> gk[D / SIDE], gv[D / SIDE];
 #pragma unroll
   for (int ct = 0; ct < D / SIDE; ++ct) gk[ct] = gv[ct] = no_sum<T>();
   Range<T> range;
-  // queries that see some key of the workgroup's
-  const int last = block + WAVES * SIDE < w.k.count ? block + WAVES * SIDE - 1 : w.k.count - 1, ahead = w.q.count - w.k.count;
-  int lo = 0, hi = w.q.count;
-  if (a.causal) {
-    lo = block + ahead > 0 ? block + ahead : 0;
-    if (a.window && (int64_t)last + a.window + ahead < hi) hi = last + a.window + ahead;
-  }
-  const uint32_t begin = (uint32_t)lo * (uint32_t)a.per_kv, end = hi > lo ? (uint32_t)hi * (uint32_t)a.per_kv : begin;
-  const int64_t head = (int64_t)w.kv * a.per_kv;
-  const char *const pq = a.q.base + w.sequence * a.q.batch + w.q.first * a.q.token + head * a.q.head;
-  const char *const pg = a.gout.base + w.sequence * a.gout.batch + w.q.first * a.gout.token + head * a.gout.head;
-  const f32x2 *const ps = stats + (w.sequence * (a.q_starts.p ? 0 : a.q_starts.all) + w.q.first) * ((int64_t)a.kv * a.per_kv) + head;
-  Pair<T, D, SIDE, WAVES * kWave> next;
-  f32x2 next_stat;
-  int next_end;
-  const auto load = [&](uint32_t at) {
-    next.template load<VEC>(
-        [&](int row, const char **x, const char **y) {
-          const uint32_t r = at + row < end ? at + row : end - 1, query = fast_quotient(r, a.heads_div), g = r - query * a.heads_div.d;
-          *x = pq + (int64_t)query * a.q.token + (int64_t)g * a.q.head;
-          *y = pg + (int64_t)query * a.gout.token + (int64_t)g * a.gout.head;
-          return at + row < end;
-        },
-        a.q.channel, a.gout.channel, a.channels, threadIdx.x);
-    if (threadIdx.x < SIDE) {
-      const uint32_t r = at + threadIdx.x < end ? at + threadIdx.x : end - 1, query = fast_quotient(r, a.heads_div), g = r - query * a.heads_div.d;
-      next_stat = at + threadIdx.x < end ? ps[(int64_t)query * ((int64_t)a.kv * a.per_kv) + g] : f32x2{-__builtin_inff(), 0.0f};
-      next_end = a.causal ? (int)query - ahead + 1 : w.k.count;
-    }
-  };
-  const auto store = [&](int turn) {
-    next.store(held + turn * 2 * SIDE * PITCH, held + (turn * 2 + 1) * SIDE * PITCH, threadIdx.x);
-    if (threadIdx.x < SIDE) of_row[turn][threadIdx.x] = next_stat, ends[turn][threadIdx.x] = next_end;
-  };
-  int turn = 0;
-  if (begin < end) {
-    load(begin);
-    store(0);
+  if (at < hi) store(0);
+  const int from = block + wave * SIDE;
+  const auto step = [&](auto masked) {
+    arrived();
     __syncthreads();
-  }
-  for (uint32_t at = begin; at < end; at += SIDE, turn ^= 1) {
-    const bool more = end - at > SIDE;
-    if (more) load(at + SIDE);
     const char *const q = held + turn * 2 * SIDE * PITCH, *const g = q + SIDE * PITCH;
-    // the keys that the first and the last of these rows see up to
-    const int first_end = ends[turn][0], last_end = ends[turn][SIDE - 1], from = block + wave * SIDE;
-    const bool some = from < last_end && (!a.window || from + SIDE > first_end - a.window);
-    if (some) {
+    const int first_end = at - ahead + 1, last_end = first_end + a.tokens - 1;
+    int next = at, next_part = part + 1;
+    if (next_part == across) next += a.tokens, next_part = 0;
+    if (next < hi) load(next, next_part, turn ^ 1);
+    if (!masked || (from < last_end && (!a.window || from + SIDE > first_end - a.window))) {
+      int here = h;
+      asm("" : "+v"(here));      // (what hangs on it is not kept in registers from tile to tile)
       acc_t<T> p = no_sum<T>(), s[1] = {no_sum<T>()};
 #pragma unroll
-      for (int c = 0; c < D / 16; ++c) p = product(rows_fragment<T, D>(q, 0, c, n, h), k[c], p);
+      for (int c = 0; c < D / 16; ++c) {
+        p = product(rows_fragment<T, D>(q, 0, c, n, h), k[c], p);
+        s[0] = product(rows_fragment<T, D>(g, 0, c, n, h), HELD ? rows_fragment<T, D>(values, wave * SIDE, c, n, h) : v[HELD ? 0 : c], s[0]);
+      }
 #pragma unroll
-      for (int c = 0; c < D / 16; ++c) s[0] = product(rows_fragment<T, D>(g, 0, c, n, h), v[c], s[0]);
-      weights_of<T>(p, s[0], a.scale, [&](int i) { return of_row[turn][own_index<T>(i) + 4 * h]; });
-      if (from + SIDE > first_end || (a.window && from < last_end - a.window)) {
-#pragma unroll
-        for (int i = 0; i < OWN; ++i) {
-          const int e = ends[turn][own_index<T>(i) + 4 * h];
-          if (key >= e || (a.window && key < e - a.window)) p[i] = s[0][i] = 0.0f;
+      for (int i = 0; i < OWN; ++i) {
+        const f32x2 r = of_row[turn][own_index<T>(i) + 4 * h];
+        p[i] = weight<T>(__builtin_fmaf(p[i], a.scale, r.x));
+        if constexpr (masked) {
+          const int e = first_end + (int)fast_quotient((uint32_t)(own_index<T>(i) + 4 * here), a.heads_div);
+          if (key >= e || (a.window && key < e - a.window)) p[i] = 0.0f;
         }
+        s[0][i] = p[i] * (s[0][i] - r.y);
       }
 #pragma unroll
       for (int x = 0; x < Tile<T>::kSteps; ++x) {
@@ -268,8 +260,14 @@ template <class T, int D, bool VEC, int WAVES> __global__ __launch_bounds__(WAVE
         for (int ct = 0; ct < D / SIDE; ++ct) gk[ct] = product(columns_fragment<T, D>(q, 16 * x, ct, lane), f, gk[ct]);
       }
     }
-    if (more) store(turn ^ 1);
-    __syncthreads();
+    if (next < hi) store(turn ^ 1);
+    at = next, part = next_part, turn ^= 1;
+  };
+  // Rows that see all of the workgroup's keys have a loop of their own
+  const int first_whole = a.causal ? end - 1 + ahead : lo, past_whole = a.window ? block + a.window + ahead : 0x7fffffff;      // (rows past the last have no weights)
+  while (at < hi) {
+    while (at < hi && at >= first_whole && at <= past_whole - a.tokens) step(std::false_type());
+    if (at < hi) step(std::true_type());
   }
   if (!mine) return;
   const float weight = kWeightTop<T> > 0.0f ? 0x1p-12f : 1.0f;
@@ -278,62 +276,111 @@ template <class T, int D, bool VEC, int WAVES> __global__ __launch_bounds__(WAVE
 }
 
 // Gradients of queries: a wavefront has a tile's side of rows, in registers, with the sums for them; keys and values go through LDS.
-template <class T, int D, bool VEC, int WAVES> __global__ __launch_bounds__(WAVES *kWave) void attention_queries_kernel(const AttentionArgs a, uint32_t first_block, const f32x2 *stats) {
+//
+// gout * out, from the rounded out, is off by as much as out is.  Against the differences gout v - gout out that is little where a row sees many keys, but where it sees few it is as large as
+// the rounding of the results.  Rows of workgroups that see kFewKeys keys at most sum p (gout v) instead, in a pass over the keys of its own, and leave it in stats for the pass over keys.
+constexpr int kFewKeys = 256;
+
+template <class T, int D, bool VEC, int WAVES, int KEYS>
+__global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kWavesAtOnce<T, D>))) void attention_queries_kernel(const AttentionArgs a, uint32_t first_block, f32x2 *stats) {
   warm_arguments<AttentionArgs>();
   constexpr int SIDE = Tile<T>::kSide, PITCH = Held<T, D>::kPitch, OWN = Tile<T>::kOwn;
-  __shared__ __align__(16) char held[2 * 2 * SIDE * PITCH];      // [2][keys, values][SIDE][PITCH]
+  __shared__ __align__(16) char held[2 * 2 * KEYS * PITCH];      // [2][keys, values][KEYS][PITCH]
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, n = lane & (SIDE - 1), h = lane / SIDE;
   Work w;
   if (!find_work(a, first_block + blockIdx.x, &w)) return;
+  const Limits all = limits_of_block(a, w), whole = limits_of_all(a, w);
+  const bool few = all.hi - all.lo <= kFewKeys;
+  if (!a.gq.base && !few) return;
   const RowPlace place = row_place(a, w, wave * SIDE + n);
-  const Limits own = limits_of(a, w, place.query), all = limits_of_block(a, w);
+  const Limits own = limits_of(a, w, place.query);
   const int64_t token = w.q.first + place.query, head = (int64_t)w.kv * a.per_kv + place.head;
+  const char *pk = a.k.base + w.sequence * a.k.batch + w.k.first * a.k.token + (int64_t)w.kv * a.k.head, *pv = a.v.base + w.sequence * a.v.batch + w.k.first * a.v.token + (int64_t)w.kv * a.v.head;
+  if (VEC && a.channels < D) {
+    clear_lds<WAVES * kWave>(held, sizeof held);
+    __syncthreads();
+  }
+  Carrier<T, D, KEYS, WAVES, VEC> ck, cv;
+  const auto load = [&](int at, int turn) {
+    char *const k = held + turn * 2 * KEYS * PITCH;
+    const int last = w.k.count - 1 - at;        // (rows past the end are the last one again)
+    ck.load(k, [&](int i) { return pk + (int64_t)(at + (i < last ? i : last)) * a.k.token; }, a.k.channel, a.channels);
+    cv.load(k + KEYS * PITCH, [&](int i) { return pv + (int64_t)(at + (i < last ? i : last)) * a.v.token; }, a.v.channel, a.channels);
+  };
+  const auto store = [&](int turn) {
+    ck.store(held + turn * 2 * KEYS * PITCH);
+    cv.store(held + (turn * 2 + 1) * KEYS * PITCH);
+  };
+  int at = all.lo / KEYS * KEYS, turn = 0;
+  if (at < all.hi) load(at, 0);
   frag_t<T> q[D / 16], g[D / 16];
   load_fragments<T, D, VEC>(q, a.q.base + w.sequence * a.q.batch + token * a.q.token + head * a.q.head, a.q.channel, place.in && !a.nothing ? a.channels : 0, h, a.negative);
   load_fragments<T, D, VEC>(g, a.gout.base + w.sequence * a.gout.batch + token * a.gout.token + head * a.gout.head, a.gout.channel, place.in ? a.channels : 0, h, false);
-  const f32x2 stat = stats[(w.sequence * (a.q_starts.p ? 0 : a.q_starts.all) + token) * ((int64_t)a.kv * a.per_kv) + head];
+  f32x2 *const stat_at = stats + (w.sequence * (a.q_starts.p ? 0 : a.q_starts.all) + token) * ((int64_t)a.kv * a.per_kv) + head;
+  f32x2 stat = *stat_at;
+  const int hi_last = __builtin_amdgcn_readlane(own.hi, SIDE - 1), lo_first = __builtin_amdgcn_readfirstlane(own.lo);
+  if (at < all.hi) store(0);
+  // scores and gout v of a tile, and the weights
+  const auto weights = [&](const char *k, const char *v, int first, acc_t<T> &p, acc_t<T> &s, auto masked) {
+    p = s = no_sum<T>();
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) {
+      p = product(rows_fragment<T, D>(k, 0, c, n, h), q[c], p);
+      s = product(rows_fragment<T, D>(v, 0, c, n, h), g[c], s);
+    }
+    const int lo = own.lo - first - 4 * h, hi = own.hi - first - 4 * h;
+#pragma unroll
+    for (int i = 0; i < OWN; ++i) {
+      p[i] = weight<T>(__builtin_fmaf(p[i], a.scale, stat.x));
+      if (masked && (own_index<T>(i) < lo || own_index<T>(i) >= hi)) p[i] = 0.0f;
+    }
+  };
+  if (few) {
+    float sum = 0.0f;
+    for (; at < all.hi; at += KEYS, turn ^= 1) {
+      arrived();
+      __syncthreads();
+      const char *const k = held + turn * 2 * KEYS * PITCH, *const v = k + KEYS * PITCH;
+      const bool more = at + KEYS < all.hi;
+      if (more) load(at + KEYS, turn ^ 1);
+#pragma nounroll
+      for (int t = 0; t < KEYS; t += SIDE) {
+        if (at + t >= hi_last || at + t + SIDE <= lo_first) continue;
+        acc_t<T> p, s;
+        weights(k + t * PITCH, v + t * PITCH, at + t, p, s, std::true_type());
+#pragma unroll
+        for (int i = 0; i < OWN; ++i) sum = __builtin_fmaf(p[i], p[i] > 0.0f ? s[i] : 0.0f, sum);
+      }
+      if (more) store(turn ^ 1);
+    }
+    stat.y = column_sum<T>(sum) * (kWeightTop<T> > 0.0f ? 0x1p-12f : 1.0f);
+    if (place.in && lane < SIDE) *stat_at = stat;
+    if (!a.gq.base) return;
+    __syncthreads();
+    at = all.lo / KEYS * KEYS, turn = 0;
+    if (at < all.hi) {
+      load(at, 0);
+      store(0);
+    }
+  }
   acc_t<T> gq[D / SIDE];
 #pragma unroll
   for (int ct = 0; ct < D / SIDE; ++ct) gq[ct] = no_sum<T>();
   Range<T> range;
-  const int hi_first = __builtin_amdgcn_readfirstlane(own.hi), hi_last = __builtin_amdgcn_readlane(own.hi, SIDE - 1), lo_first = __builtin_amdgcn_readfirstlane(own.lo),
-            lo_last = __builtin_amdgcn_readlane(own.lo, SIDE - 1);
-  const char *pk = a.k.base + w.sequence * a.k.batch + w.k.first * a.k.token + (int64_t)w.kv * a.k.head, *pv = a.v.base + w.sequence * a.v.batch + w.k.first * a.v.token + (int64_t)w.kv * a.v.head;
-  Pair<T, D, SIDE, WAVES * kWave> next;
-  const auto load = [&](int at) {
-    next.template load<VEC>(
-        [&](int row, const char **x, const char **y) {
-          const bool in = at + row < w.k.count;
-          *x = pk + (int64_t)(in ? at + row : 0) * a.k.token;
-          *y = pv + (int64_t)(in ? at + row : 0) * a.v.token;
-          return in;
-        },
-        a.k.channel, a.v.channel, a.channels, threadIdx.x);
-  };
-  int at = all.lo / SIDE * SIDE, turn = 0;
-  if (at < all.hi) {
-    load(at);
-    next.store(held, held + SIDE * PITCH, threadIdx.x);
+  const auto step = [&](auto masked) {
+    arrived();
     __syncthreads();
-  }
-  for (; at < all.hi; at += SIDE, turn ^= 1) {
-    const bool more = at + SIDE < all.hi;
-    if (more) load(at + SIDE);
-    const char *const k = held + turn * 2 * SIDE * PITCH, *const v = k + SIDE * PITCH;
-    if (at < hi_last && at + SIDE > lo_first) {
-      acc_t<T> p = no_sum<T>(), s[1] = {no_sum<T>()};
+    const char *const keys = held + turn * 2 * KEYS * PITCH, *const values = keys + KEYS * PITCH;
+    const bool more = at + KEYS < all.hi;
+    if (more) load(at + KEYS, turn ^ 1);
 #pragma unroll
-      for (int c = 0; c < D / 16; ++c) p = product(rows_fragment<T, D>(k, 0, c, n, h), q[c], p);
+    for (int t = 0; t < KEYS; t += SIDE) {
+      const char *const k = keys + t * PITCH, *const v = values + t * PITCH;
+      if (masked && (at + t >= hi_last || at + t + SIDE <= lo_first)) continue;
+      acc_t<T> p, s[1];
+      weights(k, v, at + t, p, s[0], masked);
 #pragma unroll
-      for (int c = 0; c < D / 16; ++c) s[0] = product(rows_fragment<T, D>(v, 0, c, n, h), g[c], s[0]);
-      weights_of<T>(p, s[0], a.scale, [&](int) { return stat; });
-      if (at + SIDE > hi_first || at < lo_last) {
-#pragma unroll
-        for (int i = 0; i < OWN; ++i) {
-          const int j = at + own_index<T>(i) + 4 * h;
-          if (j < own.lo || j >= own.hi) s[0][i] = 0.0f;
-        }
-      }
+      for (int i = 0; i < OWN; ++i) s[0][i] = p[i] * (s[0][i] - stat.y);
       in_range<T, 1>(s, range, gq, D / SIDE);
 #pragma unroll
       for (int x = 0; x < Tile<T>::kSteps; ++x) {
@@ -342,8 +389,12 @@ template <class T, int D, bool VEC, int WAVES> __global__ __launch_bounds__(WAVE
         for (int ct = 0; ct < D / SIDE; ++ct) gq[ct] = product(columns_fragment<T, D>(k, 16 * x, ct, lane), f, gq[ct]);
       }
     }
-    if (more) next.store(held + (turn ^ 1) * 2 * SIDE * PITCH, held + ((turn ^ 1) * 2 + 1) * SIDE * PITCH, threadIdx.x);
-    __syncthreads();
+    if (more) store(turn ^ 1);
+    at += KEYS, turn ^= 1;
+  };
+  while (at < all.hi) {
+    while (at >= whole.lo && at + KEYS <= whole.hi) step(std::false_type());
+    if (at < all.hi) step(std::true_type());
   }
   if (!place.in) return;
   const float weight = kWeightTop<T> > 0.0f ? 0x1p-12f : 1.0f;
@@ -353,6 +404,10 @@ template <class T, int D, bool VEC, int WAVES> __global__ __launch_bounds__(WAVE
 // ---------------------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------------------
+
+// (of the pass over rows; with four of 96 or 128 channels what a lane loads of a tile and keeps for it takes more registers than there are)
+template <class T, int D> constexpr int kKeyWaves = sizeof(T) == 2 && (D == 96 || D == 128) ? 8 : 4;
+template <class T> constexpr int kGradKeys = sizeof(T) == 2 ? 64 : 32;
 
 template <class Launch> int in_launches(int64_t blocks, Launch launch) {
   for (int64_t at = 0; at < blocks; at += max_launch_blocks()) {
@@ -367,29 +422,34 @@ template <class Launch> int in_launches(int64_t blocks, Launch launch) {
 }
 
 template <class T, int D, bool VEC> int run_grad(AttentionArgs &a, const AttentionSizes &sizes, const AttentionGrad &p, f32x2 *stats, hipStream_t stream) {
-  const int side = Tile<T>::kSide;
+  constexpr int side = Tile<T>::kSide;
   int rc = OCN_OK;
   const uint32_t rows = (uint32_t)p.rows;
-  if (rows) {
+  {
     const FastDiv heads = make_fastdiv((uint32_t)(a.kv * a.per_kv)), queries = make_fastdiv((uint32_t)std::max<int64_t>(1, sizes.packed ? sizes.queries : a.q_starts.all));
-    hipLaunchKernelGGL((attention_along_kernel<T, VEC>), dim3(std::min<uint32_t>((rows + 15) / 16, 8192)), dim3(kBlock), 0, stream, a, rows, heads, queries, stats);
+    hipLaunchKernelGGL((attention_along_kernel<T, VEC>), dim3(std::max(1u, std::min((rows + 15) / 16, 8192u))), dim3(kBlock), 0, stream, a, rows, heads, queries, stats);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) {
       record_hip_error((int)e);
       return OCN_ERR_LAUNCH;
     }
   }
-  if (p.keys) {
-    if (!set_key_blocks(a, sizes, side * kGradWaves)) return OCN_ERR_SHAPE;
-    rc = in_launches(key_units_of(sizes, side * kGradWaves), [&](uint32_t grid, uint32_t first) {
-      hipLaunchKernelGGL((attention_keys_kernel<T, D, VEC, kGradWaves>), dim3(grid), dim3(kGradWaves * kWave), 0, stream, a, first, stats);
+  if (rows) {
+    if (!set_blocks(a, sizes, side * kGradWaves, 1)) return OCN_ERR_SHAPE;
+    rc = in_launches(units_of(sizes, side * kGradWaves), [&](uint32_t grid, uint32_t first) {
+      hipLaunchKernelGGL((attention_queries_kernel<T, D, VEC, kGradWaves, kGradKeys<T>>), dim3(grid), dim3(kGradWaves * kWave), 0, stream, a, first, stats);
     });
     if (rc != OCN_OK) return rc;
   }
-  if (p.queries) {
-    if (!set_blocks(a, sizes, side * kGradWaves, 1)) return OCN_ERR_SHAPE;
-    rc = in_launches(units_of(sizes, side * kGradWaves), [&](uint32_t grid, uint32_t first) {
-      hipLaunchKernelGGL((attention_queries_kernel<T, D, VEC, kGradWaves>), dim3(grid), dim3(kGradWaves * kWave), 0, stream, a, first, stats);
+  if (p.keys) {
+    constexpr int waves = kKeyWaves<T, D>;
+    if (!set_key_blocks(a, sizes, side * waves)) return OCN_ERR_SHAPE;
+    // (rows of a tile: whole queries with the heads of the group, or some of those)
+    a.heads = std::max(1, std::min(a.per_kv, side));
+    a.heads_div = make_fastdiv((uint32_t)a.heads);
+    a.tokens = side / a.heads;
+    rc = in_launches(key_units_of(sizes, side * waves), [&](uint32_t grid, uint32_t first) {
+      hipLaunchKernelGGL((attention_keys_kernel<T, D, VEC, waves>), dim3(grid), dim3(waves * kWave), 0, stream, a, first, stats, stats + rows);
     });
   }
   return rc;

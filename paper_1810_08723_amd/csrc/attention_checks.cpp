@@ -242,10 +242,13 @@ int ocn_attention(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *v,
   }
 }
 
+// two numbers of each row, and of a row that is none
+static size_t grad_bytes(const AttentionSizes &s) { return (size_t)(s.queries * s.kv * s.per_kv + 1) * 2 * sizeof(float); }
+
 size_t ocn_attention_grad_workspace_bytes(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *q_starts) {
   if (check_attention_sizes(q, k, q_starts) != OCN_OK) return 0;
   const AttentionSizes s = sizes_of(q, k, q_starts);
-  return (size_t)(s.queries * s.kv * s.per_kv) * 2 * sizeof(float);
+  return grad_bytes(s);
 }
 
 int ocn_attention_grad(const ocn_tensor *gout, const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *v, const ocn_tensor *out, const ocn_tensor *log_sum,
@@ -266,10 +269,8 @@ int ocn_attention_grad(const ocn_tensor *gout, const ocn_tensor *q, const ocn_te
   p.rows = s.queries * s.kv * s.per_kv;
   p.keys = k_gin != nullptr && s.keys > 0;
   p.queries = q_gin != nullptr && p.rows > 0;
-  if (p.rows) {
-    if (!workspace || workspace_bytes < (size_t)p.rows * 2 * sizeof(float)) return OCN_ERR_WORKSPACE;
-    if ((uintptr_t)workspace % 256 != 0) return OCN_ERR_ALIGN;
-  }
+  if (!workspace || workspace_bytes < grad_bytes(s)) return OCN_ERR_WORKSPACE;
+  if ((uintptr_t)workspace % 256 != 0) return OCN_ERR_ALIGN;
   if (!p.keys && !p.queries) return OCN_OK;
   bool vec = whole_rows(q) && whole_rows(k) && whole_rows(v) && whole_rows(out) && whole_rows(gout);
   a.gout = view_of(gout), a.out = view_of(out), a.log_sum = view_of(log_sum, false);

@@ -12,13 +12,17 @@ namespace {
 // ---------------------------------------------------------------------------------------
 // One pass over the keys.  A wavefront has the rows of one tile; for some keys at a time it forms scores^T = K Q^T and out^T += V^T P^T, so that a lane holds scores
 // and results of one row: the row's largest score, the sum of its weights and what results are scaled by need no other lane than the one or three that share the row.
-// A score's maximum is raised, and results rescaled, only where a weight would pass 2^kRaise.  The difference of scores is formed before it is scaled, so that it is never
-// above zero by more than that, however large scores are.
+//
+// Weights are relative to a reference, the row's largest score when it was last set.  It is set by the first keys, and again, with results rescaled, only
+// where a lane's weights come to more than kMost: no maximum is looked for otherwise.  A weight is 2^(s scale - reference scale), one multiply-add and one exponential: the
+// reference's rounding is the same for all weights of a row.  Where scores are so large (kFine) that it could make weights too large, and for float,
+// the difference is formed before it is scaled.
 // ---------------------------------------------------------------------------------------
 
-constexpr float kRaise = 4.0f;
-// log2 of the weight of a row's largest score.  A half holds 2^-14 ... 2^16 without loss: weights are put near its upper end.
-template <class T> constexpr float kTop = std::is_same<T, f16>::value ? 11.0f : 0.0f;
+// log2 of the weight of a score that is the reference.  A half holds 2^-14 ... 2^16 without loss: weights are put near its upper end, 32 of a lane below kMost.
+template <class T> constexpr float kTop = std::is_same<T, f16>::value ? 9.0f : 0.0f;
+template <class T> constexpr float kMost = std::is_same<T, f16>::value ? 46341.0f : 512.0f;
+constexpr float kFine = 1024.0f;
 
 // What a wavefront has of its rows
 template <class T, int D> struct Rows {
@@ -26,6 +30,7 @@ template <class T, int D> struct Rows {
   acc_t<T> out[D / Tile<T>::kSide];
   float best, total;           // the score that weights are relative to (minus infinity: none yet), the sum of a lane's own weights
   int lo, hi;                  // keys that the row sees
+  bool exact;                  // differences of scores are formed before they are scaled
 };
 
 template <class T> __device__ __forceinline__ acc_t<T> zero_acc() {
@@ -72,7 +77,7 @@ template <class T, int D> struct SlowRow {
       }
       s = sum_over_row(s, kWave);
       float keep = 1.0f;
-      if ((s - best) * a.scale > kRaise) {
+      if ((s - best) * a.scale > 4.0f) {
         keep = best > -__builtin_inff() ? __builtin_amdgcn_exp2f((best - s) * a.scale) : 0.0f;
         best = s;
       }
@@ -87,58 +92,80 @@ template <class T, int D> struct SlowRow {
   }
 };
 
-// KEYS keys of a tile in LDS, from key `first` of the sequence on.  `masked`: some row does not see all of them; true: and values that it does not see may have reached it.
-template <class T, int D, int KEYS> __device__ __forceinline__ bool attend(Rows<T, D> &r, const char *k, const char *v, int first, bool masked, float scale, int lane) {
-  constexpr int SIDE = Tile<T>::kSide, TILES = KEYS / SIDE, OWN = Tile<T>::kOwn, STEPS = Tile<T>::kSteps;
-  const int n = lane & (SIDE - 1), h = lane / SIDE;
-  acc_t<T> s[TILES];
-#pragma unroll
-  for (int t = 0; t < TILES; ++t) {
-    s[t] = zero_acc<T>();
-#pragma unroll
-    for (int c = 0; c < D / 16; ++c) s[t] = product(rows_fragment<T, D>(k, t * SIDE, c, n, h), r.q[c], s[t]);
-  }
-  if (masked) {
+// the weights of scores, in their place, relative to the row's reference: their sum over a lane's own
+template <class T, int TILES> __device__ __forceinline__ float weigh(const acc_t<T> *s, acc_t<T> *p, float best, float scale, bool exact) {
+  float sum = 0.0f;
+  if (exact) {
 #pragma unroll
     for (int t = 0; t < TILES; ++t)
 #pragma unroll
-      for (int i = 0; i < OWN; ++i) {
-        const int j = first + t * SIDE + own_index<T>(i) + 4 * h;
-        if (j < r.lo || j >= r.hi) s[t][i] = -__builtin_inff();
-      }
+      for (int i = 0; i < Tile<T>::kOwn; ++i) p[t][i] = __builtin_fmaf(s[t][i] - best, scale, kTop<T>);
+  } else {
+    const float less = __builtin_fmaf(-best, scale, kTop<T>);
+#pragma unroll
+    for (int t = 0; t < TILES; ++t)
+#pragma unroll
+      for (int i = 0; i < Tile<T>::kOwn; ++i) p[t][i] = __builtin_fmaf(s[t][i], scale, less);
   }
-  float top = s[0][0];
 #pragma unroll
   for (int t = 0; t < TILES; ++t)
 #pragma unroll
-    for (int i = 0; i < OWN; ++i) top = fmaxf(top, s[t][i]);
-  top = column_max<T>(top);
-  if (__any((top - r.best) * scale > kRaise)) {       // (the first finite score is above minus infinity by more than that; no score at all is not)
-    const float best = fmaxf(r.best, top), keep = r.best > -__builtin_inff() ? __builtin_amdgcn_exp2f((r.best - best) * scale) : 0.0f;
-    r.best = best;
+    for (int i = 0; i < Tile<T>::kOwn; ++i) {
+      p[t][i] = __builtin_amdgcn_exp2f(p[t][i]);
+      sum += p[t][i];
+    }
+  return sum;
+}
+
+// KEYS keys of a tile in LDS, from key `first` of the sequence on.  MASKED: some row does not see all of them; true: and values that it does not see may have reached it.
+template <class T, int D, int KEYS, bool MASKED> __device__ __forceinline__ bool attend(Rows<T, D> &r, const char *k, const char *v, int first, float scale, int lane) {
+  constexpr int SIDE = Tile<T>::kSide, TILES = KEYS / SIDE, OWN = Tile<T>::kOwn, STEPS = Tile<T>::kSteps;
+  const int n = lane & (SIDE - 1), h = lane / SIDE;
+  acc_t<T> s[TILES], p[TILES];
+#pragma unroll
+  for (int t = 0; t < TILES; ++t) s[t] = zero_acc<T>();
+#pragma unroll
+  for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) s[t] = product(rows_fragment<T, D>(k, t * SIDE, c, n, h), r.q[c], s[t]);
+  if constexpr (MASKED) {
+    const int lo = r.lo - first - 4 * h, hi = r.hi - first - 4 * h;
+#pragma unroll
+    for (int t = 0; t < TILES; ++t)
+#pragma unroll
+      for (int i = 0; i < OWN; ++i)
+        if (t * SIDE + own_index<T>(i) < lo || t * SIDE + own_index<T>(i) >= hi) s[t][i] = -__builtin_inff();
+  }
+  float sum = weigh<T, TILES>(s, p, r.best, scale, r.exact);
+  // The first scores, or some far above the reference (no score at all, and NaNs, are not)
+  if (__any(!(sum <= kMost<T>))) {
+    float top = s[0][0];
+#pragma unroll
+    for (int t = 0; t < TILES; ++t)
+#pragma unroll
+      for (int i = 0; i < OWN; ++i) top = fmaxf(top, s[t][i]);
+    top = column_max<T>(top);
+    const bool before = r.best > -__builtin_inff(), now = before || top > -__builtin_inff();
+    const float best = before ? fmaxf(r.best, top) : now ? top : 0.0f, keep = before ? __builtin_amdgcn_exp2f((r.best - best) * scale) : 0.0f;
+    r.exact = r.exact || __any(!(__builtin_fabsf(best * scale) < kFine));
+    r.best = now ? best : -__builtin_inff();
     r.total *= keep;
 #pragma unroll
     for (int ct = 0; ct < D / SIDE; ++ct)
 #pragma unroll
       for (int i = 0; i < OWN; ++i) r.out[ct][i] *= keep;
+    sum = weigh<T, TILES>(s, p, best, scale, r.exact);
   }
-  const float best = r.best > -__builtin_inff() ? r.best : 0.0f;
-#pragma unroll
-  for (int t = 0; t < TILES; ++t)
-#pragma unroll
-    for (int i = 0; i < OWN; ++i) {
-      s[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i] - best, scale, kTop<T>));
-      r.total += s[t][i];
-    }
+  r.total += sum;
 #pragma unroll
   for (int t = 0; t < TILES; ++t)
 #pragma unroll
     for (int x = 0; x < STEPS; ++x) {
-      const frag_t<T> p = as_fragment<T>(s[t], x);
+      const frag_t<T> f = as_fragment<T>(p[t], x);
 #pragma unroll
-      for (int ct = 0; ct < D / SIDE; ++ct) r.out[ct] = product(columns_fragment<T, D>(v, t * SIDE + 16 * x, ct, lane), p, r.out[ct]);
+      for (int ct = 0; ct < D / SIDE; ++ct) r.out[ct] = product(columns_fragment<T, D>(v, t * SIDE + 16 * x, ct, lane), f, r.out[ct]);
     }
-  return masked && odd_values<T, D, KEYS>(v, lane);
+  return MASKED && odd_values<T, D, KEYS>(v, lane);
 }
 
 // Keys [first, first + KEYS) of a sequence on their way into LDS, by `LANES` lanes; those past the end are zero.
@@ -175,6 +202,7 @@ template <class T, int D, bool VEC> __device__ __forceinline__ void start_rows(R
   r.lo = l.lo, r.hi = l.hi;
   r.best = -__builtin_inff();
   r.total = 0.0f;
+  r.exact = std::is_same<T, float>::value;
 #pragma unroll
   for (int ct = 0; ct < D / SIDE; ++ct) r.out[ct] = zero_acc<T>();
   const char *at = q + (int64_t)p.query * a.q.token + (int64_t)p.head * a.q.head;
@@ -224,35 +252,53 @@ template <class T, int D> __device__ __forceinline__ void finish_row(const Atten
 }
 
 // Many rows: the wavefronts of a workgroup have a tile of rows each and share the keys, which go through LDS once for all of them, the next ones on their way.
-template <class T, int D, bool VEC, int WAVES, int KEYS> __global__ __launch_bounds__(WAVES *kWave) void attention_rows_kernel(const AttentionArgs a, uint32_t first_block) {
+template <class T, int D, bool VEC, int WAVES, int KEYS> __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kWavesAtOnce<T, D>))) void attention_rows_kernel(const AttentionArgs a, uint32_t first_block) {
   warm_arguments<AttentionArgs>();
   constexpr int SIDE = Tile<T>::kSide, PITCH = Held<T, D>::kPitch;
   __shared__ __align__(16) char lds[2 * 2 * KEYS * PITCH];        // [2][keys, values][KEYS][PITCH]
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
   Work w;
   if (!find_work(a, first_block + blockIdx.x, &w)) return;
+  const Limits all = limits_of_block(a, w), whole = limits_of_all(a, w);
+  const char *pk = a.k.base + w.sequence * a.k.batch + w.k.first * a.k.token + (int64_t)w.kv * a.k.head, *pv = a.v.base + w.sequence * a.v.batch + w.k.first * a.v.token + (int64_t)w.kv * a.v.head;
+  Carrier<T, D, KEYS, WAVES, VEC> ck, cv;
+  const auto load = [&](int at, int turn) {
+    char *const k = lds + turn * 2 * KEYS * PITCH;
+    const int last = w.k.count - 1 - at;        // (rows past the end are the last one again)
+    ck.load(k, [&](int i) { return pk + (int64_t)(at + (i < last ? i : last)) * a.k.token; }, a.k.channel, a.channels);
+    cv.load(k + KEYS * PITCH, [&](int i) { return pv + (int64_t)(at + (i < last ? i : last)) * a.v.token; }, a.v.channel, a.channels);
+  };
+  const auto store = [&](int turn) {
+    ck.store(lds + turn * 2 * KEYS * PITCH);
+    cv.store(lds + (turn * 2 + 1) * KEYS * PITCH);
+  };
+  int at = all.lo / KEYS * KEYS, turn = 0;
+  if (VEC && a.channels < D) {
+    clear_lds<WAVES * kWave>(lds, sizeof lds);
+    __syncthreads();
+  }
+  if (at < all.hi) load(at, 0);
   Rows<T, D> r;
   const int row = wave * SIDE + (lane & (SIDE - 1));
   start_rows<T, D, VEC>(r, a, w, row, lane, a.q.base + w.sequence * a.q.batch + w.q.first * a.q.token + (int64_t)w.kv * a.per_kv * a.q.head);
-  const char *pk = a.k.base + w.sequence * a.k.batch + w.k.first * a.k.token + (int64_t)w.kv * a.k.head, *pv = a.v.base + w.sequence * a.v.batch + w.k.first * a.v.token + (int64_t)w.kv * a.v.head;
-  const Limits all = limits_of_block(a, w);
   const int hi_first = __builtin_amdgcn_readfirstlane(r.hi), hi_last = __builtin_amdgcn_readlane(r.hi, SIDE - 1), lo_first = __builtin_amdgcn_readfirstlane(r.lo),
             lo_last = __builtin_amdgcn_readlane(r.lo, SIDE - 1);
-  Carried<T, D, VEC, KEYS, WAVES * kWave> next;
   bool odd = false;
-  int at = all.lo / KEYS * KEYS, turn = 0;
-  if (at < all.hi) {
-    next.load(a, pk, pv, at, w.k.count, threadIdx.x);
-    next.store(lds, lds + KEYS * PITCH, threadIdx.x);
+  if (at < all.hi) store(0);
+  // Tiles that all rows of the workgroup see whole have a loop of their own: what masks need takes none of its registers.
+  const auto step = [&](auto masked) {
+    arrived();
     __syncthreads();
-  }
-  for (; at < all.hi; at += KEYS, turn ^= 1) {
-    char *const k = lds + turn * 2 * KEYS * PITCH, *const other = lds + (turn ^ 1) * 2 * KEYS * PITCH;
+    const char *const k = lds + turn * 2 * KEYS * PITCH, *const v = k + KEYS * PITCH;
     const bool more = at + KEYS < all.hi;
-    if (more) next.load(a, pk, pv, at + KEYS, w.k.count, threadIdx.x);
-    if (at < hi_last && at + KEYS > lo_first) odd |= attend<T, D, KEYS>(r, k, k + KEYS * PITCH, at, at + KEYS > hi_first || at < lo_last, a.scale, lane);
-    if (more) next.store(other, other + KEYS * PITCH, threadIdx.x);
-    __syncthreads();
+    if (more) load(at + KEYS, turn ^ 1);
+    if (!masked || (at < hi_last && at + KEYS > lo_first)) odd |= attend<T, D, KEYS, masked>(r, k, v, at, a.scale, lane);
+    if (more) store(turn ^ 1);
+    at += KEYS, turn ^= 1;
+  };
+  while (at < all.hi) {
+    while (at >= whole.lo && at + KEYS <= whole.hi) step(std::false_type());
+    if (at < all.hi) step(std::true_type());
   }
   if (odd) {
 #pragma nounroll
@@ -326,7 +372,8 @@ template <class T, int D, bool VEC> __global__ __launch_bounds__(kFewWaves *kWav
     next.store(k, v, lane);
     if (at + kFewWaves * SIDE < split.end) next.load(a, pk, pv, at + kFewWaves * SIDE, w.k.count, lane);
     __builtin_amdgcn_wave_barrier();
-    odd |= attend<T, D, SIDE>(r, k, v, at, at + SIDE > hi_first || at < lo_last, a.scale, lane);
+    if (at >= lo_last && at + SIDE <= hi_first) attend<T, D, SIDE, false>(r, k, v, at, a.scale, lane);
+    else odd |= attend<T, D, SIDE, true>(r, k, v, at, a.scale, lane);
     __builtin_amdgcn_wave_barrier();
   }
   const float total = column_sum<T>(r.total);

@@ -137,6 +137,62 @@ template <class T, bool VEC> __device__ __forceinline__ u32x4 load_piece(const c
   return v;
 }
 
+// Wavefronts that a SIMD is to hold: two have 256 registers each, which all are operands of any instruction; a single one has half of its 512 beside the others, reached by copies.
+template <class T, int D> constexpr int kWavesAtOnce = sizeof(T) == 2 && D <= 128 ? 2 : 1;
+
+// ---- from memory to LDS ------------------------------------------------------------------------
+//
+// Whole rows go there without passing through registers: a wavefront's load writes 64 pieces one behind the other, so that a lane loads the piece that
+// belongs at its place.  The compiler does not see these loads (it would wait for all of them before any read of LDS): arrived() has to be between them and the reads.
+__device__ __forceinline__ void load_to_lds(uint32_t lds, const char *from) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory");
+}
+__device__ __forceinline__ void load_word_to_lds(uint32_t lds, const char *from) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(from) : "memory");
+}
+// every load of the wavefront's has arrived
+__device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ uint32_t lds_address(const char *p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)p; }
+
+// ROWS rows of a tensor into LDS by WAVES wavefronts.  DIRECT: past registers (rows are whole); else put() loads, and store() writes what it loaded.
+template <class T, int D, int ROWS, int WAVES, bool DIRECT> struct Carrier {
+  static constexpr int kPitch = Held<T, D>::kPitch, kSlots = kPitch / 16;            // places of a row
+  static constexpr int kAll = DIRECT ? ROWS * kSlots : ROWS * Held<T, D>::kPieces, kLanes = WAVES * kWave, kEach = (kAll + kLanes - 1) / kLanes;
+  u32x4 x[DIRECT ? 1 : kEach];
+  __device__ __forceinline__ static int row_of(int i) { return DIRECT ? (i * kLanes + (int)threadIdx.x) / kSlots : (i * kLanes + (int)threadIdx.x) / Held<T, D>::kPieces; }
+  // row(i): the address of row i; step: from channel to channel; d: channels
+  template <class Row> __device__ __forceinline__ void load(char *held, const Row &row, int64_t step, int d) {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int at = i * kLanes + (int)threadIdx.x, r = row_of(i);
+      if constexpr (DIRECT) {
+        if (kAll % kLanes != 0 && i * kLanes + (int)(threadIdx.x & ~(kWave - 1)) >= kAll) continue;
+        const int piece = at % kSlots ^ Held<T, D>::turn(r);
+        const char *from = row(r) + piece * 16;
+        const uint32_t to = __builtin_amdgcn_readfirstlane(lds_address(held) + (at & ~(kWave - 1)) * 16);
+        if (d == kSlots * 16 / (int)sizeof(T)) load_to_lds(to, from);
+        else if (piece * 16 < d * (int)sizeof(T)) load_to_lds(to, from);
+      } else {
+        const bool in = kAll % kLanes == 0 || at < kAll;
+        x[i] = load_piece<T, false>(row(in ? r : 0), step, at % Held<T, D>::kPieces * (16 / (int)sizeof(T)), in ? d : 0);
+      }
+    }
+  }
+  __device__ __forceinline__ void store(char *held) const {
+    if constexpr (!DIRECT) {
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        const int at = i * kLanes + (int)threadIdx.x;
+        if (kAll % kLanes == 0 || at < kAll) *(u32x4 *)(held + Held<T, D>::at(row_of(i), at % Held<T, D>::kPieces)) = x[i];
+      }
+    }
+  }
+};
+// what lies outside of the rows' channels has to be zero before the first load
+template <int LANES> __device__ __forceinline__ void clear_lds(char *held, int bytes) {
+  for (int i = threadIdx.x * 16; i < bytes; i += LANES * 16) *(u32x4 *)(held + i) = u32x4{0, 0, 0, 0};
+}
+
 // ---- sequences ---------------------------------------------------------------------------------
 
 struct Span { int64_t first; int32_t count; };      // tokens of a sequence
@@ -228,6 +284,13 @@ __device__ __forceinline__ Limits limits_of_block(const AttentionArgs &a, const 
   const int64_t first = (int64_t)w.block * a.tokens, end = first + a.tokens < w.q.count ? first + a.tokens : w.q.count;
   const Limits one = limits_of(a, w, (int)first), last = limits_of(a, w, (int)end - 1);
   return {one.lo, last.hi};
+}
+
+// ... and what all of them see
+__device__ __forceinline__ Limits limits_of_all(const AttentionArgs &a, const Work &w) {
+  const int64_t first = (int64_t)w.block * a.tokens, end = first + a.tokens < w.q.count ? first + a.tokens : w.q.count;
+  const Limits one = limits_of(a, w, (int)first), last = limits_of(a, w, (int)end - 1);
+  return {last.lo, one.hi};
 }
 
 }  // namespace ocn
