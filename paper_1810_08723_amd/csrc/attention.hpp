@@ -30,8 +30,10 @@ struct AttentionArgs {
   float scale, plain_scale, true_scale;    // of scores: to powers of two and to those of e, as magnitudes; as it is
   // blocks of a sequence: of `tokens` queries (keys, where a block has keys), and of `heads` query heads of a group
   int32_t heads, head_blocks, tokens, splits;
+  int32_t rows_of_tile;                    // gradients of keys: queries that a tile of rows has
   uint32_t slots, per_sequence;            // of all sequences; of one, where they are not packed
-  FastDiv heads_div, head_blocks_div, across_div, tokens_div, splits_div, per_sequence_div;
+  FastDiv heads_div, head_blocks_div, across_div, tokens_div, splits_div, sequences_div;
+  uint32_t *order;                         // [slots], those with most to do first; null: as they come
   float *parts, *part_sums;                // forward: [units][splits][rows][channels], [..][2]: largest score and sum
 };
 
@@ -60,24 +62,31 @@ int64_t key_units_of(const AttentionSizes &s, int64_t keys);
 bool set_blocks(AttentionArgs &a, const AttentionSizes &s, int64_t rows, int64_t splits);
 bool set_key_blocks(AttentionArgs &a, const AttentionSizes &s, int64_t keys);
 
+// channels that kernels are made for
+inline int padded_channels(int64_t d) { return d <= 64 ? 64 : d <= 96 ? 96 : d <= 128 ? 128 : d <= 192 ? 192 : 256; }
+
 // What the shapes alone decide of a call: whether rows are few (the wavefronts of a workgroup then share them and take keys in turn), rows of a block, the parts that a
 // sequence's keys go to, units.
-constexpr int kRowWaves = 8, kFewWaves = 4;
+constexpr int kFewWaves = 4;
 constexpr int kLeastTiles = 2 * kFewWaves;        // tiles of keys of a part, at least
-struct AttentionPlan { bool few; int rows, splits; int64_t units; };
+struct AttentionPlan { bool few; int waves, rows, splits; int64_t units; };      // waves: of a workgroup
 int run_attention_half(AttentionArgs &a, const AttentionPlan &p, bool vec, void *stream);
 int run_attention_bfloat16(AttentionArgs &a, const AttentionPlan &p, bool vec, void *stream);
 int run_attention_float(AttentionArgs &a, const AttentionPlan &p, bool vec, void *stream);
 
+// From so many units on, which are more than there are CUs, packed sequences' blocks are put in order
+constexpr int64_t kOrderUnits = kNumCUs + 1;
+inline bool ordered(const AttentionSizes &s, int64_t units) { return s.packed && units >= kOrderUnits; }
+int64_t slots_of_units(const AttentionSizes &s, int64_t rows);            // blocks that units_of counts, of all heads together
+int64_t slots_of_key_units(const AttentionSizes &s, int64_t keys);
+
 // The gradient: rows (query heads of all tokens), and which gradients are wanted
 constexpr int kGradWaves = 4;
 struct AttentionGrad { int64_t rows; bool keys, queries; };
+inline int grad_key_waves(int32_t dtype, int64_t channels) { return dtype != OCN_FLOAT && (padded_channels(channels) == 96 || padded_channels(channels) == 128) ? 8 : 4; }
 int run_attention_grad_half(AttentionArgs &a, const AttentionSizes &s, const AttentionGrad &p, bool vec, void *workspace, void *stream);
 int run_attention_grad_bfloat16(AttentionArgs &a, const AttentionSizes &s, const AttentionGrad &p, bool vec, void *workspace, void *stream);
 int run_attention_grad_float(AttentionArgs &a, const AttentionSizes &s, const AttentionGrad &p, bool vec, void *workspace, void *stream);
-
-// channels that kernels are made for
-inline int padded_channels(int64_t d) { return d <= 64 ? 64 : d <= 96 ? 96 : d <= 128 ? 128 : d <= 192 ? 192 : 256; }
 
 // CALL(type, padded channels, whole rows)
 #define OCN_BY_ROWS(T, D, vec, CALL) \

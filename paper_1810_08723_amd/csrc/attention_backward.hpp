@@ -20,7 +20,7 @@ namespace {
 // log2 of what weights are multiplied by: a half holds 2^-14 ... 2^16 without loss, and weights are at most 1
 template <class T> constexpr float kWeightTop = std::is_same<T, f16>::value ? 12.0f : 0.0f;
 
-// What the passes need of a row: minus its log_sum in powers of two (plus kWeightTop), and gout * out.  The same for all keys: one launch of its own, which reads gout and out once.
+// What the passes need of a row: minus its log_sum in powers of two (plus kWeightTop), and minus gout * out.  The same for all keys: one launch of its own, which reads gout and out once.
 template <class T, bool VEC> __global__ __launch_bounds__(kBlock) void attention_along_kernel(const AttentionArgs a, uint32_t rows, FastDiv heads, FastDiv queries, f32x2 *stats) {
   constexpr int LANES = 16, EACH = 16 / (int)sizeof(T);        // of a row; channels of a piece
   const int lane = threadIdx.x % LANES;
@@ -41,7 +41,7 @@ template <class T, bool VEC> __global__ __launch_bounds__(kBlock) void attention
     if (lane == 0) {
       const float log_sum = *(const float *)(a.log_sum.base + b * a.log_sum.batch + token * a.log_sum.token + h * a.log_sum.head);
       // (a row that sees nothing has weights of zero)
-      stats[r] = f32x2{log_sum > -__builtin_inff() || log_sum != log_sum ? kWeightTop<T> - log_sum * 1.44269504088896340736f : -__builtin_inff(), s};
+      stats[r] = f32x2{log_sum > -__builtin_inff() || log_sum != log_sum ? kWeightTop<T> - log_sum * 1.44269504088896340736f : -__builtin_inff(), -s};
     }
   }
 }
@@ -146,6 +146,9 @@ template <class T> __device__ __forceinline__ acc_t<T> no_sum() {
 // LDS, the next ones on their way: some whole queries with the query heads of the group, or some of those.
 template <int D> constexpr bool kValuesHeld = D > 64;
 
+// operands of a step of both products
+template <class T> struct Operands { frag_t<T> x, y, z; };
+
 template <class T, int D, bool VEC, int WAVES>
 __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kWavesAtOnce<T, D>))) void attention_keys_kernel(const AttentionArgs a, uint32_t first_block, const f32x2 *stats, const f32x2 *no_row) {
   warm_arguments<AttentionArgs>();
@@ -153,8 +156,8 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
   constexpr bool HELD = kValuesHeld<D>;
   __shared__ __align__(16) char held[2 * 2 * SIDE * PITCH];      // [2][q, gout][SIDE][PITCH]
   __shared__ __align__(16) char values[HELD ? BLOCK * PITCH : 16];
-  __shared__ __align__(16) f32x2 of_row[2][kWave / 2];
-  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, n = lane & (SIDE - 1), h = lane / SIDE;
+  __shared__ __align__(16) float of_row[2][2][kWave / 2];          // [2][exponent's part, minus gout out]
+  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), n = lane & (SIDE - 1), h = lane / SIDE;
   Work w;
   if (!find_work_of<true>(a, first_block + blockIdx.x, &w)) return;
   const int block = (int)(w.block * (uint32_t)BLOCK), key = block + wave * SIDE + n, end = block + BLOCK < w.k.count ? block + BLOCK : w.k.count;
@@ -169,7 +172,7 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
   const int ahead = w.q.count - w.k.count;
   int lo = 0, hi = w.q.count;
   if (a.causal) {
-    lo = block + ahead > 0 ? block + ahead : 0;
+    lo = block + ahead > 0 ? (block + ahead) / a.rows_of_tile * a.rows_of_tile : 0;
     if (a.window && (int64_t)end - 1 + a.window + ahead < hi) hi = end - 1 + a.window + ahead;
   }
   const int across = (a.per_kv + a.heads - 1) / a.heads;         // tiles that a query's heads take
@@ -190,25 +193,26 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
     cq.load(q, [&](int i) { return row(a.q, pq, i); }, a.q.channel, a.channels);
     cg.load(q + SIDE * PITCH, [&](int i) { return row(a.gout, pg, i); }, a.gout.channel, a.channels);
     if (wave == 0) {      // what the rows have in stats: a word of each lane
-      int i = lane / 2;
+      int i = lane & 31;
       asm("" : "+v"(i));
       const int t = (int)fast_quotient((uint32_t)i, a.heads_div), g = i - t * a.heads;
-      const f32x2 *from = i < SIDE && t < a.tokens && t <= last && g <= past ? ps + (int64_t)(at + t) * heads + part * a.heads + g : no_row;
-      load_word_to_lds(__builtin_amdgcn_readfirstlane(lds_address((const char *)of_row[turn])), (const char *)from + (lane & 1) * 4);
+      const f32x2 *from = i < SIDE && t < a.rows_of_tile && t <= last && g <= past ? ps + (int64_t)(at + t) * heads + part * a.heads + g : no_row;
+      load_word_to_lds(__builtin_amdgcn_readfirstlane(lds_address((const char *)of_row[turn])), (const char *)from + (lane >> 5) * 4);
     }
   };
   const auto store = [&](int turn) {
     cq.store(held + turn * 2 * SIDE * PITCH);
     cg.store(held + (turn * 2 + 1) * SIDE * PITCH);
   };
-  int at = lo, part = 0, turn = 0;
+  // From the last rows to the first: workgroups with other keys of a sequence, which start at other rows, then read the same ones at about the same time.
+  int at = hi > lo ? lo + (hi - 1 - lo) / a.rows_of_tile * a.rows_of_tile : lo - 1, part = across - 1, turn = 0;
   if constexpr (HELD) {
     Carrier<T, D, BLOCK, WAVES, VEC> cv;
     const char *const pv = a.v.base + w.sequence * a.v.batch + w.k.first * a.v.token + (int64_t)w.kv * a.v.head;
     cv.load(values, [&](int i) { return pv + (int64_t)(block + i < end ? block + i : end - 1) * a.v.token; }, a.v.channel, a.channels);
     cv.store(values);
   }
-  if (at < hi) load(at, 0, 0);
+  if (at >= lo) load(at, part, 0);
   frag_t<T> k[D / 16], v[HELD ? 1 : D / 16];
   load_fragments<T, D, VEC>(k, a.k.base + w.sequence * a.k.batch + token * a.k.token + w.kv * a.k.head, a.k.channel, mine && !a.nothing ? a.channels : 0, h, a.negative);
   if constexpr (!HELD)
@@ -217,57 +221,82 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
 #pragma unroll
   for (int ct = 0; ct < D / SIDE; ++ct) gk[ct] = gv[ct] = no_sum<T>();
   Range<T> range;
-  if (at < hi) store(0);
+  if (at >= lo) store(0);
   const int from = block + wave * SIDE;
-  const auto step = [&](auto masked) {
+  const LanePlaces at_start = lane_places<T, D>(lane);
+  const auto step = [&](auto masked, auto turn) {
     arrived();
     __syncthreads();
     const char *const q = held + turn * 2 * SIDE * PITCH, *const g = q + SIDE * PITCH;
-    const int first_end = at - ahead + 1, last_end = first_end + a.tokens - 1;
-    int next = at, next_part = part + 1;
-    if (next_part == across) next += a.tokens, next_part = 0;
-    if (next < hi) load(next, next_part, turn ^ 1);
+    const int first_end = a.causal ? at - ahead + 1 : 0x7fffff00, last_end = first_end + a.rows_of_tile - 1;
+    int next = at, next_part = part - 1;
+    if (next_part < 0) next -= a.rows_of_tile, next_part = across - 1;
+    if (next >= lo) load(next, next_part, turn ^ 1);
     if (!masked || (from < last_end && (!a.window || from + SIDE > first_end - a.window))) {
       int here = h;
-      asm("" : "+v"(here));      // (what hangs on it is not kept in registers from tile to tile)
-      acc_t<T> p = no_sum<T>(), s[1] = {no_sum<T>()};
+      LanePlaces places = at_start;
+      asm("" : "+v"(here), "+v"(places.row), "+v"(places.column));      // (what hangs on them is not kept in registers from tile to tile)
+      acc_t<T> p = no_sum<T>(), s[1];
 #pragma unroll
-      for (int c = 0; c < D / 16; ++c) {
-        p = product(rows_fragment<T, D>(q, 0, c, n, h), k[c], p);
-        s[0] = product(rows_fragment<T, D>(g, 0, c, n, h), HELD ? rows_fragment<T, D>(values, wave * SIDE, c, n, h) : v[HELD ? 0 : c], s[0]);
+      for (int i = 0; i < OWN; i += 4) {
+        const f32x4 less = *(const f32x4 *)&of_row[turn][1][own_index<T>(i) + 4 * h];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[0][i + e] = less[e];
       }
+      pipelined<D / 16, 1, Operands<T>>(
+          [&](int c) {
+            Operands<T> o;
+            o.x = rows_fragment<T, D>(q, 0, c, places);
+            o.y = rows_fragment<T, D>(g, 0, c, places);
+            if constexpr (HELD) o.z = rows_fragment<T, D>(values, wave * SIDE, c, places);
+            return o;
+          },
+          [&](int c, const Operands<T> &o) {
+            p = product(o.x, k[c], p);
+            if constexpr (HELD) s[0] = product(o.y, o.z, s[0]);
+            else s[0] = product(o.y, v[c], s[0]);
+          });
 #pragma unroll
       for (int i = 0; i < OWN; ++i) {
-        const f32x2 r = of_row[turn][own_index<T>(i) + 4 * h];
-        p[i] = weight<T>(__builtin_fmaf(p[i], a.scale, r.x));
+        p[i] = weight<T>(__builtin_fmaf(p[i], a.scale, of_row[turn][0][own_index<T>(i) + 4 * h]));
         if constexpr (masked) {
           const int e = first_end + (int)fast_quotient((uint32_t)(own_index<T>(i) + 4 * here), a.heads_div);
           if (key >= e || (a.window && key < e - a.window)) p[i] = 0.0f;
         }
-        s[0][i] = p[i] * (s[0][i] - r.y);
-      }
-#pragma unroll
-      for (int x = 0; x < Tile<T>::kSteps; ++x) {
-        const frag_t<T> f = as_fragment<T>(p, x);
-#pragma unroll
-        for (int ct = 0; ct < D / SIDE; ++ct) gv[ct] = product(columns_fragment<T, D>(g, 16 * x, ct, lane), f, gv[ct]);
+        s[0][i] *= p[i];
       }
       in_range<T, 1>(s, range, gk, D / SIDE);
+      frag_t<T> weights[Tile<T>::kSteps], slopes[Tile<T>::kSteps];
 #pragma unroll
-      for (int x = 0; x < Tile<T>::kSteps; ++x) {
-        const frag_t<T> f = as_fragment<T>(s[0], x);
-#pragma unroll
-        for (int ct = 0; ct < D / SIDE; ++ct) gk[ct] = product(columns_fragment<T, D>(q, 16 * x, ct, lane), f, gk[ct]);
-      }
+      for (int x = 0; x < Tile<T>::kSteps; ++x) weights[x] = as_fragment<T>(p, x), slopes[x] = as_fragment<T>(s[0], x);
+      constexpr int TILES = D / SIDE, EACH = TILES * Tile<T>::kSteps;
+      pipelined<2 * EACH, 2, frag_t<T>>([&](int i) { return columns_fragment<T, D>(i < EACH ? g : q, 16 * (i % EACH / TILES), i % TILES, places); },
+                                        [&](int i, frag_t<T> x) {
+                                          const int ct = i % TILES;
+                                          if (i < EACH) gv[ct] = product(x, weights[i / TILES], gv[ct]);
+                                          else gk[ct] = product(x, slopes[(i - EACH) / TILES], gk[ct]);
+                                        });
     }
-    if (next < hi) store(turn ^ 1);
-    at = next, part = next_part, turn ^= 1;
+    if (next >= lo) store(turn ^ 1);
+    at = next, part = next_part;
   };
   // Rows that see all of the workgroup's keys have a loop of their own
   const int first_whole = a.causal ? end - 1 + ahead : lo, past_whole = a.window ? block + a.window + ahead : 0x7fffffff;      // (rows past the last have no weights)
-  while (at < hi) {
-    while (at < hi && at >= first_whole && at <= past_whole - a.tokens) step(std::false_type());
-    if (at < hi) step(std::true_type());
+  const auto is_whole = [&](int t) { return t >= lo && t >= first_whole && t <= past_whole - a.rows_of_tile; };
+  while (at >= lo) {
+    if (turn == 0)      // two at a time, so that where they lie is known
+      while (is_whole(at) && is_whole(at - (across == 1 ? a.rows_of_tile : 0))) {
+        step(std::false_type(), std::integral_constant<int, 0>());
+        if (!is_whole(at)) {
+          turn = 1;
+          break;
+        }
+        step(std::false_type(), std::integral_constant<int, 1>());
+      }
+    if (at >= lo) {
+      step(std::true_type(), turn);
+      turn ^= 1;
+    }
   }
   if (!mine) return;
   const float weight = kWeightTop<T> > 0.0f ? 0x1p-12f : 1.0f;
@@ -286,7 +315,7 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
   warm_arguments<AttentionArgs>();
   constexpr int SIDE = Tile<T>::kSide, PITCH = Held<T, D>::kPitch, OWN = Tile<T>::kOwn;
   __shared__ __align__(16) char held[2 * 2 * KEYS * PITCH];      // [2][keys, values][KEYS][PITCH]
-  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, n = lane & (SIDE - 1), h = lane / SIDE;
+  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), n = lane & (SIDE - 1), h = lane / SIDE;
   Work w;
   if (!find_work(a, first_block + blockIdx.x, &w)) return;
   const Limits all = limits_of_block(a, w), whole = limits_of_all(a, w);
@@ -320,14 +349,21 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
   f32x2 stat = *stat_at;
   const int hi_last = __builtin_amdgcn_readlane(own.hi, SIDE - 1), lo_first = __builtin_amdgcn_readfirstlane(own.lo);
   if (at < all.hi) store(0);
+  const LanePlaces places = lane_places<T, D>(lane);
   // scores and gout v of a tile, and the weights
   const auto weights = [&](const char *k, const char *v, int first, acc_t<T> &p, acc_t<T> &s, auto masked) {
     p = s = no_sum<T>();
-#pragma unroll
-    for (int c = 0; c < D / 16; ++c) {
-      p = product(rows_fragment<T, D>(k, 0, c, n, h), q[c], p);
-      s = product(rows_fragment<T, D>(v, 0, c, n, h), g[c], s);
-    }
+    pipelined<D / 16, 2, Operands<T>>(
+        [&](int c) {
+          Operands<T> o;
+          o.x = rows_fragment<T, D>(k, 0, c, places);
+          o.y = rows_fragment<T, D>(v, 0, c, places);
+          return o;
+        },
+        [&](int c, const Operands<T> &o) {
+          p = product(o.x, q[c], p);
+          s = product(o.y, g[c], s);
+        });
     const int lo = own.lo - first - 4 * h, hi = own.hi - first - 4 * h;
 #pragma unroll
     for (int i = 0; i < OWN; ++i) {
@@ -353,7 +389,7 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
       }
       if (more) store(turn ^ 1);
     }
-    stat.y = column_sum<T>(sum) * (kWeightTop<T> > 0.0f ? 0x1p-12f : 1.0f);
+    stat.y = -column_sum<T>(sum) * (kWeightTop<T> > 0.0f ? 0x1p-12f : 1.0f);
     if (place.in && lane < SIDE) *stat_at = stat;
     if (!a.gq.base) return;
     __syncthreads();
@@ -367,7 +403,7 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
 #pragma unroll
   for (int ct = 0; ct < D / SIDE; ++ct) gq[ct] = no_sum<T>();
   Range<T> range;
-  const auto step = [&](auto masked) {
+  const auto step = [&](auto masked, auto turn) {
     arrived();
     __syncthreads();
     const char *const keys = held + turn * 2 * KEYS * PITCH, *const values = keys + KEYS * PITCH;
@@ -380,21 +416,28 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
       acc_t<T> p, s[1];
       weights(k, v, at + t, p, s[0], masked);
 #pragma unroll
-      for (int i = 0; i < OWN; ++i) s[0][i] = p[i] * (s[0][i] - stat.y);
+      for (int i = 0; i < OWN; ++i) s[0][i] = p[i] * (s[0][i] + stat.y);
       in_range<T, 1>(s, range, gq, D / SIDE);
+      frag_t<T> slopes[Tile<T>::kSteps];
 #pragma unroll
-      for (int x = 0; x < Tile<T>::kSteps; ++x) {
-        const frag_t<T> f = as_fragment<T>(s[0], x);
-#pragma unroll
-        for (int ct = 0; ct < D / SIDE; ++ct) gq[ct] = product(columns_fragment<T, D>(k, 16 * x, ct, lane), f, gq[ct]);
-      }
+      for (int x = 0; x < Tile<T>::kSteps; ++x) slopes[x] = as_fragment<T>(s[0], x);
+      constexpr int TILES = D / SIDE;
+      pipelined<TILES * Tile<T>::kSteps, 3, frag_t<T>>([&](int i) { return columns_fragment<T, D>(k, 16 * (i / TILES), i % TILES, places); },
+                                                       [&](int i, frag_t<T> x) { gq[i % TILES] = product(x, slopes[i / TILES], gq[i % TILES]); });
     }
     if (more) store(turn ^ 1);
-    at += KEYS, turn ^= 1;
+    at += KEYS;
   };
   while (at < all.hi) {
-    while (at >= whole.lo && at + KEYS <= whole.hi) step(std::false_type());
-    if (at < all.hi) step(std::true_type());
+    if (turn == 0 && at >= whole.lo)      // two at a time, so that where they lie is known
+      while (at + 2 * KEYS <= whole.hi) {
+        step(std::false_type(), std::integral_constant<int, 0>());
+        step(std::false_type(), std::integral_constant<int, 1>());
+      }
+    if (at < all.hi) {
+      step(std::true_type(), turn);
+      turn ^= 1;
+    }
   }
   if (!place.in) return;
   const float weight = kWeightTop<T> > 0.0f ? 0x1p-12f : 1.0f;
@@ -434,24 +477,30 @@ template <class T, int D, bool VEC> int run_grad(AttentionArgs &a, const Attenti
       return OCN_ERR_LAUNCH;
     }
   }
-  if (rows) {
-    if (!set_blocks(a, sizes, side * kGradWaves, 1)) return OCN_ERR_SHAPE;
-    rc = in_launches(units_of(sizes, side * kGradWaves), [&](uint32_t grid, uint32_t first) {
-      hipLaunchKernelGGL((attention_queries_kernel<T, D, VEC, kGradWaves, kGradKeys<T>>), dim3(grid), dim3(kGradWaves * kWave), 0, stream, a, first, stats);
-    });
+  constexpr int waves = kKeyWaves<T, D>;
+  AttentionArgs of_keys = a;
+  if (!set_blocks(a, sizes, side * kGradWaves, 1) || !set_key_blocks(of_keys, sizes, side * waves)) return OCN_ERR_SHAPE;
+  const int64_t units = units_of(sizes, side * kGradWaves), key_units = p.keys ? key_units_of(sizes, side * waves) : 0;
+  uint32_t *const order = (uint32_t *)(stats + rows + 1);
+  if (ordered(sizes, units)) a.order = order;
+  if (ordered(sizes, key_units)) of_keys.order = order + slots_of_units(sizes, side * kGradWaves);
+  if (a.order || of_keys.order) {
+    hipLaunchKernelGGL(attention_order_kernel, dim3(2), dim3(kOrderLanes), 0, stream, a, BlockPlan{a.tokens, a.slots, a.tokens_div, a.order},
+                       BlockPlan{of_keys.tokens, of_keys.slots, of_keys.tokens_div, of_keys.order});
+    rc = hipGetLastError() == hipSuccess ? OCN_OK : OCN_ERR_LAUNCH;
     if (rc != OCN_OK) return rc;
   }
-  if (p.keys) {
-    constexpr int waves = kKeyWaves<T, D>;
-    if (!set_key_blocks(a, sizes, side * waves)) return OCN_ERR_SHAPE;
-    // (rows of a tile: whole queries with the heads of the group, or some of those)
-    a.heads = std::max(1, std::min(a.per_kv, side));
-    a.heads_div = make_fastdiv((uint32_t)a.heads);
-    a.tokens = side / a.heads;
-    rc = in_launches(key_units_of(sizes, side * waves), [&](uint32_t grid, uint32_t first) {
-      hipLaunchKernelGGL((attention_keys_kernel<T, D, VEC, waves>), dim3(grid), dim3(waves * kWave), 0, stream, a, first, stats, stats + rows);
-    });
-  }
+  rc = in_launches(units, [&](uint32_t grid, uint32_t first) {
+    hipLaunchKernelGGL((attention_queries_kernel<T, D, VEC, kGradWaves, kGradKeys<T>>), dim3(grid), dim3(kGradWaves * kWave), 0, stream, a, first, stats);
+  });
+  if (rc != OCN_OK) return rc;
+  // (rows of a tile: whole queries with the heads of the group, or some of those)
+  of_keys.heads = std::max(1, std::min(a.per_kv, side));
+  of_keys.heads_div = make_fastdiv((uint32_t)of_keys.heads);
+  of_keys.rows_of_tile = side / of_keys.heads;
+  rc = in_launches(key_units, [&](uint32_t grid, uint32_t first) {
+    hipLaunchKernelGGL((attention_keys_kernel<T, D, VEC, waves>), dim3(grid), dim3(waves * kWave), 0, stream, of_keys, first, stats, stats + rows);
+  });
   return rc;
 }
 

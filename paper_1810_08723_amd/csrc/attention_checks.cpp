@@ -146,11 +146,13 @@ static int64_t slots_of(const AttentionSizes &s, int64_t all, int64_t tokens) {
   return s.packed ? all / tokens + s.sequences : s.sequences * ((all / s.sequences + tokens - 1) / tokens);
 }
 
+int64_t slots_of_units(const AttentionSizes &s, int64_t rows) { return slots_of(s, s.queries, rows / heads_of_block(s, rows)); }
+int64_t slots_of_key_units(const AttentionSizes &s, int64_t keys) { return slots_of(s, s.keys, keys); }
 int64_t units_of(const AttentionSizes &s, int64_t rows) {
   const int64_t heads = heads_of_block(s, rows);
-  return slots_of(s, s.queries, rows / heads) * s.kv * ((s.per_kv + heads - 1) / heads);
+  return slots_of_units(s, rows) * s.kv * ((s.per_kv + heads - 1) / heads);
 }
-int64_t key_units_of(const AttentionSizes &s, int64_t keys) { return slots_of(s, s.keys, keys) * s.kv; }
+int64_t key_units_of(const AttentionSizes &s, int64_t keys) { return slots_of_key_units(s, keys) * s.kv; }
 
 static bool set_all(AttentionArgs &a, const AttentionSizes &s, int64_t all, int64_t heads, int64_t head_blocks, int64_t tokens, int64_t splits) {
   const int64_t slots = slots_of(s, all, tokens);
@@ -166,7 +168,7 @@ static bool set_all(AttentionArgs &a, const AttentionSizes &s, int64_t all, int6
   a.across_div = make_fastdiv((uint32_t)std::max<int64_t>(1, s.kv * head_blocks));
   a.tokens_div = make_fastdiv((uint32_t)tokens);
   a.splits_div = make_fastdiv((uint32_t)splits);
-  a.per_sequence_div = make_fastdiv(std::max<uint32_t>(1, a.per_sequence));
+  a.sequences_div = make_fastdiv((uint32_t)std::max<int64_t>(1, s.sequences));
   return true;
 }
 
@@ -176,6 +178,7 @@ bool set_blocks(AttentionArgs &a, const AttentionSizes &s, int64_t rows, int64_t
 }
 bool set_key_blocks(AttentionArgs &a, const AttentionSizes &s, int64_t keys) { return set_all(a, s, s.keys, std::max<int64_t>(1, s.per_kv), 1, keys, 1); }
 
+constexpr int64_t kWideUnits = 512;             // workgroups of eight wavefronts, which read keys and values half as often, from so many on
 constexpr int64_t kSplitWorkgroups = 2048;      // of few rows, as many as long sequences are split for
 
 static AttentionPlan plan_of(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *q_starts) {
@@ -183,7 +186,9 @@ static AttentionPlan plan_of(const ocn_tensor *q, const ocn_tensor *k, const ocn
   const int side = q->dtype == OCN_FLOAT ? 16 : 32;
   const AttentionSizes s = sizes_of(q, k, q_starts);
   p.few = s.sequences == 0 || s.queries * s.per_kv <= side * s.sequences;
-  p.rows = p.few ? side : side * kRowWaves;
+  const int d = padded_channels(q->size[q->ndim - 1]);
+  p.waves = p.few ? kFewWaves : q->dtype != OCN_FLOAT && (d == 96 || d == 128) && units_of(s, 8 * side) >= kWideUnits ? 8 : 4;
+  p.rows = p.few ? side : side * p.waves;
   p.units = units_of(s, p.rows);
   p.splits = 1;
   if (p.few && p.units > 0) {
@@ -194,6 +199,10 @@ static AttentionPlan plan_of(const ocn_tensor *q, const ocn_tensor *k, const ocn
   return p;
 }
 
+// of the workspace: the order of blocks, or what parts of long sequences come to
+static size_t order_bytes(const AttentionPlan &p, const AttentionSizes &s) {
+  return !p.few && ordered(s, p.units) ? (size_t)slots_of_units(s, p.rows) * sizeof(uint32_t) : 0;
+}
 static size_t part_bytes(const AttentionPlan &p, int64_t channels, int side) {
   if (p.splits <= 1) return 0;
   const int64_t d = padded_channels(channels), rows = p.units * p.splits * side;
@@ -209,7 +218,8 @@ extern "C" {
 
 size_t ocn_attention_workspace_bytes(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *q_starts) {
   if (check_attention_sizes(q, k, q_starts) != OCN_OK) return 0;
-  return part_bytes(plan_of(q, k, q_starts), q->size[q->ndim - 1], q->dtype == OCN_FLOAT ? 16 : 32);
+  const AttentionPlan p = plan_of(q, k, q_starts);
+  return p.few ? part_bytes(p, q->size[q->ndim - 1], q->dtype == OCN_FLOAT ? 16 : 32) : order_bytes(p, sizes_of(q, k, q_starts));
 }
 
 int ocn_attention(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *v, const ocn_tensor *q_starts, const ocn_tensor *k_starts, double scale,
@@ -223,7 +233,7 @@ int ocn_attention(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *v,
   if ((rc = check_operands(ops, 7)) != OCN_OK) return rc;
   const AttentionPlan p = plan_of(q, k, q_starts);
   const int side = q->dtype == OCN_FLOAT ? 16 : 32;
-  const size_t need = part_bytes(p, a.channels, side);
+  const size_t need = p.few ? part_bytes(p, a.channels, side) : order_bytes(p, sizes_of(q, k, q_starts));
   if (need) {
     if (!workspace || workspace_bytes < need) return OCN_ERR_WORKSPACE;
     if ((uintptr_t)workspace % 256 != 0) return OCN_ERR_ALIGN;
@@ -232,8 +242,12 @@ int ocn_attention(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *v,
   if (!set_blocks(a, sizes_of(q, k, q_starts), p.rows, p.splits)) return OCN_ERR_SHAPE;
   a.out = view_of(out);
   if (log_sum) a.log_sum = view_of(log_sum, false);
-  a.parts = (float *)workspace;
-  a.part_sums = a.parts + p.units * p.splits * side * padded_channels(a.channels);
+  if (p.few) {
+    a.parts = (float *)workspace;
+    a.part_sums = a.parts + p.units * p.splits * side * padded_channels(a.channels);
+  } else if (need) {
+    a.order = (uint32_t *)workspace;
+  }
   const bool vec = whole_rows(q) && whole_rows(k) && whole_rows(v) && whole_rows(out);
   switch (q->dtype) {
     case OCN_HALF: return run_attention_half(a, p, vec, stream);
@@ -242,13 +256,17 @@ int ocn_attention(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *v,
   }
 }
 
-// two numbers of each row, and of a row that is none
-static size_t grad_bytes(const AttentionSizes &s) { return (size_t)(s.queries * s.kv * s.per_kv + 1) * 2 * sizeof(float); }
+// two numbers of each row, and of a row that is none; the order of blocks of queries and of keys
+static size_t grad_bytes(const AttentionSizes &s, int32_t dtype, int64_t channels) {
+  const int side = dtype == OCN_FLOAT ? 16 : 32;
+  return (size_t)(s.queries * s.kv * s.per_kv + 1) * 2 * sizeof(float) +
+         (size_t)(slots_of_units(s, side * kGradWaves) + slots_of_key_units(s, side * grad_key_waves(dtype, channels))) * sizeof(uint32_t);
+}
 
 size_t ocn_attention_grad_workspace_bytes(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *q_starts) {
   if (check_attention_sizes(q, k, q_starts) != OCN_OK) return 0;
   const AttentionSizes s = sizes_of(q, k, q_starts);
-  return grad_bytes(s);
+  return grad_bytes(s, q->dtype, q->size[q->ndim - 1]);
 }
 
 int ocn_attention_grad(const ocn_tensor *gout, const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *v, const ocn_tensor *out, const ocn_tensor *log_sum,
@@ -269,7 +287,7 @@ int ocn_attention_grad(const ocn_tensor *gout, const ocn_tensor *q, const ocn_te
   p.rows = s.queries * s.kv * s.per_kv;
   p.keys = k_gin != nullptr && s.keys > 0;
   p.queries = q_gin != nullptr && p.rows > 0;
-  if (!workspace || workspace_bytes < grad_bytes(s)) return OCN_ERR_WORKSPACE;
+  if (!workspace || workspace_bytes < grad_bytes(s, q->dtype, a.channels)) return OCN_ERR_WORKSPACE;
   if ((uintptr_t)workspace % 256 != 0) return OCN_ERR_ALIGN;
   if (!p.keys && !p.queries) return OCN_OK;
   bool vec = whole_rows(q) && whole_rows(k) && whole_rows(v) && whole_rows(out) && whole_rows(gout);

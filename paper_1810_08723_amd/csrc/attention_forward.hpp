@@ -92,6 +92,10 @@ template <class T, int D> struct SlowRow {
   }
 };
 
+// operands that are read ahead of their products
+template <class T, int D> constexpr int kScoresAhead = 4;
+template <class T, int D> constexpr int kValuesAhead = 5;
+
 // the weights of scores, in their place, relative to the row's reference: their sum over a lane's own
 template <class T, int TILES> __device__ __forceinline__ float weigh(const acc_t<T> *s, acc_t<T> *p, float best, float scale, bool exact) {
   float sum = 0.0f;
@@ -120,14 +124,13 @@ template <class T, int TILES> __device__ __forceinline__ float weigh(const acc_t
 // KEYS keys of a tile in LDS, from key `first` of the sequence on.  MASKED: some row does not see all of them; true: and values that it does not see may have reached it.
 template <class T, int D, int KEYS, bool MASKED> __device__ __forceinline__ bool attend(Rows<T, D> &r, const char *k, const char *v, int first, float scale, int lane) {
   constexpr int SIDE = Tile<T>::kSide, TILES = KEYS / SIDE, OWN = Tile<T>::kOwn, STEPS = Tile<T>::kSteps;
-  const int n = lane & (SIDE - 1), h = lane / SIDE;
+  const int h = lane / SIDE;
+  const LanePlaces places = lane_places<T, D>(lane);
   acc_t<T> s[TILES], p[TILES];
 #pragma unroll
   for (int t = 0; t < TILES; ++t) s[t] = zero_acc<T>();
-#pragma unroll
-  for (int c = 0; c < D / 16; ++c)
-#pragma unroll
-    for (int t = 0; t < TILES; ++t) s[t] = product(rows_fragment<T, D>(k, t * SIDE, c, n, h), r.q[c], s[t]);
+  pipelined<TILES * D / 16, kScoresAhead<T, D>, frag_t<T>>([&](int i) { return rows_fragment<T, D>(k, i % TILES * SIDE, i / TILES, places); },
+                                                           [&](int i, frag_t<T> x) { s[i % TILES] = product(x, r.q[i / TILES], s[i % TILES]); });
   if constexpr (MASKED) {
     const int lo = r.lo - first - 4 * h, hi = r.hi - first - 4 * h;
 #pragma unroll
@@ -157,14 +160,12 @@ template <class T, int D, int KEYS, bool MASKED> __device__ __forceinline__ bool
     sum = weigh<T, TILES>(s, p, best, scale, r.exact);
   }
   r.total += sum;
+  frag_t<T> f[TILES * STEPS];
 #pragma unroll
-  for (int t = 0; t < TILES; ++t)
-#pragma unroll
-    for (int x = 0; x < STEPS; ++x) {
-      const frag_t<T> f = as_fragment<T>(p[t], x);
-#pragma unroll
-      for (int ct = 0; ct < D / SIDE; ++ct) r.out[ct] = product(columns_fragment<T, D>(v, t * SIDE + 16 * x, ct, lane), f, r.out[ct]);
-    }
+  for (int x = 0; x < TILES * STEPS; ++x) f[x] = as_fragment<T>(p[x / STEPS], x % STEPS);
+  constexpr int OUTS = D / SIDE;
+  pipelined<TILES * STEPS * OUTS, kValuesAhead<T, D>, frag_t<T>>([&](int i) { return columns_fragment<T, D>(v, 16 * (i / OUTS), i % OUTS, places); },
+                                                                 [&](int i, frag_t<T> x) { r.out[i % OUTS] = product(x, f[i / OUTS], r.out[i % OUTS]); });
   return MASKED && odd_values<T, D, KEYS>(v, lane);
 }
 
@@ -256,7 +257,7 @@ template <class T, int D, bool VEC, int WAVES, int KEYS> __global__ __launch_bou
   warm_arguments<AttentionArgs>();
   constexpr int SIDE = Tile<T>::kSide, PITCH = Held<T, D>::kPitch;
   __shared__ __align__(16) char lds[2 * 2 * KEYS * PITCH];        // [2][keys, values][KEYS][PITCH]
-  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   Work w;
   if (!find_work(a, first_block + blockIdx.x, &w)) return;
   const Limits all = limits_of_block(a, w), whole = limits_of_all(a, w);
@@ -286,7 +287,7 @@ template <class T, int D, bool VEC, int WAVES, int KEYS> __global__ __launch_bou
   bool odd = false;
   if (at < all.hi) store(0);
   // Tiles that all rows of the workgroup see whole have a loop of their own: what masks need takes none of its registers.
-  const auto step = [&](auto masked) {
+  const auto step = [&](auto masked, auto turn) {
     arrived();
     __syncthreads();
     const char *const k = lds + turn * 2 * KEYS * PITCH, *const v = k + KEYS * PITCH;
@@ -294,11 +295,18 @@ template <class T, int D, bool VEC, int WAVES, int KEYS> __global__ __launch_bou
     if (more) load(at + KEYS, turn ^ 1);
     if (!masked || (at < hi_last && at + KEYS > lo_first)) odd |= attend<T, D, KEYS, masked>(r, k, v, at, a.scale, lane);
     if (more) store(turn ^ 1);
-    at += KEYS, turn ^= 1;
+    at += KEYS;
   };
   while (at < all.hi) {
-    while (at >= whole.lo && at + KEYS <= whole.hi) step(std::false_type());
-    if (at < all.hi) step(std::true_type());
+    if (turn == 0 && at >= whole.lo)      // two at a time, so that where they lie is known
+      while (at + 2 * KEYS <= whole.hi) {
+        step(std::false_type(), std::integral_constant<int, 0>());
+        step(std::false_type(), std::integral_constant<int, 1>());
+      }
+    if (at < all.hi) {
+      step(std::true_type(), turn);
+      turn ^= 1;
+    }
   }
   if (odd) {
 #pragma nounroll
@@ -353,7 +361,7 @@ template <class T, int D, bool VEC> __global__ __launch_bounds__(kFewWaves *kWav
   __shared__ __align__(16) char lds[kFewWaves * PART];        // [wavefronts][keys, values][SIDE][PITCH]
   __shared__ float bests[kFewWaves][SIDE], totals[kFewWaves][SIDE];
   __shared__ bool odds[kFewWaves];
-  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, n = lane & (SIDE - 1);
+  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), n = lane & (SIDE - 1);
   Work w;
   if (!find_work(a, first_block + blockIdx.x, &w)) return;
   const Limits all = limits_of_block(a, w);
@@ -487,14 +495,21 @@ int done(hipError_t e) {
 
 template <class T> constexpr int kRowKeys = sizeof(T) == 2 ? 64 : 32;
 
+template <class T, int D> constexpr bool kWide = sizeof(T) == 2 && (D == 96 || D == 128);
+
 template <class T, int D, bool VEC> int run(AttentionArgs &a, const AttentionPlan &p, hipStream_t stream) {
   const int64_t blocks = p.units * p.splits;
   int rc;
   const int64_t most = max_launch_blocks();
+  if (a.order) {
+    hipLaunchKernelGGL(attention_order_kernel, dim3(1), dim3(kOrderLanes), 0, stream, a, BlockPlan{a.tokens, a.slots, a.tokens_div, a.order}, BlockPlan{});
+    if ((rc = done(hipGetLastError())) != OCN_OK) return rc;
+  }
   for (int64_t at = 0; at < blocks; at += most) {
     const uint32_t grid = (uint32_t)std::min(blocks - at, most), first = (uint32_t)at;
     if (p.few) hipLaunchKernelGGL((attention_few_kernel<T, D, VEC>), dim3(grid), dim3(kFewWaves * kWave), 0, stream, a, first);
-    else hipLaunchKernelGGL((attention_rows_kernel<T, D, VEC, kRowWaves, kRowKeys<T>>), dim3(grid), dim3(kRowWaves * kWave), 0, stream, a, first);
+    else if (kWide<T, D> && p.waves == 8) hipLaunchKernelGGL((attention_rows_kernel<T, D, VEC, kWide<T, D> ? 8 : 4, kRowKeys<T>>), dim3(grid), dim3(8 * kWave), 0, stream, a, first);
+    else hipLaunchKernelGGL((attention_rows_kernel<T, D, VEC, 4, kRowKeys<T>>), dim3(grid), dim3(4 * kWave), 0, stream, a, first);
     if ((rc = done(hipGetLastError())) != OCN_OK) return rc;
   }
   if (p.splits == 1) return OCN_OK;

@@ -97,26 +97,38 @@ template <class T, int D> struct Held {
   __device__ __forceinline__ static int at(int row, int piece) { return row * kPitch + ((piece ^ turn(row)) << 4); }
 };
 
-// A fragment of 16 channels (16 step ...) of rows `row` + n
-template <class T, int D> __device__ __forceinline__ frag_t<T> rows_fragment(const char *held, int row, int step, int n, int h) {
-  return *(const frag_t<T> *)(held + Held<T, D>::at(row + n, step * (int)sizeof(T) + h));
+// Where a lane finds its fragments: step 0 of a row-wise one and tile 0 of a transposed one.  Those of other steps and tiles differ in bits that
+// no sum carries into.
+struct LanePlaces { int row, column; };
+template <class T, int D> __device__ __forceinline__ LanePlaces lane_places(int lane) {
+  const int n = lane & (Tile<T>::kSide - 1), h = lane / Tile<T>::kSide, j = lane & 15;
+  LanePlaces p;
+  p.row = Held<T, D>::at(n, h);
+  if constexpr (sizeof(T) == 2) p.column = Held<T, D>::at(4 * h + (j >> 2), ((lane & 16) + 4 * (j & 3)) >> 3) + 8 * (j & 1);
+  else p.column = 4 * h * Held<T, D>::kPitch + 4 * (j & 3) + ((j >> 2) << 4);
+  return p;
 }
 
-// Its transpose: lane n has channel side * tile + n of the 16 rows row ... row + 15, in a result's order
-template <class T, int D> __device__ __forceinline__ frag_t<T> columns_fragment(const char *held, int row, int tile, int lane) {
+// A fragment of 16 channels (16 step ...) of rows `row` + n
+template <class T, int D> __device__ __forceinline__ frag_t<T> rows_fragment(const char *held, int row, int step, const LanePlaces &p) {
+  return *(const frag_t<T> *)(held + ((p.row ^ step * 16 * (int)sizeof(T)) + row * Held<T, D>::kPitch));
+}
+
+// Its transpose: lane n has channel side * tile + n of the 16 rows row ... row + 15 (a multiple of 16), in a result's order
+template <class T, int D> __device__ __forceinline__ frag_t<T> columns_fragment(const char *held, int row, int tile, const LanePlaces &p) {
+  constexpr int PITCH = Held<T, D>::kPitch;
   frag_t<T> f;
   if constexpr (sizeof(T) == 2) {
-    const int h = lane >> 5, j = lane & 15, channel = tile * 32 + (lane & 16) + 4 * (j & 3), r = row + 4 * h + (j >> 2);
     typedef __attribute__((address_space(3))) s16x4 *Lds;
     union { s16x4 s[2]; frag_t<T> f; } u;
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
-      u.s[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(held + Held<T, D>::at(r + 8 * k, channel >> 3) + 2 * (channel & 7)));
+    for (int k = 0; k < 2; ++k)       // (eight rows further a row's turn differs in its last bit)
+      u.s[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(held + ((p.column ^ (tile * 64 + 16 * k)) + (row + 8 * k) * PITCH)));
     f = u.f;
   } else {
-    const int h = lane >> 4, channel = tile * 16 + (lane & 15);
+    const int h = threadIdx.x / 16 % 4;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) f[e] = *(const float *)(held + Held<T, D>::at(row + 4 * h + e, channel >> 2) + 4 * (channel & 3));
+    for (int e = 0; e < 4; ++e) f[e] = *(const float *)(held + ((p.column ^ ((tile * 4 ^ Held<T, D>::turn(4 * h + e)) << 4)) + (row + e) * PITCH));
   }
   return f;
 }
@@ -193,6 +205,29 @@ template <int LANES> __device__ __forceinline__ void clear_lds(char *held, int b
   for (int i = threadIdx.x * 16; i < bytes; i += LANES * 16) *(u32x4 *)(held + i) = u32x4{0, 0, 0, 0};
 }
 
+// ---- products with operands in LDS ----------------------------------------------------------------
+//
+// The compiler reads an operand right before the product that takes it, to save registers, and waits for LDS there.  Here N operands (or sets of them) are read AHEAD of
+// their turn, and nothing moves from one turn to another: read(i) gives operand i, use(i, operand) takes it.
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
+
+template <int N, int AHEAD, class Operand, class Read, class Use> __device__ __forceinline__ void pipelined(const Read &read, const Use &use) {
+  Operand held[AHEAD + 1];
+#pragma unroll
+  for (int i = 0; i < AHEAD && i < N; ++i) held[i] = read(i);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if (i + AHEAD < N) held[(i + AHEAD) % (AHEAD + 1)] = read(i + AHEAD);
+    in_order();
+    use(i, held[i % (AHEAD + 1)]);
+    in_order();
+  }
+  // The last results are not written before eleven or more cycles of waiting, which the compiler does not put where their reader is in another basic block:
+  // behind a loop whose last product this is it read a result's last element too early.
+  asm volatile("s_nop 15\n\ts_nop 3");
+  in_order();
+}
+
 // ---- sequences ---------------------------------------------------------------------------------
 
 struct Span { int64_t first; int32_t count; };      // tokens of a sequence
@@ -234,21 +269,23 @@ struct Work {
   Span q, k;
 };
 
-// KEYS: blocks are of keys.  False: there is no such block.  (Blocks go from the last to the first: with a causal mask the later ones have more to do.)
+// KEYS: blocks are of keys.  False: there is no such block.
 template <bool KEYS> __device__ __forceinline__ bool find_work_of(const AttentionArgs &a, uint32_t index, Work *w) {
   w->unit = fast_quotient(index, a.splits_div);
   w->split = (int)(index - w->unit * (uint32_t)a.splits);
   const uint32_t down = fast_quotient(w->unit, a.across_div), across = w->unit - down * a.across_div.d;
   if (down >= a.slots) return false;
-  const uint32_t slot = KEYS ? down : a.slots - 1 - down;
   w->kv = (int)fast_quotient(across, a.head_blocks_div);
   w->head_block = (int)(across - (uint32_t)w->kv * (uint32_t)a.head_blocks);
   const Starts &s = KEYS ? a.k_starts : a.q_starts;
+  // With a causal mask the first blocks of keys and the last ones of queries have most to do.
   if (s.p) {
+    const uint32_t slot = a.order ? a.order[down] : KEYS ? down : a.slots - 1 - down;
     if (!find_slot(s, a.tokens_div, slot, &w->sequence, &w->block)) return false;
   } else {
-    w->sequence = (int)fast_quotient(slot, a.per_sequence_div);
-    w->block = slot - (uint32_t)w->sequence * a.per_sequence;
+    const uint32_t turn = fast_quotient(down, a.sequences_div);
+    w->sequence = (int)(down - turn * a.sequences_div.d);
+    w->block = KEYS ? turn : a.per_sequence - 1 - turn;
   }
   w->q = span_of(a.q_starts, w->sequence);
   w->k = span_of(a.k_starts, w->sequence);
@@ -291,6 +328,73 @@ __device__ __forceinline__ Limits limits_of_all(const AttentionArgs &a, const Wo
   const int64_t first = (int64_t)w.block * a.tokens, end = first + a.tokens < w.q.count ? first + a.tokens : w.q.count;
   const Limits one = limits_of(a, w, (int)first), last = limits_of(a, w, (int)end - 1);
   return {last.lo, one.hi};
+}
+
+// ---- the order of blocks -----------------------------------------------------------------------
+//
+// Packed sequences may be of any lengths, which only the GPU knows.  A workgroup that takes long and is started last is waited for by all the others: where there are more of them
+// than CUs, those with most to do go first.  One workgroup sorts all blocks by what they have to do, to a sixteenth of it.
+struct BlockPlan { int32_t tokens; uint32_t slots; FastDiv tokens_div; uint32_t *order; };
+
+template <bool KEYS> __device__ inline void order_blocks(const AttentionArgs &a, const BlockPlan &b, uint32_t *places) {
+  constexpr int kSizes = 512;
+  const Starts &s = KEYS ? a.k_starts : a.q_starts;
+  const auto size_of = [&](uint32_t slot) {
+    int lo = 0, hi = s.sequences;
+    while (hi - lo > 1) {
+      const int middle = lo + (hi - lo) / 2;
+      if (fast_quotient((uint32_t)start_at(s, middle), b.tokens_div) + (uint32_t)middle <= slot) lo = middle; else hi = middle;
+    }
+    const Span q = span_of(a.q_starts, lo), k = span_of(a.k_starts, lo);
+    const int64_t block = (int64_t)slot - (fast_quotient((uint32_t)start_at(s, lo), b.tokens_div) + (uint32_t)lo), first = block * b.tokens;
+    const int64_t own = KEYS ? k.count : q.count, other = KEYS ? q.count : k.count;
+    if (block < 0 || first >= own) return 0;
+    const int64_t end = first + b.tokens < own ? first + b.tokens : own;
+    int64_t most = other;       // keys that a block of queries sees, or queries that see a block of keys
+    if (a.causal) {
+      const int64_t ahead = (int64_t)q.count - k.count;
+      const int64_t from = KEYS ? (first + ahead > 0 ? first + ahead : 0) : (a.window && first - ahead + 1 > a.window ? first - ahead + 1 - a.window : 0);
+      const int64_t to = KEYS ? (a.window && end - 1 + a.window + ahead < q.count ? end - 1 + a.window + ahead : q.count) : end - ahead;
+      most = to > from ? to - from : 0;
+    }
+    const int size = (int)(__builtin_bit_cast(uint32_t, (float)most) >> 19) - (126 << 4);       // four bits behind the first
+    return size < 1 ? 1 : size < kSizes ? size : kSizes - 1;
+  };
+  for (int i = threadIdx.x; i < kSizes; i += blockDim.x) places[i] = 0;
+  __syncthreads();
+  for (uint32_t i = threadIdx.x; i < b.slots; i += blockDim.x) atomicAdd(&places[size_of(i)], 1u);
+  __syncthreads();
+  if (threadIdx.x < kWave) {      // blocks that are larger
+    constexpr int kEach = kSizes / kWave;
+    const int lane = threadIdx.x;
+    uint32_t own[kEach], sum = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {      // from the largest down
+      own[i] = sum;
+      sum += places[kSizes - 1 - lane * kEach - i];
+    }
+    uint32_t before = sum;
+    for (int o = 1; o < kWave; o *= 2) {
+      const uint32_t x = __shfl_up(before, o);
+      if (lane >= o) before += x;
+    }
+    before -= sum;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) places[kSizes - 1 - lane * kEach - i] = before + own[i];
+  }
+  __syncthreads();
+  for (uint32_t i = threadIdx.x; i < b.slots; i += blockDim.x) b.order[atomicAdd(&places[size_of(i)], 1u)] = i;
+}
+
+// (the order of blocks of the same size is as it comes: results do not depend on it)
+constexpr int kOrderLanes = 1024;
+static __global__ __launch_bounds__(kOrderLanes) void attention_order_kernel(const AttentionArgs a, BlockPlan queries, BlockPlan keys) {
+  __shared__ uint32_t places[512];
+  if (blockIdx.x == 0) {
+    if (queries.order) order_blocks<false>(a, queries, places);
+  } else {
+    if (keys.order) order_blocks<true>(a, keys, places);
+  }
 }
 
 }  // namespace ocn

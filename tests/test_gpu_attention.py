@@ -330,3 +330,14 @@ def test_long_sequences_are_split_and_joined():
             shape = ([1] * len(lengths), lengths, heads, kv, d, True, 0)
             data = made(shape, kind, 12)
             check(shape, kind, data, both(shape, kind, data, grad=False))
+
+
+@pytest.mark.parametrize("kind", list(KIND))
+@pytest.mark.parametrize("causal,window", [(True, 0), (True, 40), (False, 0)])
+def test_many_sequences(kind, causal, window):
+    """More blocks than CUs, which are put in order: sequences of any lengths, ones without tokens among them"""
+    g = torch.Generator().manual_seed(13)
+    nq, nk = (torch.randint(0, 150, (90,), generator=g).tolist() for _ in range(2))
+    for shape in ((nk, None, 8, 4, 64, causal, window), (nq, nk, 6, 6, 128, causal, window)):
+        data = made(shape, kind, 14)
+        check(shape, kind, data, both(shape, kind, data))
