@@ -20,32 +20,6 @@ namespace {
 // log2 of what weights are multiplied by: a half holds 2^-14 ... 2^16 without loss, and weights are at most 1
 template <class T> constexpr float kWeightTop = std::is_same<T, f16>::value ? 12.0f : 0.0f;
 
-// What the passes need of a row: minus its log_sum in powers of two (plus kWeightTop), and minus gout * out.  The same for all keys: one launch of its own, which reads gout and out once.
-template <class T, bool VEC> __global__ __launch_bounds__(kBlock) void attention_along_kernel(const AttentionArgs a, uint32_t rows, FastDiv heads, FastDiv queries, f32x2 *stats) {
-  constexpr int LANES = 16, EACH = 16 / (int)sizeof(T);        // of a row; channels of a piece
-  const int lane = threadIdx.x % LANES;
-  if (blockIdx.x == 0 && threadIdx.x == 0) stats[rows] = f32x2{-__builtin_inff(), 0.0f};      // (of a row that is none)
-  for (uint32_t r = blockIdx.x * (kBlock / LANES) + threadIdx.x / LANES; r < rows; r += gridDim.x * (kBlock / LANES)) {
-    const uint32_t t = fast_quotient(r, heads), h = r - t * heads.d, b = fast_quotient(t, queries);
-    const int64_t token = t - b * queries.d;
-    const char *g = a.gout.base + b * a.gout.batch + token * a.gout.token + h * a.gout.head, *o = a.out.base + b * a.out.batch + token * a.out.token + h * a.out.head;
-    float s = 0.0f;
-    for (int e = lane * EACH; e < a.channels; e += LANES * EACH) {
-      union { u32x4 v; T t[EACH]; } x, y;
-      x.v = load_piece<T, VEC>(g, a.gout.channel, e, a.channels);
-      y.v = load_piece<T, VEC>(o, a.out.channel, e, a.channels);
-#pragma unroll
-      for (int i = 0; i < EACH; ++i) s = __builtin_fmaf((float)x.t[i], (float)y.t[i], s);
-    }
-    s = sum_over_row(s, LANES);
-    if (lane == 0) {
-      const float log_sum = *(const float *)(a.log_sum.base + b * a.log_sum.batch + token * a.log_sum.token + h * a.log_sum.head);
-      // (a row that sees nothing has weights of zero)
-      stats[r] = f32x2{log_sum > -__builtin_inff() || log_sum != log_sum ? kWeightTop<T> - log_sum * 1.44269504088896340736f : -__builtin_inff(), -s};
-    }
-  }
-}
-
 // A half's range is short for the s of all keys or rows: those of a lane's column are multiplied by a power of two of its own, chosen by the first of them and
 // lowered, with what has been summed, where one would pass 2^15.
 template <class T> struct Range {
@@ -311,16 +285,16 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
 constexpr int kFewKeys = 256;
 
 template <class T, int D, bool VEC, int WAVES, int KEYS>
-__global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kWavesAtOnce<T, D>))) void attention_queries_kernel(const AttentionArgs a, uint32_t first_block, f32x2 *stats) {
+__global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kWavesAtOnce<T, D>))) void attention_queries_kernel(const AttentionArgs a, uint32_t first_block, f32x2 *stats, f32x2 *no_row) {
   warm_arguments<AttentionArgs>();
   constexpr int SIDE = Tile<T>::kSide, PITCH = Held<T, D>::kPitch, OWN = Tile<T>::kOwn;
   __shared__ __align__(16) char held[2 * 2 * KEYS * PITCH];      // [2][keys, values][KEYS][PITCH]
   const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), n = lane & (SIDE - 1), h = lane / SIDE;
+  if (first_block + blockIdx.x == 0 && threadIdx.x == 0) *no_row = f32x2{-__builtin_inff(), 0.0f};
   Work w;
   if (!find_work(a, first_block + blockIdx.x, &w)) return;
   const Limits all = limits_of_block(a, w), whole = limits_of_all(a, w);
   const bool few = all.hi - all.lo <= kFewKeys;
-  if (!a.gq.base && !few) return;
   const RowPlace place = row_place(a, w, wave * SIDE + n);
   const Limits own = limits_of(a, w, place.query);
   const int64_t token = w.q.first + place.query, head = (int64_t)w.kv * a.per_kv + place.head;
@@ -345,8 +319,25 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
   frag_t<T> q[D / 16], g[D / 16];
   load_fragments<T, D, VEC>(q, a.q.base + w.sequence * a.q.batch + token * a.q.token + head * a.q.head, a.q.channel, place.in && !a.nothing ? a.channels : 0, h, a.negative);
   load_fragments<T, D, VEC>(g, a.gout.base + w.sequence * a.gout.batch + token * a.gout.token + head * a.gout.head, a.gout.channel, place.in ? a.channels : 0, h, false);
+  // What the passes need of a row: minus its log_sum in powers of two (plus kWeightTop), and minus gout * out.  (A row that sees nothing has weights of zero.)
   f32x2 *const stat_at = stats + (w.sequence * (a.q_starts.p ? 0 : a.q_starts.all) + token) * ((int64_t)a.kv * a.per_kv) + head;
-  f32x2 stat = *stat_at;
+  f32x2 stat;
+  {
+    frag_t<T> o[D / 16];
+    load_fragments<T, D, VEC>(o, a.out.base + w.sequence * a.out.batch + token * a.out.token + head * a.out.head, a.out.channel, a.channels, h, false);
+    const float log_sum = *(const float *)(a.log_sum.base + w.sequence * a.log_sum.batch + token * a.log_sum.token + head * a.log_sum.head);
+    float sum = 0.0f;
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+      for (int i = 0; i < Tile<T>::kFrag; ++i) sum = __builtin_fmaf((float)g[c][i], (float)o[c][i], sum);
+    stat = f32x2{log_sum > -__builtin_inff() || log_sum != log_sum ? kWeightTop<T> - log_sum * 1.44269504088896340736f : -__builtin_inff(), -column_sum<T>(sum)};
+    if (!few && place.in && lane < SIDE) *stat_at = stat;
+  }
+  if (!few && !a.gq.base) {
+    arrived();      // (LDS may be another workgroup's once this one has ended)
+    return;
+  }
   const int hi_last = __builtin_amdgcn_readlane(own.hi, SIDE - 1), lo_first = __builtin_amdgcn_readfirstlane(own.lo);
   if (at < all.hi) store(0);
   const LanePlaces places = lane_places<T, D>(lane);
@@ -468,15 +459,6 @@ template <class T, int D, bool VEC> int run_grad(AttentionArgs &a, const Attenti
   constexpr int side = Tile<T>::kSide;
   int rc = OCN_OK;
   const uint32_t rows = (uint32_t)p.rows;
-  {
-    const FastDiv heads = make_fastdiv((uint32_t)(a.kv * a.per_kv)), queries = make_fastdiv((uint32_t)std::max<int64_t>(1, sizes.packed ? sizes.queries : a.q_starts.all));
-    hipLaunchKernelGGL((attention_along_kernel<T, VEC>), dim3(std::max(1u, std::min((rows + 15) / 16, 8192u))), dim3(kBlock), 0, stream, a, rows, heads, queries, stats);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) {
-      record_hip_error((int)e);
-      return OCN_ERR_LAUNCH;
-    }
-  }
   constexpr int waves = kKeyWaves<T, D>;
   AttentionArgs of_keys = a;
   if (!set_blocks(a, sizes, side * kGradWaves, 1) || !set_key_blocks(of_keys, sizes, side * waves)) return OCN_ERR_SHAPE;
@@ -491,7 +473,7 @@ template <class T, int D, bool VEC> int run_grad(AttentionArgs &a, const Attenti
     if (rc != OCN_OK) return rc;
   }
   rc = in_launches(units, [&](uint32_t grid, uint32_t first) {
-    hipLaunchKernelGGL((attention_queries_kernel<T, D, VEC, kGradWaves, kGradKeys<T>>), dim3(grid), dim3(kGradWaves * kWave), 0, stream, a, first, stats);
+    hipLaunchKernelGGL((attention_queries_kernel<T, D, VEC, kGradWaves, kGradKeys<T>>), dim3(grid), dim3(kGradWaves * kWave), 0, stream, a, first, stats, stats + rows);
   });
   if (rc != OCN_OK) return rc;
   // (rows of a tile: whole queries with the heads of the group, or some of those)

@@ -99,38 +99,38 @@ template <bool VEC> __device__ __forceinline__ void load_factors(const char *p, 
   }
 }
 
-// Sums over the lanes of a row: of one wavefront's (WAVES 1), or of a whole workgroup's WAVES wavefronts, through LDS.  `slots` is not used again before
-// another call's barrier.
-template <int WAVES, int N> __device__ __forceinline__ void sums_over_row(float *v, int lanes, float (*slots)[N]) {
+// Sums over the lanes of a row: of one wavefront's, or (WIDE) of a whole workgroup's wavefronts, through LDS.  `slots` is not used again before another call's barrier.
+constexpr int kMostWaves = 16;
+template <bool WIDE, int N> __device__ __forceinline__ void sums_over_row(float *v, int lanes, float (*slots)[N]) {
 #pragma unroll
-  for (int n = 0; n < N; ++n) v[n] = sum_over_row(v[n], WAVES > 1 ? kWave : lanes);
-  if constexpr (WAVES > 1) {
+  for (int n = 0; n < N; ++n) v[n] = sum_over_row(v[n], WIDE ? kWave : lanes);
+  if constexpr (WIDE) {
     if (threadIdx.x % kWave == 0) {
 #pragma unroll
       for (int n = 0; n < N; ++n) slots[threadIdx.x / kWave][n] = v[n];
     }
     __syncthreads();
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-      v[n] = 0.0f;
+    for (int n = 0; n < N; ++n) v[n] = 0.0f;
+    for (int w = 0; w < lanes / kWave; ++w) {
 #pragma unroll
-      for (int w = 0; w < WAVES; ++w) v[n] += slots[w][n];
+      for (int n = 0; n < N; ++n) v[n] += slots[w][n];
     }
   }
 }
 
-// Rows of up to 64 lanes have 256 lanes' workgroups together; longer ones a workgroup of WAVES wavefronts each.
-template <int WAVES> constexpr int kLanes = WAVES > 1 ? WAVES * kWave : kBlock;
+// Rows of up to 64 lanes have 256 lanes' workgroups together; longer ones a workgroup of as many wavefronts as they need.
+template <bool WIDE> constexpr int kMostLanes = WIDE ? kMostWaves * kWave : kBlock;
 
 // A single-precision mean is off by some 2^-24 of itself; where results have as many bits, the mean of the deviations takes that away again.
 template <class T> constexpr bool kTwice = sizeof(T) == 4;
 
-template <class T, bool VEC, int WAVES, int C> __global__ __launch_bounds__(kLanes<WAVES>) void layer_norm_kernel(const LayerArgs a, uint32_t first) {
+template <class T, bool VEC, bool WIDE, int C> __global__ __launch_bounds__(kMostLanes<WIDE>) void layer_norm_kernel(const LayerArgs a, uint32_t first) {
   warm_arguments<LayerArgs>();
-  __shared__ float means[WAVES][1], squares[WAVES][2];
-  const int lanes = WAVES > 1 ? kLanes<WAVES> : 1 << a.lanes_log2, lane = threadIdx.x & (lanes - 1), width = a.width;
+  __shared__ float means[WIDE ? kMostWaves : 1][1], squares[WIDE ? kMostWaves : 1][2];
+  const int lanes = WIDE ? (int)blockDim.x : 1 << a.lanes_log2, lane = WIDE ? (int)threadIdx.x : (int)threadIdx.x & (lanes - 1), width = a.width;
   const Place<VEC> p(lane, lanes);
-  const uint32_t row = WAVES > 1 ? first + blockIdx.x : (first + blockIdx.x) * (kBlock >> a.lanes_log2) + (threadIdx.x >> a.lanes_log2);
+  const uint32_t row = WIDE ? first + blockIdx.x : (first + blockIdx.x) * (kBlock >> a.lanes_log2) + (threadIdx.x >> a.lanes_log2);
   const bool mine = row < a.lead.tokens;
   const char *from = a.x + row_offset(a.lead, a.xl, mine ? row : 0);
   eight_t<T> x[C];
@@ -142,7 +142,7 @@ template <class T, bool VEC, int WAVES, int C> __global__ __launch_bounds__(kLan
   for (int c = 0; c < C; ++c)
 #pragma unroll
     for (int i = 0; i < kEight; ++i) m[0] += (float)x[c][i];
-  sums_over_row<WAVES, 1>(m, lanes, means);
+  sums_over_row<WIDE, 1>(m, lanes, means);
   float mean = m[0] * a.over;
   float s[2] = {0.0f, 0.0f};
 #pragma unroll
@@ -153,7 +153,7 @@ template <class T, bool VEC, int WAVES, int C> __global__ __launch_bounds__(kLan
       s[0] = __builtin_fmaf(d, d, s[0]);
       if (kTwice<T>) s[1] += d;
     }
-  sums_over_row<WAVES, 2>(s, lanes, squares);
+  sums_over_row<WIDE, 2>(s, lanes, squares);
   const float rest = kTwice<T> ? s[1] * a.over : 0.0f;
   const float r = __builtin_amdgcn_rsqf(__builtin_fmaf(-rest, rest, s[0] * a.over) + a.eps);
   if (!mine) return;
@@ -173,42 +173,44 @@ template <class T, bool VEC, int WAVES, int C> __global__ __launch_bounds__(kLan
 }
 
 // The gradient.  A lane keeps the sums of its channels over all rows of its workgroup, workgroups leave theirs in the workspace, and a second launch adds them
-// up in a fixed order: no atomics, the same bits every time.  The next row is on its way while one is worked on.
-template <class T, bool VEC, int WAVES, int C> __global__ __launch_bounds__(kLanes<WAVES>) void layer_grad_kernel(const LayerArgs a) {
+// up in a fixed order: no atomics, the same bits every time.  The next rows are on their way while one is worked on, as far as there are registers for them.
+template <bool WIDE, int C> constexpr int kRowsAhead = C == 1 ? 2 : WIDE ? 0 : 1;
+
+template <class T, bool VEC, bool WIDE, int C> __global__ __launch_bounds__(kMostLanes<WIDE>) void layer_grad_kernel(const LayerArgs a) {
   warm_arguments<LayerArgs>();
-  __shared__ float means[WAVES][1], squares[WAVES][4];
-  const int lanes = WAVES > 1 ? kLanes<WAVES> : 1 << a.lanes_log2, lane = threadIdx.x & (lanes - 1), width = a.width;
+  __shared__ float means[WIDE ? kMostWaves : 1][1], squares[WIDE ? kMostWaves : 1][4];
+  const int lanes = WIDE ? (int)blockDim.x : 1 << a.lanes_log2, lane = WIDE ? (int)threadIdx.x : (int)threadIdx.x & (lanes - 1), width = a.width;
   const Place<VEC> p(lane, lanes);
-  const uint32_t rows = WAVES > 1 ? 1 : kBlock >> a.lanes_log2, mine = WAVES > 1 ? 0 : threadIdx.x >> a.lanes_log2;
+  const uint32_t rows = WIDE ? 1 : kBlock >> a.lanes_log2, mine = WIDE ? 0 : threadIdx.x >> a.lanes_log2;
   float gw[C * kEight], gb[C * kEight];
 #pragma unroll
   for (int i = 0; i < C * kEight; ++i) gw[i] = gb[i] = 0.0f;
-  eight_t<T> x[C], g[C];
-  const auto load = [&](uint32_t row) {
+  constexpr int AHEAD = kRowsAhead<WIDE, C>;
+  eight_t<T> x[AHEAD + 1][C], g[AHEAD + 1][C];       // this row and the next ones
+  const auto load = [&](uint64_t base, int u) {
+    const uint64_t row = base + mine;
     const bool in = row < a.lead.tokens;
-    const char *px = a.x + row_offset(a.lead, a.xl, in ? row : 0), *pg = a.g + row_offset(a.lead, a.gl, in ? row : 0);
+    const char *px = a.x + row_offset(a.lead, a.xl, in ? (uint32_t)row : 0), *pg = a.g + row_offset(a.lead, a.gl, in ? (uint32_t)row : 0);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      x[c] = load_chunk<T, VEC>(px, a.xe, p, c, in ? width : 0);
-      g[c] = load_chunk<T, VEC>(pg, a.ge, p, c, in ? width : 0);
+      x[u][c] = load_chunk<T, VEC>(px, a.xe, p, c, in ? width : 0);
+      g[u][c] = load_chunk<T, VEC>(pg, a.ge, p, c, in ? width : 0);
     }
   };
-  load(blockIdx.x * rows + mine);
-  // (uint64_t: rows past the last may pass 32 bits)
-  for (uint64_t base = (uint64_t)blockIdx.x * rows; base < a.lead.tokens; base += (uint64_t)gridDim.x * rows) {
+  const uint64_t step = (uint64_t)gridDim.x * rows;       // (rows past the last may pass 32 bits)
+#pragma unroll
+  for (int u = 0; u < AHEAD; ++u) load((uint64_t)blockIdx.x * rows + u * step, u);
+  for (uint64_t base = (uint64_t)blockIdx.x * rows; base < a.lead.tokens; base += step) {
     const uint32_t row = (uint32_t)base + mine;
     const bool in = row < a.lead.tokens;
-    eight_t<T> x0[C], g0[C];
-#pragma unroll
-    for (int c = 0; c < C; ++c) x0[c] = x[c], g0[c] = g[c];
-    const uint64_t next = base + (uint64_t)gridDim.x * rows;
-    if (next < a.lead.tokens) load((uint32_t)next + mine);
+    load(base + AHEAD * step, AHEAD);
+    const eight_t<T> *const x0 = x[0], *const g0 = g[0];
     float m[1] = {0.0f};
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
       for (int i = 0; i < kEight; ++i) m[0] += (float)x0[c][i];
-    sums_over_row<WAVES, 1>(m, lanes, means);
+    sums_over_row<WIDE, 1>(m, lanes, means);
     const float mean = m[0] * a.over;
     float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};       // of d^2, h, h d, d
 #pragma unroll
@@ -224,7 +226,7 @@ template <class T, bool VEC, int WAVES, int C> __global__ __launch_bounds__(kLan
         if (kTwice<T>) s[3] += d;
       }
     }
-    sums_over_row<WAVES, 4>(s, lanes, squares);
+    sums_over_row<WIDE, 4>(s, lanes, squares);
     const float rest = kTwice<T> ? s[3] * a.over : 0.0f;
     const float r = __builtin_amdgcn_rsqf(__builtin_fmaf(-rest, rest, s[0] * a.over) + a.eps);
     const float all = s[1] * a.over, along = __builtin_fmaf(-rest, s[1], s[2]) * a.over * r;
@@ -246,10 +248,14 @@ template <class T, bool VEC, int WAVES, int C> __global__ __launch_bounds__(kLan
         store_chunk<T, VEC>(to, a.oe, p, c, width, v, a.stream);
       }
     }
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+      for (int c = 0; c < C; ++c) x[u][c] = x[u + 1][c], g[u][c] = g[u + 1][c];
   }
   if (!a.partial) return;
   float *const partial = a.partial + (int64_t)blockIdx.x * 2 * width;
-  if constexpr (WAVES > 1) {
+  if constexpr (WIDE) {
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
@@ -315,18 +321,18 @@ int done(hipError_t e) {
   return OCN_ERR_LAUNCH;
 }
 
-// How rows go to lanes: chunks of eight channels, wavefronts of a row and chunks of a lane.  Up to 2048 channels a row stays inside a wavefront.
+// How rows go to lanes: wavefronts of a row (1: a row has 2^lanes_log2 lanes of one), and chunks of eight channels of a lane.  Forward a lane has two chunks of a long row, so that enough
+// is on its way; backward, where it keeps sums of its channels and the next rows, one up to 8192 channels.
 struct Shape { int waves, chunks, lanes_log2; };
-Shape shape_of(int64_t width) {
+Shape shape_of(int64_t width, bool grad) {
   int64_t lanes = 1;
   int log2 = 0;
   while (lanes * kEight < width && lanes < kWave) lanes *= 2, ++log2;
   if (width <= lanes * kEight) return {1, 1, log2};
-  if (width <= 1024) return {1, 2, 6};
-  if (width <= 2048) return {1, 4, 6};
-  if (width <= 4096) return {4, 2, 6};
-  if (width <= 8192) return {4, 4, 6};
-  return {16, 2, 6};
+  const int64_t chunk = kWave * kEight;
+  if (width <= (grad ? 2 : 4) * chunk) return {1, (int)((width + chunk - 1) / chunk), 6};
+  const int chunks = grad && width <= kMostWaves * chunk ? 1 : 2;
+  return {(int)((width + chunks * chunk - 1) / (chunks * chunk)), chunks, 6};
 }
 
 int64_t rows_of(const ocn_tensor *t) {
@@ -338,7 +344,7 @@ int64_t width_of(const ocn_tensor *t) { return t->size[t->ndim - 1]; }
 
 // workgroups of the gradient: as many as leave their sums a small part of what is read (twice as many where rows are short)
 int64_t workers_of(int64_t rows, int64_t width) {
-  const Shape s = shape_of(width);
+  const Shape s = shape_of(width, true);
   const int64_t at_once = s.waves > 1 ? 1 : kBlock >> s.lanes_log2, most = width <= 2048 ? 1024 : 512;
   const int64_t want = (rows + at_once - 1) / at_once, rounds = std::max<int64_t>(1, (want + most - 1) / most);
   return std::max<int64_t>(1, (want + rounds - 1) / rounds);
@@ -395,28 +401,34 @@ int fill(LayerArgs &a, const ocn_tensor *x, const ocn_tensor *g, const ocn_tenso
   if (weight) a.weight = start_of(weight), a.weight_stride = weight->stride[0], a.weight_type = weight->dtype, a.weight_whole = whole(weight);
   if (bias) a.bias = start_of(bias), a.bias_stride = bias->stride[0], a.bias_type = bias->dtype, a.bias_whole = whole(bias);
   a.width = (int32_t)width_of(x);
-  a.lanes_log2 = shape_of(a.width).lanes_log2;
+  a.lanes_log2 = shape_of(a.width, g != nullptr).lanes_log2;
   a.over = a.width ? 1.0f / (float)a.width : 0.0f;
   a.eps = (float)eps;
   a.stream = (int64_t)a.lead.tokens * a.width * head_type_size(out->dtype) >= kStreamBytes;
   return OCN_OK;
 }
 
-// CALL(type, whole vectors, wavefronts of a row, chunks of a lane)
-#define OCN_LAYER_SHAPES(T, VEC, s, CALL)                    \
+// CALL(type, whole vectors, whether a row has several wavefronts, chunks of a lane)
+#define OCN_NORM_SHAPES(T, VEC, s, CALL)                     \
   do {                                                       \
-    if ((s).waves == 16) CALL(T, VEC, 16, 2);                \
-    else if ((s).waves == 4 && (s).chunks == 4) CALL(T, VEC, 4, 4); \
-    else if ((s).waves == 4) CALL(T, VEC, 4, 2);             \
-    else if ((s).chunks == 4) CALL(T, VEC, 1, 4);            \
-    else if ((s).chunks == 2) CALL(T, VEC, 1, 2);            \
-    else CALL(T, VEC, 1, 1);                                 \
+    if ((s).waves > 1) CALL(T, VEC, true, 2);                \
+    else if ((s).chunks == 4) CALL(T, VEC, false, 4);        \
+    else if ((s).chunks == 3) CALL(T, VEC, false, 3);        \
+    else if ((s).chunks == 2) CALL(T, VEC, false, 2);        \
+    else CALL(T, VEC, false, 1);                             \
   } while (0)
-#define OCN_LAYER_TYPES(dtype, vec, s, CALL)                                       \
+#define OCN_GRAD_SHAPES(T, VEC, s, CALL)                     \
+  do {                                                       \
+    if ((s).waves > 1 && (s).chunks == 1) CALL(T, VEC, true, 1); \
+    else if ((s).waves > 1) CALL(T, VEC, true, 2);           \
+    else if ((s).chunks == 2) CALL(T, VEC, false, 2);        \
+    else CALL(T, VEC, false, 1);                             \
+  } while (0)
+#define OCN_LAYER_TYPES(SHAPES, dtype, vec, s, CALL)                                       \
   do {                                                                             \
-    if ((dtype) == OCN_HALF) { if (vec) OCN_LAYER_SHAPES(f16, true, s, CALL); else OCN_LAYER_SHAPES(f16, false, s, CALL); } \
-    else if ((dtype) == OCN_BFLOAT16) { if (vec) OCN_LAYER_SHAPES(bf16, true, s, CALL); else OCN_LAYER_SHAPES(bf16, false, s, CALL); } \
-    else { if (vec) OCN_LAYER_SHAPES(float, true, s, CALL); else OCN_LAYER_SHAPES(float, false, s, CALL); } \
+    if ((dtype) == OCN_HALF) { if (vec) SHAPES(f16, true, s, CALL); else SHAPES(f16, false, s, CALL); } \
+    else if ((dtype) == OCN_BFLOAT16) { if (vec) SHAPES(bf16, true, s, CALL); else SHAPES(bf16, false, s, CALL); } \
+    else { if (vec) SHAPES(float, true, s, CALL); else SHAPES(float, false, s, CALL); } \
   } while (0)
 
 }  // namespace
@@ -435,15 +447,15 @@ int ocn_layer_norm(const ocn_tensor *x, const ocn_tensor *weight, const ocn_tens
   LayerArgs a;
   if ((rc = fill(a, x, nullptr, weight, bias, out, eps)) != OCN_OK) return rc;
   if (a.width == 0 || a.lead.tokens == 0) return OCN_OK;
-  const Shape s = shape_of(a.width);
+  const Shape s = shape_of(a.width, false);
   const uint32_t at_once = s.waves > 1 ? 1 : kBlock >> s.lanes_log2;
   const int64_t blocks = ((int64_t)a.lead.tokens + at_once - 1) / at_once;
   const bool vec = whole(x) && whole(out);
   for (int64_t at = 0; at < blocks; at += max_launch_blocks()) {
     const uint32_t grid = (uint32_t)std::min<int64_t>(blocks - at, max_launch_blocks()), first = (uint32_t)at;
-#define OCN_LAYER(T, VEC, WAVES, C) \
-  hipLaunchKernelGGL((layer_norm_kernel<T, VEC, WAVES, C>), dim3(grid), dim3(kLanes<WAVES>), 0, (hipStream_t)stream, a, first)
-    OCN_LAYER_TYPES(x->dtype, vec, s, OCN_LAYER);
+#define OCN_LAYER(T, VEC, WIDE, C) \
+  hipLaunchKernelGGL((layer_norm_kernel<T, VEC, WIDE, C>), dim3(grid), dim3(WIDE ? s.waves * kWave : kBlock), 0, (hipStream_t)stream, a, first)
+    OCN_LAYER_TYPES(OCN_NORM_SHAPES, x->dtype, vec, s, OCN_LAYER);
 #undef OCN_LAYER
     if ((rc = done(hipGetLastError())) != OCN_OK) return rc;
   }
@@ -478,11 +490,11 @@ int ocn_layer_norm_grad(const ocn_tensor *gout, const ocn_tensor *x, const ocn_t
   } else if (a.lead.tokens == 0) {
     return OCN_OK;
   }
-  const Shape s = shape_of(a.width);
+  const Shape s = shape_of(a.width, true);
   const bool vec = whole(x) && whole(gout) && whole(gin);
-#define OCN_LAYER(T, VEC, WAVES, C) \
-  hipLaunchKernelGGL((layer_grad_kernel<T, VEC, WAVES, C>), dim3((uint32_t)workers), dim3(kLanes<WAVES>), 0, (hipStream_t)stream, a)
-  OCN_LAYER_TYPES(x->dtype, vec, s, OCN_LAYER);
+#define OCN_LAYER(T, VEC, WIDE, C) \
+  hipLaunchKernelGGL((layer_grad_kernel<T, VEC, WIDE, C>), dim3((uint32_t)workers), dim3(WIDE ? s.waves * kWave : kBlock), 0, (hipStream_t)stream, a)
+  OCN_LAYER_TYPES(OCN_GRAD_SHAPES, x->dtype, vec, s, OCN_LAYER);
 #undef OCN_LAYER
   if ((rc = done(hipGetLastError())) != OCN_OK || !sums) return rc;
   LayerFoldArgs f;
