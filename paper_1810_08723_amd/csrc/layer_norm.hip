@@ -182,9 +182,11 @@ template <class T, bool VEC, bool WIDE, int C> __global__ __launch_bounds__(kMos
   const int lanes = WIDE ? (int)blockDim.x : 1 << a.lanes_log2, lane = WIDE ? (int)threadIdx.x : (int)threadIdx.x & (lanes - 1), width = a.width;
   const Place<VEC> p(lane, lanes);
   const uint32_t rows = WIDE ? 1 : kBlock >> a.lanes_log2, mine = WIDE ? 0 : threadIdx.x >> a.lanes_log2;
-  float gw[C * kEight], gb[C * kEight];
+  float gw[C * kEight], gb[C * kEight], w[C][kEight];       // (weights stay: loads of theirs, which arrive in order, would wait for the rows ahead)
 #pragma unroll
   for (int i = 0; i < C * kEight; ++i) gw[i] = gb[i] = 0.0f;
+#pragma unroll
+  for (int c = 0; c < C; ++c) load_factors<VEC>(a.weight, a.weight_stride, a.weight_type, a.weight_whole, p, c, width, 1.0f, w[c]);
   constexpr int AHEAD = kRowsAhead<WIDE, C>;
   eight_t<T> x[AHEAD + 1][C], g[AHEAD + 1][C];       // this row and the next ones
   const auto load = [&](uint64_t base, int u) {
@@ -215,11 +217,9 @@ template <class T, bool VEC, bool WIDE, int C> __global__ __launch_bounds__(kMos
     float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};       // of d^2, h, h d, d
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      float w[kEight];
-      load_factors<VEC>(a.weight, a.weight_stride, a.weight_type, a.weight_whole, p, c, width, 1.0f, w);
 #pragma unroll
       for (int i = 0; i < kEight; ++i) {
-        const float d = p.at(c, i) < width ? (float)x0[c][i] - mean : 0.0f, h = (float)g0[c][i] * w[i];
+        const float d = p.at(c, i) < width ? (float)x0[c][i] - mean : 0.0f, h = (float)g0[c][i] * w[c][i];
         s[0] = __builtin_fmaf(d, d, s[0]);
         s[1] += h;
         s[2] = __builtin_fmaf(h, d, s[2]);
@@ -234,8 +234,7 @@ template <class T, bool VEC, bool WIDE, int C> __global__ __launch_bounds__(kMos
       char *to = a.out + row_offset(a.lead, a.ol, row);
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        float w[kEight], v[kEight];
-        load_factors<VEC>(a.weight, a.weight_stride, a.weight_type, a.weight_whole, p, c, width, 1.0f, w);
+        float v[kEight];
 #pragma unroll
         for (int i = 0; i < kEight; ++i) {
           float d = (float)x0[c][i] - mean;
@@ -243,7 +242,7 @@ template <class T, bool VEC, bool WIDE, int C> __global__ __launch_bounds__(kMos
           const float u = d * r, gg = (float)g0[c][i];
           gw[c * kEight + i] = __builtin_fmaf(gg, u, gw[c * kEight + i]);
           gb[c * kEight + i] += gg;
-          v[i] = r * (__builtin_fmaf(gg, w[i], -all) - u * along);
+          v[i] = r * (__builtin_fmaf(gg, w[c][i], -all) - u * along);
         }
         store_chunk<T, VEC>(to, a.oe, p, c, width, v, a.stream);
       }
