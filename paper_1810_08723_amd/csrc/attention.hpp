@@ -30,6 +30,7 @@ struct AttentionArgs {
   float scale, plain_scale, true_scale;    // of scores: to powers of two and to those of e, as magnitudes; as it is
   // blocks of a sequence: of `tokens` queries (keys, where a block has keys), and of `heads` query heads of a group
   int32_t heads, head_blocks, tokens, splits;
+  int32_t rows;                            // of a block
   int32_t rows_of_tile;                    // gradients of keys: queries that a tile of rows has
   uint32_t slots, per_sequence;            // of all sequences; of one, where they are not packed
   FastDiv heads_div, head_blocks_div, across_div, tokens_div, splits_div, sequences_div;
@@ -60,7 +61,7 @@ int64_t units_of(const AttentionSizes &s, int64_t rows);
 int64_t key_units_of(const AttentionSizes &s, int64_t keys);
 // Sets what find_work goes by; false where there are too many
 bool set_blocks(AttentionArgs &a, const AttentionSizes &s, int64_t rows, int64_t splits);
-bool set_key_blocks(AttentionArgs &a, const AttentionSizes &s, int64_t keys);
+bool set_key_blocks(AttentionArgs &a, const AttentionSizes &s, int64_t keys, int64_t splits);
 
 // channels that kernels are made for
 inline int padded_channels(int64_t d) { return d <= 64 ? 64 : d <= 96 ? 96 : d <= 128 ? 128 : d <= 192 ? 192 : 256; }
@@ -69,6 +70,7 @@ inline int padded_channels(int64_t d) { return d <= 64 ? 64 : d <= 96 ? 96 : d <
 // sequence's keys go to, units.
 constexpr int kFewWaves = 4;
 constexpr int kLeastTiles = 2 * kFewWaves;        // tiles of keys of a part, at least
+constexpr int kLeastRowTiles = 3;                 // ... where rows are many, and tiles larger
 struct AttentionPlan { bool few; int waves, rows, splits; int64_t units; };      // waves: of a workgroup
 int run_attention_half(AttentionArgs &a, const AttentionPlan &p, bool vec, void *stream);
 int run_attention_bfloat16(AttentionArgs &a, const AttentionPlan &p, bool vec, void *stream);
@@ -83,7 +85,11 @@ int64_t slots_of_key_units(const AttentionSizes &s, int64_t keys);
 // The gradient: rows (query heads of all tokens), and which gradients are wanted
 constexpr int kGradWaves = 4;
 struct AttentionGrad { int64_t rows; bool keys, queries; };
-inline int grad_key_waves(int32_t dtype, int64_t channels) { return dtype != OCN_FLOAT && (padded_channels(channels) == 96 || padded_channels(channels) == 128) ? 8 : 4; }
+// ... wavefronts and parts of a block of keys
+size_t grad_head_bytes(const AttentionSizes &s, int side, int waves);       // of the workspace before what parts leave
+struct KeyPlan { int waves, splits; int64_t units; };
+KeyPlan key_plan_of(const AttentionSizes &s, int32_t dtype, int64_t channels);
+constexpr int kLeastKeyTiles = 4;        // tiles of rows of a part, at least
 int run_attention_grad_half(AttentionArgs &a, const AttentionSizes &s, const AttentionGrad &p, bool vec, void *workspace, void *stream);
 int run_attention_grad_bfloat16(AttentionArgs &a, const AttentionSizes &s, const AttentionGrad &p, bool vec, void *workspace, void *stream);
 int run_attention_grad_float(AttentionArgs &a, const AttentionSizes &s, const AttentionGrad &p, bool vec, void *workspace, void *stream);

@@ -25,13 +25,12 @@ template <class T> constexpr float kWeightTop = std::is_same<T, f16>::value ? 12
 template <class T> struct Range {
   static constexpr bool kNeeded = std::is_same<T, f16>::value;
   float factor = kNeeded ? 0.0f : 1.0f;
+  __device__ __forceinline__ bool passes(float largest) const { return largest * factor > 32768.0f || (factor == 0.0f && largest > 0.0f); }
   // what sums so far are to be multiplied by
   __device__ __forceinline__ bool lower(float largest, float *keep) {
     if constexpr (!kNeeded) return false;
-    const bool mine = largest * factor > 32768.0f || (factor == 0.0f && largest > 0.0f);
-    if (!__any(mine)) return false;
     *keep = 1.0f;
-    if (mine) {
+    if (passes(largest)) {
       int e = 12 - __builtin_amdgcn_frexp_expf(largest);
       e = e > 120 ? 120 : e < -120 ? -120 : e;
       const float f = __builtin_ldexpf(1.0f, e);
@@ -57,7 +56,7 @@ template <class T, int TILES, class Out> __device__ __forceinline__ void in_rang
     for (int t = 0; t < TILES; ++t)
 #pragma unroll
       for (int i = 0; i < Tile<T>::kOwn; ++i) largest = fmaxf(largest, __builtin_fabsf(s[t][i]));
-    if (range.lower(column_max<T>(largest), &keep)) {
+    if (__any(range.passes(largest)) && range.lower(column_max<T>(largest), &keep)) {
 #pragma unroll
       for (int ct = 0; ct < outs; ++ct)
 #pragma unroll
@@ -70,30 +69,16 @@ template <class T, int TILES, class Out> __device__ __forceinline__ void in_rang
   }
 }
 
-// four neighbouring channels of a row, rounded
-template <class T, bool VEC> __device__ __forceinline__ void store_run(char *row, int64_t step, int e, int d, const float *v) {
-  if constexpr (VEC) {
-    typedef T V __attribute__((ext_vector_type(4)));
-    V o;
+// (of results of TILE's products, in type T)
+template <class T, int D, bool VEC, class TILE = Tile<T>> __device__ __forceinline__ void store_columns(const typename TILE::Acc *acc, char *row, int64_t step, int h, int d, float factor) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = (T)v[i];
-    if (e < d) *(V *)(row + e * (int)sizeof(T)) = o;
-  } else {
+  for (int ct = 0; ct < D / TILE::kSide; ++ct)
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (e + i < d) *(T *)(row + (e + i) * step) = (T)v[i];
-  }
-}
-
-template <class T, int D, bool VEC> __device__ __forceinline__ void store_columns(const acc_t<T> *acc, char *row, int64_t step, int h, int d, float factor) {
-#pragma unroll
-  for (int ct = 0; ct < D / Tile<T>::kSide; ++ct)
-#pragma unroll
-    for (int i = 0; i < Tile<T>::kOwn; i += 4) {
+    for (int i = 0; i < TILE::kOwn; i += 4) {
       float v[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] = acc[ct][i + e] * factor;
-      store_run<T, VEC>(row, step, ct * Tile<T>::kSide + own_index<T>(i) + 4 * h, d, v);
+      store_four<T, VEC>(row, step, ct * TILE::kSide + own_index<T>(i) + 4 * h, d, v);
     }
 }
 
@@ -116,6 +101,22 @@ template <class T> __device__ __forceinline__ acc_t<T> no_sum() {
   return a;
 }
 
+// Queries that see some key of a block (query i sees the keys before i - ahead + 1), from a multiple of a tile's on, and the tiles that they make
+struct KeyRows { int lo, hi, end, ahead, across, tiles; };
+__device__ __forceinline__ KeyRows key_rows(const AttentionArgs &a, const Work &w, int block, int keys) {
+  KeyRows r;
+  r.end = block + keys < w.k.count ? block + keys : w.k.count;
+  r.ahead = w.q.count - w.k.count;
+  r.lo = 0, r.hi = w.q.count;
+  if (a.causal) {
+    r.lo = block + r.ahead > 0 ? (block + r.ahead) / a.rows_of_tile * a.rows_of_tile : 0;
+    if (a.window && (int64_t)r.end - 1 + a.window + r.ahead < r.hi) r.hi = r.end - 1 + a.window + r.ahead;
+  }
+  r.across = (a.per_kv + a.heads - 1) / a.heads;         // tiles that a query's heads take
+  r.tiles = r.hi > r.lo ? (r.hi - 1 - r.lo) / a.rows_of_tile * r.across + r.across : 0;
+  return r;
+}
+
 // Gradients of keys and values: a wavefront has a tile's side of keys, in registers, with the sums for them (values, where registers are short, lie in LDS); rows go through
 // LDS, the next ones on their way: some whole queries with the query heads of the group, or some of those.
 template <int D> constexpr bool kValuesHeld = D > 64;
@@ -134,7 +135,11 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
   const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), n = lane & (SIDE - 1), h = lane / SIDE;
   Work w;
   if (!find_work_of<true>(a, first_block + blockIdx.x, &w)) return;
-  const int block = (int)(w.block * (uint32_t)BLOCK), key = block + wave * SIDE + n, end = block + BLOCK < w.k.count ? block + BLOCK : w.k.count;
+  const int block = (int)(w.block * (uint32_t)BLOCK), key = block + wave * SIDE + n;
+  const KeyRows rows = key_rows(a, w, block, BLOCK);
+  const int end = rows.end, ahead = rows.ahead, lo = rows.lo, hi = rows.hi, across = rows.across;
+  const Part part_here = part_of(rows.tiles, a.splits, kLeastKeyTiles, w.split);
+  if (!part_here.mine) return;
   const bool mine = key < w.k.count;
   const int64_t token = w.k.first + (mine ? key : 0);
   if (VEC && a.channels < D) {
@@ -142,14 +147,6 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
     if (HELD) clear_lds<WAVES * kWave>(values, sizeof values);
     __syncthreads();
   }
-  // queries that see some key of the workgroup's; query i sees the keys before i - ahead + 1
-  const int ahead = w.q.count - w.k.count;
-  int lo = 0, hi = w.q.count;
-  if (a.causal) {
-    lo = block + ahead > 0 ? (block + ahead) / a.rows_of_tile * a.rows_of_tile : 0;
-    if (a.window && (int64_t)end - 1 + a.window + ahead < hi) hi = end - 1 + a.window + ahead;
-  }
-  const int across = (a.per_kv + a.heads - 1) / a.heads;         // tiles that a query's heads take
   const int64_t head = (int64_t)w.kv * a.per_kv, heads = (int64_t)a.kv * a.per_kv;
   const char *const pq = a.q.base + w.sequence * a.q.batch + w.q.first * a.q.token + head * a.q.head;
   const char *const pg = a.gout.base + w.sequence * a.gout.batch + w.q.first * a.gout.token + head * a.gout.head;
@@ -179,14 +176,15 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
     cg.store(held + (turn * 2 + 1) * SIDE * PITCH);
   };
   // From the last rows to the first: workgroups with other keys of a sequence, which start at other rows, then read the same ones at about the same time.
-  int at = hi > lo ? lo + (hi - 1 - lo) / a.rows_of_tile * a.rows_of_tile : lo - 1, part = across - 1, turn = 0;
+  int left = part_here.end - part_here.first, turn = 0;
+  int at = lo + (part_here.end - 1) / across * a.rows_of_tile, part = (part_here.end - 1) % across;
   if constexpr (HELD) {
     Carrier<T, D, BLOCK, WAVES, VEC> cv;
     const char *const pv = a.v.base + w.sequence * a.v.batch + w.k.first * a.v.token + (int64_t)w.kv * a.v.head;
     cv.load(values, [&](int i) { return pv + (int64_t)(block + i < end ? block + i : end - 1) * a.v.token; }, a.v.channel, a.channels);
     cv.store(values);
   }
-  if (at >= lo) load(at, part, 0);
+  if (left > 0) load(at, part, 0);
   frag_t<T> k[D / 16], v[HELD ? 1 : D / 16];
   load_fragments<T, D, VEC>(k, a.k.base + w.sequence * a.k.batch + token * a.k.token + w.kv * a.k.head, a.k.channel, mine && !a.nothing ? a.channels : 0, h, a.negative);
   if constexpr (!HELD)
@@ -195,7 +193,7 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
 #pragma unroll
   for (int ct = 0; ct < D / SIDE; ++ct) gk[ct] = gv[ct] = no_sum<T>();
   Range<T> range;
-  if (at >= lo) store(0);
+  if (left > 0) store(0);
   const int from = block + wave * SIDE;
   const LanePlaces at_start = lane_places<T, D>(lane);
   const auto step = [&](auto masked, auto turn) {
@@ -205,7 +203,7 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
     const int first_end = a.causal ? at - ahead + 1 : 0x7fffff00, last_end = first_end + a.rows_of_tile - 1;
     int next = at, next_part = part - 1;
     if (next_part < 0) next -= a.rows_of_tile, next_part = across - 1;
-    if (next >= lo) load(next, next_part, turn ^ 1);
+    if (left > 1) load(next, next_part, turn ^ 1);
     if (!masked || (from < last_end && (!a.window || from + SIDE > first_end - a.window))) {
       int here = h;
       LanePlaces places = at_start;
@@ -251,31 +249,67 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
                                           else gk[ct] = product(x, slopes[(i - EACH) / TILES], gk[ct]);
                                         });
     }
-    if (next >= lo) store(turn ^ 1);
-    at = next, part = next_part;
+    if (left > 1) store(turn ^ 1);
+    at = next, part = next_part, --left;
   };
   // Rows that see all of the workgroup's keys have a loop of their own
   const int first_whole = a.causal ? end - 1 + ahead : lo, past_whole = a.window ? block + a.window + ahead : 0x7fffffff;      // (rows past the last have no weights)
-  const auto is_whole = [&](int t) { return t >= lo && t >= first_whole && t <= past_whole - a.rows_of_tile; };
-  while (at >= lo) {
+  const auto is_whole = [&] { return left > 0 && at >= first_whole && at <= past_whole - a.rows_of_tile; };
+  while (left > 0) {
     if (turn == 0)      // two at a time, so that where they lie is known
-      while (is_whole(at) && is_whole(at - (across == 1 ? a.rows_of_tile : 0))) {
+      while (left > 1 && is_whole()) {
         step(std::false_type(), std::integral_constant<int, 0>());
-        if (!is_whole(at)) {
+        if (!is_whole()) {
           turn = 1;
           break;
         }
         step(std::false_type(), std::integral_constant<int, 1>());
       }
-    if (at >= lo) {
+    if (left > 0) {
       step(std::true_type(), turn);
       turn ^= 1;
     }
   }
   if (!mine) return;
   const float weight = kWeightTop<T> > 0.0f ? 0x1p-12f : 1.0f;
+  if (!part_here.alone) {
+    float *const to = a.parts + (((int64_t)w.unit * a.splits + w.split) * BLOCK + wave * SIDE + n) * (2 * D);
+    store_columns<float, D, true, Tile<T>>(gk, (char *)to, 4, h, D, weight * range.back());
+    store_columns<float, D, true, Tile<T>>(gv, (char *)(to + D), 4, h, D, weight);
+    return;
+  }
   store_columns<T, D, VEC>(gk, a.gk.base + w.sequence * a.gk.batch + token * a.gk.token + w.kv * a.gk.head, a.gk.channel, h, a.channels, a.true_scale * weight * range.back());
   store_columns<T, D, VEC>(gv, a.gv.base + w.sequence * a.gv.batch + token * a.gv.token + w.kv * a.gv.head, a.gv.channel, h, a.channels, weight);
+}
+
+// What parts of a block of keys came to, in their order: a wavefront to a key, lanes having channels.
+template <class T, int D> __global__ __launch_bounds__(kBlock) void attention_keys_join_kernel(const AttentionArgs a, uint32_t first, int keys) {
+  const int lane = threadIdx.x & (kWave - 1);
+  Work w;
+  const uint32_t chunks = (uint32_t)keys / kJoinRows, unit = (first + blockIdx.x) / chunks, chunk = first + blockIdx.x - unit * chunks;
+  if (!find_work_of<true>(a, unit * (uint32_t)a.splits, &w)) return;
+  const int block = (int)(w.block * (uint32_t)keys);
+  const KeyRows rows = key_rows(a, w, block, keys);
+  if (part_of(rows.tiles, a.splits, kLeastKeyTiles, 0).alone) return;
+  for (int n = (int)chunk * kJoinRows + threadIdx.x / kWave; n < (int)(chunk + 1) * kJoinRows && block + n < rows.end; n += kBlock / kWave) {
+    float gk[(D + kWave - 1) / kWave], gv[(D + kWave - 1) / kWave];
+#pragma unroll
+    for (int c = 0; c < (D + kWave - 1) / kWave; ++c) gk[c] = gv[c] = 0.0f;
+    for (int s = 0; s < a.splits && part_of(rows.tiles, a.splits, kLeastKeyTiles, s).mine; ++s) {
+      const float *const from = a.parts + (((int64_t)w.unit * a.splits + s) * keys + n) * (2 * D);
+#pragma unroll
+      for (int c = 0; c < (D + kWave - 1) / kWave; ++c)
+        if (c * kWave + lane < D) gk[c] += from[c * kWave + lane], gv[c] += from[D + c * kWave + lane];
+    }
+    const int64_t token = w.k.first + block + n;
+#pragma unroll
+    for (int c = 0; c < (D + kWave - 1) / kWave; ++c) {
+      const int e = c * kWave + lane;
+      if (e >= a.channels) continue;
+      *(T *)(a.gk.base + w.sequence * a.gk.batch + token * a.gk.token + w.kv * a.gk.head + e * a.gk.channel) = (T)(gk[c] * a.true_scale);
+      *(T *)(a.gv.base + w.sequence * a.gv.batch + token * a.gv.token + w.kv * a.gv.head + e * a.gv.channel) = (T)gv[c];
+    }
+  }
 }
 
 // Gradients of queries: a wavefront has a tile's side of rows, in registers, with the sums for them; keys and values go through LDS.
@@ -439,18 +473,20 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
 // host
 // ---------------------------------------------------------------------------------------
 
-// (of the pass over rows; with four of 96 or 128 channels what a lane loads of a tile and keeps for it takes more registers than there are)
-template <class T, int D> constexpr int kKeyWaves = sizeof(T) == 2 && (D == 96 || D == 128) ? 8 : 4;
+template <class T, int D> constexpr bool kWideKeys = sizeof(T) == 2 && (D == 96 || D == 128);
 template <class T> constexpr int kGradKeys = sizeof(T) == 2 ? 64 : 32;
+
+int done(hipError_t e) {
+  if (e == hipSuccess) return OCN_OK;
+  record_hip_error((int)e);
+  return OCN_ERR_LAUNCH;
+}
 
 template <class Launch> int in_launches(int64_t blocks, Launch launch) {
   for (int64_t at = 0; at < blocks; at += max_launch_blocks()) {
     launch((uint32_t)std::min<int64_t>(blocks - at, max_launch_blocks()), (uint32_t)at);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) {
-      record_hip_error((int)e);
-      return OCN_ERR_LAUNCH;
-    }
+    const int rc = done(hipGetLastError());
+    if (rc != OCN_OK) return rc;
   }
   return OCN_OK;
 }
@@ -459,18 +495,17 @@ template <class T, int D, bool VEC> int run_grad(AttentionArgs &a, const Attenti
   constexpr int side = Tile<T>::kSide;
   int rc = OCN_OK;
   const uint32_t rows = (uint32_t)p.rows;
-  constexpr int waves = kKeyWaves<T, D>;
+  const KeyPlan plan = key_plan_of(sizes, sizeof(T) == 4 ? OCN_FLOAT : OCN_HALF, D);
   AttentionArgs of_keys = a;
-  if (!set_blocks(a, sizes, side * kGradWaves, 1) || !set_key_blocks(of_keys, sizes, side * waves)) return OCN_ERR_SHAPE;
-  const int64_t units = units_of(sizes, side * kGradWaves), key_units = p.keys ? key_units_of(sizes, side * waves) : 0;
+  if (!set_blocks(a, sizes, side * kGradWaves, 1) || !set_key_blocks(of_keys, sizes, side * plan.waves, plan.splits)) return OCN_ERR_SHAPE;
+  const int64_t units = units_of(sizes, side * kGradWaves), key_units = p.keys ? plan.units : 0;
   uint32_t *const order = (uint32_t *)(stats + rows + 1);
   if (ordered(sizes, units)) a.order = order;
   if (ordered(sizes, key_units)) of_keys.order = order + slots_of_units(sizes, side * kGradWaves);
   if (a.order || of_keys.order) {
     hipLaunchKernelGGL(attention_order_kernel, dim3(2), dim3(kOrderLanes), 0, stream, a, BlockPlan{a.tokens, a.slots, a.tokens_div, a.order},
                        BlockPlan{of_keys.tokens, of_keys.slots, of_keys.tokens_div, of_keys.order});
-    rc = hipGetLastError() == hipSuccess ? OCN_OK : OCN_ERR_LAUNCH;
-    if (rc != OCN_OK) return rc;
+    if ((rc = done(hipGetLastError())) != OCN_OK) return rc;
   }
   rc = in_launches(units, [&](uint32_t grid, uint32_t first) {
     hipLaunchKernelGGL((attention_queries_kernel<T, D, VEC, kGradWaves, kGradKeys<T>>), dim3(grid), dim3(kGradWaves * kWave), 0, stream, a, first, stats, stats + rows);
@@ -480,8 +515,15 @@ template <class T, int D, bool VEC> int run_grad(AttentionArgs &a, const Attenti
   of_keys.heads = std::max(1, std::min(a.per_kv, side));
   of_keys.heads_div = make_fastdiv((uint32_t)of_keys.heads);
   of_keys.rows_of_tile = side / of_keys.heads;
-  rc = in_launches(key_units, [&](uint32_t grid, uint32_t first) {
-    hipLaunchKernelGGL((attention_keys_kernel<T, D, VEC, waves>), dim3(grid), dim3(waves * kWave), 0, stream, of_keys, first, stats, stats + rows);
+  of_keys.parts = (float *)((char *)stats + grad_head_bytes(sizes, side, plan.waves));
+  rc = in_launches(key_units * plan.splits, [&](uint32_t grid, uint32_t first) {
+    constexpr int wide = kWideKeys<T, D> ? 8 : 4;
+    if (plan.waves == wide) hipLaunchKernelGGL((attention_keys_kernel<T, D, VEC, wide>), dim3(grid), dim3(wide * kWave), 0, stream, of_keys, first, stats, stats + rows);
+    else hipLaunchKernelGGL((attention_keys_kernel<T, D, VEC, 4>), dim3(grid), dim3(4 * kWave), 0, stream, of_keys, first, stats, stats + rows);
+  });
+  if (rc != OCN_OK || plan.splits == 1) return rc;
+  rc = in_launches(key_units * (side * plan.waves / kJoinRows), [&](uint32_t grid, uint32_t first) {
+    hipLaunchKernelGGL((attention_keys_join_kernel<T, D>), dim3(grid), dim3(kBlock), 0, stream, of_keys, first, side * plan.waves);
   });
   return rc;
 }

@@ -172,13 +172,40 @@ static bool set_all(AttentionArgs &a, const AttentionSizes &s, int64_t all, int6
   return true;
 }
 
+size_t grad_head_bytes(const AttentionSizes &s, int side, int waves) {
+  const size_t n = (size_t)(s.queries * s.kv * s.per_kv + 1) * 2 * sizeof(float) +
+                   (size_t)(slots_of_units(s, side * kGradWaves) + slots_of_key_units(s, side * waves)) * sizeof(uint32_t);
+  return (n + 255) / 256 * 256;
+}
+
 bool set_blocks(AttentionArgs &a, const AttentionSizes &s, int64_t rows, int64_t splits) {
   const int64_t heads = heads_of_block(s, rows);
   return set_all(a, s, s.queries, heads, std::max<int64_t>(1, (s.per_kv + heads - 1) / heads), rows / heads, splits);
 }
-bool set_key_blocks(AttentionArgs &a, const AttentionSizes &s, int64_t keys) { return set_all(a, s, s.keys, std::max<int64_t>(1, s.per_kv), 1, keys, 1); }
+bool set_key_blocks(AttentionArgs &a, const AttentionSizes &s, int64_t keys, int64_t splits) {
+  return set_all(a, s, s.keys, std::max<int64_t>(1, s.per_kv), 1, keys, splits);
+}
+
+constexpr int64_t kSplitKeyWorkgroups = 512;      // that few blocks of keys are cut into
+constexpr int64_t kShortKeys = 128;               // sequences of so many keys on average have blocks of four wavefronts
+
+KeyPlan key_plan_of(const AttentionSizes &s, int32_t dtype, int64_t channels) {
+  const int side = dtype == OCN_FLOAT ? 16 : 32, d = padded_channels(channels);
+  KeyPlan p;
+  p.waves = dtype != OCN_FLOAT && (d == 96 || d == 128) && s.keys > kShortKeys * s.sequences ? 8 : 4;
+  p.units = key_units_of(s, side * p.waves);
+  p.splits = 1;
+  if (p.units > 0 && s.sequences > 0) {
+    // (of the average sequence; the longest may be as long as all)
+    const int64_t tiles = s.queries * s.per_kv / (s.sequences * side);
+    p.splits = (int)std::max<int64_t>(1, std::min({(int64_t)kWave, kSplitKeyWorkgroups / p.units, tiles / kLeastKeyTiles}));
+  }
+  return p;
+}
 
 constexpr int64_t kWideUnits = 512;             // workgroups of eight wavefronts, which read keys and values half as often, from so many on
+constexpr int64_t kSplitRowWorkgroups = 512;     // of many rows
+constexpr int64_t kRowKeys = 64;                 // keys of a tile of theirs (of floats half as many)
 constexpr int64_t kSplitWorkgroups = 2048;      // of few rows, as many as long sequences are split for
 
 static AttentionPlan plan_of(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *q_starts) {
@@ -191,21 +218,20 @@ static AttentionPlan plan_of(const ocn_tensor *q, const ocn_tensor *k, const ocn
   p.rows = p.few ? side : side * p.waves;
   p.units = units_of(s, p.rows);
   p.splits = 1;
-  if (p.few && p.units > 0) {
-    // (the longest sequence may be as long as all keys, and is not known here)
-    const int64_t tiles = (s.keys + side - 1) / side;
-    p.splits = (int)std::max<int64_t>(1, std::min({(int64_t)kWave, kSplitWorkgroups / p.units, tiles / kLeastTiles}));
-  }
+  // (the longest sequence may be as long as all keys, and is not known here)
+  const int64_t most = (int64_t)kWave, tiles = (s.keys + side - 1) / side;
+  if (p.few && p.units > 0) p.splits = (int)std::max<int64_t>(1, std::min({most, kSplitWorkgroups / p.units, tiles / kLeastTiles}));
+  if (!p.few && p.units > 0) p.splits = (int)std::max<int64_t>(1, std::min({most, kSplitRowWorkgroups / p.units, tiles * side / (kRowKeys * kLeastRowTiles)}));
   return p;
 }
 
 // of the workspace: the order of blocks, or what parts of long sequences come to
 static size_t order_bytes(const AttentionPlan &p, const AttentionSizes &s) {
-  return !p.few && ordered(s, p.units) ? (size_t)slots_of_units(s, p.rows) * sizeof(uint32_t) : 0;
+  return p.splits == 1 && !p.few && ordered(s, p.units) ? (size_t)slots_of_units(s, p.rows) * sizeof(uint32_t) : 0;
 }
-static size_t part_bytes(const AttentionPlan &p, int64_t channels, int side) {
+static size_t part_bytes(const AttentionPlan &p, int64_t channels) {
   if (p.splits <= 1) return 0;
-  const int64_t d = padded_channels(channels), rows = p.units * p.splits * side;
+  const int64_t d = padded_channels(channels), rows = p.units * p.splits * p.rows;
   return (size_t)(rows * d + rows * 2) * sizeof(float);
 }
 
@@ -219,7 +245,7 @@ extern "C" {
 size_t ocn_attention_workspace_bytes(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *q_starts) {
   if (check_attention_sizes(q, k, q_starts) != OCN_OK) return 0;
   const AttentionPlan p = plan_of(q, k, q_starts);
-  return p.few ? part_bytes(p, q->size[q->ndim - 1], q->dtype == OCN_FLOAT ? 16 : 32) : order_bytes(p, sizes_of(q, k, q_starts));
+  return p.splits > 1 ? part_bytes(p, q->size[q->ndim - 1]) : order_bytes(p, sizes_of(q, k, q_starts));
 }
 
 int ocn_attention(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *v, const ocn_tensor *q_starts, const ocn_tensor *k_starts, double scale,
@@ -232,8 +258,7 @@ int ocn_attention(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *v,
   const HeadOperand ops[7] = {{q, false}, {k, false}, {v, false}, {q_starts, false}, {k_starts, false}, {out, true}, {log_sum, true}};
   if ((rc = check_operands(ops, 7)) != OCN_OK) return rc;
   const AttentionPlan p = plan_of(q, k, q_starts);
-  const int side = q->dtype == OCN_FLOAT ? 16 : 32;
-  const size_t need = p.few ? part_bytes(p, a.channels, side) : order_bytes(p, sizes_of(q, k, q_starts));
+  const size_t need = p.splits > 1 ? part_bytes(p, a.channels) : order_bytes(p, sizes_of(q, k, q_starts));
   if (need) {
     if (!workspace || workspace_bytes < need) return OCN_ERR_WORKSPACE;
     if ((uintptr_t)workspace % 256 != 0) return OCN_ERR_ALIGN;
@@ -242,9 +267,10 @@ int ocn_attention(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *v,
   if (!set_blocks(a, sizes_of(q, k, q_starts), p.rows, p.splits)) return OCN_ERR_SHAPE;
   a.out = view_of(out);
   if (log_sum) a.log_sum = view_of(log_sum, false);
-  if (p.few) {
+  a.rows = p.rows;
+  if (p.splits > 1) {
     a.parts = (float *)workspace;
-    a.part_sums = a.parts + p.units * p.splits * side * padded_channels(a.channels);
+    a.part_sums = a.parts + p.units * p.splits * p.rows * padded_channels(a.channels);
   } else if (need) {
     a.order = (uint32_t *)workspace;
   }
@@ -256,11 +282,11 @@ int ocn_attention(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *v,
   }
 }
 
-// two numbers of each row, and of a row that is none; the order of blocks of queries and of keys
+// two numbers of each row, and of a row that is none; the order of blocks of queries and of keys; what parts of blocks of keys come to
 static size_t grad_bytes(const AttentionSizes &s, int32_t dtype, int64_t channels) {
   const int side = dtype == OCN_FLOAT ? 16 : 32;
-  return (size_t)(s.queries * s.kv * s.per_kv + 1) * 2 * sizeof(float) +
-         (size_t)(slots_of_units(s, side * kGradWaves) + slots_of_key_units(s, side * grad_key_waves(dtype, channels))) * sizeof(uint32_t);
+  const KeyPlan k = key_plan_of(s, dtype, channels);
+  return grad_head_bytes(s, side, k.waves) + (k.splits > 1 ? (size_t)(k.units * k.splits * side * k.waves) * 2 * padded_channels(channels) * sizeof(float) : 0);
 }
 
 size_t ocn_attention_grad_workspace_bytes(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *q_starts) {

@@ -217,21 +217,6 @@ template <class T, int D, bool VEC> __device__ __forceinline__ void start_rows(R
   }
 }
 
-// four neighbouring channels of a row, rounded
-template <class T, bool VEC> __device__ __forceinline__ void store_four(char *row, int64_t step, int e, int d, const float *v) {
-  if constexpr (VEC) {
-    typedef T V __attribute__((ext_vector_type(4)));
-    V o;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = (T)v[i];
-    if (e < d) *(V *)(row + e * (int)sizeof(T)) = o;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (e + i < d) *(T *)(row + (e + i) * step) = (T)v[i];
-  }
-}
-
 // log of the sum of exponentials of a row, in natural logarithms
 template <class T> __device__ __forceinline__ float log_sum_of(const AttentionArgs &a, float best, float total) {
   return total > 0.0f || total != total ? __builtin_fmaf(best > -__builtin_inff() ? best : 0.0f, a.plain_scale, (__builtin_amdgcn_logf(total) - kTop<T>) * 0.69314718055994530942f) : -__builtin_inff();
@@ -252,6 +237,26 @@ template <class T, int D> __device__ __forceinline__ void finish_row(const Atten
   if (a.log_sum.base && lane == 0) *(float *)(a.log_sum.base + row_offset(a.log_sum, a, w, p)) = log_sum_of<T>(a, best, total);
 }
 
+// a row's place among the parts, and what a part leaves there of a row that lanes have channels of
+__device__ __forceinline__ int64_t part_row(const AttentionArgs &a, const Work &w, int row) { return ((int64_t)w.unit * a.splits + w.split) * a.rows + row; }
+template <class T, int D> __device__ __forceinline__ void leave_row(const AttentionArgs &a, const Work &w, int row, const float *x, float best, float total, int lane) {
+  const int64_t part = part_row(a, w, row);
+#pragma unroll
+  for (int c = 0; c < SlowRow<T, D>::kEach; ++c)
+    if (c * kWave + lane < D) a.parts[part * D + c * kWave + lane] = x[c];
+  if (lane == 0) a.part_sums[2 * part] = best, a.part_sums[2 * part + 1] = total;
+}
+
+// The part of a block's keys, in tiles of so many, that a workgroup has
+struct Split { int first, end; bool alone, mine; };
+__device__ __forceinline__ Split split_of(const AttentionArgs &a, const Limits &all, int keys, int least, int split) {
+  const int lo = all.lo / keys, hi = (all.hi + keys - 1) / keys;
+  const Part p = part_of(hi > lo ? hi - lo : 0, a.splits, least, split);
+  Split s = {(lo + p.first) * keys, (lo + p.end) * keys, p.alone, p.mine};
+  if (s.end > all.hi) s.end = all.hi;
+  return s;
+}
+
 // Many rows: the wavefronts of a workgroup have a tile of rows each and share the keys, which go through LDS once for all of them, the next ones on their way.
 template <class T, int D, bool VEC, int WAVES, int KEYS> __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kWavesAtOnce<T, D>))) void attention_rows_kernel(const AttentionArgs a, uint32_t first_block) {
   warm_arguments<AttentionArgs>();
@@ -260,7 +265,10 @@ template <class T, int D, bool VEC, int WAVES, int KEYS> __global__ __launch_bou
   const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   Work w;
   if (!find_work(a, first_block + blockIdx.x, &w)) return;
-  const Limits all = limits_of_block(a, w), whole = limits_of_all(a, w);
+  const Limits block = limits_of_block(a, w), whole = limits_of_all(a, w);
+  const Split split = split_of(a, block, KEYS, kLeastRowTiles, w.split);
+  if (!split.mine) return;
+  const struct { int lo, hi; } all = {split.first, split.end};
   const char *pk = a.k.base + w.sequence * a.k.batch + w.k.first * a.k.token + (int64_t)w.kv * a.k.head, *pv = a.v.base + w.sequence * a.v.batch + w.k.first * a.v.token + (int64_t)w.kv * a.v.head;
   Carrier<T, D, KEYS, WAVES, VEC> ck, cv;
   const auto load = [&](int at, int turn) {
@@ -273,7 +281,7 @@ template <class T, int D, bool VEC, int WAVES, int KEYS> __global__ __launch_bou
     ck.store(lds + turn * 2 * KEYS * PITCH);
     cv.store(lds + (turn * 2 + 1) * KEYS * PITCH);
   };
-  int at = all.lo / KEYS * KEYS, turn = 0;
+  int at = all.lo, turn = 0;
   if (VEC && a.channels < D) {
     clear_lds<WAVES * kWave>(lds, sizeof lds);
     __syncthreads();
@@ -299,7 +307,7 @@ template <class T, int D, bool VEC, int WAVES, int KEYS> __global__ __launch_bou
   };
   while (at < all.hi) {
     if (turn == 0 && at >= whole.lo)      // two at a time, so that where they lie is known
-      while (at + 2 * KEYS <= whole.hi) {
+      while (at + 2 * KEYS <= whole.hi && at + 2 * KEYS <= all.hi) {
         step(std::false_type(), std::integral_constant<int, 0>());
         step(std::false_type(), std::integral_constant<int, 1>());
       }
@@ -315,14 +323,25 @@ template <class T, int D, bool VEC, int WAVES, int KEYS> __global__ __launch_bou
       if (!p.in) continue;
       const Limits l = limits_of(a, w, p.query);
       SlowRow<T, D> slow;
-      slow.run(a, a.q.base + row_offset(a.q, a, w, p), pk, pv, l.lo, l.hi, lane);
-      finish_row<T, D>(a, w, p, slow.x, slow.best, slow.total, lane);
+      slow.run(a, a.q.base + row_offset(a.q, a, w, p), pk, pv, l.lo > all.lo ? l.lo : all.lo, l.hi < all.hi ? l.hi : all.hi, lane);
+      if (split.alone) finish_row<T, D>(a, w, p, slow.x, slow.best, slow.total, lane);
+      else leave_row<T, D>(a, w, i, slow.x, slow.best, slow.total, lane);
     }
     return;
   }
   const float total = column_sum<T>(r.total), over = total > 0.0f || total != total ? 1.0f / total : 0.0f;
   const RowPlace p = row_place(a, w, row);
   if (!p.in) return;
+  if (!split.alone) {
+    const int64_t part = part_row(a, w, row);
+#pragma unroll
+    for (int ct = 0; ct < D / SIDE; ++ct)
+#pragma unroll
+      for (int i = 0; i < Tile<T>::kOwn; i += 4)
+        *(f32x4 *)(a.parts + part * D + ct * SIDE + own_index<T>(i) + 4 * (lane / SIDE)) = f32x4{r.out[ct][i], r.out[ct][i + 1], r.out[ct][i + 2], r.out[ct][i + 3]};
+    if (lane < SIDE) a.part_sums[2 * part] = r.best, a.part_sums[2 * part + 1] = total;
+    return;
+  }
   char *const out = a.out.base + row_offset(a.out, a, w, p);
 #pragma unroll
   for (int ct = 0; ct < D / SIDE; ++ct)
@@ -340,21 +359,8 @@ template <class T, int D, bool VEC, int WAVES, int KEYS> __global__ __launch_bou
 // Few rows (single tokens): the wavefronts of a workgroup have the same tile of rows and take every fourth tile of keys, through a part of LDS of their own; a long sequence is
 // split over workgroups as well.  What they found is joined here, and that of several workgroups by a second launch.
 
-struct Split { int first, end; bool alone, mine; };      // keys of a split; whether it is the only one; whether there is it
-__device__ __forceinline__ Split split_of(const AttentionArgs &a, const Limits &all, int side, int split) {
-  const int lo = all.lo / side, hi = (all.hi + side - 1) / side, tiles = hi > lo ? hi - lo : 0;
-  int per = (tiles + a.splits - 1) / a.splits;
-  if (per < kLeastTiles) per = kLeastTiles;
-  Split s;
-  s.alone = tiles <= per;
-  s.mine = split == 0 || split * per < tiles;
-  s.first = (lo + split * per) * side;
-  s.end = (lo + (split * per + per < tiles ? split * per + per : tiles)) * side;
-  if (s.end > all.hi) s.end = all.hi;
-  return s;
-}
-
-template <class T, int D, bool VEC> __global__ __launch_bounds__(kFewWaves *kWave) void attention_few_kernel(const AttentionArgs a, uint32_t first_block) {
+template <class T, int D, bool VEC>
+__global__ __launch_bounds__(kFewWaves *kWave) __attribute__((amdgpu_waves_per_eu(kWavesAtOnce<T, D>))) void attention_few_kernel(const AttentionArgs a, uint32_t first_block) {
   warm_arguments<AttentionArgs>();
   constexpr int SIDE = Tile<T>::kSide, PITCH = Held<T, D>::kPitch, PART = 2 * SIDE * PITCH;
   static_assert(SIDE * D * 4 <= PART, "a wavefront's results take the place of its keys and values");
@@ -365,7 +371,7 @@ template <class T, int D, bool VEC> __global__ __launch_bounds__(kFewWaves *kWav
   Work w;
   if (!find_work(a, first_block + blockIdx.x, &w)) return;
   const Limits all = limits_of_block(a, w);
-  const Split split = split_of(a, all, SIDE, w.split);
+  const Split split = split_of(a, all, SIDE, kLeastTiles, w.split);
   if (!split.mine) return;
   Rows<T, D> r;
   start_rows<T, D, VEC>(r, a, w, n, lane, a.q.base + w.sequence * a.q.batch + w.q.first * a.q.token + (int64_t)w.kv * a.per_kv * a.q.head);
@@ -376,13 +382,17 @@ template <class T, int D, bool VEC> __global__ __launch_bounds__(kFewWaves *kWav
   int at = split.first + wave * SIDE;
   bool odd = false;
   if (at < split.end) next.load(a, pk, pv, at, w.k.count, lane);
-  for (; at < split.end; at += kFewWaves * SIDE) {
+  const auto step = [&](auto masked) {
     next.store(k, v, lane);
     if (at + kFewWaves * SIDE < split.end) next.load(a, pk, pv, at + kFewWaves * SIDE, w.k.count, lane);
     __builtin_amdgcn_wave_barrier();
-    if (at >= lo_last && at + SIDE <= hi_first) attend<T, D, SIDE, false>(r, k, v, at, a.scale, lane);
-    else odd |= attend<T, D, SIDE, true>(r, k, v, at, a.scale, lane);
+    odd |= attend<T, D, SIDE, masked>(r, k, v, at, a.scale, lane);
     __builtin_amdgcn_wave_barrier();
+    at += kFewWaves * SIDE;
+  };
+  while (at < split.end) {
+    while (at >= lo_last && at + SIDE <= hi_first && at < split.end) step(std::false_type());
+    if (at < split.end) step(std::true_type());
   }
   const float total = column_sum<T>(r.total);
   if (lane < SIDE) bests[wave][n] = r.best, totals[wave][n] = total;
@@ -401,11 +411,7 @@ template <class T, int D, bool VEC> __global__ __launch_bounds__(kFewWaves *kWav
       if (split.alone) {
         finish_row<T, D>(a, w, p, slow.x, slow.best, slow.total, lane);
       } else {
-        const int64_t part = ((int64_t)w.unit * a.splits + w.split) * SIDE + i;
-#pragma unroll
-        for (int c = 0; c < SlowRow<T, D>::kEach; ++c)
-          if (c * kWave + lane < D) a.parts[part * D + c * kWave + lane] = slow.x[c];
-        if (lane == 0) a.part_sums[2 * part] = slow.best, a.part_sums[2 * part + 1] = slow.total;
+        leave_row<T, D>(a, w, i, slow.x, slow.best, slow.total, lane);
       }
     }
     return;
@@ -442,7 +448,7 @@ template <class T, int D, bool VEC> __global__ __launch_bounds__(kFewWaves *kWav
       store_four<T, VEC>(a.out.base + row_offset(a.out, a, w, p), a.out.channel, e, a.channels, x);
       if (a.log_sum.base && e == 0) *(float *)(a.log_sum.base + row_offset(a.log_sum, a, w, p)) = log_sum_of<T>(a, top, sum);
     } else {
-      const int64_t part = ((int64_t)w.unit * a.splits + w.split) * SIDE + row;
+      const int64_t part = part_row(a, w, row);
       *(f32x4 *)(a.parts + part * D + e) = f32x4{x[0], x[1], x[2], x[3]};
       if (e == 0) a.part_sums[2 * part] = top, a.part_sums[2 * part + 1] = sum;
     }
@@ -450,34 +456,35 @@ template <class T, int D, bool VEC> __global__ __launch_bounds__(kFewWaves *kWav
 }
 
 // What several workgroups found of a row, joined: a wavefront to a row.
-template <class T, int D> __global__ __launch_bounds__(kBlock) void attention_join_kernel(const AttentionArgs a, uint32_t first_unit) {
-  constexpr int SIDE = Tile<T>::kSide, EACH = (D + kWave - 1) / kWave;
+template <class T, int D> __global__ __launch_bounds__(kBlock) void attention_join_kernel(const AttentionArgs a, uint32_t first, int keys, int least) {
+  constexpr int EACH = (D + kWave - 1) / kWave;
   const int lane = threadIdx.x & (kWave - 1);
   Work w;
-  if (!find_work(a, (first_unit + blockIdx.x) * (uint32_t)a.splits, &w)) return;
+  const uint32_t chunks = (uint32_t)a.rows / kJoinRows, unit = (first + blockIdx.x) / chunks, chunk = first + blockIdx.x - unit * chunks;
+  if (!find_work(a, unit * (uint32_t)a.splits, &w)) return;
   const Limits all = limits_of_block(a, w);
-  if (split_of(a, all, SIDE, 0).alone) return;
-  for (int row = threadIdx.x / kWave; row < SIDE; row += kBlock / kWave) {
+  if (split_of(a, all, keys, least, 0).alone) return;
+  for (int row = (int)chunk * kJoinRows + threadIdx.x / kWave; row < (int)(chunk + 1) * kJoinRows; row += kBlock / kWave) {
     const RowPlace p = row_place(a, w, row);
     if (!p.in) continue;
-    const int64_t part = (int64_t)w.unit * a.splits * SIDE + row;
-    const bool there = lane < a.splits && split_of(a, all, SIDE, lane).mine;
-    const float own = there ? a.part_sums[2 * (part + (int64_t)lane * SIDE)] : -__builtin_inff();
+    const int64_t part = (int64_t)w.unit * a.splits * a.rows + row;
+    const bool there = lane < a.splits && split_of(a, all, keys, least, lane).mine;
+    const float own = there ? a.part_sums[2 * (part + (int64_t)lane * a.rows)] : -__builtin_inff();
     float top = own;
 #pragma unroll
     for (int o = 32; o > 0; o /= 2) top = fmaxf(top, __shfl_xor(top, o));
     const float keep = !there ? 0.0f : own > -__builtin_inff() ? __builtin_amdgcn_exp2f((own - top) * a.scale) : 1.0f;
-    float sum = there ? a.part_sums[2 * (part + (int64_t)lane * SIDE) + 1] * keep : 0.0f;
+    float sum = there ? a.part_sums[2 * (part + (int64_t)lane * a.rows) + 1] * keep : 0.0f;
 #pragma unroll
     for (int o = 32; o > 0; o /= 2) sum += __shfl_xor(sum, o);
     float x[EACH];
 #pragma unroll
     for (int c = 0; c < EACH; ++c) x[c] = 0.0f;
-    for (int s = 0; s < a.splits && split_of(a, all, SIDE, s).mine; ++s) {
+    for (int s = 0; s < a.splits && split_of(a, all, keys, least, s).mine; ++s) {
       const float f = __shfl(keep, s);
 #pragma unroll
       for (int c = 0; c < EACH; ++c)
-        if (c * kWave + lane < D) x[c] = __builtin_fmaf(a.parts[(part + (int64_t)s * SIDE) * D + c * kWave + lane], f, x[c]);
+        if (c * kWave + lane < D) x[c] = __builtin_fmaf(a.parts[(part + (int64_t)s * a.rows) * D + c * kWave + lane], f, x[c]);
     }
     finish_row<T, D>(a, w, p, x, top, sum, lane);
   }
@@ -513,9 +520,10 @@ template <class T, int D, bool VEC> int run(AttentionArgs &a, const AttentionPla
     if ((rc = done(hipGetLastError())) != OCN_OK) return rc;
   }
   if (p.splits == 1) return OCN_OK;
-  for (int64_t at = 0; at < p.units; at += most) {
-    const uint32_t grid = (uint32_t)std::min(p.units - at, most), first = (uint32_t)at;
-    hipLaunchKernelGGL((attention_join_kernel<T, D>), dim3(grid), dim3(kBlock), 0, stream, a, first);
+  const int64_t joins = p.units * (p.rows / kJoinRows);
+  for (int64_t at = 0; at < joins; at += most) {
+    const uint32_t grid = (uint32_t)std::min(joins - at, most), first = (uint32_t)at;
+    hipLaunchKernelGGL((attention_join_kernel<T, D>), dim3(grid), dim3(kBlock), 0, stream, a, first, p.few ? (int)Tile<T>::kSide : kRowKeys<T>, p.few ? kLeastTiles : kLeastRowTiles);
     if ((rc = done(hipGetLastError())) != OCN_OK) return rc;
   }
   return OCN_OK;

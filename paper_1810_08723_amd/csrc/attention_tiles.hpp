@@ -133,20 +133,52 @@ template <class T, int D> __device__ __forceinline__ frag_t<T> columns_fragment(
   return f;
 }
 
-// 16 bytes of a row in memory, from channel e on; what lies outside of the row's d channels is zero
+// 16 bytes of a row in memory, from channel e on; what lies outside of the row's d channels is zero.  VEC: whole, aligned rows.  Others whose channels lie
+// together are loaded in pieces as well, which may begin at any element; the last one, where it is not whole, ends with the row and is shifted.
 template <class T, bool VEC> __device__ __forceinline__ u32x4 load_piece(const char *row, int64_t step, int e, int d) {
+  constexpr int EACH = 16 / (int)sizeof(T);
   u32x4 v = {0, 0, 0, 0};
   if constexpr (VEC) {
     if (e < d) v = *(const u32x4 *)(row + e * (int)sizeof(T));
+  } else if (step == (int)sizeof(T) && d >= EACH) {
+    typedef u32x4 Any __attribute__((aligned(2)));
+    if (e < d) {
+      const int past = e + EACH > d ? e + EACH - d : 0;        // channels of the piece that are none
+      v = *(const Any *)(row + (e - past) * (int)sizeof(T));
+      if (past) {
+        const int bytes = past * (int)sizeof(T);
+        if (bytes & 8) v = u32x4{v[2], v[3], 0, 0};
+        if (bytes & 4) v = u32x4{v[1], v[2], v[3], 0};
+        if (bytes & 2) v = u32x4{v[0] >> 16 | v[1] << 16, v[1] >> 16 | v[2] << 16, v[2] >> 16 | v[3] << 16, v[3] >> 16};
+      }
+    }
   } else {
-    union { T t[16 / sizeof(T)]; u32x4 v; } u;
+    union { T t[EACH]; u32x4 v; } u;
     u.v = v;
 #pragma unroll
-    for (int i = 0; i < (int)(16 / sizeof(T)); ++i)
+    for (int i = 0; i < EACH; ++i)
       if (e + i < d) u.t[i] = *(const T *)(row + (e + i) * step);
     v = u.v;
   }
   return v;
+}
+
+// four neighbouring channels of a row, rounded
+template <class T, bool VEC> __device__ __forceinline__ void store_four(char *row, int64_t step, int e, int d, const float *v) {
+  typedef T Four __attribute__((ext_vector_type(4)));
+  typedef Four Any __attribute__((aligned(2)));
+  Four o;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o[i] = (T)v[i];
+  if constexpr (VEC) {
+    if (e < d) *(Four *)(row + e * (int)sizeof(T)) = o;
+  } else if (step == (int)sizeof(T) && e + 4 <= d) {
+    *(Any *)(row + e * (int)sizeof(T)) = o;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (e + i < d) *(T *)(row + (e + i) * step) = o[i];
+  }
 }
 
 // Wavefronts that a SIMD is to hold: two have 256 registers each, which all are operands of any instruction; a single one has half of its 512 beside the others, reached by copies.
@@ -329,6 +361,23 @@ __device__ __forceinline__ Limits limits_of_all(const AttentionArgs &a, const Wo
   const Limits one = limits_of(a, w, (int)first), last = limits_of(a, w, (int)end - 1);
   return {last.lo, one.hi};
 }
+
+// ---- parts -------------------------------------------------------------------------------------
+//
+// Where blocks leave CUs without work, what a block goes over (`tiles` of them) is cut into parts, a workgroup each, of `least` tiles or more.
+struct Part { int first, end; bool alone, mine; };      // its tiles; whether it is the only one; whether there is it
+__device__ __forceinline__ Part part_of(int tiles, int splits, int least, int split) {
+  int per = (tiles + splits - 1) / splits;
+  if (per < least) per = least;
+  Part p;
+  p.alone = tiles <= per;
+  p.mine = split == 0 || split * per < tiles;
+  p.first = split * per;
+  p.end = split * per + per < tiles ? split * per + per : tiles;
+  return p;
+}
+
+constexpr int kJoinRows = 8;       // rows of a workgroup that joins parts, two of each wavefront
 
 // ---- the order of blocks -----------------------------------------------------------------------
 //
