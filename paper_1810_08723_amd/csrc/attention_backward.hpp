@@ -419,7 +419,7 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
     if (!a.gq.base) return;
     __syncthreads();
     at = all.lo / KEYS * KEYS, turn = 0;
-    if (at < all.hi) {
+    if (at + KEYS < all.hi) {      // (a single tile is there already)
       load(at, 0);
       store(0);
     }

@@ -275,23 +275,31 @@ __device__ __forceinline__ Span span_of(const Starts &s, int i) {
 }
 
 // Blocks of `size` tokens: a packed sequence has the slots start / size + its number up to the next one's, one for each of its blocks at least, as
-// a sequence that begins inside of a block's size may have one more than its length makes.
-__device__ __forceinline__ bool find_slot(const Starts &s, const FastDiv &size, uint32_t slot, int *sequence, uint32_t *block) {
-  // the last sequence whose first slot is not behind this one; all lanes of a wavefront look at once
-  int lo = 0, hi = s.sequences;      // in [lo, hi)
+// a sequence that begins inside of a block's size may have one more than its length makes.  `own`, the starts that blocks go by, and `other` give the sequence's tokens.
+__device__ __forceinline__ bool find_slot(const Starts &own, const Starts &other, const FastDiv &size, uint32_t slot, int *sequence, uint32_t *block, Span *own_span, Span *other_span) {
+  // the last sequence whose first slot is not behind this one; all lanes of a wavefront look at once, in the end with all that there is to know of a sequence each
+  int lo = 0, hi = own.sequences;      // in [lo, hi)
   const int lane = threadIdx.x & (kWave - 1);
-  while (hi - lo > 1) {
+  while (hi - lo > kWave) {
     const int step = (hi - lo + kWave - 1) / kWave, at = lo + lane * step;
-    const bool fits = at < hi && fast_quotient((uint32_t)start_at(s, at), size) + (uint32_t)at <= slot;
+    const bool fits = at < hi && fast_quotient((uint32_t)start_at(own, at), size) + (uint32_t)at <= slot;
     const uint64_t all = __ballot(fits);
     const int last = all ? 63 - __builtin_clzll(all) : 0;
     lo += last * step;
     hi = lo + step < hi ? lo + step : hi;
   }
-  *sequence = lo;
-  const uint32_t first = fast_quotient((uint32_t)start_at(s, lo), size) + (uint32_t)lo;
-  *block = slot - first;
-  return slot >= first;
+  const int at = lo + lane < hi ? lo + lane : hi - 1;
+  const uint32_t own_start = (uint32_t)start_at(own, at), own_end = (uint32_t)start_at(own, at + 1), other_start = (uint32_t)start_at(other, at), other_end = (uint32_t)start_at(other, at + 1);
+  const uint32_t first = fast_quotient(own_start, size) + (uint32_t)at;
+  const uint64_t all = __ballot(lo + lane < hi && first <= slot);
+  const int last = all ? 63 - __builtin_clzll(all) : 0;
+  const auto of_last = [&](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, last); };
+  *sequence = lo + last;
+  *block = slot - of_last(first);
+  const uint32_t a = of_last(own_start), b = of_last(own_end), c = of_last(other_start), d = of_last(other_end);
+  *own_span = {(int64_t)a, (int32_t)(b > a ? b - a : 0)};
+  *other_span = {(int64_t)c, (int32_t)(d > c ? d - c : 0)};
+  return all != 0;
 }
 
 // What a workgroup has: a block of a sequence's queries (or keys), with some heads that share a head of keys and values
@@ -313,14 +321,16 @@ template <bool KEYS> __device__ __forceinline__ bool find_work_of(const Attentio
   // With a causal mask the first blocks of keys and the last ones of queries have most to do.
   if (s.p) {
     const uint32_t slot = a.order ? a.order[down] : KEYS ? down : a.slots - 1 - down;
-    if (!find_slot(s, a.tokens_div, slot, &w->sequence, &w->block)) return false;
+    if (!find_slot(s, KEYS ? a.q_starts : a.k_starts, a.tokens_div, slot, &w->sequence, &w->block, KEYS ? &w->k : &w->q, KEYS ? &w->q : &w->k)) return false;
   } else {
     const uint32_t turn = fast_quotient(down, a.sequences_div);
     w->sequence = (int)(down - turn * a.sequences_div.d);
     w->block = KEYS ? turn : a.per_sequence - 1 - turn;
   }
-  w->q = span_of(a.q_starts, w->sequence);
-  w->k = span_of(a.k_starts, w->sequence);
+  if (!s.p) {
+    w->q = span_of(a.q_starts, w->sequence);
+    w->k = span_of(a.k_starts, w->sequence);
+  }
   return (int64_t)w->block * a.tokens < (KEYS ? w->k.count : w->q.count);
 }
 __device__ __forceinline__ bool find_work(const AttentionArgs &a, uint32_t index, Work *w) { return find_work_of<false>(a, index, w); }

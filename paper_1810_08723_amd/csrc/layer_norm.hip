@@ -28,7 +28,7 @@ struct LayerArgs {
   int64_t xl[kMaxLead], gl[kMaxLead], ol[kMaxLead];
   int64_t xe, ge, oe, weight_stride, bias_stride;
   int32_t weight_type, bias_type;
-  int32_t weight_whole, bias_whole;    // in whole vectors
+  int32_t weight_whole, bias_whole;    // their channels lie together
   int32_t width, lanes_log2;           // lanes of a row, where they lie in one wavefront
   int32_t stream;
   float eps, over;
@@ -45,8 +45,11 @@ __device__ __forceinline__ int64_t row_offset(const Lead &lead, const int64_t *s
   return o + (int64_t)row * stride[0];
 }
 
-// Where a lane's chunks of eight channels lie.  In whole vectors a chunk is eight channels in a row; else lanes have neighbouring channels,
-// so that a load of theirs is of neighbouring bytes.
+// Where a lane's chunks of eight channels lie.  Where channels lie together (VEC) a chunk is eight of them in a row, which may begin at any element: loads of 16 bytes need no
+// alignment.  Else lanes have neighbouring channels, so that a load of theirs is of neighbouring bytes, or nearly.
+template <class T> struct Anywhere { typedef eight_t<T> V __attribute__((aligned(2))); };
+template <> struct Anywhere<float> { typedef f32x8 V __attribute__((aligned(4))); };
+
 template <bool VEC> struct Place {
   int first, step, chunk;              // of chunk 0; from channel to channel; from chunk to chunk
   __device__ __forceinline__ Place(int lane, int lanes) : first(VEC ? lane * kEight : lane), step(VEC ? 1 : lanes), chunk(lanes * kEight) {}
@@ -56,7 +59,14 @@ template <bool VEC> struct Place {
 template <class T, bool VEC> __device__ __forceinline__ eight_t<T> load_chunk(const char *row, int64_t step, const Place<VEC> &p, int c, int width) {
   eight_t<T> v = {};
   if constexpr (VEC) {
-    if (p.at(c, 0) < width) v = *(const eight_t<T> *)(row + p.at(c, 0) * (int)sizeof(T));
+    const char *from = row + p.at(c, 0) * (int)sizeof(T);
+    if (p.at(c, 0) + kEight <= width) {
+      v = *(const typename Anywhere<T>::V *)from;
+    } else if (p.at(c, 0) < width) {      // the row's last ones
+#pragma unroll
+      for (int i = 0; i < kEight - 1; ++i)
+        if (p.at(c, i) < width) v[i] = *(const T *)(from + i * (int)sizeof(T));
+    }
   } else {
 #pragma unroll
     for (int i = 0; i < kEight; ++i)
@@ -66,7 +76,23 @@ template <class T, bool VEC> __device__ __forceinline__ eight_t<T> load_chunk(co
 }
 template <class T, bool VEC> __device__ __forceinline__ void store_chunk(char *row, int64_t step, const Place<VEC> &p, int c, int width, const float *v, bool stream) {
   if constexpr (VEC) {
-    if (p.at(c, 0) < width) store_eight<T, true>(row, step, p.at(c, 0), width, v, stream);
+    char *to = row + p.at(c, 0) * (int)sizeof(T);
+    if (p.at(c, 0) + kEight <= width) {
+      eight_t<T> o;
+#pragma unroll
+      for (int i = 0; i < kEight; ++i) o[i] = (T)v[i];
+      if (stream) {
+        asm volatile("");     // (these keep the two apart: made into one store, they would be an ordinary one)
+        __builtin_nontemporal_store(o, (typename Anywhere<T>::V *)to);
+        asm volatile("");
+      } else {
+        *(typename Anywhere<T>::V *)to = o;
+      }
+    } else if (p.at(c, 0) < width) {
+#pragma unroll
+      for (int i = 0; i < kEight - 1; ++i)
+        if (p.at(c, i) < width) *(T *)(to + i * (int)sizeof(T)) = (T)v[i];
+    }
   } else {
 #pragma unroll
     for (int i = 0; i < kEight; ++i)
@@ -78,14 +104,14 @@ template <bool VEC> __device__ __forceinline__ void load_factors(const char *p, 
 #pragma unroll
   for (int i = 0; i < kEight; ++i) v[i] = none;
   if (!p) return;
-  if (VEC && whole) {
-    if (at.at(c, 0) >= width) return;
+  if (VEC && whole && at.at(c, 0) + kEight <= width) {
     if (type == OCN_FLOAT) {
-      const f32x8 w = *(const f32x8 *)(p + at.at(c, 0) * 4);
+      const f32x8 w = *(const typename Anywhere<float>::V *)(p + at.at(c, 0) * 4);
 #pragma unroll
       for (int i = 0; i < kEight; ++i) v[i] = w[i];
     } else {
-      const u32x4 w = *(const u32x4 *)(p + at.at(c, 0) * 2);
+      typedef u32x4 Any __attribute__((aligned(2)));
+      const u32x4 w = *(const Any *)(p + at.at(c, 0) * 2);
 #pragma unroll
       for (int i = 0; i < kEight; ++i) {
         const uint16_t half = (uint16_t)(i % 2 ? w[i / 2] >> 16 : w[i / 2]);
@@ -256,13 +282,10 @@ template <class T, bool VEC, bool WIDE, int C> __global__ __launch_bounds__(kMos
   float *const partial = a.partial + (int64_t)blockIdx.x * 2 * width;
   if constexpr (WIDE) {
 #pragma unroll
-    for (int c = 0; c < C; ++c)
-#pragma unroll
-      for (int i = 0; i < kEight; ++i)
-        if (p.at(c, i) < width) {
-          partial[p.at(c, i)] = gw[c * kEight + i];
-          partial[width + p.at(c, i)] = gb[c * kEight + i];
-        }
+    for (int c = 0; c < C; ++c) {
+      store_chunk<float, VEC>((char *)partial, 4, p, c, width, gw + c * kEight, false);
+      store_chunk<float, VEC>((char *)(partial + width), 4, p, c, width, gb + c * kEight, false);
+    }
   } else {      // the rows that the workgroup's lanes took side by side
     __shared__ float sums[kBlock * C * kEight];
     const int wide = lanes * C * kEight;
@@ -349,13 +372,8 @@ int64_t workers_of(int64_t rows, int64_t width) {
   return std::max<int64_t>(1, (want + rounds - 1) / rounds);
 }
 
-bool whole(const ocn_tensor *t) {
-  const int64_t size = head_type_size(t->dtype);
-  if (width_of(t) % kEight != 0 || (width_of(t) > 1 && t->stride[t->ndim - 1] != size) || ((intptr_t)t->base + t->offset) % 16 != 0) return false;
-  for (int d = 0; d + 1 < t->ndim; ++d)
-    if (t->size[d] > 1 && t->stride[d] % 16 != 0) return false;
-  return true;
-}
+// channels that lie together
+bool whole(const ocn_tensor *t) { return width_of(t) <= 1 || t->stride[t->ndim - 1] == head_type_size(t->dtype); }
 
 int check_rows(const ocn_tensor *t) {
   const int rc = check_operand(t, kHeadTypes);
@@ -407,7 +425,7 @@ int fill(LayerArgs &a, const ocn_tensor *x, const ocn_tensor *g, const ocn_tenso
   return OCN_OK;
 }
 
-// CALL(type, whole vectors, whether a row has several wavefronts, chunks of a lane)
+// CALL(type, channels that lie together, whether a row has several wavefronts, chunks of a lane)
 #define OCN_NORM_SHAPES(T, VEC, s, CALL)                     \
   do {                                                       \
     if ((s).waves > 1) CALL(T, VEC, true, 2);                \
