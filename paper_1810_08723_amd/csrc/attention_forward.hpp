@@ -258,7 +258,7 @@ __device__ __forceinline__ Split split_of(const AttentionArgs &a, const Limits &
 }
 
 // Many rows: the wavefronts of a workgroup have a tile of rows each and share the keys, which go through LDS once for all of them, the next ones on their way.
-template <class T, int D, bool VEC, int WAVES, int KEYS> __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kWavesAtOnce<T, D>))) void attention_rows_kernel(const AttentionArgs a, uint32_t first_block) {
+template <class T, int D, bool VEC, int WAVES, int KEYS> __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 && (D <= 128 || VEC && D <= 192) ? 2 : 1))) void attention_rows_kernel(const AttentionArgs a, uint32_t first_block) {
   warm_arguments<AttentionArgs>();
   constexpr int SIDE = Tile<T>::kSide, PITCH = Held<T, D>::kPitch;
   __shared__ __align__(16) char lds[2 * 2 * KEYS * PITCH];        // [2][keys, values][KEYS][PITCH]
@@ -500,7 +500,8 @@ int done(hipError_t e) {
   return OCN_ERR_LAUNCH;
 }
 
-template <class T> constexpr int kRowKeys = sizeof(T) == 2 ? 64 : 32;
+// Keys of a tile of many rows: half as many where a wavefront's results take half of its registers or more, which 64 scores to a row would drive to memory (half precision, 4 sequences of 4096 tokens, 16 heads of 192 channels: 511 for 714 us; 256 channels, which stay at one wavefront to a SIMD: 860 for 810 us, and 68 for 110 where rows begin anywhere).
+template <class T, int D> constexpr int kRowKeys = sizeof(T) == 2 && D <= 128 ? 64 : 32;
 
 template <class T, int D> constexpr bool kWide = sizeof(T) == 2 && (D == 96 || D == 128);
 
@@ -515,15 +516,15 @@ template <class T, int D, bool VEC> int run(AttentionArgs &a, const AttentionPla
   for (int64_t at = 0; at < blocks; at += most) {
     const uint32_t grid = (uint32_t)std::min(blocks - at, most), first = (uint32_t)at;
     if (p.few) hipLaunchKernelGGL((attention_few_kernel<T, D, VEC>), dim3(grid), dim3(kFewWaves * kWave), 0, stream, a, first);
-    else if (kWide<T, D> && p.waves == 8) hipLaunchKernelGGL((attention_rows_kernel<T, D, VEC, kWide<T, D> ? 8 : 4, kRowKeys<T>>), dim3(grid), dim3(8 * kWave), 0, stream, a, first);
-    else hipLaunchKernelGGL((attention_rows_kernel<T, D, VEC, 4, kRowKeys<T>>), dim3(grid), dim3(4 * kWave), 0, stream, a, first);
+    else if (kWide<T, D> && p.waves == 8) hipLaunchKernelGGL((attention_rows_kernel<T, D, VEC, kWide<T, D> ? 8 : 4, kRowKeys<T, D>>), dim3(grid), dim3(8 * kWave), 0, stream, a, first);
+    else hipLaunchKernelGGL((attention_rows_kernel<T, D, VEC, 4, kRowKeys<T, D>>), dim3(grid), dim3(4 * kWave), 0, stream, a, first);
     if ((rc = done(hipGetLastError())) != OCN_OK) return rc;
   }
   if (p.splits == 1) return OCN_OK;
   const int64_t joins = p.units * (p.rows / kJoinRows);
   for (int64_t at = 0; at < joins; at += most) {
     const uint32_t grid = (uint32_t)std::min(joins - at, most), first = (uint32_t)at;
-    hipLaunchKernelGGL((attention_join_kernel<T, D>), dim3(grid), dim3(kBlock), 0, stream, a, first, p.few ? (int)Tile<T>::kSide : kRowKeys<T>, p.few ? kLeastTiles : kLeastRowTiles);
+    hipLaunchKernelGGL((attention_join_kernel<T, D>), dim3(grid), dim3(kBlock), 0, stream, a, first, p.few ? (int)Tile<T>::kSide : kRowKeys<T, D>, p.few ? kLeastTiles : kLeastRowTiles);
     if ((rc = done(hipGetLastError())) != OCN_OK) return rc;
   }
   return OCN_OK;
