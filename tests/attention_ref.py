@@ -3,7 +3,8 @@
 Bounds.  u = 2^-24 is half a step of single precision, t half a step of the tensors' type (0 where products are taken in single precision throughout: float).
     score        a sum of d products: off by (d + 2) u sum|q k| |scale| =: a; two such differ from their maximum's by 2 a, and the exponential and its argument add
                  4 u (1 + |score - best|)
-    weight       p off by e = exp(2 a + ...) - 1 of itself before it is rounded, by t more after; a half that is below 2^-14 by 2^-25 (weights are near 2^11 or 2^12: 2^-36 of the largest)
+    weight       p off by e = exp(2 a + ...) - 1 of itself before it is rounded, by t more after; a half that is below 2^-14 by 2^-25: the reference's weight is 2^9 and a row's sum is
+                 as much or more, so that this is 2^-34 of the sum; in the gradient 1 is 2^12, so that it is 2^-37, and the largest s of a column so far 2^11 or more, 2^-36 of that
     out          the product with v is a sum of n terms and the sum of weights as well: (2 n + 16) u, all of it times sum p |v|
     log_sum      a + (n + 16) u, and 4 u of itself
     gradient     the weight is made again from log_sum, which is off as above;  gout v off by (d + 2) u sum|gout v|;  gout out by what out is, and (d + 2) u;
@@ -36,7 +37,7 @@ def attended(q, k, v, q_spans, k_spans, scale, causal, window, kind, gout=None, 
     qd, kd, vd = q.double(), k.double(), v.double()
     heads, kv, d = q.shape[1], k.shape[1], q.shape[2]
     u, t = F32, (0.0 if kind == "float" else half_step(kind))
-    tiny = 2.0 ** -36 if kind == "half" else 0.0
+    tiny = 2.0 ** -36 if kind == "half" else 0.0            # of s and (more than) of p in the gradient; of weights 4 times that
     r = {"out": torch.full_like(qd, float("nan")), "log_sum": torch.full(q.shape[:2], float("nan"), dtype=torch.float64)}
     b = {n: x.clone() for n, x in r.items()}
     if gout is not None:
@@ -64,7 +65,7 @@ def attended(q, k, v, q_spans, k_spans, scale, causal, window, kind, gout=None, 
             e = torch.expm1(a + worst + 4 * u * (1 + (s - top).abs().masked_fill(~see, 0.0)))
             out = p @ z
             size = p @ z.abs()
-            off = (p * e) @ z.abs() + (p * e).sum(1, keepdim=True) * out.abs() + (t + (2 * m + 16) * u) * size + m * tiny * (z.abs().amax(0) if m else 0.0)
+            off = (p * e) @ z.abs() + (p * e).sum(1, keepdim=True) * out.abs() + (t + (2 * m + 16) * u) * size + m * 4 * tiny * (z.abs().amax(0) if m else 0.0)
             r["out"][q0:q1, h], b["out"][q0:q1, h] = out, off
             log = torch.where(any_seen, total.log() + top, -float("inf"))
             log_off = worst + (p * e).sum(1, keepdim=True) + (m + 16) * u + 4 * u * torch.where(any_seen, log.abs() + top.abs(), 0.0)

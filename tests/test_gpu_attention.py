@@ -39,7 +39,7 @@ def close(name, got, want, kind):
     there = ~value.isnan()
     same = (got == value) & there            # (infinities)
     bound = bound + (rounding(kind, value) if kind else 0.0)
-    bad = there & ~same & ~((got - value).abs() <= bound * 1.0)
+    bad = there & ~same & ~((got - value).abs() <= bound)
     assert not bad.any(), (name, int(bad.sum()), ((got - value).abs() / bound)[bad].max().item(), bad.nonzero()[:3].tolist())
 
 
@@ -341,3 +341,71 @@ def test_many_sequences(kind, causal, window):
     for shape in ((nk, None, 8, 4, 64, causal, window), (nq, nk, 6, 6, 128, causal, window)):
         data = made(shape, kind, 14)
         check(shape, kind, data, both(shape, kind, data))
+
+
+# few sequences of many rows, whose keys are cut into parts, and few keys of many rows, whose rows are; parts of which rows see none or some
+SPLIT = [([600], [3001], 2, 1, 128, True, 0), ([200, 90], [1500, 40], 4, 2, 250, False, 0), ([700], None, 3, 1, 80, True, 300), ([1500, 64], [70, 64], 4, 2, 64, False, 0),
+         ([900], [130], 6, 1, 128, True, 0), ([600], [300], 2, 2, 192, True, 100), ([333, 33], [1333, 1], 8, 8, 96, True, 700)]
+
+
+@pytest.mark.parametrize("kind", list(KIND))
+@pytest.mark.parametrize("shape", SPLIT, ids=str)
+def test_parts_of_long_sequences(shape, kind):
+    from paper_1810_08723_amd import binding
+    data = made(shape, kind, 15)
+    got = both(shape, kind, data)
+    check(shape, kind, data, got)
+    binding.set_max_launch_blocks(7)
+    try:
+        again = both(shape, kind, data, how="packed")
+    finally:
+        binding.set_max_launch_blocks(0)
+    assert all(torch.equal(got[n], again[n]) for n in got)
+
+
+@pytest.mark.parametrize("kind", list(KIND))
+def test_parts_with_odd_values_and_large_ones(kind):
+    """Keys past 2900 are NaNs and infinities, which the rows that do not see them do without; a key of one part whose scores are far above all others"""
+    shape = ([600], [3001], 2, 1, 128, True, 0)
+    data = made(shape, kind, 16)
+    q, k, v, w = (t.clone() for t in data)
+    k[100] *= 20
+    ref = reference(shape, kind, (q, k, v, w), grad=False)
+    k[2950], v[2901], v[2990] = math.nan, math.inf, -math.inf
+    got = both(shape, kind, (q, k, v, w), grad=False)
+    clean = torch.arange(600) <= 2900 - 2401          # row i sees the keys up to i + 2401
+    for n, bound_kind in (("out", kind), ("log_sum", None)):
+        close(n, got[n][clean.cuda()], tuple(x[clean] for x in ref[n]), bound_kind)
+    assert not got["out"][~clean.cuda()].isfinite().all(-1).any()
+
+
+@pytest.mark.parametrize("size", [1e-4, 1.0, 1e4])
+def test_parts_of_gradients_of_any_size_in_half(size):
+    """Rows whose gradients differ by 2^20 from part to part: each part has a range of its own"""
+    shape = ([1200], [100], 2, 1, 64, False, 0)
+    q, k, v, w = made(shape, "half", 17)
+    w = (w.float().clamp(-2, 2) * size * torch.logspace(0, -6, 1200)[:, None, None]).half()
+    data = (q, k, v, w)
+    got = both(shape, "half", data)
+    want = reference(shape, "half", data, None, got["out"].cpu())
+    for n in ("gq", "gk", "gv"):
+        value, bound = want[n]
+        fine = value.abs() < 65000
+        close(n, torch.where(fine.cuda(), got[n], 0), tuple(torch.where(fine, x, 0.0) for x in (value, bound)), "half")
+
+
+@pytest.mark.parametrize("kind", list(KIND))
+def test_sequences_as_a_dimension_with_a_window(kind):
+    """[batch, tokens, heads, channels] with more keys than queries, transposed and broadcast operands; the results of the same sequences packed"""
+    batch, n, m, heads, kv, d = 3, 40, 75, 4, 2, 72
+    g = torch.Generator().manual_seed(18)
+    q, k, v, w = (torch.randn(batch, h, t, d, generator=g).to(KIND[kind]).cuda().transpose(1, 2) for h, t in ((heads, n), (kv, m), (kv, m), (heads, n)))
+    k = k[:1].expand(batch, -1, -1, -1)
+    for causal, window in ((True, 30), (False, 0)):
+        r = {"out": torch.zeros_like(q), "log_sum": torch.zeros(batch, n, heads, device="cuda"), "gq": torch.zeros_like(q), "gk": torch.zeros(k.shape, dtype=k.dtype, device="cuda"), "gv": torch.zeros_like(v)}
+        vr = {name: view(t) for name, t in r.items()}
+        ocn.attention(view(q), view(k), view(v), vr["out"], 0.1, causal=causal, window=window, log_sum=vr["log_sum"])
+        ocn.attention_grad(view(w), view(q), view(k), view(v), vr["out"], vr["log_sum"], vr["gq"], vr["gk"], vr["gv"], 0.1, causal=causal, window=window)
+        shape = ([n] * batch, [m] * batch, heads, kv, d, causal, window)
+        data = tuple(t.flatten(0, 1).cpu() for t in (q, k, v, w))
+        check(shape, kind, data, {name: t.flatten(0, 1) for name, t in r.items()}, 0.1)
