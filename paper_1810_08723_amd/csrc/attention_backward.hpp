@@ -21,51 +21,45 @@ namespace {
 template <class T> constexpr float kWeightTop = std::is_same<T, f16>::value ? 12.0f : 0.0f;
 
 // A half's range is short for the s of all keys or rows: those of a lane's column are multiplied by a power of two of its own, chosen by the first of them and
-// lowered, with what has been summed, where one would pass 2^15.
+// lowered, with what has been summed, where one would pass 2^15.  (Its logarithm is added to that of the weights where these are for nothing but s.)  It is up
+// to 2^kMostShift, so that no product passes single precision's range (|s| < 2^41, weights up to 2^12): where all s are below 2^-60, they are short of bits that only a scale past 2^30 would show.
+constexpr int kMostShift = 60;
 template <class T> struct Range {
   static constexpr bool kNeeded = std::is_same<T, f16>::value;
-  float factor = kNeeded ? 0.0f : 1.0f;
-  __device__ __forceinline__ bool passes(float largest) const { return largest * factor > 32768.0f || (factor == 0.0f && largest > 0.0f); }
-  // what sums so far are to be multiplied by
-  __device__ __forceinline__ bool lower(float largest, float *keep) {
-    if constexpr (!kNeeded) return false;
-    *keep = 1.0f;
-    if (passes(largest)) {
-      int e = 12 - __builtin_amdgcn_frexp_expf(largest);
-      e = e > 120 ? 120 : e < -120 ? -120 : e;
-      const float f = __builtin_ldexpf(1.0f, e);
-      if (factor > 0.0f) *keep = f / factor;
-      factor = f;
-    }
-    return true;
+  float factor = 1.0f, limit = 0.0f;
+  __device__ __forceinline__ int exponent() const { return kNeeded ? __builtin_amdgcn_frexp_expf(factor) - 1 : 0; }
+  // the largest s of a column, times its factor so far: what s and sums so far are to be multiplied by
+  __device__ __forceinline__ float shift(float largest) {
+    if (!(largest > limit)) return 1.0f;
+    const int before = exponent(), e = before + 12 - __builtin_amdgcn_frexp_expf(largest);
+    const float f = __builtin_ldexpf(1.0f, (e > kMostShift ? kMostShift : e < -kMostShift ? -kMostShift : e) - before);
+    factor *= f, limit = 32768.0f;
+    return f;
   }
-  __device__ __forceinline__ float back() const { return !kNeeded ? 1.0f : factor > 0.0f ? 1.0f / factor : 0.0f; }
+  __device__ __forceinline__ float back() const { return kNeeded ? 1.0f / factor : 1.0f; }
 };
 
-// A weight from its exponent: above its row's sum by rounding alone, but of scores of any size.  (Up to 1 the instruction itself holds it to that.)
-template <class T> __device__ __forceinline__ float weight(float x) {
-  if constexpr (kWeightTop<T> > 0.0f) return __builtin_amdgcn_exp2f(fminf(x, kWeightTop<T>));
+// A weight from its exponent: above its row's sum (2^most) by rounding alone, but of scores of any size.  (Up to 1 the instruction itself holds it to that.)
+template <class T> __device__ __forceinline__ float weight(float x, float most = kWeightTop<T>) {
+  if constexpr (kWeightTop<T> > 0.0f) return __builtin_amdgcn_exp2f(fminf(x, most));
   return __builtin_amdgcn_fmed3f(__builtin_amdgcn_exp2f(x), 0.0f, 1.0f);
 }
 
-// s as fragments: times the column's factor
-template <class T, int TILES, class Out> __device__ __forceinline__ void in_range(acc_t<T> *s, Range<T> &range, Out *out, int outs) {
+// what to multiply a column's s and sums with, where some do not fit: s is times the factor
+template <class T> __device__ __forceinline__ void in_range(acc_t<T> &s, Range<T> &range, acc_t<T> *out, int outs) {
   if constexpr (Range<T>::kNeeded) {
-    float largest = 0.0f, keep;
+    float largest = 0.0f;
 #pragma unroll
-    for (int t = 0; t < TILES; ++t)
-#pragma unroll
-      for (int i = 0; i < Tile<T>::kOwn; ++i) largest = fmaxf(largest, __builtin_fabsf(s[t][i]));
-    if (__any(range.passes(largest)) && range.lower(column_max<T>(largest), &keep)) {
+    for (int i = 0; i < Tile<T>::kOwn; ++i) largest = fmaxf(largest, __builtin_fabsf(s[i]));
+    if (__any(largest > range.limit)) {
+      const float f = range.shift(column_max<T>(largest));
 #pragma unroll
       for (int ct = 0; ct < outs; ++ct)
 #pragma unroll
-        for (int i = 0; i < Tile<T>::kOwn; ++i) out[ct][i] *= keep;
+        for (int i = 0; i < Tile<T>::kOwn; ++i) out[ct][i] *= f;
+#pragma unroll
+      for (int i = 0; i < Tile<T>::kOwn; ++i) s[i] *= f;
     }
-#pragma unroll
-    for (int t = 0; t < TILES; ++t)
-#pragma unroll
-      for (int i = 0; i < Tile<T>::kOwn; ++i) s[t][i] *= range.factor;
   }
 }
 
@@ -208,12 +202,12 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
       int here = h;
       LanePlaces places = at_start;
       asm("" : "+v"(here), "+v"(places.row), "+v"(places.column));      // (what hangs on them is not kept in registers from tile to tile)
-      acc_t<T> p = no_sum<T>(), s[1];
+      acc_t<T> p = no_sum<T>(), s;
 #pragma unroll
       for (int i = 0; i < OWN; i += 4) {
         const f32x4 less = *(const f32x4 *)&of_row[turn][1][own_index<T>(i) + 4 * h];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[0][i + e] = less[e];
+        for (int e = 0; e < 4; ++e) s[i + e] = less[e];
       }
       pipelined<D / 16, 1, Operands<T>>(
           [&](int c) {
@@ -225,8 +219,8 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
           },
           [&](int c, const Operands<T> &o) {
             p = product(o.x, k[c], p);
-            if constexpr (HELD) s[0] = product(o.y, o.z, s[0]);
-            else s[0] = product(o.y, v[c], s[0]);
+            if constexpr (HELD) s = product(o.y, o.z, s);
+            else s = product(o.y, v[c], s);
           });
 #pragma unroll
       for (int i = 0; i < OWN; ++i) {
@@ -235,12 +229,12 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
           const int e = first_end + (int)fast_quotient((uint32_t)(own_index<T>(i) + 4 * here), a.heads_div);
           if (key >= e || (a.window && key < e - a.window)) p[i] = 0.0f;
         }
-        s[0][i] *= p[i];
+        s[i] *= p[i] * range.factor;
       }
-      in_range<T, 1>(s, range, gk, D / SIDE);
+      in_range<T>(s, range, gk, D / SIDE);
       frag_t<T> weights[Tile<T>::kSteps], slopes[Tile<T>::kSteps];
 #pragma unroll
-      for (int x = 0; x < Tile<T>::kSteps; ++x) weights[x] = as_fragment<T>(p, x), slopes[x] = as_fragment<T>(s[0], x);
+      for (int x = 0; x < Tile<T>::kSteps; ++x) weights[x] = as_fragment<T>(p, x), slopes[x] = as_fragment<T>(s, x);
       constexpr int TILES = D / SIDE, EACH = TILES * Tile<T>::kSteps;
       pipelined<2 * EACH, 2, frag_t<T>>([&](int i) { return columns_fragment<T, D>(i < EACH ? g : q, 16 * (i % EACH / TILES), i % TILES, places); },
                                         [&](int i, frag_t<T> x) {
@@ -375,9 +369,10 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
   const int hi_last = __builtin_amdgcn_readlane(own.hi, SIDE - 1), lo_first = __builtin_amdgcn_readfirstlane(own.lo);
   if (at < all.hi) store(0);
   const LanePlaces places = lane_places<T, D>(lane);
-  // scores and gout v of a tile, and the weights
+  Range<T> range;
+  // the weights of a tile (times the range's factor), and gout v, which is added to s
   const auto weights = [&](const char *k, const char *v, int first, acc_t<T> &p, acc_t<T> &s, auto masked) {
-    p = s = no_sum<T>();
+    p = no_sum<T>();
     pipelined<D / 16, 2, Operands<T>>(
         [&](int c) {
           Operands<T> o;
@@ -390,9 +385,10 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
           s = product(o.y, g[c], s);
         });
     const int lo = own.lo - first - 4 * h, hi = own.hi - first - 4 * h;
+    const float shift = (float)range.exponent(), less = stat.x + shift, most = kWeightTop<T> + shift;
 #pragma unroll
     for (int i = 0; i < OWN; ++i) {
-      p[i] = weight<T>(__builtin_fmaf(p[i], a.scale, stat.x));
+      p[i] = weight<T>(__builtin_fmaf(p[i], a.scale, less), most);
       if (masked && (own_index<T>(i) < lo || own_index<T>(i) >= hi)) p[i] = 0.0f;
     }
   };
@@ -407,7 +403,7 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
 #pragma nounroll
       for (int t = 0; t < KEYS; t += SIDE) {
         if (at + t >= hi_last || at + t + SIDE <= lo_first) continue;
-        acc_t<T> p, s;
+        acc_t<T> p, s = no_sum<T>();
         weights(k + t * PITCH, v + t * PITCH, at + t, p, s, std::true_type());
 #pragma unroll
         for (int i = 0; i < OWN; ++i) sum = __builtin_fmaf(p[i], p[i] > 0.0f ? s[i] : 0.0f, sum);
@@ -427,7 +423,9 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
   acc_t<T> gq[D / SIDE];
 #pragma unroll
   for (int ct = 0; ct < D / SIDE; ++ct) gq[ct] = no_sum<T>();
-  Range<T> range;
+  acc_t<T> start;      // of s
+#pragma unroll
+  for (int i = 0; i < OWN; ++i) start[i] = stat.y;
   const auto step = [&](auto masked, auto turn) {
     arrived();
     __syncthreads();
@@ -438,14 +436,14 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
     for (int t = 0; t < KEYS; t += SIDE) {
       const char *const k = keys + t * PITCH, *const v = values + t * PITCH;
       if (masked && (at + t >= hi_last || at + t + SIDE <= lo_first)) continue;
-      acc_t<T> p, s[1];
-      weights(k, v, at + t, p, s[0], masked);
+      acc_t<T> p, s = start;
+      weights(k, v, at + t, p, s, masked);
 #pragma unroll
-      for (int i = 0; i < OWN; ++i) s[0][i] = p[i] * (s[0][i] + stat.y);
-      in_range<T, 1>(s, range, gq, D / SIDE);
+      for (int i = 0; i < OWN; ++i) s[i] *= p[i];
+      in_range<T>(s, range, gq, D / SIDE);
       frag_t<T> slopes[Tile<T>::kSteps];
 #pragma unroll
-      for (int x = 0; x < Tile<T>::kSteps; ++x) slopes[x] = as_fragment<T>(s[0], x);
+      for (int x = 0; x < Tile<T>::kSteps; ++x) slopes[x] = as_fragment<T>(s, x);
       constexpr int TILES = D / SIDE;
       pipelined<TILES * Tile<T>::kSteps, 3, frag_t<T>>([&](int i) { return columns_fragment<T, D>(k, 16 * (i / TILES), i % TILES, places); },
                                                        [&](int i, frag_t<T> x) { gq[i % TILES] = product(x, slopes[i / TILES], gq[i % TILES]); });
