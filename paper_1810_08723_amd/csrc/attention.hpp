@@ -64,7 +64,10 @@ bool set_blocks(AttentionArgs &a, const AttentionSizes &s, int64_t rows, int64_t
 bool set_key_blocks(AttentionArgs &a, const AttentionSizes &s, int64_t keys, int64_t splits);
 
 // channels that kernels are made for
-inline int padded_channels(int64_t d) { return d <= 64 ? 64 : d <= 96 ? 96 : d <= 128 ? 128 : d <= 192 ? 192 : 256; }
+inline int padded_channels(int64_t d) { return d <= 64 ? 64 : d <= 80 ? 80 : d <= 96 ? 96 : d <= 128 ? 128 : d <= 192 ? 192 : 256; }
+
+// ... and those of a result, whole tiles
+inline int64_t result_channels(int32_t dtype, int64_t d) { return dtype == OCN_FLOAT ? padded_channels(d) : (padded_channels(d) + 31) / 32 * 32; }
 
 // What the shapes alone decide of a call: whether rows are few (the wavefronts of a workgroup then share them and take keys in turn), rows of a block, the parts that a
 // sequence's keys go to, units.
@@ -104,6 +107,7 @@ int run_attention_grad_float(AttentionArgs &a, const AttentionSizes &s, const At
   do {                                             \
     switch (padded_channels(d)) {                  \
       case 64: OCN_BY_ROWS(T, 64, vec, CALL);      \
+      case 80: OCN_BY_ROWS(T, 80, vec, CALL);      \
       case 96: OCN_BY_ROWS(T, 96, vec, CALL);      \
       case 128: OCN_BY_ROWS(T, 128, vec, CALL);    \
       case 192: OCN_BY_ROWS(T, 192, vec, CALL);    \

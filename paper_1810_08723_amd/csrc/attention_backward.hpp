@@ -66,7 +66,7 @@ template <class T> __device__ __forceinline__ void in_range(acc_t<T> &s, Range<T
 // (of results of TILE's products, in type T)
 template <class T, int D, bool VEC, class TILE = Tile<T>> __device__ __forceinline__ void store_columns(const typename TILE::Acc *acc, char *row, int64_t step, int h, int d, float factor) {
 #pragma unroll
-  for (int ct = 0; ct < D / TILE::kSide; ++ct)
+  for (int ct = 0; ct < kTilesOf<TILE, D>; ++ct)
 #pragma unroll
     for (int i = 0; i < TILE::kOwn; i += 4) {
       float v[4];
@@ -183,9 +183,9 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
   load_fragments<T, D, VEC>(k, a.k.base + w.sequence * a.k.batch + token * a.k.token + w.kv * a.k.head, a.k.channel, mine && !a.nothing ? a.channels : 0, h, a.negative);
   if constexpr (!HELD)
     load_fragments<T, D, VEC>(v, a.v.base + w.sequence * a.v.batch + token * a.v.token + w.kv * a.v.head, a.v.channel, mine ? a.channels : 0, h, false);
-  acc_t<T> gk[D / SIDE], gv[D / SIDE];
+  acc_t<T> gk[kTilesOf<Tile<T>, D>], gv[kTilesOf<Tile<T>, D>];
 #pragma unroll
-  for (int ct = 0; ct < D / SIDE; ++ct) gk[ct] = gv[ct] = no_sum<T>();
+  for (int ct = 0; ct < kTilesOf<Tile<T>, D>; ++ct) gk[ct] = gv[ct] = no_sum<T>();
   Range<T> range;
   if (left > 0) store(0);
   const int from = block + wave * SIDE;
@@ -231,11 +231,11 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
         }
         s[i] *= p[i] * range.factor;
       }
-      in_range<T>(s, range, gk, D / SIDE);
+      in_range<T>(s, range, gk, kTilesOf<Tile<T>, D>);
       frag_t<T> weights[Tile<T>::kSteps], slopes[Tile<T>::kSteps];
 #pragma unroll
       for (int x = 0; x < Tile<T>::kSteps; ++x) weights[x] = as_fragment<T>(p, x), slopes[x] = as_fragment<T>(s, x);
-      constexpr int TILES = D / SIDE, EACH = TILES * Tile<T>::kSteps;
+      constexpr int TILES = kTilesOf<Tile<T>, D>, EACH = TILES * Tile<T>::kSteps;
       pipelined<2 * EACH, 2, frag_t<T>>([&](int i) { return columns_fragment<T, D>(i < EACH ? g : q, 16 * (i % EACH / TILES), i % TILES, places); },
                                         [&](int i, frag_t<T> x) {
                                           const int ct = i % TILES;
@@ -267,9 +267,9 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
   if (!mine) return;
   const float weight = kWeightTop<T> > 0.0f ? 0x1p-12f : 1.0f;
   if (!part_here.alone) {
-    float *const to = a.parts + (((int64_t)w.unit * a.splits + w.split) * BLOCK + wave * SIDE + n) * (2 * D);
-    store_columns<float, D, true, Tile<T>>(gk, (char *)to, 4, h, D, weight * range.back());
-    store_columns<float, D, true, Tile<T>>(gv, (char *)(to + D), 4, h, D, weight);
+    float *const to = a.parts + (((int64_t)w.unit * a.splits + w.split) * BLOCK + wave * SIDE + n) * (2 * kWidth<T, D>);
+    store_columns<float, D, true, Tile<T>>(gk, (char *)to, 4, h, kWidth<T, D>, weight * range.back());
+    store_columns<float, D, true, Tile<T>>(gv, (char *)(to + kWidth<T, D>), 4, h, kWidth<T, D>, weight);
     return;
   }
   store_columns<T, D, VEC>(gk, a.gk.base + w.sequence * a.gk.batch + token * a.gk.token + w.kv * a.gk.head, a.gk.channel, h, a.channels, a.true_scale * weight * range.back());
@@ -290,10 +290,10 @@ template <class T, int D> __global__ __launch_bounds__(kBlock) void attention_ke
 #pragma unroll
     for (int c = 0; c < (D + kWave - 1) / kWave; ++c) gk[c] = gv[c] = 0.0f;
     for (int s = 0; s < a.splits && part_of(rows.tiles, a.splits, kLeastKeyTiles, s).mine; ++s) {
-      const float *const from = a.parts + (((int64_t)w.unit * a.splits + s) * keys + n) * (2 * D);
+      const float *const from = a.parts + (((int64_t)w.unit * a.splits + s) * keys + n) * (2 * kWidth<T, D>);
 #pragma unroll
       for (int c = 0; c < (D + kWave - 1) / kWave; ++c)
-        if (c * kWave + lane < D) gk[c] += from[c * kWave + lane], gv[c] += from[D + c * kWave + lane];
+        if (c * kWave + lane < D) gk[c] += from[c * kWave + lane], gv[c] += from[kWidth<T, D> + c * kWave + lane];
     }
     const int64_t token = w.k.first + block + n;
 #pragma unroll
@@ -420,9 +420,9 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
       store(0);
     }
   }
-  acc_t<T> gq[D / SIDE];
+  acc_t<T> gq[kTilesOf<Tile<T>, D>];
 #pragma unroll
-  for (int ct = 0; ct < D / SIDE; ++ct) gq[ct] = no_sum<T>();
+  for (int ct = 0; ct < kTilesOf<Tile<T>, D>; ++ct) gq[ct] = no_sum<T>();
   acc_t<T> start;      // of s
 #pragma unroll
   for (int i = 0; i < OWN; ++i) start[i] = stat.y;
@@ -440,11 +440,11 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
       weights(k, v, at + t, p, s, masked);
 #pragma unroll
       for (int i = 0; i < OWN; ++i) s[i] *= p[i];
-      in_range<T>(s, range, gq, D / SIDE);
+      in_range<T>(s, range, gq, kTilesOf<Tile<T>, D>);
       frag_t<T> slopes[Tile<T>::kSteps];
 #pragma unroll
       for (int x = 0; x < Tile<T>::kSteps; ++x) slopes[x] = as_fragment<T>(s, x);
-      constexpr int TILES = D / SIDE;
+      constexpr int TILES = kTilesOf<Tile<T>, D>;
       pipelined<TILES * Tile<T>::kSteps, 3, frag_t<T>>([&](int i) { return columns_fragment<T, D>(k, 16 * (i / TILES), i % TILES, places); },
                                                        [&](int i, frag_t<T> x) { gq[i % TILES] = product(x, slopes[i / TILES], gq[i % TILES]); });
     }
@@ -471,7 +471,7 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
 // host
 // ---------------------------------------------------------------------------------------
 
-template <class T, int D> constexpr bool kWideKeys = sizeof(T) == 2 && (D == 96 || D == 128);
+template <class T, int D> constexpr bool kWideKeys = sizeof(T) == 2 && (D > 64 && D <= 128);
 template <class T> constexpr int kGradKeys = sizeof(T) == 2 ? 64 : 32;
 
 int done(hipError_t e) {

@@ -192,7 +192,7 @@ constexpr int64_t kShortKeys = 128;               // sequences of so many keys o
 KeyPlan key_plan_of(const AttentionSizes &s, int32_t dtype, int64_t channels) {
   const int side = dtype == OCN_FLOAT ? 16 : 32, d = padded_channels(channels);
   KeyPlan p;
-  p.waves = dtype != OCN_FLOAT && (d == 96 || d == 128) && s.keys > kShortKeys * s.sequences ? 8 : 4;
+  p.waves = dtype != OCN_FLOAT && d > 64 && d <= 128 && s.keys > kShortKeys * s.sequences ? 8 : 4;
   p.units = key_units_of(s, side * p.waves);
   p.splits = 1;
   if (p.units > 0 && s.sequences > 0) {
@@ -214,7 +214,7 @@ static AttentionPlan plan_of(const ocn_tensor *q, const ocn_tensor *k, const ocn
   const AttentionSizes s = sizes_of(q, k, q_starts);
   p.few = s.sequences == 0 || s.queries * s.per_kv <= side * s.sequences;
   const int d = padded_channels(q->size[q->ndim - 1]);
-  p.waves = p.few ? kFewWaves : q->dtype != OCN_FLOAT && (d == 96 || d == 128) && units_of(s, 8 * side) >= kWideUnits ? 8 : 4;
+  p.waves = p.few ? kFewWaves : q->dtype != OCN_FLOAT && d > 64 && d <= 128 && units_of(s, 8 * side) >= kWideUnits ? 8 : 4;
   p.rows = p.few ? side : side * p.waves;
   p.units = units_of(s, p.rows);
   p.splits = 1;
@@ -229,9 +229,9 @@ static AttentionPlan plan_of(const ocn_tensor *q, const ocn_tensor *k, const ocn
 static size_t order_bytes(const AttentionPlan &p, const AttentionSizes &s) {
   return p.splits == 1 && !p.few && ordered(s, p.units) ? (size_t)slots_of_units(s, p.rows) * sizeof(uint32_t) : 0;
 }
-static size_t part_bytes(const AttentionPlan &p, int64_t channels) {
+static size_t part_bytes(const AttentionPlan &p, int32_t dtype, int64_t channels) {
   if (p.splits <= 1) return 0;
-  const int64_t d = padded_channels(channels), rows = p.units * p.splits * p.rows;
+  const int64_t d = result_channels(dtype, channels), rows = p.units * p.splits * p.rows;
   return (size_t)(rows * d + rows * 2) * sizeof(float);
 }
 
@@ -245,7 +245,7 @@ extern "C" {
 size_t ocn_attention_workspace_bytes(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *q_starts) {
   if (check_attention_sizes(q, k, q_starts) != OCN_OK) return 0;
   const AttentionPlan p = plan_of(q, k, q_starts);
-  return p.splits > 1 ? part_bytes(p, q->size[q->ndim - 1]) : order_bytes(p, sizes_of(q, k, q_starts));
+  return p.splits > 1 ? part_bytes(p, q->dtype, q->size[q->ndim - 1]) : order_bytes(p, sizes_of(q, k, q_starts));
 }
 
 int ocn_attention(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *v, const ocn_tensor *q_starts, const ocn_tensor *k_starts, double scale,
@@ -258,7 +258,7 @@ int ocn_attention(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *v,
   const HeadOperand ops[7] = {{q, false}, {k, false}, {v, false}, {q_starts, false}, {k_starts, false}, {out, true}, {log_sum, true}};
   if ((rc = check_operands(ops, 7)) != OCN_OK) return rc;
   const AttentionPlan p = plan_of(q, k, q_starts);
-  const size_t need = p.splits > 1 ? part_bytes(p, a.channels) : order_bytes(p, sizes_of(q, k, q_starts));
+  const size_t need = p.splits > 1 ? part_bytes(p, q->dtype, a.channels) : order_bytes(p, sizes_of(q, k, q_starts));
   if (need) {
     if (!workspace || workspace_bytes < need) return OCN_ERR_WORKSPACE;
     if ((uintptr_t)workspace % 256 != 0) return OCN_ERR_ALIGN;
@@ -270,7 +270,7 @@ int ocn_attention(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *v,
   a.rows = p.rows;
   if (p.splits > 1) {
     a.parts = (float *)workspace;
-    a.part_sums = a.parts + p.units * p.splits * p.rows * padded_channels(a.channels);
+    a.part_sums = a.parts + p.units * p.splits * p.rows * result_channels(q->dtype, a.channels);
   } else if (need) {
     a.order = (uint32_t *)workspace;
   }
@@ -286,7 +286,7 @@ int ocn_attention(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *v,
 static size_t grad_bytes(const AttentionSizes &s, int32_t dtype, int64_t channels) {
   const int side = dtype == OCN_FLOAT ? 16 : 32;
   const KeyPlan k = key_plan_of(s, dtype, channels);
-  return grad_head_bytes(s, side, k.waves) + (k.splits > 1 ? (size_t)(k.units * k.splits * side * k.waves) * 2 * padded_channels(channels) * sizeof(float) : 0);
+  return grad_head_bytes(s, side, k.waves) + (k.splits > 1 ? (size_t)(k.units * k.splits * side * k.waves) * 2 * result_channels(dtype, channels) * sizeof(float) : 0);
 }
 
 size_t ocn_attention_grad_workspace_bytes(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *q_starts) {

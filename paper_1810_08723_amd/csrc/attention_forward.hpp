@@ -27,7 +27,7 @@ constexpr float kFine = 1024.0f;
 // What a wavefront has of its rows
 template <class T, int D> struct Rows {
   frag_t<T> q[D / 16];
-  acc_t<T> out[D / Tile<T>::kSide];
+  acc_t<T> out[kTilesOf<Tile<T>, D>];
   float best, total;           // the score that weights are relative to (minus infinity: none yet), the sum of a lane's own weights
   int lo, hi;                  // keys that the row sees
   bool exact;                  // differences of scores are formed before they are scaled
@@ -154,7 +154,7 @@ template <class T, int D, int KEYS, bool MASKED> __device__ __forceinline__ bool
     r.best = now ? best : -__builtin_inff();
     r.total *= keep;
 #pragma unroll
-    for (int ct = 0; ct < D / SIDE; ++ct)
+    for (int ct = 0; ct < kTilesOf<Tile<T>, D>; ++ct)
 #pragma unroll
       for (int i = 0; i < OWN; ++i) r.out[ct][i] *= keep;
     sum = weigh<T, TILES>(s, p, best, scale, r.exact);
@@ -163,7 +163,7 @@ template <class T, int D, int KEYS, bool MASKED> __device__ __forceinline__ bool
   frag_t<T> f[TILES * STEPS];
 #pragma unroll
   for (int x = 0; x < TILES * STEPS; ++x) f[x] = as_fragment<T>(p[x / STEPS], x % STEPS);
-  constexpr int OUTS = D / SIDE;
+  constexpr int OUTS = kTilesOf<Tile<T>, D>;
   pipelined<TILES * STEPS * OUTS, kValuesAhead<T, D>, frag_t<T>>([&](int i) { return columns_fragment<T, D>(v, 16 * (i / OUTS), i % OUTS, places); },
                                                                  [&](int i, frag_t<T> x) { r.out[i % OUTS] = product(x, f[i / OUTS], r.out[i % OUTS]); });
   return MASKED && odd_values<T, D, KEYS>(v, lane);
@@ -205,7 +205,7 @@ template <class T, int D, bool VEC> __device__ __forceinline__ void start_rows(R
   r.total = 0.0f;
   r.exact = std::is_same<T, float>::value;
 #pragma unroll
-  for (int ct = 0; ct < D / SIDE; ++ct) r.out[ct] = zero_acc<T>();
+  for (int ct = 0; ct < kTilesOf<Tile<T>, D>; ++ct) r.out[ct] = zero_acc<T>();
   const char *at = q + (int64_t)p.query * a.q.token + (int64_t)p.head * a.q.head;
 #pragma unroll
   for (int c = 0; c < D / 16; ++c) {
@@ -243,7 +243,7 @@ template <class T, int D> __device__ __forceinline__ void leave_row(const Attent
   const int64_t part = part_row(a, w, row);
 #pragma unroll
   for (int c = 0; c < SlowRow<T, D>::kEach; ++c)
-    if (c * kWave + lane < D) a.parts[part * D + c * kWave + lane] = x[c];
+    if (c * kWave + lane < D) a.parts[part * kWidth<T, D> + c * kWave + lane] = x[c];
   if (lane == 0) a.part_sums[2 * part] = best, a.part_sums[2 * part + 1] = total;
 }
 
@@ -335,16 +335,16 @@ template <class T, int D, bool VEC, int WAVES, int KEYS> __global__ __launch_bou
   if (!split.alone) {
     const int64_t part = part_row(a, w, row);
 #pragma unroll
-    for (int ct = 0; ct < D / SIDE; ++ct)
+    for (int ct = 0; ct < kTilesOf<Tile<T>, D>; ++ct)
 #pragma unroll
       for (int i = 0; i < Tile<T>::kOwn; i += 4)
-        *(f32x4 *)(a.parts + part * D + ct * SIDE + own_index<T>(i) + 4 * (lane / SIDE)) = f32x4{r.out[ct][i], r.out[ct][i + 1], r.out[ct][i + 2], r.out[ct][i + 3]};
+        *(f32x4 *)(a.parts + part * kWidth<T, D> + ct * SIDE + own_index<T>(i) + 4 * (lane / SIDE)) = f32x4{r.out[ct][i], r.out[ct][i + 1], r.out[ct][i + 2], r.out[ct][i + 3]};
     if (lane < SIDE) a.part_sums[2 * part] = r.best, a.part_sums[2 * part + 1] = total;
     return;
   }
   char *const out = a.out.base + row_offset(a.out, a, w, p);
 #pragma unroll
-  for (int ct = 0; ct < D / SIDE; ++ct)
+  for (int ct = 0; ct < kTilesOf<Tile<T>, D>; ++ct)
 #pragma unroll
     for (int i = 0; i < Tile<T>::kOwn; i += 4) {
       float v[4];
@@ -363,7 +363,7 @@ template <class T, int D, bool VEC>
 __global__ __launch_bounds__(kFewWaves *kWave) __attribute__((amdgpu_waves_per_eu(kWavesAtOnce<T, D>))) void attention_few_kernel(const AttentionArgs a, uint32_t first_block) {
   warm_arguments<AttentionArgs>();
   constexpr int SIDE = Tile<T>::kSide, PITCH = Held<T, D>::kPitch, PART = 2 * SIDE * PITCH;
-  static_assert(SIDE * D * 4 <= PART, "a wavefront's results take the place of its keys and values");
+  static_assert(SIDE * kWidth<T, D> * 4 <= PART, "a wavefront's results take the place of its keys and values");
   __shared__ __align__(16) char lds[kFewWaves * PART];        // [wavefronts][keys, values][SIDE][PITCH]
   __shared__ float bests[kFewWaves][SIDE], totals[kFewWaves][SIDE];
   __shared__ bool odds[kFewWaves];
@@ -420,14 +420,14 @@ __global__ __launch_bounds__(kFewWaves *kWave) __attribute__((amdgpu_waves_per_e
 #pragma unroll
   for (int i = 1; i < kFewWaves; ++i) best = fmaxf(best, bests[i][n]);
   const float keep = r.best > -__builtin_inff() ? __builtin_amdgcn_exp2f((r.best - best) * a.scale) : 0.0f;
-  float *const own = (float *)k;       // [SIDE][D]
+  float *const own = (float *)k;       // [SIDE][kWidth]
 #pragma unroll
-  for (int ct = 0; ct < D / SIDE; ++ct)
+  for (int ct = 0; ct < kTilesOf<Tile<T>, D>; ++ct)
 #pragma unroll
-    for (int i = 0; i < Tile<T>::kOwn; ++i) own[n * D + ct * SIDE + own_index<T>(i) + 4 * (lane / SIDE)] = r.out[ct][i] * keep;
+    for (int i = 0; i < Tile<T>::kOwn; ++i) own[n * kWidth<T, D> + ct * SIDE + own_index<T>(i) + 4 * (lane / SIDE)] = r.out[ct][i] * keep;
   __syncthreads();
-  for (int i = threadIdx.x; i < SIDE * (D / 4); i += kFewWaves * kWave) {
-    const int row = i / (D / 4), e = i % (D / 4) * 4;
+  for (int i = threadIdx.x; i < SIDE * (kWidth<T, D> / 4); i += kFewWaves * kWave) {
+    const int row = i / (kWidth<T, D> / 4), e = i % (kWidth<T, D> / 4) * 4;
     const RowPlace p = row_place(a, w, row);
     if (!p.in) continue;
     float top = bests[0][row], sum = 0.0f, x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -437,7 +437,7 @@ __global__ __launch_bounds__(kFewWaves *kWave) __attribute__((amdgpu_waves_per_e
     for (int u = 0; u < kFewWaves; ++u) {
       const float b = bests[u][row];
       sum += totals[u][row] * (b > -__builtin_inff() ? __builtin_amdgcn_exp2f((b - top) * a.scale) : 1.0f);
-      const f32x4 y = *(const f32x4 *)(lds + u * PART + (row * D + e) * 4);
+      const f32x4 y = *(const f32x4 *)(lds + u * PART + (row * kWidth<T, D> + e) * 4);
 #pragma unroll
       for (int c = 0; c < 4; ++c) x[c] += y[c];
     }
@@ -449,7 +449,7 @@ __global__ __launch_bounds__(kFewWaves *kWave) __attribute__((amdgpu_waves_per_e
       if (a.log_sum.base && e == 0) *(float *)(a.log_sum.base + row_offset(a.log_sum, a, w, p)) = log_sum_of<T>(a, top, sum);
     } else {
       const int64_t part = part_row(a, w, row);
-      *(f32x4 *)(a.parts + part * D + e) = f32x4{x[0], x[1], x[2], x[3]};
+      *(f32x4 *)(a.parts + part * kWidth<T, D> + e) = f32x4{x[0], x[1], x[2], x[3]};
       if (e == 0) a.part_sums[2 * part] = top, a.part_sums[2 * part + 1] = sum;
     }
   }
@@ -484,7 +484,7 @@ template <class T, int D> __global__ __launch_bounds__(kBlock) void attention_jo
       const float f = __shfl(keep, s);
 #pragma unroll
       for (int c = 0; c < EACH; ++c)
-        if (c * kWave + lane < D) x[c] = __builtin_fmaf(a.parts[(part + (int64_t)s * a.rows) * D + c * kWave + lane], f, x[c]);
+        if (c * kWave + lane < D) x[c] = __builtin_fmaf(a.parts[(part + (int64_t)s * a.rows) * kWidth<T, D> + c * kWave + lane], f, x[c]);
     }
     finish_row<T, D>(a, w, p, x, top, sum, lane);
   }
@@ -503,7 +503,7 @@ int done(hipError_t e) {
 // Keys of a tile of many rows: half as many where a wavefront's results take half of its registers or more, which 64 scores to a row would drive to memory (half precision, 4 sequences of 4096 tokens, 16 heads of 192 channels: 511 for 714 us; 256 channels, which stay at one wavefront to a SIMD: 860 for 810 us, and 68 for 110 where rows begin anywhere).
 template <class T, int D> constexpr int kRowKeys = sizeof(T) == 2 && D <= 128 ? 64 : 32;
 
-template <class T, int D> constexpr bool kWide = sizeof(T) == 2 && (D == 96 || D == 128);
+template <class T, int D> constexpr bool kWide = sizeof(T) == 2 && (D > 64 && D <= 128);
 
 template <class T, int D, bool VEC> int run(AttentionArgs &a, const AttentionPlan &p, hipStream_t stream) {
   const int64_t blocks = p.units * p.splits;

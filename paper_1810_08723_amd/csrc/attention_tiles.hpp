@@ -58,6 +58,10 @@ template <class T> __device__ __forceinline__ frag_t<T> as_fragment(const acc_t<
   return f;
 }
 
+// tiles of channels of a result, which may have more than operands do, and channels of those
+template <class TILE, int D> constexpr int kTilesOf = (D + TILE::kSide - 1) / TILE::kSide;
+template <class T, int D> constexpr int kWidth = kTilesOf<Tile<T>, D> * Tile<T>::kSide;
+
 // over the lanes that hold a column
 template <class T> __device__ __forceinline__ float column_max(float x) {
   const auto a = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);

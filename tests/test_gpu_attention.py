@@ -345,7 +345,8 @@ def test_many_sequences(kind, causal, window):
 
 # few sequences of many rows, whose keys are cut into parts, and few keys of many rows, whose rows are; parts of which rows see none or some
 SPLIT = [([600], [3001], 2, 1, 128, True, 0), ([200, 90], [1500, 40], 4, 2, 250, False, 0), ([700], None, 3, 1, 80, True, 300), ([1500, 64], [70, 64], 4, 2, 64, False, 0),
-         ([900], [130], 6, 1, 128, True, 0), ([600], [300], 2, 2, 192, True, 100), ([333, 33], [1333, 1], 8, 8, 96, True, 700)]
+         ([900], [130], 6, 1, 128, True, 0), ([600], [300], 2, 2, 192, True, 100), ([333, 33], [1333, 1], 8, 8, 96, True, 700),
+         ([2, 3], [3000, 700], 6, 2, 80, True, 0), ([1], [2500], 1, 1, 66, False, 0), ([400], [140], 5, 1, 77, True, 90)]
 
 
 @pytest.mark.parametrize("kind", list(KIND))
