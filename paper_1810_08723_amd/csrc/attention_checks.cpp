@@ -7,15 +7,16 @@
 
 namespace ocn {
 
-constexpr int64_t kMostTokens = (int64_t)1 << 31;
+constexpr int64_t kMostRows = (int64_t)1 << 31;       // query heads of all tokens, and whatever else is counted in 32 bits: fewer than so many
+constexpr int64_t kMostTokens = (int64_t)1 << 30;     // of all sequences: sums of two positions and a window stay below 2^31
 
 static int check_rows(const ocn_tensor *t, bool packed) {
   const int rc = check_operand(t, kHeadTypes);
   if (rc != OCN_OK) return rc;
   if (t->ndim != (packed ? 3 : 4)) return OCN_ERR_NDIM;
   const int64_t *s = t->size + (packed ? 0 : 1);
-  if (s[2] > OCN_MAX_ATTENTION_CHANNELS || s[1] >= ((int64_t)1 << 24) || s[0] >= kMostTokens) return OCN_ERR_SHAPE;
-  if (!packed && (t->size[0] >= kMostTokens || (t->size[0] && s[0] >= kMostTokens / t->size[0]))) return OCN_ERR_SHAPE;
+  if (s[2] > OCN_MAX_ATTENTION_CHANNELS || s[1] >= ((int64_t)1 << 24) || s[0] > kMostTokens) return OCN_ERR_SHAPE;
+  if (!packed && (t->size[0] >= kMostRows || (t->size[0] && s[0] > kMostTokens / t->size[0]))) return OCN_ERR_SHAPE;
   return OCN_OK;
 }
 
@@ -26,7 +27,7 @@ int check_attention_sizes(const ocn_tensor *q, const ocn_tensor *k, const ocn_te
   if (packed) {
     if ((rc = check_operand(q_starts, kIndexTypes)) != OCN_OK) return rc;
     if (q_starts->ndim != 1) return OCN_ERR_NDIM;
-    if (q_starts->size[0] < 1 || q_starts->size[0] >= kMostTokens) return OCN_ERR_SHAPE;
+    if (q_starts->size[0] < 1 || q_starts->size[0] >= kMostRows) return OCN_ERR_SHAPE;
   }
   if (q->dtype != k->dtype) return OCN_ERR_DTYPE;
   const int at = packed ? 0 : 1;
@@ -36,7 +37,7 @@ int check_attention_sizes(const ocn_tensor *q, const ocn_tensor *k, const ocn_te
   if (kv == 0 ? heads != 0 : heads % kv != 0) return OCN_ERR_SHAPE;
   // (rows of a head of keys and values, and of all heads)
   const int64_t tokens = packed ? q->size[0] : q->size[0] * q->size[1];
-  if (tokens && heads >= kMostTokens / tokens) return OCN_ERR_SHAPE;
+  if (tokens && heads >= kMostRows / tokens) return OCN_ERR_SHAPE;
   return OCN_OK;
 }
 
@@ -128,7 +129,7 @@ int fill_attention(AttentionArgs &a, const ocn_tensor *q, const ocn_tensor *k, c
   a.kv = (int32_t)s.kv;
   a.per_kv = (int32_t)s.per_kv;
   a.causal = causal;
-  a.window = window >= kMostTokens ? 0 : (int32_t)window;
+  a.window = window >= a.k_starts.all ? 0 : (int32_t)window;      // (one of all keys is none)
   // (with a scale of zero queries are taken as zeros: places that are not seen have scores of minus infinity, which times zero would be NaN)
   a.nothing = scale == 0.0;
   a.negative = scale < 0.0;
@@ -156,7 +157,7 @@ int64_t key_units_of(const AttentionSizes &s, int64_t keys) { return slots_of_ke
 
 static bool set_all(AttentionArgs &a, const AttentionSizes &s, int64_t all, int64_t heads, int64_t head_blocks, int64_t tokens, int64_t splits) {
   const int64_t slots = slots_of(s, all, tokens);
-  if (slots >= kMostTokens || s.kv * head_blocks >= kMostTokens || slots * (s.kv * head_blocks) >= kMostTokens / splits) return false;
+  if (slots >= kMostRows || s.kv * head_blocks >= kMostRows || slots * (s.kv * head_blocks) >= kMostRows / splits) return false;
   a.heads = (int32_t)heads;
   a.head_blocks = (int32_t)head_blocks;
   a.tokens = (int32_t)tokens;

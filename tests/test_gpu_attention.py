@@ -410,3 +410,52 @@ def test_sequences_as_a_dimension_with_a_window(kind):
         shape = ([n] * batch, [m] * batch, heads, kv, d, causal, window)
         data = tuple(t.flatten(0, 1).cpu() for t in (q, k, v, w))
         check(shape, kind, data, {name: t.flatten(0, 1) for name, t in r.items()}, 0.1)
+
+
+@pytest.mark.parametrize("kind", list(KIND))
+@pytest.mark.parametrize("window", [19, 20, 2 ** 31 - 1, 2 ** 31, 2 ** 62])
+def test_windows_of_all_keys_and_more(kind, window):
+    """With more queries than keys, too, where positions relative to the keys are negative; the bits of no window"""
+    shape = ([50, 300, 20], [20, 7, 20], 4, 2, 64, True, window)
+    data = made(shape, kind, 19)
+    got = both(shape, kind, data)
+    check(shape, kind, data, got)
+    if window > 19:
+        want = both(shape[:6] + (0,), kind, data)
+        assert all(torch.equal(got[n], want[n]) for n in got)
+
+
+@pytest.mark.parametrize("kind", list(KIND))
+def test_nothing_of_something(kind):
+    """No queries, keys, heads, channels, sequences: zeros where there is somewhere to put them"""
+    for tokens, keys, heads, kv, d in ((0, 9, 4, 2, 64), (9, 0, 4, 2, 64), (0, 0, 4, 2, 64), (9, 9, 0, 2, 64), (9, 9, 0, 0, 64), (9, 9, 4, 2, 0), (9, 9, 4, 2, 1)):
+        q, k = torch.randn(tokens, heads, d), torch.randn(keys, kv, d)
+        data = tuple(t.to(KIND[kind]) for t in (q, k, torch.randn_like(k), torch.randn_like(q)))
+        shape = ([tokens], [keys], heads, kv, d, True, 0)
+        got = both(shape, kind, data, 0.3)
+        assert all((got[n] == 0).all() for n in ("gq", "gk", "gv") if tokens == 0 or keys == 0 or heads == 0), (tokens, keys, heads, kv, d)
+        if d == 0:
+            want = torch.arange(1, 10).double().log()[:, None]          # every score is zero
+            assert ((got["log_sum"].double().cpu() - want).abs() <= 4 * 2.0 ** -24 * (1 + want)).all()
+        elif keys == 0:
+            assert (got["out"] == 0).all() and (got["log_sum"] == -math.inf).all()
+        elif d == 1:
+            check(shape, kind, data, got, 0.3)
+        # sequences of nothing at all, as a dimension
+        ocn.attention(*(view(torch.zeros(0, n, h, d, dtype=KIND[kind], device="cuda")) for n, h in ((tokens, heads), (keys, kv), (keys, kv), (tokens, heads))), 0.3)
+
+
+def test_the_same_tensor_as_all_operands():
+    """Queries, keys, values and the gradient of the results may be one tensor"""
+    for kind in KIND:
+        shape = ([70, 9], None, 2, 2, 64, True, 0)
+        x = made(shape, kind, 20)[0]
+        want = both(shape, kind, (x, x.clone(), x.clone(), x.clone()))
+        check(shape, kind, (x, x, x, x), want)
+        t = x.cuda()
+        v, s = view(t), view(starts_of([70, 9]).cuda())
+        r = {n: torch.zeros_like(y) for n, y in want.items()}
+        vr = {n: view(y) for n, y in r.items()}
+        ocn.attention(v, v, v, vr["out"], 0.125, s, s, log_sum=vr["log_sum"])
+        ocn.attention_grad(v, v, v, v, vr["out"], vr["log_sum"], vr["gq"], vr["gk"], vr["gv"], 0.125, s, s)
+        assert all(torch.equal(r[n], want[n]) for n in want)

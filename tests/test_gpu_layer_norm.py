@@ -234,3 +234,11 @@ def test_another_stream_and_a_workspace_of_its_own():
     ocn.layer_norm_grad(view(g), view(x), view(w), view(gin2), view(got), view(gb), stream=side.cuda_stream)
     side.synchronize()
     assert torch.equal(got, want) and torch.equal(gb, wb) and torch.equal(gin, gin2)
+
+
+def test_no_rows():
+    """Gradients of factors are zeros where there are no rows"""
+    x = torch.zeros(0, 100, device="cuda")
+    gw, gb = torch.full((100,), 7.0, device="cuda"), torch.full((100,), 7.0, dtype=torch.bfloat16, device="cuda")
+    ocn.layer_norm_grad(view(x), view(x), view(torch.ones(100, device="cuda")), view(torch.zeros(0, 100, device="cuda")), view(gw), view(gb))
+    assert (gw == 0).all() and (gb == 0).all()

@@ -79,6 +79,11 @@ def test_channels_and_sizes_past_the_limits():
     assert a.refused(**many) == "SHAPE"
     keys = dict(k=T("half", (1 << 31, 2, 64), (0, 128, 2), base=1), v=T("half", (1 << 31, 2, 64), (0, 128, 2), base=2))
     assert a.refused(**keys) == "SHAPE"
+    for tokens, error in (((1 << 30) + 1, "SHAPE"), (1 << 30, "DEVICE")):      # (sums of positions are held in 32 bits; the second gets past the sizes)
+        keys = dict(k=T("half", (tokens, 2, 64), (0, 128, 2), base=1), v=T("half", (tokens, 2, 64), (0, 128, 2), base=2, device=1))
+        assert a.refused(**keys) == error
+        queries = dict(q=T("half", (tokens, 1, 64), (0, 128, 2)), k=packed(tokens=12, heads=1, base=1), v=packed(tokens=12, heads=1, base=2), out=T("half", (tokens, 1, 64), base=3, device=1))
+        assert a.refused(**queries) == error
     batch = dict(q_starts=None, k_starts=None, q=T("half", (1 << 16, 1 << 15, 2, 64), (0, 0, 128, 2)), k=T("half", (1 << 16, 4, 2, 64), (0, 0, 128, 2), base=1),
                  v=T("half", (1 << 16, 4, 2, 64), (0, 0, 128, 2), base=2), out=T("half", (1 << 16, 1 << 15, 2, 64), base=3))
     assert a.refused(**batch) == "SHAPE"
