@@ -284,20 +284,36 @@ template <class T, int D> __global__ __launch_bounds__(kBlock) void attention_ke
   if (!find_work_of<true>(a, unit * (uint32_t)a.splits, &w)) return;
   const int block = (int)(w.block * (uint32_t)keys);
   const KeyRows rows = key_rows(a, w, block, keys);
-  if (part_of(rows.tiles, a.splits, kLeastKeyTiles, 0).alone) return;
+  const int parts = part_of(rows.tiles, a.splits, kLeastKeyTiles, 0).parts;
+  if (parts == 1) return;
+  constexpr int EACH = (D + kWave - 1) / kWave, AT_ONCE = kJoinAtOnce / 2;
   for (int n = (int)chunk * kJoinRows + threadIdx.x / kWave; n < (int)(chunk + 1) * kJoinRows && block + n < rows.end; n += kBlock / kWave) {
-    float gk[(D + kWave - 1) / kWave], gv[(D + kWave - 1) / kWave];
+    float gk[EACH], gv[EACH];
 #pragma unroll
-    for (int c = 0; c < (D + kWave - 1) / kWave; ++c) gk[c] = gv[c] = 0.0f;
-    for (int s = 0; s < a.splits && part_of(rows.tiles, a.splits, kLeastKeyTiles, s).mine; ++s) {
-      const float *const from = a.parts + (((int64_t)w.unit * a.splits + s) * keys + n) * (2 * kWidth<T, D>);
+    for (int c = 0; c < EACH; ++c) gk[c] = gv[c] = 0.0f;
+    for (int s = 0; s < parts; s += AT_ONCE) {
+      float of_k[AT_ONCE][EACH], of_v[AT_ONCE][EACH];
 #pragma unroll
-      for (int c = 0; c < (D + kWave - 1) / kWave; ++c)
-        if (c * kWave + lane < D) gk[c] += from[c * kWave + lane], gv[c] += from[kWidth<T, D> + c * kWave + lane];
+      for (int u = 0; u < AT_ONCE; ++u) {
+        const float *const from = a.parts + (((int64_t)w.unit * a.splits + (s + u < parts ? s + u : parts - 1)) * keys + n) * (2 * kWidth<T, D>);
+#pragma unroll
+        for (int c = 0; c < EACH; ++c) {
+          const int e = c * kWave + lane < D ? c * kWave + lane : 0;
+          of_k[u][c] = from[e], of_v[u][c] = from[kWidth<T, D> + e];
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < AT_ONCE; ++u) {
+#pragma unroll
+        for (int c = 0; c < EACH; ++c) {
+          gk[c] = s + u < parts ? gk[c] + of_k[u][c] : gk[c];
+          gv[c] = s + u < parts ? gv[c] + of_v[u][c] : gv[c];
+        }
+      }
     }
     const int64_t token = w.k.first + block + n;
 #pragma unroll
-    for (int c = 0; c < (D + kWave - 1) / kWave; ++c) {
+    for (int c = 0; c < EACH; ++c) {
       const int e = c * kWave + lane;
       if (e >= a.channels) continue;
       *(T *)(a.gk.base + w.sequence * a.gk.batch + token * a.gk.token + w.kv * a.gk.head + e * a.gk.channel) = (T)(gk[c] * a.true_scale);

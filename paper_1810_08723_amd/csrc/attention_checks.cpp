@@ -205,9 +205,11 @@ KeyPlan key_plan_of(const AttentionSizes &s, int32_t dtype, int64_t channels) {
 }
 
 constexpr int64_t kWideUnits = 512;             // workgroups of eight wavefronts, which read keys and values half as often, from so many on
+constexpr int64_t kWideRows = 512;              // of a sequence's on average (and query heads): shorter ones leave wavefronts without rows
 constexpr int64_t kSplitRowWorkgroups = 512;     // of many rows
+constexpr int64_t kLeastRowSplits = 3;           // two parts save less than it takes to join them
 constexpr int64_t kRowKeys = 64;                 // keys of a tile of theirs (of floats half as many)
-constexpr int64_t kSplitWorkgroups = 2048;      // of few rows, as many as long sequences are split for
+constexpr int64_t kSplitWorkgroups = 512;      // of few rows, as many as long sequences are split for
 
 static AttentionPlan plan_of(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *q_starts) {
   AttentionPlan p;
@@ -215,14 +217,16 @@ static AttentionPlan plan_of(const ocn_tensor *q, const ocn_tensor *k, const ocn
   const AttentionSizes s = sizes_of(q, k, q_starts);
   p.few = s.sequences == 0 || s.queries * s.per_kv <= side * s.sequences;
   const int d = padded_channels(q->size[q->ndim - 1]);
-  p.waves = p.few ? kFewWaves : q->dtype != OCN_FLOAT && d > 64 && d <= 128 && units_of(s, 8 * side) >= kWideUnits ? 8 : 4;
+  const bool many = s.queries * s.per_kv > kWideRows * s.sequences && units_of(s, 8 * side) >= kWideUnits;
+  p.waves = p.few ? kFewWaves : q->dtype != OCN_FLOAT && d > 64 && d <= 128 && many ? 8 : 4;
   p.rows = p.few ? side : side * p.waves;
   p.units = units_of(s, p.rows);
   p.splits = 1;
   // (the longest sequence may be as long as all keys, and is not known here)
   const int64_t most = (int64_t)kWave, tiles = (s.keys + side - 1) / side;
   if (p.few && p.units > 0) p.splits = (int)std::max<int64_t>(1, std::min({most, kSplitWorkgroups / p.units, tiles / kLeastTiles}));
-  if (!p.few && p.units > 0) p.splits = (int)std::max<int64_t>(1, std::min({most, kSplitRowWorkgroups / p.units, tiles * side / (kRowKeys * kLeastRowTiles)}));
+  if (!p.few && p.units > 0) p.splits = (int)std::min({most, kSplitRowWorkgroups / p.units, tiles * side / (kRowKeys * kLeastRowTiles)});
+  if (!p.few && p.splits < kLeastRowSplits) p.splits = 1;
   return p;
 }
 

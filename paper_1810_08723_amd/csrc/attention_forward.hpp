@@ -248,11 +248,11 @@ template <class T, int D> __device__ __forceinline__ void leave_row(const Attent
 }
 
 // The part of a block's keys, in tiles of so many, that a workgroup has
-struct Split { int first, end; bool alone, mine; };
+struct Split { int first, end, parts; bool alone, mine; };
 __device__ __forceinline__ Split split_of(const AttentionArgs &a, const Limits &all, int keys, int least, int split) {
   const int lo = all.lo / keys, hi = (all.hi + keys - 1) / keys;
   const Part p = part_of(hi > lo ? hi - lo : 0, a.splits, least, split);
-  Split s = {(lo + p.first) * keys, (lo + p.end) * keys, p.alone, p.mine};
+  Split s = {(lo + p.first) * keys, (lo + p.end) * keys, p.parts, p.alone, p.mine};
   if (s.end > all.hi) s.end = all.hi;
   return s;
 }
@@ -463,12 +463,13 @@ template <class T, int D> __global__ __launch_bounds__(kBlock) void attention_jo
   const uint32_t chunks = (uint32_t)a.rows / kJoinRows, unit = (first + blockIdx.x) / chunks, chunk = first + blockIdx.x - unit * chunks;
   if (!find_work(a, unit * (uint32_t)a.splits, &w)) return;
   const Limits all = limits_of_block(a, w);
-  if (split_of(a, all, keys, least, 0).alone) return;
+  const int parts = split_of(a, all, keys, least, 0).parts;
+  if (parts == 1) return;
   for (int row = (int)chunk * kJoinRows + threadIdx.x / kWave; row < (int)(chunk + 1) * kJoinRows; row += kBlock / kWave) {
     const RowPlace p = row_place(a, w, row);
     if (!p.in) continue;
     const int64_t part = (int64_t)w.unit * a.splits * a.rows + row;
-    const bool there = lane < a.splits && split_of(a, all, keys, least, lane).mine;
+    const bool there = lane < parts;
     const float own = there ? a.part_sums[2 * (part + (int64_t)lane * a.rows)] : -__builtin_inff();
     float top = own;
 #pragma unroll
@@ -480,11 +481,20 @@ template <class T, int D> __global__ __launch_bounds__(kBlock) void attention_jo
     float x[EACH];
 #pragma unroll
     for (int c = 0; c < EACH; ++c) x[c] = 0.0f;
-    for (int s = 0; s < a.splits && split_of(a, all, keys, least, s).mine; ++s) {
-      const float f = __shfl(keep, s);
+    for (int s = 0; s < parts; s += kJoinAtOnce) {
+      float y[kJoinAtOnce][EACH];
 #pragma unroll
-      for (int c = 0; c < EACH; ++c)
-        if (c * kWave + lane < D) x[c] = __builtin_fmaf(a.parts[(part + (int64_t)s * a.rows) * kWidth<T, D> + c * kWave + lane], f, x[c]);
+      for (int u = 0; u < kJoinAtOnce; ++u) {
+        const float *const from = a.parts + (part + (int64_t)(s + u < parts ? s + u : parts - 1) * a.rows) * kWidth<T, D>;
+#pragma unroll
+        for (int c = 0; c < EACH; ++c) y[u][c] = from[c * kWave + lane < D ? c * kWave + lane : 0];
+      }
+#pragma unroll
+      for (int u = 0; u < kJoinAtOnce; ++u) {
+        const float f = __shfl(keep, (s + u) & (kWave - 1));
+#pragma unroll
+        for (int c = 0; c < EACH; ++c) x[c] = s + u < parts ? __builtin_fmaf(y[u][c], f, x[c]) : x[c];
+      }
     }
     finish_row<T, D>(a, w, p, x, top, sum, lane);
   }

@@ -379,19 +379,21 @@ __device__ __forceinline__ Limits limits_of_all(const AttentionArgs &a, const Wo
 // ---- parts -------------------------------------------------------------------------------------
 //
 // Where blocks leave CUs without work, what a block goes over (`tiles` of them) is cut into parts, a workgroup each, of `least` tiles or more.
-struct Part { int first, end; bool alone, mine; };      // its tiles; whether it is the only one; whether there is it
+struct Part { int first, end, parts; bool alone, mine; };      // its tiles; parts in all, one at least; whether it is the only one; whether there is it
 __device__ __forceinline__ Part part_of(int tiles, int splits, int least, int split) {
   int per = (tiles + splits - 1) / splits;
   if (per < least) per = least;
   Part p;
-  p.alone = tiles <= per;
-  p.mine = split == 0 || split * per < tiles;
+  p.parts = tiles <= per ? 1 : (tiles + per - 1) / per;
+  p.alone = p.parts == 1;
+  p.mine = split < p.parts;
   p.first = split * per;
   p.end = split * per + per < tiles ? split * per + per : tiles;
   return p;
 }
 
 constexpr int kJoinRows = 8;       // rows of a workgroup that joins parts, two of each wavefront
+constexpr int kJoinAtOnce = 8;     // parts of a row that are on their way from memory at once: one after the other, 64 of them took 23 us
 
 // ---- the order of blocks -----------------------------------------------------------------------
 //
