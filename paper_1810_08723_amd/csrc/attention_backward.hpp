@@ -513,12 +513,9 @@ template <class T, int D, bool VEC> int run_grad(AttentionArgs &a, const Attenti
   AttentionArgs of_keys = a;
   if (!set_blocks(a, sizes, side * kGradWaves, 1) || !set_key_blocks(of_keys, sizes, side * plan.waves, plan.splits)) return OCN_ERR_SHAPE;
   const int64_t units = units_of(sizes, side * kGradWaves), key_units = p.keys ? plan.units : 0;
-  uint32_t *const order = (uint32_t *)(stats + rows + 1);
-  if (ordered(sizes, units)) a.order = order;
-  if (ordered(sizes, key_units)) of_keys.order = order + slots_of_units(sizes, side * kGradWaves);
-  if (a.order || of_keys.order) {
-    hipLaunchKernelGGL(attention_order_kernel, dim3(2), dim3(kOrderLanes), 0, stream, a, BlockPlan{a.tokens, a.slots, a.tokens_div, a.order},
-                       BlockPlan{of_keys.tokens, of_keys.slots, of_keys.tokens_div, of_keys.order});
+  if (ordered(sizes, key_units * plan.splits)) {
+    of_keys.order = (uint32_t *)(stats + rows + 1);
+    hipLaunchKernelGGL(attention_order_kernel, dim3(1), dim3(kOrderLanes), 0, stream, of_keys);
     if ((rc = done(hipGetLastError())) != OCN_OK) return rc;
   }
   rc = in_launches(units, [&](uint32_t grid, uint32_t first) {

@@ -147,7 +147,7 @@ static int64_t slots_of(const AttentionSizes &s, int64_t all, int64_t tokens) {
   return s.packed ? all / tokens + s.sequences : s.sequences * ((all / s.sequences + tokens - 1) / tokens);
 }
 
-int64_t slots_of_units(const AttentionSizes &s, int64_t rows) { return slots_of(s, s.queries, rows / heads_of_block(s, rows)); }
+static int64_t slots_of_units(const AttentionSizes &s, int64_t rows) { return slots_of(s, s.queries, rows / heads_of_block(s, rows)); }
 int64_t slots_of_key_units(const AttentionSizes &s, int64_t keys) { return slots_of(s, s.keys, keys); }
 int64_t units_of(const AttentionSizes &s, int64_t rows) {
   const int64_t heads = heads_of_block(s, rows);
@@ -175,7 +175,7 @@ static bool set_all(AttentionArgs &a, const AttentionSizes &s, int64_t all, int6
 
 size_t grad_head_bytes(const AttentionSizes &s, int side, int waves) {
   const size_t n = (size_t)(s.queries * s.kv * s.per_kv + 1) * 2 * sizeof(float) +
-                   (size_t)(slots_of_units(s, side * kGradWaves) + slots_of_key_units(s, side * waves)) * sizeof(uint32_t);
+                   (size_t)slots_of_key_units(s, side * waves) * sizeof(uint32_t);
   return (n + 255) / 256 * 256;
 }
 
@@ -187,8 +187,10 @@ bool set_key_blocks(AttentionArgs &a, const AttentionSizes &s, int64_t keys, int
   return set_all(a, s, s.keys, std::max<int64_t>(1, s.per_kv), 1, keys, splits);
 }
 
-constexpr int64_t kSplitKeyWorkgroups = 512;      // that few blocks of keys are cut into
-constexpr int64_t kShortKeys = 128;               // sequences of so many keys on average have blocks of four wavefronts
+// Rows of few blocks of keys in parts (one sequence of 2048 tokens, 16 heads, 2 of keys, 128 channels, forward and gradient: 214 for 938 us)
+constexpr int64_t kSplitKeyWorkgroups = 512;
+// Sequences of so many keys on average have blocks of four wavefronts, so that few are left without keys (64 of 100 tokens, 8 heads, forward and gradient: 91 for 101 us)
+constexpr int64_t kShortKeys = 128;
 
 KeyPlan key_plan_of(const AttentionSizes &s, int32_t dtype, int64_t channels) {
   const int side = dtype == OCN_FLOAT ? 16 : 32, d = padded_channels(channels);
@@ -204,12 +206,16 @@ KeyPlan key_plan_of(const AttentionSizes &s, int32_t dtype, int64_t channels) {
   return p;
 }
 
-constexpr int64_t kWideUnits = 512;             // workgroups of eight wavefronts, which read keys and values half as often, from so many on
-constexpr int64_t kWideRows = 512;              // of a sequence's on average (and query heads): shorter ones leave wavefronts without rows
-constexpr int64_t kSplitRowWorkgroups = 512;     // of many rows
-constexpr int64_t kLeastRowSplits = 3;           // two parts save less than it takes to join them
+// Eight wavefronts, which share keys and values that four would read twice, where that leaves enough workgroups (32 query heads of 128 channels and 8 of keys, bfloat16: 377 for 393 us of
+// 8 sequences of 2048 tokens, but 73 for 70 of one), and where sequences are not so short that wavefronts are left without rows (64 of 100 tokens, forward and gradient: 91 for 82 us).
+constexpr int64_t kWideUnits = 512, kWideRows = 512;      // (the second: rows of a sequence, on average)
+// Parts of many rows' keys, where there are few workgroups (one sequence of 2048 tokens, 4 heads: 32 for 52 us; 100 queries over 8000 keys, 8 heads: 31 for 177).  Two parts save less than
+// it takes to join them (3 sequences of 1000 tokens, 8 heads: 43 for 33 us).
+constexpr int64_t kSplitRowWorkgroups = 512, kLeastRowSplits = 3;
 constexpr int64_t kRowKeys = 64;                 // keys of a tile of theirs (of floats half as many)
-constexpr int64_t kSplitWorkgroups = 512;      // of few rows, as many as long sequences are split for
+// Parts of few rows' keys: workgroups enough for all CUs (a token over 30000 keys, 32 heads, 8 of keys: 37 for 320 us), and more where sequences are so long that parts still have
+// kLongTiles tiles on average, as they may be of different lengths (48 of 1 to 8192: 161 for 185 us; 16 of 4000 keys, in 14 parts instead of 3: 57 for 53).
+constexpr int64_t kSplitWorkgroups = 512, kMostSplitWorkgroups = 2048, kLongTiles = 32;
 
 static AttentionPlan plan_of(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *q_starts) {
   AttentionPlan p;
@@ -224,16 +230,16 @@ static AttentionPlan plan_of(const ocn_tensor *q, const ocn_tensor *k, const ocn
   p.splits = 1;
   // (the longest sequence may be as long as all keys, and is not known here)
   const int64_t most = (int64_t)kWave, tiles = (s.keys + side - 1) / side;
-  if (p.few && p.units > 0) p.splits = (int)std::max<int64_t>(1, std::min({most, kSplitWorkgroups / p.units, tiles / kLeastTiles}));
+  if (p.few && p.units > 0) {
+    const int64_t longer = std::min(kMostSplitWorkgroups / p.units, tiles / (s.sequences * kLongTiles));
+    p.splits = (int)std::max<int64_t>(1, std::min({most, std::max(kSplitWorkgroups / p.units, longer), tiles / kLeastTiles}));
+  }
   if (!p.few && p.units > 0) p.splits = (int)std::min({most, kSplitRowWorkgroups / p.units, tiles * side / (kRowKeys * kLeastRowTiles)});
   if (!p.few && p.splits < kLeastRowSplits) p.splits = 1;
   return p;
 }
 
-// of the workspace: the order of blocks, or what parts of long sequences come to
-static size_t order_bytes(const AttentionPlan &p, const AttentionSizes &s) {
-  return p.splits == 1 && !p.few && ordered(s, p.units) ? (size_t)slots_of_units(s, p.rows) * sizeof(uint32_t) : 0;
-}
+// of the workspace: what parts of long sequences come to
 static size_t part_bytes(const AttentionPlan &p, int32_t dtype, int64_t channels) {
   if (p.splits <= 1) return 0;
   const int64_t d = result_channels(dtype, channels), rows = p.units * p.splits * p.rows;
@@ -250,7 +256,7 @@ extern "C" {
 size_t ocn_attention_workspace_bytes(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *q_starts) {
   if (check_attention_sizes(q, k, q_starts) != OCN_OK) return 0;
   const AttentionPlan p = plan_of(q, k, q_starts);
-  return p.splits > 1 ? part_bytes(p, q->dtype, q->size[q->ndim - 1]) : order_bytes(p, sizes_of(q, k, q_starts));
+  return part_bytes(p, q->dtype, q->size[q->ndim - 1]);
 }
 
 int ocn_attention(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *v, const ocn_tensor *q_starts, const ocn_tensor *k_starts, double scale,
@@ -263,7 +269,7 @@ int ocn_attention(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *v,
   const HeadOperand ops[7] = {{q, false}, {k, false}, {v, false}, {q_starts, false}, {k_starts, false}, {out, true}, {log_sum, true}};
   if ((rc = check_operands(ops, 7)) != OCN_OK) return rc;
   const AttentionPlan p = plan_of(q, k, q_starts);
-  const size_t need = p.splits > 1 ? part_bytes(p, q->dtype, a.channels) : order_bytes(p, sizes_of(q, k, q_starts));
+  const size_t need = part_bytes(p, q->dtype, a.channels);
   if (need) {
     if (!workspace || workspace_bytes < need) return OCN_ERR_WORKSPACE;
     if ((uintptr_t)workspace % 256 != 0) return OCN_ERR_ALIGN;
@@ -276,8 +282,6 @@ int ocn_attention(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *v,
   if (p.splits > 1) {
     a.parts = (float *)workspace;
     a.part_sums = a.parts + p.units * p.splits * p.rows * result_channels(q->dtype, a.channels);
-  } else if (need) {
-    a.order = (uint32_t *)workspace;
   }
   const bool vec = whole_rows(q) && whole_rows(k) && whole_rows(v) && whole_rows(out);
   switch (q->dtype) {
@@ -287,7 +291,7 @@ int ocn_attention(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *v,
   }
 }
 
-// two numbers of each row, and of a row that is none; the order of blocks of queries and of keys; what parts of blocks of keys come to
+// two numbers of each row, and of a row that is none; the order of blocks of keys; what parts of blocks of keys come to
 static size_t grad_bytes(const AttentionSizes &s, int32_t dtype, int64_t channels) {
   const int side = dtype == OCN_FLOAT ? 16 : 32;
   const KeyPlan k = key_plan_of(s, dtype, channels);

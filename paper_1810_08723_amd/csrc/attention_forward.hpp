@@ -519,10 +519,6 @@ template <class T, int D, bool VEC> int run(AttentionArgs &a, const AttentionPla
   const int64_t blocks = p.units * p.splits;
   int rc;
   const int64_t most = max_launch_blocks();
-  if (a.order) {
-    hipLaunchKernelGGL(attention_order_kernel, dim3(1), dim3(kOrderLanes), 0, stream, a, BlockPlan{a.tokens, a.slots, a.tokens_div, a.order}, BlockPlan{});
-    if ((rc = done(hipGetLastError())) != OCN_OK) return rc;
-  }
   for (int64_t at = 0; at < blocks; at += most) {
     const uint32_t grid = (uint32_t)std::min(blocks - at, most), first = (uint32_t)at;
     if (p.few) hipLaunchKernelGGL((attention_few_kernel<T, D, VEC>), dim3(grid), dim3(kFewWaves * kWave), 0, stream, a, first);

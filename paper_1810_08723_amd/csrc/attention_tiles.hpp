@@ -324,7 +324,7 @@ template <bool KEYS> __device__ __forceinline__ bool find_work_of(const Attentio
   const Starts &s = KEYS ? a.k_starts : a.q_starts;
   // With a causal mask the first blocks of keys and the last ones of queries have most to do.
   if (s.p) {
-    const uint32_t slot = a.order ? a.order[down] : KEYS ? down : a.slots - 1 - down;
+    const uint32_t slot = KEYS ? (a.order ? a.order[down] : down) : a.slots - 1 - down;
     if (!find_slot(s, KEYS ? a.q_starts : a.k_starts, a.tokens_div, slot, &w->sequence, &w->block, KEYS ? &w->k : &w->q, KEYS ? &w->q : &w->k)) return false;
   } else {
     const uint32_t turn = fast_quotient(down, a.sequences_div);
@@ -399,27 +399,26 @@ constexpr int kJoinAtOnce = 8;     // parts of a row that are on their way from 
 //
 // Packed sequences may be of any lengths, which only the GPU knows.  A workgroup that takes long and is started last is waited for by all the others: where there are more of them
 // than CUs, those with most to do go first.  One workgroup sorts all blocks by what they have to do, to a sixteenth of it.
-struct BlockPlan { int32_t tokens; uint32_t slots; FastDiv tokens_div; uint32_t *order; };
-
-template <bool KEYS> __device__ inline void order_blocks(const AttentionArgs &a, const BlockPlan &b, uint32_t *places) {
+constexpr int kOrderLanes = 1024;
+static __global__ __launch_bounds__(kOrderLanes) void attention_order_kernel(const AttentionArgs a) {
   constexpr int kSizes = 512;
-  const Starts &s = KEYS ? a.k_starts : a.q_starts;
+  __shared__ uint32_t places[kSizes];
+  const Starts &s = a.k_starts;
   const auto size_of = [&](uint32_t slot) {
     int lo = 0, hi = s.sequences;
     while (hi - lo > 1) {
       const int middle = lo + (hi - lo) / 2;
-      if (fast_quotient((uint32_t)start_at(s, middle), b.tokens_div) + (uint32_t)middle <= slot) lo = middle; else hi = middle;
+      if (fast_quotient((uint32_t)start_at(s, middle), a.tokens_div) + (uint32_t)middle <= slot) lo = middle; else hi = middle;
     }
     const Span q = span_of(a.q_starts, lo), k = span_of(a.k_starts, lo);
-    const int64_t block = (int64_t)slot - (fast_quotient((uint32_t)start_at(s, lo), b.tokens_div) + (uint32_t)lo), first = block * b.tokens;
-    const int64_t own = KEYS ? k.count : q.count, other = KEYS ? q.count : k.count;
-    if (block < 0 || first >= own) return 0;
-    const int64_t end = first + b.tokens < own ? first + b.tokens : own;
-    int64_t most = other;       // keys that a block of queries sees, or queries that see a block of keys
+    const int64_t block = (int64_t)slot - (fast_quotient((uint32_t)start_at(s, lo), a.tokens_div) + (uint32_t)lo), first = block * a.tokens;
+    if (block < 0 || first >= k.count) return 0;
+    const int64_t end = first + a.tokens < k.count ? first + a.tokens : k.count;
+    int64_t most = q.count;       // queries that see some key of the block
     if (a.causal) {
       const int64_t ahead = (int64_t)q.count - k.count;
-      const int64_t from = KEYS ? (first + ahead > 0 ? first + ahead : 0) : (a.window && first - ahead + 1 > a.window ? first - ahead + 1 - a.window : 0);
-      const int64_t to = KEYS ? (a.window && end - 1 + a.window + ahead < q.count ? end - 1 + a.window + ahead : q.count) : end - ahead;
+      const int64_t from = first + ahead > 0 ? first + ahead : 0;
+      const int64_t to = a.window && end - 1 + a.window + ahead < q.count ? end - 1 + a.window + ahead : q.count;
       most = to > from ? to - from : 0;
     }
     const int size = (int)(__builtin_bit_cast(uint32_t, (float)most) >> 19) - (126 << 4);       // four bits behind the first
@@ -427,7 +426,7 @@ template <bool KEYS> __device__ inline void order_blocks(const AttentionArgs &a,
   };
   for (int i = threadIdx.x; i < kSizes; i += blockDim.x) places[i] = 0;
   __syncthreads();
-  for (uint32_t i = threadIdx.x; i < b.slots; i += blockDim.x) atomicAdd(&places[size_of(i)], 1u);
+  for (uint32_t i = threadIdx.x; i < a.slots; i += blockDim.x) atomicAdd(&places[size_of(i)], 1u);
   __syncthreads();
   if (threadIdx.x < kWave) {      // blocks that are larger
     constexpr int kEach = kSizes / kWave;
@@ -448,18 +447,7 @@ template <bool KEYS> __device__ inline void order_blocks(const AttentionArgs &a,
     for (int i = 0; i < kEach; ++i) places[kSizes - 1 - lane * kEach - i] = before + own[i];
   }
   __syncthreads();
-  for (uint32_t i = threadIdx.x; i < b.slots; i += blockDim.x) b.order[atomicAdd(&places[size_of(i)], 1u)] = i;
-}
-
-// (the order of blocks of the same size is as it comes: results do not depend on it)
-constexpr int kOrderLanes = 1024;
-static __global__ __launch_bounds__(kOrderLanes) void attention_order_kernel(const AttentionArgs a, BlockPlan queries, BlockPlan keys) {
-  __shared__ uint32_t places[512];
-  if (blockIdx.x == 0) {
-    if (queries.order) order_blocks<false>(a, queries, places);
-  } else {
-    if (keys.order) order_blocks<true>(a, keys, places);
-  }
+  for (uint32_t i = threadIdx.x; i < a.slots; i += blockDim.x) a.order[atomicAdd(&places[size_of(i)], 1u)] = i;      // (those of the same size as they come: results do not depend on it)
 }
 
 }  // namespace ocn
