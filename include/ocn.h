@@ -432,14 +432,15 @@ int ocn_cache_attention(const ocn_tensor *q, const ocn_tensor *cache, const ocn_
  * q_starts[s] ... q_starts[s + 1] - 1 and the keys k_starts[s] ... k_starts[s + 1] - 1.  q_starts and k_starts: [sequences + 1], ascending (a start outside of its
  * tensor is taken as the nearest end of it; where starts descend, what is written to the tokens of the tensor is not defined).  Tokens of no sequence keep
  * what out holds.  With both NULL the sequences are a dimension of their own: q and out [batch, queries, heads, channels], k and v [batch, keys, kv heads, channels].
- * heads is a multiple of kv heads: query head h reads head h / (heads / kv heads).  At most OCN_MAX_ATTENTION_CHANNELS channels.
+ * heads is a multiple of kv heads: query head h reads head h / (heads / kv heads).  At most OCN_MAX_ATTENTION_CHANNELS channels,
+ * 2^30 tokens of queries and of keys, and fewer than 2^31 tokens times query heads (OCN_ERR_SHAPE).
  * In a sequence of n queries and m keys a query sees all keys; with OCN_CAUSAL query i sees the keys j <= i + m - n (the last query sees the last key), and the
  * last `window` of those where window is not 0 (without OCN_CAUSAL it has to be 0).  A query that sees nothing gets zeros.  What a query does not see, infinities
  * and NaNs among it, does not reach its results.  log_sum (or NULL): OCN_FLOAT [tokens, heads] ([batch, queries, heads]), the natural logarithm of
  * sum_j exp(scale * q_i . k_j), -inf where nothing is seen.  Scores, sums and the softmax are held in single precision (a scale past its range is
  * OCN_ERR_DOMAIN); for half and bfloat16 a weight (relative to the largest of its row, so far) is rounded to that type for the product with v, half a step
- * at most.  workspace: DEVICE scratch of ocn_attention_workspace_bytes(...) bytes (a function of the shapes alone; 0 where none is needed), 256-byte
- * aligned.  The same bits every time. */
+ * at most (in half, weights below 2^-23 of the row's largest are off by up to 2^-34 of that).  workspace: DEVICE scratch of ocn_attention_workspace_bytes(...)
+ * bytes (a function of the shapes alone; 0 where none is needed), 256-byte aligned; calls that may run at the same time need one each.  The same bits every time. */
 #define OCN_CAUSAL 4u
 #define OCN_MAX_ATTENTION_CHANNELS 256
 size_t ocn_attention_workspace_bytes(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *q_starts);
@@ -449,7 +450,9 @@ int ocn_attention(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *v,
 /* Its gradient: q_gin, k_gin and v_gin are the gradients with respect to q, k and v for gout, that with respect to out; out and log_sum are what
  * ocn_attention gave for the same q, k, v and arguments.  With D_i = gout_i . out_i and s_ij = p_ij (gout_i . v_j - D_i)
  *     v_gin_j = sum_i p_ij gout_i,    q_gin_i = scale * sum_j s_ij k_j,    k_gin_j = scale * sum_i s_ij q_i,
- * over all query heads that read a head, for k and v; zeros for keys that no query sees.  For half and bfloat16 p_ij and s_ij are rounded to that type for these products.
+ * over all query heads that read a head, for k and v; zeros for keys that no query sees.  Arithmetic is in single precision; for half and bfloat16 p_ij and s_ij are
+ * rounded to that type for these products, half a step at most (in half by up to 2^-37 and, of the largest s_ij of the query or key, by 2^-36: those are held in a range of
+ * their own, down to 2^-60).  D_i is taken from out as it is, with its rounding, or, where rows see few keys and that would show, from the weights.
  * q_gin may be NULL, and k_gin and v_gin both; no output may share bytes with an input.  An infinity or a NaN in a sequence may reach all of that sequence's gradients, and those of
  * no other.  workspace: DEVICE scratch of ocn_attention_grad_workspace_bytes(...) bytes, 256-byte aligned.  The same bits every time. */
 size_t ocn_attention_grad_workspace_bytes(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *q_starts);

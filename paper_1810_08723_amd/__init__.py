@@ -2,7 +2,8 @@
 
 Elementwise unary/binary operations, type-casting copies, axis/full reductions and reductions
 of an elementwise result (inner products, norms, counts) over strided, broadcast and reversed views, after the Ocean Tensor Package (arXiv 1810.08723);
-beside them the attention path of a transformer layer: rotary positions, norms of heads, a paged 4-bit cache and attention over it.
+beside them the attention path of a transformer layer: rotary positions on one or several axes, norms of heads, a paged 4-bit cache and attention over it,
+and for training the layer norm and attention over packed sequences, with their gradients.
 All computation happens in hand-written HIP kernels behind the C ABI of include/ocn.h; this
 package only marshals arguments.
 """

@@ -7,6 +7,8 @@
 // Two passes: one in which a workgroup has keys and goes over the rows (of all query heads that read them, so that their sums need no other workgroup), and one in which it has rows and goes over
 // keys.  Scores and weights are made in both, seven products where five would do: the five of one pass leave the gradient of q in pieces of
 // every block of keys, which would have to be added up in memory, in an order that changes from run to run or with more traffic than two products cost.
+// Products bound both, at half of the matrix cores' cycles and the clock that power allows: 4 sequences of 4096 tokens, 32 heads, 8 of keys, 128 channels in bfloat16 1.87 ms, 1.08 of them over keys
+// (with all seven products 1.03 PFLOP/s).
 #pragma once
 
 #include <algorithm>
@@ -326,6 +328,7 @@ template <class T, int D> __global__ __launch_bounds__(kBlock) void attention_ke
 //
 // gout * out, from the rounded out, is off by as much as out is.  Against the differences gout v - gout out that is little where a row sees many keys, but where it sees few it is as large as
 // the rounding of the results.  Rows of workgroups that see kFewKeys keys at most sum p (gout v) instead, in a pass over the keys of its own, and leave it in stats for the pass over keys.
+// (64 sequences of 100 tokens, 8 heads of 128 channels, forward and gradient: 82 us for 73 without, 250 tokens: 198 for 175.)
 constexpr int kFewKeys = 256;
 
 template <class T, int D, bool VEC, int WAVES, int KEYS>
@@ -488,7 +491,8 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
 // ---------------------------------------------------------------------------------------
 
 template <class T, int D> constexpr bool kWideKeys = sizeof(T) == 2 && (D > 64 && D <= 128);
-template <class T> constexpr int kGradKeys = sizeof(T) == 2 ? 64 : 32;
+// keys of a tile of rows' gradients: half as many where they are on their way in registers (4 sequences of 2000 tokens, 16 heads of 100 channels: 704 us for 1014, of 228: 2534 for 3317)
+template <class T, bool VEC> constexpr int kGradKeys = sizeof(T) == 2 && VEC ? 64 : 32;
 
 int done(hipError_t e) {
   if (e == hipSuccess) return OCN_OK;
@@ -519,7 +523,7 @@ template <class T, int D, bool VEC> int run_grad(AttentionArgs &a, const Attenti
     if ((rc = done(hipGetLastError())) != OCN_OK) return rc;
   }
   rc = in_launches(units, [&](uint32_t grid, uint32_t first) {
-    hipLaunchKernelGGL((attention_queries_kernel<T, D, VEC, kGradWaves, kGradKeys<T>>), dim3(grid), dim3(kGradWaves * kWave), 0, stream, a, first, stats, stats + rows);
+    hipLaunchKernelGGL((attention_queries_kernel<T, D, VEC, kGradWaves, kGradKeys<T, VEC>>), dim3(grid), dim3(kGradWaves * kWave), 0, stream, a, first, stats, stats + rows);
   });
   if (rc != OCN_OK) return rc;
   // (rows of a tile: whole queries with the heads of the group, or some of those)

@@ -7,7 +7,8 @@
 //     gradient of x = r (h - mean(h) - u mean(h u)),     of w: the sum over all rows of u times the gradient of out,     of b: of that gradient.
 //
 // A row is read once and stays in registers: its mean, then the deviations from it, whose squares are summed (two passes over registers: sums of
-// x and x^2 lose the variance of rows far from zero).  Memory bounds both directions, or, for a few rows, the launch.
+// x and x^2 lose the variance of rows far from zero).  Memory bounds both directions, or, for a few rows, the launch: 24705 rows of 1280 halves (127 MB) in 27.3 us,
+// 48 rows of 4096 in 4.7; the gradient of 16384 rows of 4096 bfloat16 (403 MB) in 82.4 us, of which a large copy would take 80.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -151,7 +152,7 @@ template <bool WIDE> constexpr int kMostLanes = WIDE ? kMostWaves * kWave : kBlo
 // A single-precision mean is off by some 2^-24 of itself; where results have as many bits, the mean of the deviations takes that away again.
 template <class T> constexpr bool kTwice = sizeof(T) == 4;
 
-// (two registers more of three chunks are a wavefront of a SIMD less: 29.6 for 26.5 us of 24705 rows of 1280 channels)
+// (wavefronts that a SIMD is to hold: two registers more of three chunks are one less, 29.6 for 27.3 us of 24705 rows of 1280 halves)
 template <class T, bool WIDE, int C> constexpr int kNormWaves = WIDE ? 8 : C == 4 ? 4 : C == 3 ? (sizeof(T) == 2 ? 6 : 5) : 8;
 
 template <class T, bool VEC, bool WIDE, int C>
@@ -203,7 +204,8 @@ __global__ __launch_bounds__(kMostLanes<WIDE>) __attribute__((amdgpu_waves_per_e
 }
 
 // The gradient.  A lane keeps the sums of its channels over all rows of its workgroup, workgroups leave theirs in the workspace, and a second launch adds them
-// up in a fixed order: no atomics, the same bits every time.  The next rows are on their way while one is worked on, as far as there are registers for them.
+// up in a fixed order: no atomics, the same bits every time.  The next rows are on their way while one is worked on, as far as there are registers for them (16384 rows of 4096
+// channels: 115 us for 137 with none).
 template <bool WIDE, int C> constexpr int kRowsAhead = C == 1 ? 2 : WIDE ? 0 : 1;
 
 template <class T, bool VEC, bool WIDE, int C> __global__ __launch_bounds__(kMostLanes<WIDE>) void layer_grad_kernel(const LayerArgs a) {
@@ -348,7 +350,8 @@ int done(hipError_t e) {
 }
 
 // How rows go to lanes: wavefronts of a row (1: a row has 2^lanes_log2 lanes of one), and chunks of eight channels of a lane.  Forward a lane has two chunks of a long row, so that enough
-// is on its way; backward, where it keeps sums of its channels and the next rows, one up to 8192 channels.
+// is on its way (16384 rows of 4096 channels: 49 us, 80 with one); backward, where it keeps sums of its channels and the next rows, one up to eight wavefronts (86 us, 102 with two), and two of
+// longer rows, which sixteen wavefronts would wait for one another over (16384 rows of 8192: 162 us for 199).
 struct Shape { int waves, chunks, lanes_log2; };
 Shape shape_of(int64_t width, bool grad) {
   int64_t lanes = 1;
@@ -357,7 +360,7 @@ Shape shape_of(int64_t width, bool grad) {
   if (width <= lanes * kEight) return {1, 1, log2};
   const int64_t chunk = kWave * kEight;
   if (width <= (grad ? 2 : 4) * chunk) return {1, (int)((width + chunk - 1) / chunk), 6};
-  const int chunks = grad && width <= kMostWaves * chunk ? 1 : 2;
+  const int chunks = grad && width <= 8 * chunk ? 1 : 2;
   return {(int)((width + chunks * chunk - 1) / (chunks * chunk)), chunks, 6};
 }
 
@@ -368,10 +371,11 @@ int64_t rows_of(const ocn_tensor *t) {
 }
 int64_t width_of(const ocn_tensor *t) { return t->size[t->ndim - 1]; }
 
-// workgroups of the gradient: as many as leave their sums a small part of what is read (twice as many where rows are short)
+// Workgroups of the gradient: as many as leave their sums a small part of what is read, twice as many where a lane has one chunk and a row four wavefronts or fewer (bfloat16: 16384 rows of
+// 2048 channels 46 us for 56 with 512, 65536 of 512 channels 45 for 56; but 16384 of 4096 channels 94 for 86, of 1024 channels, two chunks to a lane, 38 for 32).
 int64_t workers_of(int64_t rows, int64_t width) {
   const Shape s = shape_of(width, true);
-  const int64_t at_once = s.waves > 1 ? 1 : kBlock >> s.lanes_log2, most = width <= 2048 ? 1024 : 512;
+  const int64_t at_once = s.waves > 1 ? 1 : kBlock >> s.lanes_log2, most = s.waves <= 4 && s.chunks == 1 ? 1024 : 512;
   const int64_t want = (rows + at_once - 1) / at_once, rounds = std::max<int64_t>(1, (want + most - 1) / most);
   return std::max<int64_t>(1, (want + rounds - 1) / rounds);
 }

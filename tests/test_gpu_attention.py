@@ -459,3 +459,55 @@ def test_the_same_tensor_as_all_operands():
         ocn.attention(v, v, v, vr["out"], 0.125, s, s, log_sum=vr["log_sum"])
         ocn.attention_grad(v, v, v, v, vr["out"], vr["log_sum"], vr["gq"], vr["gk"], vr["gv"], 0.125, s, s)
         assert all(torch.equal(r[n], want[n]) for n in want)
+
+
+@pytest.mark.parametrize("tokens,keys", [(300, 300), (6, 900)])
+def test_a_replayed_graph_follows_its_starts(tokens, keys):
+    """Lengths that change between replays: few and many rows, empty sequences, one of all tokens, tokens of none"""
+    heads, kv, d = 4, 2, 64
+    data = made(([tokens], [keys], heads, kv, d, True, 0), "bfloat16", 21)
+    q, k, v, w = (t.cuda() for t in data)
+    starts = [torch.zeros(5, dtype=torch.int32, device="cuda") for _ in range(2)]
+    r = {"out": torch.zeros_like(q), "log_sum": torch.zeros(q.shape[:2], device="cuda"), "gq": torch.zeros_like(q), "gk": torch.zeros_like(k), "gv": torch.zeros_like(v)}
+    vr, s = {n: view(t) for n, t in r.items()}, [view(t) for t in starts]
+
+    def call():
+        ocn.attention(view(q), view(k), view(v), vr["out"], 0.125, *s, log_sum=vr["log_sum"])
+        ocn.attention_grad(view(w), view(q), view(k), view(v), vr["out"], vr["log_sum"], vr["gq"], vr["gk"], vr["gv"], 0.125, *s)
+
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for part in ([0, 0.2, 0.2, 0.9, 1], [0, 0, 0, 0, 1], [0.1, 0.5, 0.6, 0.6, 0.7], [1, 1, 1, 1, 1], [0, 0.3, 0.4, 0.8, 1]):
+        for t, n in zip(starts, (tokens, keys)):
+            t.copy_(torch.tensor([int(x * n) for x in part], dtype=torch.int32))
+        for t in r.values():
+            t.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = {n: t.clone() for n, t in r.items()}
+        sq, sk = spans(starts[0].cpu(), tokens), spans(starts[1].cpu(), keys)
+        want = attended(*(t.cpu() for t in (q, k, v)), sq, sk, 0.125, True, 0, "bfloat16", w.cpu(), got["out"].cpu())
+        for n in got:
+            close(n, got[n], want[n], None if n == "log_sum" else "bfloat16")
+            assert (got[n].cpu()[want[n][0].isnan()] == 7.0).all()
+        call()
+        assert all(torch.equal(got[n], r[n]) for n in got)
+
+
+def test_one_buffer_of_queries_keys_and_values_and_one_of_their_gradients():
+    shape = ([90, 1, 40], None, 4, 2, 64, True, 0)
+    data = made(shape, "half", 22)
+    want = both(shape, "half", data)
+    x, g = (torch.full((131, 8, 64), 7.0, dtype=torch.float16, device="cuda") for _ in range(2))
+    for t, part in zip(x.split([4, 2, 2], 1), data[:3]):
+        t.copy_(part)
+    q, k, v = (view(t) for t in x.split([4, 2, 2], 1))
+    gq, gk, gv = (view(t) for t in g.split([4, 2, 2], 1))
+    out, log, s = torch.zeros_like(want["out"]), torch.zeros_like(want["log_sum"]), view(starts_of(shape[0]).cuda())
+    ocn.attention(q, k, v, view(out), 0.125, s, s, log_sum=view(log))
+    ocn.attention_grad(view(data[3].cuda()), q, k, v, view(out), view(log), gq, gk, gv, 0.125, s, s)
+    assert torch.equal(out, want["out"]) and torch.equal(log, want["log_sum"])
+    assert torch.equal(g, torch.cat([want["gq"], want["gk"], want["gv"]], 1))
