@@ -114,8 +114,9 @@ __device__ __forceinline__ KeyRows key_rows(const AttentionArgs &a, const Work &
 }
 
 // Gradients of keys and values: a wavefront has a tile's side of keys, in registers, with the sums for them (values, where registers are short, lie in LDS); rows go through
-// LDS, the next ones on their way: some whole queries with the query heads of the group, or some of those.
-template <int D> constexpr bool kValuesHeld = D > 64;
+// LDS, the next ones on their way: some whole queries with the query heads of the group, or some of those.  (Up to 96 channels there are registers for values: nine sequences of 77 to 2903
+// tokens, 16 heads of 80 halves, 961 us for 989 with them in LDS.)
+template <int D> constexpr bool kValuesHeld = D > 96;
 
 // operands of a step of both products
 template <class T> struct Operands { frag_t<T> x, y, z; };
