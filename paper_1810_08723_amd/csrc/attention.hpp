@@ -81,9 +81,11 @@ int run_attention_float(AttentionArgs &a, const AttentionPlan &p, bool vec, void
 
 // From so many workgroups on, which are more than there are CUs, packed sequences' blocks of keys are put in order, by a launch of 5 us (32 query heads, 8 of keys, 128 channels,
 // bfloat16, all gradients: 1.89 for 2.27 ms of 4 sequences of 4096 tokens, 2.89 for 3.40 of 16 of 100 to 4096 in any order).  Blocks of queries, which are smaller and of which
-// neighbours that share keys are better kept together, take as long either way (forward: 0.90 and 0.90 ms of those 16).
+// neighbours that share keys are better kept together, take as long either way (forward: 0.90 and 0.90 ms of those 16).  One workgroup puts them in order, two blocks to a lane at
+// most: more are so many that the last ones matter little (400 sequences of 10 to 1000 tokens, 8 heads, 1189 blocks of each: 2.09 for 2.19 ms; 2000 of 10 to 100, 2860 blocks: 0.65 for 0.61).
 constexpr int64_t kOrderUnits = kNumCUs + 1;
-inline bool ordered(const AttentionSizes &s, int64_t units) { return s.packed && units >= kOrderUnits; }
+constexpr int kOrderLanes = 1024;
+inline bool ordered(const AttentionSizes &s, int64_t units, int64_t slots) { return s.packed && units >= kOrderUnits && slots <= 2 * kOrderLanes; }
 int64_t slots_of_key_units(const AttentionSizes &s, int64_t keys);
 
 // The gradient: rows (query heads of all tokens), and which gradients are wanted

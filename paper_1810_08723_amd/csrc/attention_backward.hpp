@@ -518,7 +518,7 @@ template <class T, int D, bool VEC> int run_grad(AttentionArgs &a, const Attenti
   AttentionArgs of_keys = a;
   if (!set_blocks(a, sizes, side * kGradWaves, 1) || !set_key_blocks(of_keys, sizes, side * plan.waves, plan.splits)) return OCN_ERR_SHAPE;
   const int64_t units = units_of(sizes, side * kGradWaves), key_units = p.keys ? plan.units : 0;
-  if (ordered(sizes, key_units * plan.splits)) {
+  if (ordered(sizes, key_units * plan.splits, slots_of_key_units(sizes, side * plan.waves))) {
     of_keys.order = (uint32_t *)(stats + rows + 1);
     hipLaunchKernelGGL(attention_order_kernel, dim3(1), dim3(kOrderLanes), 0, stream, of_keys);
     if ((rc = done(hipGetLastError())) != OCN_OK) return rc;

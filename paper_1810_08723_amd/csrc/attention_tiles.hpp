@@ -399,7 +399,6 @@ constexpr int kJoinAtOnce = 8;     // parts of a row that are on their way from 
 //
 // Packed sequences may be of any lengths, which only the GPU knows.  A workgroup that takes long and is started last is waited for by all the others: where there are more of them
 // than CUs, those with most to do go first.  One workgroup sorts all blocks by what they have to do, to a sixteenth of it.
-constexpr int kOrderLanes = 1024;
 static __global__ __launch_bounds__(kOrderLanes) void attention_order_kernel(const AttentionArgs a) {
   constexpr int kSizes = 512;
   __shared__ uint32_t places[kSizes];

@@ -511,3 +511,11 @@ def test_one_buffer_of_queries_keys_and_values_and_one_of_their_gradients():
     ocn.attention_grad(view(data[3].cuda()), q, k, v, view(out), view(log), gq, gk, gv, 0.125, s, s)
     assert torch.equal(out, want["out"]) and torch.equal(log, want["log_sum"])
     assert torch.equal(g, torch.cat([want["gq"], want["gk"], want["gv"]], 1))
+
+
+def test_more_sequences_than_are_put_in_order():
+    """2600 short sequences, some of them empty"""
+    lengths = torch.randint(0, 9, (2600,), generator=torch.Generator().manual_seed(23)).tolist()
+    shape = (lengths, None, 1, 1, 16, True, 0)
+    data = made(shape, "half", 23)
+    check(shape, "half", data, both(shape, "half", data))
