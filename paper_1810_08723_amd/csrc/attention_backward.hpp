@@ -267,6 +267,7 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
       turn ^= 1;
     }
   }
+  arrived();      // (the values, where no query sees a key of the block and no step has waited for them: LDS may be another workgroup's once this one has ended)
   if (!mine) return;
   const float weight = kWeightTop<T> > 0.0f ? 0x1p-12f : 1.0f;
   if (!part_here.alone) {
@@ -382,10 +383,8 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
     stat = f32x2{log_sum > -__builtin_inff() || log_sum != log_sum ? kWeightTop<T> - log_sum * 1.44269504088896340736f : -__builtin_inff(), -column_sum<T>(sum)};
     if (!few && place.in && lane < SIDE) *stat_at = stat;
   }
-  if (!few && !a.gq.base) {
-    arrived();      // (LDS may be another workgroup's once this one has ended)
-    return;
-  }
+  arrived();      // (the sums above have waited for loads behind these; LDS may be another workgroup's once this one has ended)
+  if (!few && !a.gq.base) return;
   const int hi_last = __builtin_amdgcn_readlane(own.hi, SIDE - 1), lo_first = __builtin_amdgcn_readfirstlane(own.lo);
   if (at < all.hi) store(0);
   const LanePlaces places = lane_places<T, D>(lane);
@@ -432,6 +431,7 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
     }
     stat.y = -column_sum<T>(sum) * (kWeightTop<T> > 0.0f ? 0x1p-12f : 1.0f);
     if (place.in && lane < SIDE) *stat_at = stat;
+    arrived();
     if (!a.gq.base) return;
     __syncthreads();
     at = all.lo / KEYS * KEYS, turn = 0;
@@ -482,6 +482,7 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
       turn ^= 1;
     }
   }
+  arrived();
   if (!place.in) return;
   const float weight = kWeightTop<T> > 0.0f ? 0x1p-12f : 1.0f;
   store_columns<T, D, VEC>(gq, a.gq.base + w.sequence * a.gq.batch + token * a.gq.token + head * a.gq.head, a.gq.channel, h, a.channels, a.true_scale * weight * range.back());

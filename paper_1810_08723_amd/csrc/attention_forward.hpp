@@ -319,6 +319,7 @@ template <class T, int D, bool VEC, int WAVES, int KEYS> __global__ __launch_bou
       turn ^= 1;
     }
   }
+  arrived();
   if (odd) {
 #pragma nounroll
     for (int i = wave * SIDE; i < wave * SIDE + SIDE; ++i) {

@@ -198,7 +198,7 @@ __device__ __forceinline__ void load_to_lds(uint32_t lds, const char *from) {
 __device__ __forceinline__ void load_word_to_lds(uint32_t lds, const char *from) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(from) : "memory");
 }
-// every load of the wavefront's has arrived
+// Every load of the wavefront's has arrived.  Kernels call it behind their loops as well: no path through them ends with a copy into LDS on its way.
 __device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ uint32_t lds_address(const char *p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)p; }
 
