@@ -108,3 +108,30 @@ def test_copies_have_arrived_before_the_end(which, tmp_path):
     assert len(found) == len(kernels)
     for name, (ends, copies) in found.items():
         assert copies > 0 and not ends, (name, copies, ends)
+
+
+@pytest.mark.skipif(not os.path.exists(HIPCC), reason="hipcc not installed")
+@pytest.mark.parametrize("copy", ["load_to_lds", "load_word_to_lds"])
+def test_copies_say_that_they_set_their_place(copy, tmp_path):
+    """The compiler, which keeps the register of a copy's place in LDS from one of its own copies to the next, sets it again behind one of these"""
+    from paper_1810_08723_amd.build import COMMON
+    source, listing = tmp_path / "kernel.hip", tmp_path / "kernel.s"
+    source.write_text(f'''#include "{os.path.join(CSRC, "attention_tiles.hpp")}"
+namespace ocn {{
+typedef __attribute__((address_space(1))) const uint32_t *Global;
+typedef __attribute__((address_space(3))) uint32_t *Lds;
+extern "C" __global__ void three_copies(const uint32_t *from, uint32_t *to, uint32_t at) {{
+  __shared__ __align__(16) uint32_t held[1024];
+  __builtin_amdgcn_global_load_lds((Global)from, (Lds)held, 4, 0, 0);
+  {copy}(lds_address((const char *)held) + at, (const char *)from);
+  __builtin_amdgcn_global_load_lds((Global)(from + 64), (Lds)held, 4, 0, 0);
+  arrived();
+  to[threadIdx.x] = held[threadIdx.x];
+}}
+}}
+''')
+    r = subprocess.run([HIPCC, *COMMON, "--cuda-device-only", "-S", "-x", "hip", str(source), "-o", str(listing)], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
+    body = listing.read_text().split("three_copies:")[1].split(".Lfunc_end")[0]
+    order = [m[1] for m in re.finditer(r"^\s*(s_mov_b32 m0|global_load_lds)", body, flags=re.M)]
+    assert order == ["s_mov_b32 m0", "global_load_lds"] * 3
