@@ -130,8 +130,8 @@ int fill_attention(AttentionArgs &a, const ocn_tensor *q, const ocn_tensor *k, c
   a.per_kv = (int32_t)s.per_kv;
   a.causal = causal;
   a.window = window >= a.k_starts.all ? 0 : (int32_t)window;      // (one of all keys is none)
-  // (with a scale of zero queries are taken as zeros: places that are not seen have scores of minus infinity, which times zero would be NaN)
-  a.nothing = scale == 0.0;
+  // (With a scale of zero, as single precision has it, queries are taken as zeros: places that are not seen have scores of minus infinity, which times zero would be NaN.)
+  a.nothing = (float)powers == 0.0f || (float)std::fabs(scale) == 0.0f;
   a.negative = scale < 0.0;
   a.scale = a.nothing ? 1.0f : (float)powers;
   a.plain_scale = a.nothing ? 1.0f : (float)std::fabs(scale);

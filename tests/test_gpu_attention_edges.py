@@ -2,7 +2,7 @@
 import pytest
 
 from heads_ref import KIND
-from test_gpu_attention import both, check, made
+from test_gpu_attention import both, check, close, made, reference
 
 pytestmark = pytest.mark.gpu
 
@@ -19,3 +19,18 @@ def test_keys_that_no_query_sees(shape, kind):
     check(shape, kind, data, got)
     if shape[0][0] == 0:
         assert all((got[n][:shape[1][0]] == 0).all() for n in ("gk", "gv"))
+
+
+@pytest.mark.parametrize("scale", [1e-44, 1e-46, -1e-46, 1e-300, -5e-324])
+def test_scales_below_single_precision(scale):
+    """All keys that a query sees weigh the same; keys that it does not see weigh nothing.  (The scale itself is off by half of single precision's least number where gradients are multiplied by it.)"""
+    shape = ([70, 5, 300], [70, 40, 300], 4, 2, 64, True, 0)
+    for kind in KIND:
+        data = made(shape, kind, 31)
+        got = both(shape, kind, data, scale)
+        want = reference(shape, kind, data, scale, got["out"].cpu())
+        for n in got:
+            value, bound = want[n]
+            if n in ("gq", "gk"):
+                bound = bound + 2.0 ** -150 * (1 + (value / scale).abs())
+            close(n, got[n], (value, bound), None if n == "log_sum" else kind)
