@@ -7,12 +7,14 @@
 //     gradient of x = r (h - mean(h) - u mean(h u)),     of w: the sum over all rows of u times the gradient of out,     of b: of that gradient.
 //
 // A row is read once and stays in registers: its mean, then the deviations from it, whose squares are summed (two passes over registers: sums of
-// x and x^2 lose the variance of rows far from zero).  Memory bounds both directions, or, for a few rows, the launch: 24705 rows of 1280 halves (127 MB) in 27.3 us,
+// x and x^2 lose the variance of rows far from zero).  A mean that is off by its own rounding is as far from a constant row as that row's deviations would be, and 1 / sqrt(eps) makes
+// results of the difference: means are of exact sums where values are alike, and divided exactly.  Memory bounds both directions, or, for a few rows, the launch: 24705 rows of 1280 halves (127 MB) in 27.3 us,
 // 48 rows of 4096 in 4.7; the gradient of 16384 rows of 4096 bfloat16 (403 MB) in 82.4 us, of which a large copy would take 80.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
 #include <cstring>
+#include <type_traits>
 
 #include "dev_types.hpp"
 #include "head_types.hpp"
@@ -32,7 +34,8 @@ struct LayerArgs {
   int32_t weight_whole, bias_whole;    // their channels lie together
   int32_t width, lanes_log2;           // lanes of a row, where they lie in one wavefront
   int32_t stream;
-  float eps, over;
+  float eps, over, wide;               // over: 1 / wide
+  double count, one_over;              // the same
 };
 
 __device__ __forceinline__ int64_t row_offset(const Lead &lead, const int64_t *stride, uint32_t row) {
@@ -149,8 +152,56 @@ template <bool WIDE, int N> __device__ __forceinline__ void sums_over_row(float 
 // Rows of up to 64 lanes have 256 lanes' workgroups together; longer ones a workgroup of as many wavefronts as they need.
 template <bool WIDE> constexpr int kMostLanes = WIDE ? kMostWaves * kWave : kBlock;
 
-// A single-precision mean is off by some 2^-24 of itself; where results have as many bits, the mean of the deviations takes that away again.
-template <class T> constexpr bool kTwice = sizeof(T) == 4;
+template <int CTRL> __device__ __forceinline__ double other_lane(double x) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  return __builtin_bit_cast(double, (uint64_t)other_lane_bits<CTRL>((uint32_t)(u >> 32)) << 32 | other_lane_bits<CTRL>((uint32_t)u));
+}
+__device__ __forceinline__ double sum_over_row(double v, int lanes) {
+  if (lanes > 1) v += other_lane<0xb1>(v);
+  if (lanes > 2) v += other_lane<0x4e>(v);
+  if (lanes > 4) v += other_lane<0x141>(v);
+  if (lanes > 8) v += other_lane<0x140>(v);
+  if (lanes > 16) v += __shfl_xor(v, 16);
+  if (lanes > 32) v += __shfl_xor(v, 32);
+  return v;
+}
+
+// A row's mean: rounded to single precision, and what it is more than that (single precision only; of the other types values have fewer bits than that rounding leaves).  Values of
+// single precision are summed in double.  Those of 11 bits and fewer that are alike have exact sums of 64 x 16 in single precision; wavefronts' sums are added in double.
+template <class T> constexpr bool kWhole = sizeof(T) == 4;
+struct Mean { float near, rest; };
+// s / n: where that is a number of the type, exactly that
+__device__ __forceinline__ double quotient(double s, double n, double over) {
+  const double q = s * over;
+  return __builtin_fma(__builtin_fma(-q, n, s), over, q);
+}
+__device__ __forceinline__ float quotient(float s, float n, float over) {
+  const float q = s * over;
+  return __builtin_fmaf(__builtin_fmaf(-q, n, s), over, q);
+}
+template <class T, bool WIDE, int C> __device__ __forceinline__ Mean mean_of_row(const LayerArgs &a, const eight_t<T> *x, int lanes, double *slots) {
+  typedef std::conditional_t<kWhole<T>, double, float> Sum;
+  Sum own = 0;
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+#pragma unroll
+    for (int i = 0; i < kEight; ++i) own += (Sum)x[c][i];
+  own = sum_over_row(own, WIDE ? kWave : lanes);
+  if constexpr (WIDE) {
+    if (threadIdx.x % kWave == 0) slots[threadIdx.x / kWave] = (double)own;
+    __syncthreads();
+    double all = 0.0;
+    for (int w = 0; w < lanes / kWave; ++w) all += slots[w];
+    const double mean = quotient(all, a.count, a.one_over);
+    return {(float)mean, kWhole<T> ? (float)(mean - (double)(float)mean) : 0.0f};
+  } else if constexpr (kWhole<T>) {
+    const double mean = quotient(own, a.count, a.one_over);
+    return {(float)mean, (float)(mean - (double)(float)mean)};
+  } else {
+    return {quotient(own, a.wide, a.over), 0.0f};
+  }
+}
+template <class T> __device__ __forceinline__ float deviation(float x, const Mean &m) { return kWhole<T> ? (x - m.near) - m.rest : x - m.near; }
 
 // (wavefronts that a SIMD is to hold: two registers more of three chunks are one less, 29.6 for 27.3 us of 24705 rows of 1280 halves)
 template <class T, bool WIDE, int C> constexpr int kNormWaves = WIDE ? 8 : C == 4 ? 4 : C == 3 ? (sizeof(T) == 2 ? 6 : 5) : 8;
@@ -158,7 +209,8 @@ template <class T, bool WIDE, int C> constexpr int kNormWaves = WIDE ? 8 : C == 
 template <class T, bool VEC, bool WIDE, int C>
 __global__ __launch_bounds__(kMostLanes<WIDE>) __attribute__((amdgpu_waves_per_eu(kNormWaves<T, WIDE, C>))) void layer_norm_kernel(const LayerArgs a, uint32_t first) {
   warm_arguments<LayerArgs>();
-  __shared__ float means[WIDE ? kMostWaves : 1][1], squares[WIDE ? kMostWaves : 1][2];
+  __shared__ double means[WIDE ? kMostWaves : 1];
+  __shared__ float squares[WIDE ? kMostWaves : 1][1];
   const int lanes = WIDE ? (int)blockDim.x : 1 << a.lanes_log2, lane = WIDE ? (int)threadIdx.x : (int)threadIdx.x & (lanes - 1), width = a.width;
   const Place<VEC> p(lane, lanes);
   const uint32_t row = WIDE ? first + blockIdx.x : (first + blockIdx.x) * (kBlock >> a.lanes_log2) + (threadIdx.x >> a.lanes_log2);
@@ -168,25 +220,17 @@ __global__ __launch_bounds__(kMostLanes<WIDE>) __attribute__((amdgpu_waves_per_e
 #pragma unroll
   for (int c = 0; c < C; ++c) x[c] = load_chunk<T, VEC>(from, a.xe, p, c, mine ? width : 0);
   char *to = a.out + row_offset(a.lead, a.ol, mine ? row : 0);
-  float m[1] = {0.0f};
-#pragma unroll
-  for (int c = 0; c < C; ++c)
-#pragma unroll
-    for (int i = 0; i < kEight; ++i) m[0] += (float)x[c][i];
-  sums_over_row<WIDE, 1>(m, lanes, means);
-  float mean = m[0] * a.over;
-  float s[2] = {0.0f, 0.0f};
+  const Mean mean = mean_of_row<T, WIDE, C>(a, x, lanes, means);
+  float s[1] = {0.0f};
 #pragma unroll
   for (int c = 0; c < C; ++c)
 #pragma unroll
     for (int i = 0; i < kEight; ++i) {
-      const float d = p.at(c, i) < width ? (float)x[c][i] - mean : 0.0f;
+      const float d = p.at(c, i) < width ? deviation<T>((float)x[c][i], mean) : 0.0f;
       s[0] = __builtin_fmaf(d, d, s[0]);
-      if (kTwice<T>) s[1] += d;
     }
-  sums_over_row<WIDE, 2>(s, lanes, squares);
-  const float rest = kTwice<T> ? s[1] * a.over : 0.0f;
-  const float r = __builtin_amdgcn_rsqf(__builtin_fmaf(-rest, rest, s[0] * a.over) + a.eps);
+  sums_over_row<WIDE, 1>(s, lanes, squares);
+  const float r = __builtin_amdgcn_rsqf(s[0] * a.over + a.eps);
   if (!mine) return;
 #pragma unroll
   for (int c = 0; c < C; ++c) {
@@ -195,9 +239,7 @@ __global__ __launch_bounds__(kMostLanes<WIDE>) __attribute__((amdgpu_waves_per_e
     load_factors<VEC>(a.bias, a.bias_stride, a.bias_type, a.bias_whole, p, c, width, 0.0f, b);
 #pragma unroll
     for (int i = 0; i < kEight; ++i) {
-      float d = (float)x[c][i] - mean;
-      if (kTwice<T>) d -= rest;
-      v[i] = __builtin_fmaf(d * r, w[i], b[i]);
+      v[i] = __builtin_fmaf(deviation<T>((float)x[c][i], mean) * r, w[i], b[i]);
     }
     store_chunk<T, VEC>(to, a.oe, p, c, width, v, a.stream);
   }
@@ -210,7 +252,8 @@ template <bool WIDE, int C> constexpr int kRowsAhead = C == 1 ? 2 : WIDE ? 0 : 1
 
 template <class T, bool VEC, bool WIDE, int C> __global__ __launch_bounds__(kMostLanes<WIDE>) void layer_grad_kernel(const LayerArgs a) {
   warm_arguments<LayerArgs>();
-  __shared__ float means[WIDE ? kMostWaves : 1][1], squares[WIDE ? kMostWaves : 1][4];
+  __shared__ double means[WIDE ? kMostWaves : 1];
+  __shared__ float squares[WIDE ? kMostWaves : 1][3];
   const int lanes = WIDE ? (int)blockDim.x : 1 << a.lanes_log2, lane = WIDE ? (int)threadIdx.x : (int)threadIdx.x & (lanes - 1), width = a.width;
   const Place<VEC> p(lane, lanes);
   const uint32_t rows = WIDE ? 1 : kBlock >> a.lanes_log2, mine = WIDE ? 0 : threadIdx.x >> a.lanes_log2;
@@ -239,29 +282,21 @@ template <class T, bool VEC, bool WIDE, int C> __global__ __launch_bounds__(kMos
     const bool in = row < a.lead.tokens;
     load(base + AHEAD * step, AHEAD);
     const eight_t<T> *const x0 = x[0], *const g0 = g[0];
-    float m[1] = {0.0f};
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-#pragma unroll
-      for (int i = 0; i < kEight; ++i) m[0] += (float)x0[c][i];
-    sums_over_row<WIDE, 1>(m, lanes, means);
-    const float mean = m[0] * a.over;
-    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};       // of d^2, h, h d, d
+    const Mean mean = mean_of_row<T, WIDE, C>(a, x0, lanes, means);
+    float s[3] = {0.0f, 0.0f, 0.0f};       // of d^2, h, h d
 #pragma unroll
     for (int c = 0; c < C; ++c) {
 #pragma unroll
       for (int i = 0; i < kEight; ++i) {
-        const float d = p.at(c, i) < width ? (float)x0[c][i] - mean : 0.0f, h = (float)g0[c][i] * w[c][i];
+        const float d = p.at(c, i) < width ? deviation<T>((float)x0[c][i], mean) : 0.0f, h = (float)g0[c][i] * w[c][i];
         s[0] = __builtin_fmaf(d, d, s[0]);
         s[1] += h;
         s[2] = __builtin_fmaf(h, d, s[2]);
-        if (kTwice<T>) s[3] += d;
       }
     }
-    sums_over_row<WIDE, 4>(s, lanes, squares);
-    const float rest = kTwice<T> ? s[3] * a.over : 0.0f;
-    const float r = __builtin_amdgcn_rsqf(__builtin_fmaf(-rest, rest, s[0] * a.over) + a.eps);
-    const float all = s[1] * a.over, along = __builtin_fmaf(-rest, s[1], s[2]) * a.over * r;
+    sums_over_row<WIDE, 3>(s, lanes, squares);
+    const float r = __builtin_amdgcn_rsqf(s[0] * a.over + a.eps);
+    const float all = s[1] * a.over, along = s[2] * a.over * r;
     if (in) {
       char *to = a.out + row_offset(a.lead, a.ol, row);
 #pragma unroll
@@ -269,9 +304,7 @@ template <class T, bool VEC, bool WIDE, int C> __global__ __launch_bounds__(kMos
         float v[kEight];
 #pragma unroll
         for (int i = 0; i < kEight; ++i) {
-          float d = (float)x0[c][i] - mean;
-          if (kTwice<T>) d -= rest;
-          const float u = d * r, gg = (float)g0[c][i];
+          const float u = deviation<T>((float)x0[c][i], mean) * r, gg = (float)g0[c][i];
           gw[c * kEight + i] = __builtin_fmaf(gg, u, gw[c * kEight + i]);
           gb[c * kEight + i] += gg;
           v[i] = r * (__builtin_fmaf(gg, w[c][i], -all) - u * along);
@@ -428,6 +461,9 @@ int fill(LayerArgs &a, const ocn_tensor *x, const ocn_tensor *g, const ocn_tenso
   a.width = (int32_t)width_of(x);
   a.lanes_log2 = shape_of(a.width, g != nullptr).lanes_log2;
   a.over = a.width ? 1.0f / (float)a.width : 0.0f;
+  a.wide = (float)a.width;
+  a.count = (double)a.width;
+  a.one_over = a.width ? 1.0 / a.count : 0.0;
   a.eps = (float)eps;
   a.stream = (int64_t)a.lead.tokens * a.width * head_type_size(out->dtype) >= kStreamBytes;
   return OCN_OK;
