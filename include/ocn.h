@@ -450,7 +450,8 @@ int ocn_attention(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *v,
 /* Its gradient: q_gin, k_gin and v_gin are the gradients with respect to q, k and v for gout, that with respect to out; out and log_sum are what
  * ocn_attention gave for the same q, k, v and arguments.  With D_i = gout_i . out_i and s_ij = p_ij (gout_i . v_j - D_i)
  *     v_gin_j = sum_i p_ij gout_i,    q_gin_i = scale * sum_j s_ij k_j,    k_gin_j = scale * sum_i s_ij q_i,
- * over all query heads that read a head, for k and v; zeros for keys that no query sees.  Arithmetic is in single precision; for half and bfloat16 p_ij and s_ij are
+ * over all query heads that read a head, for k and v; zeros for keys that no query sees.  Arithmetic is in single precision, for scores of any size: p_ij comes from the score and log_sum where
+ * log_sum is within 88 of zero (and is off by less than 3e-5 of itself), past that from the row's largest score, found again, and the sum relative to it.  For half and bfloat16 p_ij and s_ij are
  * rounded to that type for these products, half a step at most (in half by up to 2^-37 and, of the largest s_ij of the query or key, by 2^-36: those are held in a range of
  * their own, down to 2^-60).  D_i is taken from out as it is, with its rounding, or, where rows see few keys and that would show, from the weights.
  * q_gin may be NULL, and k_gin and v_gin both; no output may share bytes with an input.  An infinity or a NaN in a sequence may reach all of that sequence's gradients, and those of

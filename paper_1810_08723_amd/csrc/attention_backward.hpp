@@ -97,6 +97,47 @@ template <class T> __device__ __forceinline__ acc_t<T> no_sum() {
   return a;
 }
 
+// ---- scores far from zero ------------------------------------------------------------------------
+//
+// A weight is 2^(score scale - log2 of the row's sum), and log_sum as it is given, rounded at its own size, is off by as much as a score of that size.  The four half steps of single precision that the exponent
+// is off by change a weight by less than 3 10^-5 of itself up to kFar.  Past that a row has a reference, its largest score, as forward has one, and the sum of its weights relative to it: the
+// pass over rows finds both, from its own scores, before anything else.  A weight is 2^((score - reference) scale - log2 of that sum), with the difference formed first.  Both passes make the same
+// bits of a score: products of the same channels in the same order.
+constexpr float kFar = 128.0f;
+
+// What the passes need of a row, in the workspace, and of a row that is none, which has weights of zero: the exponent's part, minus gout * out, the reference (0: not far).  The order of blocks of
+// keys is behind them.
+constexpr int kRowPairs = 2;
+
+// The largest score of the rows of a wavefront and the sum of their weights relative to it; `lo` and `hi`: what a row sees, `from` and `to`: what any of the rows do.  Keys come straight from memory.
+template <class T, int D, bool VEC>
+__device__ __forceinline__ void far_sums(const AttentionArgs &a, const frag_t<T> *q, const char *keys, int count, int lo, int hi, int from, int to, int lane, float *largest, float *sum) {
+  constexpr int SIDE = Tile<T>::kSide, OWN = Tile<T>::kOwn;
+  const int n = lane & (SIDE - 1), h = lane / SIDE;
+  float best = -__builtin_inff(), total = 0.0f;
+#pragma nounroll
+  for (int first = from / SIDE * SIDE; first < to; first += SIDE) {
+    frag_t<T> k[D / 16];
+    load_fragments<T, D, VEC>(k, keys + (int64_t)(first + n < count ? first + n : count - 1) * a.k.token, a.k.channel, a.channels, h, false);
+    acc_t<T> p = no_sum<T>();
+    pipelined<D / 16, 0, frag_t<T>>([&](int c) { return k[c]; }, [&](int c, frag_t<T> x) { p = product(x, q[c], p); });
+    float top = best;
+#pragma unroll
+    for (int i = 0; i < OWN; ++i) {
+      const int j = first + 4 * h + own_index<T>(i);
+      if (j < lo || j >= hi) p[i] = -__builtin_inff();
+      top = fmaxf(top, p[i]);
+    }
+    top = column_max<T>(top);
+    const float base = top > -__builtin_inff() ? top : 0.0f;
+    total *= __builtin_amdgcn_exp2f((best - base) * a.scale);
+#pragma unroll
+    for (int i = 0; i < OWN; ++i) total += __builtin_amdgcn_exp2f((p[i] - base) * a.scale);
+    best = top;
+  }
+  *largest = best, *sum = column_sum<T>(total);
+}
+
 // Queries that see some key of a block (query i sees the keys before i - ahead + 1), from a multiple of a tile's on, and the tiles that they make
 struct KeyRows { int lo, hi, end, ahead, across, tiles; };
 __device__ __forceinline__ KeyRows key_rows(const AttentionArgs &a, const Work &w, int block, int keys) {
@@ -128,7 +169,7 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
   constexpr bool HELD = kValuesHeld<D>;
   __shared__ __align__(16) char held[2 * 2 * SIDE * PITCH];      // [2][q, gout][SIDE][PITCH]
   __shared__ __align__(16) char values[HELD ? BLOCK * PITCH : 16];
-  __shared__ __align__(16) float of_row[2][2][kWave / 2];          // [2][exponent's part, minus gout out]
+  __shared__ __align__(16) float of_row[2][4][kWave / 2];          // [2][exponent's part, minus gout out, reference, nothing]
   const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), n = lane & (SIDE - 1), h = lane / SIDE;
   Work w;
   if (!find_work_of<true>(a, first_block + blockIdx.x, &w)) return;
@@ -147,9 +188,9 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
   const int64_t head = (int64_t)w.kv * a.per_kv, heads = (int64_t)a.kv * a.per_kv;
   const char *const pq = a.q.base + w.sequence * a.q.batch + w.q.first * a.q.token + head * a.q.head;
   const char *const pg = a.gout.base + w.sequence * a.gout.batch + w.q.first * a.gout.token + head * a.gout.head;
-  const f32x2 *const ps = stats + (w.sequence * (a.q_starts.p ? 0 : a.q_starts.all) + w.q.first) * heads + head;
+  const f32x2 *const ps = stats + kRowPairs * ((w.sequence * (a.q_starts.p ? 0 : a.q_starts.all) + w.q.first) * heads + head);
   Carrier<T, D, SIDE, WAVES, VEC> cq, cg;
-  const auto load = [&](int at, int part, int turn) {
+  const auto load = [&](int at, int part, int turn) __attribute__((always_inline)) {
     char *const q = held + turn * 2 * SIDE * PITCH;
     const int last = hi - 1 - at, past = a.per_kv - 1 - part * a.heads;
     const auto row = [&](const HeadView &x, const char *p, int i) {       // (rows that are none are some other one)
@@ -164,8 +205,10 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
       int i = lane & 31;
       asm("" : "+v"(i));
       const int t = (int)fast_quotient((uint32_t)i, a.heads_div), g = i - t * a.heads;
-      const f32x2 *from = i < SIDE && t < a.rows_of_tile && t <= last && g <= past ? ps + (int64_t)(at + t) * heads + part * a.heads + g : no_row;
-      load_word_to_lds(__builtin_amdgcn_readfirstlane(lds_address((const char *)of_row[turn])), (const char *)from + (lane >> 5) * 4);
+      const f32x2 *from = i < SIDE && t < a.rows_of_tile && t <= last && g <= past ? ps + kRowPairs * ((int64_t)(at + t) * heads + part * a.heads + g) : no_row;
+      const uint32_t to = __builtin_amdgcn_readfirstlane(lds_address((const char *)of_row[turn]));
+      load_word_to_lds(to, (const char *)from + (lane >> 5) * 4);
+      load_word_to_lds(to + kWave * 4, (const char *)(from + 1) + (lane >> 5) * 4);
     }
   };
   const auto store = [&](int turn) {
@@ -193,7 +236,7 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
   if (left > 0) store(0);
   const int from = block + wave * SIDE;
   const LanePlaces at_start = lane_places<T, D>(lane);
-  const auto step = [&](auto masked, auto turn) {
+  const auto step = [&](auto masked, auto turn) __attribute__((always_inline)) {
     arrived();
     __syncthreads();
     const char *const q = held + turn * 2 * SIDE * PITCH, *const g = q + SIDE * PITCH;
@@ -212,6 +255,7 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[i + e] = less[e];
       }
+      const bool far = __any(of_row[turn][2][lane & 31] != 0.0f);
       pipelined<D / 16, 1, Operands<T>>(
           [&](int c) {
             Operands<T> o;
@@ -225,6 +269,9 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
             if constexpr (HELD) s = product(o.y, o.z, s);
             else s = product(o.y, v[c], s);
           });
+      if (__builtin_expect(far, 0))
+#pragma unroll
+        for (int i = 0; i < OWN; ++i) p[i] -= of_row[turn][2][own_index<T>(i) + 4 * here];
 #pragma unroll
       for (int i = 0; i < OWN; ++i) {
         p[i] = weight<T>(__builtin_fmaf(p[i], a.scale, of_row[turn][0][own_index<T>(i) + 4 * h]));
@@ -339,7 +386,7 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
   constexpr int SIDE = Tile<T>::kSide, PITCH = Held<T, D>::kPitch, OWN = Tile<T>::kOwn;
   __shared__ __align__(16) char held[2 * 2 * KEYS * PITCH];      // [2][keys, values][KEYS][PITCH]
   const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), n = lane & (SIDE - 1), h = lane / SIDE;
-  if (first_block + blockIdx.x == 0 && threadIdx.x == 0) *no_row = f32x2{-__builtin_inff(), 0.0f};
+  if (first_block + blockIdx.x == 0 && threadIdx.x == 0) no_row[0] = f32x2{-__builtin_inff(), 0.0f}, no_row[1] = f32x2{0.0f, 0.0f};
   Work w;
   if (!find_work(a, first_block + blockIdx.x, &w)) return;
   const Limits all = limits_of_block(a, w), whole = limits_of_all(a, w);
@@ -369,8 +416,10 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
   load_fragments<T, D, VEC>(q, a.q.base + w.sequence * a.q.batch + token * a.q.token + head * a.q.head, a.q.channel, place.in && !a.nothing ? a.channels : 0, h, a.negative);
   load_fragments<T, D, VEC>(g, a.gout.base + w.sequence * a.gout.batch + token * a.gout.token + head * a.gout.head, a.gout.channel, place.in ? a.channels : 0, h, false);
   // What the passes need of a row: minus its log_sum in powers of two (plus kWeightTop), and minus gout * out.  (A row that sees nothing has weights of zero.)
-  f32x2 *const stat_at = stats + (w.sequence * (a.q_starts.p ? 0 : a.q_starts.all) + token) * ((int64_t)a.kv * a.per_kv) + head;
+  const int64_t stat_at = kRowPairs * ((w.sequence * (a.q_starts.p ? 0 : a.q_starts.all) + token) * ((int64_t)a.kv * a.per_kv) + head);
+  const int hi_last = __builtin_amdgcn_readlane(own.hi, SIDE - 1), lo_first = __builtin_amdgcn_readfirstlane(own.lo);
   f32x2 stat;
+  float reference = 0.0f;
   {
     frag_t<T> o[D / 16];
     load_fragments<T, D, VEC>(o, a.out.base + w.sequence * a.out.batch + token * a.out.token + head * a.out.head, a.out.channel, a.channels, h, false);
@@ -380,12 +429,24 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
     for (int c = 0; c < D / 16; ++c)
 #pragma unroll
       for (int i = 0; i < Tile<T>::kFrag; ++i) sum = __builtin_fmaf((float)g[c][i], (float)o[c][i], sum);
-    stat = f32x2{log_sum > -__builtin_inff() || log_sum != log_sum ? kWeightTop<T> - log_sum * 1.44269504088896340736f : -__builtin_inff(), -column_sum<T>(sum)};
-    if (!few && place.in && lane < SIDE) *stat_at = stat;
+    const float powers = log_sum * 1.44269504088896340736f;
+    stat = f32x2{log_sum > -__builtin_inff() || log_sum != log_sum ? kWeightTop<T> - powers : -__builtin_inff(), -column_sum<T>(sum)};
+    // (minus infinity, too, where a score past single precision's range may be what it stands for)
+    const bool past = __builtin_fabsf(powers) > kFar && own.hi > own.lo;
+    if (__any(past)) {
+      float largest, total;
+      far_sums<T, D, VEC>(a, q, pk, w.k.count, own.lo, own.hi, lo_first, hi_last, lane, &largest, &total);
+      if (past && largest > -__builtin_inff()) stat.x = kWeightTop<T> - __builtin_amdgcn_logf(total), reference = largest;
+    }
   }
+  const bool far = __any(reference != 0.0f);
+  const auto leave = [&] {
+    if (!place.in || lane >= SIDE) return;
+    stats[stat_at] = stat, stats[stat_at + 1] = f32x2{reference, 0.0f};
+  };
+  if (!few) leave();
   arrived();      // (the sums above have waited for loads behind these; LDS may be another workgroup's once this one has ended)
   if (!few && !a.gq.base) return;
-  const int hi_last = __builtin_amdgcn_readlane(own.hi, SIDE - 1), lo_first = __builtin_amdgcn_readfirstlane(own.lo);
   if (at < all.hi) store(0);
   const LanePlaces places = lane_places<T, D>(lane);
   Range<T> range;
@@ -403,6 +464,9 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
           p = product(o.x, q[c], p);
           s = product(o.y, g[c], s);
         });
+    if (D > 128 || far)
+#pragma unroll
+      for (int i = 0; i < OWN; ++i) p[i] -= reference;
     const int lo = own.lo - first - 4 * h, hi = own.hi - first - 4 * h;
     const float shift = (float)range.exponent(), less = stat.x + shift, most = kWeightTop<T> + shift;
 #pragma unroll
@@ -430,11 +494,10 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
       if (more) store(turn ^ 1);
     }
     stat.y = -column_sum<T>(sum) * (kWeightTop<T> > 0.0f ? 0x1p-12f : 1.0f);
-    if (place.in && lane < SIDE) *stat_at = stat;
+    leave();
     arrived();
-    if (!a.gq.base) return;
     __syncthreads();
-    at = all.lo / KEYS * KEYS, turn = 0;
+    at = a.gq.base ? all.lo / KEYS * KEYS : all.hi, turn = 0;      // (no tile where nothing is left to do)
     if (at + KEYS < all.hi) {      // (a single tile is there already)
       load(at, 0);
       store(0);
@@ -446,7 +509,7 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
   acc_t<T> start;      // of s
 #pragma unroll
   for (int i = 0; i < OWN; ++i) start[i] = stat.y;
-  const auto step = [&](auto masked, auto turn) {
+  const auto step = [&](auto masked, auto turn) __attribute__((always_inline)) {
     arrived();
     __syncthreads();
     const char *const keys = held + turn * 2 * KEYS * PITCH, *const values = keys + KEYS * PITCH;
@@ -483,7 +546,7 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
     }
   }
   arrived();
-  if (!place.in) return;
+  if (!place.in || !a.gq.base) return;
   const float weight = kWeightTop<T> > 0.0f ? 0x1p-12f : 1.0f;
   store_columns<T, D, VEC>(gq, a.gq.base + w.sequence * a.gq.batch + token * a.gq.token + head * a.gq.head, a.gq.channel, h, a.channels, a.true_scale * weight * range.back());
 }
@@ -520,12 +583,12 @@ template <class T, int D, bool VEC> int run_grad(AttentionArgs &a, const Attenti
   if (!set_blocks(a, sizes, side * kGradWaves, 1) || !set_key_blocks(of_keys, sizes, side * plan.waves, plan.splits)) return OCN_ERR_SHAPE;
   const int64_t units = units_of(sizes, side * kGradWaves), key_units = p.keys ? plan.units : 0;
   if (ordered(sizes, key_units * plan.splits, slots_of_key_units(sizes, side * plan.waves))) {
-    of_keys.order = (uint32_t *)(stats + rows + 1);
+    of_keys.order = (uint32_t *)(stats + kRowPairs * ((int64_t)rows + 1));
     hipLaunchKernelGGL(attention_order_kernel, dim3(1), dim3(kOrderLanes), 0, stream, of_keys);
     if ((rc = done(hipGetLastError())) != OCN_OK) return rc;
   }
   rc = in_launches(units, [&](uint32_t grid, uint32_t first) {
-    hipLaunchKernelGGL((attention_queries_kernel<T, D, VEC, kGradWaves, kGradKeys<T, VEC>>), dim3(grid), dim3(kGradWaves * kWave), 0, stream, a, first, stats, stats + rows);
+    hipLaunchKernelGGL((attention_queries_kernel<T, D, VEC, kGradWaves, kGradKeys<T, VEC>>), dim3(grid), dim3(kGradWaves * kWave), 0, stream, a, first, stats, stats + kRowPairs * (int64_t)rows);
   });
   if (rc != OCN_OK) return rc;
   // (rows of a tile: whole queries with the heads of the group, or some of those)
@@ -535,8 +598,8 @@ template <class T, int D, bool VEC> int run_grad(AttentionArgs &a, const Attenti
   of_keys.parts = (float *)((char *)stats + grad_head_bytes(sizes, side, plan.waves));
   rc = in_launches(key_units * plan.splits, [&](uint32_t grid, uint32_t first) {
     constexpr int wide = kWideKeys<T, D> ? 8 : 4;
-    if (plan.waves == wide) hipLaunchKernelGGL((attention_keys_kernel<T, D, VEC, wide>), dim3(grid), dim3(wide * kWave), 0, stream, of_keys, first, stats, stats + rows);
-    else hipLaunchKernelGGL((attention_keys_kernel<T, D, VEC, 4>), dim3(grid), dim3(4 * kWave), 0, stream, of_keys, first, stats, stats + rows);
+    if (plan.waves == wide) hipLaunchKernelGGL((attention_keys_kernel<T, D, VEC, wide>), dim3(grid), dim3(wide * kWave), 0, stream, of_keys, first, stats, stats + kRowPairs * (int64_t)rows);
+    else hipLaunchKernelGGL((attention_keys_kernel<T, D, VEC, 4>), dim3(grid), dim3(4 * kWave), 0, stream, of_keys, first, stats, stats + kRowPairs * (int64_t)rows);
   });
   if (rc != OCN_OK || plan.splits == 1) return rc;
   rc = in_launches(key_units * (side * plan.waves / kJoinRows), [&](uint32_t grid, uint32_t first) {

@@ -174,7 +174,7 @@ static bool set_all(AttentionArgs &a, const AttentionSizes &s, int64_t all, int6
 }
 
 size_t grad_head_bytes(const AttentionSizes &s, int side, int waves) {
-  const size_t n = (size_t)(s.queries * s.kv * s.per_kv + 1) * 2 * sizeof(float) +
+  const size_t n = (size_t)(s.queries * s.kv * s.per_kv + 1) * 4 * sizeof(float) +
                    (size_t)slots_of_key_units(s, side * waves) * sizeof(uint32_t);
   return (n + 255) / 256 * 256;
 }
@@ -291,7 +291,7 @@ int ocn_attention(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *v,
   }
 }
 
-// two numbers of each row, and of a row that is none; the order of blocks of keys; what parts of blocks of keys come to
+// four numbers of each row, and of a row that is none; the order of blocks of keys; what parts of blocks of keys come to
 static size_t grad_bytes(const AttentionSizes &s, int32_t dtype, int64_t channels) {
   const int side = dtype == OCN_FLOAT ? 16 : 32;
   const KeyPlan k = key_plan_of(s, dtype, channels);

@@ -191,7 +191,7 @@ template <class T, int D> constexpr int kWavesAtOnce = sizeof(T) == 2 && D <= 12
 // ---- from memory to LDS ------------------------------------------------------------------------
 //
 // Whole rows go there without passing through registers: a wavefront's load writes 64 pieces one behind the other, so that a lane loads the piece that
-// belongs at its place.  The compiler does not see these loads (it would wait for all of them before any read of LDS): arrived() has to be between them and the reads.  (Their place in LDS is in m0, which a scalar move writes: one wait.)
+// belongs at its place.  The compiler does not see these loads (it would wait for all of them before any read of LDS): arrived() has to be between them and the reads.  (Their place in LDS is in m0, which scalar instructions write: one wait.)
 __device__ __forceinline__ void load_to_lds(uint32_t lds, const char *from) {
   asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"{m0}"(lds), "v"(from) : "memory");
 }

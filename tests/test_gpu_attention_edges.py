@@ -1,7 +1,11 @@
 """Attention over whole sequences and its gradient where blocks, scores or values are out of the ordinary, against the forms and bounds of attention_ref."""
-import pytest
+import math
 
-from heads_ref import KIND
+import pytest
+import torch
+
+from attention_ref import seen
+from heads_ref import F32, KIND, half_step
 from test_gpu_attention import both, check, close, made, reference
 
 pytestmark = pytest.mark.gpu
@@ -34,3 +38,100 @@ def test_scales_below_single_precision(scale):
             if n in ("gq", "gk"):
                 bound = bound + 2.0 ** -150 * (1 + (value / scale).abs())
             close(n, got[n], (value, bound), None if n == "log_sum" else kind)
+
+
+def gradient_of(p, q, k, v, w, out, scale, kind):
+    """Gradients in 64 bits for weights p [heads, queries, keys] of one sequence, and how far the framework's may be from them where each weight that is not zero is right
+    to 32 half steps of single precision: D is taken from out as it was rounded, at worst"""
+    u, t = F32, (0.0 if kind == "float" else half_step(kind))
+    tiny = 2.0 ** -36 if kind == "half" else 0.0
+    group = q.shape[1] // k.shape[1]
+    q, w, out = (x.double().transpose(0, 1) for x in (q, w, out))
+    k, v = (x.double().transpose(0, 1).repeat_interleave(group, 0) for x in (k, v))
+    d, rows = q.shape[2], q.shape[0] // (k.shape[0] // group) * q.shape[1]
+    dp, size = w @ v.transpose(1, 2), w.abs() @ v.abs().transpose(1, 2)
+    along = (p * dp).sum(2, keepdim=True)
+    c = p * (dp - along)
+    along_off = 2 * (t + F32) * (w.abs() * out.abs()).sum(2, keepdim=True) + (p.shape[2] + d + 64) * u * (p * size).sum(2, keepdim=True)
+    c_off = 1.01 * (p * ((d + 2) * u * size + along_off) + (t + 64 * u) * c.abs())
+    c_off = c_off + tiny * c_off.amax() + tiny * c.abs().amax()
+    gq, gk, gv = scale * (c @ k), scale * (c.transpose(1, 2) @ q), p.transpose(1, 2) @ w
+    gq_off = abs(scale) * (c_off @ k.abs() + (p.shape[2] + 4) * u * (c.abs() @ k.abs()))
+    gk_off = abs(scale) * (c_off.transpose(1, 2) @ q.abs() + (rows + 4) * u * (c.abs().transpose(1, 2) @ q.abs()))
+    gv_off = (p * (t + 32 * u) + tiny).transpose(1, 2) @ w.abs() + (rows + 4) * u * (p.transpose(1, 2) @ w.abs())
+    of_head = lambda x: x.view(-1, group, *x.shape[1:]).sum(1).transpose(0, 1)
+    return {"gq": (gq.transpose(0, 1), gq_off.transpose(0, 1)), "gk": (of_head(gk), of_head(gk_off)), "gv": (of_head(gv), of_head(gv_off))}
+
+
+def largest_alone(s):
+    """Weights of scores of which the largest ones are the same, and others so far below that they weigh nothing"""
+    best = s == s.amax(2, keepdim=True)
+    rest = torch.where(best, -math.inf, s).amax(2)
+    assert ((s.amax(2) - rest) > 110).all()
+    return best.double() / best.sum(2, keepdim=True)
+
+
+@pytest.mark.parametrize("kind,size,scale", [("half", 200.0, 10.0), ("half", 60000.0, 0.1), ("bfloat16", 1e9, 1.0), ("bfloat16", 1e15, -1.0), ("float", 3000.0, 1.0), ("float", 1e12, -1.0),
+                                             ("bfloat16", 1e-20, 1e32), ("float", 1e30, 1e20), ("bfloat16", 1e30, -1e20)])
+@pytest.mark.parametrize("queries,keys", [(1, 200), (50, 200), (300, 900), (700, 90)])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_gradients_of_scores_of_any_size(kind, size, scale, queries, keys, sign):
+    """One channel of queries that is not zero, so that scores are exact, and keys that differ by a tenth there: the largest have all the weight, however large scores are, or how far below zero"""
+    d, g = 64, torch.Generator().manual_seed(32)
+    q, k, v, w = torch.zeros(queries, 2, d), torch.randn(keys, 1, d, generator=g), torch.randn(keys, 1, d, generator=g), torch.randn(queries, 2, d, generator=g)
+    q[..., 0] = size
+    k[:, 0, 0] = torch.linspace(0.125, 1.625, 16)[torch.randint(0, 16, (keys,), generator=g)] * sign
+    data = tuple(t.to(KIND[kind]) for t in (q, k, v, w))
+    got = both(([queries], [keys], 2, 1, d, False, 0), kind, data, scale)
+    q, k, v, w = data
+    p = largest_alone((q.double()[..., 0].t()[..., None] * k.double()[:, 0, 0]) * scale)
+    want = gradient_of(p, q, k, v, w, got["out"].cpu(), scale, kind)
+    out = (p @ v.double()[:, 0]).transpose(0, 1)
+    close("out", got["out"], (out, (half_step(kind) + (keys + 64) * F32) * (p @ v.double()[:, 0].abs()).transpose(0, 1)), kind)
+    most = torch.finfo(KIND[kind]).max / 2
+    for n, (value, off) in want.items():
+        fits = (value.abs() + off < most) & (value.abs() + off < 1e38)
+        assert n == "gk" or fits.all()
+        close(n, torch.where(fits.cuda(), got[n], 0), tuple(torch.where(fits, x, 0.0) for x in (value, off)), kind)
+
+
+@pytest.mark.parametrize("kind", list(KIND))
+@pytest.mark.parametrize("n,heads,kv,d,window", [(40, 2, 2, 64, 0), (300, 4, 2, 128, 0), (700, 4, 1, 128, 0), (500, 2, 1, 80, 150), (90, 3, 1, 192, 0), (350, 2, 2, 256, 0), (400, 2, 1, 100, 0)])
+def test_gradients_of_far_scores(kind, n, heads, kv, d, window):
+    """Scores of all channels up to 1e11: a row's largest key has all of its weight, which is one in both passes where they make the same score of it"""
+    scale, shape = 1e9, ([n], None, heads, kv, d, True, window)
+    q, k, v, w = data = made(shape, kind, 33)
+    s = (q.double().transpose(0, 1) @ k.double().transpose(0, 1).repeat_interleave(heads // kv, 0).transpose(1, 2) * scale).masked_fill(~seen(n, n, True, window), -math.inf)
+    size = q.double().abs().transpose(0, 1) @ k.double().abs().transpose(0, 1).repeat_interleave(heads // kv, 0).transpose(1, 2) * scale
+    gaps = s.topk(2, 2).values.diff(dim=2).neg()
+    clear = (gaps[..., 0] > 4 * (d + 2) * F32 * size.amax(2)) | (torch.arange(n) == 0)
+    data = (q, k, v, w) = (q, k, v, w * clear.t()[..., None].to(w.dtype))          # (rows whose largest two are too near to each other for single precision have no part in it)
+    assert clear.double().mean() > 0.9
+    got = both(shape, kind, data, scale)
+    want = gradient_of(largest_alone(torch.where(clear[..., None], s, torch.where(torch.arange(n) == 0, 0.0, -math.inf))), q, k, v, w, got["out"].cpu(), scale, kind)
+    for name, (value, off) in want.items():
+        fits = value.abs() + off < torch.finfo(KIND[kind]).max / 2
+        if name == "gq":
+            fits = fits & clear.t()[..., None]
+        close(name, torch.where(fits.cuda(), got[name], 0), tuple(torch.where(fits, x, 0.0) for x in (value, off)), kind)
+        assert name != "gv" or fits.all()
+
+
+@pytest.mark.parametrize("kind", list(KIND))
+@pytest.mark.parametrize("d", [64, 128, 192])
+def test_a_single_key(kind, d):
+    """A window of one: the gradient of a value is that of its query's result, at any scale.  (In single precision the exponent of a weight is off by four half steps of 128 at most.)"""
+    shape = ([300, 7], None, 2, 2, d, True, 1)
+    data = made(shape, kind, 34)
+    for scale in (0.1, 1e3, -1e6, 1e9, 1e20):
+        got = both(shape, kind, data, scale)
+        assert torch.equal(got["out"].cpu(), data[2])
+        assert ((got["gv"].cpu().double() - data[3].double()).abs() <= (360 * F32 if kind == "float" else 0.0) * data[3].double().abs()).all(), scale
+
+
+@pytest.mark.parametrize("kind", list(KIND))
+def test_one_row_of_far_scores(kind):
+    for shape in (([90], None, 2, 1, 64, True, 0), ([700], None, 4, 2, 128, True, 0)):
+        q, k, v, w = made(shape, kind, 35)
+        q[60, 1] *= 300
+        check(shape, kind, (q, k, v, w), both(shape, kind, (q, k, v, w)))

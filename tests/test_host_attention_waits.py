@@ -107,7 +107,7 @@ def test_copies_have_arrived_before_the_end(which, tmp_path):
     found = {name: lines for name, lines in found.items() if f"attention_{which}" in name}
     assert len(found) == len(kernels)
     for lines in found.values():       # (a copy may follow a scalar instruction's result after one wait, a vector instruction's only after five)
-        assert all(line.startswith("s_mov") for line in lines if re.match(r"\w+ m0\b", line))
+        assert all(line.startswith("s_") for line in lines if re.match(r"\w+ m0\b", line))
     found = {name: on_their_way(lines) for name, lines in found.items()}
     for name, (ends, copies) in found.items():
         assert copies > 0 and not ends, (name, copies, ends)
