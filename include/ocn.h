@@ -454,8 +454,8 @@ int ocn_attention(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *v,
  * log_sum is within 88 of zero (and is off by less than 3e-5 of itself), past that from the row's largest score, found again, and the sum relative to it.  For half and bfloat16 p_ij and s_ij are
  * rounded to that type for these products, half a step at most (in half by up to 2^-37 and, of the largest s_ij of the query or key, by 2^-36: those are held in a range of
  * their own, down to 2^-60).  D_i is taken from out as it is, with its rounding, or, where rows see few keys and that would show, from the weights.
- * q_gin may be NULL, and k_gin and v_gin both; no output may share bytes with an input.  An infinity or a NaN in a sequence may reach all of that sequence's gradients, and those of
- * no other.  workspace: DEVICE scratch of ocn_attention_grad_workspace_bytes(...) bytes, 256-byte aligned.  The same bits every time. */
+ * q_gin may be NULL, and k_gin and v_gin both; no output may share bytes with an input.  Where the formulas give NaN for what a sequence holds (a query
+ * whose log_sum is NaN, say) these do too, and an infinity or a NaN in a sequence may reach all of that sequence's gradients, but those of no other.  workspace: DEVICE scratch of ocn_attention_grad_workspace_bytes(...) bytes, 256-byte aligned.  The same bits every time. */
 size_t ocn_attention_grad_workspace_bytes(const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *q_starts);
 int ocn_attention_grad(const ocn_tensor *gout, const ocn_tensor *q, const ocn_tensor *k, const ocn_tensor *v, const ocn_tensor *out, const ocn_tensor *log_sum,
                        const ocn_tensor *q_starts, const ocn_tensor *k_starts, double scale, int64_t window, uint32_t flags, const ocn_tensor *q_gin,

@@ -41,11 +41,8 @@ template <class T> struct Range {
   __device__ __forceinline__ float back() const { return kNeeded ? 1.0f / factor : 1.0f; }
 };
 
-// A weight from its exponent: above its row's sum (2^most) by rounding alone, but of scores of any size.  (Up to 1 the instruction itself holds it to that.)
-template <class T> __device__ __forceinline__ float weight(float x, float most = kWeightTop<T>) {
-  if constexpr (kWeightTop<T> > 0.0f) return __builtin_amdgcn_exp2f(fminf(x, most));
-  return __builtin_amdgcn_fmed3f(__builtin_amdgcn_exp2f(x), 0.0f, 1.0f);
-}
+// A weight from its exponent: a row's sum (2^kWeightTop) at most, and what that is off by.  (NaNs stay what they are, and where a query does not see the key it is set to zero behind this.)
+__device__ __forceinline__ float weight(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // what to multiply a column's s and sums with, where some do not fit: s is times the factor
 template <class T> __device__ __forceinline__ void in_range(acc_t<T> &s, Range<T> &range, acc_t<T> *out, int outs) {
@@ -102,7 +99,8 @@ template <class T> __device__ __forceinline__ acc_t<T> no_sum() {
 // A weight is 2^(score scale - log2 of the row's sum), and log_sum as it is given, rounded at its own size, is off by as much as a score of that size.  The four half steps of single precision that the exponent
 // is off by change a weight by less than 3 10^-5 of itself up to kFar.  Past that a row has a reference, its largest score, as forward has one, and the sum of its weights relative to it: the
 // pass over rows finds both, from its own scores, before anything else.  A weight is 2^((score - reference) scale - log2 of that sum), with the difference formed first.  Both passes make the same
-// bits of a score: products of the same channels in the same order.
+// bits of a score: products of the same channels in the same order.  (4 sequences of 4096 tokens, 32 heads, 8 of keys, 128 channels in bfloat16: 2.64 ms instead of 1.91 where all rows are far; with a
+// reference for every row 0.6 % more where none is.)
 constexpr float kFar = 128.0f;
 
 // What the passes need of a row, in the workspace, and of a row that is none, which has weights of zero: the exponent's part, minus gout * out, the reference (0: not far).  The order of blocks of
@@ -274,7 +272,7 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
         for (int i = 0; i < OWN; ++i) p[i] -= of_row[turn][2][own_index<T>(i) + 4 * here];
 #pragma unroll
       for (int i = 0; i < OWN; ++i) {
-        p[i] = weight<T>(__builtin_fmaf(p[i], a.scale, of_row[turn][0][own_index<T>(i) + 4 * h]));
+        p[i] = weight(__builtin_fmaf(p[i], a.scale, of_row[turn][0][own_index<T>(i) + 4 * h]));
         if constexpr (masked) {
           const int e = first_end + (int)fast_quotient((uint32_t)(own_index<T>(i) + 4 * here), a.heads_div);
           if (key >= e || (a.window && key < e - a.window)) p[i] = 0.0f;
@@ -468,10 +466,10 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
 #pragma unroll
       for (int i = 0; i < OWN; ++i) p[i] -= reference;
     const int lo = own.lo - first - 4 * h, hi = own.hi - first - 4 * h;
-    const float shift = (float)range.exponent(), less = stat.x + shift, most = kWeightTop<T> + shift;
+    const float less = stat.x + (float)range.exponent();
 #pragma unroll
     for (int i = 0; i < OWN; ++i) {
-      p[i] = weight<T>(__builtin_fmaf(p[i], a.scale, less), most);
+      p[i] = weight(__builtin_fmaf(p[i], a.scale, less));
       if (masked && (own_index<T>(i) < lo || own_index<T>(i) >= hi)) p[i] = 0.0f;
     }
   };
@@ -489,7 +487,7 @@ __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(kW
         acc_t<T> p, s = no_sum<T>();
         weights(k + t * PITCH, v + t * PITCH, at + t, p, s, std::true_type());
 #pragma unroll
-        for (int i = 0; i < OWN; ++i) sum = __builtin_fmaf(p[i], p[i] > 0.0f ? s[i] : 0.0f, sum);
+        for (int i = 0; i < OWN; ++i) sum = __builtin_fmaf(p[i], p[i] == 0.0f ? 0.0f : s[i], sum);
       }
       if (more) store(turn ^ 1);
     }

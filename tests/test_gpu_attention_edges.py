@@ -135,3 +135,62 @@ def test_one_row_of_far_scores(kind):
         q, k, v, w = made(shape, kind, 35)
         q[60, 1] *= 300
         check(shape, kind, (q, k, v, w), both(shape, kind, (q, k, v, w)))
+
+
+def reached(shape, rows=None, keys=None):
+    """[queries, keys] of the last sequence: whether a query that is among the rows, or sees one of the keys, sees the key"""
+    n = shape[0][-1]
+    see = seen(n, n, True, shape[6])
+    hit = torch.zeros(n, dtype=torch.bool)
+    if rows is not None:
+        hit[rows] = True
+    if keys is not None:
+        hit |= see[:, keys].any(1)
+    return hit, (see & hit[:, None]).any(0)
+
+
+@pytest.mark.parametrize("kind", list(KIND))
+@pytest.mark.parametrize("d", [64, 80, 128, 256])
+@pytest.mark.parametrize("n", [100, 900])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_what_is_no_number_in_one_operand(kind, d, n, bad):
+    """A NaN or an infinity in one operand alone of one sequence: gradients are NaN wherever the definition's are, and those of other sequences are as they were"""
+    shape = ([70, n], None, 4, 2, d, True, 0)
+    data = made(shape, kind, 36)
+    plain = both(shape, kind, data)
+    row, first = n // 2, 70
+    for which in range(4):
+        tensors = [t.clone() for t in data]
+        tensors[which][first + row, 1, 3] = bad
+        got = {name: t.cpu() for name, t in both(shape, kind, tensors).items()}
+        assert all(torch.equal(got[name][:first], plain[name].cpu()[:first]) for name in got)
+        # head 1 of the queries reads head 0 of the keys; head 1 of the keys is read by the heads 2 and 3
+        of_query = which in (0, 3)
+        hit, held = reached(shape, rows=[row]) if of_query else reached(shape, keys=[row])
+        heads, kv = ([1], 0) if of_query else ([2, 3], 1)
+        gk, gv = got["gk"][first:, kv][held], got["gv"][first:, kv][held]
+        for h in heads:
+            gq = got["gq"][first:, h][hit]
+            # (an infinity of a key makes scores of minus infinity too, weights of zero, and NaNs of those times itself)
+            assert (gq if which != 1 or bad != bad else gq[:, 3]).isnan().all(), (which, "gq")
+        if bad != bad:
+            assert gk.isnan().all() and (which not in (0, 1) or gv.isnan().all()) and (which != 3 or gv[:, 3].isnan().all()), which
+        elif which >= 2:
+            assert not gk.isfinite().any() and (which != 3 or not gv[:, 3].isfinite().any()), which
+
+
+@pytest.mark.parametrize("kind", ["bfloat16", "float"])
+@pytest.mark.parametrize("n", [100, 900])
+def test_scores_that_are_no_numbers(kind, n):
+    """Finite queries and keys whose products pass single precision: results that are NaN have gradients that are"""
+    shape = ([70, n], None, 2, 1, 64, True, 0)
+    q, k, v, w = made(shape, kind, 37)
+    q[70 + n // 2, 0] = 1e30
+    k[70 + n // 4, 0] = 1e30
+    got = {name: t.cpu() for name, t in both(shape, kind, (q, k, v, w)).items()}
+    odd = got["out"].isnan().any(2)
+    assert odd[70 + n // 2, 0] and odd.sum() == 1
+    assert got["gq"][70 + n // 2, 0].isnan().all()
+    for name in ("gk", "gv"):
+        assert got[name][70:70 + n // 2 + 1].isnan().all()
+        assert got[name][:70].isfinite().all()
