@@ -40,13 +40,22 @@ template <class T> __device__ __forceinline__ acc_t<T> zero_acc() {
   return a;
 }
 
-// Whether there is anything but numbers among KEYS keys' values in LDS.  Weights of zero would make NaNs of those in the products.
+// ---- values that are no numbers -------------------------------------------------------------------
+//
+// Weights of zero would make NaNs of infinities and NaNs in the products, so that they would reach rows that do not see them.  In tiles that some row does not see whole they are looked for; where there
+// are any, it is found which keys have one in a channel, lanes note which of their row's results they reach, in two bits of a result that are kept in LDS (infinity, minus infinity; both: NaN), and the
+// tile's values become zeros.  Results take from the bits what they are in the end.  (4096 tokens, 8 heads, all values NaN, call included: 135 us, with numbers 128; with rows by themselves, key by key, 75 ms.)
+
+// Whether there are any among KEYS keys' values in LDS
 template <class T, int D, int KEYS> __device__ __forceinline__ bool odd_values(const char *v, int lane) {
   constexpr uint32_t exponent = std::is_same<T, float>::value ? 0x7f800000u : std::is_same<T, f16>::value ? 0x7c007c00u : 0x7f807f80u;
   constexpr uint32_t one = std::is_same<T, float>::value ? 0x00800000u : std::is_same<T, f16>::value ? 0x04000400u : 0x00800080u;
   uint32_t odd = 0;
-#pragma nounroll
-  for (int i = lane; i < KEYS * Held<T, D>::kPieces; i += kWave) {
+  asm volatile("" : "+v"(lane));      // (what hangs on it is not kept in registers from tile to tile)
+  static_assert(KEYS * Held<T, D>::kPieces % kWave == 0, "all lanes have as many pieces");
+#pragma unroll 4
+  for (int n = 0; n < KEYS * Held<T, D>::kPieces / kWave; ++n) {
+    const int i = n * kWave + lane;
     const u32x4 x = *(const u32x4 *)(v + Held<T, D>::at(i / Held<T, D>::kPieces, i % Held<T, D>::kPieces));
 #pragma unroll
     for (int e = 0; e < 4; ++e) odd |= (x[e] & exponent) + one;      // (into the sign's place where all bits of an exponent are set)
@@ -54,43 +63,84 @@ template <class T, int D, int KEYS> __device__ __forceinline__ bool odd_values(c
   return __any((odd & (sizeof(T) == 2 ? 0x80008000u : 0x80000000u)) != 0);
 }
 
-// A row by itself, key by key: what a tile's row that does not see such a value gets instead.  Lanes have channels.
-template <class T, int D> struct SlowRow {
-  static constexpr int kEach = (D + kWave - 1) / kWave;
-  float best, total, x[kEach];
-  __device__ __forceinline__ void run(const AttentionArgs &a, const char *q, const char *k, const char *v, int lo, int hi, int lane) {
-    float mine[kEach];
-    best = -__builtin_inff(), total = 0.0f;
-#pragma unroll
-    for (int c = 0; c < kEach; ++c) {
-      const int e = c * kWave + lane;
-      x[c] = 0.0f;
-      mine[c] = e < a.channels && !a.nothing ? (float)*(const T *)(q + e * a.q.channel) * (a.negative ? -1.0f : 1.0f) : 0.0f;
-    }
+__device__ __forceinline__ bool is_odd(float x) { return !(__builtin_fabsf(x) < __builtin_inff()); }
+// the bits of a lane's results: a word for each tile of channels
+template <class T, int D, int WAVES> struct Bits { uint32_t words[kTilesOf<Tile<T>, D>][WAVES * kWave]; };
+
+// ... and which of a tile's keys have one in a channel: infinities and NaNs, infinities below zero and NaNs
+template <class T, int D, int KEYS> struct OddKeys { uint32_t of[kWidth<T, D>][2][(KEYS + 31) / 32]; };
+
+// From KEYS keys' values in LDS, by LANES lanes
+template <class T, int D, int KEYS, int LANES> __device__ __forceinline__ void find_odd_keys(OddKeys<T, D, KEYS> &keys, const char *v, int lane) {
+  constexpr int EACH = KEYS < 32 ? KEYS : 32;
+  asm volatile("" : "+v"(lane));      // (what hangs on it is not kept in registers from tile to tile)
 #pragma nounroll
-    for (int j = lo; j < hi; ++j) {
-      float s = 0.0f;
-#pragma unroll
-      for (int c = 0; c < kEach; ++c) {
-        const int e = c * kWave + lane;
-        if (e < a.channels) s = __builtin_fmaf(mine[c], (float)*(const T *)(k + (int64_t)j * a.k.token + e * a.k.channel), s);
+  for (int c = lane; c < D; c += LANES)
+#pragma nounroll
+    for (int w = 0; w < KEYS / EACH; ++w) {
+      uint32_t up = 0, down = 0;
+#pragma unroll 4
+      for (int i = 0; i < EACH; ++i) {
+        const float x = (float)*(const T *)(v + Held<T, D>::at(w * EACH + i, c * (int)sizeof(T) / 16) + c * (int)sizeof(T) % 16);
+        const uint32_t one = is_odd(x) ? 1u << i : 0u;
+        up |= x < 0.0f ? 0u : one, down |= x > 0.0f ? 0u : one;
       }
-      s = sum_over_row(s, kWave);
-      float keep = 1.0f;
-      if ((s - best) * a.scale > 4.0f) {
-        keep = best > -__builtin_inff() ? __builtin_amdgcn_exp2f((best - s) * a.scale) : 0.0f;
-        best = s;
-      }
-      const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s - (best > -__builtin_inff() ? best : 0.0f), a.scale, kTop<T>));
-      total = __builtin_fmaf(total, keep, p);
-#pragma unroll
-      for (int c = 0; c < kEach; ++c) {
-        const int e = c * kWave + lane;
-        if (e < a.channels) x[c] = __builtin_fmaf(x[c], keep, p * (float)*(const T *)(v + (int64_t)j * a.v.token + e * a.v.channel));
-      }
+      keys.of[c][0][w] = up, keys.of[c][1][w] = down;
     }
+}
+// What of them reaches a lane's results, which see the keys lo ... hi - 1: into its bits, which are none so far where `any` is not set
+template <class T, int D, int KEYS, int WAVES> __device__ __forceinline__ void note_odd_keys(Bits<T, D, WAVES> &bits, bool *any, const OddKeys<T, D, KEYS> &keys, int lo, int hi, int lane) {
+  constexpr int WORDS = (KEYS + 31) / 32;
+  int thread = threadIdx.x;
+  asm volatile("" : "+v"(lane), "+v"(thread));
+  uint32_t sees[WORDS];
+#pragma unroll
+  for (int w = 0; w < WORDS; ++w) {
+    const auto below = [&](int n) { return n <= w * 32 ? 0u : n >= w * 32 + 32 ? ~0u : (1u << (n - w * 32)) - 1u; };      // keys before n
+    sees[w] = below(hi) & ~below(lo);
   }
-};
+#pragma nounroll
+  for (int ct = 0; ct < kTilesOf<Tile<T>, D>; ++ct) {
+    uint32_t own = *any ? bits.words[ct][thread] : 0u;
+#pragma unroll 2
+    for (int i = 0; i < Tile<T>::kOwn; ++i) {
+      const int c = ct * Tile<T>::kSide + own_index<T>(i) + 4 * (lane / Tile<T>::kSide);
+      uint32_t up = 0, down = 0;
+#pragma unroll
+      for (int w = 0; w < WORDS; ++w) up |= keys.of[c][0][w] & sees[w], down |= keys.of[c][1][w] & sees[w];
+      own |= ((up ? 1u : 0u) | (down ? 2u : 0u)) << 2 * i;
+    }
+    bits.words[ct][thread] = own;
+  }
+  *any = true;
+}
+// zeros in their places, by LANES lanes
+template <class T, int D, int KEYS, int LANES> __device__ __forceinline__ void clear_odd_values(char *v, int lane) {
+  asm volatile("" : "+v"(lane));
+#pragma nounroll
+  for (int i = lane; i < KEYS * Held<T, D>::kPieces; i += LANES) {
+    union { u32x4 v; T t[16 / sizeof(T)]; } x;
+    u32x4 *const at = (u32x4 *)(v + Held<T, D>::at(i / Held<T, D>::kPieces, i % Held<T, D>::kPieces));
+    x.v = *at;
+#pragma unroll
+    for (int e = 0; e < 16 / (int)sizeof(T); ++e)
+      if (is_odd((float)x.t[e])) x.t[e] = (T)0.0f;
+    *at = x.v;
+  }
+}
+// a lane's results in the end
+template <class T, int D, int WAVES> __device__ __forceinline__ void take_odd_values(const Bits<T, D, WAVES> &bits, acc_t<T> *out) {
+#pragma unroll
+  for (int ct = 0; ct < kTilesOf<Tile<T>, D>; ++ct) {
+    const uint32_t own = bits.words[ct][threadIdx.x];
+#pragma unroll
+    for (int i = 0; i < Tile<T>::kOwn; ++i) {
+      const uint32_t two = own >> 2 * i & 3u;
+      out[ct][i] += two == 3u ? __builtin_nanf("") : two == 2u ? -__builtin_inff() : two == 1u ? __builtin_inff() : 0.0f;
+    }
+    in_order();
+  }
+}
 
 // operands that are read ahead of their products (one, as the compiler has it: 1833 us of the prompts below instead of 1763)
 template <class T, int D> constexpr int kScoresAhead = 4;
@@ -121,8 +171,8 @@ template <class T, int TILES> __device__ __forceinline__ float weigh(const acc_t
   return sum;
 }
 
-// KEYS keys of a tile in LDS, from key `first` of the sequence on.  MASKED: some row does not see all of them; true: and values that it does not see may have reached it.
-template <class T, int D, int KEYS, bool MASKED> __device__ __forceinline__ bool attend(Rows<T, D> &r, const char *k, const char *v, int first, float scale, int lane) {
+// KEYS keys of a tile in LDS, from key `first` of the sequence on.  MASKED: some row does not see all of them.
+template <class T, int D, int KEYS, bool MASKED> __device__ __forceinline__ void attend(Rows<T, D> &r, const char *k, const char *v, int first, float scale, int lane) {
   constexpr int SIDE = Tile<T>::kSide, TILES = KEYS / SIDE, OWN = Tile<T>::kOwn, STEPS = Tile<T>::kSteps;
   const int h = lane / SIDE;
   const LanePlaces places = lane_places<T, D>(lane);
@@ -166,7 +216,6 @@ template <class T, int D, int KEYS, bool MASKED> __device__ __forceinline__ bool
   constexpr int OUTS = kTilesOf<Tile<T>, D>;
   pipelined<TILES * STEPS * OUTS, kValuesAhead<T, D>, frag_t<T>>([&](int i) { return columns_fragment<T, D>(v, 16 * (i / OUTS), i % OUTS, places); },
                                                                  [&](int i, frag_t<T> x) { r.out[i % OUTS] = product(x, f[i / OUTS], r.out[i % OUTS]); });
-  return MASKED && odd_values<T, D, KEYS>(v, lane);
 }
 
 // Keys [first, first + KEYS) of a sequence on their way into LDS, by `LANES` lanes; those past the end are zero.
@@ -237,15 +286,8 @@ template <class T, int D> __device__ __forceinline__ void finish_row(const Atten
   if (a.log_sum.base && lane == 0) *(float *)(a.log_sum.base + row_offset(a.log_sum, a, w, p)) = log_sum_of<T>(a, best, total);
 }
 
-// a row's place among the parts, and what a part leaves there of a row that lanes have channels of
+// a row's place among the parts
 __device__ __forceinline__ int64_t part_row(const AttentionArgs &a, const Work &w, int row) { return ((int64_t)w.unit * a.splits + w.split) * a.rows + row; }
-template <class T, int D> __device__ __forceinline__ void leave_row(const AttentionArgs &a, const Work &w, int row, const float *x, float best, float total, int lane) {
-  const int64_t part = part_row(a, w, row);
-#pragma unroll
-  for (int c = 0; c < SlowRow<T, D>::kEach; ++c)
-    if (c * kWave + lane < D) a.parts[part * kWidth<T, D> + c * kWave + lane] = x[c];
-  if (lane == 0) a.part_sums[2 * part] = best, a.part_sums[2 * part + 1] = total;
-}
 
 // The part of a block's keys, in tiles of so many, that a workgroup has
 struct Split { int first, end, parts; bool alone, mine; };
@@ -265,6 +307,8 @@ template <class T, int D, bool VEC, int WAVES, int KEYS> __global__ __launch_bou
   warm_arguments<AttentionArgs>();
   constexpr int SIDE = Tile<T>::kSide, PITCH = Held<T, D>::kPitch;
   __shared__ __align__(16) char lds[2 * 2 * KEYS * PITCH];        // [2][keys, values][KEYS][PITCH]
+  __shared__ Bits<T, D, WAVES> bits;
+  __shared__ OddKeys<T, D, KEYS> odd_keys;
   const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   Work w;
   if (!find_work(a, first_block + blockIdx.x, &w)) return;
@@ -301,10 +345,19 @@ template <class T, int D, bool VEC, int WAVES, int KEYS> __global__ __launch_bou
   const auto step = [&](auto masked, auto turn) {
     arrived();
     __syncthreads();
-    const char *const k = lds + turn * 2 * KEYS * PITCH, *const v = k + KEYS * PITCH;
+    char *const k = lds + turn * 2 * KEYS * PITCH, *const v = k + KEYS * PITCH;
     const bool more = at + KEYS < all.hi;
     if (more) load(at + KEYS, turn ^ 1);
-    if (!masked || (at < hi_last && at + KEYS > lo_first)) odd |= attend<T, D, KEYS, masked>(r, k, v, at, a.scale, lane);
+    if constexpr (masked) {
+      if (__builtin_expect(odd_values<T, D, KEYS>(v, lane), 0)) {      // (all wavefronts find the same)
+        find_odd_keys<T, D, KEYS, WAVES * kWave>(odd_keys, v, threadIdx.x);
+        __syncthreads();
+        clear_odd_values<T, D, KEYS, WAVES * kWave>(v, threadIdx.x);
+        note_odd_keys<T, D, KEYS, WAVES>(bits, &odd, odd_keys, r.lo - at, r.hi - at, lane);
+        __syncthreads();
+      }
+    }
+    if (!masked || (at < hi_last && at + KEYS > lo_first)) attend<T, D, KEYS, masked>(r, k, v, at, a.scale, lane);
     if (more) store(turn ^ 1);
     at += KEYS;
   };
@@ -320,19 +373,7 @@ template <class T, int D, bool VEC, int WAVES, int KEYS> __global__ __launch_bou
     }
   }
   arrived();
-  if (odd) {
-#pragma nounroll
-    for (int i = wave * SIDE; i < wave * SIDE + SIDE; ++i) {
-      const RowPlace p = row_place(a, w, i);
-      if (!p.in) continue;
-      const Limits l = limits_of(a, w, p.query);
-      SlowRow<T, D> slow;
-      slow.run(a, a.q.base + row_offset(a.q, a, w, p), pk, pv, l.lo > all.lo ? l.lo : all.lo, l.hi < all.hi ? l.hi : all.hi, lane);
-      if (split.alone) finish_row<T, D>(a, w, p, slow.x, slow.best, slow.total, lane);
-      else leave_row<T, D>(a, w, i, slow.x, slow.best, slow.total, lane);
-    }
-    return;
-  }
+  if (odd) take_odd_values<T, D, WAVES>(bits, r.out);
   const float total = column_sum<T>(r.total), over = total > 0.0f || total != total ? 1.0f / total : 0.0f;
   const RowPlace p = row_place(a, w, row);
   if (!p.in) return;
@@ -371,7 +412,8 @@ __global__ __launch_bounds__(kFewWaves *kWave) __attribute__((amdgpu_waves_per_e
   static_assert(SIDE * kWidth<T, D> * 4 <= PART, "a wavefront's results take the place of its keys and values");
   __shared__ __align__(16) char lds[kFewWaves * PART];        // [wavefronts][keys, values][SIDE][PITCH]
   __shared__ float bests[kFewWaves][SIDE], totals[kFewWaves][SIDE];
-  __shared__ bool odds[kFewWaves];
+  __shared__ Bits<T, D, kFewWaves> bits;
+  __shared__ OddKeys<T, D, SIDE> odd_keys[kFewWaves];
   const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), n = lane & (SIDE - 1);
   Work w;
   if (!find_work(a, first_block + blockIdx.x, &w)) return;
@@ -391,7 +433,16 @@ __global__ __launch_bounds__(kFewWaves *kWave) __attribute__((amdgpu_waves_per_e
     next.store(k, v, lane);
     if (at + kFewWaves * SIDE < split.end) next.load(a, pk, pv, at + kFewWaves * SIDE, w.k.count, lane);
     __builtin_amdgcn_wave_barrier();
-    odd |= attend<T, D, SIDE, masked>(r, k, v, at, a.scale, lane);
+    if constexpr (masked) {
+      if (__builtin_expect(odd_values<T, D, SIDE>(v, lane), 0)) {
+        find_odd_keys<T, D, SIDE, kWave>(odd_keys[wave], v, lane);
+        __builtin_amdgcn_wave_barrier();
+        clear_odd_values<T, D, SIDE, kWave>(v, lane);
+        note_odd_keys<T, D, SIDE, kFewWaves>(bits, &odd, odd_keys[wave], r.lo - at, r.hi - at, lane);
+        __builtin_amdgcn_wave_barrier();
+      }
+    }
+    attend<T, D, SIDE, masked>(r, k, v, at, a.scale, lane);
     __builtin_amdgcn_wave_barrier();
     at += kFewWaves * SIDE;
   };
@@ -399,28 +450,10 @@ __global__ __launch_bounds__(kFewWaves *kWave) __attribute__((amdgpu_waves_per_e
     while (at >= lo_last && at + SIDE <= hi_first && at < split.end) step(std::false_type());
     if (at < split.end) step(std::true_type());
   }
+  if (odd) take_odd_values<T, D, kFewWaves>(bits, r.out);
   const float total = column_sum<T>(r.total);
   if (lane < SIDE) bests[wave][n] = r.best, totals[wave][n] = total;
-  if (lane == 0) odds[wave] = odd;
   __syncthreads();
-#pragma unroll
-  for (int i = 0; i < kFewWaves; ++i) odd |= odds[i];
-  if (odd) {
-#pragma nounroll
-    for (int i = wave; i < SIDE; i += kFewWaves) {
-      const RowPlace p = row_place(a, w, i);
-      if (!p.in) continue;
-      const Limits l = limits_of(a, w, p.query);
-      SlowRow<T, D> slow;
-      slow.run(a, a.q.base + row_offset(a.q, a, w, p), pk, pv, l.lo > split.first ? l.lo : split.first, l.hi < split.end ? l.hi : split.end, lane);
-      if (split.alone) {
-        finish_row<T, D>(a, w, p, slow.x, slow.best, slow.total, lane);
-      } else {
-        leave_row<T, D>(a, w, i, slow.x, slow.best, slow.total, lane);
-      }
-    }
-    return;
-  }
   float best = bests[0][n];
 #pragma unroll
   for (int i = 1; i < kFewWaves; ++i) best = fmaxf(best, bests[i][n]);

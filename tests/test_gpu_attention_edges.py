@@ -4,9 +4,10 @@ import math
 import pytest
 import torch
 
+import paper_1810_08723_amd as ocn
 from attention_ref import seen
-from heads_ref import F32, KIND, half_step
-from test_gpu_attention import both, check, close, made, reference
+from heads_ref import F32, KIND, half_step, view
+from test_gpu_attention import both, check, close, made, reference, starts_of
 
 pytestmark = pytest.mark.gpu
 
@@ -194,3 +195,63 @@ def test_scores_that_are_no_numbers(kind, n):
     for name in ("gk", "gv"):
         assert got[name][70:70 + n // 2 + 1].isnan().all()
         assert got[name][:70].isfinite().all()
+
+
+def with_odd_values(v, share, seed):
+    """v with NaNs and infinities, in whole keys of the first heads and here and there"""
+    g = torch.Generator().manual_seed(seed)
+    v = v.clone()
+    what = torch.tensor([math.nan, math.inf, -math.inf]).to(v.dtype)[torch.randint(0, 3, v.shape, generator=g)]
+    where = torch.rand(v.shape, generator=g) < share
+    where[:, 0] &= torch.rand(len(v), 1, generator=g) < 0.3
+    return torch.where(where, what, v)
+
+
+@pytest.mark.parametrize("kind", list(KIND))
+@pytest.mark.parametrize("share", [0.0005, 0.05, 1.0])
+@pytest.mark.parametrize("shape", [([130, 40], None, 4, 2, 64, True, 0), ([700], None, 2, 2, 128, True, 200), ([90], [300], 4, 2, 80, False, 0), ([1, 3, 1], [70, 300, 1500], 8, 2, 128, True, 33),
+                                   ([2], [3000], 4, 1, 100, True, 0), ([150], None, 2, 1, 192, True, 0), ([77], None, 3, 3, 256, True, 30), ([200], [2500], 2, 1, 64, True, 0)], ids=str)
+def test_values_that_are_no_numbers(shape, share, kind):
+    """Results have what the values that a query sees have, channel by channel: a NaN or infinities of both signs make a NaN, an infinity itself, and without them they are those of numbers alone"""
+    q, k, v, w = made(shape, kind, 38)
+    v = with_odd_values(v, share, 39)
+    got = both(shape, kind, (q, k, v, w), grad=False)
+    number = v.float().isfinite()
+    finite = reference(shape, kind, (q, k, torch.where(number, v, torch.zeros_like(v)), w), grad=False)
+    nq, nk, heads, kv, d, causal, window = shape
+    want, bound = (x.clone() for x in finite["out"])
+    at_q = at_k = 0
+    for n, m in zip(nq, nq if nk is None else nk):
+        see = seen(n, m, causal, window).float()
+        for h in range(heads):
+            x = v[at_k:at_k + m, h * kv // heads].float()
+            nan, up, down = (see @ y.float() > 0 for y in (x.isnan(), x == math.inf, x == -math.inf))
+            rows = want[at_q:at_q + n, h]
+            rows[up], rows[down], rows[nan | up & down] = math.inf, -math.inf, math.nan
+        at_q, at_k = at_q + n, at_k + m
+    out = got["out"].double().cpu()
+    assert torch.equal(out.isnan(), want.isnan())
+    close("out", torch.where(want.isnan(), 0.0, out), (torch.where(want.isnan(), 0.0, want), bound), kind)
+    close("log_sum", got["log_sum"], finite["log_sum"], None)
+
+
+@pytest.mark.parametrize("kind", list(KIND))
+def test_values_that_are_all_nan_take_no_longer(kind):
+    """As after a step that went astray: not key by key (1200 times as long), but within a few times of numbers"""
+    shape = ([2000], None, 4, 1, 128, True, 0)
+    q, k, v, _ = (t.cuda() for t in made(shape, kind, 40))
+    out, s = torch.zeros_like(q), starts_of([2000]).cuda()
+    times = []
+    for values in (v, torch.full_like(v, math.nan)):
+        best = math.inf
+        for _ in range(5):
+            begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            begin.record()
+            for _ in range(4):
+                ocn.attention(view(q), view(k), view(values), view(out), 0.1, view(s), view(s))
+            end.record()
+            torch.cuda.synchronize()
+            best = min(best, begin.elapsed_time(end))
+        times.append(best)
+    assert out.isnan().all()
+    assert times[1] <= 10 * times[0], times
