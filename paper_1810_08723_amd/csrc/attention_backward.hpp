@@ -7,7 +7,7 @@
 // Two passes: one in which a workgroup has keys and goes over the rows (of all query heads that read them, so that their sums need no other workgroup), and one in which it has rows and goes over
 // keys.  Scores and weights are made in both, seven products where five would do: the five of one pass leave the gradient of q in pieces of
 // every block of keys, which would have to be added up in memory, in an order that changes from run to run or with more traffic than two products cost.
-// Products bound both, at half of the matrix cores' cycles and the clock that power allows: 4 sequences of 4096 tokens, 32 heads, 8 of keys, 128 channels in bfloat16 1.87 ms, 1.08 of them over keys
+// Products bound both, at half of the matrix cores' cycles and the clock that power allows: 4 sequences of 4096 tokens, 32 heads, 8 of keys, 128 channels in bfloat16 1.88 ms, 1.09 of them over keys
 // (with all seven products 1.03 PFLOP/s).
 #pragma once
 

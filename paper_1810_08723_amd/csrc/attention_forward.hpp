@@ -301,7 +301,7 @@ __device__ __forceinline__ Split split_of(const AttentionArgs &a, const Limits &
 
 // Many rows: the wavefronts of a workgroup have a tile of rows each and share the keys, which go through LDS once for all of them, the next ones on their way.
 // Products bound it, and exponentials, which take about as many cycles (of 128 channels; of 64 more), at the clock that power allows: 16 prompts of 101 to 6000 tokens, 32 heads, 8 of
-// keys, 128 channels in bfloat16 1728 us (955 TFLOP/s; a large product 1263), one of 30011 tokens, 16 heads, 4 of keys, 64 channels in half precision 2043 (903).  Two wavefronts to a SIMD, whose results
+// keys, 128 channels in bfloat16 1690 to 1774 us on different cards (970 to 930 TFLOP/s; a large product 1263), one of 30011 tokens, 16 heads, 4 of keys, 64 channels in half precision 2040 to 2161 (905 to 855).  Two wavefronts to a SIMD, whose results
 // and queries fill their registers, take each other's waits (3873 us of those prompts with one, and rows through registers).
 template <class T, int D, bool VEC, int WAVES, int KEYS> __global__ __launch_bounds__(WAVES *kWave) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 && (D <= 128 || VEC && D <= 192) ? 2 : 1))) void attention_rows_kernel(const AttentionArgs a, uint32_t first_block) {
   warm_arguments<AttentionArgs>();

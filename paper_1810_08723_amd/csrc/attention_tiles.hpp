@@ -49,7 +49,8 @@ __device__ __forceinline__ f32x4 product(f32x4 a, f32x4 b, f32x4 c) {
 // index of element i of a result (of which 4 h is the lane's own part)
 template <class T> __device__ __forceinline__ constexpr int own_index(int i) { return 8 * (i / 4) + i % 4; }
 
-// elements 16 s ... of a result as a fragment, rounded to the type
+// Elements 16 s ... of a result as a fragment, rounded to the type: weights, and differences times weights in the gradient, are off by half a step at most.  The matrix units take operands of one type, and two
+// parts of each, which would hold twice the bits, would be twice the products that take them; results are rounded as much again.  Scores, sums and the weights' exponents stay in single precision.
 template <class T> __device__ __forceinline__ frag_t<T> as_fragment(const acc_t<T> &a, int s) {
   frag_t<T> f;
   constexpr int N = Tile<T>::kFrag;

@@ -8,8 +8,8 @@
 //
 // A row is read once and stays in registers: its mean, then the deviations from it, whose squares are summed (two passes over registers: sums of
 // x and x^2 lose the variance of rows far from zero).  A mean that is off by its own rounding is as far from a constant row as that row's deviations would be, and 1 / sqrt(eps) makes
-// results of the difference: means are of exact sums where values are alike, and divided exactly.  Memory bounds both directions, or, for a few rows, the launch: 24705 rows of 1280 halves (127 MB) in 27.3 us,
-// 48 rows of 4096 in 4.7; the gradient of 16384 rows of 4096 bfloat16 (403 MB) in 82.4 us, of which a large copy would take 80.
+// results of the difference: means are of exact sums where values are alike, and divided exactly.  Memory bounds both directions, or, for a few rows, the launch: 24705 rows of 1280 halves (127 MB) in 27.4 us,
+// 48 rows of 4096 in 4.8; the gradient of 16384 rows of 4096 bfloat16 (403 MB) in 82.8 us, of which a large copy would take 80.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
