@@ -438,7 +438,7 @@ int ocn_cache_attention(const ocn_tensor *q, const ocn_tensor *cache, const ocn_
  * last `window` of those where window is not 0 (without OCN_CAUSAL it has to be 0).  A query that sees nothing gets zeros.  What a query does not see, infinities
  * and NaNs among it, does not reach its results.  log_sum (or NULL): OCN_FLOAT [tokens, heads] ([batch, queries, heads]), the natural logarithm of
  * sum_j exp(scale * q_i . k_j), -inf where nothing is seen.  Scores, sums and the softmax are held in single precision (a scale past its range is
- * OCN_ERR_DOMAIN); for half and bfloat16 a weight (relative to the largest of its row, so far) is rounded to that type for the product with v, half a step
+ * OCN_ERR_DOMAIN, one that it has as zero is zero); for half and bfloat16 a weight (relative to the largest of its row, so far) is rounded to that type for the product with v, half a step
  * at most (in half, weights below 2^-23 of the row's largest are off by up to 2^-34 of that).  workspace: DEVICE scratch of ocn_attention_workspace_bytes(...)
  * bytes (a function of the shapes alone; 0 where none is needed), 256-byte aligned; calls that may run at the same time need one each.  The same bits every time. */
 #define OCN_CAUSAL 4u
@@ -464,6 +464,7 @@ int ocn_attention_grad(const ocn_tensor *gout, const ocn_tensor *q, const ocn_te
 /*
  * The layer norm over the last dimension, of at most OCN_MAX_WIDTH channels, of tensors of any strides with up to six dimensions before it (fewer than 2^31 rows):
  *     out = (x - mean(x)) / sqrt(mean((x - mean(x))^2) + eps) * weight + bias.
+ * Rows of one value alone have a mean of that value, so that the bias is left, however large it is.
  * x and out share one of the types of heads; weight and bias: [channels], half, bfloat16 or float each, or NULL for ones and zeros.  Arithmetic, sharing of bytes
  * and errors are as for the operators over heads; out may be the identical view of x. */
 #define OCN_MAX_WIDTH 16384

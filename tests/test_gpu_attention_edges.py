@@ -131,6 +131,36 @@ def test_a_single_key(kind, d):
 
 
 @pytest.mark.parametrize("kind", list(KIND))
+def test_far_scores_of_sequences_as_a_dimension(kind):
+    """[batch, tokens, heads, channels], heads first in memory: a single key again; and the same bits in several launches, on another stream and from a workspace of anything"""
+    from paper_1810_08723_amd import binding
+    batch, n, heads, d = 3, 150, 4, 128
+    q, k, v, w = (t.cuda().view(batch, n, heads, d).transpose(1, 2).contiguous().transpose(1, 2) for t in made(([batch * n], None, heads, heads, d, True, 0), kind, 41))
+
+    def run(window, scale, stream=None):
+        r = {"out": torch.zeros_like(q), "log_sum": torch.zeros(batch, n, heads, device="cuda"), "gq": torch.zeros_like(q), "gk": torch.zeros_like(k), "gv": torch.zeros_like(v)}
+        vr = {name: view(t) for name, t in r.items()}
+        space = torch.full((ocn.attention_grad_workspace_bytes(view(q), view(k)),), 255, dtype=torch.uint8, device="cuda")
+        torch.cuda.synchronize()
+        ocn.attention(view(q), view(k), view(v), vr["out"], scale, window=window, log_sum=vr["log_sum"], stream=stream)
+        ocn.attention_grad(view(w), view(q), view(k), view(v), vr["out"], vr["log_sum"], vr["gq"], vr["gk"], vr["gv"], scale, window=window, workspace=space, stream=stream)
+        torch.cuda.synchronize()
+        return r
+
+    got = run(1, 1e9)
+    assert torch.equal(got["out"], v) and torch.equal(got["gv"], w)
+    first = run(0, 1e9)
+    assert all(t.isfinite().all() for name, t in first.items() if kind != "half" or name in ("out", "log_sum", "gv"))
+    binding.set_max_launch_blocks(3)
+    try:
+        again = run(0, 1e9)
+    finally:
+        binding.set_max_launch_blocks(0)
+    other = run(0, 1e9, torch.cuda.Stream().cuda_stream)
+    assert all(torch.equal(first[name].nan_to_num(), x[name].nan_to_num()) for name in first for x in (again, other))
+
+
+@pytest.mark.parametrize("kind", list(KIND))
 def test_one_row_of_far_scores(kind):
     for shape in (([90], None, 2, 1, 64, True, 0), ([700], None, 4, 2, 128, True, 0)):
         q, k, v, w = made(shape, kind, 35)
